@@ -146,6 +146,8 @@ def prepare(case, seed):
         import paper_1708_04801_b200 as P
 
         s["ctx"] = P.Context(case.get("models", 1), case.get("d", 1))
+        if op == "clip":
+            s["list"] = P.GradList(s["grads"], s["outs"])
     return s
 
 
@@ -198,7 +200,7 @@ def _gradient(s):
 
 def _clip(s):
     if own:
-        norm = s["ctx"].clip_grad_norm(s["grads"], s["max_norm"], out=s["outs"])
+        norm = s["ctx"].clip_grad_norm(s["list"], s["max_norm"])
         return {"norm": norm, "grads": s["flat_out"]}
     norm = s["flat"].float().square().sum(dtype=torch.float64).sqrt()  # in 64 bits: a long sum
     factor = torch.where(norm > s["max_norm"], s["max_norm"] / norm, torch.ones_like(norm)).float()
