@@ -223,6 +223,61 @@ wpsgd_status wpsgd_objective_csr(wpsgd_ctx* ctx, const int64_t* row_ptr, const i
                                  const float* y, int64_t n_rows, const float* w, float lambda, wpsgd_loss loss,
                                  double* out);
 
+/* ---- Operators on whole sets of rows ---------------------------------------------------------------------------------------
+ * They use the context's d, stream and device, and not its models. Those that need a workspace (objective_grad*, grad_norm,
+ * clip_grad_norm) allocate it at the context's first such call, which therefore has to come before a stream capture
+ * (WPSGD_ERR_STATE within one), and keep it at its place: later calls allocate nothing and can be captured. Calls of one context
+ * share the workspace, so graphs captured from one context must not run at the same time as each other or as other calls of it.
+ * Results do not depend on timing. */
+
+/* Rows packed to 8 bits. For each block of 128 columns of each row (the last may be shorter), with a = the largest |x| of the
+ * block but at least 2^-100:  scale = a / 448,  q = e4m3(x (448 / a)), rounded to nearest even;  x is about q scale.
+ *   X          DEVICE [n_rows, ld_elems], the first d columns of a row are read.
+ *   Q          DEVICE [n_rows, ld_q] e4m3, 16-byte aligned, ld_q >= d a multiple of 16; bytes from column d on stay as they are.
+ *   scales     DEVICE [n_rows, ld_s], ld_s >= ceil(d / 128).
+ * A NaN stays one. An infinity makes the scale of its block infinite, and every margin of its row NaN. */
+wpsgd_status wpsgd_quantize_rows(wpsgd_ctx* ctx, const void* X, wpsgd_xtype xt, int64_t ld_elems, int64_t n_rows, uint8_t* Q,
+                                 int64_t ld_q, float* scales, int64_t ld_s);
+
+/* Margins of n_models models on n_rows rows, both packed as above: Z[i, m] = sum_c x_i,c w_m,c with x = q scale, w = p scale.
+ * The products of a block of 128 columns are summed without their scales, the blocks' sums times both scales in fp32.
+ *   Q, q_scales, M, m_scales   DEVICE, as wpsgd_quantize_rows makes them.
+ *   Z          DEVICE [n_rows, ld_z >= n_models], fp32 or bf16 per `zt`; columns from n_models on stay as they are. */
+wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* ctx, const uint8_t* Q, int64_t ld_q, const float* q_scales, int64_t ld_qs,
+                               int64_t n_rows, const uint8_t* M, int64_t ld_m, const float* m_scales, int64_t ld_ms,
+                               int64_t n_models, void* Z, wpsgd_xtype zt, int64_t ld_z);
+
+/* Objective of Eq. 3-4 with its gradient over all rows, in one pass over them:
+ *   out = { (lambda/2)|w|^2 + mean_i L(y_i, w.x_i), share of rows with sign(w.x) != sign(y) },
+ *   grad = lambda w + mean_i L'(y_i, w.x_i) x_i.
+ * Arguments as wpsgd_objective, but out DEVICE [2] and grad DEVICE [d] are fp32; w, grad and out must not overlap. Margins that
+ * rounding could move across a jump (y z = 1 of the hinge loss, z = 0 of the error) are formed in fp64. Without rows: the regulariser alone. */
+wpsgd_status wpsgd_objective_grad(wpsgd_ctx* ctx, const void* X, wpsgd_xtype xt, int64_t ld_elems, const float* y, int64_t n_rows,
+                                  const float* w, float lambda, wpsgd_loss loss, float* grad, float* out);
+
+/* The same on packed rows (Q, scales as wpsgd_quantize_rows makes them; w, grad and out as above). The 16-byte unit that holds a
+ * row's last byte is read whole. */
+wpsgd_status wpsgd_objective_grad_fp8(wpsgd_ctx* ctx, const uint8_t* Q, int64_t ld_q, const float* scales, int64_t ld_s,
+                                      const float* y, int64_t n_rows, const float* w, float lambda, wpsgd_loss loss, float* grad,
+                                      float* out);
+
+/* A list of gradients for the two functions below, made once for tensors that stay where they are.
+ *   grads      HOST [n_tensors] of DEVICE pointers, n_elems HOST [n_tensors], types HOST [n_tensors] (fp32 or bf16, each its own).
+ *   out        HOST [n_tensors] of DEVICE pointers: where the clipped gradients go, of the same types and sizes; NULL: in place.
+ * Tensors may have any size, also 0, and any alignment of their elements. An output must be its own input or lie apart from every
+ * other tensor of the list (WPSGD_ERR_INVALID_ARG). Needs no GPU; wpsgd_last_error(NULL) has the text of a failure. */
+typedef struct wpsgd_grad_list wpsgd_grad_list;
+wpsgd_status wpsgd_grad_list_create(const void* const* grads, void* const* out, const int64_t* n_elems, const wpsgd_xtype* types,
+                                    int32_t n_tensors, wpsgd_grad_list** list);
+wpsgd_status wpsgd_grad_list_destroy(wpsgd_grad_list* list); /* NULL is accepted; enqueued work is not affected */
+
+/* N = sqrt(sum of the squares of all elements of all tensors), to norm_out DEVICE [1]. */
+wpsgd_status wpsgd_grad_norm(wpsgd_ctx* ctx, const wpsgd_grad_list* list, float* norm_out);
+
+/* The same, and clipping: out = g (max_norm / N) where N > max_norm, else out = g. max_norm >= 0, infinity allowed. An infinite
+ * N scales by 0; an N that is not a number leaves the values as they are. norm_out gets the norm before clipping. */
+wpsgd_status wpsgd_clip_grad_norm(wpsgd_ctx* ctx, const wpsgd_grad_list* list, double max_norm, float* norm_out);
+
 /* Whole path from HOST buffers: copies X HOST [N, d] (dense, contiguous), y HOST [N] and w0 HOST [d]
  * (or NULL) to the device, runs the chains and the combination, copies v back to v_out HOST [d], and
  * waits for completion. Page-locked host buffers give full copy speed. Device staging buffers are

@@ -18,7 +18,8 @@ EXPORTED_SYMBOLS = [
     "wpsgd_combine", "wpsgd_combine_weighted", "wpsgd_last_chain_ms", "wpsgd_get_models", "wpsgd_set_models", "wpsgd_get_weights", "wpsgd_weights",
     "wpsgd_sample_indices", "wpsgd_objective", "wpsgd_objective_csr", "wpsgd_solve_host", "wpsgd_solve_static", "wpsgd_check", "wpsgd_launch_count",
     "wpsgd_last_error", "wpsgd_continue_csr", "wpsgd_validate_csr", "wpsgd_span_valid", "wpsgd_sample_indices_host",
-    "wpsgd_check_static", "wpsgd_solve_host_csr",
+    "wpsgd_check_static", "wpsgd_solve_host_csr", "wpsgd_quantize_rows", "wpsgd_margins_fp8", "wpsgd_objective_grad",
+    "wpsgd_objective_grad_fp8", "wpsgd_grad_list_create", "wpsgd_grad_list_destroy", "wpsgd_grad_norm", "wpsgd_clip_grad_norm",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -75,6 +76,14 @@ def load_library() -> ctypes.CDLL:
     lib.wpsgd_sample_indices_host.argtypes = [u64, i32, i64, i64, i64, i32, vp]
     lib.wpsgd_check_static.argtypes = [ci, vp]
     lib.wpsgd_solve_host_csr.argtypes = [vp, vp, vp, vp, vp, vp, vp, f32, ci, f32, ci, u64, vp, f64, vp]
+    lib.wpsgd_quantize_rows.argtypes = [vp, vp, ci, i64, i64, vp, i64, vp, i64]
+    lib.wpsgd_margins_fp8.argtypes = [vp, vp, i64, vp, i64, i64, vp, i64, vp, i64, i64, vp, ci, i64]
+    lib.wpsgd_objective_grad.argtypes = [vp, vp, ci, i64, vp, i64, vp, f32, ci, vp, vp]
+    lib.wpsgd_objective_grad_fp8.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, f32, ci, vp, vp]
+    lib.wpsgd_grad_list_create.argtypes = [vp, vp, vp, vp, i32, ctypes.POINTER(vp)]
+    lib.wpsgd_grad_list_destroy.argtypes = [vp]
+    lib.wpsgd_grad_norm.argtypes = [vp, vp, vp]
+    lib.wpsgd_clip_grad_norm.argtypes = [vp, vp, f64, vp]
     lib.wpsgd_launch_count.argtypes = [vp]
     lib.wpsgd_launch_count.restype = i64
     lib.wpsgd_last_error.argtypes = [vp]
@@ -176,6 +185,50 @@ def solve_static(X, y, shard_off, n_steps, eta0, sched, lam, loss, seed, w0=None
     if st:
         raise WpsgdError(st, "wpsgd_solve_static", lib.wpsgd_last_error(None).decode())
     return out
+
+
+def packed_width(d: int) -> int:
+    """Bytes from one packed row of d columns to the next: rows start on 16 bytes."""
+    return (d + 15) // 16 * 16
+
+
+class GradList:
+    """A wpsgd_grad_list: gradients (contiguous CUDA tensors, float32 or bfloat16) whose norm is taken and which are clipped
+    together, in place or into `out`. Made once for tensors that stay where they are; keeps them alive."""
+
+    def __init__(self, grads, out=None):
+        import torch
+
+        self._h = None
+        self._lib = load_library()
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        if len(self.out) != len(self.grads):
+            raise ValueError("out must have a tensor for each gradient")
+        n = len(self.grads)
+        self.device = self.grads[0].device.index if n else None
+        for g, o in zip(self.grads, self.out):
+            for t in (g, o):
+                if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != self.device:
+                    raise TypeError("expected CUDA tensors on one device")
+                if not t.is_contiguous():
+                    raise TypeError("expected contiguous tensors")
+            if g.dtype not in (torch.float32, torch.bfloat16) or o.dtype != g.dtype or o.numel() != g.numel():
+                raise TypeError("gradients must be float32 or bfloat16, outputs of the same types and sizes")
+        ptrs = np.array([t.data_ptr() for t in self.grads], dtype=np.uint64)
+        outs = np.array([t.data_ptr() for t in self.out], dtype=np.uint64)
+        sizes = np.array([t.numel() for t in self.grads], dtype=np.int64)
+        types = np.array([_xtype(t) for t in self.grads], dtype=np.int32)
+        h = ctypes.c_void_p()
+        st = self._lib.wpsgd_grad_list_create(ptrs.ctypes.data, outs.ctypes.data, sizes.ctypes.data, types.ctypes.data, n, ctypes.byref(h))
+        if st:
+            raise WpsgdError(st, "wpsgd_grad_list_create", self._lib.wpsgd_last_error(None).decode())
+        self._h = h
+
+    def __del__(self):
+        if getattr(self, "_h", None):
+            self._lib.wpsgd_grad_list_destroy(self._h)
+            self._h = None
 
 
 class Context:
@@ -384,6 +437,126 @@ class Context:
                                                self._dev(y, torch.float32), n_rows, self._dev(w, torch.float32, self.d),
                                                lam, loss, self._dev(out)), "wpsgd_objective_csr")
         return out
+
+    # -- operators on whole sets of rows ------------------------------------------------------------------
+    def _empty(self, shape, dtype):
+        """A tensor for the context's stream to write: allocated for that stream, so that its memory is not reused under it."""
+        import torch
+
+        dev = torch.device("cuda", self.device)
+        if torch.cuda.current_stream(dev) == self._stream:
+            return torch.empty(shape, dtype=dtype, device=dev)
+        with torch.cuda.stream(self._stream):
+            return torch.empty(shape, dtype=dtype, device=dev)
+
+    def _matrix(self, t, dtypes, cols, what):
+        """Pointer, row stride and row count of a 2-D tensor with `cols` columns and contiguous rows on the context's device."""
+        import torch
+
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != self.device:
+            raise TypeError(f"{what}: expected a CUDA tensor on the context's device")
+        if t.dtype not in dtypes:
+            raise TypeError(f"{what}: expected dtype {' or '.join(map(str, dtypes))}, got {t.dtype}")
+        if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+            raise ValueError(f"{what}: expected rows of {cols} contiguous elements, got shape {tuple(t.shape)} with strides {t.stride()}")
+        n = t.shape[0]
+        return ctypes.c_void_p(t.data_ptr()), t.stride(0) if n > 1 else None, n
+
+    def _packed(self, q, scales, what):
+        """Arguments of packed rows: pointer, stride, scales, their stride, row count."""
+        import torch
+
+        qp, ld, n = self._matrix(q, (torch.float8_e4m3fn, torch.uint8), self.d, what)
+        nb = (self.d + 127) // 128
+        sp, ld_s, m = self._matrix(scales, (torch.float32,), nb, what + " scales")
+        if m != n:
+            raise ValueError(f"{what}: {n} rows, but scales of {m}")
+        return qp, packed_width(self.d) if ld is None else ld, sp, nb if ld_s is None else ld_s, n
+
+    def quantize_rows(self, X, out=None, scales=None):
+        """Rows packed to 8 bits: (e4m3 [n, d] with rows that start on 16 bytes, fp32 scales [n, ceil(d / 128)])."""
+        import torch
+
+        xp, ld, n = self._matrix(X, (torch.float32, torch.bfloat16), self.d, "X")
+        if out is None:
+            out = self._empty((n, packed_width(self.d)), torch.float8_e4m3fn)[:, :self.d]
+        if scales is None:
+            scales = self._empty((n, (self.d + 127) // 128), torch.float32)
+        qp, ld_q, sp, ld_s, m = self._packed(out, scales, "out")
+        if m != n:
+            raise ValueError(f"out has {m} rows, X {n}")
+        self._ck(self._lib.wpsgd_quantize_rows(self._h, xp, _xtype(X), self.d if ld is None else ld, n, qp, ld_q, sp, ld_s), "wpsgd_quantize_rows")
+        return out, scales
+
+    def margins_fp8(self, Q, q_scales, M, m_scales, out=None, dtype=None):
+        """Margins [n, models] of packed models M on packed rows Q, float32 (or `dtype`: bfloat16)."""
+        import torch
+
+        qp, ld_q, qs, ld_qs, n = self._packed(Q, q_scales, "Q")
+        mp, ld_m, ms, ld_ms, k = self._packed(M, m_scales, "M")
+        if out is None:
+            out = self._empty((n, k), dtype or torch.float32)
+        elif dtype is not None and out.dtype != dtype:
+            raise TypeError(f"out has dtype {out.dtype}, asked for {dtype}")
+        zp, ld_z, rows = self._matrix(out, (torch.float32, torch.bfloat16), k, "out")
+        if rows != n:
+            raise ValueError(f"out has {rows} rows, Q {n}")
+        self._ck(self._lib.wpsgd_margins_fp8(self._h, qp, ld_q, qs, ld_qs, n, mp, ld_m, ms, ld_ms, k, zp, _xtype(out), k if ld_z is None else ld_z),
+                 "wpsgd_margins_fp8")
+        return out
+
+    def _grad_outputs(self, grad, out):
+        import torch
+
+        grad = self._empty((self.d,), torch.float32) if grad is None else grad
+        out = self._empty((2,), torch.float32) if out is None else out
+        return grad, self._dev(grad, torch.float32, self.d), out, self._dev(out, torch.float32, 2)
+
+    def objective_grad(self, X, y, w, lam: float, loss: int, grad=None, out=None):
+        """(fp32 [2] = {objective, error}, fp32 [d] = its gradient) over all rows of X."""
+        import torch
+
+        xp, ld, n = self._matrix(X, (torch.float32, torch.bfloat16), self.d, "X")
+        grad, gp, out, op = self._grad_outputs(grad, out)
+        self._ck(self._lib.wpsgd_objective_grad(self._h, xp, _xtype(X), self.d if ld is None else ld, self._dev(y, torch.float32, n), n,
+                                                self._dev(w, torch.float32, self.d), lam, loss, gp, op), "wpsgd_objective_grad")
+        return out, grad
+
+    def objective_grad_fp8(self, Q, scales, y, w, lam: float, loss: int, grad=None, out=None):
+        """objective_grad over packed rows."""
+        import torch
+
+        qp, ld_q, sp, ld_s, n = self._packed(Q, scales, "Q")
+        grad, gp, out, op = self._grad_outputs(grad, out)
+        self._ck(self._lib.wpsgd_objective_grad_fp8(self._h, qp, ld_q, sp, ld_s, self._dev(y, torch.float32, n), n, self._dev(w, torch.float32, self.d),
+                                                    lam, loss, gp, op), "wpsgd_objective_grad_fp8")
+        return out, grad
+
+    def _grad_list(self, grads):
+        if not isinstance(grads, GradList):
+            grads = GradList(grads)
+        if grads.device is not None and grads.device != self.device:
+            raise TypeError("expected tensors on the context's device")
+        return grads
+
+    def grad_norm(self, grads, norm=None):
+        """fp32 [1]: the global norm of the gradients (a GradList or a sequence of tensors)."""
+        import torch
+
+        grads = self._grad_list(grads)
+        norm = self._empty((1,), torch.float32) if norm is None else norm
+        self._ck(self._lib.wpsgd_grad_norm(self._h, grads._h, self._dev(norm, torch.float32, 1)), "wpsgd_grad_norm")
+        return norm
+
+    def clip_grad_norm(self, grads, max_norm: float, norm=None):
+        """Scales the gradients down to max_norm where their global norm is above it, in place or into the list's outputs;
+        returns the norm before, fp32 [1]."""
+        import torch
+
+        grads = self._grad_list(grads)
+        norm = self._empty((1,), torch.float32) if norm is None else norm
+        self._ck(self._lib.wpsgd_clip_grad_norm(self._h, grads._h, max_norm, self._dev(norm, torch.float32, 1)), "wpsgd_clip_grad_norm")
+        return norm
 
     def solve_host(self, X, y, shard_off, n_steps, eta0, sched, lam, loss, seed, w0=None, r: float = 0.0, out=None):
         """Host tensors in (ideally pinned), host tensor out; copies are part of the call."""

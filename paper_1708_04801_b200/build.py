@@ -9,7 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwpsgd.so")
-SOURCES = ["wpsgd_api.cu"]
+OBJ = os.path.join(HERE, "_build")
+SOURCES = ["wpsgd_api.cu", "wpsgd_rows.cu"]
 
 
 def _nvcc() -> str:
@@ -28,17 +29,44 @@ def _newest_source_mtime() -> float:
     return m
 
 
+def _fresh(obj: str) -> bool:
+    """Whether an object file is newer than every file that its last compilation read (nvcc wrote the list beside it)."""
+    try:
+        text = open(obj + ".d").read()
+        made = os.path.getmtime(obj)
+        read = text.split(":", 1)[1].replace("\\\n", " ").split()
+        return all(os.path.getmtime(f) <= made for f in read)
+    except (OSError, IndexError):
+        return False
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source_mtime():
         return LIB
-    tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-DWPSGD_BUILD",  # no fast-math: expf and division must round as written
-           "-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
+    os.makedirs(OBJ, exist_ok=True)
+    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",
+             "-DWPSGD_BUILD"]  # no fast-math: expf and division must round as written
     if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    subprocess.check_call(cmd)
+        flags = ["-Xptxas", "-v"] + flags
+    objs, jobs = [], []
+    for s in SOURCES:
+        obj = os.path.join(OBJ, s + ".o")
+        objs.append(obj)
+        if force or not _fresh(obj):
+            tmp = obj + f".tmp{os.getpid()}"
+            cmd = [_nvcc()] + flags + ["-MD", "-MF", tmp + ".d", "-c", "-o", tmp, os.path.join(CSRC, s)]
+            jobs.append((obj, tmp, cmd, subprocess.Popen(cmd)))
+    failed = None
+    for obj, tmp, cmd, job in jobs:
+        if job.wait() != 0:
+            failed = failed or subprocess.CalledProcessError(job.returncode, cmd)
+        else:
+            os.replace(tmp + ".d", obj + ".d")
+            os.replace(tmp, obj)
+    if failed:
+        raise failed
+    tmp = LIB + f".tmp{os.getpid()}"
+    subprocess.check_call([_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", tmp] + objs)
     os.replace(tmp, LIB)
     return LIB
 

@@ -92,20 +92,6 @@ __global__ void broadcast_model_kernel(float* __restrict__ W, double* __restrict
 }
 
 // ---- objective of Eq. 3-4 and 0/1 error ----------------------------------------------------------------------------------
-__device__ __forceinline__ double loss_value(int loss, float yy, float z) {
-  if (loss == LOSS_HINGE) return fmax(0.0, 1.0 - (double)yy * (double)z);
-  if (loss == LOSS_LOGISTIC) {
-    const double t = (double)yy * (double)z;
-    return t > 0 ? log1p(exp(-t)) : -t + log1p(exp(t));
-  }
-  return 0.5 * ((double)z - (double)yy) * ((double)z - (double)yy);
-}
-__device__ __forceinline__ double warp_sum_f64(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
 // The end of both objective kernels: sums of the block (loss, error count, its share of |w|^2) go to part[3 blockIdx.x ..];
 // the block that finishes last adds all of them up in block order and writes out (so the result does not depend on which
 // block that is) and resets the ticket for the next launch.

@@ -44,12 +44,28 @@ __device__ __forceinline__ float loss_derivative(int loss, float y, float z) {
   return z - y;
 }
 
+// The losses themselves, in fp64 for the evaluation measures.
+__device__ __forceinline__ double loss_value(int loss, float yy, double z) {
+  if (loss == LOSS_HINGE) return fmax(0.0, 1.0 - (double)yy * z);
+  if (loss == LOSS_LOGISTIC) {
+    const double t = (double)yy * z;
+    return t > 0 ? log1p(exp(-t)) : -t + log1p(exp(t));
+  }
+  return 0.5 * (z - (double)yy) * (z - (double)yy);
+}
+
 // eta_n for the 1-based step number n.
 __device__ __forceinline__ float step_size(float eta0, int sched, long long n) {
   return sched == LR_INV_SQRT ? eta0 / sqrtf((float)n) : eta0;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+__device__ __forceinline__ double warp_sum_f64(double v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;

@@ -1,0 +1,329 @@
+// C ABI of the operators on whole sets of rows (see include/wpsgd.h): 8-bit rows, margins of many models, the objective with its
+// gradient, norm and clipping of gradients. Argument checks, workspaces, choice of kernels, launches.
+#include <cmath>
+#include <memory>
+#include <new>
+#include <type_traits>
+
+#include "clip.cuh"
+#include "context.cuh"
+#include "gradient.cuh"
+#include "margins.cuh"
+#include "quantize.cuh"
+
+using namespace wpsgd;
+
+namespace {
+
+// ---- workspace -----------------------------------------------------------------------------------------------------------
+// One buffer per context, allocated by the first call that needs it and never moved (a captured graph keeps its address). Its size
+// depends on d alone. Calls of one context follow each other on its stream, so they can share it.
+constexpr int kMaxBlocks = 148 * 8;             // of any kernel that leaves sums here
+constexpr int kGradParts = 148 * 2;             // partial gradients at most
+constexpr long long kCoefRows = 1 << 16;        // rows per step of the two-pass gradient
+struct RowsLayout {
+  int parts;
+  size_t sums, coef, part, total;
+  explicit RowsLayout(long long d) {
+    parts = (int)std::max(1ll, std::min<long long>(kGradParts, (1ll << 23) / d));
+    sums = 0;
+    coef = sums + kMaxBlocks * 2 * sizeof(double);
+    part = coef + kCoefRows * sizeof(float);
+    total = part + (size_t)parts * (size_t)d * sizeof(float);
+  }
+};
+wpsgd_status rows_workspace(wpsgd_ctx* c) {
+  if (c->rows_ws) return WPSGD_OK;
+  cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+  CU_TRY(c, cudaStreamIsCapturing(c->stream, &capturing));
+  if (capturing != cudaStreamCaptureStatusNone)
+    return fail(c, WPSGD_ERR_STATE, "the first call of a gradient, norm or clipping operator on a context allocates its workspace: make one before the capture");
+  CU_TRY(c, cudaMalloc(&c->rows_ws, RowsLayout(c->d).total));
+  return WPSGD_OK;
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+size_t element_size(wpsgd_xtype t) { return t == WPSGD_X_F32 ? 4 : 2; }
+bool known(wpsgd_xtype t) { return t == WPSGD_X_F32 || t == WPSGD_X_BF16; }
+long long blocks_of(long long d) { return (d + Q_BLOCK - 1) / Q_BLOCK; }
+
+// 8-bit rows as every entry point takes them
+const char* check_rows8(const uint8_t* Q, int64_t ld_q, const float* scales, int64_t ld_s, int64_t n, long long d) {
+  if (n < 0) return "negative row count";
+  if (n > 0 && (!Q || !scales)) return "8-bit rows or scales are NULL";
+  if (ld_q < d || ld_q % 16) return "8-bit rows need a stride of at least d and a multiple of 16 bytes";
+  if (n > 0 && !aligned16(Q)) return "8-bit rows must start on 16 bytes";
+  if (ld_s < blocks_of(d)) return "scales need a stride of at least ceil(d / 128)";
+  return nullptr;
+}
+
+// ---- gradient ------------------------------------------------------------------------------------------------------------
+template <typename RT>
+wpsgd_status gradient_any_width(wpsgd_ctx* c, GradParams p, int* parts, int* n_sums) {
+  const RowsLayout lay(c->d);
+  float* coef = (float*)((char*)c->rows_ws + lay.coef);
+  const int slabs = (int)((p.d + GRAD_THREADS - 1) / GRAD_THREADS);
+  const long long first = std::min(p.n_rows, kCoefRows);
+  *parts = (int)std::max(1ll, std::min<long long>({(long long)lay.parts, (long long)(kMaxBlocks / slabs), (first + 31) / 32}));
+  *n_sums = grid_for(first, GRAD_THREADS / 32, kMaxBlocks);
+  for (long long row0 = 0; row0 < p.n_rows; row0 += kCoefRows) {
+    const long long count = std::min(p.n_rows - row0, kCoefRows);
+    launch(gradient_margins_kernel<RT>, *n_sums, GRAD_THREADS, 0, c->stream, p, row0, count, row0 == 0, coef);
+    CU_TRY(c, cudaGetLastError());
+    launch(gradient_columns_kernel<RT>, dim3(slabs, *parts), GRAD_THREADS, 0, c->stream, p, row0, count, row0 == 0, coef);
+    CU_TRY(c, cudaGetLastError());
+    c->launches += 2;
+  }
+  return WPSGD_OK;
+}
+
+template <typename RT>
+wpsgd_status gradient(wpsgd_ctx* c, GradParams p, float lambda, float* grad, float* out) {
+  wpsgd_status s = rows_workspace(c);
+  if (s != WPSGD_OK) return s;
+  const RowsLayout lay(c->d);
+  p.sums = (double*)((char*)c->rows_ws + lay.sums);
+  p.part = (float*)((char*)c->rows_ws + lay.part);
+  int parts = 0, n_sums = 0;
+  if (p.n_rows > 0) {
+    s = gradient_any_width<RT>(c, p, &parts, &n_sums);
+    if (s != WPSGD_OK) return s;
+  }
+  launch(gradient_finish_kernel, (unsigned)((p.d + 31) / 32), 32 * GRAD_FINISH_WARPS, 0, c->stream, p.part, parts, p.sums, n_sums, p.w, p.d, p.n_rows, lambda, grad, out);
+  CU_TRY(c, cudaGetLastError());
+  c->launches++;
+  return WPSGD_OK;
+}
+
+const char* check_gradient(const wpsgd_ctx* c, const float* y, int64_t n_rows, const float* w, float lambda, wpsgd_loss loss, const float* grad, const float* out) {
+  if (!w || !grad || !out || (n_rows > 0 && !y)) return "NULL argument";
+  if ((int)loss < 0 || (int)loss > 2) return "unknown loss";
+  if (!std::isfinite(lambda)) return "lambda is not finite";
+  const size_t nd = (size_t)c->d * 4;
+  if (overlap(grad, nd, w, nd) || overlap(out, 8, w, nd) || overlap(out, 8, grad, nd)) return "grad, out and w overlap";
+  return nullptr;
+}
+
+// ---- norm and clipping ---------------------------------------------------------------------------------------------------
+constexpr int kFewTensors = 32, kManyTensors = 1000;  // per launch: 1 and 28 KB of kernel arguments
+
+struct Range {
+  uintptr_t lo, hi;
+  bool out;
+};
+
+}  // namespace
+
+// What wpsgd_grad_list_create makes of its arguments: the kernels' arguments, launch by launch, and the address ranges by address.
+struct wpsgd_grad_list {
+  std::vector<TensorList<kFewTensors>> few;  // one of the two: `few` where one launch of it is enough
+  std::vector<TensorList<kManyTensors>> many;
+  std::vector<Range> ranges;
+  uintptr_t longest = 0;   // range, bytes
+  long long chunks = 0;    // of the launch with most
+  bool in_place = true;
+};
+
+namespace {
+
+template <int N>
+void add_tensor(std::vector<TensorList<N>>& lists, const void* src, void* dst, long long n, bool bf16) {
+  const long long chunks = (n + CLIP_CHUNK - 1) / CLIP_CHUNK;
+  if (lists.empty() || lists.back().n == N || lists.back().first_chunk[lists.back().n] + chunks > INT32_MAX) {
+    lists.emplace_back();
+    lists.back().n = 0;
+    lists.back().first_chunk[0] = 0;
+  }
+  TensorList<N>& l = lists.back();
+  l.src[l.n] = src;
+  l.dst[l.n] = dst;
+  l.elems_type[l.n] = n * 2 + (bf16 ? 1 : 0);
+  l.first_chunk[l.n + 1] = l.first_chunk[l.n] + (int)chunks;
+  l.n++;
+}
+
+// nullptr, or what is wrong
+const char* make_list(wpsgd_grad_list* list, const void* const* src, void* const* dst, const int64_t* n_elems, const wpsgd_xtype* types, int32_t n_tensors) {
+  int filled = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (!known(types[i])) return "unknown element type";
+    if (n_elems[i] < 0 || n_elems[i] > (1ll << 43)) return "element count out of range";
+    filled += n_elems[i] > 0;
+  }
+  list->ranges.reserve(2 * (size_t)filled);
+  for (int i = 0; i < n_tensors; ++i) {
+    const long long n = n_elems[i];
+    if (n == 0) continue;
+    const size_t es = element_size(types[i]);
+    void* to = dst ? dst[i] : const_cast<void*>(src[i]);
+    if (!src[i] || !to) return "a tensor is NULL";
+    if ((uintptr_t)src[i] % es || (uintptr_t)to % es) return "a tensor is not aligned to its elements";
+    if (filled <= kFewTensors) add_tensor(list->few, src[i], to, n, types[i] == WPSGD_X_BF16);
+    else add_tensor(list->many, src[i], to, n, types[i] == WPSGD_X_BF16);
+    list->in_place = list->in_place && src[i] == to;
+    list->ranges.push_back({(uintptr_t)to, (uintptr_t)to + (size_t)n * es, true});
+    if (src[i] != to) list->ranges.push_back({(uintptr_t)src[i], (uintptr_t)src[i] + (size_t)n * es, false});
+    list->longest = std::max<uintptr_t>(list->longest, (size_t)n * es);
+  }
+  for (const auto& l : list->few) list->chunks = std::max<long long>(list->chunks, l.first_chunk[l.n]);
+  for (const auto& l : list->many) list->chunks = std::max<long long>(list->chunks, l.first_chunk[l.n]);
+  // every element is written by one thread and read by no other: outputs are disjoint, and each is its own input or apart from all
+  std::sort(list->ranges.begin(), list->ranges.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
+  uintptr_t end_all = 0, end_out = 0;  // ends of what lies before: of all ranges, of outputs
+  for (const Range& q : list->ranges) {
+    if (q.lo < end_out || (q.out && q.lo < end_all)) return "an output overlaps another output or another tensor's input";
+    end_all = std::max(end_all, q.hi);
+    if (q.out) end_out = std::max(end_out, q.hi);
+  }
+  return nullptr;
+}
+
+template <int N>
+wpsgd_status norm_and_scale(wpsgd_ctx* c, const std::vector<TensorList<N>>& lists, int blocks, bool scale, bool in_place, double max_norm, float* norm_out) {
+  double* part = (double*)((char*)c->rows_ws + RowsLayout(c->d).sums);
+  static_assert(CLIP_BLOCKS <= 2 * kMaxBlocks, "block sums must fit the workspace");
+  for (size_t i = 0; i < lists.size(); ++i) {
+    launch(squares_kernel<N>, blocks, CLIP_THREADS, 0, c->stream, lists[i], i == 0, part);
+    CU_TRY(c, cudaGetLastError());
+    c->launches++;
+  }
+  if (!scale || lists.empty()) {
+    launch(norm_kernel, 1, CLIP_THREADS, 0, c->stream, part, lists.empty() ? 0 : blocks, norm_out);
+    CU_TRY(c, cudaGetLastError());
+    c->launches++;
+    return WPSGD_OK;
+  }
+  for (size_t i = lists.size(); i-- > 0;) {
+    launch(scale_kernel<N>, blocks, CLIP_THREADS, 0, c->stream, lists[i], part, blocks, max_norm, in_place, norm_out);
+    CU_TRY(c, cudaGetLastError());
+    c->launches++;
+  }
+  return WPSGD_OK;
+}
+
+wpsgd_status run_list(wpsgd_ctx* c, const wpsgd_grad_list* list, bool scale, double max_norm, float* norm_out) {
+  if (!list || !norm_out) return fail(c, WPSGD_ERR_INVALID_ARG, "the list or norm_out is NULL");
+  // norm_out in no range: of those that start before its end, only such as start less than the longest before it can reach it
+  const uintptr_t lo = (uintptr_t)norm_out, hi = lo + sizeof(float);
+  auto it = std::lower_bound(list->ranges.begin(), list->ranges.end(), hi, [](const Range& r, uintptr_t v) { return r.lo < v; });
+  while (it != list->ranges.begin()) {
+    --it;
+    if (it->hi > lo) return fail(c, WPSGD_ERR_INVALID_ARG, "norm_out overlaps a tensor of the list");
+    if (it->lo + list->longest <= lo) break;
+  }
+  DeviceGuard guard(c->device);
+  wpsgd_status s = rows_workspace(c);
+  if (s != WPSGD_OK) return s;
+  const int blocks = (int)std::max(1ll, std::min<long long>(CLIP_BLOCKS, list->chunks));
+  return list->many.empty() ? norm_and_scale(c, list->few, blocks, scale, list->in_place, max_norm, norm_out)
+                            : norm_and_scale(c, list->many, blocks, scale, list->in_place, max_norm, norm_out);
+}
+
+}  // namespace
+
+extern "C" {
+
+wpsgd_status wpsgd_quantize_rows(wpsgd_ctx* c, const void* X, wpsgd_xtype xt, int64_t ld_elems, int64_t n_rows, uint8_t* Q, int64_t ld_q, float* scales, int64_t ld_s) {
+  if (!c) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "ctx is NULL");
+  if (!known(xt)) return fail(c, WPSGD_ERR_INVALID_ARG, "unknown feature type");
+  if (ld_elems < c->d || (n_rows > 0 && !X)) return fail(c, WPSGD_ERR_INVALID_ARG, "quantize_rows: bad argument");
+  if (const char* why = check_rows8(Q, ld_q, scales, ld_s, n_rows, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("quantize_rows: ") + why);
+  if (n_rows == 0) return WPSGD_OK;
+  const size_t es = element_size(xt);
+  if ((uintptr_t)X % es) return fail(c, WPSGD_ERR_INVALID_ARG, "quantize_rows: X is not aligned to its elements");
+  DeviceGuard guard(c->device);
+  const long long nb = blocks_of(c->d);
+  if (nb > INT32_MAX || n_rows > INT64_MAX / nb / 64) return fail(c, WPSGD_ERR_UNSUPPORTED, "quantize_rows: more than 2^57 blocks");
+  const bool vec = aligned16(X) && ((size_t)ld_elems * es) % 16 == 0 && ((size_t)c->d * es) % 16 == 0;
+  auto go = [&](auto tag, auto vec_tag) {
+    using XT = decltype(tag);
+    constexpr int U = 4, per_block = 8 * U * (32 / (Q_BLOCK / XVec<XT>::V));
+    launch(quantize_rows_kernel<XT, decltype(vec_tag)::value, U>, grid_for(n_rows * nb, per_block, 148 * 8), 256, 0, c->stream, (const XT*)X, ld_elems, n_rows, c->d, (int)nb, Q, ld_q, scales, ld_s);
+  };
+  if (xt == WPSGD_X_F32) vec ? go(float(), std::true_type()) : go(float(), std::false_type());
+  else vec ? go(__nv_bfloat16(), std::true_type()) : go(__nv_bfloat16(), std::false_type());
+  CU_TRY(c, cudaGetLastError());
+  c->launches++;
+  return WPSGD_OK;
+}
+
+wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld_q, const float* q_scales, int64_t ld_qs, int64_t n_rows, const uint8_t* M, int64_t ld_m,
+                               const float* m_scales, int64_t ld_ms, int64_t n_models, void* Z, wpsgd_xtype zt, int64_t ld_z) {
+  if (!c) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "ctx is NULL");
+  if (!known(zt)) return fail(c, WPSGD_ERR_INVALID_ARG, "margins_fp8: unknown output type");
+  if (const char* why = check_rows8(Q, ld_q, q_scales, ld_qs, n_rows, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("margins_fp8: rows: ") + why);
+  if (const char* why = check_rows8(M, ld_m, m_scales, ld_ms, n_models, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("margins_fp8: models: ") + why);
+  if (n_rows > INT32_MAX || n_models > INT32_MAX) return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: 2^31 rows or models and more");
+  if (n_rows == 0 || n_models == 0) return WPSGD_OK;
+  if (!Z || ld_z < n_models || (uintptr_t)Z % element_size(zt)) return fail(c, WPSGD_ERR_INVALID_ARG, "margins_fp8: Z is NULL, not aligned to its elements, or its stride is below n_models");
+  DeviceGuard guard(c->device);
+  const dim3 grid((unsigned)((n_rows + 63) / 64), (unsigned)((n_models + 63) / 64));
+  const size_t smem = 2 * 64 * 129 * sizeof(float);
+  auto go = [&](auto tag) {
+    using OT = decltype(tag);
+    cudaError_t e = allow_all_smem(margins_kernel<OT>);
+    if (e != cudaSuccess) return e;
+    return launch(margins_kernel<OT>, grid, 256, smem, c->stream, Q, ld_q, q_scales, ld_qs, n_rows, M, ld_m, m_scales, ld_ms, n_models, c->d, (OT*)Z, ld_z);
+  };
+  CU_TRY(c, zt == WPSGD_X_F32 ? go(float()) : go(__nv_bfloat16()));
+  c->launches++;
+  return WPSGD_OK;
+}
+
+wpsgd_status wpsgd_objective_grad(wpsgd_ctx* c, const void* X, wpsgd_xtype xt, int64_t ld_elems, const float* y, int64_t n_rows, const float* w, float lambda,
+                                  wpsgd_loss loss, float* grad, float* out) {
+  if (!c) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "ctx is NULL");
+  if (!known(xt)) return fail(c, WPSGD_ERR_INVALID_ARG, "unknown feature type");
+  if (n_rows < 0 || ld_elems < c->d || (n_rows > 0 && !X)) return fail(c, WPSGD_ERR_INVALID_ARG, "objective_grad: bad argument");
+  if (const char* why = check_gradient(c, y, n_rows, w, lambda, loss, grad, out)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("objective_grad: ") + why);
+  if ((uintptr_t)X % element_size(xt)) return fail(c, WPSGD_ERR_INVALID_ARG, "objective_grad: X is not aligned to its elements");
+  DeviceGuard guard(c->device);
+  const GradParams p = {X, ld_elems, nullptr, 0, y, w, n_rows, c->d, (int)loss, nullptr, nullptr};
+  return xt == WPSGD_X_F32 ? gradient<float>(c, p, lambda, grad, out) : gradient<__nv_bfloat16>(c, p, lambda, grad, out);
+}
+
+wpsgd_status wpsgd_objective_grad_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld_q, const float* scales, int64_t ld_s, const float* y, int64_t n_rows, const float* w,
+                                      float lambda, wpsgd_loss loss, float* grad, float* out) {
+  if (!c) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "ctx is NULL");
+  if (const char* why = check_rows8(Q, ld_q, scales, ld_s, n_rows, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("objective_grad_fp8: ") + why);
+  if (const char* why = check_gradient(c, y, n_rows, w, lambda, loss, grad, out)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("objective_grad_fp8: ") + why);
+  DeviceGuard guard(c->device);
+  const GradParams p = {Q, ld_q, scales, ld_s, y, w, n_rows, c->d, (int)loss, nullptr, nullptr};
+  return gradient<Row8>(c, p, lambda, grad, out);
+}
+
+wpsgd_status wpsgd_grad_list_create(const void* const* grads, void* const* out, const int64_t* n_elems, const wpsgd_xtype* types, int32_t n_tensors,
+                                    wpsgd_grad_list** list) {
+  if (!list) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "list is NULL");
+  *list = nullptr;
+  if (n_tensors < 0 || (n_tensors > 0 && (!grads || !n_elems || !types))) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "grad_list_create: bad argument");
+  try {
+    std::unique_ptr<wpsgd_grad_list> l(new wpsgd_grad_list());
+    if (const char* why = make_list(l.get(), grads, out, n_elems, types, n_tensors)) return fail(nullptr, WPSGD_ERR_INVALID_ARG, std::string("grad_list_create: ") + why);
+    *list = l.release();
+  } catch (const std::bad_alloc&) {
+    return fail(nullptr, WPSGD_ERR_ALLOC, "grad_list_create: no memory");
+  }
+  return WPSGD_OK;
+}
+
+wpsgd_status wpsgd_grad_list_destroy(wpsgd_grad_list* list) {
+  delete list;
+  return WPSGD_OK;
+}
+
+wpsgd_status wpsgd_grad_norm(wpsgd_ctx* c, const wpsgd_grad_list* list, float* norm_out) {
+  if (!c) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "ctx is NULL");
+  return run_list(c, list, false, 0.0, norm_out);
+}
+
+wpsgd_status wpsgd_clip_grad_norm(wpsgd_ctx* c, const wpsgd_grad_list* list, double max_norm, float* norm_out) {
+  if (!c) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "ctx is NULL");
+  if (!(max_norm >= 0.0)) return fail(c, WPSGD_ERR_INVALID_ARG, "clip_grad_norm: max_norm must be >= 0");
+  return run_list(c, list, true, max_norm, norm_out);
+}
+
+}  // extern "C"
