@@ -60,6 +60,74 @@ const char* check_rows8(const uint8_t* Q, int64_t ld_q, const float* scales, int
   return nullptr;
 }
 
+// ---- margins -------------------------------------------------------------------------------------------------------------
+struct MarginsCall {
+  const uint8_t* Q;
+  long long ld_q;
+  const uint8_t* M;
+  long long ld_m, d;
+  MarginsParams p;
+};
+
+// The driver's encoder of tensor maps, asked for by name: the library does not link against the driver.
+decltype(&cuTensorMapEncodeTiled) tensor_map_encoder() {
+  static const auto fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      f = nullptr;
+    }
+    return (decltype(&cuTensorMapEncodeTiled))f;
+  }();
+  return fn;
+}
+// Boxes of 128 columns and `box_rows` rows of an 8-bit matrix; what lies outside it reads as zeros.
+bool encode_rows8(CUtensorMap* map, const uint8_t* base, long long d, long long rows, long long ld, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {Q_BLOCK, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+  return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename OT, int BN>
+wpsgd_status launch_margins(wpsgd_ctx* c, const MarginsCall& call) {
+  using Shape = MarginsShape<BN>;
+  static_assert(Shape::stages >= 3 && Shape::smem <= (int)kSmemMax, "a ring of three stages must fit");
+  CUtensorMap map_q, map_m;
+  MarginsParams p = call.p;
+  if (!tensor_map_encoder()) return fail(c, WPSGD_ERR_CUDA, "margins_fp8: the driver has no cuTensorMapEncodeTiled");
+  if (!encode_rows8(&map_q, call.Q, call.d, p.n_rows, call.ld_q, MG_ROWS) || !encode_rows8(&map_m, call.M, call.d, p.n_models, call.ld_m, BN))
+    return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: sizes or strides that a tensor map cannot describe");
+  p.tiles_m = (p.n_models + BN - 1) / BN;
+  const long long tiles = (long long)((p.n_rows + MG_ROWS - 1) / MG_ROWS) * p.tiles_m;
+  if (tiles > INT32_MAX - 148 || tiles / 148 * p.blocks > INT32_MAX) return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: too many tiles");
+  p.tiles = (int)tiles;
+  CU_TRY(c, allow_all_smem(margins_kernel<OT, BN>));
+  CU_TRY(c, launch(margins_kernel<OT, BN>, (unsigned)std::min<long long>(tiles, 148), Shape::threads, Shape::smem, c->stream, map_q, map_m, p));
+  c->launches++;
+  return WPSGD_OK;
+}
+
+template <typename OT>
+wpsgd_status margins_of(wpsgd_ctx* c, const MarginsCall& call) {
+  // Width of a tile by the time of the busiest SM, in cycles: per tile and block of columns the products (2 per model), the copies
+  // (16 KB of rows and 128 bytes per model at about 40 bytes a cycle) or the hand-over from role to role, whichever is longest.
+  auto cycles = [&](long long bn) {
+    const long long tiles = ((call.p.n_rows + MG_ROWS - 1) / MG_ROWS) * ((call.p.n_models + bn - 1) / bn), rounds = (tiles + 147) / 148;
+    const long long step = std::max(2 * bn, (MG_ROWS + bn) * Q_BLOCK / 40);
+    return rounds * (call.p.blocks * step + 12 * bn);
+  };
+  long long best = 16;
+  for (long long bn : {32, 64, 128, 256})
+    if (cycles(bn) < cycles(best)) best = bn;
+  if (best == 16) return launch_margins<OT, 16>(c, call);
+  if (best == 32) return launch_margins<OT, 32>(c, call);
+  if (best == 64) return launch_margins<OT, 64>(c, call);
+  if (best == 128) return launch_margins<OT, 128>(c, call);
+  return launch_margins<OT, 256>(c, call);
+}
+
 // ---- gradient ------------------------------------------------------------------------------------------------------------
 template <typename RT>
 wpsgd_status gradient_any_width(wpsgd_ctx* c, GradParams p, int* parts, int* n_sums) {
@@ -260,17 +328,9 @@ wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld_q, con
   if (n_rows == 0 || n_models == 0) return WPSGD_OK;
   if (!Z || ld_z < n_models || (uintptr_t)Z % element_size(zt)) return fail(c, WPSGD_ERR_INVALID_ARG, "margins_fp8: Z is NULL, not aligned to its elements, or its stride is below n_models");
   DeviceGuard guard(c->device);
-  const dim3 grid((unsigned)((n_rows + 63) / 64), (unsigned)((n_models + 63) / 64));
-  const size_t smem = 2 * 64 * 129 * sizeof(float);
-  auto go = [&](auto tag) {
-    using OT = decltype(tag);
-    cudaError_t e = allow_all_smem(margins_kernel<OT>);
-    if (e != cudaSuccess) return e;
-    return launch(margins_kernel<OT>, grid, 256, smem, c->stream, Q, ld_q, q_scales, ld_qs, n_rows, M, ld_m, m_scales, ld_ms, n_models, c->d, (OT*)Z, ld_z);
-  };
-  CU_TRY(c, zt == WPSGD_X_F32 ? go(float()) : go(__nv_bfloat16()));
-  c->launches++;
-  return WPSGD_OK;
+  const MarginsCall call = {Q, ld_q, M, ld_m, c->d, {q_scales, ld_qs, m_scales, ld_ms, Z, ld_z, (int)n_rows, (int)n_models, (int)blocks_of(c->d), 0, 0,
+                            aligned16(Z) && ld_z * element_size(zt) % 16 == 0, c->opt_spin_limit, c->opt_drop_block, c->status}};
+  return zt == WPSGD_X_F32 ? margins_of<float>(c, call) : margins_of<__nv_bfloat16>(c, call);
 }
 
 wpsgd_status wpsgd_objective_grad(wpsgd_ctx* c, const void* X, wpsgd_xtype xt, int64_t ld_elems, const float* y, int64_t n_rows, const float* w, float lambda,
