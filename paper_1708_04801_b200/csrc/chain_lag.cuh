@@ -189,12 +189,6 @@ __device__ __forceinline__ void st_async_f32_if(uint32_t addr, float v, uint32_t
       "f"(v), "r"(mbar), "r"((int)yes)
       : "memory");
 }
-// one thread of a converged warp; the compiler knows that it is one
-__device__ __forceinline__ bool elect_one() {
-  uint32_t yes;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
-  return yes != 0;
-}
 
 __device__ __forceinline__ float4 lds_f32x4(uint32_t a) {
   float4 v;

@@ -8,8 +8,9 @@
 //
 // One persistent CTA per SM, a role per warp: warp 0 brings the tiles of Q and M into a ring of stages (TMA, 128-byte swizzle; what lies outside
 // the matrices arrives as zeros), warp 1 issues the products, warp 2 brings the scales of a block's 128 rows and BN models (cp.async) into a
-// ring of its own, warp 3 owns the tensor memory, the warps from 4 on add up: thread = row, 128 rows per four warps. The margins
-// leave through a staging buffer of each warp, so that stores cover 64 bytes of a row.
+// ring of its own, warp 3 owns the tensor memory, the warps from 4 on add up. They read tensor memory in the order of a matrix fragment, four rows
+// and 2 of 8 models per thread, and not a row per thread: a thread then needs COLS / 4 + 4 scales for COLS sums instead of COLS + 1,
+// and it was the return of those from shared memory (128 bytes a cycle) that bounded the kernel.
 // Every wait is bounded. When one runs out it is recorded in the status word, all roles leave, the copies and products in flight are waited
 // for (bounded again), and the tensor memory is given back.
 #pragma once
@@ -23,19 +24,19 @@
 namespace wpsgd {
 
 constexpr int MG_ROWS = 128;       // of a tile: the lanes of tensor memory
-constexpr int MG_SCALE_SLOTS = 8;  // blocks whose scales are in shared memory at a time
+constexpr int MG_WINDOW = 4;       // blocks of columns whose scales are brought together
+constexpr int MG_WINDOWS = 2;      // of them in shared memory
 
 template <int BN>
 struct MarginsShape {
-  static constexpr int groups = BN >= 64 ? 2 : 1;     // of four adding warps: each takes BN / groups models
-  static constexpr int cols = BN / groups;
+  static constexpr int cols = BN == 256 ? 64 : BN == 128 ? 32 : 16;  // models of an adding warp
+  static constexpr int groups = BN / cols;                           // of four such warps
   static constexpr int threads = 128 + 128 * groups;
   static constexpr int buffers = BN == 256 ? 2 : 4;   // of D_b in tensor memory
   static constexpr int tmem_cols = buffers * BN;      // a power of two, 64 .. 512
   static constexpr int stage_bytes = (MG_ROWS + BN) * Q_BLOCK;
-  static constexpr int slot_bytes = (MG_ROWS + BN) * 4;
-  static constexpr int staging_bytes = 4 * groups * 32 * 80;
-  static constexpr int fixed_bytes = 1024 + MG_SCALE_SLOTS * slot_bytes + staging_bytes + 512;  // 1024: alignment of the ring
+  static constexpr int slot = MG_ROWS + BN + 8;       // scales of a block; + 8: 4 blocks of 8 rows lie in different banks
+  static constexpr int fixed_bytes = 1024 + MG_WINDOWS * MG_WINDOW * slot * 4 + 512;  // 1024: alignment of the ring
   static constexpr int stages = (227 * 1024 - fixed_bytes) / stage_bytes < 10 ? (227 * 1024 - fixed_bytes) / stage_bytes : 10;
   static constexpr int smem = fixed_bytes + stages * stage_bytes;
 };
@@ -49,7 +50,7 @@ struct MarginsParams {
   long long ld_z;
   int n_rows, n_models, blocks;   // blocks of 128 columns
   int tiles_m, tiles;             // tiles of models per tile of rows, tiles in all
-  bool vector;                    // 16-byte stores reach every row's margins
+  bool pairs;                     // two neighbouring margins of a row share an aligned access
   long long spin_limit;
   long long drop_block;           // test hook: this block of columns is never requested (-1: none)
   DevStatus* status;
@@ -80,17 +81,15 @@ __device__ __forceinline__ void tmem_alloc(uint32_t* to, uint32_t cols) {
 __device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t cols) {
   asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
 }
-// 16 columns of this warp's 32 lanes, a lane per thread
-__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&v)[16]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
-                 "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-               : "r"(addr));
+// 8 columns of a warp's 32 lanes in the order of matrix fragments: thread t gets columns 2 (t % 4) and the next of lanes t / 4 (v[0], v[1]),
+// t / 4 + 8 (v[2], v[3]), t / 4 + 16 and t / 4 + 24
+__device__ __forceinline__ void tmem_load8(uint32_t addr, uint32_t (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr));
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(addr + (16u << 16)));
 }
-__device__ __forceinline__ void tmem_wait_load(uint32_t (&v)[16]) {  // names the registers, so that no use of them moves before the wait
+__device__ __forceinline__ void tmem_wait_load(uint32_t (&v)[8]) {  // names the registers, so that no use of them moves before the wait
   asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
-                 "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7])::"memory");
 }
 __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, unsigned long long* bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"((uint32_t)__cvta_generic_to_shared(dst)),
@@ -106,8 +105,27 @@ __device__ __forceinline__ void cp_async_arrive(unsigned long long* bar) {  // o
 __device__ __forceinline__ void mbar_arrive_one(unsigned long long* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"((uint32_t)__cvta_generic_to_shared(bar)) : "memory");
 }
-// pairs of fp32 in one instruction
-__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
+__device__ __forceinline__ float lds_f32(uint32_t a) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint64_t lds_pair(uint32_t a) {
+  uint64_t v;
+  asm volatile("ld.shared.b64 %0, [%1];" : "=l"(v) : "r"(a));
+  return v;
+}
+// two fp32 in one instruction
+__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 halves(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
@@ -117,14 +135,6 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   uint64_t r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
-}
-__device__ __forceinline__ uint4 lds16(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ void sts16(uint32_t a, uint4 v) {
-  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
 // A wait that gives up: after its own limit, or when another role has (dead). False: leave.
@@ -143,22 +153,39 @@ struct MarginsWait {
   }
 };
 
+// Two margins of a row, of which `left` exist, in one access where they lie on its boundary (pairs)
+__device__ __forceinline__ void store_pair(float* to, float2 z, int left, bool pairs) {
+  if (pairs && left > 1) {
+    *(float2*)to = z;
+  } else {
+    if (left > 0) to[0] = z.x;
+    if (left > 1) to[1] = z.y;
+  }
+}
+__device__ __forceinline__ void store_pair(__nv_bfloat16* to, float2 z, int left, bool pairs) {
+  if (pairs && left > 1) {
+    *(__nv_bfloat162*)to = __floats2bfloat162_rn(z.x, z.y);
+  } else {
+    if (left > 0) to[0] = __float2bfloat16_rn(z.x);
+    if (left > 1) to[1] = __float2bfloat16_rn(z.y);
+  }
+}
+
 template <typename OT, int BN>
 __global__ void __launch_bounds__(MarginsShape<BN>::threads, 1)
 margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_m, const __grid_constant__ MarginsParams p) {
   using Shape = MarginsShape<BN>;
-  constexpr int S = Shape::stages, NB = Shape::buffers, SS = MG_SCALE_SLOTS, COLS = Shape::cols;
+  constexpr int S = Shape::stages, NB = Shape::buffers, SS = MG_WINDOWS, COLS = Shape::cols;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   float* scales = (float*)(ring + S * Shape::stage_bytes);
-  unsigned char* staging = (unsigned char*)(scales + SS * (MG_ROWS + BN));
-  unsigned long long* bars = (unsigned long long*)(staging + Shape::staging_bytes);
+  unsigned long long* bars = (unsigned long long*)(scales + MG_WINDOWS * MG_WINDOW * Shape::slot);
   unsigned long long *full = bars, *empty = full + S, *acc_full = empty + S, *acc_empty = acc_full + NB, *sc_full = acc_empty + NB, *sc_empty = sc_full + SS,
                      *drained = sc_empty + SS;
   static_assert(8 * (2 * S + 2 * NB + 2 * SS + 1) + 8 <= 512, "barriers, tensor memory address and flag must fit");
   uint32_t& tmem_base = *(uint32_t*)(drained + 1);  // (no static shared memory: the dynamic part may be all of the SM's)
   volatile int* dead_flag = (volatile int*)(drained + 1) + 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (shfl: known to be the same in all lanes)
   kernel_started();
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
@@ -197,152 +224,115 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         for (uint32_t j = it > S ? it - S : 0; j < it; ++j) mbar_wait_bounded(&full[j % S], j / S & 1, p.spin_limit);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
-      for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x) {
-        for (int k = 0; k < nk; ++k, ++it) {
-          const uint32_t s = it % S, b = it % NB;
-          if (!(ok = wait(&acc_empty[b], (it / NB & 1) ^ 1, 42) && wait(&full[s], it / S & 1, 43))) break;
-          tmem_fence_after();
-          const uint32_t a = (uint32_t)__cvta_generic_to_shared(ring + s * Shape::stage_bytes), m = a + MG_ROWS * Q_BLOCK;
+    // the whole warp goes through the loop, so that addresses and descriptors stay in uniform registers; one elected thread issues
+    const uint64_t first = mma_operand((uint32_t)__cvta_generic_to_shared(ring));
+    uint32_t s = 0, s_parity = 0, b = 0, b_parity = 1;
+    bool ok = true;
+    for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x) {
+      for (int k = 0; k < nk; ++k) {
+        ok = wait(&full[s], s_parity, 43) && wait(&acc_empty[b], b_parity, 42);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        tmem_fence_after();
+        const uint64_t q = first + s * (Shape::stage_bytes >> 4), m = q + (MG_ROWS * Q_BLOCK >> 4);
+        if (elect_one()) {
 #pragma unroll
           for (int j = 0; j < Q_BLOCK / 32; ++j)  // 32 columns a product
-            mma_e4m3(tmem + b * BN, mma_operand(a + 32 * j), mma_operand(m + 32 * j), mma_shape<BN>(), j > 0);
+            mma_e4m3(tmem + b * BN, q + 2 * j, m + 2 * j, mma_shape<BN>(), j > 0);
           mma_commit(&empty[s]);
           mma_commit(&acc_full[b]);
         }
-      }
-      if (!ok) {  // products in flight end before tensor memory is given back
-        mma_commit(drained);
-        mbar_wait_bounded(drained, 0, p.spin_limit);
+        __syncwarp();
+        if (++s == S) { s = 0; s_parity ^= 1; }
+        if (++b == NB) { b = 0; b_parity ^= 1; }
       }
     }
+    if (!ok) {  // products in flight end before tensor memory is given back
+      if (elect_one()) mma_commit(drained);
+      mbar_wait_bounded(drained, 0, p.spin_limit);
+    }
   } else if (warp == 2) {
-    uint32_t it = 0;
+    // a lane brings one of 4 blocks of 8 rows: 16 bytes of a row in one instruction
+    uint32_t win = 0;
     bool ok = true;
+    const int ahead = lane % MG_WINDOW, sub = lane / MG_WINDOW;
     for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x) {
       const int row0 = t / p.tiles_m * MG_ROWS, m0 = t % p.tiles_m * BN;
-      for (int k = 0; k < nk; ++k, ++it) {
-        const uint32_t q = it % SS;
-        if (!(ok = wait(&sc_empty[q], (it / SS & 1) ^ 1, 44))) break;
-        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(scales + q * (MG_ROWS + BN));
+      for (int k0 = 0; k0 < nk; k0 += MG_WINDOW, ++win) {
+        if (!(ok = wait(&sc_empty[win % SS], (win / SS & 1) ^ 1, 44))) break;
+        const int k = k0 + ahead;
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(scales + (win % SS * MG_WINDOW + ahead) * Shape::slot);
 #pragma unroll
-        for (int i = 0; i < MG_ROWS / 32; ++i) {
-          const int r = row0 + 32 * i + lane;
-          const bool in = r < p.n_rows;
-          cp_async4_or_zero(dst + (32 * i + lane) * 4, p.q_scales + (in ? r : 0) * p.ld_qs + k, in);
+        for (int i = 0; i < MG_ROWS; i += 32 / MG_WINDOW) {
+          const int r = row0 + i + sub;
+          const bool in = r < p.n_rows && k < nk;
+          cp_async4_or_zero(dst + (i + sub) * 4, p.q_scales + (in ? r * p.ld_qs + k : 0), in);
         }
 #pragma unroll
-        for (int i = 0; i < (BN + 31) / 32; ++i) {
-          const int m = m0 + 32 * i + lane;
-          const bool in = m < p.n_models;
-          if (32 * i + lane < BN) cp_async4_or_zero(dst + (MG_ROWS + 32 * i + lane) * 4, p.m_scales + (in ? m : 0) * p.ld_ms + k, in);
+        for (int i = 0; i < BN; i += 32 / MG_WINDOW) {
+          const int m = m0 + i + sub;
+          const bool in = m < p.n_models && k < nk;
+          cp_async4_or_zero(dst + (MG_ROWS + i + sub) * 4, p.m_scales + (in ? m * p.ld_ms + k : 0), in);
         }
-        cp_async_arrive(&sc_full[q]);
+        cp_async_arrive(&sc_full[win % SS]);
       }
-      ok = __all_sync(0xffffffffu, ok);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= 4) {
     const int quarter = warp & 3, group = (warp - 4) >> 2;  // a warp reads the 32 lanes of tensor memory of its number modulo 4
     const uint32_t my_tmem = tmem + ((uint32_t)(32 * quarter) << 16) + group * COLS;
-    const uint32_t my_staging = (uint32_t)__cvta_generic_to_shared(staging + (warp - 4) * 32 * 80);
+    const uint32_t my_row = 32 * quarter + lane / 4, my_col = group * COLS + 2 * (lane % 4);  // the first of this thread's rows and models
     const uint32_t scales_at = (uint32_t)__cvta_generic_to_shared(scales);
-    uint32_t it = 0;
+    uint32_t it = 0, win = 0;
     bool ok = true;
     for (int t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-      const int row0 = t / p.tiles_m * MG_ROWS + 32 * quarter, m0 = t % p.tiles_m * BN + group * COLS;
-      uint64_t acc[COLS / 2];
+      uint64_t acc[4][COLS / 8];  // row my_row + 8 i, models my_col + 8 j and the next
 #pragma unroll
-      for (int i = 0; i < COLS / 2; ++i) acc[i] = 0;
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < COLS / 8; ++j) acc[i][j] = 0;
       for (int k = 0; k < nk; ++k, ++it) {
-        const uint32_t b = it % NB, q = it % SS;
-        ok = wait(&sc_full[q], it / SS & 1, 45) && wait(&acc_full[b], it / NB & 1, 46);
+        const uint32_t b = it % NB, q = win % SS;
+        ok = (k % MG_WINDOW || wait(&sc_full[q], win / SS & 1, 45)) && wait(&acc_full[b], it / NB & 1, 46);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tmem_fence_after();
-        const uint32_t slot = scales_at + q * Shape::slot_bytes;
-        float rs;
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(rs) : "r"(slot + (32 * quarter + lane) * 4));
-        const uint64_t rs2 = pair_of(__float_as_uint(rs), __float_as_uint(rs));
-        const uint32_t cs = slot + (MG_ROWS + group * COLS) * 4;
+        const uint32_t slot = scales_at + (q * MG_WINDOW + k % MG_WINDOW) * Shape::slot * 4;
+        uint64_t rs[4];
 #pragma unroll
-        for (int c = 0; c < COLS; c += 16) {
-          uint32_t v[16];
-          tmem_load16(my_tmem + b * BN + c, v);
-          tmem_wait_load(v);
-#pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const uint4 w = lds16(cs + (c + e) * 4);
-            acc[(c + e) / 2] = fma2(pair_of(v[e], v[e + 1]), mul2(rs2, pair_of(w.x, w.y)), acc[(c + e) / 2]);
-            acc[(c + e) / 2 + 1] = fma2(pair_of(v[e + 2], v[e + 3]), mul2(rs2, pair_of(w.z, w.w)), acc[(c + e) / 2 + 1]);
-          }
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t r = __float_as_uint(lds_f32(slot + (my_row + 8 * i) * 4));
+          rs[i] = pair_of(r, r);
         }
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive_one(&acc_empty[b]);
-          mbar_arrive_one(&sc_empty[q]);
+        uint32_t v[2][8];
+        tmem_load8(my_tmem + b * BN, v[0]);
+#pragma unroll
+        for (int c = 0; c < COLS / 8; ++c) {  // the next 8 columns are on their way while these are added
+          const uint64_t cs = lds_pair(slot + (MG_ROWS + my_col + 8 * c) * 4);
+          tmem_wait_load(v[c % 2]);
+          if (c + 1 < COLS / 8) {
+            tmem_load8(my_tmem + b * BN + 8 * (c + 1), v[(c + 1) % 2]);
+          } else {  // the last of this block: its buffer is free
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_one(&acc_empty[b]);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i][c] = fma2(pair_of(v[c % 2][2 * i], v[c % 2][2 * i + 1]), mul2(rs[i], cs), acc[i][c]);
+        }
+        if (k % MG_WINDOW == MG_WINDOW - 1 || k == nk - 1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive_one(&sc_empty[q]);
+          ++win;
         }
       }
       if (!ok) break;
-      // 16 words of each row at a time: 16 fp32 margins, or 32 of bf16
-      constexpr int PER_WORD = sizeof(OT) == 4 ? 1 : 2, STEP = 16 * PER_WORD < COLS ? 16 * PER_WORD : COLS, WORDS = STEP / PER_WORD;
+      const int row = t / p.tiles_m * MG_ROWS + my_row, model = t % p.tiles_m * BN + my_col;
 #pragma unroll
-      for (int c = 0; c < COLS; c += STEP) {
-        __syncwarp();
+      for (int i = 0; i < 4; ++i) {
+        if (row + 8 * i >= p.n_rows) continue;
+        OT* to = (OT*)p.Z + (long long)(row + 8 * i) * p.ld_z + model;
 #pragma unroll
-        for (int e = 0; e < WORDS; e += 4) {
-          uint32_t w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (PER_WORD == 1) {
-              const uint64_t a = acc[(c + e + i) / 2];
-              w[i] = (e + i) % 2 ? (uint32_t)(a >> 32) : (uint32_t)a;
-            } else {
-              const uint64_t a = acc[c / 2 + e + i];
-              const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32)));
-              w[i] = *(const uint32_t*)&h;
-            }
-          }
-          sts16(my_staging + lane * 80 + e * 4, make_uint4(w[0], w[1], w[2], w[3]));
-        }
-        __syncwarp();
-        if (p.vector) {
-          constexpr int LANES = WORDS / 4;  // that cover a row
-#pragma unroll
-          for (int j = 0; j < LANES; ++j) {
-            const int r = j * (32 / LANES) + lane / LANES, e = lane % LANES * 4, m = m0 + c + e * PER_WORD;
-            const uint4 w = lds16(my_staging + r * 80 + e * 4);
-            if (row0 + r >= p.n_rows) continue;
-            OT* to = (OT*)p.Z + (long long)(row0 + r) * p.ld_z + m;
-            if (m + 4 * PER_WORD <= p.n_models) {
-              *(uint4*)to = w;
-            } else {
-              const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-              for (int i = 0; i < 4 * PER_WORD; ++i)
-                if (m + i < p.n_models) {
-                  if constexpr (PER_WORD == 1) ((uint32_t*)to)[i] = x[i];
-                  else ((uint16_t*)to)[i] = (uint16_t)(x[i / 2] >> 16 * (i % 2));
-                }
-            }
-          }
-        } else {
-          constexpr int LANES = STEP < 32 ? STEP : 32;  // a margin each
-#pragma unroll 4
-          for (int r0 = 0; r0 < 32; r0 += 32 / LANES) {
-            const int r = r0 + lane / LANES, e = lane % LANES, m = m0 + c + e;
-            uint32_t w;
-            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(my_staging + r * 80 + e / PER_WORD * 4));
-            if (row0 + r < p.n_rows && m < p.n_models) {
-              OT* to = (OT*)p.Z + (long long)(row0 + r) * p.ld_z + m;
-              if constexpr (PER_WORD == 1) *(uint32_t*)to = w;
-              else *(uint16_t*)to = (uint16_t)(w >> 16 * (e % 2));
-            }
-          }
-        }
+        for (int j = 0; j < COLS / 8; ++j) store_pair(to + 8 * j, halves(acc[i][j]), p.n_models - model - 8 * j, p.pairs);
       }
     }
   }

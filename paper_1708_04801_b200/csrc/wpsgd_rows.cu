@@ -324,12 +324,12 @@ wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld_q, con
   if (!known(zt)) return fail(c, WPSGD_ERR_INVALID_ARG, "margins_fp8: unknown output type");
   if (const char* why = check_rows8(Q, ld_q, q_scales, ld_qs, n_rows, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("margins_fp8: rows: ") + why);
   if (const char* why = check_rows8(M, ld_m, m_scales, ld_ms, n_models, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("margins_fp8: models: ") + why);
-  if (n_rows > INT32_MAX || n_models > INT32_MAX) return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: 2^31 rows or models and more");
+  if (n_rows > INT32_MAX - 256 || n_models > INT32_MAX - 256) return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: 2^31 - 256 rows or models and more");
   if (n_rows == 0 || n_models == 0) return WPSGD_OK;
   if (!Z || ld_z < n_models || (uintptr_t)Z % element_size(zt)) return fail(c, WPSGD_ERR_INVALID_ARG, "margins_fp8: Z is NULL, not aligned to its elements, or its stride is below n_models");
   DeviceGuard guard(c->device);
   const MarginsCall call = {Q, ld_q, M, ld_m, c->d, {q_scales, ld_qs, m_scales, ld_ms, Z, ld_z, (int)n_rows, (int)n_models, (int)blocks_of(c->d), 0, 0,
-                            aligned16(Z) && ld_z * element_size(zt) % 16 == 0, c->opt_spin_limit, c->opt_drop_block, c->status}};
+                            ld_z % 2 == 0 && (uintptr_t)Z % (2 * element_size(zt)) == 0, c->opt_spin_limit, c->opt_drop_block, c->status}};
   return zt == WPSGD_X_F32 ? margins_of<float>(c, call) : margins_of<__nv_bfloat16>(c, call);
 }
 
