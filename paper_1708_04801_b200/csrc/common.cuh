@@ -112,6 +112,28 @@ __device__ __forceinline__ float widen_scalar<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ float widen_scalar<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
 
+// Pairs of fp32 in 64 bits, and operations on both at once.
+__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 halves(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // Read-only 16-byte global load that does not allocate in L1 (rows are streamed once per visit).
 __device__ __forceinline__ uint4 ld_stream16(const void* p) {
   uint4 r;

@@ -43,13 +43,18 @@ struct GradParams {
   double* sums;          // [blocks, 2] losses and errors
 };
 
-// 16 bytes of a row, widened
+// 16 bytes of a row, widened to pairs
 struct Row8 {};  // tag of 8-bit rows
 template <typename RT>
 struct RowUnit {
   static constexpr int V = XVec<RT>::V;
   using Scalar = RT;
-  __device__ __forceinline__ static void widen(const uint4& raw, float (&f)[V]) { XVec<RT>::widen(raw, f); }
+  __device__ __forceinline__ static void widen(const uint4& raw, uint64_t (&f)[V / 2]) {
+    float x[V];
+    XVec<RT>::widen(raw, x);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) f[i] = pair_of(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]));
+  }
 };
 template <>
 struct RowUnit<Row8> {
@@ -60,12 +65,13 @@ struct RowUnit<Row8> {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
     return __half22float2(*(const __half2*)&h);
   }
-  __device__ __forceinline__ static void widen(const uint4& raw, float (&f)[16]) {
+  __device__ __forceinline__ static void widen(const uint4& raw, uint64_t (&f)[8]) {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float2 a = pair(w[i] & 0xffffu), b = pair(w[i] >> 16);
-      f[4 * i] = a.x; f[4 * i + 1] = a.y; f[4 * i + 2] = b.x; f[4 * i + 3] = b.y;
+      f[2 * i] = pair_of(__float_as_uint(a.x), __float_as_uint(a.y));
+      f[2 * i + 1] = pair_of(__float_as_uint(b.x), __float_as_uint(b.y));
     }
   }
 };
@@ -89,9 +95,12 @@ __device__ __forceinline__ double exact_product(const GradParams& p, long long r
   }
 }
 
-// Bound of the fp32 margin's error, see above. 1.01: the norms are fp32 sums themselves; 2^-120: products below fp32's range.
+// Bound of the fp32 margin's error, see above. 1.01: the norms are fp32 sums themselves, and the root may be off by 2^-10;
+// 2^-120: products below fp32's range.
 __device__ __forceinline__ float margin_error(float terms, float w_norm, float x_squares) {
-  return w_norm > 0.0f ? fmaf(terms * 0x1p-24f * 1.01f * w_norm, sqrtf(x_squares), 0x1p-120f) : 0.0f;
+  float root;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(x_squares));
+  return w_norm > 0.0f ? fmaf(terms * 0x1p-24f * 1.01f * w_norm, root, 0x1p-120f) : 0.0f;
 }
 // Whether an error of `err` in z could move the row across a jump of the loss's derivative or of the sign.
 __device__ __forceinline__ bool near_jump(int loss, float y, float z, float err) {
@@ -178,6 +187,321 @@ __global__ void __launch_bounds__(GRAD_THREADS) gradient_columns_kernel(const Gr
   for (long long i = i0; i < i1; ++i) acc = fmaf(coef[i], row_element<RT>(p, row0 + i, c), acc);
   float* to = p.part + blockIdx.y * p.d + c;
   *to = first ? acc : *to + acc;
+}
+
+// ---- rows that a group of threads holds in registers: one pass ----------------------------------------------------------------
+// Sums over the lanes of each row group of R rows at a time: halves the rows a lane answers for at every step, so that R sums over L lanes take
+// about R + log2(L / R) exchanges. Lane l of its L ends with the sum of row (l / (L / R)).
+template <int R, int L>
+__device__ __forceinline__ float transpose_sum(float (&v)[R], int l) {
+  static_assert(R <= L, "a lane for each row");
+#pragma unroll
+  for (int o = L / 2, n = R / 2; o > 0; o >>= 1, n >>= 1) {
+    if (n > 0) {
+      const bool upper = (l & o) != 0;
+#pragma unroll
+      for (int i = 0; i < R / 2; ++i)
+        if (i < n) {
+          const float mine = upper ? v[i + n] : v[i], other = upper ? v[i] : v[i + n];
+          v[i] = mine + __shfl_xor_sync(0xffffffffu, other, o);
+        }
+    } else {
+      v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    }
+  }
+  return v[0];
+}
+
+// G threads per row, each CH units of 16 bytes of it (VEC) or the same number of single elements; R rows at a time.
+template <typename RT, bool VEC, int G, int CH, int R>
+struct GradShape {
+  static constexpr int V = RowUnit<RT>::V;
+  static constexpr bool scaled = std::is_same<RT, Row8>::value;
+  static constexpr int threads = G > GRAD_THREADS ? G : GRAD_THREADS;
+  static constexpr int per_sm = threads > GRAD_THREADS ? 1 : 2;
+  static constexpr int groups = threads / G;       // of a block
+  static constexpr int lanes = G < 32 ? G : 32;    // of a warp that work on the same rows
+  static constexpr int warps = G < 32 ? 1 : G / 32;
+  // VEC: each thread keeps its part of the next rows in shared memory, in slots of R rows that no other thread touches
+  static constexpr int slot_bytes = threads * R * CH * (scaled ? 20 : 16);
+  static constexpr int slots = VEC ? 96 * 1024 * 2 / per_sm / slot_bytes : 0;
+  static constexpr int fold_bytes = groups > 1 ? threads * CH * V * 4 : 0;
+  static constexpr int smem = slots * slot_bytes > fold_bytes ? slots * slot_bytes : fold_bytes;
+};
+
+template <typename RT, bool VEC, int G, int CH, int R>
+__global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradShape<RT, VEC, G, CH, R>::per_sm) gradient_rows_kernel(const __grid_constant__ GradParams p) {
+  using Shape = GradShape<RT, VEC, G, CH, R>;
+  constexpr int V = Shape::V, L = Shape::lanes, W = Shape::warps, E = CH * V, T = Shape::threads;
+  constexpr bool SCALED = Shape::scaled;
+  extern __shared__ __align__(16) unsigned char grad_smem[];
+  __shared__ float2 cross[2][T / 32][R];  // a warp's sums of w x and x x of each row
+  __shared__ double cross64[T / 32];
+  __shared__ double sums[2][T / 32];
+  kernel_started();
+  kernel_inputs_ready();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = threadIdx.x / G, gl = threadIdx.x % G, l = lane % L;
+  const int units = (int)(VEC ? (p.d + V - 1) / V : p.d);
+  auto group_barrier = [&]() {
+    if constexpr (W > 1) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(G) : "memory");
+  };
+  // column of element i: VEC (unit gl + j G) V + e, else gl + i G
+  auto column = [&](int i) { return VEC ? (gl + i / V * G) * V + i % V : gl + i * G; };
+  auto has = [&](int i) { return column(i) < p.d; };
+
+  const long long stride = (long long)gridDim.x * Shape::groups * R;  // rows that all groups take at a time
+  const long long first = ((long long)blockIdx.x * Shape::groups + group) * R;
+  // ---- VEC: rows through this thread's slots. What lies behind a row's end arrives as zeros.
+  constexpr int S = VEC ? Shape::slots : 1;
+  const uint32_t slots = (uint32_t)__cvta_generic_to_shared(grad_smem) + threadIdx.x * 16;
+  const uint32_t slot_scales = (uint32_t)__cvta_generic_to_shared(grad_smem) + S * T * R * CH * 16 + threadIdx.x * 4;
+  const long long row_bytes = VEC ? p.ld * (16 / V) : 0;
+  const char* from = VEC ? (const char*)p.X + (first < p.n_rows ? first : 0) * row_bytes : nullptr;  // the next rows to request
+  const float* from_scale = SCALED ? p.scales + (first < p.n_rows ? first : 0) * p.ld_s : nullptr;
+  long long left = p.n_rows - first;  // rows from there on
+  int bytes[CH], offset[CH];  // of unit j: bytes of the row, place in it (the row's start for units behind its end: nothing is read there)
+#pragma unroll
+  for (int j = 0; j < CH; ++j) {
+    const long long b = (p.d - (long long)(gl + j * G) * V) * (16 / V);
+    bytes[j] = b < 0 ? 0 : b > 16 ? 16 : (int)b;
+    offset[j] = b > 0 ? (gl + j * G) * 16 : 0;
+  }
+  auto request = [&](int slot) {
+    const char* row = from;
+    const float* row_scale = from_scale;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool yes = r < left;
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        const int at = (slot * R + r) * CH + j;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slots + at * (T * 16)), "l"(row + offset[j]), "r"(yes ? bytes[j] : 0) : "memory");
+        if constexpr (SCALED)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(slot_scales + at * (T * 4)), "l"(row_scale + offset[j] / Q_BLOCK), "r"(yes && bytes[j] ? 4 : 0) : "memory");
+      }
+      if (r + 1 < left) {  // never beyond the last row
+        row += row_bytes;
+        if constexpr (SCALED) row_scale += p.ld_s;
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (left > stride) {
+      from += stride * row_bytes;
+      if constexpr (SCALED) from_scale += stride * p.ld_s;
+    }
+    left -= stride;
+  };
+  // ---- else: rows through registers, the next R on their way
+  float next[VEC ? 1 : R][VEC ? 1 : E];
+  auto load = [&](long long row0) {
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < E; ++i) next[r][i] = row0 + r < p.n_rows && has(i) ? widen_scalar<RT>(((const RT*)p.X)[(row0 + r) * p.ld + column(i)]) : 0.0f;
+    }
+  };
+  if constexpr (VEC) {
+#pragma unroll 1
+    for (int i = 0; i < S - 1; ++i) request(i);
+  } else {
+    load(first);
+  }
+
+  uint64_t w[E / 2], acc[E / 2];
+#pragma unroll
+  for (int i = 0; i < E; i += 2) {
+    w[i / 2] = pair_of(__float_as_uint(has(i) ? p.w[column(i)] : 0.0f), __float_as_uint(has(i + 1) ? p.w[column(i + 1)] : 0.0f));
+    acc[i / 2] = 0;
+  }
+  const float w_norm = block_w_norm(p.w, p.d, cross64);
+  constexpr float terms = E + W + 8;  // additions a product takes part in: the thread's, 5 in the warp, W over the warps; 3 roundings for scales
+
+  // losses: their margins wait, a lane each, until the warp has a full set to evaluate side by side
+  double loss = 0.0;
+  float z_held = 0.0f, y_held = 0.0f;
+  int held = 0, wrong = 0;
+  auto evaluate = [&]() {
+    if (lane < held && y_held == y_held) loss += isnan(z_held) ? (double)z_held : loss_value(p.loss, y_held, z_held);
+    held = 0;
+  };
+
+  int round = 0, slot = 0;
+  const int own = l / (L / R);  // of the R rows, the one whose sums this lane ends with
+  float y_next = first + own < p.n_rows ? p.y[first + own] : 0.0f;
+  // groups within a warp go round together (shuffles over the warp)
+  for (long long row0 = first; L < 32 ? __any_sync(0xffffffffu, row0 < p.n_rows) : row0 < p.n_rows; row0 += stride, ++round) {
+    const bool in = row0 + own < p.n_rows;
+    const float y = y_next;
+    y_next = row0 + stride + own < p.n_rows ? p.y[row0 + stride + own] : 0.0f;
+    float plain[VEC ? 1 : R][VEC ? 1 : E];
+    const int cur = slot;
+    if constexpr (VEC) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
+      request(slot == 0 ? S - 1 : slot - 1);  // into the slot of one round ago
+      slot = slot == S - 1 ? 0 : slot + 1;
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < E; ++i) plain[r][i] = next[r][i];
+      load(row0 + stride);
+    }
+    // VEC: read from the slot both for the margin and for the gradient; widened values of all R rows would not fit the registers
+    auto values = [&](int r, int j, uint64_t (&x)[V / 2]) {
+      if constexpr (VEC) {
+        uint4 raw;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w) : "r"(slots + ((cur * R + r) * CH + j) * (T * 16)));
+        RowUnit<RT>::widen(raw, x);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) x[e] = pair_of(__float_as_uint(plain[r][j * V + 2 * e]), __float_as_uint(plain[r][j * V + 2 * e + 1]));
+      }
+    };
+    auto scale_of = [&](int r, int j) {
+      float v;
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(slot_scales + ((cur * R + r) * CH + j) * (T * 4)));
+      return v;
+    };
+
+    float z[R], xx[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      uint64_t z2 = 0, x2 = 0;
+      z[r] = xx[r] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        uint64_t x[V / 2];
+        values(r, j, x);
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) {
+          z2 = fma2(w[j * (V / 2) + e], x[e], z2);
+          if constexpr (!SCALED) x2 = fma2(x[e], x[e], x2);
+        }
+        if constexpr (SCALED) {
+          const float2 h = halves(z2);
+          const float scale = scale_of(r, j);
+          z[r] = fmaf(scale, h.x + h.y, z[r]);
+          xx[r] = fmaf(scale * (V * Q_MAX * Q_MAX), scale, xx[r]);  // a bound: no |q| is above 448
+          z2 = 0;
+        }
+      }
+      if constexpr (!SCALED) {
+        const float2 h = halves(z2), q = halves(x2);
+        z[r] = h.x + h.y;
+        xx[r] = q.x + q.y;
+      }
+    }
+    float zs = transpose_sum<R, L>(z, l), xs = transpose_sum<R, L>(xx, l);
+    if constexpr (W > 1) {  // every warp of the group adds up and goes on alike: one barrier a round
+      if (l % (L / R) == 0) cross[round & 1][warp][own] = make_float2(zs, xs);
+      group_barrier();
+      zs = xs = 0.0f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float2 c = cross[round & 1][group * W + i][own];
+        zs += c.x;
+        xs += c.y;
+      }
+    }
+    double zd = zs;
+    // the same in all lanes that hold the row, and in all warps of the group
+    const unsigned redo = __ballot_sync(0xffffffffu, in && near_jump(p.loss, y, zs, margin_error(terms, w_norm, xs)));
+    if (redo) {
+#pragma unroll 1
+      for (int r = 0; r < R; ++r) {
+        if (!__any_sync(0xffffffffu, own == r && (redo >> lane & 1))) continue;
+        double s = 0.0;  // this thread's columns once more, with exact products
+        if constexpr (VEC) {
+#pragma unroll
+          for (int j = 0; j < CH; ++j) {
+            uint64_t x[V / 2];
+            values(r, j, x);
+            const double scale = SCALED ? (double)scale_of(r, j) : 1.0;
+#pragma unroll
+            for (int e = 0; e < V / 2; ++e) {
+              const float2 xe = halves(x[e]), we = halves(w[j * (V / 2) + e]);
+              s += (double)we.x * (scale * (double)xe.x) + (double)we.y * (scale * (double)xe.y);
+            }
+          }
+        } else if (row0 + r < p.n_rows) {
+#pragma unroll
+          for (int i = 0; i < E; ++i)
+            if (has(i)) s += exact_product<RT>(p, row0 + r, column(i));
+        }
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if constexpr (W > 1) {
+          group_barrier();
+          if (lane == 0) cross64[warp] = s;
+          group_barrier();
+          s = 0.0;
+#pragma unroll 1
+          for (int i = 0; i < W; ++i) s += cross64[group * W + i];
+        }
+        if (own == r) zd = s;
+      }
+    }
+    const float g = in ? loss_derivative_f64(p.loss, y, zd) : 0.0f;
+    if (W == 1 || round % W == warp - group * W) {  // the warps of a group take turns with the losses
+      constexpr int N = R * (32 / L);               // rows of the warp; row i's margin is in lane i L / R
+      wrong += __popc(__ballot_sync(0xffffffffu, in && l % (L / R) == 0 && (zd >= 0.0) != (y >= 0.0f)));
+      if (held + N > 32) evaluate();
+      const float zv = __shfl_sync(0xffffffffu, (float)zd, (lane - held) * (L / R)), yv = __shfl_sync(0xffffffffu, in ? y : nanf(""), (lane - held) * (L / R));
+      if (lane >= held && lane < held + N) { z_held = zv; y_held = yv; }
+      held += N;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float gr = __shfl_sync(0xffffffffu, g, r * (L / R), L);
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        uint64_t x[V / 2];
+        values(r, j, x);
+        float gs = gr;
+        if constexpr (SCALED) gs *= scale_of(r, j);
+        const uint64_t g2 = pair_of(__float_as_uint(gs), __float_as_uint(gs));
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) acc[j * (V / 2) + e] = fma2(g2, x[e], acc[j * (V / 2) + e]);
+      }
+    }
+  }
+  evaluate();
+
+  loss = warp_sum_f64(loss);
+  if (lane == 0) { sums[0][warp] = loss; sums[1][warp] = wrong; }
+  auto own_sum = [&](int i) { return i % 2 ? halves(acc[i / 2]).y : halves(acc[i / 2]).x; };
+  float* fold = (float*)grad_smem;
+  if constexpr (VEC) asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();  // the slots are done with
+  if constexpr (Shape::groups > 1) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) fold[(i * Shape::groups + group) * G + gl] = own_sum(i);
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    double t = 0.0;
+    for (int i = 0; i < T / 32; ++i) t += sums[threadIdx.x][i];
+    p.sums[2 * blockIdx.x + threadIdx.x] = t;
+  }
+  float* to = p.part + (long long)blockIdx.x * p.d;
+  if constexpr (Shape::groups > 1) {
+    for (int c = threadIdx.x; c < E * G; c += T) {  // element c / G of thread c % G of every group
+      const int i = c / G, t = c % G;
+      const int col = VEC ? (t + i / V * G) * V + i % V : t + i * G;
+      if (col < p.d) {
+        float s = 0.0f;
+#pragma unroll
+        for (int g = 0; g < Shape::groups; ++g) s += fold[(i * Shape::groups + g) * G + t];
+        to[col] = s;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (has(i)) to[column(i)] = own_sum(i);
+  }
 }
 
 // grad = lambda w + (sum of the partial gradients) / n, and the measures. A block owns 32 columns, its warps split the partials; the warps'

@@ -42,6 +42,12 @@ wpsgd_status rows_workspace(wpsgd_ctx* c) {
   return WPSGD_OK;
 }
 
+// More than 48 KB of shared memory for a kernel whose launches all have the same size.
+template <typename Kernel>
+cudaError_t allow_smem(Kernel kern, int bytes) {
+  return bytes > 48 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
+}
+
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
@@ -148,6 +154,41 @@ wpsgd_status gradient_any_width(wpsgd_ctx* c, GradParams p, int* parts, int* n_s
   return WPSGD_OK;
 }
 
+// One pass with G threads per row and CH units per thread; false: the rows are wider.
+template <typename RT, bool VEC, int G, int CH, int R>
+wpsgd_status gradient_one_pass(wpsgd_ctx* c, const GradParams& p, int* parts) {
+  using Shape = GradShape<RT, VEC, G, CH, R>;
+  const long long batches = (p.n_rows + R - 1) / R, blocks = (batches + Shape::groups - 1) / Shape::groups;
+  *parts = (int)std::min<long long>({blocks, (long long)RowsLayout(c->d).parts, 148ll * Shape::per_sm});
+  static_assert(Shape::smem + 8192 <= (int)kSmemMax / Shape::per_sm, "the slots of the blocks of an SM must fit");
+  CU_TRY(c, allow_smem(gradient_rows_kernel<RT, VEC, G, CH, R>, Shape::smem));
+  CU_TRY(c, launch(gradient_rows_kernel<RT, VEC, G, CH, R>, *parts, Shape::threads, Shape::smem, c->stream, p));
+  c->launches++;
+  return WPSGD_OK;
+}
+template <typename RT, bool VEC>
+wpsgd_status gradient_by_width(wpsgd_ctx* c, const GradParams& p, int* parts, int* n_sums) {
+  constexpr int V = RowUnit<RT>::V, R = V == 16 || (V == 8 && !VEC) ? 4 : 8;
+  const long long units = (p.d + V - 1) / V;
+  auto run = [&](auto g, auto ch, auto r) {
+    const wpsgd_status s = gradient_one_pass<RT, VEC, decltype(g)::value, decltype(ch)::value, decltype(r)::value>(c, p, parts);
+    *n_sums = *parts;
+    return s;
+  };
+#define GRAD_RUN(G, CH, R_) run(std::integral_constant<int, G>(), std::integral_constant<int, CH>(), std::integral_constant<int, R_>())
+  if (units <= 4) return GRAD_RUN(4, 1, 4);
+  if (units <= 8) return GRAD_RUN(8, 1, R);
+  if (units <= 16) return GRAD_RUN(16, 1, R);
+  if (units <= 32) return GRAD_RUN(32, 1, R);
+  if (units <= 64) return GRAD_RUN(64, 1, R);
+  if (units <= 128) return GRAD_RUN(128, 1, R);
+  if (units <= 256) return GRAD_RUN(256, 1, R);
+  if (units <= 512) return GRAD_RUN(256, 2, R / 2);
+  if (units <= 1024) return GRAD_RUN(512, 2, R / 2);
+#undef GRAD_RUN
+  return gradient_any_width<RT>(c, p, parts, n_sums);
+}
+
 template <typename RT>
 wpsgd_status gradient(wpsgd_ctx* c, GradParams p, float lambda, float* grad, float* out) {
   wpsgd_status s = rows_workspace(c);
@@ -157,7 +198,9 @@ wpsgd_status gradient(wpsgd_ctx* c, GradParams p, float lambda, float* grad, flo
   p.part = (float*)((char*)c->rows_ws + lay.part);
   int parts = 0, n_sums = 0;
   if (p.n_rows > 0) {
-    s = gradient_any_width<RT>(c, p, &parts, &n_sums);
+    const bool vec = std::is_same<RT, Row8>::value || (aligned16(p.X) && p.ld % RowUnit<RT>::V == 0);
+    if constexpr (std::is_same<RT, Row8>::value) s = gradient_by_width<RT, true>(c, p, &parts, &n_sums);
+    else s = vec ? gradient_by_width<RT, true>(c, p, &parts, &n_sums) : gradient_by_width<RT, false>(c, p, &parts, &n_sums);
     if (s != WPSGD_OK) return s;
   }
   launch(gradient_finish_kernel, (unsigned)((p.d + 31) / 32), 32 * GRAD_FINISH_WARPS, 0, c->stream, p.part, parts, p.sums, n_sums, p.w, p.d, p.n_rows, lambda, grad, out);
