@@ -244,6 +244,8 @@ class Context:
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
         self._stream = stream  # keep alive
+        self._torch, self._torch_device, self._raw_stream = torch, torch.device("cuda", self.device), stream.cuda_stream
+        self._current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
         self.k, self.d = int(k), int(d)
         h = ctypes.c_void_p()
         st = self._lib.wpsgd_create(self.device, ctypes.c_void_p(stream.cuda_stream), self.k, self.d, ctypes.byref(h))
@@ -439,33 +441,40 @@ class Context:
         return out
 
     # -- operators on whole sets of rows ------------------------------------------------------------------
+    # (calls of a few microseconds: sizes are asked one by one and pointers passed as numbers, which costs less than tuples and
+    # ctypes objects)
     def _empty(self, shape, dtype):
         """A tensor for the context's stream to write: allocated for that stream, so that its memory is not reused under it."""
-        import torch
-
-        dev = torch.device("cuda", self.device)
-        if torch.cuda.current_stream(dev) == self._stream:
-            return torch.empty(shape, dtype=dtype, device=dev)
+        torch = self._torch
+        if self._current_raw_stream(self.device) == self._raw_stream:
+            return torch.empty(shape, dtype=dtype, device=self._torch_device)
         with torch.cuda.stream(self._stream):
-            return torch.empty(shape, dtype=dtype, device=dev)
+            return torch.empty(shape, dtype=dtype, device=self._torch_device)
 
     def _matrix(self, t, dtypes, cols, what):
-        """Pointer, row stride and row count of a 2-D tensor with `cols` columns and contiguous rows on the context's device."""
-        import torch
-
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != self.device:
+        """Pointer, row stride (None: a single row) and row count of a 2-D tensor of rows of `cols` contiguous elements."""
+        if not isinstance(t, self._torch.Tensor) or t.get_device() != self.device:
             raise TypeError(f"{what}: expected a CUDA tensor on the context's device")
         if t.dtype not in dtypes:
             raise TypeError(f"{what}: expected dtype {' or '.join(map(str, dtypes))}, got {t.dtype}")
-        if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        if t.dim() != 2 or t.size(1) != cols or (cols > 1 and t.stride(1) != 1):
             raise ValueError(f"{what}: expected rows of {cols} contiguous elements, got shape {tuple(t.shape)} with strides {t.stride()}")
-        n = t.shape[0]
-        return ctypes.c_void_p(t.data_ptr()), t.stride(0) if n > 1 else None, n
+        n = t.size(0)
+        return t.data_ptr(), t.stride(0) if n > 1 else None, n
+
+    def _vector(self, t, n, what):
+        """Pointer of a contiguous fp32 tensor of at least n elements."""
+        if not isinstance(t, self._torch.Tensor) or t.get_device() != self.device:
+            raise TypeError(f"{what}: expected a CUDA tensor on the context's device")
+        if t.dtype is not self._torch.float32 or not t.is_contiguous():
+            raise TypeError(f"{what}: expected a contiguous float32 tensor")
+        if t.numel() < n:
+            raise ValueError(f"{what}: {t.numel()} elements, expected {n}")
+        return t.data_ptr()
 
     def _packed(self, q, scales, what):
         """Arguments of packed rows: pointer, stride, scales, their stride, row count."""
-        import torch
-
+        torch = self._torch
         qp, ld, n = self._matrix(q, (torch.float8_e4m3fn, torch.uint8), self.d, what)
         nb = (self.d + 127) // 128
         sp, ld_s, m = self._matrix(scales, (torch.float32,), nb, what + " scales")
@@ -475,23 +484,25 @@ class Context:
 
     def quantize_rows(self, X, out=None, scales=None):
         """Rows packed to 8 bits: (e4m3 [n, d] with rows that start on 16 bytes, fp32 scales [n, ceil(d / 128)])."""
-        import torch
-
+        torch = self._torch
         xp, ld, n = self._matrix(X, (torch.float32, torch.bfloat16), self.d, "X")
         if out is None:
-            out = self._empty((n, packed_width(self.d)), torch.float8_e4m3fn)[:, :self.d]
+            out = self._empty((n, packed_width(self.d)), torch.float8_e4m3fn)
+            if out.size(1) != self.d:
+                out = out[:, :self.d]
         if scales is None:
             scales = self._empty((n, (self.d + 127) // 128), torch.float32)
         qp, ld_q, sp, ld_s, m = self._packed(out, scales, "out")
         if m != n:
             raise ValueError(f"out has {m} rows, X {n}")
-        self._ck(self._lib.wpsgd_quantize_rows(self._h, xp, _xtype(X), self.d if ld is None else ld, n, qp, ld_q, sp, ld_s), "wpsgd_quantize_rows")
+        st = self._lib.wpsgd_quantize_rows(self._h, xp, X_BF16 if X.dtype is torch.bfloat16 else X_F32, self.d if ld is None else ld, n, qp, ld_q, sp, ld_s)
+        if st:
+            self._ck(st, "wpsgd_quantize_rows")
         return out, scales
 
     def margins_fp8(self, Q, q_scales, M, m_scales, out=None, dtype=None):
         """Margins [n, models] of packed models M on packed rows Q, float32 (or `dtype`: bfloat16)."""
-        import torch
-
+        torch = self._torch
         qp, ld_q, qs, ld_qs, n = self._packed(Q, q_scales, "Q")
         mp, ld_m, ms, ld_ms, k = self._packed(M, m_scales, "M")
         if out is None:
@@ -501,35 +512,36 @@ class Context:
         zp, ld_z, rows = self._matrix(out, (torch.float32, torch.bfloat16), k, "out")
         if rows != n:
             raise ValueError(f"out has {rows} rows, Q {n}")
-        self._ck(self._lib.wpsgd_margins_fp8(self._h, qp, ld_q, qs, ld_qs, n, mp, ld_m, ms, ld_ms, k, zp, _xtype(out), k if ld_z is None else ld_z),
-                 "wpsgd_margins_fp8")
+        st = self._lib.wpsgd_margins_fp8(self._h, qp, ld_q, qs, ld_qs, n, mp, ld_m, ms, ld_ms, k, zp, X_BF16 if out.dtype is torch.bfloat16 else X_F32,
+                                         k if ld_z is None else ld_z)
+        if st:
+            self._ck(st, "wpsgd_margins_fp8")
         return out
 
     def _grad_outputs(self, grad, out):
-        import torch
-
-        grad = self._empty((self.d,), torch.float32) if grad is None else grad
-        out = self._empty((2,), torch.float32) if out is None else out
-        return grad, self._dev(grad, torch.float32, self.d), out, self._dev(out, torch.float32, 2)
+        f32 = self._torch.float32
+        grad = self._empty((self.d,), f32) if grad is None else grad
+        out = self._empty((2,), f32) if out is None else out
+        return grad, self._vector(grad, self.d, "grad"), out, self._vector(out, 2, "out")
 
     def objective_grad(self, X, y, w, lam: float, loss: int, grad=None, out=None):
         """(fp32 [2] = {objective, error}, fp32 [d] = its gradient) over all rows of X."""
-        import torch
-
+        torch = self._torch
         xp, ld, n = self._matrix(X, (torch.float32, torch.bfloat16), self.d, "X")
         grad, gp, out, op = self._grad_outputs(grad, out)
-        self._ck(self._lib.wpsgd_objective_grad(self._h, xp, _xtype(X), self.d if ld is None else ld, self._dev(y, torch.float32, n), n,
-                                                self._dev(w, torch.float32, self.d), lam, loss, gp, op), "wpsgd_objective_grad")
+        st = self._lib.wpsgd_objective_grad(self._h, xp, X_BF16 if X.dtype is torch.bfloat16 else X_F32, self.d if ld is None else ld,
+                                            self._vector(y, n, "y"), n, self._vector(w, self.d, "w"), lam, loss, gp, op)
+        if st:
+            self._ck(st, "wpsgd_objective_grad")
         return out, grad
 
     def objective_grad_fp8(self, Q, scales, y, w, lam: float, loss: int, grad=None, out=None):
         """objective_grad over packed rows."""
-        import torch
-
         qp, ld_q, sp, ld_s, n = self._packed(Q, scales, "Q")
         grad, gp, out, op = self._grad_outputs(grad, out)
-        self._ck(self._lib.wpsgd_objective_grad_fp8(self._h, qp, ld_q, sp, ld_s, self._dev(y, torch.float32, n), n, self._dev(w, torch.float32, self.d),
-                                                    lam, loss, gp, op), "wpsgd_objective_grad_fp8")
+        st = self._lib.wpsgd_objective_grad_fp8(self._h, qp, ld_q, sp, ld_s, self._vector(y, n, "y"), n, self._vector(w, self.d, "w"), lam, loss, gp, op)
+        if st:
+            self._ck(st, "wpsgd_objective_grad_fp8")
         return out, grad
 
     def _grad_list(self, grads):
@@ -541,21 +553,21 @@ class Context:
 
     def grad_norm(self, grads, norm=None):
         """fp32 [1]: the global norm of the gradients (a GradList or a sequence of tensors)."""
-        import torch
-
         grads = self._grad_list(grads)
-        norm = self._empty((1,), torch.float32) if norm is None else norm
-        self._ck(self._lib.wpsgd_grad_norm(self._h, grads._h, self._dev(norm, torch.float32, 1)), "wpsgd_grad_norm")
+        norm = self._empty((1,), self._torch.float32) if norm is None else norm
+        st = self._lib.wpsgd_grad_norm(self._h, grads._h, self._vector(norm, 1, "norm"))
+        if st:
+            self._ck(st, "wpsgd_grad_norm")
         return norm
 
     def clip_grad_norm(self, grads, max_norm: float, norm=None):
         """Scales the gradients down to max_norm where their global norm is above it, in place or into the list's outputs;
         returns the norm before, fp32 [1]."""
-        import torch
-
         grads = self._grad_list(grads)
-        norm = self._empty((1,), torch.float32) if norm is None else norm
-        self._ck(self._lib.wpsgd_clip_grad_norm(self._h, grads._h, max_norm, self._dev(norm, torch.float32, 1)), "wpsgd_clip_grad_norm")
+        norm = self._empty((1,), self._torch.float32) if norm is None else norm
+        st = self._lib.wpsgd_clip_grad_norm(self._h, grads._h, max_norm, self._vector(norm, 1, "norm"))
+        if st:
+            self._ck(st, "wpsgd_clip_grad_norm")
         return norm
 
     def solve_host(self, X, y, shard_off, n_steps, eta0, sched, lam, loss, seed, w0=None, r: float = 0.0, out=None):

@@ -107,11 +107,22 @@ __device__ __forceinline__ bool near_jump(int loss, float y, float z, float err)
   if (fabsf(z) < err) return true;
   return loss == LOSS_HINGE && fabsf(1.0f - y * z) < fmaf(fabsf(y), err, 0x1p-22f);
 }
-// A margin that is not a number gives a derivative and a loss that are none, whatever the loss.
-__device__ __forceinline__ float loss_derivative_f64(int loss, float y, double z) {
-  if (isnan(z)) return (float)z;
-  if (loss == LOSS_HINGE) return (double)y * z < 1.0 ? -y : 0.0f;
-  return loss_derivative(loss, y, (float)z);
+// A margin or label that is not a number gives a derivative and a loss that are none, whatever the loss.
+__device__ __forceinline__ double loss_of(int loss, float y, double z) {
+  return isnan(z + (double)y) ? z + (double)y : loss_value(loss, y, z);
+}
+// L' of a row whose margin no rounding can move across a jump
+__device__ __forceinline__ float row_derivative(int loss, float y, float z) {
+  const float t = y * z;
+  if (loss == LOSS_HINGE) return t < 1.0f ? -y : t >= 1.0f ? 0.0f : t;
+  if (loss == LOSS_LOGISTIC) return __fdividef(-y, 1.0f + expf(t));  // off by 2^-22 at most, and 0 instead of values below 2^-126
+  return z - y;
+}
+// and by the margin in fp64
+__device__ __forceinline__ float row_derivative(int loss, float y, double z) {
+  if (loss != LOSS_HINGE) return row_derivative(loss, y, (float)z);
+  const double t = (double)y * z;
+  return t < 1.0 ? -y : t >= 1.0 ? 0.0f : (float)t;
 }
 
 // |w| by a block, to every thread (any block size of whole warps up to 512)
@@ -158,8 +169,8 @@ __global__ void __launch_bounds__(GRAD_THREADS) gradient_margins_kernel(const Gr
       zd = warp_sum_f64(zd);
     }
     if (lane == 0) {
-      coef[i] = loss_derivative_f64(p.loss, y, zd);
-      loss += isnan(zd) ? zd : loss_value(p.loss, y, zd);
+      coef[i] = row_derivative(p.loss, y, zd);
+      loss += loss_of(p.loss, y, zd);
       wrong += (zd >= 0.0) != (y >= 0.0f) ? 1.0 : 0.0;
     }
   }
@@ -322,8 +333,9 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
   double loss = 0.0;
   float z_held = 0.0f, y_held = 0.0f;
   int held = 0, wrong = 0;
+  bool in_held = false;
   auto evaluate = [&]() {
-    if (lane < held && y_held == y_held) loss += isnan(z_held) ? (double)z_held : loss_value(p.loss, y_held, z_held);
+    if (lane < held && in_held) loss += loss_of(p.loss, y_held, z_held);
     held = 0;
   };
 
@@ -405,7 +417,8 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
         xs += c.y;
       }
     }
-    double zd = zs;
+    float g = in ? row_derivative(p.loss, y, zs) : 0.0f;
+    bool positive = zs >= 0.0f;
     // the same in all lanes that hold the row, and in all warps of the group
     const unsigned redo = __ballot_sync(0xffffffffu, in && near_jump(p.loss, y, zs, margin_error(terms, w_norm, xs)));
     if (redo) {
@@ -440,16 +453,21 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
 #pragma unroll 1
           for (int i = 0; i < W; ++i) s += cross64[group * W + i];
         }
-        if (own == r) zd = s;
+        if (own == r && in) {
+          g = row_derivative(p.loss, y, s);
+          positive = s >= 0.0;
+          zs = (float)s;
+        }
       }
     }
-    const float g = in ? loss_derivative_f64(p.loss, y, zd) : 0.0f;
     if (W == 1 || round % W == warp - group * W) {  // the warps of a group take turns with the losses
       constexpr int N = R * (32 / L);               // rows of the warp; row i's margin is in lane i L / R
-      wrong += __popc(__ballot_sync(0xffffffffu, in && l % (L / R) == 0 && (zd >= 0.0) != (y >= 0.0f)));
+      wrong += __popc(__ballot_sync(0xffffffffu, in && l % (L / R) == 0 && positive != (y >= 0.0f)));
       if (held + N > 32) evaluate();
-      const float zv = __shfl_sync(0xffffffffu, (float)zd, (lane - held) * (L / R)), yv = __shfl_sync(0xffffffffu, in ? y : nanf(""), (lane - held) * (L / R));
-      if (lane >= held && lane < held + N) { z_held = zv; y_held = yv; }
+      const int from_lane = (lane - held) * (L / R) & 31;
+      const float zv = __shfl_sync(0xffffffffu, zs, from_lane), yv = __shfl_sync(0xffffffffu, y, from_lane);
+      const unsigned inside = __ballot_sync(0xffffffffu, in);
+      if (lane >= held && lane < held + N) { z_held = zv; y_held = yv; in_held = inside >> from_lane & 1; }
       held += N;
     }
 #pragma unroll

@@ -1,5 +1,6 @@
 // C ABI of the operators on whole sets of rows (see include/wpsgd.h): 8-bit rows, margins of many models, the objective with its
 // gradient, norm and clipping of gradients. Argument checks, workspaces, choice of kernels, launches.
+#include <atomic>
 #include <cmath>
 #include <memory>
 #include <new>
@@ -42,10 +43,17 @@ wpsgd_status rows_workspace(wpsgd_ctx* c) {
   return WPSGD_OK;
 }
 
-// More than 48 KB of shared memory for a kernel whose launches all have the same size.
-template <typename Kernel>
-cudaError_t allow_smem(Kernel kern, int bytes) {
-  return bytes > 48 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
+// All of an SM's shared memory for a kernel (see allow_all_smem), asked for once per device: the call takes part of a microsecond.
+template <auto Kernel>
+cudaError_t allow_smem(const wpsgd_ctx* c) {
+  static std::atomic<uint64_t> done{0};  // a bit per device
+  const uint64_t bit = c->device < 64 ? 1ull << c->device : 0;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  cudaFuncAttributes at;
+  cudaError_t e = cudaFuncGetAttributes(&at, Kernel);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmemMax - at.sharedSizeBytes));
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
@@ -109,7 +117,7 @@ wpsgd_status launch_margins(wpsgd_ctx* c, const MarginsCall& call) {
   const long long tiles = (long long)((p.n_rows + MG_ROWS - 1) / MG_ROWS) * p.tiles_m;
   if (tiles > INT32_MAX - 148 || tiles / 148 * p.blocks > INT32_MAX) return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: too many tiles");
   p.tiles = (int)tiles;
-  CU_TRY(c, allow_all_smem(margins_kernel<OT, BN>));
+  CU_TRY(c, (allow_smem<margins_kernel<OT, BN>>(c)));
   CU_TRY(c, launch(margins_kernel<OT, BN>, (unsigned)std::min<long long>(tiles, 148), Shape::threads, Shape::smem, c->stream, map_q, map_m, p));
   c->launches++;
   return WPSGD_OK;
@@ -161,7 +169,7 @@ wpsgd_status gradient_one_pass(wpsgd_ctx* c, const GradParams& p, int* parts) {
   const long long batches = (p.n_rows + R - 1) / R, blocks = (batches + Shape::groups - 1) / Shape::groups;
   *parts = (int)std::min<long long>({blocks, (long long)RowsLayout(c->d).parts, 148ll * Shape::per_sm});
   static_assert(Shape::smem + 8192 <= (int)kSmemMax / Shape::per_sm, "the slots of the blocks of an SM must fit");
-  CU_TRY(c, allow_smem(gradient_rows_kernel<RT, VEC, G, CH, R>, Shape::smem));
+  CU_TRY(c, (allow_smem<gradient_rows_kernel<RT, VEC, G, CH, R>>(c)));
   CU_TRY(c, launch(gradient_rows_kernel<RT, VEC, G, CH, R>, *parts, Shape::threads, Shape::smem, c->stream, p));
   c->launches++;
   return WPSGD_OK;

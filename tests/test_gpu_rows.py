@@ -243,7 +243,7 @@ def problem(n, d, loss, seed=0):
     return x, y, 0.8 * w + 0.2 * normal((d,), seed + 5)
 
 
-SHAPES = [(1, 1), (1, 4096), (3, 5), (40, 64), (257, 100), (1000, 256), (333, 999), (64, 1024), (130, 4096), (50, 8192), (20, 16384),
+SHAPES = [(1, 1), (1, 4096), (3, 5), (300, 8), (90, 72), (1200, 520), (600, 2056), (40, 64), (257, 100), (1000, 256), (333, 999), (64, 1024), (130, 4096), (50, 8192), (20, 16384),
           (9, 20000), (70, 132), (2000, 16), (515, 40)]
 
 
@@ -340,6 +340,24 @@ def test_gradient_of_values_that_are_not_finite(P, loss):
         out, grad = ctx.objective_grad(x.cuda(), y.cuda(), w.cuda(), 0.01, loss)
         ctx.check()
     assert math.isnan(float(out[0])) and bool(torch.isnan(grad).all())   # the row's margin is none, so its derivative is none
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "two passes"])
+@pytest.mark.parametrize("loss", [HINGE, LOGISTIC, SQUARED])
+def test_gradient_with_a_label_or_a_row_that_is_not_a_number(P, loss, kind):
+    d = 40000 if kind == "two passes" else 200
+    x, y, w = problem(30, d, loss)
+    x = x.to(torch.bfloat16) if kind == "bf16" else x
+    for at in ("label", "row"):
+        xb, yb = x.clone(), y.clone()
+        if at == "label":
+            yb[11] = float("nan")
+        else:
+            xb[29, d - 1] = float("nan")
+        with P.Context(1, d) as ctx:
+            out, grad = ctx.objective_grad(xb.cuda(), yb.cuda(), w.cuda(), 0.01, loss)
+            ctx.check()
+        assert math.isnan(float(out[0])) and bool(torch.isnan(grad).all())
 
 
 @pytest.mark.parametrize("loss", [LOGISTIC, SQUARED])
