@@ -1,7 +1,7 @@
 // Global norm of a list of gradients and clipping:  N = sqrt(sum over all tensors and elements of g^2),
 // out = g * f with f = max_norm / N where N > max_norm, else 1.
 //
-// Two launches: block sums of g^2, then the scaled copies, each block of which adds the block sums up again in the same order (so
+// Two launches (short lists: one, clip_small_kernel): block sums of g^2, then the scaled copies, each block of which adds the block sums up again in the same order (so
 // no result depends on timing, and no block waits for another). The list travels as a kernel argument: nothing is copied before
 // the launch and nothing is kept after it.
 // Sums: the squares of a batch of 16-byte units in fp32, the batches in fp64. Where a batch's sum leaves the range in which fp32
@@ -229,6 +229,44 @@ __global__ void __launch_bounds__(CLIP_THREADS) scale_kernel(const __grid_consta
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   const bool clips = norm > max_norm;
   if (!clips && in_place) return;  // times 1
+  const float f = clips ? (float)(max_norm / norm) : 1.0f;
+  for_own_chunks(list, true, [&](int i, int chunk) {
+    const long long n = list.elems_type[i] >> 1;
+    if (list.elems_type[i] & 1) chunk_scale((const __nv_bfloat16*)list.src[i], (__nv_bfloat16*)list.dst[i], n, chunk, f);
+    else chunk_scale((const float*)list.src[i], (float*)list.dst[i], n, chunk, f);
+  });
+}
+
+// Both steps of a short list in one launch: a cluster of blocks that give each other their sums through distributed shared memory.
+// 16 tensors of 1024 fp32 elements: 5.0 us a call with two launches, 3.3 with one.
+constexpr int CLIP_CLUSTER = 8;
+constexpr int CLIP_SMALL_CHUNKS = 2 * CLIP_CLUSTER;
+template <int N>
+__global__ void __cluster_dims__(CLIP_CLUSTER, 1, 1) __launch_bounds__(CLIP_THREADS)
+clip_small_kernel(const __grid_constant__ TensorList<N> list, bool scale, double max_norm, bool in_place, float* __restrict__ norm_out) {
+  __shared__ double sh[CLIP_THREADS / 32];
+  __shared__ double sums[CLIP_CLUSTER];
+  kernel_started();
+  kernel_inputs_ready();
+  double sum = 0.0;
+  for_own_chunks(list, false, [&](int i, int chunk) {
+    const long long n = list.elems_type[i] >> 1;
+    sum += list.elems_type[i] & 1 ? chunk_squares((const __nv_bfloat16*)list.src[i], n, chunk) : chunk_squares((const float*)list.src[i], n, chunk);
+  });
+  sum = block_sum_f64(sum, sh);
+  if (threadIdx.x < CLIP_CLUSTER) {
+    uint32_t to;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(sums + blockIdx.x)), "r"(threadIdx.x));
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(sum) : "memory");
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  double all = 0.0;
+#pragma unroll
+  for (int i = 0; i < CLIP_CLUSTER; ++i) all += sums[i];
+  const double norm = sqrt(all);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+  const bool clips = norm > max_norm;
+  if (!scale || (!clips && in_place)) return;
   const float f = clips ? (float)(max_norm / norm) : 1.0f;
   for_own_chunks(list, true, [&](int i, int chunk) {
     const long long n = list.elems_type[i] >> 1;

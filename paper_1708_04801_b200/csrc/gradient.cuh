@@ -20,6 +20,7 @@
 
 #include <cuda_fp8.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "common.cuh"
@@ -29,6 +30,7 @@ namespace wpsgd {
 
 constexpr int GRAD_THREADS = 256;
 constexpr int GRAD_FINISH_WARPS = 16;
+constexpr int GRAD_LAST_BLOCK = 8192;  // up to so many elements of partial gradients, the block that finishes last adds them up
 
 struct GradParams {
   const void* X;
@@ -39,8 +41,12 @@ struct GradParams {
   const float* w;
   long long n_rows, d;
   int loss;
+  float lambda;
+  float* grad;           // [d]
+  float* out;            // [2]
   float* part;           // [blocks, d] partial gradients
   double* sums;          // [blocks, 2] losses and errors
+  unsigned* ticket;      // blocks that have finished (zero between launches); null: gradient_finish_kernel follows
 };
 
 // 16 bytes of a row, widened to pairs
@@ -136,6 +142,51 @@ __device__ __forceinline__ float block_w_norm(const float* __restrict__ w, long 
   for (int i = 0; i < (int)blockDim.x / 32; ++i) t += sh[i];
   __syncthreads();
   return (float)sqrt(t) * 1.0001f;
+}
+
+// grad = lambda w + (sum of the partial gradients) / n for columns 32 slab and on, and for slab 0 the measures. The block's warps split
+// the partials, the warps' sums are added in warp order: the same result whichever block does it.
+template <int WARPS>
+__device__ __forceinline__ void gradient_finish(const GradParams& p, int parts, int n_sums, int slab, double (*sh)[33]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long c = (long long)slab * 32 + lane;
+  double t = 0.0;
+  if (c < p.d) {
+#pragma unroll 8
+    for (int i = warp; i < parts; i += WARPS) t += (double)__ldcg(p.part + (long long)i * p.d + c);
+  }
+  __syncthreads();
+  sh[warp][lane] = t;
+  __syncthreads();
+  const double n = p.n_rows > 0 ? (double)p.n_rows : 1.0;
+  if (warp == 0 && c < p.d) {
+    t = 0.0;
+    for (int i = 0; i < WARPS; ++i) t += sh[i][lane];
+    p.grad[c] = (float)fma((double)p.lambda, (double)p.w[c], t / n);
+  }
+  if (slab != 0) return;
+  __syncthreads();
+  double ww = 0.0, loss = 0.0, wrong = 0.0;
+  for (long long i = threadIdx.x; i < p.d; i += 32 * WARPS) ww = fma((double)p.w[i], (double)p.w[i], ww);
+  for (int i = threadIdx.x; i < n_sums; i += 32 * WARPS) {
+    loss += __ldcg(p.sums + 2 * i);
+    wrong += __ldcg(p.sums + 2 * i + 1);
+  }
+  ww = warp_sum_f64(ww); loss = warp_sum_f64(loss); wrong = warp_sum_f64(wrong);
+  if (lane == 0) { sh[warp][0] = ww; sh[warp][1] = loss; sh[warp][2] = wrong; }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    ww = loss = wrong = 0.0;
+    for (int i = 0; i < WARPS; ++i) { ww += sh[i][0]; loss += sh[i][1]; wrong += sh[i][2]; }
+    p.out[0] = (float)(0.5 * (double)p.lambda * ww + loss / n);
+    p.out[1] = (float)(wrong / n);
+  }
+}
+__global__ void __launch_bounds__(32 * GRAD_FINISH_WARPS) gradient_finish_kernel(const __grid_constant__ GradParams p, int parts, int n_sums) {
+  __shared__ double sh[GRAD_FINISH_WARPS][33];
+  kernel_started();
+  kernel_inputs_ready();
+  gradient_finish<GRAD_FINISH_WARPS>(p, parts, n_sums, blockIdx.x, sh);
 }
 
 // ---- rows of any width: two passes ---------------------------------------------------------------------------------------
@@ -237,7 +288,8 @@ struct GradShape {
   static constexpr int slot_bytes = threads * R * CH * (scaled ? 20 : 16);
   static constexpr int slots = VEC ? 96 * 1024 * 2 / per_sm / slot_bytes : 0;
   static constexpr int fold_bytes = groups > 1 ? threads * CH * V * 4 : 0;
-  static constexpr int smem = slots * slot_bytes > fold_bytes ? slots * slot_bytes : fold_bytes;
+  static constexpr int finish_bytes = threads / 32 * 33 * 8;
+  static constexpr int smem = std::max({slots * slot_bytes, fold_bytes, finish_bytes});
 };
 
 template <typename RT, bool VEC, int G, int CH, int R>
@@ -520,48 +572,18 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
     for (int i = 0; i < E; ++i)
       if (has(i)) to[column(i)] = own_sum(i);
   }
-}
-
-// grad = lambda w + (sum of the partial gradients) / n, and the measures. A block owns 32 columns, its warps split the partials; the warps'
-// sums are added in warp order. Block 0 also forms |w|^2 and adds up the blocks' losses and errors.
-__global__ void __launch_bounds__(32 * GRAD_FINISH_WARPS) gradient_finish_kernel(const float* __restrict__ part, int parts, const double* __restrict__ sums, int n_sums,
-                                                                                 const float* __restrict__ w, long long d, long long n_rows, float lambda,
-                                                                                 float* __restrict__ grad, float* __restrict__ out) {
-  __shared__ double sh[GRAD_FINISH_WARPS][33];
-  kernel_started();
-  kernel_inputs_ready();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long c = (long long)blockIdx.x * 32 + lane;
-  double t = 0.0;
-  if (c < d) {
-#pragma unroll 4
-    for (int i = warp; i < parts; i += GRAD_FINISH_WARPS) t += (double)__ldcg(part + (long long)i * d + c);
-  }
-  sh[warp][lane] = t;
-  __syncthreads();
-  const double n = n_rows > 0 ? (double)n_rows : 1.0;
-  if (warp == 0 && c < d) {
-    t = 0.0;
-    for (int i = 0; i < GRAD_FINISH_WARPS; ++i) t += sh[i][lane];
-    grad[c] = (float)fma((double)lambda, (double)w[c], t / n);
-  }
-  if (blockIdx.x != 0) return;
-  __syncthreads();
-  double ww = 0.0, loss = 0.0, wrong = 0.0;
-  for (long long i = threadIdx.x; i < d; i += 32 * GRAD_FINISH_WARPS) ww = fma((double)w[i], (double)w[i], ww);
-  for (int i = threadIdx.x; i < n_sums; i += 32 * GRAD_FINISH_WARPS) {
-    loss += __ldcg(sums + 2 * i);
-    wrong += __ldcg(sums + 2 * i + 1);
-  }
-  ww = warp_sum_f64(ww); loss = warp_sum_f64(loss); wrong = warp_sum_f64(wrong);
-  if (lane == 0) { sh[warp][0] = ww; sh[warp][1] = loss; sh[warp][2] = wrong; }
+  if (!p.ticket) return;
+  __shared__ bool last;
+  __threadfence();
   __syncthreads();
   if (threadIdx.x == 0) {
-    ww = loss = wrong = 0.0;
-    for (int i = 0; i < GRAD_FINISH_WARPS; ++i) { ww += sh[i][0]; loss += sh[i][1]; wrong += sh[i][2]; }
-    out[0] = (float)(0.5 * (double)lambda * ww + loss / n);
-    out[1] = (float)(wrong / n);
+    last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+    if (last) *p.ticket = 0u;
   }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  for (int slab = 0; slab * 32 < p.d; ++slab) gradient_finish<T / 32>(p, gridDim.x, gridDim.x, slab, (double (*)[33])grad_smem);
 }
 
 }  // namespace wpsgd

@@ -24,10 +24,11 @@ constexpr int kGradParts = 148 * 2;             // partial gradients at most
 constexpr long long kCoefRows = 1 << 16;        // rows per step of the two-pass gradient
 struct RowsLayout {
   int parts;
-  size_t sums, coef, part, total;
+  size_t ticket, sums, coef, part, total;
   explicit RowsLayout(long long d) {
     parts = (int)std::max(1ll, std::min<long long>(kGradParts, (1ll << 23) / d));
-    sums = 0;
+    ticket = 0;
+    sums = 256;
     coef = sums + kMaxBlocks * 2 * sizeof(double);
     part = coef + kCoefRows * sizeof(float);
     total = part + (size_t)parts * (size_t)d * sizeof(float);
@@ -39,7 +40,14 @@ wpsgd_status rows_workspace(wpsgd_ctx* c) {
   CU_TRY(c, cudaStreamIsCapturing(c->stream, &capturing));
   if (capturing != cudaStreamCaptureStatusNone)
     return fail(c, WPSGD_ERR_STATE, "the first call of a gradient, norm or clipping operator on a context allocates its workspace: make one before the capture");
-  CU_TRY(c, cudaMalloc(&c->rows_ws, RowsLayout(c->d).total));
+  void* ws = nullptr;
+  CU_TRY(c, cudaMalloc(&ws, RowsLayout(c->d).total));
+  cudaError_t e = cudaMemsetAsync(ws, 0, RowsLayout(c->d).sums, c->stream);
+  if (e != cudaSuccess) {
+    cudaFree(ws);
+    CU_TRY(c, e);
+  }
+  c->rows_ws = ws;
   return WPSGD_OK;
 }
 
@@ -164,18 +172,19 @@ wpsgd_status gradient_any_width(wpsgd_ctx* c, GradParams p, int* parts, int* n_s
 
 // One pass with G threads per row and CH units per thread; false: the rows are wider.
 template <typename RT, bool VEC, int G, int CH, int R>
-wpsgd_status gradient_one_pass(wpsgd_ctx* c, const GradParams& p, int* parts) {
+wpsgd_status gradient_one_pass(wpsgd_ctx* c, GradParams& p, int* parts) {
   using Shape = GradShape<RT, VEC, G, CH, R>;
   const long long batches = (p.n_rows + R - 1) / R, blocks = (batches + Shape::groups - 1) / Shape::groups;
   *parts = (int)std::min<long long>({blocks, (long long)RowsLayout(c->d).parts, 148ll * Shape::per_sm});
   static_assert(Shape::smem + 8192 <= (int)kSmemMax / Shape::per_sm, "the slots of the blocks of an SM must fit");
   CU_TRY(c, (allow_smem<gradient_rows_kernel<RT, VEC, G, CH, R>>(c)));
+  if ((long long)*parts * p.d <= GRAD_LAST_BLOCK) p.ticket = (unsigned*)((char*)c->rows_ws + RowsLayout(c->d).ticket);
   CU_TRY(c, launch(gradient_rows_kernel<RT, VEC, G, CH, R>, *parts, Shape::threads, Shape::smem, c->stream, p));
   c->launches++;
   return WPSGD_OK;
 }
 template <typename RT, bool VEC>
-wpsgd_status gradient_by_width(wpsgd_ctx* c, const GradParams& p, int* parts, int* n_sums) {
+wpsgd_status gradient_by_width(wpsgd_ctx* c, GradParams& p, int* parts, int* n_sums) {
   constexpr int V = RowUnit<RT>::V, R = V == 16 || (V == 8 && !VEC) ? 4 : 8;
   const long long units = (p.d + V - 1) / V;
   auto run = [&](auto g, auto ch, auto r) {
@@ -198,7 +207,7 @@ wpsgd_status gradient_by_width(wpsgd_ctx* c, const GradParams& p, int* parts, in
 }
 
 template <typename RT>
-wpsgd_status gradient(wpsgd_ctx* c, GradParams p, float lambda, float* grad, float* out) {
+wpsgd_status gradient(wpsgd_ctx* c, GradParams p) {
   wpsgd_status s = rows_workspace(c);
   if (s != WPSGD_OK) return s;
   const RowsLayout lay(c->d);
@@ -209,9 +218,9 @@ wpsgd_status gradient(wpsgd_ctx* c, GradParams p, float lambda, float* grad, flo
     const bool vec = std::is_same<RT, Row8>::value || (aligned16(p.X) && p.ld % RowUnit<RT>::V == 0);
     if constexpr (std::is_same<RT, Row8>::value) s = gradient_by_width<RT, true>(c, p, &parts, &n_sums);
     else s = vec ? gradient_by_width<RT, true>(c, p, &parts, &n_sums) : gradient_by_width<RT, false>(c, p, &parts, &n_sums);
-    if (s != WPSGD_OK) return s;
+    if (s != WPSGD_OK || p.ticket) return s;
   }
-  launch(gradient_finish_kernel, (unsigned)((p.d + 31) / 32), 32 * GRAD_FINISH_WARPS, 0, c->stream, p.part, parts, p.sums, n_sums, p.w, p.d, p.n_rows, lambda, grad, out);
+  launch(gradient_finish_kernel, (unsigned)((p.d + 31) / 32), 32 * GRAD_FINISH_WARPS, 0, c->stream, p, parts, n_sums);
   CU_TRY(c, cudaGetLastError());
   c->launches++;
   return WPSGD_OK;
@@ -334,6 +343,11 @@ wpsgd_status run_list(wpsgd_ctx* c, const wpsgd_grad_list* list, bool scale, dou
     if (it->lo + list->longest <= lo) break;
   }
   DeviceGuard guard(c->device);
+  if (list->few.size() == 1 && list->chunks <= CLIP_SMALL_CHUNKS) {
+    CU_TRY(c, launch(clip_small_kernel<kFewTensors>, CLIP_CLUSTER, CLIP_THREADS, 0, c->stream, list->few[0], scale, max_norm, list->in_place, norm_out));
+    c->launches++;
+    return WPSGD_OK;
+  }
   wpsgd_status s = rows_workspace(c);
   if (s != WPSGD_OK) return s;
   const int blocks = (int)std::max(1ll, std::min<long long>(CLIP_BLOCKS, list->chunks));
@@ -392,8 +406,8 @@ wpsgd_status wpsgd_objective_grad(wpsgd_ctx* c, const void* X, wpsgd_xtype xt, i
   if (const char* why = check_gradient(c, y, n_rows, w, lambda, loss, grad, out)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("objective_grad: ") + why);
   if ((uintptr_t)X % element_size(xt)) return fail(c, WPSGD_ERR_INVALID_ARG, "objective_grad: X is not aligned to its elements");
   DeviceGuard guard(c->device);
-  const GradParams p = {X, ld_elems, nullptr, 0, y, w, n_rows, c->d, (int)loss, nullptr, nullptr};
-  return xt == WPSGD_X_F32 ? gradient<float>(c, p, lambda, grad, out) : gradient<__nv_bfloat16>(c, p, lambda, grad, out);
+  const GradParams p = {X, ld_elems, nullptr, 0, y, w, n_rows, c->d, (int)loss, lambda, grad, out, nullptr, nullptr, nullptr};
+  return xt == WPSGD_X_F32 ? gradient<float>(c, p) : gradient<__nv_bfloat16>(c, p);
 }
 
 wpsgd_status wpsgd_objective_grad_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld_q, const float* scales, int64_t ld_s, const float* y, int64_t n_rows, const float* w,
@@ -402,8 +416,8 @@ wpsgd_status wpsgd_objective_grad_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld
   if (const char* why = check_rows8(Q, ld_q, scales, ld_s, n_rows, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("objective_grad_fp8: ") + why);
   if (const char* why = check_gradient(c, y, n_rows, w, lambda, loss, grad, out)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("objective_grad_fp8: ") + why);
   DeviceGuard guard(c->device);
-  const GradParams p = {Q, ld_q, scales, ld_s, y, w, n_rows, c->d, (int)loss, nullptr, nullptr};
-  return gradient<Row8>(c, p, lambda, grad, out);
+  const GradParams p = {Q, ld_q, scales, ld_s, y, w, n_rows, c->d, (int)loss, lambda, grad, out, nullptr, nullptr, nullptr};
+  return gradient<Row8>(c, p);
 }
 
 wpsgd_status wpsgd_grad_list_create(const void* const* grads, void* const* out, const int64_t* n_elems, const wpsgd_xtype* types, int32_t n_tensors,
