@@ -23,6 +23,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "async.cuh"
 #include "common.cuh"
 #include "quantize.cuh"
 
@@ -47,6 +48,9 @@ struct GradParams {
   float* part;           // [blocks, d] partial gradients
   double* sums;          // [blocks, 2] losses and errors
   unsigned* ticket;      // blocks that have finished (zero between launches); null: gradient_finish_kernel follows
+  int slots;             // of a ring (FEED_BULK)
+  long long spin_limit, drop_block;
+  DevStatus* status;
 };
 
 // 16 bytes of a row, widened to pairs
@@ -274,8 +278,15 @@ __device__ __forceinline__ float transpose_sum(float (&v)[R], int l) {
   return v[0];
 }
 
-// G threads per row, each CH units of 16 bytes of it (VEC) or the same number of single elements; R rows at a time.
-template <typename RT, bool VEC, int G, int CH, int R>
+// How rows reach the threads that work on them.
+enum RowFeed {
+  FEED_ELEMENTS = 0,  // element by element into registers: rows that do not start on 16 bytes
+  FEED_UNITS = 1,     // each thread its own 16-byte units (cp.async): rows whose last unit is not whole
+  FEED_BULK = 2       // whole rows in bulk copies. 65536 bf16 rows of 4096 columns: by units 109 us without any work on them, in bulk 85
+};
+
+// G threads per row, each CH units of 16 bytes of it (or the same number of single elements); R rows at a time.
+template <typename RT, int FEED, int G, int CH, int R>
 struct GradShape {
   static constexpr int V = RowUnit<RT>::V;
   static constexpr bool scaled = std::is_same<RT, Row8>::value;
@@ -284,24 +295,41 @@ struct GradShape {
   static constexpr int groups = threads / G;       // of a block
   static constexpr int lanes = G < 32 ? G : 32;    // of a warp that work on the same rows
   static constexpr int warps = G < 32 ? 1 : G / 32;
-  // VEC: each thread keeps its part of the next rows in shared memory, in slots of R rows that no other thread touches
-  static constexpr int slot_bytes = threads * R * CH * (scaled ? 20 : 16);
-  static constexpr int slots = VEC ? 96 * 1024 * 2 / per_sm / slot_bytes : 0;
+  static constexpr int budget = 96 * 1024 * 2 / per_sm;
+  // FEED_UNITS: slots of R rows, each thread's part of them its own
+  static constexpr int unit_slot_bytes = threads * R * CH * (scaled ? 20 : 16);
+  static constexpr int unit_slots = budget / unit_slot_bytes;
+  // FEED_BULK: rings of slots of `rows` rows, a ring per group, or per warp where groups are smaller; 16 zeros in front
+  static constexpr int rings = threads / 32 / warps, rows = R * (32 / lanes);
+  static int bulk_slots(long long row_bytes) { return (int)std::min<long long>(8, (budget - 16) / (rings * rows * row_bytes)); }
   static constexpr int fold_bytes = groups > 1 ? threads * CH * V * 4 : 0;
   static constexpr int finish_bytes = threads / 32 * 33 * 8;
-  static constexpr int smem = std::max({slots * slot_bytes, fold_bytes, finish_bytes});
+  static int smem(long long row_bytes) {
+    const int ring = FEED == FEED_UNITS ? unit_slots * unit_slot_bytes : FEED == FEED_BULK ? 16 + (int)(bulk_slots(row_bytes) * rings * rows * row_bytes) : 0;
+    return std::max({ring, fold_bytes, finish_bytes});
+  }
 };
 
-template <typename RT, bool VEC, int G, int CH, int R>
-__global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradShape<RT, VEC, G, CH, R>::per_sm) gradient_rows_kernel(const __grid_constant__ GradParams p) {
-  using Shape = GradShape<RT, VEC, G, CH, R>;
+template <typename RT, int FEED, int G, int CH, int R>
+__global__ void __launch_bounds__(GradShape<RT, FEED, G, CH, R>::threads, GradShape<RT, FEED, G, CH, R>::per_sm)
+gradient_rows_kernel(const __grid_constant__ GradParams p) {
+  using Shape = GradShape<RT, FEED, G, CH, R>;
   constexpr int V = Shape::V, L = Shape::lanes, W = Shape::warps, E = CH * V, T = Shape::threads;
-  constexpr bool SCALED = Shape::scaled;
+  constexpr bool SCALED = Shape::scaled, VEC = FEED != FEED_ELEMENTS, BULK = FEED == FEED_BULK;
   extern __shared__ __align__(16) unsigned char grad_smem[];
   __shared__ float2 cross[2][T / 32][R];  // a warp's sums of w x and x x of each row
   __shared__ double cross64[T / 32];
   __shared__ double sums[2][T / 32];
+  __shared__ unsigned long long bars[BULK ? Shape::rings * 8 : 1];
   kernel_started();
+  if constexpr (BULK) {
+    if (threadIdx.x == 0) {
+      for (int i = 0; i < Shape::rings * 8; ++i) mbar_init(&bars[i], 1);
+      mbar_fence_init();
+    }
+    if (threadIdx.x < 4) ((uint32_t*)grad_smem)[threadIdx.x] = 0u;
+    __syncthreads();
+  }
   kernel_inputs_ready();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int group = threadIdx.x / G, gl = threadIdx.x % G, l = lane % L;
@@ -315,8 +343,8 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
 
   const long long stride = (long long)gridDim.x * Shape::groups * R;  // rows that all groups take at a time
   const long long first = ((long long)blockIdx.x * Shape::groups + group) * R;
-  // ---- VEC: rows through this thread's slots. What lies behind a row's end arrives as zeros.
-  constexpr int S = VEC ? Shape::slots : 1;
+  // ---- FEED_UNITS: rows through this thread's slots. What lies behind a row's end arrives as zeros.
+  constexpr int S = FEED == FEED_UNITS ? Shape::unit_slots : 2;
   const uint32_t slots = (uint32_t)__cvta_generic_to_shared(grad_smem) + threadIdx.x * 16;
   const uint32_t slot_scales = (uint32_t)__cvta_generic_to_shared(grad_smem) + S * T * R * CH * 16 + threadIdx.x * 4;
   const long long row_bytes = VEC ? p.ld * (16 / V) : 0;
@@ -330,7 +358,7 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
     bytes[j] = b < 0 ? 0 : b > 16 ? 16 : (int)b;
     offset[j] = b > 0 ? (gl + j * G) * 16 : 0;
   }
-  auto request = [&](int slot) {
+  auto request_units = [&](int slot) {
     const char* row = from;
     const float* row_scale = from_scale;
 #pragma unroll
@@ -355,6 +383,38 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
     }
     left -= stride;
   };
+  // ---- FEED_BULK: the ring of this group or warp. Rows behind the last are zeros.
+  const int ring_slots = p.slots, ring = warp / W, bulk_row = (int)(p.d * (16 / V)), bulk_slot = Shape::rows * bulk_row;
+  unsigned char* ring_base = grad_smem + 16 + (size_t)ring * ring_slots * bulk_slot;
+  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring_base) + (L < 32 ? lane / L * (R * bulk_row) : 0) + gl * 16;  // this thread's first unit
+  const uint32_t zeros_at = (uint32_t)__cvta_generic_to_shared(grad_smem);
+  const long long ring_first = ((long long)blockIdx.x * Shape::rings + ring) * Shape::rows;  // the warp's first row
+  unsigned long long* full = bars + ring * 8;
+  auto request_rows = [&](int slot, long long row0, long long round) {  // by one warp
+    if (row0 >= p.n_rows || round == p.drop_block) return;
+    const int rows = p.n_rows - row0 < Shape::rows ? (int)(p.n_rows - row0) : Shape::rows;
+    unsigned char* to = ring_base + (size_t)slot * bulk_slot;
+    const char* src = (const char*)p.X + row0 * row_bytes;
+    for (int i = rows * bulk_row + lane * 16; i < bulk_slot; i += 512) *(uint4*)(to + i) = make_uint4(0u, 0u, 0u, 0u);
+    __syncwarp();
+    if (lane == 0) mbar_arrive_expect_tx(&full[slot], rows * bulk_row);
+    if (row_bytes == bulk_row) {
+      if (lane == 0) bulk_copy_g2s(to, src, rows * bulk_row, &full[slot]);
+    } else {
+      __syncwarp();
+      for (int r = lane; r < rows; r += 32) bulk_copy_g2s(to + r * bulk_row, src + r * row_bytes, bulk_row, &full[slot]);
+    }
+  };
+  float scale_next[BULK && SCALED ? R : 1][BULK && SCALED ? CH : 1];
+  auto load_scales = [&](long long row0) {
+    if constexpr (BULK && SCALED) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+          scale_next[r][j] = row0 + r < p.n_rows && gl + j * G < units ? __ldg(p.scales + (row0 + r) * p.ld_s + (gl + j * G) / (Q_BLOCK / 16)) : 0.0f;
+    }
+  };
   // ---- else: rows through registers, the next R on their way
   float next[VEC ? 1 : R][VEC ? 1 : E];
   auto load = [&](long long row0) {
@@ -365,9 +425,13 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
         for (int i = 0; i < E; ++i) next[r][i] = row0 + r < p.n_rows && has(i) ? widen_scalar<RT>(((const RT*)p.X)[(row0 + r) * p.ld + column(i)]) : 0.0f;
     }
   };
-  if constexpr (VEC) {
+  if constexpr (BULK) {
+    if (W == 1 || warp % W == 0)
+      for (int i = 0; i < ring_slots; ++i) request_rows(i, ring_first + i * stride, i);
+    load_scales(first);
+  } else if constexpr (VEC) {
 #pragma unroll 1
-    for (int i = 0; i < S - 1; ++i) request(i);
+    for (int i = 0; i < S - 1; ++i) request_units(i);
   } else {
     load(first);
   }
@@ -392,6 +456,8 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
   };
 
   int round = 0, slot = 0;
+  uint32_t parity = 0;
+  bool dead = false;
   const int own = l / (L / R);  // of the R rows, the one whose sums this lane ends with
   float y_next = first + own < p.n_rows ? p.y[first + own] : 0.0f;
   // groups within a warp go round together (shuffles over the warp)
@@ -401,9 +467,24 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
     y_next = row0 + stride + own < p.n_rows ? p.y[row0 + stride + own] : 0.0f;
     float plain[VEC ? 1 : R][VEC ? 1 : E];
     const int cur = slot;
-    if constexpr (VEC) {
+    float scale[BULK && SCALED ? R : 1][BULK && SCALED ? CH : 1];
+    if constexpr (BULK) {
+      if (!dead && !mbar_wait_bounded(&full[cur], parity, p.spin_limit)) {
+        dead = true;
+        set_status(p.status, DEV_TIMEOUT, 51, blockIdx.x);
+      }
+      __syncwarp();
+      if (++slot == ring_slots) { slot = 0; parity ^= 1; }
+      if constexpr (SCALED) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int j = 0; j < CH; ++j) scale[r][j] = scale_next[r][j];
+        load_scales(row0 + stride);
+      }
+    } else if constexpr (VEC) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
-      request(slot == 0 ? S - 1 : slot - 1);  // into the slot of one round ago
+      request_units(slot == 0 ? S - 1 : slot - 1);  // into the slot of one round ago
       slot = slot == S - 1 ? 0 : slot + 1;
     } else {
 #pragma unroll
@@ -412,11 +493,13 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
         for (int i = 0; i < E; ++i) plain[r][i] = next[r][i];
       load(row0 + stride);
     }
-    // VEC: read from the slot both for the margin and for the gradient; widened values of all R rows would not fit the registers
+    // read from the slot both for the margin and for the gradient; widened values of all R rows would not fit the registers
     auto values = [&](int r, int j, uint64_t (&x)[V / 2]) {
       if constexpr (VEC) {
+        uint32_t at = slots + ((cur * R + r) * CH + j) * (T * 16);
+        if constexpr (BULK) at = gl + j * G < units ? ring_at + cur * bulk_slot + r * bulk_row + j * (G * 16) : zeros_at;
         uint4 raw;
-        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w) : "r"(slots + ((cur * R + r) * CH + j) * (T * 16)));
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w) : "r"(at));
         RowUnit<RT>::widen(raw, x);
       } else {
 #pragma unroll
@@ -424,6 +507,7 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
       }
     };
     auto scale_of = [&](int r, int j) {
+      if constexpr (BULK && SCALED) return scale[r][j];
       float v;
       asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(slot_scales + ((cur * R + r) * CH + j) * (T * 4)));
       return v;
@@ -461,6 +545,9 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
     if constexpr (W > 1) {  // every warp of the group adds up and goes on alike: one barrier a round
       if (l % (L / R) == 0) cross[round & 1][warp][own] = make_float2(zs, xs);
       group_barrier();
+      if constexpr (BULK) {  // the rows of one round ago are done with
+        if (round > 0 && round % W == warp - group * W) request_rows(cur == 0 ? ring_slots - 1 : cur - 1, row0 + (ring_slots - 1) * stride, round + ring_slots - 1ll);
+      }
       zs = xs = 0.0f;
 #pragma unroll
       for (int i = 0; i < W; ++i) {
@@ -483,7 +570,12 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
           for (int j = 0; j < CH; ++j) {
             uint64_t x[V / 2];
             values(r, j, x);
-            const double scale = SCALED ? (double)scale_of(r, j) : 1.0;
+            double scale = 1.0;
+            if constexpr (BULK && SCALED) {
+              if (row0 + r < p.n_rows && gl + j * G < units) scale = (double)p.scales[(row0 + r) * p.ld_s + (gl + j * G) / (Q_BLOCK / 16)];
+            } else if constexpr (SCALED) {
+              scale = (double)scale_of(r, j);
+            }
 #pragma unroll
             for (int e = 0; e < V / 2; ++e) {
               const float2 xe = halves(x[e]), we = halves(w[j * (V / 2) + e]);
@@ -536,6 +628,14 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
         for (int e = 0; e < V / 2; ++e) acc[j * (V / 2) + e] = fma2(g2, x[e], acc[j * (V / 2) + e]);
       }
     }
+    if constexpr (BULK && W == 1) {
+      __syncwarp();
+      request_rows(cur, row0 - first + ring_first + ring_slots * stride, round + (long long)ring_slots);
+    }
+  }
+  if constexpr (BULK) {
+    if (dead && lane == 0 && (W == 1 || warp % W == 0))  // copies in flight land before the block ends
+      for (int i = 0; i < ring_slots; ++i) mbar_wait_bounded(&full[i], i < slot ? parity ^ 1 : parity, p.spin_limit);
   }
   evaluate();
 
@@ -543,7 +643,7 @@ __global__ void __launch_bounds__(GradShape<RT, VEC, G, CH, R>::threads, GradSha
   if (lane == 0) { sums[0][warp] = loss; sums[1][warp] = wrong; }
   auto own_sum = [&](int i) { return i % 2 ? halves(acc[i / 2]).y : halves(acc[i / 2]).x; };
   float* fold = (float*)grad_smem;
-  if constexpr (VEC) asm volatile("cp.async.wait_all;" ::: "memory");
+  if constexpr (FEED == FEED_UNITS) asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();  // the slots are done with
   if constexpr (Shape::groups > 1) {
 #pragma unroll

@@ -171,24 +171,27 @@ wpsgd_status gradient_any_width(wpsgd_ctx* c, GradParams p, int* parts, int* n_s
 }
 
 // One pass with G threads per row and CH units per thread; false: the rows are wider.
-template <typename RT, bool VEC, int G, int CH, int R>
+template <typename RT, int FEED, int G, int CH, int R>
 wpsgd_status gradient_one_pass(wpsgd_ctx* c, GradParams& p, int* parts) {
-  using Shape = GradShape<RT, VEC, G, CH, R>;
+  using Shape = GradShape<RT, FEED, G, CH, R>;
   const long long batches = (p.n_rows + R - 1) / R, blocks = (batches + Shape::groups - 1) / Shape::groups;
   *parts = (int)std::min<long long>({blocks, (long long)RowsLayout(c->d).parts, 148ll * Shape::per_sm});
-  static_assert(Shape::smem + 8192 <= (int)kSmemMax / Shape::per_sm, "the slots of the blocks of an SM must fit");
-  CU_TRY(c, (allow_smem<gradient_rows_kernel<RT, VEC, G, CH, R>>(c)));
+  const long long row_bytes = p.d * (16 / Shape::V);
+  p.slots = FEED == FEED_BULK ? Shape::bulk_slots(row_bytes) : 0;
+  const int smem = Shape::smem(row_bytes);
+  if (FEED == FEED_BULK && p.slots < 2) return fail(c, WPSGD_ERR_STATE, "gradient: a ring of two slots must fit");
+  CU_TRY(c, (allow_smem<gradient_rows_kernel<RT, FEED, G, CH, R>>(c)));
   if ((long long)*parts * p.d <= GRAD_LAST_BLOCK) p.ticket = (unsigned*)((char*)c->rows_ws + RowsLayout(c->d).ticket);
-  CU_TRY(c, launch(gradient_rows_kernel<RT, VEC, G, CH, R>, *parts, Shape::threads, Shape::smem, c->stream, p));
+  CU_TRY(c, launch(gradient_rows_kernel<RT, FEED, G, CH, R>, *parts, Shape::threads, smem, c->stream, p));
   c->launches++;
   return WPSGD_OK;
 }
-template <typename RT, bool VEC>
+template <typename RT, int FEED>
 wpsgd_status gradient_by_width(wpsgd_ctx* c, GradParams& p, int* parts, int* n_sums) {
-  constexpr int V = RowUnit<RT>::V, R = V == 16 || (V == 8 && !VEC) ? 4 : 8;
+  constexpr int V = RowUnit<RT>::V, R = V == 16 || (V == 8 && FEED == FEED_ELEMENTS) ? 4 : 8;
   const long long units = (p.d + V - 1) / V;
   auto run = [&](auto g, auto ch, auto r) {
-    const wpsgd_status s = gradient_one_pass<RT, VEC, decltype(g)::value, decltype(ch)::value, decltype(r)::value>(c, p, parts);
+    const wpsgd_status s = gradient_one_pass<RT, FEED, decltype(g)::value, decltype(ch)::value, decltype(r)::value>(c, p, parts);
     *n_sums = *parts;
     return s;
   };
@@ -215,9 +218,10 @@ wpsgd_status gradient(wpsgd_ctx* c, GradParams p) {
   p.part = (float*)((char*)c->rows_ws + lay.part);
   int parts = 0, n_sums = 0;
   if (p.n_rows > 0) {
-    const bool vec = std::is_same<RT, Row8>::value || (aligned16(p.X) && p.ld % RowUnit<RT>::V == 0);
-    if constexpr (std::is_same<RT, Row8>::value) s = gradient_by_width<RT, true>(c, p, &parts, &n_sums);
-    else s = vec ? gradient_by_width<RT, true>(c, p, &parts, &n_sums) : gradient_by_width<RT, false>(c, p, &parts, &n_sums);
+    const bool units = std::is_same<RT, Row8>::value || (aligned16(p.X) && p.ld % RowUnit<RT>::V == 0);
+    if (units && p.d % RowUnit<RT>::V == 0) s = gradient_by_width<RT, FEED_BULK>(c, p, &parts, &n_sums);
+    else if constexpr (std::is_same<RT, Row8>::value) s = gradient_by_width<RT, FEED_UNITS>(c, p, &parts, &n_sums);
+    else s = units ? gradient_by_width<RT, FEED_UNITS>(c, p, &parts, &n_sums) : gradient_by_width<RT, FEED_ELEMENTS>(c, p, &parts, &n_sums);
     if (s != WPSGD_OK || p.ticket) return s;
   }
   launch(gradient_finish_kernel, (unsigned)((p.d + 31) / 32), 32 * GRAD_FINISH_WARPS, 0, c->stream, p, parts, n_sums);
@@ -406,7 +410,7 @@ wpsgd_status wpsgd_objective_grad(wpsgd_ctx* c, const void* X, wpsgd_xtype xt, i
   if (const char* why = check_gradient(c, y, n_rows, w, lambda, loss, grad, out)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("objective_grad: ") + why);
   if ((uintptr_t)X % element_size(xt)) return fail(c, WPSGD_ERR_INVALID_ARG, "objective_grad: X is not aligned to its elements");
   DeviceGuard guard(c->device);
-  const GradParams p = {X, ld_elems, nullptr, 0, y, w, n_rows, c->d, (int)loss, lambda, grad, out, nullptr, nullptr, nullptr};
+  const GradParams p = {X, ld_elems, nullptr, 0, y, w, n_rows, c->d, (int)loss, lambda, grad, out, nullptr, nullptr, nullptr, 0, c->opt_spin_limit, c->opt_drop_block, c->status};
   return xt == WPSGD_X_F32 ? gradient<float>(c, p) : gradient<__nv_bfloat16>(c, p);
 }
 
@@ -416,7 +420,7 @@ wpsgd_status wpsgd_objective_grad_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld
   if (const char* why = check_rows8(Q, ld_q, scales, ld_s, n_rows, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("objective_grad_fp8: ") + why);
   if (const char* why = check_gradient(c, y, n_rows, w, lambda, loss, grad, out)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("objective_grad_fp8: ") + why);
   DeviceGuard guard(c->device);
-  const GradParams p = {Q, ld_q, scales, ld_s, y, w, n_rows, c->d, (int)loss, lambda, grad, out, nullptr, nullptr, nullptr};
+  const GradParams p = {Q, ld_q, scales, ld_s, y, w, n_rows, c->d, (int)loss, lambda, grad, out, nullptr, nullptr, nullptr, 0, c->opt_spin_limit, c->opt_drop_block, c->status};
   return gradient<Row8>(c, p);
 }
 
