@@ -443,13 +443,15 @@ class Context:
     # -- operators on whole sets of rows ------------------------------------------------------------------
     # (calls of a few microseconds: sizes are asked one by one and pointers passed as numbers, which costs less than tuples and
     # ctypes objects)
-    def _empty(self, shape, dtype):
+    def _empty(self, shape, dtype, strides=None):
         """A tensor for the context's stream to write: allocated for that stream, so that its memory is not reused under it."""
         torch = self._torch
-        if self._current_raw_stream(self.device) == self._raw_stream:
+        if self._current_raw_stream(self.device) != self._raw_stream:
+            with torch.cuda.stream(self._stream):
+                return torch.empty(shape, dtype=dtype, device=self._torch_device) if strides is None else torch.empty_strided(shape, strides, dtype=dtype, device=self._torch_device)
+        if strides is None:
             return torch.empty(shape, dtype=dtype, device=self._torch_device)
-        with torch.cuda.stream(self._stream):
-            return torch.empty(shape, dtype=dtype, device=self._torch_device)
+        return torch.empty_strided(shape, strides, dtype=dtype, device=self._torch_device)
 
     def _matrix(self, t, dtypes, cols, what):
         """Pointer, row stride (None: a single row) and row count of a 2-D tensor of rows of `cols` contiguous elements."""
@@ -487,9 +489,7 @@ class Context:
         torch = self._torch
         xp, ld, n = self._matrix(X, (torch.float32, torch.bfloat16), self.d, "X")
         if out is None:
-            out = self._empty((n, packed_width(self.d)), torch.float8_e4m3fn)
-            if out.size(1) != self.d:
-                out = out[:, :self.d]
+            out = self._empty((n, self.d), torch.float8_e4m3fn, (packed_width(self.d), 1))
         if scales is None:
             scales = self._empty((n, (self.d + 127) // 128), torch.float32)
         qp, ld_q, sp, ld_s, m = self._packed(out, scales, "out")

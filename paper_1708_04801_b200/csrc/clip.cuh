@@ -8,7 +8,8 @@
 // squares are exact to rounding (elements below 2^-40 alone, above 2^60, not finite) it is formed again in fp64, so that norms of
 // very small and very large gradients come out right.
 // Bound by memory: reads the gradients once for the norm and once more, from L2 as far as they fit, for the copies. The second
-// pass therefore goes through each block's part backwards, latest read first.
+// pass therefore goes through each block's part backwards, latest read first, and all but the last 72 MB of the first pass, and
+// all of the second, is marked to leave L2 first.
 #pragma once
 
 #include "common.cuh"
@@ -16,8 +17,9 @@
 namespace wpsgd {
 
 constexpr int CLIP_CHUNK = 8192;   // elements per unit of work
-constexpr int CLIP_BLOCKS = 148 * 4;
-constexpr int CLIP_THREADS = 256;
+constexpr int CLIP_BLOCKS = 148 * 8;
+constexpr int CLIP_THREADS = 128;
+constexpr long long CLIP_KEEP = 72ll << 20;  // bytes that the first pass leaves in L2 for the second
 
 // N tensors at most. elems_type = elements * 2 + (1: bf16, 0: fp32); first_chunk[i]: chunks of the tensors before i.
 template <int N>
@@ -27,6 +29,7 @@ struct TensorList {
   long long elems_type[N];
   int first_chunk[N + 1];
   int n;
+  uint16_t start[CLIP_BLOCKS];  // tensor that holds the first chunk of each block's share
 };
 
 // Elements of a tensor as 16-byte units of the source: `head` elements before the first aligned address, whole units, the rest.
@@ -68,7 +71,7 @@ __device__ __forceinline__ double batch_squares_f64(const uint4 (&raw)[U]) {
 
 // this thread's share of the squares of chunk `chunk` (of its tensor)
 template <typename T>
-__device__ __forceinline__ double chunk_squares(const T* src, long long n, int chunk) {
+__device__ __forceinline__ double chunk_squares(const T* src, long long n, int chunk, bool keep) {
   constexpr int V = XVec<T>::V, UNITS = CLIP_CHUNK / V, U = 4;
   const TensorParts tp(src, n, sizeof(T));
   const uint4* body = (const uint4*)(src + tp.head);
@@ -79,7 +82,7 @@ __device__ __forceinline__ double chunk_squares(const T* src, long long n, int c
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       raw[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (u + i * CLIP_THREADS < u1) raw[i] = __ldg(body + u + i * CLIP_THREADS);
+      if (u + i * CLIP_THREADS < u1) raw[i] = keep ? __ldg(body + u + i * CLIP_THREADS) : __ldcs(body + u + i * CLIP_THREADS);
     }
     const float s = batch_squares<T>(raw, U);
     if (s > 0x1p-80f && s < 0x1p120f) sum += (double)s;
@@ -134,12 +137,12 @@ __device__ __forceinline__ void chunk_scale(const T* src, T* dst, long long n, i
     uint4 raw[U];
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if (u + i * CLIP_THREADS < u1) raw[i] = body[u + i * CLIP_THREADS];
+      if (u + i * CLIP_THREADS < u1) raw[i] = __ldcs(body + u + i * CLIP_THREADS);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       if (u + i * CLIP_THREADS >= u1) continue;
       if (whole) {
-        ((uint4*)to)[u + i * CLIP_THREADS] = scaled_unit(raw[i], f, T());
+        __stcs((uint4*)to + u + i * CLIP_THREADS, scaled_unit(raw[i], f, T()));
       } else {
         float x[V];
         XVec<T>::widen(raw[i], x);
@@ -157,25 +160,19 @@ __device__ __forceinline__ void chunk_scale(const T* src, T* dst, long long n, i
   }
 }
 
-// Chunks b q .. of block b, an even share of all; the tensor of the first by bisection, of the next by stepping.
+// The chunks of a block's even share of all, first to last or last to first: f(tensor, chunk of it, chunks to go)
 template <int N, typename F>
 __device__ __forceinline__ void for_own_chunks(const TensorList<N>& list, bool backwards, F f) {
   const int total = list.first_chunk[list.n];
   const int c0 = (int)((long long)total * blockIdx.x / gridDim.x), c1 = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
   if (c0 >= c1) return;
   const int start = backwards ? c1 - 1 : c0;
-  int lo = 0, hi = list.n - 1;  // last tensor with first_chunk <= start (tensors without elements have no chunk)
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (list.first_chunk[mid] <= start) lo = mid;
-    else hi = mid - 1;
-  }
-  int i = lo;
+  int i = list.start[blockIdx.x];
   for (int k = 0; k < c1 - c0; ++k) {
     const int c = backwards ? start - k : start + k;
     while (c >= list.first_chunk[i + 1]) ++i;
     while (c < list.first_chunk[i]) --i;
-    f(i, c - list.first_chunk[i]);
+    f(i, c - list.first_chunk[i], c1 - c0 - k);
   }
 }
 
@@ -191,14 +188,15 @@ __device__ __forceinline__ double block_sum_f64(double v, double* sh) {  // of a
 
 // part[block] = squares of the block's share (added to what the launches before it found, where the list takes several)
 template <int N>
-__global__ void __launch_bounds__(CLIP_THREADS) squares_kernel(const __grid_constant__ TensorList<N> list, bool first, double* __restrict__ part) {
+__global__ void __launch_bounds__(CLIP_THREADS, 8) squares_kernel(const __grid_constant__ TensorList<N> list, bool first, double* __restrict__ part) {
   __shared__ double sh[CLIP_THREADS / 32];
   kernel_started();
   kernel_inputs_ready();
   double sum = 0.0;
-  for_own_chunks(list, false, [&](int i, int chunk) {
+  const int kept = (int)(CLIP_KEEP / (CLIP_CHUNK * 4) / gridDim.x);  // of a block's chunks, the last: the second pass starts with them
+  for_own_chunks(list, false, [&](int i, int chunk, int to_go) {
     const long long n = list.elems_type[i] >> 1;
-    sum += list.elems_type[i] & 1 ? chunk_squares((const __nv_bfloat16*)list.src[i], n, chunk) : chunk_squares((const float*)list.src[i], n, chunk);
+    sum += list.elems_type[i] & 1 ? chunk_squares((const __nv_bfloat16*)list.src[i], n, chunk, to_go <= kept) : chunk_squares((const float*)list.src[i], n, chunk, to_go <= kept);
   });
   sum = block_sum_f64(sum, sh);
   if (threadIdx.x == 0) part[blockIdx.x] = first ? sum : part[blockIdx.x] + sum;
@@ -220,7 +218,7 @@ __global__ void __launch_bounds__(CLIP_THREADS) norm_kernel(const double* __rest
 }
 
 template <int N>
-__global__ void __launch_bounds__(CLIP_THREADS) scale_kernel(const __grid_constant__ TensorList<N> list, const double* __restrict__ part, int parts,
+__global__ void __launch_bounds__(CLIP_THREADS, 8) scale_kernel(const __grid_constant__ TensorList<N> list, const double* __restrict__ part, int parts,
                                                              double max_norm, bool in_place, float* __restrict__ norm_out) {
   __shared__ double sh[CLIP_THREADS / 32];
   kernel_started();
@@ -230,7 +228,7 @@ __global__ void __launch_bounds__(CLIP_THREADS) scale_kernel(const __grid_consta
   const bool clips = norm > max_norm;
   if (!clips && in_place) return;  // times 1
   const float f = clips ? (float)(max_norm / norm) : 1.0f;
-  for_own_chunks(list, true, [&](int i, int chunk) {
+  for_own_chunks(list, true, [&](int i, int chunk, int) {
     const long long n = list.elems_type[i] >> 1;
     if (list.elems_type[i] & 1) chunk_scale((const __nv_bfloat16*)list.src[i], (__nv_bfloat16*)list.dst[i], n, chunk, f);
     else chunk_scale((const float*)list.src[i], (float*)list.dst[i], n, chunk, f);
@@ -249,9 +247,10 @@ clip_small_kernel(const __grid_constant__ TensorList<N> list, bool scale, double
   kernel_started();
   kernel_inputs_ready();
   double sum = 0.0;
-  for_own_chunks(list, false, [&](int i, int chunk) {
+  const int kept = (int)(CLIP_KEEP / (CLIP_CHUNK * 4) / gridDim.x);  // of a block's chunks, the last: the second pass starts with them
+  for_own_chunks(list, false, [&](int i, int chunk, int to_go) {
     const long long n = list.elems_type[i] >> 1;
-    sum += list.elems_type[i] & 1 ? chunk_squares((const __nv_bfloat16*)list.src[i], n, chunk) : chunk_squares((const float*)list.src[i], n, chunk);
+    sum += list.elems_type[i] & 1 ? chunk_squares((const __nv_bfloat16*)list.src[i], n, chunk, to_go <= kept) : chunk_squares((const float*)list.src[i], n, chunk, to_go <= kept);
   });
   sum = block_sum_f64(sum, sh);
   if (threadIdx.x < CLIP_CLUSTER) {
@@ -268,7 +267,7 @@ clip_small_kernel(const __grid_constant__ TensorList<N> list, bool scale, double
   const bool clips = norm > max_norm;
   if (!scale || (!clips && in_place)) return;
   const float f = clips ? (float)(max_norm / norm) : 1.0f;
-  for_own_chunks(list, true, [&](int i, int chunk) {
+  for_own_chunks(list, true, [&](int i, int chunk, int) {
     const long long n = list.elems_type[i] >> 1;
     if (list.elems_type[i] & 1) chunk_scale((const __nv_bfloat16*)list.src[i], (__nv_bfloat16*)list.dst[i], n, chunk, f);
     else chunk_scale((const float*)list.src[i], (float*)list.dst[i], n, chunk, f);

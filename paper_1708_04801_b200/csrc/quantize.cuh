@@ -27,59 +27,138 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
   return r;
 }
 
-// A group of 128 / V lanes per block, each lane V elements of it: one 16-byte load and one store of V bytes. VEC = false (rows that do
-// not start on 16 bytes, or whose last 16 bytes are not whole): the same lanes and elements, loaded one by one.
-template <typename XT, bool VEC, int U>
+// U blocks at a time per group of G lanes: lane g < U divides 448 / a of block g, lane U + g the scale a / 448, so that two divisions of ten
+// instructions are done once and not by every lane. `a` is left in all lanes of the group.
+template <int U, int G>
+__device__ __forceinline__ void block_scales(float (&a)[U], float (&inv)[U], float& scale, int gl) {
+  static_assert(2 * U <= G, "a lane for each division");
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) a[u] = fmaxf(a[u], __shfl_xor_sync(0xffffffffu, a[u], o));
+  float own = a[0];
+#pragma unroll
+  for (int u = 1; u < U; ++u) own = gl % U == u ? a[u] : own;
+  scale = gl < U ? Q_MAX / own : own / Q_MAX;
+#pragma unroll
+  for (int u = 0; u < U; ++u) inv[u] = __shfl_sync(0xffffffffu, scale, u, G);
+}
+
+// The blocks (row, block of columns) first, first + apart, .. first + (U - 1) apart of all rows' blocks, and on by `stride` each step,
+// without a division per step.
+template <int U>
+struct BlockWalk {
+  long long row[U], rows_per_step;
+  int block[U], blocks_per_step;
+  __device__ __forceinline__ BlockWalk(long long first, int apart, long long stride, int nb) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      row[u] = row_of(first + u * apart, nb);
+      block[u] = (int)(first + u * apart - row[u] * nb);
+    }
+    rows_per_step = row_of(stride, nb);
+    blocks_per_step = (int)(stride - rows_per_step * nb);
+  }
+  __device__ __forceinline__ void step(int nb) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      row[u] += rows_per_step;
+      block[u] += blocks_per_step;
+      if (block[u] >= nb) { block[u] -= nb; ++row[u]; }
+    }
+  }
+};
+
+// Rows that start on 16 bytes: a group of 128 / V lanes per block, each lane V elements of it in one 16-byte load and one store of V
+// bytes. U blocks in flight per group.
+template <typename XT, int U>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const XT* __restrict__ X, long long ld, long long n_rows, long long d, int nb,
                                                             uint8_t* __restrict__ Q, long long ld_q, float* __restrict__ scales, long long ld_s) {
   kernel_started();
   kernel_inputs_ready();
   constexpr int V = XVec<XT>::V, G = Q_BLOCK / V, PER_WARP = 32 / G;
   const int lane = threadIdx.x & 31, gl = lane % G;
-  const long long warps = (long long)gridDim.x * 8, total = n_rows * nb;
-  for (long long t0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * (PER_WARP * U); t0 < total; t0 += warps * (PER_WARP * U)) {
-    float x[U][V];
-    long long row[U], c[U];
-    bool in[U];
+  BlockWalk<U> at(((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * (PER_WARP * U) + lane / G, PER_WARP, (long long)gridDim.x * 8 * (PER_WARP * U), nb);
+  for (; __any_sync(0xffffffffu, at.row[0] < n_rows); at.step(nb)) {
+    uint4 raw[U];
+    bool in[U];  // this lane has a part of a row
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long long t = t0 + u * PER_WARP + lane / G;
-      in[u] = t < total;
-      row[u] = in[u] ? row_of(t, nb) : 0;
-      c[u] = (t - row[u] * nb) * Q_BLOCK + gl * V;
-      if constexpr (VEC) {
-        XVec<XT>::widen(ld_stream16_if(X + row[u] * ld + c[u], in[u] && c[u] < d), x[u]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) x[u][e] = in[u] && c[u] + e < d ? widen_scalar<XT>(X[row[u] * ld + c[u] + e]) : 0.0f;
-      }
+      const int c = at.block[u] * Q_BLOCK + gl * V;
+      in[u] = at.row[u] < n_rows && c < d;
+      raw[u] = ld_stream16_if(X + at.row[u] * ld + c, in[u]);
     }
+    float a[U], inv[U], scale;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float a = Q_AMAX_MIN;
+      float x[V];
+      XVec<XT>::widen(raw[u], x);
+      a[u] = Q_AMAX_MIN;
 #pragma unroll
-      for (int e = 0; e < V; ++e) a = fmaxf(a, fabsf(x[u][e]));
+      for (int e = 0; e < V; ++e) a[u] = fmaxf(a[u], fabsf(x[e]));
+    }
+    block_scales<U, G>(a, inv, scale, gl);
 #pragma unroll
-      for (int o = G / 2; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-      const float inv = Q_MAX / a;
+    for (int u = 0; u < U; ++u) {
+      float x[V];
+      XVec<XT>::widen(raw[u], x);
       uint32_t q[V / 4];
 #pragma unroll
       for (int e = 0; e < V; e += 4) {
-        const uint32_t lo = to_e4m3x2(x[u][e] * inv, x[u][e + 1] * inv), hi = to_e4m3x2(x[u][e + 2] * inv, x[u][e + 3] * inv);
+        const uint32_t lo = to_e4m3x2(x[e] * inv[u], x[e + 1] * inv[u]), hi = to_e4m3x2(x[e + 2] * inv[u], x[e + 3] * inv[u]);
         q[e / 4] = lo | hi << 16;
       }
-      if (in[u] && c[u] < d) {
-        uint8_t* dst = Q + row[u] * ld_q + c[u];
-        if (VEC || c[u] + V <= d) {
-          if constexpr (V == 8) *(uint2*)dst = make_uint2(q[0], q[1]);
-          else *(uint32_t*)dst = q[0];
-        } else {
-#pragma unroll
-          for (int e = 0; e < V; ++e)
-            if (c[u] + e < d) dst[e] = (uint8_t)(q[e / 4] >> 8 * (e % 4));
-        }
-        if (gl == 0) scales[row[u] * ld_s + c[u] / Q_BLOCK] = a / Q_MAX;
+      if (in[u]) {
+        uint8_t* dst = Q + at.row[u] * ld_q + at.block[u] * Q_BLOCK + gl * V;
+        if constexpr (V == 8) *(uint2*)dst = make_uint2(q[0], q[1]);
+        else *(uint32_t*)dst = q[0];
       }
+      if (gl == U + u && at.row[u] < n_rows) scales[at.row[u] * ld_s + at.block[u]] = scale;
+    }
+  }
+}
+
+// Any other rows: a warp per block, lane l the columns l, l + 32, l + 64, l + 96 (neighbouring lanes load neighbouring elements), whose
+// codes it exchanges for those of columns 4 l to 4 l + 3.
+template <typename XT, int U>
+__global__ void __launch_bounds__(256) quantize_elements_kernel(const XT* __restrict__ X, long long ld, long long n_rows, long long d, int nb,
+                                                                uint8_t* __restrict__ Q, long long ld_q, float* __restrict__ scales, long long ld_s) {
+  kernel_started();
+  kernel_inputs_ready();
+  const int lane = threadIdx.x & 31;
+  BlockWalk<U> at(((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * U, 1, (long long)gridDim.x * 8 * U, nb);
+  for (; at.row[0] < n_rows; at.step(nb)) {
+    float x[U][4], a[U], inv[U], scale;
+    int left[U];  // columns of the block
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long rest = d - (long long)at.block[u] * Q_BLOCK;
+      left[u] = at.row[u] < n_rows ? (int)(rest < Q_BLOCK ? rest : Q_BLOCK) : 0;
+      a[u] = Q_AMAX_MIN;
+      const XT* src = X + at.row[u] * ld + at.block[u] * Q_BLOCK + lane;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[u][e] = lane + 32 * e < left[u] ? widen_scalar<XT>(src[32 * e]) : 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[u] = fmaxf(a[u], fabsf(x[u][e]));
+    block_scales<U, 32>(a, inv, scale, lane);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t q = to_e4m3x2(x[u][0] * inv[u], x[u][1] * inv[u]) | to_e4m3x2(x[u][2] * inv[u], x[u][3] * inv[u]) << 16;
+      uint32_t w = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w |= (__shfl_sync(0xffffffffu, q, lane % 8 * 4 + i) >> lane / 8 * 8 & 0xffu) << 8 * i;
+      uint8_t* dst = Q + at.row[u] * ld_q + at.block[u] * Q_BLOCK + 4 * lane;
+      if (4 * lane + 4 <= left[u]) {
+        *(uint32_t*)dst = w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (4 * lane + i < left[u]) dst[i] = (uint8_t)(w >> 8 * i);
+      }
+      if (lane == U + u && left[u] > 0) scales[at.row[u] * ld_s + at.block[u]] = scale;
     }
   }
 }

@@ -256,6 +256,7 @@ struct wpsgd_grad_list {
   std::vector<Range> ranges;
   uintptr_t longest = 0;   // range, bytes
   long long chunks = 0;    // of the launch with most
+  int blocks = 1;
   bool in_place = true;
 };
 
@@ -275,6 +276,20 @@ void add_tensor(std::vector<TensorList<N>>& lists, const void* src, void* dst, l
   l.elems_type[l.n] = n * 2 + (bf16 ? 1 : 0);
   l.first_chunk[l.n + 1] = l.first_chunk[l.n] + (int)chunks;
   l.n++;
+}
+
+// The first tensor of each block's share, so that no block has to search for it
+template <int N>
+void set_starts(std::vector<TensorList<N>>& lists, int blocks) {
+  for (TensorList<N>& l : lists) {
+    const long long total = l.first_chunk[l.n];
+    int i = 0;
+    for (int b = 0; b < blocks; ++b) {
+      const int c0 = (int)(total * b / blocks);
+      while (i + 1 < l.n && l.first_chunk[i + 1] <= c0) ++i;
+      l.start[b] = (uint16_t)i;
+    }
+  }
 }
 
 // nullptr, or what is wrong
@@ -302,6 +317,9 @@ const char* make_list(wpsgd_grad_list* list, const void* const* src, void* const
   }
   for (const auto& l : list->few) list->chunks = std::max<long long>(list->chunks, l.first_chunk[l.n]);
   for (const auto& l : list->many) list->chunks = std::max<long long>(list->chunks, l.first_chunk[l.n]);
+  list->blocks = list->few.size() == 1 && list->chunks <= CLIP_SMALL_CHUNKS ? CLIP_CLUSTER : (int)std::max(1ll, std::min<long long>(CLIP_BLOCKS, list->chunks));
+  set_starts(list->few, list->blocks);
+  set_starts(list->many, list->blocks);
   // every element is written by one thread and read by no other: outputs are disjoint, and each is its own input or apart from all
   std::sort(list->ranges.begin(), list->ranges.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
   uintptr_t end_all = 0, end_out = 0;  // ends of what lies before: of all ranges, of outputs
@@ -354,7 +372,7 @@ wpsgd_status run_list(wpsgd_ctx* c, const wpsgd_grad_list* list, bool scale, dou
   }
   wpsgd_status s = rows_workspace(c);
   if (s != WPSGD_OK) return s;
-  const int blocks = (int)std::max(1ll, std::min<long long>(CLIP_BLOCKS, list->chunks));
+  const int blocks = list->blocks;
   return list->many.empty() ? norm_and_scale(c, list->few, blocks, scale, list->in_place, max_norm, norm_out)
                             : norm_and_scale(c, list->many, blocks, scale, list->in_place, max_norm, norm_out);
 }
@@ -373,15 +391,16 @@ wpsgd_status wpsgd_quantize_rows(wpsgd_ctx* c, const void* X, wpsgd_xtype xt, in
   if ((uintptr_t)X % es) return fail(c, WPSGD_ERR_INVALID_ARG, "quantize_rows: X is not aligned to its elements");
   DeviceGuard guard(c->device);
   const long long nb = blocks_of(c->d);
-  if (nb > INT32_MAX || n_rows > INT64_MAX / nb / 64) return fail(c, WPSGD_ERR_UNSUPPORTED, "quantize_rows: more than 2^57 blocks");
+  if (c->d > INT32_MAX - Q_BLOCK || n_rows > INT64_MAX / nb / 64) return fail(c, WPSGD_ERR_UNSUPPORTED, "quantize_rows: 2^31 columns or 2^57 blocks and more");
   const bool vec = aligned16(X) && ((size_t)ld_elems * es) % 16 == 0 && ((size_t)c->d * es) % 16 == 0;
-  auto go = [&](auto tag, auto vec_tag) {
+  auto go = [&](auto tag) {
     using XT = decltype(tag);
-    constexpr int U = 4, per_block = 8 * U * (32 / (Q_BLOCK / XVec<XT>::V));
-    launch(quantize_rows_kernel<XT, decltype(vec_tag)::value, U>, grid_for(n_rows * nb, per_block, 148 * 8), 256, 0, c->stream, (const XT*)X, ld_elems, n_rows, c->d, (int)nb, Q, ld_q, scales, ld_s);
+    constexpr int U = 4, per_warp = 32 / (Q_BLOCK / XVec<XT>::V);
+    if (vec) launch(quantize_rows_kernel<XT, U>, grid_for(n_rows * nb, 8 * U * per_warp, 148 * 8), 256, 0, c->stream, (const XT*)X, ld_elems, n_rows, c->d, (int)nb, Q, ld_q, scales, ld_s);
+    else launch(quantize_elements_kernel<XT, U>, grid_for(n_rows * nb, 8 * U, 148 * 8), 256, 0, c->stream, (const XT*)X, ld_elems, n_rows, c->d, (int)nb, Q, ld_q, scales, ld_s);
   };
-  if (xt == WPSGD_X_F32) vec ? go(float(), std::true_type()) : go(float(), std::false_type());
-  else vec ? go(__nv_bfloat16(), std::true_type()) : go(__nv_bfloat16(), std::false_type());
+  if (xt == WPSGD_X_F32) go(float());
+  else go(__nv_bfloat16());
   CU_TRY(c, cudaGetLastError());
   c->launches++;
   return WPSGD_OK;
