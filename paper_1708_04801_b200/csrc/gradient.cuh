@@ -67,7 +67,7 @@ struct RowUnit {
   }
 };
 template <>
-struct RowUnit<Row8> {
+struct RowUnit<Row8> {  // (never element by element)
   static constexpr int V = 16;
   using Scalar = uint8_t;
   __device__ __forceinline__ static float2 pair(uint32_t two) {  // exact: e4m3 is a subset of fp16
@@ -416,13 +416,14 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     }
   };
   // ---- else: rows through registers, the next R on their way
-  float next[VEC ? 1 : R][VEC ? 1 : E];
+  using Scalar = typename RowUnit<RT>::Scalar;  // kept as loaded: a conversion would wait for the load
+  Scalar next[VEC ? 1 : R][VEC ? 1 : E];
   auto load = [&](long long row0) {
     if constexpr (!VEC) {
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int i = 0; i < E; ++i) next[r][i] = row0 + r < p.n_rows && has(i) ? widen_scalar<RT>(((const RT*)p.X)[(row0 + r) * p.ld + column(i)]) : 0.0f;
+        for (int i = 0; i < E; ++i) next[r][i] = row0 + r < p.n_rows && has(i) ? ((const Scalar*)p.X)[(row0 + r) * p.ld + column(i)] : Scalar(0.0f);
     }
   };
   if constexpr (BULK) {
@@ -465,7 +466,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     const bool in = row0 + own < p.n_rows;
     const float y = y_next;
     y_next = row0 + stride + own < p.n_rows ? p.y[row0 + stride + own] : 0.0f;
-    float plain[VEC ? 1 : R][VEC ? 1 : E];
+    Scalar plain[VEC ? 1 : R][VEC ? 1 : E];
     const int cur = slot;
     float scale[BULK && SCALED ? R : 1][BULK && SCALED ? CH : 1];
     if constexpr (BULK) {
@@ -503,7 +504,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
         RowUnit<RT>::widen(raw, x);
       } else {
 #pragma unroll
-        for (int e = 0; e < V / 2; ++e) x[e] = pair_of(__float_as_uint(plain[r][j * V + 2 * e]), __float_as_uint(plain[r][j * V + 2 * e + 1]));
+        for (int e = 0; e < V / 2; ++e) x[e] = pair_of(__float_as_uint(widen_scalar<Scalar>(plain[r][j * V + 2 * e])), __float_as_uint(widen_scalar<Scalar>(plain[r][j * V + 2 * e + 1])));
       }
     };
     auto scale_of = [&](int r, int j) {

@@ -205,6 +205,8 @@ wpsgd_status gradient_by_width(wpsgd_ctx* c, GradParams& p, int* parts, int* n_s
   if (units <= 256) return GRAD_RUN(256, 1, R);
   if (units <= 512) return GRAD_RUN(256, 2, R / 2);
   if (units <= 1024) return GRAD_RUN(512, 2, R / 2);
+  if constexpr (V < 16)
+    if (units <= 2048) return GRAD_RUN(512, 4, 2);
 #undef GRAD_RUN
   return gradient_any_width<RT>(c, p, parts, n_sums);
 }
