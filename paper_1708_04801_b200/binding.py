@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from typing import Optional, Tuple
 
@@ -24,6 +25,7 @@ EXPORTED_SYMBOLS = [
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _lib = None
+_rows = None
 
 
 class WpsgdError(RuntimeError):
@@ -187,6 +189,20 @@ def solve_static(X, y, shard_off, n_steps, eta0, sched, lam, loss, seed, w0=None
     return out
 
 
+def load_rows():
+    """The built extension behind the operators on whole sets of rows. Raises if it is missing: there is no other path."""
+    global _rows
+    if _rows is None:
+        path = os.path.join(_HERE, "_rows.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python -m paper_1708_04801_b200.build`")
+        spec = importlib.util.spec_from_file_location("paper_1708_04801_b200._rows", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _rows = module
+    return _rows
+
+
 def packed_width(d: int) -> int:
     """Bytes from one packed row of d columns to the next: rows start on 16 bytes."""
     return (d + 15) // 16 * 16
@@ -244,14 +260,14 @@ class Context:
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
         self._stream = stream  # keep alive
-        self._torch, self._torch_device, self._raw_stream = torch, torch.device("cuda", self.device), stream.cuda_stream
-        self._current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        self._torch, self._rows = torch, load_rows()
         self.k, self.d = int(k), int(d)
         h = ctypes.c_void_p()
         st = self._lib.wpsgd_create(self.device, ctypes.c_void_p(stream.cuda_stream), self.k, self.d, ctypes.byref(h))
         if st:
             raise WpsgdError(st, "wpsgd_create", self._lib.wpsgd_last_error(None).decode())
         self._h = h
+        self._head = (h.value, self.device, stream.cuda_stream, self.d)
 
     # -- plumbing ---------------------------------------------------------------------------------------
     def _ck(self, st: int, where: str):
@@ -277,6 +293,7 @@ class Context:
         if getattr(self, "_h", None):
             self._lib.wpsgd_destroy(self._h)
             self._h = None
+            self._head = (0,) + self._head[1:]  # calls on a destroyed context are refused like those on a null one
 
     def __del__(self):
         try:
@@ -440,112 +457,36 @@ class Context:
                                                lam, loss, self._dev(out)), "wpsgd_objective_csr")
         return out
 
-    # -- operators on whole sets of rows ------------------------------------------------------------------
-    # (calls of a few microseconds: sizes are asked one by one and pointers passed as numbers, which costs less than tuples and
-    # ctypes objects)
-    def _empty(self, shape, dtype, strides=None):
-        """A tensor for the context's stream to write: allocated for that stream, so that its memory is not reused under it."""
-        torch = self._torch
-        if self._current_raw_stream(self.device) != self._raw_stream:
-            with torch.cuda.stream(self._stream):
-                return torch.empty(shape, dtype=dtype, device=self._torch_device) if strides is None else torch.empty_strided(shape, strides, dtype=dtype, device=self._torch_device)
-        if strides is None:
-            return torch.empty(shape, dtype=dtype, device=self._torch_device)
-        return torch.empty_strided(shape, strides, dtype=dtype, device=self._torch_device)
-
-    def _matrix(self, t, dtypes, cols, what):
-        """Pointer, row stride (None: a single row) and row count of a 2-D tensor of rows of `cols` contiguous elements."""
-        if not isinstance(t, self._torch.Tensor) or t.get_device() != self.device:
-            raise TypeError(f"{what}: expected a CUDA tensor on the context's device")
-        if t.dtype not in dtypes:
-            raise TypeError(f"{what}: expected dtype {' or '.join(map(str, dtypes))}, got {t.dtype}")
-        if t.dim() != 2 or t.size(1) != cols or (cols > 1 and t.stride(1) != 1):
-            raise ValueError(f"{what}: expected rows of {cols} contiguous elements, got shape {tuple(t.shape)} with strides {t.stride()}")
-        n = t.size(0)
-        return t.data_ptr(), t.stride(0) if n > 1 else None, n
-
-    def _vector(self, t, n, what):
-        """Pointer of a contiguous fp32 tensor of at least n elements."""
-        if not isinstance(t, self._torch.Tensor) or t.get_device() != self.device:
-            raise TypeError(f"{what}: expected a CUDA tensor on the context's device")
-        if t.dtype is not self._torch.float32 or not t.is_contiguous():
-            raise TypeError(f"{what}: expected a contiguous float32 tensor")
-        if t.numel() < n:
-            raise ValueError(f"{what}: {t.numel()} elements, expected {n}")
-        return t.data_ptr()
-
-    def _packed(self, q, scales, what):
-        """Arguments of packed rows: pointer, stride, scales, their stride, row count."""
-        torch = self._torch
-        qp, ld, n = self._matrix(q, (torch.float8_e4m3fn, torch.uint8), self.d, what)
-        nb = (self.d + 127) // 128
-        sp, ld_s, m = self._matrix(scales, (torch.float32,), nb, what + " scales")
-        if m != n:
-            raise ValueError(f"{what}: {n} rows, but scales of {m}")
-        return qp, packed_width(self.d) if ld is None else ld, sp, nb if ld_s is None else ld_s, n
-
+    # -- operators on whole sets of rows (arguments are checked in csrc/rows_binding.cpp) --------------------
     def quantize_rows(self, X, out=None, scales=None):
         """Rows packed to 8 bits: (e4m3 [n, d] with rows that start on 16 bytes, fp32 scales [n, ceil(d / 128)])."""
-        torch = self._torch
-        xp, ld, n = self._matrix(X, (torch.float32, torch.bfloat16), self.d, "X")
-        if out is None:
-            out = self._empty((n, self.d), torch.float8_e4m3fn, (packed_width(self.d), 1))
-        if scales is None:
-            scales = self._empty((n, (self.d + 127) // 128), torch.float32)
-        qp, ld_q, sp, ld_s, m = self._packed(out, scales, "out")
-        if m != n:
-            raise ValueError(f"out has {m} rows, X {n}")
-        st = self._lib.wpsgd_quantize_rows(self._h, xp, X_BF16 if X.dtype is torch.bfloat16 else X_F32, self.d if ld is None else ld, n, qp, ld_q, sp, ld_s)
-        if st:
-            self._ck(st, "wpsgd_quantize_rows")
-        return out, scales
+        r = self._rows.quantize_rows(*self._head, X, out, scales)
+        return r if r.__class__ is tuple else self._ck(r, "wpsgd_quantize_rows")
 
     def margins_fp8(self, Q, q_scales, M, m_scales, out=None, dtype=None):
         """Margins [n, models] of packed models M on packed rows Q, float32 (or `dtype`: bfloat16)."""
-        torch = self._torch
-        qp, ld_q, qs, ld_qs, n = self._packed(Q, q_scales, "Q")
-        mp, ld_m, ms, ld_ms, k = self._packed(M, m_scales, "M")
-        if out is None:
-            out = self._empty((n, k), dtype or torch.float32)
-        elif dtype is not None and out.dtype != dtype:
-            raise TypeError(f"out has dtype {out.dtype}, asked for {dtype}")
-        zp, ld_z, rows = self._matrix(out, (torch.float32, torch.bfloat16), k, "out")
-        if rows != n:
-            raise ValueError(f"out has {rows} rows, Q {n}")
-        st = self._lib.wpsgd_margins_fp8(self._h, qp, ld_q, qs, ld_qs, n, mp, ld_m, ms, ld_ms, k, zp, X_BF16 if out.dtype is torch.bfloat16 else X_F32,
-                                         k if ld_z is None else ld_z)
-        if st:
-            self._ck(st, "wpsgd_margins_fp8")
-        return out
-
-    def _grad_outputs(self, grad, out):
-        f32 = self._torch.float32
-        grad = self._empty((self.d,), f32) if grad is None else grad
-        out = self._empty((2,), f32) if out is None else out
-        return grad, self._vector(grad, self.d, "grad"), out, self._vector(out, 2, "out")
+        bf16 = False
+        if dtype is not None:
+            bf16 = dtype is self._torch.bfloat16
+            if not bf16 and dtype is not self._torch.float32:
+                raise TypeError(f"margins are float32 or bfloat16, not {dtype}")
+            if out is not None and out.dtype is not dtype:
+                raise TypeError(f"out has dtype {out.dtype}, asked for {dtype}")
+        r = self._rows.margins_fp8(*self._head, Q, q_scales, M, m_scales, out, bf16)
+        return r if r.__class__ is not int else self._ck(r, "wpsgd_margins_fp8")
 
     def objective_grad(self, X, y, w, lam: float, loss: int, grad=None, out=None):
         """(fp32 [2] = {objective, error}, fp32 [d] = its gradient) over all rows of X."""
-        torch = self._torch
-        xp, ld, n = self._matrix(X, (torch.float32, torch.bfloat16), self.d, "X")
-        grad, gp, out, op = self._grad_outputs(grad, out)
-        st = self._lib.wpsgd_objective_grad(self._h, xp, X_BF16 if X.dtype is torch.bfloat16 else X_F32, self.d if ld is None else ld,
-                                            self._vector(y, n, "y"), n, self._vector(w, self.d, "w"), lam, loss, gp, op)
-        if st:
-            self._ck(st, "wpsgd_objective_grad")
-        return out, grad
+        r = self._rows.objective_grad(*self._head, X, y, w, lam, loss, grad, out)
+        return r if r.__class__ is tuple else self._ck(r, "wpsgd_objective_grad")
 
     def objective_grad_fp8(self, Q, scales, y, w, lam: float, loss: int, grad=None, out=None):
         """objective_grad over packed rows."""
-        qp, ld_q, sp, ld_s, n = self._packed(Q, scales, "Q")
-        grad, gp, out, op = self._grad_outputs(grad, out)
-        st = self._lib.wpsgd_objective_grad_fp8(self._h, qp, ld_q, sp, ld_s, self._vector(y, n, "y"), n, self._vector(w, self.d, "w"), lam, loss, gp, op)
-        if st:
-            self._ck(st, "wpsgd_objective_grad_fp8")
-        return out, grad
+        r = self._rows.objective_grad_fp8(*self._head, Q, scales, y, w, lam, loss, grad, out)
+        return r if r.__class__ is tuple else self._ck(r, "wpsgd_objective_grad_fp8")
 
     def _grad_list(self, grads):
-        if not isinstance(grads, GradList):
+        if grads.__class__ is not GradList:
             grads = GradList(grads)
         if grads.device is not None and grads.device != self.device:
             raise TypeError("expected tensors on the context's device")
@@ -554,21 +495,15 @@ class Context:
     def grad_norm(self, grads, norm=None):
         """fp32 [1]: the global norm of the gradients (a GradList or a sequence of tensors)."""
         grads = self._grad_list(grads)
-        norm = self._empty((1,), self._torch.float32) if norm is None else norm
-        st = self._lib.wpsgd_grad_norm(self._h, grads._h, self._vector(norm, 1, "norm"))
-        if st:
-            self._ck(st, "wpsgd_grad_norm")
-        return norm
+        r = self._rows.grad_norm(*self._head, grads._h.value, None, norm)
+        return r if r.__class__ is not int else self._ck(r, "wpsgd_grad_norm")
 
     def clip_grad_norm(self, grads, max_norm: float, norm=None):
         """Scales the gradients down to max_norm where their global norm is above it, in place or into the list's outputs;
         returns the norm before, fp32 [1]."""
         grads = self._grad_list(grads)
-        norm = self._empty((1,), self._torch.float32) if norm is None else norm
-        st = self._lib.wpsgd_clip_grad_norm(self._h, grads._h, max_norm, self._vector(norm, 1, "norm"))
-        if st:
-            self._ck(st, "wpsgd_clip_grad_norm")
-        return norm
+        r = self._rows.grad_norm(*self._head, grads._h.value, max_norm, norm)
+        return r if r.__class__ is not int else self._ck(r, "wpsgd_clip_grad_norm")
 
     def solve_host(self, X, y, shard_off, n_steps, eta0, sched, lam, loss, seed, w0=None, r: float = 0.0, out=None):
         """Host tensors in (ideally pinned), host tensor out; copies are part of the call."""

@@ -1,4 +1,5 @@
-"""Builds libwpsgd.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libwpsgd.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _rows.so (the Python entry of the operators on
+whole sets of rows) with the host compiler."""
 from __future__ import annotations
 
 import os
@@ -9,6 +10,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwpsgd.so")
+BINDING = os.path.join(HERE, "_rows.so")
+BINDING_SOURCE = os.path.join(CSRC, "rows_binding.cpp")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["wpsgd_api.cu", "wpsgd_rows.cu"]
 
@@ -40,7 +43,32 @@ def _fresh(obj: str) -> bool:
         return False
 
 
+def build_binding(force: bool = False) -> str:
+    """_rows.so, which calls libwpsgd.so beside it; has to be built after it."""
+    read = (BINDING_SOURCE, os.path.join(os.path.dirname(HERE), "include", "wpsgd.h"))
+    if not force and os.path.exists(BINDING) and all(os.path.getmtime(BINDING) >= os.path.getmtime(f) for f in read):
+        return BINDING
+    import sysconfig
+
+    from torch.utils import cpp_extension
+
+    tmp = BINDING + f".tmp{os.getpid()}"
+    include = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")]
+    libs = cpp_extension.library_paths()
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-o", tmp, BINDING_SOURCE]
+                          + [f"-I{i}" for i in include] + [f"-L{i}" for i in libs]
+                          + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", f"-L{HERE}", "-l:libwpsgd.so", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    lib = build_library(force, verbose)
+    build_binding(force)
+    return lib
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source_mtime():
         return LIB
     os.makedirs(OBJ, exist_ok=True)
