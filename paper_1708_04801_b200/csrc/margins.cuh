@@ -6,6 +6,9 @@
 // rows and BN models, one block of 128 columns at a time; the scales differ from block to block on both sides, so each D_b is read
 // back and added to fp32 registers with its scales while the tensor cores form the next ones in other buffers.
 //
+// Few tiles with many blocks of columns: a cluster of CTAs per tile, each with a share of the blocks, whose sums meet in the first.
+// 2 rows of 5918 columns on 15 models: 16.1 us with one CTA, see margins_of for the rule.
+//
 // One persistent CTA per SM, a role per warp: warp 0 brings the tiles of Q and M into a ring of stages (TMA, 128-byte swizzle; what lies outside
 // the matrices arrives as zeros), warp 1 issues the products, warp 2 brings the scales of a block's 128 rows and BN models (cp.async) into a
 // ring of its own, warp 3 owns the tensor memory, the warps from 4 on add up. They read tensor memory in the order of a matrix fragment, four rows
@@ -39,6 +42,8 @@ struct MarginsShape {
   static constexpr int fixed_bytes = 1024 + MG_WINDOWS * MG_WINDOW * slot * 4 + 512;  // 1024: alignment of the ring
   static constexpr int stages = (227 * 1024 - fixed_bytes) / stage_bytes < 10 ? (227 * 1024 - fixed_bytes) / stage_bytes : 10;
   static constexpr int smem = fixed_bytes + stages * stage_bytes;
+  // the others' sums reach the first CTA of a cluster through its ring
+  static constexpr int max_splits = 7 * BN * MG_ROWS * 4 <= stages * stage_bytes ? 8 : 3 * BN * MG_ROWS * 4 <= stages * stage_bytes ? 4 : 1;
 };
 
 struct MarginsParams {
@@ -50,6 +55,7 @@ struct MarginsParams {
   long long ld_z;
   int n_rows, n_models, blocks;   // blocks of 128 columns
   int tiles_m, tiles;             // tiles of models per tile of rows, tiles in all
+  int splits;                     // CTAs of a cluster that share a tile's blocks of columns (1: none; more: one tile per cluster)
   bool pairs;                     // two neighbouring margins of a row share an aligned access
   long long spin_limit;
   long long drop_block;           // test hook: this block of columns is never requested (-1: none)
@@ -116,6 +122,14 @@ __device__ __forceinline__ uint64_t lds_pair(uint32_t a) {
   return v;
 }
 
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// barrier of a cluster, for warps that need not be converged
+__device__ __forceinline__ void cluster_sync_any() { asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory"); }
+
 // A wait that gives up: after its own limit, or when another role has (dead). False: leave.
 struct MarginsWait {
   long long limit;
@@ -150,7 +164,7 @@ __device__ __forceinline__ void store_pair(__nv_bfloat16* to, float2 z, int left
   }
 }
 
-template <typename OT, int BN>
+template <typename OT, int BN, bool SPLIT>
 __global__ void __launch_bounds__(MarginsShape<BN>::threads, 1)
 margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_m, const __grid_constant__ MarginsParams p) {
   using Shape = MarginsShape<BN>;
@@ -181,15 +195,16 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   const uint32_t tmem = tmem_base;
   kernel_inputs_ready();
   const MarginsWait wait{p.spin_limit, dead_flag, p.status};
-  const int nk = p.blocks;
+  const int rank = SPLIT ? blockIdx.x % p.splits : 0, first_tile = SPLIT ? blockIdx.x / p.splits : blockIdx.x, tile_step = SPLIT ? gridDim.x / p.splits : gridDim.x;
+  const int k0 = SPLIT ? (int)((long long)p.blocks * rank / p.splits) : 0, k1 = SPLIT ? (int)((long long)p.blocks * (rank + 1) / p.splits) : p.blocks;
 
   if (warp == 0) {
     if (lane == 0) {
       uint32_t it = 0;
       bool ok = true;
-      for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x) {
+      for (int t = first_tile; t < p.tiles && ok; t += tile_step) {
         const int row0 = t / p.tiles_m * MG_ROWS, m0 = t % p.tiles_m * BN;
-        for (int k = 0; k < nk; ++k, ++it) {
+        for (int k = k0; k < k1; ++k, ++it) {
           const uint32_t s = it % S;
           if (!(ok = wait(&empty[s], (it / S & 1) ^ 1, 41))) break;
           if (k == p.drop_block) continue;
@@ -207,8 +222,8 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     const uint64_t first = mma_operand((uint32_t)__cvta_generic_to_shared(ring));
     uint32_t s = 0, s_parity = 0, b = 0, b_parity = 1;
     bool ok = true;
-    for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x) {
-      for (int k = 0; k < nk; ++k) {
+    for (int t = first_tile; t < p.tiles && ok; t += tile_step) {
+      for (int k = k0; k < k1; ++k) {
         ok = wait(&full[s], s_parity, 43) && wait(&acc_empty[b], b_parity, 42);
         if (!(ok = __all_sync(0xffffffffu, ok))) break;
         tmem_fence_after();
@@ -234,22 +249,22 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     uint32_t win = 0;
     bool ok = true;
     const int ahead = lane % MG_WINDOW, sub = lane / MG_WINDOW;
-    for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x) {
+    for (int t = first_tile; t < p.tiles && ok; t += tile_step) {
       const int row0 = t / p.tiles_m * MG_ROWS, m0 = t % p.tiles_m * BN;
-      for (int k0 = 0; k0 < nk; k0 += MG_WINDOW, ++win) {
+      for (int kw = k0; kw < k1; kw += MG_WINDOW, ++win) {
         if (!(ok = wait(&sc_empty[win % SS], (win / SS & 1) ^ 1, 44))) break;
-        const int k = k0 + ahead;
+        const int k = kw + ahead;
         const uint32_t dst = (uint32_t)__cvta_generic_to_shared(scales + (win % SS * MG_WINDOW + ahead) * Shape::slot);
 #pragma unroll
         for (int i = 0; i < MG_ROWS; i += 32 / MG_WINDOW) {
           const int r = row0 + i + sub;
-          const bool in = r < p.n_rows && k < nk;
+          const bool in = r < p.n_rows && k < k1;
           cp_async4_or_zero(dst + (i + sub) * 4, p.q_scales + (in ? r * p.ld_qs + k : 0), in);
         }
 #pragma unroll
         for (int i = 0; i < BN; i += 32 / MG_WINDOW) {
           const int m = m0 + i + sub;
-          const bool in = m < p.n_models && k < nk;
+          const bool in = m < p.n_models && k < k1;
           cp_async4_or_zero(dst + (MG_ROWS + i + sub) * 4, p.m_scales + (in ? m * p.ld_ms + k : 0), in);
         }
         cp_async_arrive(&sc_full[win % SS]);
@@ -263,19 +278,19 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     const uint32_t scales_at = (uint32_t)__cvta_generic_to_shared(scales);
     uint32_t it = 0, win = 0;
     bool ok = true;
-    for (int t = blockIdx.x; t < p.tiles; t += gridDim.x) {
+    for (int t = first_tile; t < p.tiles; t += tile_step) {
       uint64_t acc[4][COLS / 8];  // row my_row + 8 i, models my_col + 8 j and the next
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < COLS / 8; ++j) acc[i][j] = 0;
-      for (int k = 0; k < nk; ++k, ++it) {
+      for (int k = k0; k < k1; ++k, ++it) {
         const uint32_t b = it % NB, q = win % SS;
-        ok = (k % MG_WINDOW || wait(&sc_full[q], win / SS & 1, 45)) && wait(&acc_full[b], it / NB & 1, 46);
+        ok = ((k - k0) % MG_WINDOW || wait(&sc_full[q], win / SS & 1, 45)) && wait(&acc_full[b], it / NB & 1, 46);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tmem_fence_after();
-        const uint32_t slot = scales_at + (q * MG_WINDOW + k % MG_WINDOW) * Shape::slot * 4;
+        const uint32_t slot = scales_at + (q * MG_WINDOW + (k - k0) % MG_WINDOW) * Shape::slot * 4;
         uint64_t rs[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -298,11 +313,32 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll
           for (int i = 0; i < 4; ++i) acc[i][c] = fma2(pair_of(v[c % 2][2 * i], v[c % 2][2 * i + 1]), mul2(rs[i], cs), acc[i][c]);
         }
-        if (k % MG_WINDOW == MG_WINDOW - 1 || k == nk - 1) {
+        if ((k - k0) % MG_WINDOW == MG_WINDOW - 1 || k == k1 - 1) {
           __syncwarp();
           if (lane == 0) mbar_arrive_one(&sc_empty[q]);
           ++win;
         }
+      }
+      if constexpr (SPLIT) {  // the cluster's sums meet in its first CTA, in the order of the blocks of columns
+        constexpr int PT = 128 * Shape::groups;
+        const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + (threadIdx.x - 128) * 8;
+        cluster_sync_any();  // rings are done with
+        if (rank > 0) {
+          uint32_t to;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to) : "r"(ring_at));
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < COLS / 8; ++j)
+              asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to + (((rank - 1) * 4 + i) * (COLS / 8) + j) * (PT * 8)), "l"(acc[i][j]) : "memory");
+        }
+        cluster_sync_any();
+        if (rank > 0) break;
+        for (int r = 1; r < p.splits; ++r)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < COLS / 8; ++j) acc[i][j] = add2(acc[i][j], lds_pair(ring_at + (((r - 1) * 4 + i) * (COLS / 8) + j) * (PT * 8)));
       }
       if (!ok) break;
       const int row = t / p.tiles_m * MG_ROWS + my_row, model = t % p.tiles_m * BN + my_col;
@@ -314,6 +350,10 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         for (int j = 0; j < COLS / 8; ++j) store_pair(to + 8 * j, halves(acc[i][j]), p.n_models - model - 8 * j, p.pairs);
       }
     }
+  }
+  if (SPLIT && warp < 4) {  // as often as the adding warps
+    cluster_sync_any();
+    cluster_sync_any();
   }
   tmem_fence_before();
   __syncthreads();

@@ -64,6 +64,25 @@ cudaError_t allow_smem(const wpsgd_ctx* c) {
   return e;
 }
 
+// launch() of clusters of `cluster` blocks
+template <typename... P, typename... A>
+cudaError_t launch_clusters(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, unsigned cluster, A&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
+}
+
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
@@ -113,7 +132,7 @@ bool encode_rows8(CUtensorMap* map, const uint8_t* base, long long d, long long 
 }
 
 template <typename OT, int BN>
-wpsgd_status launch_margins(wpsgd_ctx* c, const MarginsCall& call) {
+wpsgd_status launch_margins(wpsgd_ctx* c, const MarginsCall& call, int splits) {
   using Shape = MarginsShape<BN>;
   static_assert(Shape::stages >= 3 && Shape::smem <= (int)kSmemMax, "a ring of three stages must fit");
   CUtensorMap map_q, map_m;
@@ -125,29 +144,43 @@ wpsgd_status launch_margins(wpsgd_ctx* c, const MarginsCall& call) {
   const long long tiles = (long long)((p.n_rows + MG_ROWS - 1) / MG_ROWS) * p.tiles_m;
   if (tiles > INT32_MAX - 148 || tiles / 148 * p.blocks > INT32_MAX) return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: too many tiles");
   p.tiles = (int)tiles;
-  CU_TRY(c, (allow_smem<margins_kernel<OT, BN>>(c)));
-  CU_TRY(c, launch(margins_kernel<OT, BN>, (unsigned)std::min<long long>(tiles, 148), Shape::threads, Shape::smem, c->stream, map_q, map_m, p));
+  p.splits = splits;
+  if (splits == 1) {
+    CU_TRY(c, (allow_smem<margins_kernel<OT, BN, false>>(c)));
+    CU_TRY(c, launch(margins_kernel<OT, BN, false>, (unsigned)std::min<long long>(tiles, 148), Shape::threads, Shape::smem, c->stream, map_q, map_m, p));
+  } else if constexpr (Shape::max_splits > 1) {
+    CU_TRY(c, (allow_smem<margins_kernel<OT, BN, true>>(c)));
+    CU_TRY(c, launch_clusters(margins_kernel<OT, BN, true>, (unsigned)(tiles * splits), Shape::threads, Shape::smem, c->stream, (unsigned)splits, map_q, map_m, p));
+  }
   c->launches++;
   return WPSGD_OK;
 }
 
 template <typename OT>
 wpsgd_status margins_of(wpsgd_ctx* c, const MarginsCall& call) {
-  // Width of a tile by the time of the busiest SM, in cycles: per tile and block of columns the products (2 per model), the copies
-  // (16 KB of rows and 128 bytes per model at about 40 bytes a cycle) or the hand-over from role to role, whichever is longest.
-  auto cycles = [&](long long bn) {
+  // Width of a tile and CTAs per tile by the time of the busiest SM, in cycles: per tile and block of columns the products (2 per
+  // model), the copies (16 KB of rows and 128 bytes per model at about 40 bytes a cycle) or the hand-over from role to role (600),
+  // whichever is longest; 5000 for the sums of a cluster to meet. 2047 rows of 999 columns on 37 models, 48 tiles of 16: 5.3 us, in pairs
+  // of CTAs 6.6; 2 rows of 5918 columns on 15 models, one tile: 16.1 us by one CTA, 6.6 by eight.
+  struct Choice {
+    long long bn, splits, cycles;
+  } best = {0, 1, 0};
+  for (long long bn : {16, 32, 64, 128, 256}) {
     const long long tiles = ((call.p.n_rows + MG_ROWS - 1) / MG_ROWS) * ((call.p.n_models + bn - 1) / bn), rounds = (tiles + 147) / 148;
-    const long long step = std::max(2 * bn, (MG_ROWS + bn) * Q_BLOCK / 40);
-    return rounds * (call.p.blocks * step + 12 * bn);
-  };
-  long long best = 16;
-  for (long long bn : {32, 64, 128, 256})
-    if (cycles(bn) < cycles(best)) best = bn;
-  if (best == 16) return launch_margins<OT, 16>(c, call);
-  if (best == 32) return launch_margins<OT, 32>(c, call);
-  if (best == 64) return launch_margins<OT, 64>(c, call);
-  if (best == 128) return launch_margins<OT, 128>(c, call);
-  return launch_margins<OT, 256>(c, call);
+    const long long step = std::max({2 * bn, (MG_ROWS + bn) * Q_BLOCK / 40, 600ll});
+    const int most = bn == 16 ? MarginsShape<16>::max_splits : bn == 32 ? MarginsShape<32>::max_splits : bn == 64 ? MarginsShape<64>::max_splits : bn == 128 ? MarginsShape<128>::max_splits : 1;
+    for (long long splits : {1, 2, 4, 8}) {
+      if (splits > 1 && (splits > most || tiles * splits > 148 || call.p.blocks < 2 * splits)) continue;
+      const long long cycles = rounds * ((call.p.blocks + splits - 1) / splits * step + 12 * bn) + (splits > 1 ? 5000 : 0);
+      if (best.bn == 0 || cycles < best.cycles) best = {bn, splits, cycles};
+    }
+  }
+  const int splits = (int)best.splits;
+  if (best.bn == 16) return launch_margins<OT, 16>(c, call, splits);
+  if (best.bn == 32) return launch_margins<OT, 32>(c, call, splits);
+  if (best.bn == 64) return launch_margins<OT, 64>(c, call, splits);
+  if (best.bn == 128) return launch_margins<OT, 128>(c, call, splits);
+  return launch_margins<OT, 256>(c, call, splits);
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------------------------
@@ -242,7 +275,7 @@ const char* check_gradient(const wpsgd_ctx* c, const float* y, int64_t n_rows, c
 }
 
 // ---- norm and clipping ---------------------------------------------------------------------------------------------------
-constexpr int kFewTensors = 32, kManyTensors = 1000;  // per launch: 1 and 28 KB of kernel arguments
+constexpr int kFewTensors = 32, kManyTensors = 1072;  // per launch: 3 and 32 KB of kernel arguments (of which 32764 bytes are allowed)
 
 struct Range {
   uintptr_t lo, hi;
@@ -418,7 +451,7 @@ wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld_q, con
   if (n_rows == 0 || n_models == 0) return WPSGD_OK;
   if (!Z || ld_z < n_models || (uintptr_t)Z % element_size(zt)) return fail(c, WPSGD_ERR_INVALID_ARG, "margins_fp8: Z is NULL, not aligned to its elements, or its stride is below n_models");
   DeviceGuard guard(c->device);
-  const MarginsCall call = {Q, ld_q, M, ld_m, c->d, {q_scales, ld_qs, m_scales, ld_ms, Z, ld_z, (int)n_rows, (int)n_models, (int)blocks_of(c->d), 0, 0,
+  const MarginsCall call = {Q, ld_q, M, ld_m, c->d, {q_scales, ld_qs, m_scales, ld_ms, Z, ld_z, (int)n_rows, (int)n_models, (int)blocks_of(c->d), 0, 0, 1,
                             ld_z % 2 == 0 && (uintptr_t)Z % (2 * element_size(zt)) == 0, c->opt_spin_limit, c->opt_drop_block, c->status}};
   return zt == WPSGD_X_F32 ? margins_of<float>(c, call) : margins_of<__nv_bfloat16>(c, call);
 }

@@ -131,7 +131,7 @@ def check_margins(z, q, s, p, t, dtype):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n,m,d,pad", [
     (1, 1, 1, 0), (1, 1024, 256, 0), (7, 3, 64, 16), (129, 17, 128, 0), (128, 16, 129, 32), (300, 37, 999, 0), (64, 1, 4096, 0),
-    (1, 5, 8200, 0), (513, 130, 640, 64), (5, 300, 33, 0), (1000, 257, 256, 0), (40, 64, 2000, 0),
+    (1, 5, 8200, 0), (2, 15, 5918, 0), (130, 100, 3000, 0), (257, 30, 1500, 16), (1, 40, 20000, 0), (513, 130, 640, 64), (5, 300, 33, 0), (1000, 257, 256, 0), (40, 64, 2000, 0),
 ])
 def test_margins(P, dtype, n, m, d, pad):
     q, s, dq, ds = packed(normal((n, d), 5 * n + d), pad)
