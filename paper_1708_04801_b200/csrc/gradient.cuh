@@ -186,6 +186,44 @@ __device__ __forceinline__ void gradient_finish(const GradParams& p, int parts, 
     p.out[1] = (float)(wrong / n);
   }
 }
+// The same by one block of WARPS warps for all of few columns: slabs side by side, one barrier.
+template <int WARPS>
+__device__ __forceinline__ void gradient_finish_small(const GradParams& p, int parts, int n_sums, double (*sh)[36]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int slabs = (int)((p.d + 31) / 32), per_slab = WARPS / slabs > 1 ? WARPS / slabs : 1, first = warp / per_slab, step = WARPS / per_slab;
+  const double n = p.n_rows > 0 ? (double)p.n_rows : 1.0;
+  double ww = 0.0, loss = 0.0, wrong = 0.0;
+  for (long long i = threadIdx.x; i < p.d; i += 32 * WARPS) ww = fma((double)p.w[i], (double)p.w[i], ww);
+  for (int i = threadIdx.x; i < n_sums; i += 32 * WARPS) {
+    loss += __ldcg(p.sums + 2 * i);
+    wrong += __ldcg(p.sums + 2 * i + 1);
+  }
+  for (int slab = first; slab < slabs; slab += step) {  // more than once only where a warp has a slab to itself
+    const long long c = (long long)slab * 32 + lane;
+    double t = 0.0;
+    if (c < p.d) {
+#pragma unroll 8
+      for (int i = warp % per_slab; i < parts; i += per_slab) t += (double)__ldcg(p.part + (long long)i * p.d + c);
+      if (per_slab == 1) p.grad[c] = (float)fma((double)p.lambda, (double)p.w[c], t / n);
+    }
+    sh[warp][lane] = t;
+  }
+  ww = warp_sum_f64(ww); loss = warp_sum_f64(loss); wrong = warp_sum_f64(wrong);
+  if (lane == 0) { sh[warp][32] = ww; sh[warp][33] = loss; sh[warp][34] = wrong; }
+  __syncthreads();
+  if (per_slab > 1 && warp % per_slab == 0 && first < slabs) {
+    const long long c = (long long)first * 32 + lane;
+    double t = 0.0;
+    for (int i = 0; i < per_slab; ++i) t += sh[warp + i][lane];
+    if (c < p.d) p.grad[c] = (float)fma((double)p.lambda, (double)p.w[c], t / n);
+  }
+  if (threadIdx.x == 0) {
+    ww = loss = wrong = 0.0;
+    for (int i = 0; i < WARPS; ++i) { ww += sh[i][32]; loss += sh[i][33]; wrong += sh[i][34]; }
+    p.out[0] = (float)(0.5 * (double)p.lambda * ww + loss / n);
+    p.out[1] = (float)(wrong / n);
+  }
+}
 __global__ void __launch_bounds__(32 * GRAD_FINISH_WARPS) gradient_finish_kernel(const __grid_constant__ GradParams p, int parts, int n_sums) {
   __shared__ double sh[GRAD_FINISH_WARPS][33];
   kernel_started();
@@ -281,7 +319,7 @@ __device__ __forceinline__ float transpose_sum(float (&v)[R], int l) {
 // How rows reach the threads that work on them.
 enum RowFeed {
   FEED_ELEMENTS = 0,  // element by element into registers: rows that do not start on 16 bytes
-  FEED_UNITS = 1,     // each thread its own 16-byte units (cp.async): rows whose last unit is not whole
+  FEED_UNITS = 1,     // each thread its own 16-byte units (cp.async), with their scales: 8-bit rows, and others whose last unit is not whole
   FEED_BULK = 2       // whole rows in bulk copies. 65536 bf16 rows of 4096 columns: by units 109 us without any work on them, in bulk 85
 };
 
@@ -303,7 +341,7 @@ struct GradShape {
   static constexpr int rings = threads / 32 / warps, rows = R * (32 / lanes);
   static int bulk_slots(long long row_bytes) { return (int)std::min<long long>(8, (budget - 16) / (rings * rows * row_bytes)); }
   static constexpr int fold_bytes = groups > 1 ? threads * CH * V * 4 : 0;
-  static constexpr int finish_bytes = threads / 32 * 33 * 8;
+  static constexpr int finish_bytes = threads / 32 * 36 * 8;
   static int smem(long long row_bytes) {
     const int ring = FEED == FEED_UNITS ? unit_slots * unit_slot_bytes : FEED == FEED_BULK ? 16 + (int)(bulk_slots(row_bytes) * rings * rows * row_bytes) : 0;
     return std::max({ring, fold_bytes, finish_bytes});
@@ -405,16 +443,6 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
       for (int r = lane; r < rows; r += 32) bulk_copy_g2s(to + r * bulk_row, src + r * row_bytes, bulk_row, &full[slot]);
     }
   };
-  float scale_next[BULK && SCALED ? R : 1][BULK && SCALED ? CH : 1];
-  auto load_scales = [&](long long row0) {
-    if constexpr (BULK && SCALED) {
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < CH; ++j)
-          scale_next[r][j] = row0 + r < p.n_rows && gl + j * G < units ? __ldg(p.scales + (row0 + r) * p.ld_s + (gl + j * G) / (Q_BLOCK / 16)) : 0.0f;
-    }
-  };
   // ---- else: rows through registers, the next R on their way
   using Scalar = typename RowUnit<RT>::Scalar;  // kept as loaded: a conversion would wait for the load
   Scalar next[VEC ? 1 : R][VEC ? 1 : E];
@@ -429,7 +457,6 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
   if constexpr (BULK) {
     if (W == 1 || warp % W == 0)
       for (int i = 0; i < ring_slots; ++i) request_rows(i, ring_first + i * stride, i);
-    load_scales(first);
   } else if constexpr (VEC) {
 #pragma unroll 1
     for (int i = 0; i < S - 1; ++i) request_units(i);
@@ -443,7 +470,20 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     w[i / 2] = pair_of(__float_as_uint(has(i) ? p.w[column(i)] : 0.0f), __float_as_uint(has(i + 1) ? p.w[column(i + 1)] : 0.0f));
     acc[i / 2] = 0;
   }
-  const float w_norm = block_w_norm(p.w, p.d, cross64);
+  float w_norm;  // |w|
+  if constexpr (W > 1) {
+    w_norm = block_w_norm(p.w, p.d, cross64);
+  } else {  // narrow rows: from the group's registers
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+      const float2 h = halves(w[i]);
+      s = fma((double)h.x, (double)h.x, fma((double)h.y, (double)h.y, s));
+    }
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    w_norm = (float)sqrt(s) * 1.0001f;
+  }
   constexpr float terms = E + W + 8;  // additions a product takes part in: the thread's, 5 in the warp, W over the warps; 3 roundings for scales
 
   // losses: their margins wait, a lane each, until the warp has a full set to evaluate side by side
@@ -468,7 +508,6 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     y_next = row0 + stride + own < p.n_rows ? p.y[row0 + stride + own] : 0.0f;
     Scalar plain[VEC ? 1 : R][VEC ? 1 : E];
     const int cur = slot;
-    float scale[BULK && SCALED ? R : 1][BULK && SCALED ? CH : 1];
     if constexpr (BULK) {
       if (!dead && !mbar_wait_bounded(&full[cur], parity, p.spin_limit)) {
         dead = true;
@@ -476,13 +515,6 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
       }
       __syncwarp();
       if (++slot == ring_slots) { slot = 0; parity ^= 1; }
-      if constexpr (SCALED) {
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-          for (int j = 0; j < CH; ++j) scale[r][j] = scale_next[r][j];
-        load_scales(row0 + stride);
-      }
     } else if constexpr (VEC) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
       request_units(slot == 0 ? S - 1 : slot - 1);  // into the slot of one round ago
@@ -508,7 +540,6 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
       }
     };
     auto scale_of = [&](int r, int j) {
-      if constexpr (BULK && SCALED) return scale[r][j];
       float v;
       asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(slot_scales + ((cur * R + r) * CH + j) * (T * 4)));
       return v;
@@ -571,12 +602,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
           for (int j = 0; j < CH; ++j) {
             uint64_t x[V / 2];
             values(r, j, x);
-            double scale = 1.0;
-            if constexpr (BULK && SCALED) {
-              if (row0 + r < p.n_rows && gl + j * G < units) scale = (double)p.scales[(row0 + r) * p.ld_s + (gl + j * G) / (Q_BLOCK / 16)];
-            } else if constexpr (SCALED) {
-              scale = (double)scale_of(r, j);
-            }
+            const double scale = SCALED ? (double)scale_of(r, j) : 1.0;
 #pragma unroll
             for (int e = 0; e < V / 2; ++e) {
               const float2 xe = halves(x[e]), we = halves(w[j * (V / 2) + e]);
@@ -684,7 +710,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
   __syncthreads();
   if (!last) return;
   __threadfence();
-  for (int slab = 0; slab * 32 < p.d; ++slab) gradient_finish<T / 32>(p, gridDim.x, gridDim.x, slab, (double (*)[33])grad_smem);
+  gradient_finish_small<T / 32>(p, gridDim.x, gridDim.x, (double (*)[36])grad_smem);
 }
 
 }  // namespace wpsgd

@@ -253,9 +253,9 @@ wpsgd_status gradient(wpsgd_ctx* c, GradParams p) {
   p.part = (float*)((char*)c->rows_ws + lay.part);
   int parts = 0, n_sums = 0;
   if (p.n_rows > 0) {
-    const bool units = std::is_same<RT, Row8>::value || (aligned16(p.X) && p.ld % RowUnit<RT>::V == 0);
-    if (units && p.d % RowUnit<RT>::V == 0) s = gradient_by_width<RT, FEED_BULK>(c, p, &parts, &n_sums);
-    else if constexpr (std::is_same<RT, Row8>::value) s = gradient_by_width<RT, FEED_UNITS>(c, p, &parts, &n_sums);
+    const bool units = aligned16(p.X) && p.ld % RowUnit<RT>::V == 0;
+    if constexpr (std::is_same<RT, Row8>::value) s = gradient_by_width<RT, FEED_UNITS>(c, p, &parts, &n_sums);
+    else if (units && p.d % RowUnit<RT>::V == 0) s = gradient_by_width<RT, FEED_BULK>(c, p, &parts, &n_sums);
     else s = units ? gradient_by_width<RT, FEED_UNITS>(c, p, &parts, &n_sums) : gradient_by_width<RT, FEED_ELEMENTS>(c, p, &parts, &n_sums);
     if (s != WPSGD_OK || p.ticket) return s;
   }
