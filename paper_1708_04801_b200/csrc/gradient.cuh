@@ -422,6 +422,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     left -= stride;
   };
   // ---- FEED_BULK: the ring of this group or warp. Rows behind the last are zeros.
+  bool dead = false;  // a wait has run out: go on without waiting and without new requests
   const int ring_slots = p.slots, ring = warp / W, bulk_row = (int)(p.d * (16 / V)), bulk_slot = Shape::rows * bulk_row;
   unsigned char* ring_base = grad_smem + 16 + (size_t)ring * ring_slots * bulk_slot;
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring_base) + (L < 32 ? lane / L * (R * bulk_row) : 0) + gl * 16;  // this thread's first unit
@@ -429,7 +430,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
   const long long ring_first = ((long long)blockIdx.x * Shape::rings + ring) * Shape::rows;  // the warp's first row
   unsigned long long* full = bars + ring * 8;
   auto request_rows = [&](int slot, long long row0, long long round) {  // by one warp
-    if (row0 >= p.n_rows || round == p.drop_block) return;
+    if (row0 >= p.n_rows || round == p.drop_block || dead) return;
     const int rows = p.n_rows - row0 < Shape::rows ? (int)(p.n_rows - row0) : Shape::rows;
     unsigned char* to = ring_base + (size_t)slot * bulk_slot;
     const char* src = (const char*)p.X + row0 * row_bytes;
@@ -497,8 +498,8 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
   };
 
   int round = 0, slot = 0;
-  uint32_t parity = 0;
-  bool dead = false;
+  uint32_t parity = 0, dead_parity = 0;
+  int dead_slot = 0;
   const int own = l / (L / R);  // of the R rows, the one whose sums this lane ends with
   float y_next = first + own < p.n_rows ? p.y[first + own] : 0.0f;
   // groups within a warp go round together (shuffles over the warp)
@@ -511,6 +512,8 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     if constexpr (BULK) {
       if (!dead && !mbar_wait_bounded(&full[cur], parity, p.spin_limit)) {
         dead = true;
+        dead_slot = cur;
+        dead_parity = parity;
         set_status(p.status, DEV_TIMEOUT, 51, blockIdx.x);
       }
       __syncwarp();
@@ -662,7 +665,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
   }
   if constexpr (BULK) {
     if (dead && lane == 0 && (W == 1 || warp % W == 0))  // copies in flight land before the block ends
-      for (int i = 0; i < ring_slots; ++i) mbar_wait_bounded(&full[i], i < slot ? parity ^ 1 : parity, p.spin_limit);
+      for (int i = 0; i < ring_slots; ++i) mbar_wait_bounded(&full[i], i < dead_slot ? dead_parity ^ 1 : dead_parity, p.spin_limit);
   }
   evaluate();
 

@@ -175,9 +175,10 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   unsigned long long* bars = (unsigned long long*)(scales + MG_WINDOWS * MG_WINDOW * Shape::slot);
   unsigned long long *full = bars, *empty = full + S, *acc_full = empty + S, *acc_empty = acc_full + NB, *sc_full = acc_empty + NB, *sc_empty = sc_full + SS,
                      *drained = sc_empty + SS;
-  static_assert(8 * (2 * S + 2 * NB + 2 * SS + 1) + 8 <= 512, "barriers, tensor memory address and flag must fit");
+  static_assert(8 * (2 * S + 2 * NB + 2 * SS + 1) + 12 <= 512, "barriers, tensor memory address, flag and count must fit");
   uint32_t& tmem_base = *(uint32_t*)(drained + 1);  // (no static shared memory: the dynamic part may be all of the SM's)
   volatile int* dead_flag = (volatile int*)(drained + 1) + 1;
+  volatile uint32_t* issued = (volatile uint32_t*)(drained + 1) + 2;  // stages that the producer has gone through
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (shfl: known to be the same in all lanes)
   kernel_started();
   if (threadIdx.x == 0) {
@@ -214,8 +215,7 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           tma_load_2d(stage + MG_ROWS * Q_BLOCK, &map_m, k * Q_BLOCK, m0, &full[s]);
         }
       }
-      if (!ok)  // copies in flight land before the block ends: the last S requests
-        for (uint32_t j = it > S ? it - S : 0; j < it; ++j) mbar_wait_bounded(&full[j % S], j / S & 1, p.spin_limit);
+      *issued = it;
     }
   } else if (warp == 1) {
     // the whole warp goes through the loop, so that addresses and descriptors stay in uniform registers; one elected thread issues
@@ -239,10 +239,6 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         if (++s == S) { s = 0; s_parity ^= 1; }
         if (++b == NB) { b = 0; b_parity ^= 1; }
       }
-    }
-    if (!ok) {  // products in flight end before tensor memory is given back
-      if (elect_one()) mma_commit(drained);
-      mbar_wait_bounded(drained, 0, p.spin_limit);
     }
   } else if (warp == 2) {
     // a lane brings one of 4 blocks of 8 rows: 16 bytes of a row in one instruction
@@ -358,6 +354,17 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
+  if (*dead_flag) {  // copies and products in flight end before the block does and tensor memory is given back
+    if (warp == 0 && lane == 0) {
+      const uint32_t n = *issued;
+      for (uint32_t j = n > S ? n - S : 0; j < n; ++j) mbar_wait_bounded(&full[j % S], j / S & 1, p.spin_limit);
+    }
+    if (warp == 1 && lane == 0) {
+      mma_commit(drained);
+      mbar_wait_bounded(drained, 0, p.spin_limit);
+    }
+    __syncthreads();
+  }
   if (warp == 3) tmem_free(tmem, Shape::tmem_cols);
 }
 

@@ -573,6 +573,45 @@ def test_refusals_of_the_binding(P):
         ctx.check()
 
 
+# ---- bounded waits ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n,m,d", [(300, 40, 700), (2, 15, 5918), (40000, 16, 256)])
+def test_margins_report_a_wait_that_runs_out_and_the_context_stays_usable(P, n, m, d):
+    q, s, dq, ds = packed(normal((n, d), 1))
+    p, t, dp, dt = packed(normal((m, d), 2))
+    with P.Context(1, d) as ctx:
+        ctx.set_option("spin_limit", 2000)
+        ctx.set_option("test_drop_block", 0)   # the first block of columns of every tile is never requested
+        ctx.margins_fp8(dq, ds, dp, dt)
+        with pytest.raises(P.WpsgdError) as e:
+            ctx.check()
+        assert e.value.status_name == "TIMEOUT"
+        ctx.set_option("test_drop_block", -1)
+        ctx.set_option("spin_limit", 1 << 20)
+        z = ctx.margins_fp8(dq, ds, dp, dt)
+        ctx.check()
+    check_margins(z, q, s, p, t, torch.float32)
+
+
+@pytest.mark.parametrize("n,d", [(50000, 64), (9000, 1024), (3000, 8192)])
+def test_gradient_reports_a_wait_that_runs_out_and_the_context_stays_usable(P, n, d):
+    x, y, w = problem(n, d, LOGISTIC)
+    x, y, w = x.cuda(), y.cuda(), w.cuda()
+    with P.Context(1, d) as ctx:
+        want = ctx.objective_grad(x, y, w, 0.01, LOGISTIC)
+        ctx.check()
+        ctx.set_option("spin_limit", 2000)
+        ctx.set_option("test_drop_block", 0)   # the first rows of every ring are never requested
+        ctx.objective_grad(x, y, w, 0.01, LOGISTIC)
+        with pytest.raises(P.WpsgdError) as e:
+            ctx.check()
+        assert e.value.status_name == "TIMEOUT"
+        ctx.set_option("test_drop_block", -1)
+        ctx.set_option("spin_limit", 1 << 20)
+        again = ctx.objective_grad(x, y, w, 0.01, LOGISTIC)
+        ctx.check()
+    assert torch.equal(want[0], again[0]) and torch.equal(want[1], again[1])
+
+
 # ---- streams, graphs, a run of them together -------------------------------------------------------------------------------
 def test_first_call_inside_a_capture_is_refused_and_later_ones_are_captured(P):
     d, n = 200, 300
