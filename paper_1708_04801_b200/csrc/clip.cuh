@@ -9,7 +9,8 @@
 // very small and very large gradients come out right.
 // Bound by memory: reads the gradients once for the norm and once more, from L2 as far as they fit, for the copies. The second
 // pass therefore goes through each block's part backwards, latest read first, and all but the last 72 MB of the first pass, and
-// all of the second, is marked to leave L2 first.
+// all of the second, is marked to leave L2 first (64 tensors of 2^20 fp32 elements: 140.8 us without the marks, 138.5 with them). The
+// norm alone takes 45.7 us there, 5.9 TB/s, the second pass 92, 5.8 TB/s of reads and writes.
 #pragma once
 
 #include "common.cuh"
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(CLIP_THREADS, 8) scale_kernel(const __grid_con
 }
 
 // Both steps of a short list in one launch: a cluster of blocks that give each other their sums through distributed shared memory.
-// 16 tensors of 1024 fp32 elements: 5.0 us a call with two launches, 3.3 with one.
+// 16 tensors of 1024 fp32 elements: 6.0 us of host time a call with two launches, 3.7 with one.
 constexpr int CLIP_CLUSTER = 8;
 constexpr int CLIP_SMALL_CHUNKS = 2 * CLIP_CLUSTER;
 template <int N>

@@ -9,6 +9,10 @@
 // Few tiles with many blocks of columns: a cluster of CTAs per tile, each with a share of the blocks, whose sums meet in the first.
 // 2 rows of 5918 columns on 15 models: 16.1 us with one CTA, see margins_of for the rule.
 //
+// Bound by the rows where there are few models (262144 rows of 4096 columns on 16: 176 us, 6.4 TB/s), else by the reading back
+// of D_b: fragments leave tensor memory at some 200 bytes a cycle, 128 KB per block of columns and SM take 700 cycles, while its products
+// take 512 (65536 rows of 4096 columns on 1024 models: 472 us, 1160 TFLOP/s).
+//
 // One persistent CTA per SM, a role per warp: warp 0 brings the tiles of Q and M into a ring of stages (TMA, 128-byte swizzle; what lies outside
 // the matrices arrives as zeros), warp 1 issues the products, warp 2 brings the scales of a block's 128 rows and BN models (cp.async) into a
 // ring of its own, warp 3 owns the tensor memory, the warps from 4 on add up. They read tensor memory in the order of a matrix fragment, four rows

@@ -431,8 +431,8 @@ wpsgd_status wpsgd_quantize_rows(wpsgd_ctx* c, const void* X, wpsgd_xtype xt, in
   auto go = [&](auto tag) {
     using XT = decltype(tag);
     constexpr int U = 4, per_warp = 32 / (Q_BLOCK / XVec<XT>::V);
-    if (vec) launch(quantize_rows_kernel<XT, U>, grid_for(n_rows * nb, 8 * U * per_warp, 148 * 8), 256, 0, c->stream, (const XT*)X, ld_elems, n_rows, c->d, (int)nb, Q, ld_q, scales, ld_s);
-    else launch(quantize_elements_kernel<XT, U>, grid_for(n_rows * nb, 8 * U, 148 * 8), 256, 0, c->stream, (const XT*)X, ld_elems, n_rows, c->d, (int)nb, Q, ld_q, scales, ld_s);
+    if (vec) launch(quantize_rows_kernel<XT, U>, grid_for(n_rows * nb, 8 * U * per_warp, 148 * 4), 256, 0, c->stream, (const XT*)X, ld_elems, n_rows, c->d, (int)nb, Q, ld_q, scales, ld_s);
+    else launch(quantize_elements_kernel<XT, U>, grid_for(n_rows * nb, 8 * U, 148 * 4), 256, 0, c->stream, (const XT*)X, ld_elems, n_rows, c->d, (int)nb, Q, ld_q, scales, ld_s);
   };
   if (xt == WPSGD_X_F32) go(float());
   else go(__nv_bfloat16());
