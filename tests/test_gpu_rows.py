@@ -265,7 +265,8 @@ def test_gradient(P, loss, kind, n, d):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
-@pytest.mark.parametrize("d,pad,offset", [(64, 1, 0), (256, 0, 1), (512, 8, 0), (1000, 3, 5), (2050, 6, 2), (4096, 16, 8)])
+@pytest.mark.parametrize("d,pad,offset", [(64, 1, 0), (256, 0, 1), (512, 8, 0), (1000, 3, 5), (2050, 6, 2), (4096, 16, 8), (33, 70, 1),
+                                          (1, 0, 3), (7, 101, 0), (999, 101, 3), (5001, 77, 1), (8191, 0, 1), (130, 33, 7)])
 def test_gradient_of_rows_of_any_stride_and_alignment(P, kind, d, pad, offset):
     n = 77
     x, y, w = problem(n, d, LOGISTIC)
