@@ -255,8 +255,7 @@ wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* ctx, const uint8_t* Q, int64_t ld_q, c
 wpsgd_status wpsgd_objective_grad(wpsgd_ctx* ctx, const void* X, wpsgd_xtype xt, int64_t ld_elems, const float* y, int64_t n_rows,
                                   const float* w, float lambda, wpsgd_loss loss, float* grad, float* out);
 
-/* The same on packed rows (Q, scales as wpsgd_quantize_rows makes them; w, grad and out as above). The 16-byte unit that holds a
- * row's last byte is read whole. */
+/* The same on packed rows (Q, scales as wpsgd_quantize_rows makes them; w, grad and out as above). */
 wpsgd_status wpsgd_objective_grad_fp8(wpsgd_ctx* ctx, const uint8_t* Q, int64_t ld_q, const float* scales, int64_t ld_s,
                                       const float* y, int64_t n_rows, const float* w, float lambda, wpsgd_loss loss, float* grad,
                                       float* out);

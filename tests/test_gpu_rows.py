@@ -613,6 +613,53 @@ def test_gradient_reports_a_wait_that_runs_out_and_the_context_stays_usable(P, n
     assert torch.equal(want[0], again[0]) and torch.equal(want[1], again[1])
 
 
+def test_calls_on_a_destroyed_context_are_refused(P):
+    x = torch.zeros(4, 100).cuda()
+    ctx = P.Context(1, 100)
+    q, s = ctx.quantize_rows(x)
+    ctx.destroy()
+    for call in (lambda: ctx.quantize_rows(x), lambda: ctx.margins_fp8(q, s, q, s), lambda: ctx.grad_norm([x]), lambda: ctx.clip_grad_norm([x], 1.0),
+                 lambda: ctx.objective_grad(x, x[:, 0].contiguous(), x[0], 0.1, HINGE), lambda: ctx.objective_grad_fp8(q, s, x[:, 0].contiguous(), x[0], 0.1, HINGE)):
+        with pytest.raises(P.WpsgdError) as e:
+            call()
+        assert e.value.status_name == "INVALID_ARG"
+
+
+def test_two_graphs_of_two_contexts_replayed_at_once(P):
+    # each context has its own workspace, so its graph may run beside the other's
+    d, n = 700, 30000
+    sides = []
+    for i in range(2):
+        x, y, w = (t.cuda() for t in problem(n, d, LOGISTIC, seed=10 * i))
+        stream = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            ctx = P.Context(1, d, stream=stream)
+            want = ctx.objective_grad(x, y, w, 0.01, LOGISTIC)
+            grads = [torch.randn(200000, device="cuda") for _ in range(3)]
+            outs, norm = [torch.empty_like(g) for g in grads], torch.empty(1).cuda()
+            lists = P.GradList(grads, outs)
+            ctx.grad_norm(lists)
+            grad, out = torch.empty(d).cuda(), torch.empty(2).cuda()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                ctx.objective_grad(x, y, w, 0.01, LOGISTIC, grad=grad, out=out)
+                ctx.clip_grad_norm(lists, 1.0, norm=norm)
+        sides.append((stream, ctx, graph, want, grad, out, grads, outs, norm, (x, y, w, lists)))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for stream, _, graph, *_ in sides:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, ctx, graph, want, grad, out, grads, outs, norm, _ in sides:
+        ctx.check()
+        assert torch.equal(want[0], out) and torch.equal(want[1], grad)
+        check_clip(norm, outs, grads, 1.0)
+        del graph
+        ctx.destroy()
+
+
 # ---- streams, graphs, a run of them together -------------------------------------------------------------------------------
 def test_first_call_inside_a_capture_is_refused_and_later_ones_are_captured(P):
     d, n = 200, 300
