@@ -5,16 +5,16 @@
 //
 // Rows fp32, bf16, or 8-bit with a scale for each block of 128 columns (x = scale q, as quantize.cuh makes them).
 //
-// One pass over the rows (gradient_rows_kernel): a group of threads holds R rows in registers, each thread its columns of them; the
-// margins are summed over the group, and the same registers are then added, times L', to the thread's columns of the gradient. A group is a
-// part of a warp for narrow rows and up to 16 warps for wide ones, so that a thread holds one to four 16-byte units of a row; the next R
-// rows are requested before the present ones are worked on. Rows wider than that (16384 columns, fp32 8192) take two passes
+// One pass over the rows (gradient_rows_kernel): a group of threads takes R rows at a time from shared memory, each thread its columns of them;
+// the margins are summed over the group, and the rows are then read again and added, times L', to the gradient, whose columns each
+// thread keeps in registers. A group is a part of a warp for narrow rows and up to 16 warps for wide ones, so that a thread has one to
+// four 16-byte units of a row; the rows after the next are requested while the present ones are worked on. Rows wider than that (16384 columns, fp32 8192) take two passes
 // (gradient_margins_kernel, gradient_columns_kernel). Either way each block leaves a partial gradient, and
 // gradient_finish_kernel adds those up in fp64 in block order. Nothing depends on timing.
 //
 // Bound by the read of the rows as far as the instructions allow: two packed multiply-adds per pair of elements for the margin and its
 // bound, one for the gradient, and the widening of bf16 and 8-bit values, twice, because widened rows would not fit the registers.
-// 131072 fp32 rows of 4096 columns 335 us (6.4 TB/s), 262144 bf16 rows 402 to 450 us (5.3 to 4.8 TB/s), 131072 8-bit rows of 999 columns
+// 131072 fp32 rows of 4096 columns 335 us (6.4 TB/s), 262144 bf16 rows 402 to 450 us (5.3 to 4.8 TB/s, the less the longer the GPU has been at work), 131072 8-bit rows of 999 columns
 // 62 us (2.2 TB/s: about 160 instructions per 16 elements).
 //
 // Hinge losses and signs jump: L' where y z = 1, the error where z = 0. The fp32 sum of a margin is off by at most
