@@ -245,6 +245,7 @@ __global__ void __cluster_dims__(CLIP_CLUSTER, 1, 1) __launch_bounds__(CLIP_THRE
 clip_small_kernel(const __grid_constant__ TensorList<N> list, bool scale, double max_norm, bool in_place, float* __restrict__ norm_out) {
   __shared__ double sh[CLIP_THREADS / 32];
   __shared__ double sums[CLIP_CLUSTER];
+  asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");  // start-up, waited for below
   kernel_started();
   kernel_inputs_ready();
   double sum = 0.0;
@@ -254,6 +255,7 @@ clip_small_kernel(const __grid_constant__ TensorList<N> list, bool scale, double
     sum += list.elems_type[i] & 1 ? chunk_squares((const __nv_bfloat16*)list.src[i], n, chunk, to_go <= kept) : chunk_squares((const float*)list.src[i], n, chunk, to_go <= kept);
   });
   sum = block_sum_f64(sum, sh);
+  asm volatile("barrier.cluster.wait;" ::: "memory");  // every block of the cluster runs, so its shared memory is there
   if (threadIdx.x < CLIP_CLUSTER) {
     uint32_t to;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(sums + blockIdx.x)), "r"(threadIdx.x));

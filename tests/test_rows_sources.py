@@ -1,0 +1,36 @@
+"""Rules of the memory model that no run shows reliably, looked up in the kernels' sources."""
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1708_04801_b200", "csrc")
+
+
+def kernels():
+    """(file, name, body without comments) of every __global__ function."""
+    for f in sorted(os.listdir(CSRC)):
+        if not f.endswith((".cu", ".cuh")):
+            continue
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, f)).read())
+        for m in re.finditer(r"__global__\s+void", text):
+            start = text.index("{", m.end())
+            depth, end = 1, start + 1
+            while depth:
+                depth += {"{": 1, "}": -1}.get(text[end], 0)
+                end += 1
+            yield f, re.search(r"(\w*kernel\w*)\s*\(", text[m.end():start]).group(1), text[start:end]
+
+
+REMOTE = [(f, name, body) for f, name, body in kernels() if "mapa." in body]
+
+
+def test_kernels_that_reach_other_blocks_shared_memory_are_found():
+    assert {name for _, name, _ in REMOTE} >= {"clip_small_kernel", "margins_kernel"}
+
+
+@pytest.mark.parametrize("name,body", [(name, body) for _, name, body in REMOTE], ids=[name for _, name, _ in REMOTE])
+def test_no_block_reaches_anothers_shared_memory_before_all_of_the_cluster_run(name, body):
+    # a block's shared memory exists from its start on: a barrier of the cluster lies before the first access
+    before = body[:body.index("mapa.")]
+    assert re.search(r"barrier\.cluster\.wait|cluster_sync_any\(\)|cluster_barrier\(\)|cluster_wait\(\)", before)
