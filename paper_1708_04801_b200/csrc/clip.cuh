@@ -83,7 +83,7 @@ __device__ __forceinline__ double chunk_squares(const T* src, long long n, int c
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       raw[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (u + i * CLIP_THREADS < u1) raw[i] = keep ? __ldg(body + u + i * CLIP_THREADS) : __ldcs(body + u + i * CLIP_THREADS);
+      if (u + i * CLIP_THREADS < u1) raw[i] = keep ? body[u + i * CLIP_THREADS] : __ldcs(body + u + i * CLIP_THREADS);  // (ordinary loads: clip_small_kernel writes in place)
     }
     const float s = batch_squares<T>(raw, U);
     if (s > 0x1p-80f && s < 0x1p120f) sum += (double)s;

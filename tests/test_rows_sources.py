@@ -34,3 +34,9 @@ def test_no_block_reaches_anothers_shared_memory_before_all_of_the_cluster_run(n
     # a block's shared memory exists from its start on: a barrier of the cluster lies before the first access
     before = body[:body.index("mapa.")]
     assert re.search(r"barrier\.cluster\.wait|cluster_sync_any\(\)|cluster_barrier\(\)|cluster_wait\(\)", before)
+
+
+def test_gradients_that_a_kernel_scales_in_place_are_not_read_past_the_coherent_caches():
+    # ld.global.nc is for memory that nothing writes while the kernel runs; clip_small_kernel reads and writes the same gradients
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "clip.cuh")).read())
+    assert "chunk_squares" in text and not re.search(r"__ldg|ld\.global\.nc|ld_stream16", text)
