@@ -364,6 +364,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
   __shared__ double cross64[T / 32];
   __shared__ double sums[2][T / 32];
   __shared__ unsigned long long bars[BULK ? Shape::rings * 8 : 1];
+  __shared__ bool gave_up[2][BULK && W > 1 ? Shape::groups : 1];  // in an even or odd round, by a warp of the group
   kernel_started();
   if constexpr (BULK) {
     if (threadIdx.x == 0) {
@@ -371,6 +372,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
       mbar_fence_init();
     }
     if (threadIdx.x < 4) ((uint32_t*)grad_smem)[threadIdx.x] = 0u;
+    if (W > 1 && threadIdx.x < 2 * Shape::groups) (&gave_up[0][0])[threadIdx.x] = false;
     __syncthreads();
   }
   kernel_inputs_ready();
@@ -427,7 +429,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     left -= stride;
   };
   // ---- FEED_BULK: the ring of this group or warp. Rows behind the last are zeros.
-  bool dead = false;  // a wait has run out: go on without waiting and without new requests
+  int dead = -1;  // round in which a wait ran out: go on without waiting and without new requests. The same in a warp, and in a group after a round's barrier
   const int ring_slots = p.slots, ring = warp / W, bulk_row = (int)(p.d * (16 / V)), bulk_slot = Shape::rows * bulk_row;
   unsigned char* ring_base = grad_smem + 16 + (size_t)ring * ring_slots * bulk_slot;
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring_base) + (L < 32 ? lane / L * (R * bulk_row) : 0) + gl * 16;  // this thread's first unit
@@ -435,7 +437,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
   const long long ring_first = ((long long)blockIdx.x * Shape::rings + ring) * Shape::rows;  // the warp's first row
   unsigned long long* full = bars + ring * 8;
   auto request_rows = [&](int slot, long long row0, long long round) {  // by one warp
-    if (row0 >= p.n_rows || round == p.drop_block || dead) return;
+    if (row0 >= p.n_rows || round == p.drop_block || dead >= 0) return;
     const int rows = p.n_rows - row0 < Shape::rows ? (int)(p.n_rows - row0) : Shape::rows;
     unsigned char* to = ring_base + (size_t)slot * bulk_slot;
     const char* src = (const char*)p.X + row0 * row_bytes;
@@ -503,8 +505,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
   };
 
   int round = 0, slot = 0;
-  uint32_t parity = 0, dead_parity = 0;
-  int dead_slot = 0;
+  uint32_t parity = 0;
   const int own = l / (L / R);  // of the R rows, the one whose sums this lane ends with
   float y_next = first + own < p.n_rows ? p.y[first + own] : 0.0f;
   // groups within a warp go round together (shuffles over the warp)
@@ -515,13 +516,11 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     Scalar plain[VEC ? 1 : R][VEC ? 1 : E];
     const int cur = slot;
     if constexpr (BULK) {
-      if (!dead && !mbar_wait_bounded(&full[cur], parity, p.spin_limit)) {
-        dead = true;
-        dead_slot = cur;
-        dead_parity = parity;
-        set_status(p.status, DEV_TIMEOUT, 51, blockIdx.x);
+      if (dead < 0 && !__all_sync(0xffffffffu, mbar_wait_bounded(&full[cur], parity, p.spin_limit))) {  // (the lanes' waits may end differently)
+        dead = round;
+        if (W > 1) gave_up[round & 1][group] = true;
+        if (lane == 0) set_status(p.status, DEV_TIMEOUT, 51, blockIdx.x);
       }
-      __syncwarp();
       if (++slot == ring_slots) { slot = 0; parity ^= 1; }
     } else if constexpr (VEC) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
@@ -586,6 +585,7 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
       if (l % (L / R) == 0) cross[round & 1][warp][own] = make_float2(zs, xs);
       group_barrier();
       if constexpr (BULK) {  // the rows of one round ago are done with
+        if (dead < 0 && gave_up[round & 1][group]) dead = round;  // (a warp that is ahead by a round writes the other flag)
         if (round > 0 && round % W == warp - group * W) request_rows(cur == 0 ? ring_slots - 1 : cur - 1, row0 + (ring_slots - 1) * stride, round + ring_slots - 1ll);
       }
       zs = xs = 0.0f;
@@ -669,8 +669,8 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     }
   }
   if constexpr (BULK) {
-    if (dead && lane == 0 && (W == 1 || warp % W == 0))  // copies in flight land before the block ends
-      for (int i = 0; i < ring_slots; ++i) mbar_wait_bounded(&full[i], i < dead_slot ? dead_parity ^ 1 : dead_parity, p.spin_limit);
+    if (dead >= 0 && lane == 0 && (W == 1 || warp % W == 0))  // copies in flight land before the block ends
+      for (int i = dead; i < dead + ring_slots; ++i) mbar_wait_bounded(&full[i % ring_slots], i / ring_slots & 1, p.spin_limit);
   }
   evaluate();
 

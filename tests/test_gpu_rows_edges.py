@@ -30,3 +30,32 @@ def test_norms_of_short_lists_call_after_call(P, tensors):
         ctx.check()
     # squares of at most 16 elements a thread in fp32 (products and additions: 16 u), half of it in the root, rounded once; the rest in fp64
     assert bool((norms == norms[0]).all()) and abs(float(norms[0]) - want) <= 10 * U * want
+
+
+# ---- waits that run out ------------------------------------------------------------------------------------------------------
+def rows_problem(n, d, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(n, d, generator=g, device="cuda") / math.sqrt(d)
+    w = torch.randn(d, generator=g, device="cuda")
+    return x, torch.where(torch.randn(n, generator=g, device="cuda") >= 0, 1.0, -1.0), w
+
+
+@pytest.mark.parametrize("round_lost", [1, 3, 6])
+@pytest.mark.parametrize("n,d", [(600000, 16), (300000, 64), (40000, 1024), (9000, 4096), (4000, 8192)])
+def test_gradient_after_a_wait_that_runs_out_in_the_middle(P, n, d, round_lost):
+    # the rows of a later round never come: by then every slot of the rings has been used and others are on their way
+    x, y, w = rows_problem(n, d)
+    with P.Context(1, d) as ctx:
+        want = ctx.objective_grad(x, y, w, 0.01, 1)
+        ctx.check()
+        ctx.set_option("spin_limit", 2000)
+        ctx.set_option("test_drop_block", round_lost)
+        ctx.objective_grad(x, y, w, 0.01, 1)
+        with pytest.raises(P.WpsgdError) as e:
+            ctx.check()
+        assert e.value.status_name == "TIMEOUT"
+        ctx.set_option("test_drop_block", -1)
+        ctx.set_option("spin_limit", 1 << 20)
+        again = ctx.objective_grad(x, y, w, 0.01, 1)
+        ctx.check()
+    assert torch.equal(want[0], again[0]) and torch.equal(want[1], again[1])

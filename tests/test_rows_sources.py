@@ -40,3 +40,11 @@ def test_gradients_that_a_kernel_scales_in_place_are_not_read_past_the_coherent_
     # ld.global.nc is for memory that nothing writes while the kernel runs; clip_small_kernel reads and writes the same gradients
     text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "clip.cuh")).read())
     assert "chunk_squares" in text and not re.search(r"__ldg|ld\.global\.nc|ld_stream16", text)
+
+
+def test_waits_of_whole_warps_end_alike_in_all_lanes():
+    # a bounded wait can run out in one lane and not in the next; what follows has barriers of the warp, so the outcome is put to a vote
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "gradient.cuh")).read())
+    loop = text[text.index("gradient_rows_kernel(const"):text.index("evaluate();\n\n")]
+    waits = [loop[max(0, m.start() - 40):m.start()] for m in re.finditer(r"mbar_wait_bounded\(&full\[cur\]", loop)]
+    assert waits and all("__all_sync(0xffffffffu, " in w for w in waits)
