@@ -363,9 +363,10 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       const uint32_t n = *issued;
       for (uint32_t j = n > S ? n - S : 0; j < n; ++j) mbar_wait_bounded(&full[j % S], j / S & 1, p.spin_limit);
     }
-    if (warp == 1 && lane == 0) {
-      mma_commit(drained);
-      mbar_wait_bounded(drained, 0, p.spin_limit);
+    if (warp == 1) {
+      if (elect_one()) mma_commit(drained);  // by the thread that issued the products: a commit covers its own alone
+      __syncwarp();
+      if (lane == 0) mbar_wait_bounded(drained, 0, p.spin_limit);
     }
     __syncthreads();
   }

@@ -48,3 +48,14 @@ def test_waits_of_whole_warps_end_alike_in_all_lanes():
     loop = text[text.index("gradient_rows_kernel(const"):text.index("evaluate();\n\n")]
     waits = [loop[max(0, m.start() - 40):m.start()] for m in re.finditer(r"mbar_wait_bounded\(&full\[cur\]", loop)]
     assert waits and all("__all_sync(0xffffffffu, " in w for w in waits)
+
+
+def test_products_are_issued_and_committed_by_the_same_thread():
+    # tcgen05.commit covers the products of the thread that executes it, and which lane elect.sync chooses is not specified
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "margins.cuh")).read())
+    kernel = text[text.index("margins_kernel("):]
+    uses = [m.start() for m in re.finditer(r"mma_commit\(|mma_e4m3\(", kernel)]
+    assert len(uses) == 4
+    for at in uses:
+        last = max(kernel.rfind("elect_one()", 0, at), kernel.rfind("lane == 0", 0, at))
+        assert kernel.startswith("elect_one()", last)
