@@ -31,6 +31,9 @@ __device__ __forceinline__ bool mbar_wait_bounded(unsigned long long* bar, uint3
     if (mbar_try_wait(bar, parity)) return true;
   return false;
 }
+// Polls for what is in flight when a block leaves after a wait that ran out, whatever the limit of that wait was: shared memory that a copy still
+// writes, or products still read, must not pass to the next block.
+constexpr long long DRAIN_LIMIT = 1 << 20;
 // One contiguous global -> shared copy (no multicast); bytes a multiple of 16, both addresses 16-byte aligned.
 __device__ __forceinline__ void bulk_copy_g2s(void* smem_dst, const void* gmem_src, uint32_t bytes, unsigned long long* bar) {
   const uint32_t d = (uint32_t)__cvta_generic_to_shared(smem_dst), b = (uint32_t)__cvta_generic_to_shared(bar);

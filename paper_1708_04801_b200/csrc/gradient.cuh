@@ -669,8 +669,11 @@ gradient_rows_kernel(const __grid_constant__ GradParams p) {
     }
   }
   if constexpr (BULK) {
-    if (dead >= 0 && lane == 0 && (W == 1 || warp % W == 0))  // copies in flight land before the block ends
-      for (int i = dead; i < dead + ring_slots; ++i) mbar_wait_bounded(&full[i % ring_slots], i / ring_slots & 1, p.spin_limit);
+    if (dead >= 0 && lane == 0 && (W == 1 || warp % W == 0)) {  // copies in flight land before the block ends
+      const int requested = dead + ring_slots - (W > 1 && dead > 0 ? 1 : 0);  // rounds; larger groups request in the round after
+      for (int i = dead; i < requested; ++i)
+        if (ring_first + i * stride < p.n_rows && i != p.drop_block) mbar_wait_bounded(&full[i % ring_slots], i / ring_slots & 1, DRAIN_LIMIT);
+    }
   }
   evaluate();
 

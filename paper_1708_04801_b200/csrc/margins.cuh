@@ -361,12 +361,13 @@ margins_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   if (*dead_flag) {  // copies and products in flight end before the block does and tensor memory is given back
     if (warp == 0 && lane == 0) {
       const uint32_t n = *issued;
-      for (uint32_t j = n > S ? n - S : 0; j < n; ++j) mbar_wait_bounded(&full[j % S], j / S & 1, p.spin_limit);
+      for (uint32_t j = n > S ? n - S : 0; j < n; ++j)
+        if (k0 + j % (uint32_t)(k1 - k0) != p.drop_block) mbar_wait_bounded(&full[j % S], j / S & 1, DRAIN_LIMIT);
     }
     if (warp == 1) {
       if (elect_one()) mma_commit(drained);  // by the thread that issued the products: a commit covers its own alone
       __syncwarp();
-      if (lane == 0) mbar_wait_bounded(drained, 0, p.spin_limit);
+      if (lane == 0) mbar_wait_bounded(drained, 0, DRAIN_LIMIT);
     }
     __syncthreads();
   }

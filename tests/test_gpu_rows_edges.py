@@ -59,3 +59,59 @@ def test_gradient_after_a_wait_that_runs_out_in_the_middle(P, n, d, round_lost):
         again = ctx.objective_grad(x, y, w, 0.01, 1)
         ctx.check()
     assert torch.equal(want[0], again[0]) and torch.equal(want[1], again[1])
+
+
+def packed_normal(n, d, seed):
+    """8-bit rows and scales made by torch on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(n, d, generator=g, device="cuda")
+    nb = -(-d // 128)
+    a = torch.nn.functional.pad(x, (0, nb * 128 - d)).view(n, nb, 128).abs().amax(2)
+    q = torch.zeros(n, -(-d // 16) * 16, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)[:, :d]
+    q.copy_((x * (448.0 / a).repeat_interleave(128, 1)[:, :d]).to(torch.float8_e4m3fn))
+    return q, a / 448.0
+
+
+LIMITS = [1, 2, 3, 5, 8, 13, 21, 34, 55, 89, 144, 1000]
+
+
+@pytest.mark.parametrize("n,d", [(600000, 16), (40000, 1024), (9000, 4096), (4000, 8192)])
+def test_gradient_with_waits_that_run_out_here_and_there(P, n, d):
+    # limits so low that rows on their way are given up: reported, or the result is whole; what comes after is as before
+    x, y, w = rows_problem(n, d)
+    with P.Context(1, d) as ctx:
+        want = ctx.objective_grad(x, y, w, 0.01, 1)
+        ctx.check()
+        for limit in LIMITS:
+            ctx.set_option("spin_limit", limit)
+            got = ctx.objective_grad(x, y, w, 0.01, 1)
+            try:
+                ctx.check()
+                assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+            except P.WpsgdError as e:
+                assert e.status_name == "TIMEOUT"
+            ctx.set_option("spin_limit", 1 << 20)
+            again = ctx.objective_grad(x, y, w, 0.01, 1)
+            ctx.check()
+            assert torch.equal(want[0], again[0]) and torch.equal(want[1], again[1])
+
+
+@pytest.mark.parametrize("n,m,d", [(2, 15, 5918), (40000, 16, 1024), (9000, 1000, 2000)])
+def test_margins_with_waits_that_run_out_here_and_there(P, n, m, d):
+    q, s = packed_normal(n, d, 1)
+    p, t = packed_normal(m, d, 2)
+    with P.Context(1, d) as ctx:
+        want = ctx.margins_fp8(q, s, p, t)
+        ctx.check()
+        for limit in LIMITS:
+            ctx.set_option("spin_limit", limit)
+            got = ctx.margins_fp8(q, s, p, t)
+            try:
+                ctx.check()
+                assert torch.equal(want, got)
+            except P.WpsgdError as e:
+                assert e.status_name == "TIMEOUT"
+            ctx.set_option("spin_limit", 1 << 20)
+            again = ctx.margins_fp8(q, s, p, t)
+            ctx.check()
+            assert torch.equal(want, again)

@@ -59,3 +59,13 @@ def test_products_are_issued_and_committed_by_the_same_thread():
     for at in uses:
         last = max(kernel.rfind("elect_one()", 0, at), kernel.rfind("lane == 0", 0, at))
         assert kernel.startswith("elect_one()", last)
+
+
+def test_what_is_in_flight_is_waited_for_whatever_the_limit_of_the_other_waits():
+    # "spin_limit" may be 1: a block that gave up after one poll still has to let its copies and products end before its memory passes on
+    for f, kernel, drains in (("gradient.cuh", "gradient_rows_kernel(const", 1), ("margins.cuh", "margins_kernel(const", 2)):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, f)).read())
+        text = text[text.index(kernel):]
+        after = text[text.index("dead_flag) {" if f == "margins.cuh" else "if (dead >= 0 && lane == 0"):]
+        waits = re.findall(r"mbar_wait_bounded\((.*?), (\S+)\);", after)
+        assert len(waits) == drains and all(limit == "DRAIN_LIMIT" for _, limit in waits)
