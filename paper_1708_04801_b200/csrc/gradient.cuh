@@ -111,10 +111,10 @@ __device__ __forceinline__ double exact_product(const GradParams& p, long long r
 }
 
 // Bound of the fp32 margin's error, see above. 1.01: the norms are fp32 sums themselves, and the root may be off by 2^-10;
-// 2^-120: products below fp32's range.
+// 2^-110: squares below fp32's range, of which each loses 2^-150 at most (2^40 of them); 2^-120: products below it.
 __device__ __forceinline__ float margin_error(float terms, float w_norm, float x_squares) {
   float root;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(x_squares));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(x_squares + 0x1p-110f));
   return w_norm > 0.0f ? fmaf(terms * 0x1p-24f * 1.01f * w_norm, root, 0x1p-120f) : 0.0f;
 }
 // Whether an error of `err` in z could move the row across a jump of the loss's derivative or of the sign.

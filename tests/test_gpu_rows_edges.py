@@ -115,3 +115,75 @@ def test_margins_with_waits_that_run_out_here_and_there(P, n, m, d):
             again = ctx.margins_fp8(q, s, p, t)
             ctx.check()
             assert torch.equal(want, again)
+
+
+# ---- decisions at the jumps, at the ends of fp32's range ----------------------------------------------------------------------
+HINGE = 0
+KINDS = ["f32", "bf16", "e4m3", "two passes"]
+
+
+def rows_of(kind, x):
+    """(rows and scales as the entry points take them, their values in 64 bits)"""
+    if kind == "e4m3":
+        n, d = x.shape
+        nb = -(-d // 128)
+        a = torch.nn.functional.pad(x, (0, nb * 128 - d)).view(n, nb, 128).abs().amax(2)
+        q = torch.zeros(n, -(-d // 16) * 16, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)[:, :d]
+        q.copy_((x * torch.div(torch.full_like(a, 448.0), a).repeat_interleave(128, 1)[:, :d]).to(torch.float8_e4m3fn))
+        s = a / 448.0
+        return (q, s), q.float().double() * s.double().repeat_interleave(128, 1)[:, :d]
+    x = x.to(torch.bfloat16 if kind == "bf16" else torch.float32)
+    return (x,), x.double()
+
+
+def decided(ctx, kind, rows, values, y, w):
+    """Error count and gradient (lambda 0) are those of margins summed in 64 bits."""
+    fn = ctx.objective_grad_fp8 if kind == "e4m3" else ctx.objective_grad
+    out, grad = fn(*rows, y, w, 0.0, HINGE)
+    ctx.check()
+    n, yd = values.shape[0], y.double()
+    z = values @ w.double()
+    wrong = ((z >= 0) != (yd >= 0)).double().mean()
+    assert float(out[1]) == float(wrong.float())
+    g = torch.where(yd * z < 1, -yd, torch.zeros_like(yd))
+    want, size = values.T @ g / n, values.abs().T @ g.abs() / n
+    # a row's part of the gradient: its product and at most n additions; the result 2. Divided by the largest: squares of 2^-80 are out of range
+    assert bool(((grad.double() - want).abs() <= (n + 4) * U * size).all())
+
+
+def width(kind, d):
+    return 8200 + d if kind == "two passes" else d
+
+
+@pytest.mark.parametrize("power", [0, -60, -80, -90, 60])
+@pytest.mark.parametrize("d", [64, 700])
+@pytest.mark.parametrize("kind", KINDS)
+def test_hinge_is_decided_as_exact_sums_do_whatever_the_size_of_the_rows(P, kind, d, power):
+    # rows of size 2^power on a model of size 2^-power, margins within a few units of rounding of the hinge
+    n, d = 400, width(kind, d)
+    g = torch.Generator(device="cuda").manual_seed(d + power)
+    rows, values = rows_of(kind, torch.randn(n, d, generator=g, device="cuda") / math.sqrt(d) * 2.0 ** power)
+    w = torch.randn(d, generator=g, device="cuda") * 2.0 ** -power
+    y = (1 / (values @ w.double())).float()
+    assert float((y.double() * (values @ w.double()) - 1).abs().max()) < 2.0 ** -22
+    with P.Context(1, d) as ctx:
+        decided(ctx, kind, rows, values, y, w)
+
+
+@pytest.mark.parametrize("power", [0, -60, -80, -90, 60])
+@pytest.mark.parametrize("d", [64, 700])
+@pytest.mark.parametrize("kind", KINDS)
+def test_signs_are_those_of_exact_sums_whatever_the_size_of_the_rows(P, kind, d, power):
+    # the second half of each row undoes the first but for a rounding: what is left of the margin is smaller than the error of an fp32 sum
+    n, d = 400, width(kind, d) // 2 * 2
+    g = torch.Generator(device="cuda").manual_seed(d + power)
+    half = torch.randn(n, d // 2, generator=g, device="cuda")
+    w = torch.randn(d, generator=g, device="cuda")
+    w[d // 2:] = w[:d // 2] * (1 + torch.randn(d // 2, generator=g, device="cuda") * 2.0 ** -23)
+    rows, values = rows_of(kind, torch.cat([half, -half], 1) * 2.0 ** power)
+    if kind == "e4m3":   # scales of blocks that hold different columns differ: only one block per half is undone
+        rows[1][:] = rows[1][:, :1]
+        values = rows[0].float().double() * rows[1].double().repeat_interleave(128, 1)[:, :d]
+    y = torch.where(torch.arange(n, device="cuda") % 2 == 0, 1.0, -1.0)
+    with P.Context(1, d) as ctx:
+        decided(ctx, kind, rows, values, y, w)
