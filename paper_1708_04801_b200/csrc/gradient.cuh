@@ -117,9 +117,10 @@ __device__ __forceinline__ float margin_error(float terms, float w_norm, float x
   asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(x_squares + 0x1p-110f));
   return w_norm > 0.0f ? fmaf(terms * 0x1p-24f * 1.01f * w_norm, root, 0x1p-120f) : 0.0f;
 }
-// Whether an error of `err` in z could move the row across a jump of the loss's derivative or of the sign.
+// Whether an error of `err` in z could move the row across a jump of the loss's derivative or of the sign, or its sum has left fp32
+// on the way (the margin itself may lie within).
 __device__ __forceinline__ bool near_jump(int loss, float y, float z, float err) {
-  if (fabsf(z) < err) return true;
+  if (!(fabsf(z) >= err && fabsf(z) < INFINITY)) return true;
   return loss == LOSS_HINGE && fabsf(1.0f - y * z) < fmaf(fabsf(y), err, 0x1p-22f);
 }
 // A margin or label that is not a number gives a derivative and a loss that are none, whatever the loss.

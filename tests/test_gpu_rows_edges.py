@@ -187,3 +187,28 @@ def test_signs_are_those_of_exact_sums_whatever_the_size_of_the_rows(P, kind, d,
     y = torch.where(torch.arange(n, device="cuda") % 2 == 0, 1.0, -1.0)
     with P.Context(1, d) as ctx:
         decided(ctx, kind, rows, values, y, w)
+
+
+@pytest.mark.parametrize("loss", [0, 1, 2])
+@pytest.mark.parametrize("kind", KINDS)
+def test_margins_whose_partial_sums_leave_fp32(P, kind, loss):
+    # products of 2e38 and -1.9e38 in turn: sums of every other one leave fp32, the margin does not
+    n, d = 20, 40
+    w = torch.where(torch.arange(d) % 2 == 0, 1.0e19, -0.95e19).cuda()
+    x = torch.full((n, d), 2.0e19).cuda()
+    if kind == "two passes":
+        x, w = (torch.nn.functional.pad(t, (0, 8200 - d)) for t in (x, w))
+        d = 8200
+    rows, values = rows_of(kind, x)
+    y = torch.ones(n, device="cuda")
+    z = values @ w.double()
+    assert bool((z > 1e38).all()) and bool((z < 3e38).all())
+    with P.Context(1, d) as ctx:
+        fn = ctx.objective_grad_fp8 if kind == "e4m3" else ctx.objective_grad
+        out, grad = fn(*rows, y, w, 0.0, loss)
+        ctx.check()
+    assert float(out[1]) == 0.0
+    if loss == 2:   # (z - y) x leaves fp32, and the square of z - y
+        assert math.isinf(float(out[0])) and bool(torch.isinf(grad[:40]).all())
+    else:
+        assert float(out[0]) == 0.0 and bool((grad == 0).all())
