@@ -161,6 +161,26 @@ __device__ __forceinline__ void chunk_scale(const T* src, T* dst, long long n, i
   }
 }
 
+// The same by a factor that has no normal fp32 (gradients of 1e38 brought down to a norm of 1 and less): products in fp64.
+template <typename T>
+__device__ __forceinline__ void chunk_scale_f64(const T* src, T* dst, long long n, int chunk, double q) {
+  const long long i0 = (long long)chunk * CLIP_CHUNK, i1 = i0 + CLIP_CHUNK < n ? i0 + CLIP_CHUNK : n;
+  for (long long i = i0 + threadIdx.x; i < i1; i += CLIP_THREADS) dst[i] = scaled<T>((float)((double)widen_scalar<T>(src[i]) * q), 1.0f);
+}
+// out = g q, q = max_norm / N or 1
+template <int N>
+__device__ __forceinline__ void scale_chunk_of(const TensorList<N>& list, int i, int chunk, double q) {
+  const long long n = list.elems_type[i] >> 1;
+  const bool bf16 = list.elems_type[i] & 1;
+  if (q < 0x1p-126 && q > 0.0) {
+    if (bf16) chunk_scale_f64((const __nv_bfloat16*)list.src[i], (__nv_bfloat16*)list.dst[i], n, chunk, q);
+    else chunk_scale_f64((const float*)list.src[i], (float*)list.dst[i], n, chunk, q);
+  } else {
+    if (bf16) chunk_scale((const __nv_bfloat16*)list.src[i], (__nv_bfloat16*)list.dst[i], n, chunk, (float)q);
+    else chunk_scale((const float*)list.src[i], (float*)list.dst[i], n, chunk, (float)q);
+  }
+}
+
 // The chunks of a block's even share of all, first to last or last to first: f(tensor, chunk of it, chunks to go)
 template <int N, typename F>
 __device__ __forceinline__ void for_own_chunks(const TensorList<N>& list, bool backwards, F f) {
@@ -228,12 +248,8 @@ __global__ void __launch_bounds__(CLIP_THREADS, 8) scale_kernel(const __grid_con
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   const bool clips = norm > max_norm;
   if (!clips && in_place) return;  // times 1
-  const float f = clips ? (float)(max_norm / norm) : 1.0f;
-  for_own_chunks(list, true, [&](int i, int chunk, int) {
-    const long long n = list.elems_type[i] >> 1;
-    if (list.elems_type[i] & 1) chunk_scale((const __nv_bfloat16*)list.src[i], (__nv_bfloat16*)list.dst[i], n, chunk, f);
-    else chunk_scale((const float*)list.src[i], (float*)list.dst[i], n, chunk, f);
-  });
+  const double q = clips ? max_norm / norm : 1.0;
+  for_own_chunks(list, true, [&](int i, int chunk, int) { scale_chunk_of(list, i, chunk, q); });
 }
 
 // Both steps of a short list in one launch: a cluster of blocks that give each other their sums through distributed shared memory.
@@ -269,12 +285,8 @@ clip_small_kernel(const __grid_constant__ TensorList<N> list, bool scale, double
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   const bool clips = norm > max_norm;
   if (!scale || (!clips && in_place)) return;
-  const float f = clips ? (float)(max_norm / norm) : 1.0f;
-  for_own_chunks(list, true, [&](int i, int chunk, int) {
-    const long long n = list.elems_type[i] >> 1;
-    if (list.elems_type[i] & 1) chunk_scale((const __nv_bfloat16*)list.src[i], (__nv_bfloat16*)list.dst[i], n, chunk, f);
-    else chunk_scale((const float*)list.src[i], (float*)list.dst[i], n, chunk, f);
-  });
+  const double q = clips ? max_norm / norm : 1.0;
+  for_own_chunks(list, true, [&](int i, int chunk, int) { scale_chunk_of(list, i, chunk, q); });
 }
 
 }  // namespace wpsgd

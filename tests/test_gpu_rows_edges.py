@@ -212,3 +212,31 @@ def test_margins_whose_partial_sums_leave_fp32(P, kind, loss):
         assert math.isinf(float(out[0])) and bool(torch.isinf(grad[:40]).all())
     else:
         assert float(out[0]) == 0.0 and bool((grad == 0).all())
+
+
+# ---- clipping --------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("place", ["in place", "apart"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_norm", [1.0, 1e-3, 1e-7, 1e-20])
+@pytest.mark.parametrize("sizes", [[7], [5000, 3, 9001], [700000, 20001], [1500] * 40])
+def test_clip_by_a_factor_below_the_normal_numbers_of_fp32(P, sizes, max_norm, dtype, place):
+    # gradients up to 3e38 brought down to max_norm: the factor itself has no fp32 of full precision, the results have
+    grads = []
+    for i, n in enumerate(sizes):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        size = 10.0 ** (30 + 8 * torch.rand(n, generator=g, device="cuda", dtype=torch.float64))
+        grads.append((torch.where(torch.rand(n, generator=g, device="cuda") < 0.5, -1.0, 1.0) * size).to(dtype))
+    kept = [g.clone() for g in grads]
+    outs = None if place == "in place" else [torch.full_like(g, 9.0) for g in grads]
+    lists = P.GradList(grads, outs)
+    with P.Context(1, 8) as ctx:
+        norm = ctx.clip_grad_norm(lists, max_norm)
+        ctx.check()
+    want = math.sqrt(sum(float((g.double() ** 2).sum()) for g in kept))
+    if want < 3e38:
+        assert abs(float(norm) - want) <= 18 * U * want
+    for o, g in zip(lists.out, kept):
+        s = g.double() * (max_norm / want)
+        # as for any other factor: 20 u, a rounding to the result's type; results below 2^-126 are multiples of 2^-149
+        tol = (20 * U + (2.0 ** -8 if dtype == torch.bfloat16 else 0)) * s.abs() + (2.0 ** -133 if dtype == torch.bfloat16 else 2.0 ** -149)
+        assert bool(((o.double() - s).abs() <= tol).all())
