@@ -235,6 +235,7 @@ wpsgd_status wpsgd_objective_csr(wpsgd_ctx* ctx, const int64_t* row_ptr, const i
  *   X          DEVICE [n_rows, ld_elems], the first d columns of a row are read.
  *   Q          DEVICE [n_rows, ld_q] e4m3, 16-byte aligned, ld_q >= d a multiple of 16; bytes from column d on stay as they are.
  *   scales     DEVICE [n_rows, ld_s], ld_s >= ceil(d / 128).
+ * X, Q and scales must not overlap (WPSGD_ERR_INVALID_ARG); the scales may lie behind the codes of each row.
  * A NaN stays one. An infinity makes the scale of its block infinite, and every margin of its row NaN. */
 wpsgd_status wpsgd_quantize_rows(wpsgd_ctx* ctx, const void* X, wpsgd_xtype xt, int64_t ld_elems, int64_t n_rows, uint8_t* Q,
                                  int64_t ld_q, float* scales, int64_t ld_s);
@@ -242,7 +243,8 @@ wpsgd_status wpsgd_quantize_rows(wpsgd_ctx* ctx, const void* X, wpsgd_xtype xt, 
 /* Margins of n_models models on n_rows rows, both packed as above: Z[i, m] = sum_c x_i,c w_m,c with x = q scale, w = p scale.
  * The products of a block of 128 columns are summed without their scales, the blocks' sums times both scales in fp32.
  *   Q, q_scales, M, m_scales   DEVICE, as wpsgd_quantize_rows makes them.
- *   Z          DEVICE [n_rows, ld_z >= n_models], fp32 or bf16 per `zt`; columns from n_models on stay as they are. */
+ *   Z          DEVICE [n_rows, ld_z >= n_models], fp32 or bf16 per `zt`; columns from n_models on stay as they are. It must not overlap
+ *              any of the others (WPSGD_ERR_INVALID_ARG). */
 wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* ctx, const uint8_t* Q, int64_t ld_q, const float* q_scales, int64_t ld_qs,
                                int64_t n_rows, const uint8_t* M, int64_t ld_m, const float* m_scales, int64_t ld_ms,
                                int64_t n_models, void* Z, wpsgd_xtype zt, int64_t ld_z);
@@ -250,7 +252,8 @@ wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* ctx, const uint8_t* Q, int64_t ld_q, c
 /* Objective of Eq. 3-4 with its gradient over all rows, in one pass over them:
  *   out = { (lambda/2)|w|^2 + mean_i L(y_i, w.x_i), share of rows with sign(w.x) != sign(y) },
  *   grad = lambda w + mean_i L'(y_i, w.x_i) x_i.
- * Arguments as wpsgd_objective, but out DEVICE [2] and grad DEVICE [d] are fp32; w, grad and out must not overlap. Margins that
+ * Arguments as wpsgd_objective, but out DEVICE [2] and grad DEVICE [d] are fp32; w, grad and out must not overlap (X and y may: they are read
+ * before grad and out are written). Margins that
  * rounding could move across a jump (y z = 1 of the hinge loss, z = 0 of the error) are formed in fp64. Without rows: the regulariser alone. */
 wpsgd_status wpsgd_objective_grad(wpsgd_ctx* ctx, const void* X, wpsgd_xtype xt, int64_t ld_elems, const float* y, int64_t n_rows,
                                   const float* w, float lambda, wpsgd_loss loss, float* grad, float* out);

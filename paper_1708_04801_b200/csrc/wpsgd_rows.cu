@@ -87,6 +87,31 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
+// Rows of `width` bytes, `stride` apart
+struct Region {
+  const void* p;
+  long long width, stride, n;
+};
+// Whether two sets of rows share a byte. One may lie in the padding of the other (scales behind the codes of each row).
+bool meet(const Region& a, const Region& b) {
+  if (a.n < 1 || b.n < 1 || a.width < 1 || b.width < 1) return false;
+  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
+  if (a0 + (a.n - 1) * a.stride + a.width <= b0 || b0 + (b.n - 1) * b.stride + b.width <= a0) return false;
+  if (a.stride == b.stride) {  // each row of one at the same place of a row of the other: no need to go through them
+    const uintptr_t place = b0 >= a0 ? (b0 - a0) % a.stride : (a.stride - (a0 - b0) % a.stride) % a.stride;
+    if (place >= (uintptr_t)a.width && place + b.width <= (uintptr_t)a.stride) return false;
+  }
+  const Region &few = a.n <= b.n ? a : b, &many = a.n <= b.n ? b : a;
+  const uintptr_t m0 = (uintptr_t)many.p;
+  for (long long i = 0; i < few.n; ++i) {
+    const uintptr_t lo = (uintptr_t)few.p + i * few.stride, hi = lo + few.width;
+    if (hi <= m0) continue;
+    const long long last = std::min<long long>((hi - 1 - m0) / many.stride, many.n - 1);  // the last row of `many` that starts before hi
+    if (m0 + last * many.stride + many.width > lo) return true;
+  }
+  return false;
+}
+
 size_t element_size(wpsgd_xtype t) { return t == WPSGD_X_F32 ? 4 : 2; }
 bool known(wpsgd_xtype t) { return t == WPSGD_X_F32 || t == WPSGD_X_BF16; }
 long long blocks_of(long long d) { return (d + Q_BLOCK - 1) / Q_BLOCK; }
@@ -427,9 +452,11 @@ wpsgd_status wpsgd_quantize_rows(wpsgd_ctx* c, const void* X, wpsgd_xtype xt, in
   if (n_rows == 0) return WPSGD_OK;
   const size_t es = element_size(xt);
   if ((uintptr_t)X % es) return fail(c, WPSGD_ERR_INVALID_ARG, "quantize_rows: X is not aligned to its elements");
-  DeviceGuard guard(c->device);
   const long long nb = blocks_of(c->d);
   if (c->d > INT32_MAX - Q_BLOCK || n_rows > INT64_MAX / nb / 64) return fail(c, WPSGD_ERR_UNSUPPORTED, "quantize_rows: 2^31 columns or 2^57 blocks and more");
+  const Region x = {X, (long long)(c->d * es), (long long)(ld_elems * es), n_rows}, q = {Q, c->d, ld_q, n_rows}, s = {scales, nb * 4, ld_s * 4, n_rows};
+  if (meet(x, q) || meet(x, s) || meet(q, s)) return fail(c, WPSGD_ERR_INVALID_ARG, "quantize_rows: X, Q and scales overlap");
+  DeviceGuard guard(c->device);
   const bool vec = aligned16(X) && ((size_t)ld_elems * es) % 16 == 0 && ((size_t)c->d * es) % 16 == 0;
   auto go = [&](auto tag) {
     using XT = decltype(tag);
@@ -453,6 +480,10 @@ wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld_q, con
   if (n_rows > INT32_MAX - 256 || n_models > INT32_MAX - 256) return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: 2^31 - 256 rows or models and more");
   if (n_rows == 0 || n_models == 0) return WPSGD_OK;
   if (!Z || ld_z < n_models || (uintptr_t)Z % element_size(zt)) return fail(c, WPSGD_ERR_INVALID_ARG, "margins_fp8: Z is NULL, not aligned to its elements, or its stride is below n_models");
+  const long long zs = (long long)element_size(zt), nb = blocks_of(c->d);
+  const Region z = {Z, n_models * zs, ld_z * zs, n_rows};
+  if (meet(z, {Q, c->d, ld_q, n_rows}) || meet(z, {q_scales, nb * 4, ld_qs * 4, n_rows}) || meet(z, {M, c->d, ld_m, n_models}) || meet(z, {m_scales, nb * 4, ld_ms * 4, n_models}))
+    return fail(c, WPSGD_ERR_INVALID_ARG, "margins_fp8: Z overlaps rows, models or their scales");
   DeviceGuard guard(c->device);
   const MarginsCall call = {Q, ld_q, M, ld_m, c->d, {q_scales, ld_qs, m_scales, ld_ms, Z, ld_z, (int)n_rows, (int)n_models, (int)blocks_of(c->d), 0, 0, 1,
                             ld_z % 2 == 0 && (uintptr_t)Z % (2 * element_size(zt)) == 0, c->opt_spin_limit, c->opt_drop_block, c->status}};

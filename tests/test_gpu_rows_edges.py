@@ -240,3 +240,64 @@ def test_clip_by_a_factor_below_the_normal_numbers_of_fp32(P, sizes, max_norm, d
         # as for any other factor: 20 u, a rounding to the result's type; results below 2^-126 are multiples of 2^-149
         tol = (20 * U + (2.0 ** -8 if dtype == torch.bfloat16 else 0)) * s.abs() + (2.0 ** -133 if dtype == torch.bfloat16 else 2.0 ** -149)
         assert bool(((o.double() - s).abs() <= tol).all())
+
+
+# ---- arguments that overlap --------------------------------------------------------------------------------------------------------
+def test_rows_packed_over_themselves_and_margins_over_their_rows_are_refused(P, wpsgd_lib):
+    lib, n, d = wpsgd_lib, 50, 100
+    x = torch.randn(n, 128, device="cuda")
+    q = torch.zeros(n, 512, dtype=torch.uint8, device="cuda")
+    s, m, t = torch.zeros(n, 4, device="cuda"), torch.zeros(7, 112, dtype=torch.uint8, device="cuda"), torch.zeros(7, 1, device="cuda")
+    z = torch.zeros(n, 7, device="cuda")
+    with P.Context(1, d) as ctx:
+        h = ctx._h
+
+        def status(fn, *args):
+            return fn(h, *[a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args])
+
+        quant = lib.wpsgd_quantize_rows
+        assert status(quant, x, 0, 128, n, x, 512, s, 4) == 1                           # codes over the rows
+        assert status(quant, x, 0, 128, n, x.data_ptr() + 128 * 4 * (n - 1) + 16, 512, s, 4) == 1
+        assert status(quant, x, 0, 128, n, q, 512, x, 128) == 1                         # scales over the rows
+        assert status(quant, x, 0, 128, n, q, 512, q, 128) == 1                         # scales over the codes
+        assert status(quant, x, 0, 128, n, x.data_ptr() + 400, 512, s, 4) == 0          # codes of the first rows in the padding of the rows
+        marg = lib.wpsgd_margins_fp8
+        for over in (q, m, s, t):
+            assert status(marg, q, 512, s, 4, n, m, 112, t, 1, 7, over, 0, 7) == 1
+        assert status(marg, q, 512, s, 4, n, m, 112, t, 1, 7, q.data_ptr() + 96, 1, 256) == 1
+        assert lib.wpsgd_last_error(h) == b"margins_fp8: Z overlaps rows, models or their scales"
+        assert status(marg, q, 512, s, 4, n, m, 112, t, 1, 7, z, 0, 7) == 0
+        ctx.check()
+
+
+def test_scales_and_margins_in_the_padding_of_the_packed_rows(P):
+    # one buffer: 100 codes, 4 bytes of scale at 100, margins on 7 models from 112 on
+    n, d, m = 300, 100, 7
+    x, w = torch.randn(n, d, device="cuda"), torch.randn(m, d, device="cuda")
+    buf = torch.full((n, 256), 0x55, dtype=torch.uint8, device="cuda")
+    f = buf.view(torch.float32)
+    with P.Context(1, d) as ctx:
+        Q, S = ctx.quantize_rows(x)
+        M, T = ctx.quantize_rows(w)
+        ctx.quantize_rows(x, buf[:, :d], f[:, 25:26])
+        z = ctx.margins_fp8(Q, S, M, T)
+        ctx.margins_fp8(buf[:, :d], f[:, 25:26], M, T, out=f[:, 28:35])
+        ctx.check()
+    assert torch.equal(buf[:, :d], Q.view(torch.uint8)) and torch.equal(f[:, 25:26], S) and torch.equal(f[:, 28:35], z)
+    assert bool((buf[:, 104:112] == 0x55).all()) and bool((buf[:, 140:] == 0x55).all())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "e4m3", "two passes"])
+@pytest.mark.parametrize("n", [40, 30000])
+def test_gradient_written_over_the_rows_and_labels_it_was_made_from(P, kind, n):
+    # everything is read before grad and out are written
+    d = 8200 if kind == "two passes" else 200
+    x, y, w = rows_problem(n, d)
+    rows, _ = rows_of(kind, x)
+    with P.Context(1, d) as ctx:
+        fn = ctx.objective_grad_fp8 if kind == "e4m3" else ctx.objective_grad
+        out, grad = fn(*rows, y, w, 0.01, 1)
+        over = torch.as_strided(rows[0].view(torch.uint8) if kind == "e4m3" else rows[0], (4 * d // rows[0].element_size(),), (1,)).view(torch.float32)
+        fn(*rows, y, w, 0.01, 1, grad=over, out=y[5:7])
+        ctx.check()
+    assert torch.equal(over, grad) and torch.equal(y[5:7], out)
