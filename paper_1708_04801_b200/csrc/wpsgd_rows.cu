@@ -122,6 +122,7 @@ const char* check_rows8(const uint8_t* Q, int64_t ld_q, const float* scales, int
   if (n > 0 && (!Q || !scales)) return "8-bit rows or scales are NULL";
   if (ld_q < d || ld_q % 16) return "8-bit rows need a stride of at least d and a multiple of 16 bytes";
   if (n > 0 && !aligned16(Q)) return "8-bit rows must start on 16 bytes";
+  if ((uintptr_t)scales % sizeof(float)) return "scales are not aligned to their elements";
   if (ld_s < blocks_of(d)) return "scales need a stride of at least ceil(d / 128)";
   return nullptr;
 }
@@ -295,6 +296,7 @@ wpsgd_status gradient(wpsgd_ctx* c, GradParams p) {
 
 const char* check_gradient(const wpsgd_ctx* c, const float* y, int64_t n_rows, const float* w, float lambda, wpsgd_loss loss, const float* grad, const float* out) {
   if (!w || !grad || !out || (n_rows > 0 && !y)) return "NULL argument";
+  if (((uintptr_t)y | (uintptr_t)w | (uintptr_t)grad | (uintptr_t)out) % sizeof(float)) return "y, w, grad or out is not aligned to its elements";
   if ((int)loss < 0 || (int)loss > 2) return "unknown loss";
   if (!std::isfinite(lambda)) return "lambda is not finite";
   const size_t nd = (size_t)c->d * 4;
@@ -419,6 +421,7 @@ wpsgd_status norm_and_scale(wpsgd_ctx* c, const std::vector<TensorList<N>>& list
 
 wpsgd_status run_list(wpsgd_ctx* c, const wpsgd_grad_list* list, bool scale, double max_norm, float* norm_out) {
   if (!list || !norm_out) return fail(c, WPSGD_ERR_INVALID_ARG, "the list or norm_out is NULL");
+  if ((uintptr_t)norm_out % sizeof(float)) return fail(c, WPSGD_ERR_INVALID_ARG, "norm_out is not aligned to its element");
   // norm_out in no range: of those that start before its end, only such as start less than the longest before it can reach it
   const uintptr_t lo = (uintptr_t)norm_out, hi = lo + sizeof(float);
   auto it = std::lower_bound(list->ranges.begin(), list->ranges.end(), hi, [](const Range& r, uintptr_t v) { return r.lo < v; });

@@ -301,3 +301,30 @@ def test_gradient_written_over_the_rows_and_labels_it_was_made_from(P, kind, n):
         fn(*rows, y, w, 0.01, 1, grad=over, out=y[5:7])
         ctx.check()
     assert torch.equal(over, grad) and torch.equal(y[5:7], out)
+
+
+def test_pointers_off_their_elements_are_refused(P, wpsgd_lib):
+    # an access to them would end the process's use of the GPU: only ever run against a library that refuses
+    lib, n, d = wpsgd_lib, 4, 100
+    x = torch.zeros(n, d, device="cuda")
+    q, s = torch.zeros(n, 112, dtype=torch.uint8, device="cuda"), torch.zeros(n + 1, 1, device="cuda")
+    y, w, g, out = (torch.zeros(k + 1, device="cuda") for k in (n, d, d, 2))
+    z = torch.zeros(n, n, device="cuda")
+    with P.Context(1, d) as ctx:
+        def refused(fn, *args, why=b"aligned to"):
+            assert fn(ctx._h, *[a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args]) == 1
+            assert why in lib.wpsgd_last_error(ctx._h)
+
+        off = lambda t, by=2: t.data_ptr() + by
+        refused(lib.wpsgd_quantize_rows, x, 0, d, n, q, 112, off(s), 1)
+        refused(lib.wpsgd_margins_fp8, q, 112, off(s), 1, n, q, 112, s, 1, n, z, 0, n)
+        refused(lib.wpsgd_margins_fp8, q, 112, s, 1, n, q, 112, off(s, 1), 1, n, z, 0, n)
+        for i in range(4):
+            at = [off(t, 1 + i % 3) if i == k else t for k, t in enumerate((y, w, g, out))]
+            refused(lib.wpsgd_objective_grad, x, 0, d, at[0], n, at[1], 0.1, 0, at[2], at[3])
+            refused(lib.wpsgd_objective_grad_fp8, q, 112, s, 1, at[0], n, at[1], 0.1, 0, at[2], at[3])
+        refused(lib.wpsgd_objective_grad_fp8, q, 112, off(s), 1, y, n, w, 0.1, 0, g, out)
+        lists = P.GradList([x])
+        refused(lib.wpsgd_grad_norm, lists._h, off(out))
+        refused(lib.wpsgd_clip_grad_norm, lists._h, 1.0, off(out))
+        ctx.check()
