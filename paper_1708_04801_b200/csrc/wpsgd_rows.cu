@@ -481,6 +481,7 @@ wpsgd_status wpsgd_margins_fp8(wpsgd_ctx* c, const uint8_t* Q, int64_t ld_q, con
   if (const char* why = check_rows8(Q, ld_q, q_scales, ld_qs, n_rows, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("margins_fp8: rows: ") + why);
   if (const char* why = check_rows8(M, ld_m, m_scales, ld_ms, n_models, c->d)) return fail(c, WPSGD_ERR_INVALID_ARG, std::string("margins_fp8: models: ") + why);
   if (n_rows > INT32_MAX - 256 || n_models > INT32_MAX - 256) return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: 2^31 - 256 rows or models and more");
+  if (c->d > INT32_MAX - Q_BLOCK) return fail(c, WPSGD_ERR_UNSUPPORTED, "margins_fp8: 2^31 columns and more");  // columns of a tile are 32-bit coordinates
   if (n_rows == 0 || n_models == 0) return WPSGD_OK;
   if (!Z || ld_z < n_models || (uintptr_t)Z % element_size(zt)) return fail(c, WPSGD_ERR_INVALID_ARG, "margins_fp8: Z is NULL, not aligned to its elements, or its stride is below n_models");
   const long long zs = (long long)element_size(zt), nb = blocks_of(c->d);

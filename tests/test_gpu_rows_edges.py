@@ -328,3 +328,14 @@ def test_pointers_off_their_elements_are_refused(P, wpsgd_lib):
         refused(lib.wpsgd_grad_norm, lists._h, off(out))
         refused(lib.wpsgd_clip_grad_norm, lists._h, 1.0, off(out))
         ctx.check()
+
+
+def test_margins_and_packing_of_2_to_the_31_columns_are_refused(P, wpsgd_lib):
+    # places in a tile are 32-bit coordinates: beyond, they would turn negative and read zeros. Nothing is read here
+    lib, d = wpsgd_lib, 1 << 31
+    q, s, z = torch.zeros(16, dtype=torch.uint8, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    with P.Context(1, d) as ctx:
+        assert lib.wpsgd_margins_fp8(ctx._h, q.data_ptr(), d, s.data_ptr(), d // 128, 1, q.data_ptr(), d, s.data_ptr(), d // 128, 1, z.data_ptr(), 0, 1) == 5
+        assert lib.wpsgd_last_error(ctx._h).startswith(b"margins_fp8: 2^31 columns")
+        assert lib.wpsgd_quantize_rows(ctx._h, z.data_ptr(), 0, d, 1, q.data_ptr(), d, s.data_ptr(), d // 128) == 5
+        ctx.check()
