@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 import importlib.util
 import os
 from typing import Optional, Tuple
@@ -260,7 +261,7 @@ class Context:
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
         self._stream = stream  # keep alive
-        self._torch, self._rows = torch, load_rows()
+        self._torch = torch
         self.k, self.d = int(k), int(d)
         h = ctypes.c_void_p()
         st = self._lib.wpsgd_create(self.device, ctypes.c_void_p(stream.cuda_stream), self.k, self.d, ctypes.byref(h))
@@ -268,6 +269,10 @@ class Context:
             raise WpsgdError(st, "wpsgd_create", self._lib.wpsgd_last_error(None).decode())
         self._h = h
         self._head = (h.value, self.device, stream.cuda_stream, self.d)
+
+    @functools.cached_property
+    def _rows(self):  # by the first operator that needs it: chains need libwpsgd.so alone
+        return load_rows()
 
     # -- plumbing ---------------------------------------------------------------------------------------
     def _ck(self, st: int, where: str):

@@ -43,10 +43,25 @@ def _fresh(obj: str) -> bool:
         return False
 
 
+def _binding_stamp() -> str:
+    """What _rows.so is built for beside its sources, and carries: it uses torch's C++ classes and Python's C API."""
+    import importlib.metadata
+    import sysconfig
+
+    return f"torch {importlib.metadata.version('torch')} python {sysconfig.get_config_var('SOABI')}"
+
+
+def _binding_fresh() -> bool:
+    read = (BINDING_SOURCE, os.path.join(os.path.dirname(HERE), "include", "wpsgd.h"))
+    try:
+        return all(os.path.getmtime(BINDING) >= os.path.getmtime(f) for f in read) and _binding_stamp().encode() in open(BINDING, "rb").read()
+    except OSError:
+        return False
+
+
 def build_binding(force: bool = False) -> str:
     """_rows.so, which calls libwpsgd.so beside it; has to be built after it."""
-    read = (BINDING_SOURCE, os.path.join(os.path.dirname(HERE), "include", "wpsgd.h"))
-    if not force and os.path.exists(BINDING) and all(os.path.getmtime(BINDING) >= os.path.getmtime(f) for f in read):
+    if not force and _binding_fresh():
         return BINDING
     import sysconfig
 
@@ -55,7 +70,7 @@ def build_binding(force: bool = False) -> str:
     tmp = BINDING + f".tmp{os.getpid()}"
     include = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")]
     libs = cpp_extension.library_paths()
-    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-o", tmp, BINDING_SOURCE]
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f'-DROWS_BUILT_FOR="{_binding_stamp()}"', "-o", tmp, BINDING_SOURCE]
                           + [f"-I{i}" for i in include] + [f"-L{i}" for i in libs]
                           + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", f"-L{HERE}", "-l:libwpsgd.so", "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, BINDING)

@@ -228,4 +228,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rows", nullptr, -1, methods, null
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__rows() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__rows() {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for", ROWS_BUILT_FOR) < 0) Py_CLEAR(m);
+  return m;
+}
