@@ -41,7 +41,12 @@ wpsgd_status rows_workspace(wpsgd_ctx* c) {
   if (capturing != cudaStreamCaptureStatusNone)
     return fail(c, WPSGD_ERR_STATE, "the first call of a gradient, norm or clipping operator on a context allocates its workspace: make one before the capture");
   void* ws = nullptr;
-  CU_TRY(c, cudaMalloc(&ws, RowsLayout(c->d).total));
+  // another stream of the process may be under capture: an allocation does not touch it, which "relaxed" says
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  CU_TRY(c, cudaThreadExchangeStreamCaptureMode(&mode));
+  const cudaError_t allocated = cudaMalloc(&ws, RowsLayout(c->d).total);
+  cudaThreadExchangeStreamCaptureMode(&mode);
+  CU_TRY(c, allocated);
   cudaError_t e = cudaMemsetAsync(ws, 0, RowsLayout(c->d).sums, c->stream);
   if (e != cudaSuccess) {
     cudaFree(ws);

@@ -339,3 +339,29 @@ def test_margins_and_packing_of_2_to_the_31_columns_are_refused(P, wpsgd_lib):
         assert lib.wpsgd_last_error(ctx._h).startswith(b"margins_fp8: 2^31 columns")
         assert lib.wpsgd_quantize_rows(ctx._h, z.data_ptr(), 0, d, 1, q.data_ptr(), d, s.data_ptr(), d // 128) == 5
         ctx.check()
+
+
+# ---- a first call beside another stream's capture ---------------------------------------------------------------------------------
+def test_a_first_call_while_another_stream_is_captured(P):
+    # the workspace is allocated then, which must not end the capture (of another context, in CUDA's strictest mode)
+    n, d = 300, 200
+    x, y, w = rows_problem(n, d)
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    grads, outs = [torch.zeros(d, device="cuda") for _ in sides], [torch.zeros(2, device="cuda") for _ in sides]
+    a, b = (P.Context(1, d, stream=s) for s in sides)
+    with torch.cuda.stream(sides[0]):
+        want = a.objective_grad(x, y, w, 0.01, 1)
+        sides[0].synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=sides[0], capture_error_mode="global"):
+            a.objective_grad(x, y, w, 0.01, 1, grad=grads[0], out=outs[0])
+            b.objective_grad(x, y, w, 0.01, 1, grad=grads[1], out=outs[1])
+        graph.replay()
+    a.check()
+    b.check()
+    for grad, out in zip(grads, outs):
+        assert torch.equal(grad, want[1]) and torch.equal(out, want[0])
+    del graph
+    a.destroy()
+    b.destroy()
