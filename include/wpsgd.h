@@ -108,7 +108,8 @@ wpsgd_status wpsgd_destroy(wpsgd_ctx* ctx);
  *   "timing"          1: record events around the chain kernel (see wpsgd_last_chain_ms). Default 0.
  *   "test_drop_block" test hook of the bounded waits, not for production use: the rows of that block of every chain
  *                     are never requested, so the wait for them runs out and WPSGD_ERR_TIMEOUT is reported by
- *                     wpsgd_check; -1 (default) = off. */
+ *                     wpsgd_check; -1 (default) = off. Of wpsgd_margins_fp8 it drops that block of 128 columns, of
+ *                     wpsgd_objective_grad the rows that each group of threads takes in that round (rows in bulk copies). */
 wpsgd_status wpsgd_set_option(wpsgd_ctx* ctx, const char* name, int64_t value);
 
 /* Node numbers that enter the sample stream in place of 0..k-1 (HOST [k], >= 0; NULL restores the
@@ -226,7 +227,8 @@ wpsgd_status wpsgd_objective_csr(wpsgd_ctx* ctx, const int64_t* row_ptr, const i
 /* ---- Operators on whole sets of rows ---------------------------------------------------------------------------------------
  * They use the context's d, stream and device, and not its models. Those that need a workspace (objective_grad*, grad_norm,
  * clip_grad_norm) allocate it at the context's first such call, which therefore has to come before a stream capture
- * (WPSGD_ERR_STATE within one), and keep it at its place: later calls allocate nothing and can be captured. Calls of one context
+ * (WPSGD_ERR_STATE within one), and keep it at its place: later calls allocate nothing and can be captured. The workspace takes up to 34 MB (4 d bytes
+ * where that is more) and the first call some 40 us longer, so a program keeps its contexts. Calls of one context
  * share the workspace, so graphs captured from one context must not run at the same time as each other or as other calls of it.
  * Results do not depend on timing. */
 
@@ -241,7 +243,8 @@ wpsgd_status wpsgd_quantize_rows(wpsgd_ctx* ctx, const void* X, wpsgd_xtype xt, 
                                  int64_t ld_q, float* scales, int64_t ld_s);
 
 /* Margins of n_models models on n_rows rows, both packed as above: Z[i, m] = sum_c x_i,c w_m,c with x = q scale, w = p scale.
- * The products of a block of 128 columns are summed without their scales, the blocks' sums times both scales in fp32.
+ * The products of a block of 128 columns are summed without their scales, the blocks' sums times both scales in fp32: scales whose product
+ * lies outside fp32's normal numbers (rows and models both below 1e-17 or above 1e22, say) lose precision or give infinities.
  *   Q, q_scales, M, m_scales   DEVICE, as wpsgd_quantize_rows makes them.
  *   Z          DEVICE [n_rows, ld_z >= n_models], fp32 or bf16 per `zt`; columns from n_models on stay as they are. It must not overlap
  *              any of the others (WPSGD_ERR_INVALID_ARG). */

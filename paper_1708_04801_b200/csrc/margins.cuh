@@ -7,11 +7,13 @@
 // back and added to fp32 registers with its scales while the tensor cores form the next ones in other buffers.
 //
 // Few tiles with many blocks of columns: a cluster of CTAs per tile, each with a share of the blocks, whose sums meet in the first.
-// 2 rows of 5918 columns on 15 models: 16.1 us with one CTA, see margins_of for the rule.
+// 2 rows of 5918 columns on 15 models: 16.1 us with one CTA, 6.6 with eight, see margins_of for the rule.
 //
-// Bound by the rows where there are few models (262144 rows of 4096 columns on 16: 176 us, 6.4 TB/s), else by the reading back
-// of D_b: fragments leave tensor memory at some 200 bytes a cycle, 128 KB per block of columns and SM take 700 cycles, while its products
-// take 512 (65536 rows of 4096 columns on 1024 models: 472 us, 1160 TFLOP/s).
+// Bound by the rows where there are few models (262144 rows of 4096 columns on 16: 177 us, 6.3 TB/s), else by the way of D_b from the
+// tensor cores to the sums (65536 rows of 4096 columns on 1024 models: 480 us, 1150 TFLOP/s). Of 1650 cycles per block of columns and SM the products take 520
+// and the adding warps 900 (740 to read 128 KB of fragments from tensor memory, some 200 bytes a cycle); these wait 220 more for products and 80 for scales,
+// storing takes 150, and 300 are not accounted for. A buffer is refilled when all adding warps have read it, and nothing is multiplied
+// while a tile is stored.
 //
 // One persistent CTA per SM, a role per warp: warp 0 brings the tiles of Q and M into a ring of stages (TMA, 128-byte swizzle; what lies outside
 // the matrices arrives as zeros), warp 1 issues the products, warp 2 brings the scales of a block's 128 rows and BN models (cp.async) into a

@@ -4,8 +4,10 @@
 //
 // 448 is the largest e4m3 value, so the largest magnitude of a block uses the whole range. The lower limit of `a` keeps 448 / a
 // finite for blocks of zeros or of subnormal numbers. Each q is rounded twice, to 24 bits by the product (2^-24 of it) and to
-// e4m3's 4 bits (2^-4): the product instead of a division moves a value across a rounding border of e4m3 in about one of 2^20
-// cases, and costs one instruction where the division costs ten. An infinity makes the scale infinite and its block NaN or 0
+// e4m3's 4 bits (2^-4): the product instead of a division costs one instruction instead of ten and moves a value across a rounding border of
+// e4m3 in one of 2 million codes of fp32 rows, and in one of 4100 of bf16 rows, whose quotients are exact ties in 0.5 % of the cases (counted on
+// 16.8 million normal values). The quotient 448 / a is the nearest fp32; 448 times a rounded 1 / a would miss that in a quarter of the blocks and change
+// 0.08 % of the codes of bf16 rows. An infinity makes the scale infinite and its block NaN or 0
 // (0 * infinity is NaN again in every margin); a NaN stays a NaN and does not enter `a`.
 // Bound by memory: reads 4 or 2 bytes per element, writes 1. 131072 bf16 rows of 4096 columns: 311 us, 5.3 TB/s.
 #pragma once
