@@ -507,7 +507,7 @@ class Context:
         """Scales the gradients down to max_norm where their global norm is above it, in place or into the list's outputs;
         returns the norm before, fp32 [1]."""
         grads = self._grad_list(grads)
-        r = self._rows.grad_norm(*self._head, grads._h.value, max_norm, norm)
+        r = self._rows.grad_norm(*self._head, grads._h.value, float(max_norm), norm)
         return r if r.__class__ is not int else self._ck(r, "wpsgd_clip_grad_norm")
 
     def solve_host(self, X, y, shard_off, n_steps, eta0, sched, lam, loss, seed, w0=None, r: float = 0.0, out=None):

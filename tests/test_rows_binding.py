@@ -50,3 +50,20 @@ def test_the_extension_is_built_anew_for_another_torch(wpsgd_lib, monkeypatch):
     assert torch.__version__ in build._binding_stamp() and binding.load_rows().built_for == build._binding_stamp()
     monkeypatch.setattr(build, "_binding_stamp", lambda: "another torch")
     assert not build._binding_fresh()
+
+
+def test_clipping_needs_a_norm_to_clip_to(monkeypatch):
+    # the extension takes None for "the norm alone": a clip without a limit would return and leave the gradients as they are
+    from paper_1708_04801_b200 import binding
+
+    calls = []
+    monkeypatch.setattr(binding, "load_library", FakeLibrary)
+    monkeypatch.setattr(binding, "load_rows", lambda: types.SimpleNamespace(grad_norm=lambda *a: calls.append(a) or "norm"))
+    monkeypatch.setattr(binding.Context, "_grad_list", lambda self, grads: types.SimpleNamespace(_h=types.SimpleNamespace(value=7)))
+    with binding.Context(1, 4, device=0, stream=types.SimpleNamespace(cuda_stream=0)) as ctx:
+        for limit in (None, "much", [1.0]):
+            with pytest.raises((TypeError, ValueError)):
+                ctx.clip_grad_norm([], limit)
+        assert not calls
+        assert ctx.clip_grad_norm([], 2) == "norm" and calls[0][4:] == (7, 2.0, None)
+        assert ctx.grad_norm([]) == "norm" and calls[1][4:] == (7, None, None)
