@@ -164,6 +164,7 @@ struct GradientArgs {
     if (!vector(a[0], c, n, "y", &y) || !vector(a[1], c, c.d, "w", &w)) return false;
     lambda = PyFloat_AsDouble(a[2]);
     if ((lambda == -1.0 && PyErr_Occurred()) || !number(a[3], &loss)) return false;
+    if (loss != (int)loss) loss = -1;  // unknown, as it is, and not what its low 32 bits are
     if (a[4] == Py_None) grad.take(empty(c, {c.d}, {1}, at::kFloat));
     else grad.take(a[4]);
     if (a[5] == Py_None) out.take(empty(c, {2}, {1}, at::kFloat));

@@ -365,3 +365,15 @@ def test_a_first_call_while_another_stream_is_captured(P):
     del graph
     a.destroy()
     b.destroy()
+
+
+@pytest.mark.parametrize("loss", [3, -1, 1 << 32, (1 << 32) + 1, -(1 << 32)])
+def test_unknown_losses_are_refused(P, loss):
+    x, y, w = rows_problem(4, 100)
+    with P.Context(1, 100) as ctx:
+        q, s = ctx.quantize_rows(x)
+        for call in (lambda: ctx.objective_grad(x, y, w, 0.1, loss), lambda: ctx.objective_grad_fp8(q, s, y, w, 0.1, loss)):
+            with pytest.raises(P.WpsgdError) as e:
+                call()
+            assert e.value.status_name == "INVALID_ARG"
+        ctx.check()
