@@ -283,6 +283,99 @@ wpsgd_status wpsgd_grad_norm(wpsgd_ctx* ctx, const wpsgd_grad_list* list, float*
  * N scales by 0; an N that is not a number leaves the values as they are. norm_out gets the norm before clipping. */
 wpsgd_status wpsgd_clip_grad_norm(wpsgd_ctx* ctx, const wpsgd_grad_list* list, double max_norm, float* norm_out);
 
+/* ---- Rows that go to several nodes ---------------------------------------------------------------------------------------------
+ * A row has `top` places, each with a node. wpsgd_sort_rows gives every place a position among the rows sorted by node, and the nodes'
+ * shards; wpsgd_gather_rows lays the rows out in that order, as wpsgd_run and wpsgd_delta_run take them; wpsgd_combine_rows brings what the
+ * nodes give back to the rows' order, added up with a weight for each place. The gradient of gather is combine without weights, that of combine
+ * is wpsgd_combine_rows_grad. The calls use the context's stream and device, allocate nothing and can be captured. Rows are fp32 or bf16, of
+ * any width d, stride and alignment of their elements; rows that do not start on 16 bytes are read in whole aligned 16-byte units: up to 15 bytes
+ * before the first and after the last byte of a row are read and not used, within the unit that holds it (never across a page). Outputs must not overlap
+ * inputs (WPSGD_ERR_INVALID_ARG). A node or position past the end counts as none and is reported by the next wpsgd_check (WPSGD_ERR_CUDA). */
+
+/* Places sorted by node, equal nodes in the order of their places (i * top + j for place j of row i).
+ *   node       DEVICE [n_rows, top]; negative: no node. n_nodes at most 16384 (WPSGD_ERR_UNSUPPORTED).
+ *   where      DEVICE [n_rows, top]: the place's position, -1 where it has no node.
+ *   order      DEVICE [n_rows * top] or NULL: the place at each position, -1 behind the last.
+ *   shard_off  DEVICE [n_nodes + 1]: node k has the positions [shard_off[k], shard_off[k+1]). */
+wpsgd_status wpsgd_sort_rows(wpsgd_ctx* ctx, const int32_t* node, int64_t n_rows, int32_t top, int32_t n_nodes, int32_t* where,
+                             int32_t* order, int64_t* shard_off);
+
+/* out[where[i, j]] = X[i] for every place with a position; other rows of out stay as they are. Positions must differ from each other (as
+ * those of wpsgd_sort_rows do): a position that two places have gets parts of either row.
+ *   X DEVICE [n_rows, ld_x], where DEVICE [n_rows, top], out DEVICE [n_sorted, ld_out]; columns from d on stay as they are. */
+wpsgd_status wpsgd_gather_rows(wpsgd_ctx* ctx, const void* X, wpsgd_xtype xt, int64_t ld_x, int64_t d, const int32_t* where,
+                               int64_t n_rows, int32_t top, void* out, int64_t ld_out, int64_t n_sorted);
+
+/* out[i] = sum_j weights[i, j] Y[where[i, j]] over the places that have a position (a row without any: zeros), summed in fp32 in the order of j.
+ * weights DEVICE [n_rows, top] or NULL for 1; Y DEVICE [n_sorted, ld_y], out DEVICE [n_rows, ld_out]. Positions may repeat. */
+wpsgd_status wpsgd_combine_rows(wpsgd_ctx* ctx, const void* Y, wpsgd_xtype xt, int64_t ld_y, int64_t d, int64_t n_sorted,
+                                const int32_t* where, const float* weights, int64_t n_rows, int32_t top, void* out, int64_t ld_out);
+
+/* Gradients of wpsgd_combine_rows from dout, that of its result: dY[where[i, j]] = weights[i, j] dout[i] (other rows stay as they are; positions must
+ * differ from each other) and dweights[i, j] = dout[i] . Y[where[i, j]] in fp32, 0 where there is no position (dweights may be NULL). */
+wpsgd_status wpsgd_combine_rows_grad(wpsgd_ctx* ctx, const void* dout, int64_t ld_dout, const void* Y, int64_t ld_y, wpsgd_xtype xt,
+                                     int64_t d, int64_t n_sorted, const int32_t* where, const float* weights, int64_t n_rows,
+                                     int32_t top, void* dY, int64_t ld_dy, float* dweights);
+
+/* ---- Chains whose labels are vectors (gated delta rule) -----------------------------------------------------------------------------
+ * A chain owns the rows [shard_off[c], shard_off[c+1]) and runs over them once, in order. Each of its heads_v heads keeps dv linear models on dk
+ * features, W [dv, dk]; a row t brings features k_t, a vector of labels v_t, a step size beta_t and a log decay g_t, and is answered at q_t:
+ *     W <- e^{g_t} W,   W <- W - beta_t (W k_t - v_t) k_t^T,   o_t = scale W q_t.
+ * This is Eq. 5 for the squared loss with a label for each model, e^{g_t} = 1 - eta lambda and beta_t = eta, the decay taken before the margin.
+ * q and k have heads_k heads, heads_v a multiple of heads_k: head h of v takes head h / (heads_v / heads_k) of them.
+ *
+ * Rows: all of one type, DEVICE, row t of q at q + t * ld_q: q, k [n_rows, heads_k, dk], v [n_rows, heads_v, dv], g, beta [n_rows, heads_v], heads one behind
+ * the other. Rows outside every chain are not read. dk and dv at most 128 (WPSGD_ERR_UNSUPPORTED). g is at most 0 in use; below -128 it counts as -128 (its
+ * exponential is 0 in fp32). Lengths and offsets are read on the device: offsets that decrease or leave [0, n_rows] are reported by the next wpsgd_check
+ * (WPSGD_ERR_CUDA), and nothing is computed.
+ *
+ * Models are fp32, [n_chains, heads_v, dv, dk], and are kept in fp32 on the way. bf16 rows are taken 64 at a time on the tensor cores: products with
+ * models, with the inverse of a chunk's triangular system and with its steps split their fp32 side into two bf16 parts (relative error of the models 3e-6 or so
+ * against 64 bits), answers and gradients use some operands rounded to bf16 once. fp32 rows are taken one by one in fp32. A NaN or an infinity stays in its
+ * chain and head; in bf16 rows it can reach the answers of up to 15 rows before it.
+ *
+ * The calls use the context's stream and device and allocate nothing: `workspace` is DEVICE memory of the caller, 16-byte aligned, of the size that
+ * wpsgd_delta_workspace gives, used until the call's work has ended. So calls can be captured, and graphs share nothing that the caller does not. */
+typedef struct {
+  const void *q, *k, *v, *g, *beta;
+  int64_t ld_q, ld_k, ld_v, ld_g, ld_beta; /* elements from row to row */
+  const int64_t* shard_off;                /* DEVICE [n_chains + 1] */
+  int64_t n_rows;
+  int32_t n_chains, heads_k, heads_v, dk, dv;
+  wpsgd_xtype type;
+  float scale;
+} wpsgd_delta_rows;
+
+typedef enum { WPSGD_DELTA_RUN = 0, WPSGD_DELTA_RUN_SAVE = 1, WPSGD_DELTA_GRAD = 2 } wpsgd_delta_use;
+
+/* Bytes of workspace for `rows` (sizes, strides, pointers and type are read; nothing is followed): for wpsgd_delta_run, for wpsgd_delta_run whose
+ * workspace then goes to wpsgd_delta_grad, and for wpsgd_delta_grad itself. */
+wpsgd_status wpsgd_delta_workspace(const wpsgd_delta_rows* rows, wpsgd_delta_use use, int64_t* bytes);
+
+/* Runs the chains.
+ *   W0         DEVICE [n_chains, heads_v, dv, dk] models to start from, or NULL for zeros.
+ *   W_out      DEVICE, the same shape: the models at the end, or NULL. May be W0.
+ *   out        DEVICE [n_rows, heads_v, dv], rows ld_out apart, of the rows' type. Rows outside every chain stay as they are.
+ *   use        WPSGD_DELTA_RUN, or WPSGD_DELTA_RUN_SAVE (bf16 rows): the workspace keeps what wpsgd_delta_grad needs. */
+wpsgd_status wpsgd_delta_run(wpsgd_ctx* ctx, const wpsgd_delta_rows* rows, const float* W0, float* W_out, void* out, int64_t ld_out,
+                             wpsgd_delta_use use, void* workspace, int64_t workspace_bytes);
+
+/* Gradients of a run (bf16 rows; WPSGD_ERR_UNSUPPORTED otherwise). rows: the same rows, unchanged; saved: the run's workspace (WPSGD_DELTA_RUN_SAVE), which is
+ * only read.
+ *   dout       DEVICE [n_rows, heads_v, dv], rows ld_dout apart: gradient of out.
+ *   dW         DEVICE [n_chains, heads_v, dv, dk] fp32: gradient of the models at the end, or NULL for zeros.
+ *   dq, dk, dv, dg, dbeta   DEVICE, contiguous, of the rows' type, shaped as q, k, v, g and beta; rows outside every chain stay as they are.
+ *   dW0        DEVICE fp32: gradient of the models at the start, or NULL. May be dW. */
+wpsgd_status wpsgd_delta_grad(wpsgd_ctx* ctx, const wpsgd_delta_rows* rows, const void* saved, int64_t saved_bytes, const void* dout, int64_t ld_dout, const float* dW,
+                              void* dq, void* dk, void* dv, void* dg, void* dbeta, float* dW0, void* workspace, int64_t workspace_bytes);
+
+/* One row for each of n_rows chains, on models that stay where they are: the form for serving. shard_off and n_chains are not used.
+ *   W          DEVICE [n_slots, heads_v, dv, dk] fp32, updated in place.
+ *   slots      DEVICE [n_rows] int32: the models of each row; negative: the row is padding, its answer stays as it is. NULL: row i has models i. A slot
+ *              past the end, or one that an earlier row has, counts as negative and is reported by the next wpsgd_check (WPSGD_ERR_CUDA).
+ *   out        DEVICE [n_rows, heads_v, dv], rows ld_out apart. */
+wpsgd_status wpsgd_delta_step(wpsgd_ctx* ctx, const wpsgd_delta_rows* rows, float* W, const int32_t* slots, int64_t n_slots, void* out, int64_t ld_out);
+
 /* Whole path from HOST buffers: copies X HOST [N, d] (dense, contiguous), y HOST [N] and w0 HOST [d]
  * (or NULL) to the device, runs the chains and the combination, copies v back to v_out HOST [d], and
  * waits for completion. Page-locked host buffers give full copy speed. Device staging buffers are

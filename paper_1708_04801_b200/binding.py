@@ -22,6 +22,8 @@ EXPORTED_SYMBOLS = [
     "wpsgd_last_error", "wpsgd_continue_csr", "wpsgd_validate_csr", "wpsgd_span_valid", "wpsgd_sample_indices_host",
     "wpsgd_check_static", "wpsgd_solve_host_csr", "wpsgd_quantize_rows", "wpsgd_margins_fp8", "wpsgd_objective_grad",
     "wpsgd_objective_grad_fp8", "wpsgd_grad_list_create", "wpsgd_grad_list_destroy", "wpsgd_grad_norm", "wpsgd_clip_grad_norm",
+    "wpsgd_sort_rows", "wpsgd_gather_rows", "wpsgd_combine_rows", "wpsgd_combine_rows_grad",
+    "wpsgd_delta_workspace", "wpsgd_delta_run", "wpsgd_delta_grad", "wpsgd_delta_step",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -87,6 +89,14 @@ def load_library() -> ctypes.CDLL:
     lib.wpsgd_grad_list_destroy.argtypes = [vp]
     lib.wpsgd_grad_norm.argtypes = [vp, vp, vp]
     lib.wpsgd_clip_grad_norm.argtypes = [vp, vp, f64, vp]
+    lib.wpsgd_sort_rows.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp]
+    lib.wpsgd_gather_rows.argtypes = [vp, vp, ci, i64, i64, vp, i64, i32, vp, i64, i64]
+    lib.wpsgd_combine_rows.argtypes = [vp, vp, ci, i64, i64, i64, vp, vp, i64, i32, vp, i64]
+    lib.wpsgd_combine_rows_grad.argtypes = [vp, vp, i64, vp, i64, ci, i64, i64, vp, vp, i64, i32, vp, i64, vp]
+    lib.wpsgd_delta_workspace.argtypes = [vp, ci, ctypes.POINTER(i64)]
+    lib.wpsgd_delta_run.argtypes = [vp, vp, vp, vp, vp, i64, ci, vp, i64]
+    lib.wpsgd_delta_grad.argtypes = [vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64]
+    lib.wpsgd_delta_step.argtypes = [vp, vp, vp, vp, i64, vp, i64]
     lib.wpsgd_launch_count.argtypes = [vp]
     lib.wpsgd_launch_count.restype = i64
     lib.wpsgd_last_error.argtypes = [vp]
@@ -246,6 +256,15 @@ class GradList:
         if getattr(self, "_h", None):
             self._lib.wpsgd_grad_list_destroy(self._h)
             self._h = None
+
+
+class DeltaSaved:
+    """What a delta_run with save=True leaves for delta_grad: its rows, which must stay as they are until then, and its workspace."""
+
+    __slots__ = ("args",)
+
+    def __init__(self, *args):
+        self.args = args
 
 
 class Context:
@@ -509,6 +528,50 @@ class Context:
         grads = self._grad_list(grads)
         r = self._rows.grad_norm(*self._head, grads._h.value, float(max_norm), norm)
         return r if r.__class__ is not int else self._ck(r, "wpsgd_clip_grad_norm")
+
+    # -- rows that go to several nodes (arguments are checked in csrc/rows_binding.cpp) -----------------------
+    def sort_rows(self, node, n_nodes: Optional[int] = None):
+        """Places [n, top] (int32, negative: no node) sorted by node: (where [n, top] int32, order [n * top] int32, shard_off
+        [n_nodes + 1] int64), all on the device. n_nodes defaults to the context's k."""
+        r = self._rows.sort_rows(*self._head, node, self.k if n_nodes is None else n_nodes)
+        return r if r.__class__ is tuple else self._ck(r, "wpsgd_sort_rows")
+
+    def gather_rows(self, X, where, out=None):
+        """Rows in the order of their nodes: out[where[i, j]] = X[i]. A new `out` has a row for every place; rows without one stay as they are."""
+        r = self._rows.gather_rows(*self._head, X, where, out)
+        return r if r.__class__ is not int else self._ck(r, "wpsgd_gather_rows")
+
+    def combine_rows(self, Y, where, weights=None, out=None):
+        """Rows back from their nodes: out[i] = sum_j weights[i, j] Y[where[i, j]] (weights None: 1, the gradient of gather_rows)."""
+        r = self._rows.combine_rows(*self._head, Y, where, weights, out)
+        return r if r.__class__ is not int else self._ck(r, "wpsgd_combine_rows")
+
+    def combine_rows_grad(self, dout, Y, where, weights=None, dY=None, dweights=None):
+        """Gradients of combine_rows: (dY like Y, whose rows without a place stay as they are, and dweights [n, top] fp32)."""
+        r = self._rows.combine_rows_grad(*self._head, dout, Y, where, weights, dY, dweights)
+        return r if r.__class__ is tuple else self._ck(r, "wpsgd_combine_rows_grad")
+
+    # -- chains whose labels are vectors (arguments are checked in csrc/rows_binding.cpp) ----------------------
+    def delta_run(self, q, k, v, g, beta, shard_off, W0=None, scale: Optional[float] = None, W_out=None, out=None, save: bool = False):
+        """Runs chains of the gated delta rule (see wpsgd_delta_run): q, k [n, heads_k, dk], v [n, heads_v, dv], g (log decay) and beta
+        [n, heads_v], float32 or bfloat16, shard_off [n_chains + 1] int64 on the device. Returns (out like v, models [n_chains, heads_v, dv, dk] fp32), and
+        with save=True (bfloat16) a DeltaSaved for delta_grad as well. scale defaults to dk ** -0.5."""
+        r = self._rows.delta_run(*self._head, q, k, v, g, beta, scale, shard_off, W0, W_out, out, bool(save))
+        if r.__class__ is not tuple:
+            self._ck(r, "wpsgd_delta_run")
+        return r[:2] if not save else (r[0], r[1], DeltaSaved(q, k, v, g, beta, scale, shard_off, r[2]))
+
+    def delta_grad(self, saved: "DeltaSaved", dout, dW=None, start: bool = False):
+        """Gradients of a delta_run with save=True from those of its answers and, if given, of its final models: (dq, dk, dv, dg, dbeta, dW0), the
+        last None unless start=True asks for the gradient of the models it started from. Rows outside every chain are not written."""
+        r = self._rows.delta_grad(*self._head, *saved.args, dout, dW, bool(start))
+        return r if r.__class__ is tuple else self._ck(r, "wpsgd_delta_grad")
+
+    def delta_step(self, q, k, v, g, beta, W, slots=None, scale: Optional[float] = None, out=None):
+        """One row for each of n chains on models W [n_slots, heads_v, dv, dk] (fp32, updated in place); slots [n] int32 says whose models each
+        row has (negative: none; None: row i has models i). Returns the answers [n, heads_v, dv]."""
+        r = self._rows.delta_step(*self._head, q, k, v, g, beta, scale, W, slots, out)
+        return r if r.__class__ is not int else self._ck(r, "wpsgd_delta_step")
 
     def solve_host(self, X, y, shard_off, n_steps, eta0, sched, lam, loss, seed, w0=None, r: float = 0.0, out=None):
         """Host tensors in (ideally pinned), host tensor out; copies are part of the call."""

@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libwpsgd.so")
 BINDING = os.path.join(HERE, "_rows.so")
 BINDING_SOURCE = os.path.join(CSRC, "rows_binding.cpp")
 OBJ = os.path.join(HERE, "_build")
-SOURCES = ["wpsgd_api.cu", "wpsgd_rows.cu"]
+SOURCES = ["wpsgd_api.cu", "wpsgd_rows.cu", "wpsgd_nodes.cu", "wpsgd_delta.cu"]
 
 
 def _nvcc() -> str:

@@ -1,0 +1,664 @@
+// Chains whose labels are vectors, 64 rows at a time on the tensor cores (gated delta rule, see include/wpsgd.h). bf16 rows, fp32 models.
+//
+// A chunk of C = 64 rows of a head from the models S (features x labels here, W^T): with b the sums of the log decays up to each row of the chunk,
+// c_i = e^{b_i}, D_ij = e^{b_i - b_j} for i >= j, the steps U (rows x labels) that all rows take solve a unit triangular system:
+//   (I + A) U = R,   A_ij = beta_i D_ij k_i.k_j (i > j),   R = beta (V - c K S)
+//   answers          O = scale (c Q S) + P U,   P_ij = scale D_ij q_i.k_j (i >= j)
+//   models after it  S' = e^{b_C} S + K^T (r U),  r_i = e^{b_C - b_i}.
+// Only S ties the chunks of a chain together. So a first kernel forms T = (I + A)^{-1} and P for all chunks at once, and a second walks
+// the chunks of each chain: three products a chunk with S, T and K, and two for the answers.
+//
+// Columns of S, U, R and O (labels) know nothing of each other. A warp of the second kernel has 16 labels for good: S^T, [16 x dk], is the fp32 accumulator
+// of mma.sync m16n8k16, whose layout is that of the A operand of the next product, so S, R and U go from product to product
+// in registers, K, Q, T and P come from shared memory as B operands (with ldmatrix, transposed where needed), and nothing is exchanged
+// between warps: no barrier but that of the ring that brings the chunks. tcgen05 would have to carry S, R and U through tensor memory and shared memory
+// between five dependent products of 64 x 16 to 128 columns, and a chain has no other work to hide that behind.
+//
+// Rounding: an fp32 factor x enters a product as two bf16 parts, x = hi + lo (2^-17 of x is left out), wherever the models come of it: K S and K^T U two
+// products, T R three. The answers, which leave as bf16, take S and P as one bf16 part and U as two.
+#pragma once
+
+#include "async.cuh"
+#include "common.cuh"
+#include "delta_rows.cuh"
+
+namespace wpsgd {
+
+constexpr int DC = 64;             // rows of a chunk
+constexpr int DC_TILE = DC + 8;    // elements from row to row of a 64 x 64 tile: ldmatrix reads 8 rows from 8 different bank groups
+constexpr int DC_TILE_BYTES = DC * DC_TILE * 2;
+// What the first kernel leaves for each chunk and head, brought by one copy: T in two parts, P, the factors of the rows, b in fp64
+struct DeltaFactors {
+  float c[DC], r[DC], beta[DC], last, pad[3];
+  double b[DC];
+};
+constexpr int DC_T_LO = DC_TILE_BYTES, DC_P = 2 * DC_TILE_BYTES, DC_FACTORS = 3 * DC_TILE_BYTES, DC_BLOCK = DC_FACTORS + (int)sizeof(DeltaFactors);
+static_assert(DC_BLOCK % 16 == 0, "blocks are copied in units of 16 bytes");
+
+struct DeltaChunk {
+  long long row0;
+  int len, chain;
+};
+
+// Rows of bf16 heads that start on 16 bytes; width a multiple of 8
+struct DeltaHeads {
+  const __nv_bfloat16* p;
+  long long ld;
+  int heads, width;
+};
+
+struct DeltaChunkParams {
+  const long long* shard_off;
+  long long n_rows;
+  int n_chains, hk, hv, dk, dv;  // dk, dv as the caller has them
+  int dvp;                       // dv rounded up to 16
+  DeltaHeads q, k, v, dout;
+  const __nv_bfloat16 *g, *beta;
+  long long ld_g, ld_beta;
+  float scale;
+  int* chunk_off;      // [n_chains + 1]: first chunk of each chain
+  int* order;          // [n_chains]: longest first
+  DeltaChunk* chunks;  // [chunk_off[n_chains]]
+  unsigned char* blocks;        // [chunks][hv][DC_BLOCK]
+  __nv_bfloat16* starts;        // [chunks][hv][dvp][DK]: models before the chunk, for the gradient
+  __nv_bfloat16* steps;         // [chunks][hv][DC][dvp]: U
+  const float* W0;
+  float* W;
+  __nv_bfloat16* out;
+  long long ld_out;
+  int vec_out, slices;
+  long long spin_limit, drop;
+  DevStatus* status;
+};
+
+// ---- tensor-core helpers ------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void stsm_t(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t smem32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t pack2(float x, float y) {  // x in the low half
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  return r;
+}
+// (x, y) = hi + lo
+__device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
+  hi = pack2(x, y);
+  lo = pack2(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
+}
+// Two neighbouring accumulator tiles [16 x 8] as the A operand of a product over their 16 columns
+__device__ __forceinline__ void a_parts(const float (&x)[4], const float (&y)[4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+  split2(x[0], x[1], hi[0], lo[0]);
+  split2(x[2], x[3], hi[1], lo[1]);
+  split2(y[0], y[1], hi[2], lo[2]);
+  split2(y[2], y[3], hi[3], lo[3]);
+}
+// Byte offset of a lane's row for 16 x 16 elements at (0, 0) of a tile with `stride` elements a row. lane_nk: B operand of [n][k] (plain), A operand of [k][m]
+// (transposed); lane_mk: A operand of [m][k] (plain), B operand of [k][n] (transposed).
+__device__ __forceinline__ uint32_t lane_nk(int lane, int stride) { return (((lane & 7) + ((lane >> 4) & 1) * 8) * stride + ((lane >> 3) & 1) * 8) * 2; }
+__device__ __forceinline__ uint32_t lane_mk(int lane, int stride) { return (((lane & 7) + ((lane >> 3) & 1) * 8) * stride + ((lane >> 4) & 1) * 8) * 2; }
+
+// ---- chunks of the chains ---------------------------------------------------------------------------------------------------------------
+// Offsets checked, chunks counted and listed, chains ordered by length. One block; offsets that are out of order leave no chunks at all.
+constexpr int PLAN_THREADS = 1024, PLAN_ORDER = 1024;  // chains that are put in order
+
+__global__ void __launch_bounds__(PLAN_THREADS) delta_plan_kernel(const __grid_constant__ DeltaChunkParams p) {
+  __shared__ int warp_sums[32], lengths[PLAN_ORDER];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  kernel_started();
+  kernel_inputs_ready();
+  int bad = 0;
+  for (int c = tid; c < p.n_chains; c += PLAN_THREADS) {
+    const long long a = p.shard_off[c], b = p.shard_off[c + 1];
+    if (a < 0 || b < a || b > p.n_rows) bad = 1;
+  }
+  bad = __syncthreads_or(bad);
+  if (bad && tid == 0) set_status(p.status, DEV_BOUNDS, 24, 0);
+  int carry = 0;
+  for (int base = 0; base < p.n_chains; base += PLAN_THREADS) {
+    const int c = base + tid;
+    int n = 0;
+    if (c < p.n_chains && !bad) n = (int)((p.shard_off[c + 1] - p.shard_off[c] + DC - 1) / DC);
+    int sum = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    if (lane == 31) warp_sums[warp] = sum;
+    __syncthreads();
+    int ws = warp_sums[lane];
+    const int w = ws;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, ws, o);
+      if (lane >= o) ws += v;
+    }
+    const int first = carry + __shfl_sync(0xffffffffu, ws - w, warp) + sum - n;
+    carry += __shfl_sync(0xffffffffu, ws, 31);
+    if (c < p.n_chains) {
+      p.chunk_off[c] = first;
+      if (c < PLAN_ORDER) lengths[c] = n;
+    }
+    __syncthreads();
+  }
+  if (tid == 0) p.chunk_off[p.n_chains] = carry;
+  __syncthreads();
+  for (int c = warp; c < p.n_chains; c += PLAN_THREADS / 32) {
+    const int first = p.chunk_off[c], n = (c + 1 < p.n_chains ? p.chunk_off[c + 1] : carry) - first;
+    const long long row0 = p.shard_off[c], rows = p.shard_off[c + 1] - row0;
+    for (int i = lane; i < n; i += 32) p.chunks[first + i] = {row0 + (long long)i * DC, (int)min((long long)DC, rows - (long long)i * DC), c};
+  }
+  for (int c = tid; c < p.n_chains; c += PLAN_THREADS) {
+    int rank = c;
+    if (p.n_chains <= PLAN_ORDER) {
+      rank = 0;
+      for (int o = 0; o < p.n_chains; ++o) rank += lengths[o] > lengths[c] || (lengths[o] == lengths[c] && o < c);
+    }
+    p.order[rank] = c;
+  }
+}
+
+// Heads of a width that is no multiple of 8, or that do not start on 16 bytes, laid out anew: [n_rows][heads][width rounded up], zeros behind.
+// Rows outside the chains are copied too, and not used.
+__global__ void __launch_bounds__(256) delta_pack_kernel(const __nv_bfloat16* from, long long ld, int heads, int width, __nv_bfloat16* to, int width8, long long n_rows) {
+  kernel_started();
+  kernel_inputs_ready();
+  const long long units = n_rows * heads * (width8 / 8);
+  for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < units; u += (long long)gridDim.x * 256) {
+    const long long head = row_of(u, width8 / 8), row = row_of(head, heads);
+    const int col = (int)(u - head * (width8 / 8)) * 8, h = (int)(head - row * heads);
+    const unsigned short* src = (const unsigned short*)from + row * ld + (long long)h * width;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = col + 2 * i < width ? src[col + 2 * i] : 0, b = col + 2 * i + 1 < width ? src[col + 2 * i + 1] : 0;
+      w[i] = a | b << 16;
+    }
+    *(uint4*)(to + head * width8 + col) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// 16 bytes to shared memory, zeros where `yes` is false
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool yes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(yes ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory"); }
+
+// ---- T, P and the factors of a chunk ----------------------------------------------------------------------------------------------------------
+// One block of four warps for each chunk and head. K K^T and Q K^T on the tensor cores, a warp with 16 rows and the columns up to them; then T by blocks: the four
+// diagonal blocks of 16 by substitution, a column to a lane, and what is below them by T_10 = -T_11 A_10 T_00, first for blocks of 16, then for
+// those of 32, all in fp32.
+constexpr int PREP_THREADS = 128, PREP_A = DC + 4;  // fp32 elements from row to row
+
+template <int DK>
+struct PrepShape {
+  static constexpr int row = DK + 8;
+  static constexpr int smem = 2 * DC * row * 2 + 2 * DC * PREP_A * 4 + DC_TILE_BYTES;
+};
+
+template <int DK>
+__global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __grid_constant__ DeltaChunkParams p) {
+  constexpr int ROW = PrepShape<DK>::row;
+  extern __shared__ __align__(16) unsigned char prep_smem[];
+  __nv_bfloat16* Ks = (__nv_bfloat16*)prep_smem;
+  __nv_bfloat16* Qs = Ks + DC * ROW;
+  float* As = (float*)(Qs + DC * ROW);
+  float* Ts = As + DC * PREP_A;
+  unsigned char* Ps = (unsigned char*)(Ts + DC * PREP_A);
+  float* Xs = (float*)prep_smem;  // over K and Q, once their products are done
+  __shared__ double bs[DC];
+  __shared__ float betas[DC];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  kernel_started();
+  kernel_inputs_ready();
+  const int chunk = blockIdx.x / p.hv, h = blockIdx.x % p.hv, kh = h / (p.hv / p.hk);
+  if (chunk >= p.chunk_off[p.n_chains]) return;
+  const DeltaChunk at = p.chunks[chunk];
+
+  for (int u = tid; u < DC * (DK / 8); u += PREP_THREADS) {
+    const int row = u / (DK / 8), col = u % (DK / 8) * 8;
+    const bool there = row < at.len && col < p.k.width;
+    const long long i = there ? at.row0 + row : 0;
+    const int c = there ? kh * p.k.width + col : 0;
+    copy16(smem32(Ks + row * ROW + col), p.k.p + i * p.k.ld + c, there);
+    copy16(smem32(Qs + row * ROW + col), p.q.p + i * p.q.ld + c, there);
+  }
+  if (warp == 0) {  // b by a scan over the lanes, two rows a lane
+    double d[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = 2 * lane + i;
+      const float gg = row < at.len ? __bfloat162float(p.g[(at.row0 + row) * p.ld_g + h]) : 0.0f;
+      d[i] = gg < DELTA_MIN_G ? DELTA_MIN_G : gg;
+      betas[row] = row < at.len ? __bfloat162float(p.beta[(at.row0 + row) * p.ld_beta + h]) : 0.0f;
+    }
+    double sum = d[0] + d[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    bs[2 * lane + 1] = sum;
+    bs[2 * lane] = sum - d[1];
+  }
+  copies_done();
+  __syncthreads();
+
+  float kk[4][2][4], qk[4][2][4];
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) kk[n][i][e] = qk[n][i][e] = 0.0f;
+  const uint32_t ka = smem32(Ks) + lane_mk(lane, ROW) + warp * 16 * ROW * 2, qa = smem32(Qs) + lane_mk(lane, ROW) + warp * 16 * ROW * 2, kb = smem32(Ks) + lane_nk(lane, ROW);
+#pragma unroll
+  for (int x = 0; x < DK / 16; ++x) {
+    uint32_t ak[4], aq[4], b[4];
+    ldsm(ak, ka + x * 32);
+    ldsm(aq, qa + x * 32);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      if (n > warp) break;
+      ldsm(b, kb + n * 16 * ROW * 2 + x * 32);
+      mma16(kk[n][0], ak, b[0], b[1]);
+      mma16(kk[n][1], ak, b[2], b[3]);
+      mma16(qk[n][0], aq, b[0], b[1]);
+      mma16(qk[n][1], aq, b[2], b[3]);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        const int row = warp * 16 + g + 4 * e, col = n * 16 + i * 8 + 2 * t;
+        float a[2], pr[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const float d = col + y <= row ? expf((float)(bs[row] - bs[col + y])) : 0.0f;
+          a[y] = col + y < row ? betas[row] * d * kk[n][i][e + y] : 0.0f;
+          pr[y] = col + y <= row ? p.scale * d * qk[n][i][e + y] : 0.0f;
+        }
+        *(float2*)(As + row * PREP_A + col) = make_float2(a[0], a[1]);
+        *(float2*)(Ts + row * PREP_A + col) = make_float2(0.0f, 0.0f);
+        *(uint32_t*)(Ps + (row * DC_TILE + col) * 2) = pack2(pr[0], pr[1]);
+      }
+  __syncthreads();
+
+  if (lane < 16) {  // column `lane` of the warp's diagonal block
+    const float* a = As + warp * 16 * (PREP_A + 1);
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float s = i == lane ? 1.0f : 0.0f;
+#pragma unroll
+      for (int m = 0; m < i; ++m) s = fmaf(-a[i * PREP_A + m], x[m], s);
+      x[i] = s;
+      Ts[warp * 16 * (PREP_A + 1) + i * PREP_A + lane] = s;
+    }
+  }
+  __syncthreads();
+  {  // blocks of 16: two of them, 4 columns of a row to a thread
+    const int o = tid / 64 * 32, r = tid % 64 / 4, c = tid % 4 * 4;
+    float x[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int m = 0; m < 16; ++m) {
+      const float a = As[(o + 16 + r) * PREP_A + o + m];
+      const float4 v = *(const float4*)(Ts + (o + m) * PREP_A + o + c);
+      x[0] = fmaf(a, v.x, x[0]), x[1] = fmaf(a, v.y, x[1]), x[2] = fmaf(a, v.z, x[2]), x[3] = fmaf(a, v.w, x[3]);
+    }
+    *(float4*)(Xs + (o / 2 + r) * 36 + c) = make_float4(x[0], x[1], x[2], x[3]);
+    __syncthreads();
+    float y[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int m = 0; m < 16; ++m) {
+      const float a = Ts[(o + 16 + r) * PREP_A + o + 16 + m];
+      const float4 v = *(const float4*)(Xs + (o / 2 + m) * 36 + c);
+      y[0] = fmaf(-a, v.x, y[0]), y[1] = fmaf(-a, v.y, y[1]), y[2] = fmaf(-a, v.z, y[2]), y[3] = fmaf(-a, v.w, y[3]);
+    }
+    *(float4*)(Ts + (o + 16 + r) * PREP_A + o + c) = make_float4(y[0], y[1], y[2], y[3]);
+    __syncthreads();
+  }
+  {  // blocks of 32: 4 columns of two rows to a thread
+    const int r = tid / 8 * 2, c = tid % 8 * 4;
+    float x[2][4] = {};
+#pragma unroll 8
+    for (int m = 0; m < 32; ++m) {
+      const float4 v = *(const float4*)(Ts + m * PREP_A + c);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float a = As[(32 + r + i) * PREP_A + m];
+        x[i][0] = fmaf(a, v.x, x[i][0]), x[i][1] = fmaf(a, v.y, x[i][1]), x[i][2] = fmaf(a, v.z, x[i][2]), x[i][3] = fmaf(a, v.w, x[i][3]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *(float4*)(Xs + (r + i) * 36 + c) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+    __syncthreads();
+    float y[2][4] = {};
+#pragma unroll 8
+    for (int m = 0; m < 32; ++m) {
+      const float4 v = *(const float4*)(Xs + m * 36 + c);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float a = Ts[(32 + r + i) * PREP_A + 32 + m];
+        y[i][0] = fmaf(-a, v.x, y[i][0]), y[i][1] = fmaf(-a, v.y, y[i][1]), y[i][2] = fmaf(-a, v.z, y[i][2]), y[i][3] = fmaf(-a, v.w, y[i][3]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *(float4*)(Ts + (32 + r + i) * PREP_A + c) = make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
+  }
+  __syncthreads();
+
+  unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int u = i * PREP_THREADS + tid, row = u / 8, col = u % 8 * 8;
+    const float4 v0 = *(const float4*)(Ts + row * PREP_A + col), v1 = *(const float4*)(Ts + row * PREP_A + col + 4);
+    uint4 hi, lo;
+    split2(v0.x, v0.y, hi.x, lo.x);
+    split2(v0.z, v0.w, hi.y, lo.y);
+    split2(v1.x, v1.y, hi.z, lo.z);
+    split2(v1.z, v1.w, hi.w, lo.w);
+    const int to = (row * DC_TILE + col) * 2;
+    *(uint4*)(block + to) = hi;
+    *(uint4*)(block + DC_T_LO + to) = lo;
+    *(uint4*)(block + DC_P + to) = *(const uint4*)(Ps + to);
+  }
+  if (tid < DC) {
+    DeltaFactors* f = (DeltaFactors*)(block + DC_FACTORS);
+    f->c[tid] = expf((float)bs[tid]);
+    f->r[tid] = expf((float)(bs[DC - 1] - bs[tid]));
+    f->beta[tid] = betas[tid];
+    f->b[tid] = bs[tid];
+    if (tid == 0) f->last = expf((float)bs[DC - 1]);
+  }
+}
+
+// ---- the walk over a chain's chunks ---------------------------------------------------------------------------------------------------------------
+// A block has a chain, a head and 16 NW labels of it: NW warps as described above, and one that brings the chunks (bulk copies, a ring of
+// `stages`).
+template <int DK, int NW>
+struct ChainShape {
+  static constexpr int row = DK + 8, vrow = 16 * NW + 8;
+  static constexpr int stage = DC_BLOCK + 2 * DC * row * 2 + DC * vrow * 2;
+  static constexpr int stages = 3 * stage <= 226 * 1024 ? 3 : 2;
+  static constexpr int smem = stages * stage;
+  static constexpr int threads = 32 * NW + 32;
+};
+
+// Columns of rows that no copy fills read as zeros
+__device__ __forceinline__ void clear_smem(unsigned char* smem, int bytes, int tid, int threads) {
+  for (int i = tid * 16; i < bytes; i += threads * 16) *(uint4*)(smem + i) = make_uint4(0, 0, 0, 0);
+}
+
+// Rows of `bytes` bytes for one chunk, by the lanes of a warp: zeros behind the chunk's end and in `more` bytes behind each row, before the copies are announced
+__device__ __forceinline__ void fill_rows(unsigned char* to, int stride, int len, int bytes, int more, int lane) {
+  for (int r = lane; r < DC; r += 32)
+    for (int i = r < len ? bytes : 0; i < bytes + more; i += 16) *(uint4*)(to + r * stride + i) = make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void copy_rows(unsigned char* to, int stride, const __nv_bfloat16* from, long long ld, int len, int bytes, int lane, unsigned long long* full) {
+  for (int r = lane; r < len; r += 32) bulk_copy_g2s(to + r * stride, from + r * ld, bytes, full);
+}
+
+// 16 labels of 64 rows from registers (labels x rows, two rows in a word) to memory, by way of the warp's own columns of the tile that its labels came in
+template <bool VEC>
+__device__ __forceinline__ void put_labels(const float (&x)[8][4], unsigned char* tile, int stride, int lane, __nv_bfloat16* to, long long ld, int rows, int cols) {
+  __syncwarp();
+  const uint32_t at = smem32(tile) + lane_nk(lane, stride / 2);
+#pragma unroll
+  for (int n = 0; n < 4; ++n) stsm_t(at + n * 16 * stride, pack2(x[2 * n][0], x[2 * n][1]), pack2(x[2 * n][2], x[2 * n][3]), pack2(x[2 * n + 1][0], x[2 * n + 1][1]), pack2(x[2 * n + 1][2], x[2 * n + 1][3]));
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int u = i * 32 + lane, row = u / 2, col = u % 2 * 8;
+    if (row >= rows || col >= cols) continue;
+    const uint4 v = *(const uint4*)(tile + row * stride + col * 2);
+    __nv_bfloat16* o = to + row * ld + col;
+    if (VEC) {
+      *(uint4*)o = v;
+    } else {
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < cols) ((unsigned short*)o)[e] = (unsigned short)(w[e / 2] >> (16 * (e % 2)));
+    }
+  }
+}
+
+template <int DK, int NW, bool SAVE>
+__global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_constant__ DeltaChunkParams p) {
+  using Shape = ChainShape<DK, NW>;
+  constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages;  // bytes from row to row
+  constexpr int Q_AT = DC * ROW, V_AT = 2 * DC * ROW, BLOCK_AT = V_AT + DC * VROW;
+  extern __shared__ __align__(16) unsigned char chain_smem[];
+  __shared__ unsigned long long full[STAGES], empty[STAGES];
+  __shared__ int dead_flag;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  kernel_started();
+  clear_smem(chain_smem, Shape::smem, tid, Shape::threads);
+  kernel_inputs_ready();
+  const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
+  const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
+  const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
+  if (tid == 0) {
+    dead_flag = 0;
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], warps);
+    }
+    mbar_fence_init();
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the zeros lie before what the copies write
+  __syncthreads();
+  volatile int* dead = &dead_flag;
+
+  if (warp == NW) {  // copies
+    const int vbytes = min(16 * NW, p.v.width - col0) * 2, kbytes = p.k.width * 2;
+    int issued = 0;
+    for (int i = 0; i < n && !*dead; ++i) {
+      const int s = i % STAGES;
+      if (i >= STAGES && !__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], (i / STAGES - 1) & 1, p.spin_limit))) {
+        if (lane == 0) {
+          set_status(p.status, DEV_TIMEOUT, 25, i);
+          *dead = 1;
+        }
+        break;
+      }
+      if (i == p.drop) break;  // test hook: this chunk and those behind it are never brought
+      const DeltaChunk at = p.chunks[first + i];
+      unsigned char* st = chain_smem + s * Shape::stage;
+      fill_rows(st, ROW, at.len, kbytes, 0, lane);
+      fill_rows(st + Q_AT, ROW, at.len, kbytes, 0, lane);
+      fill_rows(st + V_AT, VROW, at.len, vbytes, vbytes % 32, lane);  // answers have been put over a warp's 16 labels
+      __syncwarp();
+      if (lane == 0) mbar_arrive_expect_tx(&full[s], DC_BLOCK + at.len * (2 * kbytes + vbytes));
+      __syncwarp();
+      issued = i + 1;
+      if (lane == 0) bulk_copy_g2s(st + BLOCK_AT, p.blocks + ((long long)(first + i) * p.hv + h) * DC_BLOCK, DC_BLOCK, &full[s]);
+      copy_rows(st, ROW, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, kbytes, lane, &full[s]);
+      copy_rows(st + Q_AT, ROW, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, kbytes, lane, &full[s]);
+      copy_rows(st + V_AT, VROW, p.v.p + at.row0 * p.v.ld + h * p.v.width + col0, p.v.ld, at.len, vbytes, lane, &full[s]);
+    }
+    for (int i = max(0, issued - STAGES); i < issued; ++i) mbar_wait_bounded(&full[i % STAGES], (i / STAGES) & 1, DRAIN_LIMIT);  // nothing is in flight when the block leaves
+    return;
+  }
+  if (warp >= warps) return;
+
+  // S^T: labels g and g + 8 of the warp's 16, features 8 n + 2 t and the next
+  float S[DK / 8][4];
+  const int label = col0 + warp * 16 + g;
+  const long long model = ((long long)chain * p.hv + h) * p.dv;
+#pragma unroll
+  for (int x = 0; x < DK / 8; ++x)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int f = 8 * x + 2 * t + (e & 1), l = label + (e >> 1) * 8;
+      S[x][e] = p.W0 && f < p.dk && l < p.dv ? p.W0[(model + l) * p.dk + f] : 0.0f;
+    }
+
+  for (int i = 0; i < n; ++i) {
+    const int s = i % STAGES;
+    if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (i / STAGES) & 1, p.spin_limit))) {
+      if (lane == 0) {
+        set_status(p.status, DEV_TIMEOUT, 26, i);
+        *dead = 1;
+      }
+      return;
+    }
+    unsigned char* st = chain_smem + s * Shape::stage;
+    const unsigned char* block = st + BLOCK_AT;
+    const DeltaFactors* f = (const DeltaFactors*)(block + DC_FACTORS);
+    const long long which = (long long)(first + i) * p.hv + h;
+    const uint32_t k_nk = smem32(st) + lane_nk(lane, Shape::row), q_nk = k_nk + Q_AT, k_mk = smem32(st) + lane_mk(lane, Shape::row);
+    const uint32_t t_nk = smem32(block) + lane_nk(lane, DC_TILE), v_nk = smem32(st + V_AT) + warp * 32 + lane_nk(lane, Shape::vrow);
+
+    // S^T K^T and S^T Q^T
+    float R[8][4], O[8][4];
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) R[x][e] = O[x][e] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < DK / 16; ++x) {
+      uint32_t hi[4], lo[4], b[4][4];
+      a_parts(S[2 * x], S[2 * x + 1], hi, lo);
+      if (SAVE) {  // models before the chunk, one bf16 part
+        uint32_t* to = (uint32_t*)(p.starts + (which * p.dvp + label) * DK + 16 * x + 2 * t);
+        to[0] = hi[0];
+        to[4 * DK] = hi[1];
+        to[4] = hi[2];
+        to[4 * DK + 4] = hi[3];
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) ldsm(b[y], k_nk + y * 16 * ROW + x * 32);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        mma16(R[2 * y], hi, b[y][0], b[y][1]);
+        mma16(R[2 * y + 1], hi, b[y][2], b[y][3]);
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        mma16(R[2 * y], lo, b[y][0], b[y][1]);
+        mma16(R[2 * y + 1], lo, b[y][2], b[y][3]);
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) ldsm(b[y], q_nk + y * 16 * ROW + x * 32);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        mma16(O[2 * y], hi, b[y][0], b[y][1]);
+        mma16(O[2 * y + 1], hi, b[y][2], b[y][3]);
+      }
+    }
+    // R^T = beta (V^T - c S^T K^T), and the answers' share of the models
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      uint32_t v[4];
+      ldsm_t(v, v_nk + y * 16 * VROW);
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int x = 2 * y + z, at = 8 * x + 2 * t;
+        const float2 c = *(const float2*)(f->c + at), be = *(const float2*)(f->beta + at);
+        const uint32_t v0 = v[2 * z], v1 = v[2 * z + 1];
+        R[x][0] = be.x * (__uint_as_float(v0 << 16) - c.x * R[x][0]);
+        R[x][1] = be.y * (__uint_as_float(v0 & 0xffff0000u) - c.y * R[x][1]);
+        R[x][2] = be.x * (__uint_as_float(v1 << 16) - c.x * R[x][2]);
+        R[x][3] = be.y * (__uint_as_float(v1 & 0xffff0000u) - c.y * R[x][3]);
+        const float cx = p.scale * c.x, cy = p.scale * c.y;
+        O[x][0] *= cx, O[x][1] *= cy, O[x][2] *= cx, O[x][3] *= cy;
+      }
+    }
+    // U^T = R^T T^T: rows of T from the block of 16 columns on
+    float U[8][4];
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) U[x][e] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      uint32_t hi[4], lo[4], bh[4], bl[4];
+      a_parts(R[2 * x], R[2 * x + 1], hi, lo);
+#pragma unroll
+      for (int y = x; y < 4; ++y) {
+        ldsm(bh, t_nk + y * 16 * DC_TILE * 2 + x * 32);
+        ldsm(bl, t_nk + DC_T_LO + y * 16 * DC_TILE * 2 + x * 32);
+        mma16(U[2 * y], hi, bh[0], bh[1]);
+        mma16(U[2 * y + 1], hi, bh[2], bh[3]);
+        mma16(U[2 * y], lo, bh[0], bh[1]);
+        mma16(U[2 * y + 1], lo, bh[2], bh[3]);
+        mma16(U[2 * y], hi, bl[0], bl[1]);
+        mma16(U[2 * y + 1], hi, bl[2], bl[3]);
+      }
+    }
+    // O^T += U^T P^T
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      uint32_t hi[4], lo[4], b[4];
+      a_parts(U[2 * x], U[2 * x + 1], hi, lo);
+#pragma unroll
+      for (int y = x; y < 4; ++y) {
+        ldsm(b, t_nk + DC_P + y * 16 * DC_TILE * 2 + x * 32);
+        mma16(O[2 * y], hi, b[0], b[1]);
+        mma16(O[2 * y + 1], hi, b[2], b[3]);
+        mma16(O[2 * y], lo, b[0], b[1]);
+        mma16(O[2 * y + 1], lo, b[2], b[3]);
+      }
+    }
+    if (SAVE) put_labels<true>(U, st + V_AT + warp * 32, VROW, lane, p.steps + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
+    // S^T <- e^{b_C} S^T + (r U)^T K
+    const float last = f->last;
+#pragma unroll
+    for (int x = 0; x < DK / 8; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[x][e] *= last;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      uint32_t hi[4], lo[4], b[4];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const float2 r = *(const float2*)(f->r + 16 * x + 8 * z + 2 * t);
+        U[2 * x + z][0] *= r.x, U[2 * x + z][1] *= r.y, U[2 * x + z][2] *= r.x, U[2 * x + z][3] *= r.y;
+      }
+      a_parts(U[2 * x], U[2 * x + 1], hi, lo);
+#pragma unroll
+      for (int y = 0; y < DK / 16; ++y) {
+        ldsm_t(b, k_mk + x * 16 * ROW + y * 32);
+        mma16(S[2 * y], hi, b[0], b[1]);
+        mma16(S[2 * y + 1], hi, b[2], b[3]);
+        mma16(S[2 * y], lo, b[0], b[1]);
+        mma16(S[2 * y + 1], lo, b[2], b[3]);
+      }
+    }
+    const DeltaChunk at = p.chunks[first + i];
+    __nv_bfloat16* out = p.out + at.row0 * p.ld_out + h * p.dv + col0 + warp * 16;
+    const int cols = min(16, p.dv - col0 - warp * 16);
+    if (p.vec_out) put_labels<true>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, at.len, cols);
+    else put_labels<false>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, at.len, cols);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // what this warp wrote over its labels lies before the next copy
+    __syncwarp();
+    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem32(&empty[s])) : "memory");
+  }
+  if (p.W)
+#pragma unroll
+    for (int x = 0; x < DK / 8; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int f = 8 * x + 2 * t + (e & 1), l = label + (e >> 1) * 8;
+        if (f < p.dk && l < p.dv) p.W[(model + l) * p.dk + f] = S[x][e];
+      }
+}
+
+}  // namespace wpsgd

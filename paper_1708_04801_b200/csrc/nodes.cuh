@@ -1,0 +1,399 @@
+// Rows that go to several nodes: sorted by node, laid out in that order, and brought back with weights (see include/wpsgd.h).
+//
+// A row i has `top` places, each with a node (negative: none). A place is a pair (i, j), numbered i top + j; its position is where its row
+// stands among all rows sorted by node, equal nodes in the order of their places.
+#pragma once
+
+#include "common.cuh"
+
+namespace wpsgd {
+
+// ---- sorting ---------------------------------------------------------------------------------------------------------------
+// A stable counting sort in one launch: a cluster of blocks, each warp with a run of places and a counter per node in shared
+// memory. Count; add up over warps, blocks and nodes; go over the places again and hand the positions out. Lanes with the same node
+// find each other with one match instruction, so no counter is reached twice at a time and positions do not depend on timing.
+//
+// Bounds: latency. The places are read twice and the positions written once (1.5 MB for 131072 places), by at most 8 blocks: a
+// cluster's blocks exchange their counts through distributed shared memory in about 2 us, where a second launch and a grid-wide scan
+// would take as long each.
+constexpr int SORT_THREADS = 1024;
+constexpr int SORT_COUNTERS = 32768;      // of all warps of a block
+constexpr int SORT_MAX_NODES = 16384;     // counters of two warps, and a total per node beside them
+
+struct SortParams {
+  const int* node;
+  long long places;
+  int nodes, warps;  // warps of a block that count
+  long long run;     // places of a warp, a multiple of 32
+  int *where, *order;
+  long long* shard_off;
+  DevStatus* status;
+};
+
+__device__ __forceinline__ void cluster_barrier() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+__global__ void __launch_bounds__(SORT_THREADS) sort_rows_kernel(const __grid_constant__ SortParams p) {
+  extern __shared__ unsigned sort_smem[];
+  unsigned* totals = sort_smem;                // [nodes] of this block
+  unsigned* counters = sort_smem + p.nodes;    // [warps][nodes]
+  __shared__ unsigned warp_sums[32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = p.nodes;
+  unsigned rank, blocks;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));
+  kernel_started();
+  for (int i = tid; i < p.warps * n; i += SORT_THREADS) counters[i] = 0;
+  kernel_inputs_ready();
+  __syncthreads();
+
+  const long long begin = ((long long)rank * p.warps + warp) * p.run, end = min(begin + p.run, p.places);
+  unsigned* mine = counters + (size_t)warp * n;
+  constexpr int AHEAD = 8;  // loads in flight: one at a time would wait 600 cycles for each 32 places
+  // calls f(place, node or -1, lanes with the same node) for the warp's places in order
+  auto go_over = [&](auto f) {
+    for (long long at = begin; at < end; at += 32 * AHEAD) {
+      int key[AHEAD];
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        const long long e = at + a * 32 + lane;
+        key[a] = e < end ? p.node[e] : -1;
+      }
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        if (at + a * 32 >= end) break;
+        const int k = key[a] >= 0 && key[a] < n ? key[a] : -1;
+        f(at + a * 32 + lane, key[a], k, __match_any_sync(0xffffffffu, k));
+        __syncwarp();
+      }
+    }
+  };
+  if (warp < p.warps) {
+    go_over([&](long long e, int given, int k, unsigned same) {
+      if (k >= 0 && lane == __ffs(same) - 1) mine[k] += __popc(same);
+      if (given >= n) set_status(p.status, DEV_BOUNDS, 20, e);
+    });
+  }
+  __syncthreads();
+  for (int k = tid; k < n; k += SORT_THREADS) {  // counters: places of earlier warps
+    unsigned sum = 0;
+    for (int w = 0; w < p.warps; ++w) {
+      const unsigned c = counters[(size_t)w * n + k];
+      counters[(size_t)w * n + k] = sum;
+      sum += c;
+    }
+    totals[k] = sum;
+  }
+  cluster_barrier();
+
+  unsigned carry = 0;  // places of lower nodes
+  for (int base = 0; base < n; base += SORT_THREADS) {
+    const int k = base + tid;
+    unsigned all = 0, before = 0;
+    if (k < n)
+      for (unsigned r = 0; r < blocks; ++r) {
+        uint32_t from, c;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"((uint32_t)__cvta_generic_to_shared(totals + k)), "r"(r));
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(from) : "memory");
+        if (r < rank) before += c;
+        all += c;
+      }
+    unsigned sum = all;  // over the nodes up to this one
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    if (lane == 31) warp_sums[warp] = sum;
+    __syncthreads();
+    unsigned w = warp_sums[lane], ws = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned v = __shfl_up_sync(0xffffffffu, ws, o);
+      if (lane >= o) ws += v;
+    }
+    const unsigned first = carry + __shfl_sync(0xffffffffu, ws - w, warp) + sum - all;
+    carry += __shfl_sync(0xffffffffu, ws, 31);
+    if (k < n) {
+      if (rank == 0) p.shard_off[k] = first;
+      for (int v = 0; v < p.warps; ++v) counters[(size_t)v * n + k] += first + before;
+    }
+    __syncthreads();
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this block has read the others' totals
+  if (rank == 0 && tid == 0) p.shard_off[n] = carry;
+
+  if (warp < p.warps) {
+    go_over([&](long long e, int, int k, unsigned same) {
+      int pos = -1;
+      if (k >= 0) pos = (int)(mine[k] + __popc(same & ((1u << lane) - 1)));
+      __syncwarp();
+      if (k >= 0 && lane == __ffs(same) - 1) mine[k] += __popc(same);
+      if (e < end) p.where[e] = pos;
+      if (k >= 0 && p.order) p.order[pos] = (int)e;
+    });
+  }
+  if (p.order)
+    for (long long i = carry + (long long)rank * SORT_THREADS + tid; i < p.places; i += (long long)blocks * SORT_THREADS) p.order[i] = -1;
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // no block leaves while its totals are read
+}
+
+// ---- rows at any place in memory, by 16 bytes ----------------------------------------------------------------------------------
+// 16 bytes of a row from byte `c` on (c may be negative or reach behind the row's `width`: those bytes are anything). Where the row's bytes do not
+// start on 16, the two aligned units around them are read, if any byte of the row lies in them, and shifted together.
+template <bool ALIGNED>
+__device__ __forceinline__ uint4 row16(const char* row, long long c, long long width) {
+  if constexpr (ALIGNED) {
+    return ld_stream16(row + c);
+  } else {
+    const unsigned off = (unsigned)((uintptr_t)(row + c) & 15);
+    const uint4* at = (const uint4*)(row + c - off);
+    const long long from = c - off;  // of the first unit in the row
+    uint4 a = make_uint4(0, 0, 0, 0), b = a;
+    if (from + 16 > 0 && from < width) a = __ldg(at);
+    if (off == 0) return a;
+    if (from + 32 > 0 && from + 16 < width) b = __ldg(at + 1);
+    unsigned w0 = a.x, w1 = a.y, w2 = a.z, w3 = a.w, w4 = b.x, w5 = b.y, w6 = b.z, w7 = b.w;
+    if (off & 8) w0 = w2, w1 = w3, w2 = w4, w3 = w5, w4 = w6, w5 = w7;
+    if (off & 4) w0 = w1, w1 = w2, w2 = w3, w3 = w4, w4 = w5;
+    const unsigned bits = (off & 3) * 8;
+    return make_uint4(__funnelshift_r(w0, w1, bits), __funnelshift_r(w1, w2, bits), __funnelshift_r(w2, w3, bits), __funnelshift_r(w3, w4, bits));
+  }
+}
+// 16 bytes to a row from byte `c` on, a multiple of 16 in memory; those that lie in the row are written.
+template <typename XT, bool ALIGNED>
+__device__ __forceinline__ void put16(char* row, long long c, long long width, uint4 v) {
+  if (ALIGNED || (c >= 0 && c + 16 <= width)) {
+    *(uint4*)(row + c) = v;
+  } else {
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 16 / (int)sizeof(XT); ++i) {
+      const long long at = c + i * (int)sizeof(XT);
+      if (at < 0 || at >= width) continue;
+      if constexpr (sizeof(XT) == 4) *(unsigned*)(row + at) = w[i];
+      else *(unsigned short*)(row + at) = (unsigned short)(w[i / 2] >> (16 * (i % 2)));
+    }
+  }
+}
+template <typename XT>
+__device__ __forceinline__ uint4 narrow16(const float (&f)[XVec<XT>::V]) {
+  if constexpr (sizeof(XT) == 4) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  } else {
+    uint4 r;
+    unsigned* w = &r.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *(const unsigned*)&h;
+    }
+    return r;
+  }
+}
+
+// A group of 2^lg threads has a row; a thread's units of 16 bytes are 2^lg apart. Several rows to a block of 256 threads.
+constexpr int NODES_THREADS = 256;
+
+struct NodesParams {
+  const int* where;      // [n_rows, top]
+  const float* weights;  // [n_rows, top], or NULL: all 1
+  long long n_rows, n_sorted;
+  int top, lg;
+  long long width;            // bytes of a row
+  const char* rows;           // [n_rows]: read by gather and by the gradient
+  long long ld_rows;          // strides in bytes
+  const char* sorted;         // [n_sorted]: read by combine and by the gradient
+  long long ld_sorted;
+  char* out;                  // [n_rows] of combine, [n_sorted] of gather and the gradient
+  long long ld_out;
+  float* dweights;            // [n_rows, top]
+  DevStatus* status;
+};
+
+// A place's position, -1 where it has none or one outside the sorted rows (reported)
+__device__ __forceinline__ int position(const NodesParams& p, long long place, bool report) {
+  const int pos = __ldg(p.where + place);
+  if (pos >= p.n_sorted) {
+    if (report) set_status(p.status, DEV_BOUNDS, 21, place);
+    return -1;
+  }
+  return pos;
+}
+
+// out[where[i, j]] = rows[i]: every row is read once and written `top` times. Bounds: bytes.
+template <typename XT, bool ALIGNED>
+__global__ void __launch_bounds__(NODES_THREADS) gather_rows_kernel(const __grid_constant__ NodesParams p) {
+  kernel_started();
+  kernel_inputs_ready();
+  const int per = NODES_THREADS >> p.lg, t = threadIdx.x & ((1 << p.lg) - 1), step = 16 << p.lg;
+  for (long long i = (long long)blockIdx.x * per + (threadIdx.x >> p.lg); i < p.n_rows; i += (long long)gridDim.x * per) {
+    const char* row = p.rows + i * p.ld_rows;
+    if constexpr (ALIGNED) {
+      for (long long c = t * 16; c < p.width; c += 4 * step) {
+        uint4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (c + u * step < p.width) v[u] = ld_stream16(row + c + u * step);
+        for (int j = 0; j < p.top; ++j) {
+          const int pos = position(p, i * p.top + j, c == 0);
+          if (pos < 0) continue;
+          char* out = p.out + pos * p.ld_out + c;
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (c + u * step < p.width) *(uint4*)(out + u * step) = v[u];
+        }
+      }
+    } else {  // units of the output, whose rows start anywhere
+      for (int j = 0; j < p.top; ++j) {
+        const int pos = position(p, i * p.top + j, t == 0);
+        if (pos < 0) continue;
+        char* out = p.out + pos * p.ld_out;
+        for (long long c = t * 16 - (long long)((uintptr_t)out & 15); c < p.width; c += 4 * step) {
+          uint4 v[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[u] = row16<false>(row, c + u * step, p.width);
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (c + u * step < p.width) put16<XT, false>(out, c + u * step, p.width, v[u]);
+        }
+      }
+    }
+  }
+}
+
+// out[i] = sum_j weights[i, j] sorted[where[i, j]], j ascending, in fp32. Places without a position are left out, whatever their weight.
+// Four places of a unit are under way at a time. Bounds: bytes.
+template <typename XT, bool ALIGNED>
+__global__ void __launch_bounds__(NODES_THREADS) combine_rows_kernel(const __grid_constant__ NodesParams p) {
+  constexpr int V = XVec<XT>::V;
+  kernel_started();
+  kernel_inputs_ready();
+  const int per = NODES_THREADS >> p.lg, t = threadIdx.x & ((1 << p.lg) - 1), step = 16 << p.lg;
+  for (long long i = (long long)blockIdx.x * per + (threadIdx.x >> p.lg); i < p.n_rows; i += (long long)gridDim.x * per) {
+    char* out = p.out + i * p.ld_out;
+    for (long long c = t * 16 - (ALIGNED ? 0 : (long long)((uintptr_t)out & 15)); c < p.width; c += step) {
+      float acc[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+      for (int j = 0; j < p.top; j += 4) {
+        uint4 v[4];
+        float w[4];
+        bool there[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int pos = j + a < p.top ? position(p, i * p.top + j + a, t == 0 && c <= 0) : -1;
+          there[a] = pos >= 0;
+          w[a] = there[a] ? (p.weights ? __ldg(p.weights + i * p.top + j + a) : 1.0f) : 0.0f;
+          v[a] = make_uint4(0, 0, 0, 0);
+          if (there[a]) v[a] = row16<ALIGNED>(p.sorted + pos * p.ld_sorted, c, p.width);
+        }
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          if (!there[a]) continue;
+          float f[V];
+          XVec<XT>::widen(v[a], f);
+#pragma unroll
+          for (int e = 0; e < V; ++e) acc[e] = fmaf(w[a], f[e], acc[e]);
+        }
+      }
+      put16<XT, ALIGNED>(out, c, p.width, narrow16<XT>(acc));
+    }
+  }
+}
+
+// out[where[i, j]] = weights[i, j] rows[i] and dweights[i, j] = rows[i] . sorted[where[i, j]], with rows the gradient of combine's result.
+// All three are gone through once; BATCH places have their sums in registers at a time. The sums of a group's threads are
+// added in a fixed order. Bounds: bytes.
+template <typename XT, bool ALIGNED>
+__global__ void __launch_bounds__(NODES_THREADS) combine_grad_kernel(const __grid_constant__ NodesParams p) {
+  constexpr int V = XVec<XT>::V, BATCH = 4;
+  __shared__ float sums[NODES_THREADS / 32][BATCH];
+  kernel_started();
+  kernel_inputs_ready();
+  const int per = NODES_THREADS >> p.lg, g = 1 << p.lg, t = threadIdx.x & (g - 1), step = 16 << p.lg, warp = threadIdx.x >> 5;
+  // all threads of a block go round together: groups of more than a warp meet at barriers
+  for (long long i0 = (long long)blockIdx.x * per; i0 < p.n_rows; i0 += (long long)gridDim.x * per) {
+    const long long i = i0 + (threadIdx.x >> p.lg);
+    const bool row_there = i < p.n_rows;
+    const char* row = p.rows + i * p.ld_rows;
+    for (int j = 0; j < p.top; j += BATCH) {
+      int pos[BATCH];
+      float w[BATCH], dot[BATCH];
+#pragma unroll
+      for (int a = 0; a < BATCH; ++a) {
+        const long long place = i * p.top + j + a;
+        pos[a] = row_there && j + a < p.top ? position(p, place, t == 0) : -1;
+        w[a] = pos[a] >= 0 && p.weights ? __ldg(p.weights + place) : 1.0f;
+        dot[a] = 0.0f;
+      }
+      if constexpr (ALIGNED) {
+        if (row_there)
+          for (long long c = t * 16; c < p.width; c += step) {
+            float d[V], f[V];
+            uint4 v[BATCH];
+            const uint4 dv = ld_stream16(row + c);
+#pragma unroll
+            for (int a = 0; a < BATCH; ++a) v[a] = ld_stream16_if(p.sorted + (pos[a] < 0 ? 0 : pos[a]) * p.ld_sorted + c, pos[a] >= 0);
+            XVec<XT>::widen(dv, d);
+#pragma unroll
+            for (int a = 0; a < BATCH; ++a) {
+              if (pos[a] < 0) continue;
+              XVec<XT>::widen(v[a], f);
+              float o[V];
+#pragma unroll
+              for (int e = 0; e < V; ++e) {
+                dot[a] = fmaf(d[e], f[e], dot[a]);
+                o[e] = w[a] * d[e];
+              }
+              *(uint4*)(p.out + pos[a] * p.ld_out + c) = narrow16<XT>(o);
+            }
+          }
+      } else {
+#pragma unroll
+        for (int a = 0; a < BATCH; ++a) {
+          if (pos[a] < 0) continue;
+          char* out = p.out + pos[a] * p.ld_out;
+          const char* from = p.sorted + pos[a] * p.ld_sorted;
+          for (long long c = t * 16 - (long long)((uintptr_t)out & 15); c < p.width; c += step) {
+            float d[V], f[V], o[V];
+            XVec<XT>::widen(row16<false>(row, c, p.width), d);
+            XVec<XT>::widen(row16<false>(from, c, p.width), f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              const long long at = c + e * (int)sizeof(XT);
+              if (at >= 0 && at < p.width) dot[a] = fmaf(d[e], f[e], dot[a]);
+              o[e] = w[a] * d[e];
+            }
+            put16<XT, false>(out, c, p.width, narrow16<XT>(o));
+          }
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < BATCH; ++a)
+        for (int o = min(g, 32) / 2; o > 0; o >>= 1) dot[a] += __shfl_xor_sync(0xffffffffu, dot[a], o);
+      if (g > 32) {
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0)
+#pragma unroll
+          for (int a = 0; a < BATCH; ++a) sums[warp][a] = dot[a];
+        __syncthreads();
+        if (t < BATCH) {
+          float sum = 0.0f;
+          for (int v = 0; v < g / 32; ++v) sum += sums[warp + v][t];
+#pragma unroll
+          for (int a = 0; a < BATCH; ++a)
+            if (a == t) dot[a] = sum;
+        }
+      }
+      if (row_there && p.dweights) {
+        if (g >= BATCH) {
+#pragma unroll
+          for (int a = 0; a < BATCH; ++a)
+            if (t == a && j + a < p.top) p.dweights[i * p.top + j + a] = pos[a] >= 0 ? dot[a] : 0.0f;
+        }
+      }
+    }
+  }
+}
+
+}  // namespace wpsgd

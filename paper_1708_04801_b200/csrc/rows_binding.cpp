@@ -11,6 +11,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+
 #include "../../include/wpsgd.h"
 
 namespace {
@@ -217,12 +219,330 @@ PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// contiguous [n, top] of one type
+bool places(PyObject* o, const Call& c, at::ScalarType type, const char* what, Matrix* m) {
+  const at::Tensor* t = on_device(o, c, what);
+  if (!t) return false;
+  if (t->scalar_type() != type || t->dim() != 2 || !t->is_contiguous()) {
+    PyErr_Format(PyExc_TypeError, "%s: expected a contiguous 2-D %s tensor", what, at::toString(type));
+    return false;
+  }
+  m->p = t->data_ptr();
+  m->n = t->size(0);
+  m->ld = t->size(1);
+  return true;
+}
+bool same_places(const Matrix& a, const Matrix& b, const char* what) {
+  if (a.n != b.n || a.ld != b.ld) PyErr_Format(PyExc_ValueError, "%s: [%lld, %lld], expected [%lld, %lld]", what, (long long)b.n, (long long)b.ld, (long long)a.n, (long long)a.ld);
+  return a.n == b.n && a.ld == b.ld;
+}
+// the number of columns of a 2-D tensor, -1 with an error set
+int64_t columns(PyObject* o, const Call& c, const char* what) {
+  const at::Tensor* t = on_device(o, c, what);
+  if (!t) return -1;
+  if (t->dim() != 2) {
+    PyErr_Format(PyExc_ValueError, "%s: expected a 2-D tensor", what);
+    return -1;
+  }
+  return t->size(1);
+}
+// rows of either type, `cols` contiguous elements each, of the type of `like` where one is given
+bool rows_like(PyObject* o, const Call& c, int64_t cols, const Matrix* like, const char* what, Matrix* m) {
+  return matrix(o, c, like ? like->type : at::kFloat, like ? like->type : at::kBFloat16, cols, cols, what, m);
+}
+bool int32_of(PyObject* o, const char* what, int32_t* v) {
+  long long n;
+  if (!number(o, &n)) return false;
+  if (n != (int32_t)n) PyErr_Format(PyExc_ValueError, "%s: %lld", what, n);
+  *v = (int32_t)n;
+  return n == (int32_t)n;
+}
+
+// (head, node, n_nodes) -> (where, order, shard_off)
+PyObject* sort_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c;
+  Matrix node;
+  int32_t n_nodes;
+  if (!count(n_args, 6) || !head(args, &c) || !places(args[4], c, at::kInt, "node", &node) || !int32_of(args[5], "n_nodes", &n_nodes)) return nullptr;
+  if (node.ld > INT32_MAX) return PyErr_Format(PyExc_ValueError, "node: too many places a row");
+  at::Tensor where = empty(c, {node.n, node.ld}, {node.ld, 1}, at::kInt), order = empty(c, {node.n * node.ld}, {1}, at::kInt),
+             off = empty(c, {std::max<int64_t>(n_nodes, 0) + 1}, {1}, at::kLong);
+  const wpsgd_status st = wpsgd_sort_rows(c.ctx, (const int32_t*)node.p, node.n, (int32_t)node.ld, n_nodes, (int32_t*)where.data_ptr(), (int32_t*)order.data_ptr(), (int64_t*)off.data_ptr());
+  if (st) return PyLong_FromLong(st);
+  Output a, b, o;
+  a.take(std::move(where));
+  b.take(std::move(order));
+  o.take(std::move(off));
+  return PyTuple_Pack(3, a.o, b.o, o.o);
+  END_HANDLE_TH_ERRORS
+}
+
+// (head, X, where, out or None) -> out
+PyObject* gather_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c;
+  Matrix x, where, to;
+  int64_t d;
+  if (!count(n_args, 7) || !head(args, &c) || (d = columns(args[4], c, "X")) < 0 || !rows_like(args[4], c, d, nullptr, "X", &x) || !places(args[5], c, at::kInt, "where", &where)) return nullptr;
+  if (x.n != where.n) return PyErr_Format(PyExc_ValueError, "where has %lld rows, X %lld", (long long)where.n, (long long)x.n);
+  Output out;
+  if (args[6] == Py_None) out.take(empty(c, {where.n * where.ld, d}, {d, 1}, x.type));
+  else out.take(args[6]);
+  if (!rows_like(out.o, c, d, &x, "out", &to)) return nullptr;
+  const wpsgd_status st = wpsgd_gather_rows(c.ctx, x.p, element(x.type), x.ld, d, (const int32_t*)where.p, where.n, (int32_t)where.ld, to.p, to.ld, to.n);
+  if (st) return PyLong_FromLong(st);
+  Py_INCREF(out.o);
+  return out.o;
+  END_HANDLE_TH_ERRORS
+}
+
+// (head, Y, where, weights or None, out or None) -> out
+PyObject* combine_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c;
+  Matrix y, where, weights, to;
+  int64_t d;
+  if (!count(n_args, 8) || !head(args, &c) || (d = columns(args[4], c, "Y")) < 0 || !rows_like(args[4], c, d, nullptr, "Y", &y) || !places(args[5], c, at::kInt, "where", &where)) return nullptr;
+  if (args[6] != Py_None && (!places(args[6], c, at::kFloat, "weights", &weights) || !same_places(where, weights, "weights"))) return nullptr;
+  Output out;
+  if (args[7] == Py_None) out.take(empty(c, {where.n, d}, {d, 1}, y.type));
+  else out.take(args[7]);
+  if (!rows_like(out.o, c, d, &y, "out", &to)) return nullptr;
+  if (to.n != where.n) return PyErr_Format(PyExc_ValueError, "out has %lld rows, where %lld", (long long)to.n, (long long)where.n);
+  const wpsgd_status st = wpsgd_combine_rows(c.ctx, y.p, element(y.type), y.ld, d, y.n, (const int32_t*)where.p, (const float*)weights.p, where.n, (int32_t)where.ld, to.p, to.ld);
+  if (st) return PyLong_FromLong(st);
+  Py_INCREF(out.o);
+  return out.o;
+  END_HANDLE_TH_ERRORS
+}
+
+// (head, dout, Y, where, weights or None, dY or None, dweights or None) -> (dY, dweights)
+PyObject* combine_rows_grad(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c;
+  Matrix y, dout, where, weights, to, tow;
+  int64_t d;
+  if (!count(n_args, 10) || !head(args, &c) || (d = columns(args[5], c, "Y")) < 0 || !rows_like(args[5], c, d, nullptr, "Y", &y) || !rows_like(args[4], c, d, &y, "dout", &dout) ||
+      !places(args[6], c, at::kInt, "where", &where))
+    return nullptr;
+  if (args[7] != Py_None && (!places(args[7], c, at::kFloat, "weights", &weights) || !same_places(where, weights, "weights"))) return nullptr;
+  if (dout.n != where.n) return PyErr_Format(PyExc_ValueError, "dout has %lld rows, where %lld", (long long)dout.n, (long long)where.n);
+  Output dy, dw;
+  if (args[8] == Py_None) dy.take(empty(c, {y.n, d}, {d, 1}, y.type));
+  else dy.take(args[8]);
+  if (args[9] == Py_None) dw.take(empty(c, {where.n, where.ld}, {where.ld, 1}, at::kFloat));
+  else dw.take(args[9]);
+  if (!rows_like(dy.o, c, d, &y, "dY", &to) || !places(dw.o, c, at::kFloat, "dweights", &tow) || !same_places(where, tow, "dweights")) return nullptr;
+  if (to.n != y.n) return PyErr_Format(PyExc_ValueError, "dY has %lld rows, Y %lld", (long long)to.n, (long long)y.n);
+  const wpsgd_status st = wpsgd_combine_rows_grad(c.ctx, dout.p, dout.ld, y.p, y.ld, element(y.type), d, y.n, (const int32_t*)where.p, (const float*)weights.p, where.n, (int32_t)where.ld,
+                                                  to.p, to.ld, (float*)tow.p);
+  return st ? PyLong_FromLong(st) : pair(dy, dw);
+  END_HANDLE_TH_ERRORS
+}
+
+// rows [n, heads, width] of one type with heads one behind the other; ld: elements from row to row
+struct Heads {
+  const void* p = nullptr;
+  int64_t n = 0, heads = 0, width = 0, ld = 0;
+};
+bool heads_of(PyObject* o, const Call& c, at::ScalarType type, int64_t dims, const char* what, Heads* m) {
+  const at::Tensor* t = on_device(o, c, what);
+  if (!t) return false;
+  if (t->scalar_type() != type) {
+    PyErr_Format(PyExc_TypeError, "%s: expected dtype %s, got %s", what, at::toString(type), at::toString(t->scalar_type()));
+    return false;
+  }
+  if (t->dim() != dims) {
+    PyErr_Format(PyExc_ValueError, "%s: expected %lld dimensions", what, (long long)dims);
+    return false;
+  }
+  m->n = t->size(0);
+  m->heads = t->size(1);
+  m->width = dims == 3 ? t->size(2) : 1;
+  if ((m->width > 1 && t->stride(2) != 1) || (m->heads > 1 && t->stride(1) != m->width)) {
+    PyErr_Format(PyExc_ValueError, "%s: the heads of a row must lie one behind the other", what);
+    return false;
+  }
+  m->ld = m->n > 1 ? t->stride(0) : m->heads * m->width;
+  m->p = t->data_ptr();
+  return true;
+}
+bool fits32(int64_t v) { return v >= 0 && v <= INT32_MAX; }
+// q, k, v, g, beta, scale
+bool delta_rows(PyObject* const* a, const Call& c, wpsgd_delta_rows* r, at::ScalarType* type) {
+  if (!THPVariable_Check(a[0])) {
+    PyErr_Format(PyExc_TypeError, "q: expected a tensor");
+    return false;
+  }
+  *type = THPVariable_Unpack(a[0]).scalar_type();
+  if (*type != at::kFloat && *type != at::kBFloat16) {
+    PyErr_Format(PyExc_TypeError, "q: expected dtype Float or BFloat16, got %s", at::toString(*type));
+    return false;
+  }
+  Heads q, k, v, g, beta;
+  if (!heads_of(a[0], c, *type, 3, "q", &q) || !heads_of(a[1], c, *type, 3, "k", &k) || !heads_of(a[2], c, *type, 3, "v", &v) || !heads_of(a[3], c, *type, 2, "g", &g) ||
+      !heads_of(a[4], c, *type, 2, "beta", &beta))
+    return false;
+  if (k.n != q.n || v.n != q.n || g.n != q.n || beta.n != q.n || k.heads != q.heads || k.width != q.width || g.heads != v.heads || beta.heads != v.heads || !fits32(q.heads) ||
+      !fits32(q.width) || !fits32(v.heads) || !fits32(v.width)) {
+    PyErr_Format(PyExc_ValueError, "q and k are [n, heads_k, dk], v [n, heads_v, dv], g and beta [n, heads_v]");
+    return false;
+  }
+  double scale = 0.0;
+  if (a[5] == Py_None) scale = 1.0 / std::sqrt((double)q.width);
+  else scale = PyFloat_AsDouble(a[5]);
+  if (scale == -1.0 && PyErr_Occurred()) return false;
+  *r = {q.p, k.p, v.p, g.p, beta.p, q.ld, k.ld, v.ld, g.ld, beta.ld, nullptr, q.n, 0, (int32_t)q.heads, (int32_t)v.heads, (int32_t)q.width, (int32_t)v.width, element(*type), (float)scale};
+  return true;
+}
+bool shards(PyObject* o, const Call& c, wpsgd_delta_rows* r) {
+  const at::Tensor* t = on_device(o, c, "shard_off");
+  if (!t) return false;
+  if (t->scalar_type() != at::kLong || t->dim() != 1 || !t->is_contiguous() || t->numel() < 1 || !fits32(t->numel() - 1)) {
+    PyErr_Format(PyExc_TypeError, "shard_off: expected a contiguous int64 tensor [n_chains + 1]");
+    return false;
+  }
+  r->shard_off = (const int64_t*)t->data_ptr();
+  r->n_chains = (int32_t)(t->numel() - 1);
+  return true;
+}
+// models [n, heads_v, dv, dk], or None where that is allowed (then *p stays NULL)
+bool models(PyObject* o, const Call& c, const wpsgd_delta_rows& r, int64_t n, const char* what, float** p, int64_t* got = nullptr) {
+  if (o == Py_None && !got) return true;
+  const at::Tensor* t = on_device(o, c, what);
+  if (!t) return false;
+  if (t->scalar_type() != at::kFloat || !t->is_contiguous()) {
+    PyErr_Format(PyExc_TypeError, "%s: expected a contiguous float32 tensor", what);
+    return false;
+  }
+  if (t->dim() != 4 || (n >= 0 && t->size(0) != n) || t->size(1) != r.heads_v || t->size(2) != r.dv || t->size(3) != r.dk) {
+    PyErr_Format(PyExc_ValueError, "%s: expected [%s, heads_v, dv, dk]", what, n >= 0 ? "n_chains" : "n_slots");
+    return false;
+  }
+  if (got) *got = t->size(0);
+  *p = (float*)t->data_ptr();
+  return true;
+}
+bool rows_out(PyObject* o, const Call& c, at::ScalarType type, const wpsgd_delta_rows& r, const char* what, Heads* m) {
+  if (!heads_of(o, c, type, 3, what, m)) return false;
+  if (m->n != r.n_rows || m->heads != r.heads_v || m->width != r.dv) {
+    PyErr_Format(PyExc_ValueError, "%s: expected [n, heads_v, dv]", what);
+    return false;
+  }
+  return true;
+}
+// Rows that have no workspace are refused by the call that it is for, with its text
+void workspace(const Call& c, const wpsgd_delta_rows& r, wpsgd_delta_use use, at::Tensor* ws, int64_t* bytes) {
+  if (wpsgd_delta_workspace(&r, use, bytes) == WPSGD_OK) *ws = empty(c, {*bytes}, {1}, at::kByte);
+}
+
+// (head, q, k, v, g, beta, scale or None, shard_off, W0 or None, W_out or None, out or None, save) -> (out, W, workspace or None)
+PyObject* delta_run(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c;
+  wpsgd_delta_rows r;
+  at::ScalarType type;
+  if (!count(n_args, 15) || !head(args, &c) || !delta_rows(args + 4, c, &r, &type) || !shards(args[10], c, &r)) return nullptr;
+  float *W0 = nullptr, *W1 = nullptr;
+  Output W, out, saved;
+  if (args[12] == Py_None) W.take(empty(c, {r.n_chains, r.heads_v, r.dv, r.dk}, {(int64_t)r.heads_v * r.dv * r.dk, (int64_t)r.dv * r.dk, r.dk, 1}, at::kFloat));
+  else W.take(args[12]);
+  if (args[13] == Py_None) out.take(empty(c, {r.n_rows, r.heads_v, r.dv}, {(int64_t)r.heads_v * r.dv, r.dv, 1}, type));
+  else out.take(args[13]);
+  Heads o;
+  if (!models(args[11], c, r, r.n_chains, "W0", &W0) || !models(W.o, c, r, r.n_chains, "W_out", &W1) || !rows_out(out.o, c, type, r, "out", &o)) return nullptr;
+  const wpsgd_delta_use use = args[14] == Py_True ? WPSGD_DELTA_RUN_SAVE : WPSGD_DELTA_RUN;
+  at::Tensor ws;
+  int64_t bytes = 0;
+  workspace(c, r, use, &ws, &bytes);
+  const wpsgd_status st = wpsgd_delta_run(c.ctx, &r, W0, W1, (void*)o.p, o.ld, use, bytes ? ws.data_ptr() : nullptr, bytes);
+  if (st) return PyLong_FromLong(st);
+  if (use == WPSGD_DELTA_RUN_SAVE) saved.take(std::move(ws));
+  else saved.take(Py_None);
+  return PyTuple_Pack(3, out.o, W.o, saved.o);
+  END_HANDLE_TH_ERRORS
+}
+
+// (head, q, k, v, g, beta, scale or None, shard_off, saved, dout, dW or None, whether dW0 is asked for) -> (dq, dk, dv, dg, dbeta, dW0 or None)
+PyObject* delta_grad(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c;
+  wpsgd_delta_rows r;
+  at::ScalarType type;
+  if (!count(n_args, 15) || !head(args, &c) || !delta_rows(args + 4, c, &r, &type) || !shards(args[10], c, &r)) return nullptr;
+  const at::Tensor* saved = on_device(args[11], c, "saved");
+  if (!saved) return nullptr;
+  Heads dout;
+  float *dW = nullptr, *dW0 = nullptr;
+  if (!rows_out(args[12], c, type, r, "dout", &dout) || !models(args[13], c, r, r.n_chains, "dW", &dW)) return nullptr;
+  Output dq, dk, dv, dg, db, dw;
+  const int64_t n = r.n_rows, hk = r.heads_k, hv = r.heads_v;
+  const auto rows = [&](int64_t heads, int64_t width) { return empty(c, {n, heads, width}, {heads * width, width, 1}, type); };
+  at::Tensor tq = rows(hk, r.dk), tk = rows(hk, r.dk), tv = rows(hv, r.dv), tg = empty(c, {n, hv}, {hv, 1}, type), tb = empty(c, {n, hv}, {hv, 1}, type), ws;
+  if (args[14] == Py_True) {
+    at::Tensor t = empty(c, {r.n_chains, hv, r.dv, r.dk}, {hv * r.dv * r.dk, (int64_t)r.dv * r.dk, r.dk, 1}, at::kFloat);
+    dW0 = (float*)t.data_ptr();
+    dw.take(std::move(t));
+  } else {
+    dw.take(Py_None);
+  }
+  int64_t bytes = 0;
+  workspace(c, r, WPSGD_DELTA_GRAD, &ws, &bytes);
+  const wpsgd_status st = wpsgd_delta_grad(c.ctx, &r, saved->data_ptr(), (int64_t)saved->numel(), dout.p, dout.ld, dW, tq.data_ptr(), tk.data_ptr(), tv.data_ptr(), tg.data_ptr(), tb.data_ptr(), dW0,
+                        bytes ? ws.data_ptr() : nullptr, bytes);
+  if (st) return PyLong_FromLong(st);
+  dq.take(std::move(tq));
+  dk.take(std::move(tk));
+  dv.take(std::move(tv));
+  dg.take(std::move(tg));
+  db.take(std::move(tb));
+  return PyTuple_Pack(6, dq.o, dk.o, dv.o, dg.o, db.o, dw.o);
+  END_HANDLE_TH_ERRORS
+}
+
+// (head, q, k, v, g, beta, scale or None, W, slots or None, out or None) -> out
+PyObject* delta_step(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  Call c;
+  wpsgd_delta_rows r;
+  at::ScalarType type;
+  float* W = nullptr;
+  int64_t n_slots = 0;
+  const int32_t* slots = nullptr;
+  if (!count(n_args, 13) || !head(args, &c) || !delta_rows(args + 4, c, &r, &type) || !models(args[10], c, r, -1, "W", &W, &n_slots)) return nullptr;
+  if (args[11] != Py_None) {
+    const at::Tensor* t = on_device(args[11], c, "slots");
+    if (!t) return nullptr;
+    if (t->scalar_type() != at::kInt || t->dim() != 1 || !t->is_contiguous()) return PyErr_Format(PyExc_TypeError, "slots: expected a contiguous int32 tensor");
+    if (t->numel() != r.n_rows) return PyErr_Format(PyExc_ValueError, "slots: %lld, expected %lld", (long long)t->numel(), (long long)r.n_rows);
+    slots = (const int32_t*)t->data_ptr();
+  }
+  Output out;
+  if (args[12] == Py_None) out.take(empty(c, {r.n_rows, r.heads_v, r.dv}, {(int64_t)r.heads_v * r.dv, r.dv, 1}, type));
+  else out.take(args[12]);
+  Heads o;
+  if (!rows_out(out.o, c, type, r, "out", &o)) return nullptr;
+  const wpsgd_status st = wpsgd_delta_step(c.ctx, &r, W, slots, n_slots, (void*)o.p, o.ld);
+  if (st) return PyLong_FromLong(st);
+  Py_INCREF(out.o);
+  return out.o;
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"quantize_rows", (PyCFunction)(void*)quantize_rows, METH_FASTCALL, nullptr},
     {"margins_fp8", (PyCFunction)(void*)margins_fp8, METH_FASTCALL, nullptr},
     {"objective_grad", (PyCFunction)(void*)objective_grad, METH_FASTCALL, nullptr},
     {"objective_grad_fp8", (PyCFunction)(void*)objective_grad_fp8, METH_FASTCALL, nullptr},
     {"grad_norm", (PyCFunction)(void*)grad_norm, METH_FASTCALL, nullptr},
+    {"sort_rows", (PyCFunction)(void*)sort_rows, METH_FASTCALL, nullptr},
+    {"gather_rows", (PyCFunction)(void*)gather_rows, METH_FASTCALL, nullptr},
+    {"combine_rows", (PyCFunction)(void*)combine_rows, METH_FASTCALL, nullptr},
+    {"combine_rows_grad", (PyCFunction)(void*)combine_rows_grad, METH_FASTCALL, nullptr},
+    {"delta_run", (PyCFunction)(void*)delta_run, METH_FASTCALL, nullptr},
+    {"delta_grad", (PyCFunction)(void*)delta_grad, METH_FASTCALL, nullptr},
+    {"delta_step", (PyCFunction)(void*)delta_step, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rows", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
