@@ -25,14 +25,19 @@
 namespace wpsgd {
 
 constexpr int DC = 64;             // rows of a chunk
-constexpr int DC_TILE = DC + 8;    // elements from row to row of a 64 x 64 tile: ldmatrix reads 8 rows from 8 different bank groups
+constexpr int DC_TILE = DC + 8;    // elements from row to row of a 64 x 64 tile in shared memory: ldmatrix reads 8 rows from 8 different bank groups
 constexpr int DC_TILE_BYTES = DC * DC_TILE * 2;
-// What the first kernel leaves for each chunk and head, brought by one copy: T in two parts, P, the factors of the rows, b in fp64
+// Lower triangles are kept as their ten blocks of 16 x 16, 512 bytes each, block (i, j) at i (i + 1) / 2 + j. A row of a block is two units of 16 bytes, swapped in rows 4 to 7 and
+// 12 to 15, so that the 8 rows that ldmatrix reads at a time lie in different banks.
+constexpr int DC_TRI = 10 * 512;
+__host__ __device__ constexpr int tri_at(int i, int j) { return (i * (i + 1) / 2 + j) * 512; }
+__device__ __forceinline__ int tri_unit(int row, int half) { return row * 32 + ((half ^ (row >> 2 & 1)) << 4); }
+// What the first kernel leaves for each chunk and head, brought by one copy: T in two parts, P, the factors of the rows. b is held as b log2(e) = hi + lo
+// (its sums are formed in 64 bits): D_ij = 2^{(hi_i - hi_j) + (lo_i - lo_j)} is then as good as its fp32 exponent.
 struct DeltaFactors {
-  float c[DC], r[DC], beta[DC], last, pad[3];
-  double b[DC];
+  float c[DC], r[DC], beta[DC], hi[DC], lo[DC], last, pad[3];
 };
-constexpr int DC_T_LO = DC_TILE_BYTES, DC_P = 2 * DC_TILE_BYTES, DC_FACTORS = 3 * DC_TILE_BYTES, DC_BLOCK = DC_FACTORS + (int)sizeof(DeltaFactors);
+constexpr int DC_T_LO = DC_TRI, DC_P = 2 * DC_TRI, DC_FACTORS = 3 * DC_TRI, DC_BLOCK = DC_FACTORS + (int)sizeof(DeltaFactors);
 static_assert(DC_BLOCK % 16 == 0, "blocks are copied in units of 16 bytes");
 
 struct DeltaChunk {
@@ -62,6 +67,7 @@ struct DeltaChunkParams {
   unsigned char* blocks;        // [chunks][hv][DC_BLOCK]
   __nv_bfloat16* starts;        // [chunks][hv][dvp][DK]: models before the chunk, for the gradient
   __nv_bfloat16* steps;         // [chunks][hv][DC][dvp]: U
+  unsigned char* gram;          // [chunks][hv][DC_TRI]: D_ij k_i.k_j, for the gradient; NULL where it is not kept
   const float* W0;
   float* W;
   __nv_bfloat16* out;
@@ -108,6 +114,14 @@ __device__ __forceinline__ void a_parts(const float (&x)[4], const float (&y)[4]
 // (transposed); lane_mk: A operand of [m][k] (plain), B operand of [k][n] (transposed).
 __device__ __forceinline__ uint32_t lane_nk(int lane, int stride) { return (((lane & 7) + ((lane >> 4) & 1) * 8) * stride + ((lane >> 3) & 1) * 8) * 2; }
 __device__ __forceinline__ uint32_t lane_mk(int lane, int stride) { return (((lane & 7) + ((lane >> 3) & 1) * 8) * stride + ((lane >> 4) & 1) * 8) * 2; }
+// The same in a block of a triangle
+__device__ __forceinline__ uint32_t tri_nk(int lane) { return tri_unit((lane & 7) + ((lane >> 4) & 1) * 8, (lane >> 3) & 1); }
+__device__ __forceinline__ uint32_t tri_mk(int lane) { return tri_unit((lane & 7) + ((lane >> 3) & 1) * 8, (lane >> 4) & 1); }
+__device__ __forceinline__ float exp2_fast(float x) {  // 2 ulp, zero below 2^-126
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 
 // ---- chunks of the chains ---------------------------------------------------------------------------------------------------------------
 // Offsets checked, chunks counted and listed, chains ordered by length. One block; offsets that are out of order leave no chunks at all.
@@ -198,28 +212,48 @@ __device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_gr
 
 // ---- T, P and the factors of a chunk ----------------------------------------------------------------------------------------------------------
 // One block of four warps for each chunk and head. K K^T and Q K^T on the tensor cores, a warp with 16 rows and the columns up to them; then T by blocks: the four
-// diagonal blocks of 16 by substitution, a column to a lane, and what is below them by T_10 = -T_11 A_10 T_00, first for blocks of 16, then for
-// those of 32, all in fp32.
-constexpr int PREP_THREADS = 128, PREP_A = DC + 4;  // fp32 elements from row to row
+// diagonal blocks of 16 by substitution in fp32, a column to a lane, and what is below them by T_10 = -T_11 A_10 T_00, first for blocks of 16, then for
+// those of 32. These products are taken transposed, T_10^T = -(T_00^T A_10^T) T_11^T: the accumulator of the first is the A operand of the second, and
+// every factor is in two bf16 parts, three products each.
+constexpr int PREP_THREADS = 128;
 
 template <int DK>
 struct PrepShape {
   static constexpr int row = DK + 8;
-  static constexpr int smem = 2 * DC * row * 2 + 2 * DC * PREP_A * 4 + DC_TILE_BYTES;
+  static constexpr int rows = 2 * DC * row * 2, tris = 5 * DC_TRI, diag = 4 * 16 * 17 * 4;  // K and Q; T, A in two parts and P; diagonal blocks of A
+  static constexpr int smem = (rows > tris ? rows : tris) + diag;
 };
+
+// acc += a b for a = ah + al, b = bh + bl, 16 x 16 in two tiles
+__device__ __forceinline__ void mma_split(float (&c0)[4], float (&c1)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const uint32_t (&bh)[4], const uint32_t (&bl)[4]) {
+  mma16(c0, ah, bh[0], bh[1]);
+  mma16(c1, ah, bh[2], bh[3]);
+  mma16(c0, al, bh[0], bh[1]);
+  mma16(c1, al, bh[2], bh[3]);
+  mma16(c0, ah, bl[0], bl[1]);
+  mma16(c1, ah, bl[2], bl[3]);
+}
+// Two parts of a 16 x 16 accumulator, negated and transposed, to a block of T
+__device__ __forceinline__ void put_negative_t(uint32_t at, const float (&c0)[4], const float (&c1)[4]) {
+  uint32_t hi[4], lo[4];
+  split2(-c0[0], -c0[1], hi[0], lo[0]);
+  split2(-c0[2], -c0[3], hi[1], lo[1]);
+  split2(-c1[0], -c1[1], hi[2], lo[2]);
+  split2(-c1[2], -c1[3], hi[3], lo[3]);
+  stsm_t(at, hi[0], hi[1], hi[2], hi[3]);
+  stsm_t(at + DC_T_LO, lo[0], lo[1], lo[2], lo[3]);
+}
 
 template <int DK>
 __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __grid_constant__ DeltaChunkParams p) {
   constexpr int ROW = PrepShape<DK>::row;
+  constexpr int T_AT = 0, P_AT = 2 * DC_TRI, A_AT = 3 * DC_TRI;  // T and P as they are kept, then A
   extern __shared__ __align__(16) unsigned char prep_smem[];
   __nv_bfloat16* Ks = (__nv_bfloat16*)prep_smem;
   __nv_bfloat16* Qs = Ks + DC * ROW;
-  float* As = (float*)(Qs + DC * ROW);
-  float* Ts = As + DC * PREP_A;
-  unsigned char* Ps = (unsigned char*)(Ts + DC * PREP_A);
-  float* Xs = (float*)prep_smem;  // over K and Q, once their products are done
-  __shared__ double bs[DC];
-  __shared__ float betas[DC];
+  unsigned char* tris = prep_smem;  // over K and Q, once their products are done
+  float* diag = (float*)(prep_smem + PrepShape<DK>::smem - PrepShape<DK>::diag);
+  __shared__ float bhi[DC], blo[DC], betas[DC];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   kernel_started();
   kernel_inputs_ready();
@@ -235,14 +269,16 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
     copy16(smem32(Ks + row * ROW + col), p.k.p + i * p.k.ld + c, there);
     copy16(smem32(Qs + row * ROW + col), p.q.p + i * p.q.ld + c, there);
   }
-  if (warp == 0) {  // b by a scan over the lanes, two rows a lane
+  unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK;
+  if (warp == 0) {  // b by a scan over the lanes, two rows a lane, in 64 bits
     double d[2];
+    float beta[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int row = 2 * lane + i;
       const float gg = row < at.len ? __bfloat162float(p.g[(at.row0 + row) * p.ld_g + h]) : 0.0f;
       d[i] = gg < DELTA_MIN_G ? DELTA_MIN_G : gg;
-      betas[row] = row < at.len ? __bfloat162float(p.beta[(at.row0 + row) * p.ld_beta + h]) : 0.0f;
+      beta[i] = row < at.len ? __bfloat162float(p.beta[(at.row0 + row) * p.ld_beta + h]) : 0.0f;
     }
     double sum = d[0] + d[1];
 #pragma unroll
@@ -250,8 +286,23 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
       const double v = __shfl_up_sync(0xffffffffu, sum, o);
       if (lane >= o) sum += v;
     }
-    bs[2 * lane + 1] = sum;
-    bs[2 * lane] = sum - d[1];
+    const double last = __shfl_sync(0xffffffffu, sum, 31);
+    DeltaFactors* f = (DeltaFactors*)(block + DC_FACTORS);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = 2 * lane + i;
+      const double b = i ? sum : sum - d[1], b2 = b * 1.4426950408889634;
+      const float hi = (float)b2, lo = (float)(b2 - (double)hi);
+      bhi[row] = hi;
+      blo[row] = lo;
+      betas[row] = beta[i];
+      f->c[row] = expf((float)b);
+      f->r[row] = expf((float)(last - b));
+      f->beta[row] = beta[i];
+      f->hi[row] = hi;
+      f->lo[row] = lo;
+    }
+    if (lane == 0) f->last = expf((float)last);
   }
   copies_done();
   __syncthreads();
@@ -279,118 +330,112 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
       mma16(qk[n][1], aq, b[2], b[3]);
     }
   }
+  __syncthreads();
+  const float hi0 = bhi[warp * 16 + g], lo0 = blo[warp * 16 + g], hi1 = bhi[warp * 16 + g + 8], lo1 = blo[warp * 16 + g + 8], be0 = betas[warp * 16 + g], be1 = betas[warp * 16 + g + 8];
 #pragma unroll
-  for (int n = 0; n < 4; ++n)
+  for (int n = 0; n < 4; ++n) {
+    if (n > warp) break;
+    unsigned char* to = tris + (warp * (warp + 1) / 2 + n) * 512;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i) {
+      const int col = n * 16 + i * 8 + 2 * t;
+      const float2 ch = *(const float2*)(bhi + col), cl = *(const float2*)(blo + col);
 #pragma unroll
       for (int e = 0; e < 4; e += 2) {
-        const int row = warp * 16 + g + 4 * e, col = n * 16 + i * 8 + 2 * t;
-        float a[2], pr[2];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const float d = col + y <= row ? expf((float)(bs[row] - bs[col + y])) : 0.0f;
-          a[y] = col + y < row ? betas[row] * d * kk[n][i][e + y] : 0.0f;
-          pr[y] = col + y <= row ? p.scale * d * qk[n][i][e + y] : 0.0f;
+        const int row = warp * 16 + g + 4 * e;
+        const float hi = e ? hi1 : hi0, lo = e ? lo1 : lo0, be = e ? be1 : be0;
+        float d0 = exp2_fast((hi - ch.x) + (lo - cl.x)), d1 = exp2_fast((hi - ch.y) + (lo - cl.y));
+        if (n == warp) {  // selected, not multiplied: above the diagonal the exponent is of the other sign
+          d0 = col <= row ? d0 : 0.0f;
+          d1 = col + 1 <= row ? d1 : 0.0f;
         }
-        *(float2*)(As + row * PREP_A + col) = make_float2(a[0], a[1]);
-        *(float2*)(Ts + row * PREP_A + col) = make_float2(0.0f, 0.0f);
-        *(uint32_t*)(Ps + (row * DC_TILE + col) * 2) = pack2(pr[0], pr[1]);
+        const int unit = tri_unit(g + 4 * e, i) + 4 * t;
+        *(uint32_t*)(to + P_AT + unit) = pack2(p.scale * d0 * qk[n][i][e], p.scale * d1 * qk[n][i][e + 1]);
+        const float k0 = d0 * kk[n][i][e], k1 = d1 * kk[n][i][e + 1], a0 = be * k0, a1 = be * k1;
+        if (p.gram) *(uint32_t*)(p.gram + ((long long)chunk * p.hv + h) * DC_TRI + (warp * (warp + 1) / 2 + n) * 512 + unit) = pack2(k0, k1);
+        if (n == warp) {
+          float* a = diag + (warp * 16 + g + 4 * e) * 17 + i * 8 + 2 * t;
+          a[0] = a0;  // the substitution reads below the diagonal only
+          a[1] = a1;
+        } else {
+          uint32_t h2, l2;
+          split2(a0, a1, h2, l2);
+          *(uint32_t*)(to + A_AT + unit) = h2;
+          *(uint32_t*)(to + A_AT + DC_TRI + unit) = l2;
+        }
       }
-  __syncthreads();
-
+    }
+  }
+  __syncwarp();
   if (lane < 16) {  // column `lane` of the warp's diagonal block
-    const float* a = As + warp * 16 * (PREP_A + 1);
+    const float* a = diag + warp * 16 * 17;
+    unsigned char* to = tris + T_AT + (warp * (warp + 1) / 2 + warp) * 512;
     float x[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       float s = i == lane ? 1.0f : 0.0f;
 #pragma unroll
-      for (int m = 0; m < i; ++m) s = fmaf(-a[i * PREP_A + m], x[m], s);
+      for (int m = 0; m < i; ++m) s = fmaf(-a[i * 17 + m], x[m], s);
       x[i] = s;
-      Ts[warp * 16 * (PREP_A + 1) + i * PREP_A + lane] = s;
+      const __nv_bfloat16 hi = __float2bfloat16_rn(s);
+      const int unit = tri_unit(i, lane >> 3) + (lane & 7) * 2;
+      *(__nv_bfloat16*)(to + unit) = hi;
+      *(__nv_bfloat16*)(to + DC_T_LO + unit) = __float2bfloat16_rn(s - __bfloat162float(hi));
     }
   }
   __syncthreads();
-  {  // blocks of 16: two of them, 4 columns of a row to a thread
-    const int o = tid / 64 * 32, r = tid % 64 / 4, c = tid % 4 * 4;
-    float x[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int m = 0; m < 16; ++m) {
-      const float a = As[(o + 16 + r) * PREP_A + o + m];
-      const float4 v = *(const float4*)(Ts + (o + m) * PREP_A + o + c);
-      x[0] = fmaf(a, v.x, x[0]), x[1] = fmaf(a, v.y, x[1]), x[2] = fmaf(a, v.z, x[2]), x[3] = fmaf(a, v.w, x[3]);
-    }
-    *(float4*)(Xs + (o / 2 + r) * 36 + c) = make_float4(x[0], x[1], x[2], x[3]);
-    __syncthreads();
-    float y[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int m = 0; m < 16; ++m) {
-      const float a = Ts[(o + 16 + r) * PREP_A + o + 16 + m];
-      const float4 v = *(const float4*)(Xs + (o / 2 + m) * 36 + c);
-      y[0] = fmaf(-a, v.x, y[0]), y[1] = fmaf(-a, v.y, y[1]), y[2] = fmaf(-a, v.z, y[2]), y[3] = fmaf(-a, v.w, y[3]);
-    }
-    *(float4*)(Ts + (o + 16 + r) * PREP_A + o + c) = make_float4(y[0], y[1], y[2], y[3]);
-    __syncthreads();
-  }
-  {  // blocks of 32: 4 columns of two rows to a thread
-    const int r = tid / 8 * 2, c = tid % 8 * 4;
-    float x[2][4] = {};
-#pragma unroll 8
-    for (int m = 0; m < 32; ++m) {
-      const float4 v = *(const float4*)(Ts + m * PREP_A + c);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float a = As[(32 + r + i) * PREP_A + m];
-        x[i][0] = fmaf(a, v.x, x[i][0]), x[i][1] = fmaf(a, v.y, x[i][1]), x[i][2] = fmaf(a, v.z, x[i][2]), x[i][3] = fmaf(a, v.w, x[i][3]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) *(float4*)(Xs + (r + i) * 36 + c) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
-    __syncthreads();
-    float y[2][4] = {};
-#pragma unroll 8
-    for (int m = 0; m < 32; ++m) {
-      const float4 v = *(const float4*)(Xs + m * 36 + c);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float a = Ts[(32 + r + i) * PREP_A + 32 + m];
-        y[i][0] = fmaf(-a, v.x, y[i][0]), y[i][1] = fmaf(-a, v.y, y[i][1]), y[i][2] = fmaf(-a, v.z, y[i][2]), y[i][3] = fmaf(-a, v.w, y[i][3]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) *(float4*)(Ts + (32 + r + i) * PREP_A + c) = make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
+  const uint32_t nk = smem32(tris) + tri_nk(lane);
+  if (warp & 1) {  // blocks (1, 0) and (3, 2)
+    const int o = warp - 1, d0 = (o * (o + 1) / 2 + o) * 512, d1 = (warp * (warp + 1) / 2 + warp) * 512, od = (warp * (warp + 1) / 2 + o) * 512;
+    float x[2][4] = {}, y[2][4] = {};
+    uint32_t ah[4], al[4], bh[4], bl[4];
+    ldsm_t(ah, nk + T_AT + d0);
+    ldsm_t(al, nk + T_AT + DC_T_LO + d0);
+    ldsm(bh, nk + A_AT + od);
+    ldsm(bl, nk + A_AT + DC_TRI + od);
+    mma_split(x[0], x[1], ah, al, bh, bl);
+    a_parts(x[0], x[1], ah, al);
+    ldsm(bh, nk + T_AT + d1);
+    ldsm(bl, nk + T_AT + DC_T_LO + d1);
+    mma_split(y[0], y[1], ah, al, bh, bl);
+    put_negative_t(nk + T_AT + od, y[0], y[1]);
   }
   __syncthreads();
-
-  unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK;
+  {  // the block of 32: columns 16 j of it, rows 32 + 16 i
+    const int j = warp & 1, i = warp >> 1;
+    float x[4][4] = {}, y[2][4] = {};
+    uint32_t ah[4], al[4], bh[4], bl[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int u = i * PREP_THREADS + tid, row = u / 8, col = u % 8 * 8;
-    const float4 v0 = *(const float4*)(Ts + row * PREP_A + col), v1 = *(const float4*)(Ts + row * PREP_A + col + 4);
-    uint4 hi, lo;
-    split2(v0.x, v0.y, hi.x, lo.x);
-    split2(v0.z, v0.w, hi.y, lo.y);
-    split2(v1.x, v1.y, hi.z, lo.z);
-    split2(v1.z, v1.w, hi.w, lo.w);
-    const int to = (row * DC_TILE + col) * 2;
-    *(uint4*)(block + to) = hi;
-    *(uint4*)(block + DC_T_LO + to) = lo;
-    *(uint4*)(block + DC_P + to) = *(const uint4*)(Ps + to);
+    for (int m = 0; m < 2; ++m) {  // X^T = T_00^T A_10^T over rows of T_00 from its diagonal on
+      if (m < j) continue;
+      const int tt = (m * (m + 1) / 2 + j) * 512;
+      ldsm_t(ah, nk + T_AT + tt);
+      ldsm_t(al, nk + T_AT + DC_T_LO + tt);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int aa = tri_at(2 + n, m);
+        ldsm(bh, nk + A_AT + aa);
+        ldsm(bl, nk + A_AT + DC_TRI + aa);
+        mma_split(x[2 * n], x[2 * n + 1], ah, al, bh, bl);
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      if (m > i) continue;
+      const int tt = ((2 + i) * (3 + i) / 2 + 2 + m) * 512;
+      a_parts(x[2 * m], x[2 * m + 1], ah, al);
+      ldsm(bh, nk + T_AT + tt);
+      ldsm(bl, nk + T_AT + DC_T_LO + tt);
+      mma_split(y[0], y[1], ah, al, bh, bl);
+    }
+    put_negative_t(nk + T_AT + ((2 + i) * (3 + i) / 2 + j) * 512, y[0], y[1]);
   }
-  if (tid < DC) {
-    DeltaFactors* f = (DeltaFactors*)(block + DC_FACTORS);
-    f->c[tid] = expf((float)bs[tid]);
-    f->r[tid] = expf((float)(bs[DC - 1] - bs[tid]));
-    f->beta[tid] = betas[tid];
-    f->b[tid] = bs[tid];
-    if (tid == 0) f->last = expf((float)bs[DC - 1]);
-  }
+  __syncthreads();
+  for (int u = tid; u < 3 * DC_TRI / 16; u += PREP_THREADS) *(uint4*)(block + u * 16) = *(const uint4*)(tris + u * 16);
 }
 
 // ---- the walk over a chain's chunks ---------------------------------------------------------------------------------------------------------------
-// A block has a chain, a head and 16 NW labels of it: NW warps as described above, and one that brings the chunks (bulk copies, a ring of
-// `stages`).
+// A block has a chain, a head and 16 NW labels of it: NW warps as described above, and one that brings the chunks (a ring of `stages`).
 template <int DK, int NW>
 struct ChainShape {
   static constexpr int row = DK + 8, vrow = 16 * NW + 8;
@@ -400,18 +445,24 @@ struct ChainShape {
   static constexpr int threads = 32 * NW + 32;
 };
 
-// Columns of rows that no copy fills read as zeros
-__device__ __forceinline__ void clear_smem(unsigned char* smem, int bytes, int tid, int threads) {
-  for (int i = tid * 16; i < bytes; i += threads * 16) *(uint4*)(smem + i) = make_uint4(0, 0, 0, 0);
+// 64 rows of a tile, `units` units of 16 bytes a row, by the lanes of a warp; zeros behind the chunk's end and from column `width` on. (A bulk copy for each row
+// takes 64 cycles to issue, whatever its size: 0.8 ms of 1.1 for 16384 chunks of 128 features and labels.)
+template <int UNITS>
+__device__ __forceinline__ void copy_rows(unsigned char* to, int stride, const __nv_bfloat16* from, long long ld, int len, int width, int lane) {
+  constexpr int per = 32 / UNITS > 0 ? 32 / UNITS : 1;  // rows at a time
+  static_assert(UNITS <= 32 && 32 % UNITS == 0, "a warp has whole rows");
+  const int row = lane / UNITS, col = lane % UNITS * 8;
+  const bool in = col < width;
+  const __nv_bfloat16* src = from + row * ld + (in ? col : 0);
+  const uint32_t dst = smem32(to) + row * stride + col * 2;
+#pragma unroll 8
+  for (int r = 0; r < DC; r += per) {
+    const bool there = in && r + row < len;
+    copy16(dst + r * stride, there ? src + r * ld : from, there);
+  }
 }
-
-// Rows of `bytes` bytes for one chunk, by the lanes of a warp: zeros behind the chunk's end and in `more` bytes behind each row, before the copies are announced
-__device__ __forceinline__ void fill_rows(unsigned char* to, int stride, int len, int bytes, int more, int lane) {
-  for (int r = lane; r < DC; r += 32)
-    for (int i = r < len ? bytes : 0; i < bytes + more; i += 16) *(uint4*)(to + r * stride + i) = make_uint4(0, 0, 0, 0);
-}
-__device__ __forceinline__ void copy_rows(unsigned char* to, int stride, const __nv_bfloat16* from, long long ld, int len, int bytes, int lane, unsigned long long* full) {
-  for (int r = lane; r < len; r += 32) bulk_copy_g2s(to + r * stride, from + r * ld, bytes, full);
+__device__ __forceinline__ void arrive_when_copied(unsigned long long* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem32(bar)) : "memory");
 }
 
 // 16 labels of 64 rows from registers (labels x rows, two rows in a word) to memory, by way of the warp's own columns of the tile that its labels came in
@@ -449,7 +500,6 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
   __shared__ int dead_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   kernel_started();
-  clear_smem(chain_smem, Shape::smem, tid, Shape::threads);
   kernel_inputs_ready();
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
@@ -457,17 +507,15 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
   if (tid == 0) {
     dead_flag = 0;
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full[s], 1);
+      mbar_init(&full[s], 33);  // the lanes' copies, and the block's
       mbar_init(&empty[s], warps);
     }
     mbar_fence_init();
   }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the zeros lie before what the copies write
   __syncthreads();
   volatile int* dead = &dead_flag;
 
   if (warp == NW) {  // copies
-    const int vbytes = min(16 * NW, p.v.width - col0) * 2, kbytes = p.k.width * 2;
     int issued = 0;
     for (int i = 0; i < n && !*dead; ++i) {
       const int s = i % STAGES;
@@ -481,17 +529,15 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
       if (i == p.drop) break;  // test hook: this chunk and those behind it are never brought
       const DeltaChunk at = p.chunks[first + i];
       unsigned char* st = chain_smem + s * Shape::stage;
-      fill_rows(st, ROW, at.len, kbytes, 0, lane);
-      fill_rows(st + Q_AT, ROW, at.len, kbytes, 0, lane);
-      fill_rows(st + V_AT, VROW, at.len, vbytes, vbytes % 32, lane);  // answers have been put over a warp's 16 labels
-      __syncwarp();
-      if (lane == 0) mbar_arrive_expect_tx(&full[s], DC_BLOCK + at.len * (2 * kbytes + vbytes));
-      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&full[s], DC_BLOCK);
+        bulk_copy_g2s(st + BLOCK_AT, p.blocks + ((long long)(first + i) * p.hv + h) * DC_BLOCK, DC_BLOCK, &full[s]);
+      }
+      copy_rows<DK / 8>(st, ROW, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, p.k.width, lane);
+      copy_rows<DK / 8>(st + Q_AT, ROW, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, p.k.width, lane);
+      copy_rows<2 * NW>(st + V_AT, VROW, p.v.p + at.row0 * p.v.ld + h * p.v.width + col0, p.v.ld, at.len, p.v.width - col0, lane);
+      arrive_when_copied(&full[s]);
       issued = i + 1;
-      if (lane == 0) bulk_copy_g2s(st + BLOCK_AT, p.blocks + ((long long)(first + i) * p.hv + h) * DC_BLOCK, DC_BLOCK, &full[s]);
-      copy_rows(st, ROW, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, kbytes, lane, &full[s]);
-      copy_rows(st + Q_AT, ROW, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, kbytes, lane, &full[s]);
-      copy_rows(st + V_AT, VROW, p.v.p + at.row0 * p.v.ld + h * p.v.width + col0, p.v.ld, at.len, vbytes, lane, &full[s]);
     }
     for (int i = max(0, issued - STAGES); i < issued; ++i) mbar_wait_bounded(&full[i % STAGES], (i / STAGES) & 1, DRAIN_LIMIT);  // nothing is in flight when the block leaves
     return;
@@ -524,7 +570,7 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
     const DeltaFactors* f = (const DeltaFactors*)(block + DC_FACTORS);
     const long long which = (long long)(first + i) * p.hv + h;
     const uint32_t k_nk = smem32(st) + lane_nk(lane, Shape::row), q_nk = k_nk + Q_AT, k_mk = smem32(st) + lane_mk(lane, Shape::row);
-    const uint32_t t_nk = smem32(block) + lane_nk(lane, DC_TILE), v_nk = smem32(st + V_AT) + warp * 32 + lane_nk(lane, Shape::vrow);
+    const uint32_t t_nk = smem32(block) + tri_nk(lane), v_nk = smem32(st + V_AT) + warp * 32 + lane_nk(lane, Shape::vrow);
 
     // S^T K^T and S^T Q^T
     float R[8][4], O[8][4];
@@ -593,8 +639,8 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
       a_parts(R[2 * x], R[2 * x + 1], hi, lo);
 #pragma unroll
       for (int y = x; y < 4; ++y) {
-        ldsm(bh, t_nk + y * 16 * DC_TILE * 2 + x * 32);
-        ldsm(bl, t_nk + DC_T_LO + y * 16 * DC_TILE * 2 + x * 32);
+        ldsm(bh, t_nk + tri_at(y, x));
+        ldsm(bl, t_nk + DC_T_LO + tri_at(y, x));
         mma16(U[2 * y], hi, bh[0], bh[1]);
         mma16(U[2 * y + 1], hi, bh[2], bh[3]);
         mma16(U[2 * y], lo, bh[0], bh[1]);
@@ -610,7 +656,7 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
       a_parts(U[2 * x], U[2 * x + 1], hi, lo);
 #pragma unroll
       for (int y = x; y < 4; ++y) {
-        ldsm(b, t_nk + DC_P + y * 16 * DC_TILE * 2 + x * 32);
+        ldsm(b, t_nk + DC_P + tri_at(y, x));
         mma16(O[2 * y], hi, b[0], b[1]);
         mma16(O[2 * y + 1], hi, b[2], b[3]);
         mma16(O[2 * y], lo, b[0], b[1]);
@@ -647,7 +693,6 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
     const int cols = min(16, p.dv - col0 - warp * 16);
     if (p.vec_out) put_labels<true>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, at.len, cols);
     else put_labels<false>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, at.len, cols);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // what this warp wrote over its labels lies before the next copy
     __syncwarp();
     if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem32(&empty[s])) : "memory");
   }

@@ -7,10 +7,10 @@
 // from product to product. It leaves dR and G of every chunk, and a third kernel takes all chunks at once:
 //   F = scale D o tril(O' U^T),  E = -D o stril(dR U^T),
 //   dQ = scale c O' S^T + F K,   x = E K - c dR S^T,   back = F^T Q + (beta E)^T K + r U G^T,   dK = beta x + back,
-//   dbeta_i = dR_i.v_i + x_i.k_i,   db_i = q_i.dQ_i + k_i.(beta_i x_i - back_i),   db_last also takes e^{b_C} S.G + sum_i k_i.(r U G^T)_i,
-//   dg_i = sum of db from i to the chunk's end.
-// (b enters P, A, c and r; each place multiplies by e^{+-b_i} a term that q_i or k_i is a factor of, so its derivative is q_i or k_i times that term's
-// gradient. What db_last takes is S'.G, the decay's effect on all that follows.)
+//   dbeta_i = dR_i.v_i + x_i.k_i.
+// dg_i is what passes the decay of row i: with H_ab = (O' U^T)_ab P_ab - (dR U^T)_ab A_ab, what the step of row b gives the answer and the step of row a,
+//   dg_i = sum_{a >= i > b} H_ab + sum_{a >= i} (scale c_a O'_a S^T q_a - beta_a c_a dR_a S^T k_a) + sum_{b < i} r_b U_b G^T k_b + e^{b_C} S.G,
+// the first sum from the end of the chunk on by the row sums of H less its column sums: the same numbers on both sides, so that what does not pass row i cancels.
 //
 // Rounding: G in two bf16 parts in the walk's products, as are dU, scale c O' and beta c dR; S, U, G, dR, F and E are rounded to bf16
 // once where the third kernel multiplies them. Gradients leave as bf16.
@@ -41,7 +41,6 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
   __shared__ int dead_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   kernel_started();
-  clear_smem(chain_smem, Shape::smem, tid, Shape::threads);
   kernel_inputs_ready();
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);
@@ -49,17 +48,15 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
   if (tid == 0) {
     dead_flag = 0;
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full[s], 1);
+      mbar_init(&full[s], 33);
       mbar_init(&empty[s], warps);
     }
     mbar_fence_init();
   }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncthreads();
   volatile int* dead = &dead_flag;
 
   if (warp == NW) {  // copies, the last chunk first
-    const int vbytes = min(16 * NW, p.dout.width - col0) * 2, kbytes = p.k.width * 2;
     int issued = 0;
     for (int i = 0; i < n && !*dead; ++i) {
       const int s = i % STAGES, chunk = first + n - 1 - i;
@@ -73,17 +70,15 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
       if (i == p.drop) break;
       const DeltaChunk at = p.chunks[chunk];
       unsigned char* st = chain_smem + s * Shape::stage;
-      fill_rows(st, ROW, at.len, kbytes, 0, lane);
-      fill_rows(st + Q_AT, ROW, at.len, kbytes, 0, lane);
-      fill_rows(st + V_AT, VROW, at.len, vbytes, vbytes % 32, lane);
-      __syncwarp();
-      if (lane == 0) mbar_arrive_expect_tx(&full[s], DC_BLOCK + at.len * (2 * kbytes + vbytes));
-      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&full[s], DC_BLOCK);
+        bulk_copy_g2s(st + BLOCK_AT, p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK, DC_BLOCK, &full[s]);
+      }
+      copy_rows<DK / 8>(st, ROW, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, p.k.width, lane);
+      copy_rows<DK / 8>(st + Q_AT, ROW, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, p.k.width, lane);
+      copy_rows<2 * NW>(st + V_AT, VROW, p.dout.p + at.row0 * p.dout.ld + h * p.dout.width + col0, p.dout.ld, at.len, p.dout.width - col0, lane);
+      arrive_when_copied(&full[s]);
       issued = i + 1;
-      if (lane == 0) bulk_copy_g2s(st + BLOCK_AT, p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK, DC_BLOCK, &full[s]);
-      copy_rows(st, ROW, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, kbytes, lane, &full[s]);
-      copy_rows(st + Q_AT, ROW, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, kbytes, lane, &full[s]);
-      copy_rows(st + V_AT, VROW, p.dout.p + at.row0 * p.dout.ld + h * p.dout.width + col0, p.dout.ld, at.len, vbytes, lane, &full[s]);
     }
     for (int i = max(0, issued - STAGES); i < issued; ++i) mbar_wait_bounded(&full[i % STAGES], (i / STAGES) & 1, DRAIN_LIMIT);
     return;
@@ -115,7 +110,7 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
     const DeltaFactors* f = (const DeltaFactors*)(block + DC_FACTORS);
     const long long which = (long long)chunk * p.hv + h;
     const uint32_t k_nk = smem32(st) + lane_nk(lane, Shape::row), k_mk = smem32(st) + lane_mk(lane, Shape::row), q_mk = k_mk + Q_AT;
-    const uint32_t t_mk = smem32(block) + lane_mk(lane, DC_TILE), v_nk = smem32(st + V_AT) + warp * 32 + lane_nk(lane, Shape::vrow);
+    const uint32_t t_mk = smem32(block) + tri_mk(lane), v_nk = smem32(st + V_AT) + warp * 32 + lane_nk(lane, Shape::vrow);
 
     // dU^T = r G^T K^T + O'^T P
     float M[8][4];
@@ -162,7 +157,7 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
       ldsm_t(a, v_nk + x * 16 * VROW);
 #pragma unroll
       for (int y = 0; y <= x; ++y) {
-        ldsm_t(b, t_mk + DC_P + x * 16 * DC_TILE * 2 + y * 32);
+        ldsm_t(b, t_mk + DC_P + tri_at(x, y));
         mma16(M[2 * y], a, b[0], b[1]);
         mma16(M[2 * y + 1], a, b[2], b[3]);
       }
@@ -192,8 +187,8 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
       a_parts(M[2 * x], M[2 * x + 1], hi, lo);
 #pragma unroll
       for (int y = 0; y <= x; ++y) {
-        ldsm_t(bh, t_mk + x * 16 * DC_TILE * 2 + y * 32);
-        ldsm_t(bl, t_mk + DC_T_LO + x * 16 * DC_TILE * 2 + y * 32);
+        ldsm_t(bh, t_mk + tri_at(x, y));
+        ldsm_t(bl, t_mk + DC_T_LO + tri_at(x, y));
         mma16(R[2 * y], hi, bh[0], bh[1]);
         mma16(R[2 * y + 1], hi, bh[2], bh[3]);
         mma16(R[2 * y], lo, bh[0], bh[1]);
@@ -231,7 +226,6 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
     const int cols = min(16, p.dv - col0 - warp * 16);
     if (gp.vec_dv) put_labels<true>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, at.len, cols);
     else put_labels<false>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, at.len, cols);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem32(&empty[s])) : "memory");
   }
@@ -255,7 +249,7 @@ template <int DK>
 struct RowsShape {
   static constexpr int row = DK + 8, vrow = ROWS_SLICE + 8;
   static constexpr int models = ROWS_SLICE * row * 2, labels = DC * vrow * 2, stage = 2 * models + 4 * labels;
-  static constexpr int qk = 2 * DC * row * 2, tiles = 3 * DC_TILE_BYTES, sums = 4 * DC * 4 * 4, totals = 2 * DC * DK * 4;
+  static constexpr int qk = 2 * DC * row * 2, tiles = 3 * DC_TILE_BYTES, sums = 4 * DC * 5 * 4, totals = 2 * DC * DK * 4;
   static constexpr int smem(bool grouped) { return qk + 2 * stage + tiles + (int)sizeof(DeltaFactors) + sums + (grouped ? totals : 0); }
 };
 
@@ -272,7 +266,8 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
   unsigned char *Es = Fs + DC_TILE_BYTES, *Bs = Es + DC_TILE_BYTES;  // E, and beta E
   DeltaFactors* f = (DeltaFactors*)(Bs + DC_TILE_BYTES);
   float* sums = (float*)(f + 1);  // [4 quarters][DC][4]
-  float* totals = sums + 4 * DC * 4;
+  float* cols = sums + 4 * DC * 4;  // [4 blocks of rows][DC]
+  float* totals = cols + 4 * DC;
   __shared__ float label_dots[DC], model_dots[ROWS_THREADS / 32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, wr = warp & 3, wc = warp >> 2;
   kernel_started();
@@ -320,6 +315,20 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     const unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK + DC_FACTORS;
     for (int i = tid; i < (int)sizeof(DeltaFactors) / 16; i += ROWS_THREADS) copy16(smem32((unsigned char*)f + i * 16), block + i * 16, true);
     bring(h, 0);
+    uint32_t P2[2][2], K2[2][2];  // two elements each of P and D o K K^T, laid out as dP and dA
+    if (wc <= wr) {
+      const long long which = (long long)chunk * p.hv + h;
+      const unsigned char *from = p.blocks + which * DC_BLOCK + DC_P, *gram = p.gram + which * DC_TRI;
+      const int at_tri = (wr * (wr + 1) / 2 + wc) * 512;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int unit = at_tri + tri_unit(g + 8 * e, x) + 4 * t;
+          P2[x][e] = __ldg((const uint32_t*)(from + unit));
+          K2[x][e] = __ldg((const uint32_t*)(gram + unit));
+        }
+    }
     float dP[2][4], dA[2][4], aQ[NT][4], aX[NT][4], aH[NT][4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -383,23 +392,44 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
       __syncthreads();
     }
 
-    // F, E and beta E of the warp's 16 x 16 elements
+    // F, E and beta E of the warp's 16 x 16 elements, and the sums of H over its rows and columns
+    float row_p[2] = {}, row_a[2] = {}, col_h[2][2] = {};
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int e = 0; e < 4; e += 2) {
         const int i = row0 + g + 4 * e, j = wc * 16 + 8 * x + 2 * t;
-        float F[2], E[2];
+        float F[2] = {}, E[2] = {};
+        if (wc <= wr) {
+          const float be = f->beta[i];
+          const uint32_t p2 = P2[x][e / 2], k2 = K2[x][e / 2];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const float d = j + y <= i ? expf((float)(f->b[i] - f->b[j + y])) : 0.0f;
-          F[y] = j + y <= i ? p.scale * d * dP[x][e + y] : 0.0f;
-          E[y] = j + y < i ? -d * dA[x][e + y] : 0.0f;
+          for (int y = 0; y < 2; ++y) {
+            const float d = exp2_fast((f->hi[i] - f->hi[j + y]) + (f->lo[i] - f->lo[j + y]));
+            const float pp = y ? __uint_as_float(p2 & 0xffff0000u) : __uint_as_float(p2 << 16), kk = y ? __uint_as_float(k2 & 0xffff0000u) : __uint_as_float(k2 << 16);
+            const bool below = j + y < i;
+            F[y] = j + y <= i ? p.scale * d * dP[x][e + y] : 0.0f;
+            E[y] = below ? -d * dA[x][e + y] : 0.0f;
+            const float hp = below ? dP[x][e + y] * pp : 0.0f, ha = below ? -dA[x][e + y] * kk : 0.0f;
+            row_p[e / 2] += hp;
+            row_a[e / 2] += ha;
+            col_h[x][y] += fmaf(be, ha, hp);
+          }
         }
         const int to = (i * DC_TILE + j) * 2;
         *(uint32_t*)(Fs + to) = pack2(F[0], F[1]);
         *(uint32_t*)(Es + to) = pack2(E[0], E[1]);
         *(uint32_t*)(Bs + to) = pack2(f->beta[i] * E[0], f->beta[i] * E[1]);
+      }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        float v = col_h[x][y];
+        v += __shfl_xor_sync(0xffffffffu, v, 4);
+        v += __shfl_xor_sync(0xffffffffu, v, 8);
+        v += __shfl_xor_sync(0xffffffffu, v, 16);
+        if (g == 0) cols[wr * DC + wc * 16 + 8 * x + 2 * t + y] = v;
       }
     label_dot += __shfl_xor_sync(0xffffffffu, label_dot, 1);
     label_dot += __shfl_xor_sync(0xffffffffu, label_dot, 2);
@@ -410,8 +440,9 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     __syncthreads();
 
     const int i0 = row0 + g, i1 = i0 + 8;
-    float dots[4][2] = {};  // q.dQ, k.x, k.back, k.(r U G^T) of rows i0 and i1
     const float c0 = f->c[i0], c1 = f->c[i1], r0 = f->r[i0], r1 = f->r[i1], be0 = f->beta[i0], be1 = f->beta[i1];
+    // of rows i0 and i1: what passes from S and from H's rows, x.k, k.(r U G^T)
+    float dots[3][2] = {{fmaf(be0, row_a[0], row_p[0]), fmaf(be1, row_a[1], row_p[1])}, {row_a[0], row_a[1]}, {0.0f, 0.0f}};
     auto pair_at = [&](const __nv_bfloat16* tile, int row, int x) {  // two elements of a row in the warp's columns
       const uint32_t v = *(const uint32_t*)(tile + row * ROW + colw + 8 * x + 2 * t);
       return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
@@ -421,9 +452,14 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
       aQ[x][0] *= p.scale * c0, aQ[x][1] *= p.scale * c0, aQ[x][2] *= p.scale * c1, aQ[x][3] *= p.scale * c1;
       aX[x][0] *= -c0, aX[x][1] *= -c0, aX[x][2] *= -c1, aX[x][3] *= -c1;
       aH[x][0] *= r0, aH[x][1] *= r0, aH[x][2] *= r1, aH[x][3] *= r1;
-      const float2 k0 = pair_at(Ks, i0, x), k1 = pair_at(Ks, i1, x);
-      dots[3][0] += k0.x * aH[x][0] + k0.y * aH[x][1];
-      dots[3][1] += k1.x * aH[x][2] + k1.y * aH[x][3];
+      const float2 k0 = pair_at(Ks, i0, x), k1 = pair_at(Ks, i1, x), q0 = pair_at(Qs, i0, x), q1 = pair_at(Qs, i1, x);
+      const float x0 = k0.x * aX[x][0] + k0.y * aX[x][1], x1 = k1.x * aX[x][2] + k1.y * aX[x][3];
+      dots[0][0] += fmaf(be0, x0, q0.x * aQ[x][0] + q0.y * aQ[x][1]);
+      dots[0][1] += fmaf(be1, x1, q1.x * aQ[x][2] + q1.y * aQ[x][3]);
+      dots[1][0] += x0;
+      dots[1][1] += x1;
+      dots[2][0] += k0.x * aH[x][0] + k0.y * aH[x][1];
+      dots[2][1] += k1.x * aH[x][2] + k1.y * aH[x][3];
     }
     const uint32_t k_mk = smem32(Ks) + lane_mk(lane, ROW) + colw * 2, q_mk = smem32(Qs) + lane_mk(lane, ROW) + colw * 2;
     const uint32_t f_mk = smem32(Fs) + lane_mk(lane, DC_TILE) + row0 * DC_TILE * 2, f_nk = smem32(Fs) + lane_nk(lane, DC_TILE) + row0 * 2;
@@ -458,18 +494,11 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     }
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
-      const float2 k0 = pair_at(Ks, i0, x), k1 = pair_at(Ks, i1, x), q0 = pair_at(Qs, i0, x), q1 = pair_at(Qs, i1, x);
-      dots[0][0] += q0.x * aQ[x][0] + q0.y * aQ[x][1];
-      dots[0][1] += q1.x * aQ[x][2] + q1.y * aQ[x][3];
-      dots[1][0] += k0.x * aX[x][0] + k0.y * aX[x][1];
-      dots[1][1] += k1.x * aX[x][2] + k1.y * aX[x][3];
-      dots[2][0] += k0.x * aH[x][0] + k0.y * aH[x][1];
-      dots[2][1] += k1.x * aH[x][2] + k1.y * aH[x][3];
       aX[x][0] = fmaf(be0, aX[x][0], aH[x][0]), aX[x][1] = fmaf(be0, aX[x][1], aH[x][1]);  // dK
       aX[x][2] = fmaf(be1, aX[x][2], aH[x][2]), aX[x][3] = fmaf(be1, aX[x][3], aH[x][3]);
     }
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+    for (int d = 0; d < 3; ++d)
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
         float v = dots[d][z];
@@ -524,12 +553,13 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
         const int i = 2 * lane + z;
-        float v[4] = {0, 0, 0, 0};
+        float v[3] = {0, 0, 0};
         for (int w = 0; w < 4; ++w)
 #pragma unroll
-          for (int d = 0; d < 4; ++d) v[d] += sums[(w * DC + i) * 4 + d];
-        db[z] = v[0] + f->beta[i] * v[1] - v[2];
-        ahead += v[3];
+          for (int d = 0; d < 3; ++d) v[d] += sums[(w * DC + i) * 4 + d];
+        for (int w = i / 16; w < 4; ++w) v[0] -= cols[w * DC + i];
+        db[z] = v[0] - v[2];
+        ahead += v[2];
         if (i < at.len) gp.dbeta[(at.row0 + i) * p.hv + h] = __float2bfloat16_rn(label_dots[i] + v[1]);
       }
       const float decay = f->last * warp_sum(lane < ROWS_THREADS / 32 ? model_dots[lane] : 0.0f) + warp_sum(ahead);

@@ -87,8 +87,8 @@ wpsgd_status run_step(wpsgd_ctx* c, const DeltaRowsParams& p) {
 struct DeltaLayout {
   long long chunks;  // at most: the offsets are known on the device only
   int DK, dvp, dk8, dv8;
-  bool pack_k, pack_v;
-  size_t chunk_off, order, table, q, k, v, blocks, starts, steps, total;
+  bool pack_k, pack_v, kept;
+  size_t chunk_off, order, table, q, k, v, blocks, starts, steps, gram, total;
   DeltaLayout(const wpsgd_delta_rows* r, bool save) {
     auto fits = [](const void* p, int64_t ld, int width) { return width % 8 == 0 && aligned16(p) && ld % 8 == 0; };
     chunks = r->n_rows / DC + r->n_chains;
@@ -113,7 +113,9 @@ struct DeltaLayout {
     blocks = take((size_t)chunks * r->heads_v * DC_BLOCK);
     starts = take(save ? (size_t)chunks * r->heads_v * dvp * DK * 2 : 0);
     steps = take(save ? (size_t)chunks * r->heads_v * DC * dvp * 2 : 0);
+    gram = take(save ? (size_t)chunks * r->heads_v * DC_TRI : 0);
     total = at;
+    kept = save;
   }
 };
 
@@ -134,6 +136,7 @@ DeltaChunkParams chunk_params(const wpsgd_ctx* c, const wpsgd_delta_rows* r, con
   p.blocks = ws + lay.blocks;
   p.starts = (__nv_bfloat16*)(ws + lay.starts);
   p.steps = (__nv_bfloat16*)(ws + lay.steps);
+  p.gram = lay.kept ? ws + lay.gram : nullptr;
   p.spin_limit = c->opt_spin_limit, p.drop = c->opt_drop_block;
   p.status = c->status;
   return p;
