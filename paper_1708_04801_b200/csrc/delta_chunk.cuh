@@ -11,11 +11,11 @@
 // Columns of S, U, R and O (labels) know nothing of each other. A warp of the second kernel has 16 labels for good: S^T, [16 x dk], is the fp32 accumulator
 // of mma.sync m16n8k16, whose layout is that of the A operand of the next product, so S, R and U go from product to product
 // in registers, K, Q, T and P come from shared memory as B operands (with ldmatrix, transposed where needed), and nothing is exchanged
-// between warps: no barrier but that of the ring that brings the chunks. tcgen05 would have to carry S, R and U through tensor memory and shared memory
+// between warps: no barrier but those of the ring that brings the chunks. tcgen05 would have to carry S, R and U through tensor memory and shared memory
 // between five dependent products of 64 x 16 to 128 columns, and a chain has no other work to hide that behind.
 //
-// Rounding: an fp32 factor x enters a product as two bf16 parts, x = hi + lo (2^-17 of x is left out), wherever the models come of it: K S and K^T U two
-// products, T R three. The answers, which leave as bf16, take S and P as one bf16 part and U as two.
+// Rounding: an fp32 factor x enters a product as two bf16 parts, x = hi + lo (2^-17 of x is left out): K S and K^T U
+// two products, T R and P U three. The answers, which leave as bf16, take S as one bf16 part (1e-3 of them; one part of P would be 2.5e-3).
 #pragma once
 
 #include "async.cuh"
@@ -32,12 +32,12 @@ constexpr int DC_TILE_BYTES = DC * DC_TILE * 2;
 constexpr int DC_TRI = 10 * 512;
 __host__ __device__ constexpr int tri_at(int i, int j) { return (i * (i + 1) / 2 + j) * 512; }
 __device__ __forceinline__ int tri_unit(int row, int half) { return row * 32 + ((half ^ (row >> 2 & 1)) << 4); }
-// What the first kernel leaves for each chunk and head, brought by one copy: T in two parts, P, the factors of the rows. b is held as b log2(e) = hi + lo
+// What the first kernel leaves for each chunk and head, brought by one copy: T and P in two parts each, the factors of the rows. b is held as b log2(e) = hi + lo
 // (its sums are formed in 64 bits): D_ij = 2^{(hi_i - hi_j) + (lo_i - lo_j)} is then as good as its fp32 exponent.
 struct DeltaFactors {
   float c[DC], r[DC], beta[DC], hi[DC], lo[DC], last, pad[3];
 };
-constexpr int DC_T_LO = DC_TRI, DC_P = 2 * DC_TRI, DC_FACTORS = 3 * DC_TRI, DC_BLOCK = DC_FACTORS + (int)sizeof(DeltaFactors);
+constexpr int DC_T_LO = DC_TRI, DC_P = 2 * DC_TRI, DC_P_LO = 3 * DC_TRI, DC_FACTORS = 4 * DC_TRI, DC_BLOCK = DC_FACTORS + (int)sizeof(DeltaFactors);
 static_assert(DC_BLOCK % 16 == 0, "blocks are copied in units of 16 bytes");
 
 struct DeltaChunk {
@@ -220,7 +220,7 @@ constexpr int PREP_THREADS = 128;
 template <int DK>
 struct PrepShape {
   static constexpr int row = DK + 8;
-  static constexpr int rows = 2 * DC * row * 2, tris = 5 * DC_TRI, diag = 4 * 16 * 17 * 4;  // K and Q; T, A in two parts and P; diagonal blocks of A
+  static constexpr int rows = 2 * DC * row * 2, tris = 6 * DC_TRI, diag = 4 * 16 * 17 * 4;  // K and Q; T, P and A in two parts; diagonal blocks of A
   static constexpr int smem = (rows > tris ? rows : tris) + diag;
 };
 
@@ -247,7 +247,7 @@ __device__ __forceinline__ void put_negative_t(uint32_t at, const float (&c0)[4]
 template <int DK>
 __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __grid_constant__ DeltaChunkParams p) {
   constexpr int ROW = PrepShape<DK>::row;
-  constexpr int T_AT = 0, P_AT = 2 * DC_TRI, A_AT = 3 * DC_TRI;  // T and P as they are kept, then A
+  constexpr int T_AT = 0, P_AT = DC_P, A_AT = 4 * DC_TRI;  // T and P as they are kept, then A
   extern __shared__ __align__(16) unsigned char prep_smem[];
   __nv_bfloat16* Ks = (__nv_bfloat16*)prep_smem;
   __nv_bfloat16* Qs = Ks + DC * ROW;
@@ -350,7 +350,10 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
           d1 = col + 1 <= row ? d1 : 0.0f;
         }
         const int unit = tri_unit(g + 4 * e, i) + 4 * t;
-        *(uint32_t*)(to + P_AT + unit) = pack2(p.scale * d0 * qk[n][i][e], p.scale * d1 * qk[n][i][e + 1]);
+        uint32_t h2, l2;
+        split2(p.scale * d0 * qk[n][i][e], p.scale * d1 * qk[n][i][e + 1], h2, l2);
+        *(uint32_t*)(to + P_AT + unit) = h2;
+        *(uint32_t*)(to + P_AT + DC_TRI + unit) = l2;
         const float k0 = d0 * kk[n][i][e], k1 = d1 * kk[n][i][e + 1], a0 = be * k0, a1 = be * k1;
         if (p.gram) *(uint32_t*)(p.gram + ((long long)chunk * p.hv + h) * DC_TRI + (warp * (warp + 1) / 2 + n) * 512 + unit) = pack2(k0, k1);
         if (n == warp) {
@@ -358,7 +361,6 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
           a[0] = a0;  // the substitution reads below the diagonal only
           a[1] = a1;
         } else {
-          uint32_t h2, l2;
           split2(a0, a1, h2, l2);
           *(uint32_t*)(to + A_AT + unit) = h2;
           *(uint32_t*)(to + A_AT + DC_TRI + unit) = l2;
@@ -431,39 +433,49 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
     put_negative_t(nk + T_AT + ((2 + i) * (3 + i) / 2 + j) * 512, y[0], y[1]);
   }
   __syncthreads();
-  for (int u = tid; u < 3 * DC_TRI / 16; u += PREP_THREADS) *(uint4*)(block + u * 16) = *(const uint4*)(tris + u * 16);
+  for (int u = tid; u < 4 * DC_TRI / 16; u += PREP_THREADS) *(uint4*)(block + u * 16) = *(const uint4*)(tris + u * 16);
 }
 
 // ---- the walk over a chain's chunks ---------------------------------------------------------------------------------------------------------------
-// A block has a chain, a head and 16 NW labels of it: NW warps as described above, and one that brings the chunks (a ring of `stages`).
+// A block has a chain, a head and 16 NW labels of it: NW warps as described above. Each brings its share of the next chunk while it works on this one, so that a
+// scheduler's registers go to the two warps that multiply (a ninth warp that only copies would leave them 168 each). Three stages where they fit: a warp may be a
+// chunk ahead of the slowest.
 template <int DK, int NW>
 struct ChainShape {
   static constexpr int row = DK + 8, vrow = 16 * NW + 8;
-  static constexpr int stage = DC_BLOCK + 2 * DC * row * 2 + DC * vrow * 2;
+  static constexpr int q_at = DC * row * 2, v_at = 2 * q_at, block_at = v_at + DC * vrow * 2, stage = block_at + DC_BLOCK;
   static constexpr int stages = 3 * stage <= 226 * 1024 ? 3 : 2;
   static constexpr int smem = stages * stage;
-  static constexpr int threads = 32 * NW + 32;
+  static constexpr int threads = 32 * NW;
 };
 
-// 64 rows of a tile, `units` units of 16 bytes a row, by the lanes of a warp; zeros behind the chunk's end and from column `width` on. (A bulk copy for each row
-// takes 64 cycles to issue, whatever its size: 0.8 ms of 1.1 for 16384 chunks of 128 features and labels.)
+// A warp's share of 64 rows of a tile, `UNITS` units of 16 bytes a row; zeros behind the chunk's end and from column `width` on. (A bulk copy for each row takes 64
+// cycles to issue, whatever its size: 0.8 ms for 16384 chunks of 128 features and labels.)
 template <int UNITS>
-__device__ __forceinline__ void copy_rows(unsigned char* to, int stride, const __nv_bfloat16* from, long long ld, int len, int width, int lane) {
-  constexpr int per = 32 / UNITS > 0 ? 32 / UNITS : 1;  // rows at a time
+__device__ __forceinline__ void copy_rows(uint32_t to, int stride, const __nv_bfloat16* from, long long ld, int len, int width, int warp, int warps, int lane) {
+  constexpr int per = 32 / UNITS;  // rows at a time
   static_assert(UNITS <= 32 && 32 % UNITS == 0, "a warp has whole rows");
-  const int row = lane / UNITS, col = lane % UNITS * 8;
-  const bool in = col < width;
-  const __nv_bfloat16* src = from + row * ld + (in ? col : 0);
-  const uint32_t dst = smem32(to) + row * stride + col * 2;
-#pragma unroll 8
-  for (int r = 0; r < DC; r += per) {
-    const bool there = in && r + row < len;
-    copy16(dst + r * stride, there ? src + r * ld : from, there);
+  const int col = lane % UNITS * 8;
+#pragma unroll 4
+  for (int r = warp * per + lane / UNITS; r < DC; r += warps * per) {
+    const bool there = col < width && r < len;
+    copy16(to + r * stride + col * 2, from + (there ? r * ld + col : 0), there);
   }
 }
-__device__ __forceinline__ void arrive_when_copied(unsigned long long* bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem32(bar)) : "memory");
+// A warp's share of a chunk: features, queries, labels (or their gradients) and the block of the first kernel. The barrier takes an arrival of every thread.
+template <int DK, int NW>
+__device__ __forceinline__ void bring_chunk(const DeltaChunkParams& p, const DeltaHeads& labels, uint32_t st, int chunk, int h, int kh, int col0, int warp, int warps, int lane, unsigned long long* full) {
+  using Shape = ChainShape<DK, NW>;
+  const DeltaChunk at = p.chunks[chunk];
+  copy_rows<DK / 8>(st, Shape::row * 2, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, p.k.width, warp, warps, lane);
+  copy_rows<DK / 8>(st + Shape::q_at, Shape::row * 2, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, p.q.width, warp, warps, lane);
+  copy_rows<2 * NW>(st + Shape::v_at, Shape::vrow * 2, labels.p + at.row0 * labels.ld + h * labels.width + col0, labels.ld, at.len, labels.width - col0, warp, warps, lane);
+  const unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK;
+#pragma unroll 4
+  for (int i = (warp * 32 + lane) * 16; i < DC_BLOCK; i += warps * 512) copy16(st + Shape::block_at + i, block + i, true);
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem32(full)) : "memory");
 }
+__device__ __forceinline__ void arrive(unsigned long long* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem32(bar)) : "memory"); }
 
 // 16 labels of 64 rows from registers (labels x rows, two rows in a word) to memory, by way of the warp's own columns of the tile that its labels came in
 template <bool VEC>
@@ -491,13 +503,11 @@ __device__ __forceinline__ void put_labels(const float (&x)[8][4], unsigned char
 }
 
 template <int DK, int NW, bool SAVE>
-__global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_constant__ DeltaChunkParams p) {
+__global__ void __launch_bounds__(32 * NW) delta_chain_kernel(const __grid_constant__ DeltaChunkParams p) {
   using Shape = ChainShape<DK, NW>;
-  constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages;  // bytes from row to row
-  constexpr int Q_AT = DC * ROW, V_AT = 2 * DC * ROW, BLOCK_AT = V_AT + DC * VROW;
+  constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages, Q_AT = Shape::q_at, V_AT = Shape::v_at;  // bytes
   extern __shared__ __align__(16) unsigned char chain_smem[];
   __shared__ unsigned long long full[STAGES], empty[STAGES];
-  __shared__ int dead_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   kernel_started();
   kernel_inputs_ready();
@@ -505,44 +515,15 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
   if (tid == 0) {
-    dead_flag = 0;
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full[s], 33);  // the lanes' copies, and the block's
+      mbar_init(&full[s], 32 * warps);
       mbar_init(&empty[s], warps);
     }
     mbar_fence_init();
   }
   __syncthreads();
-  volatile int* dead = &dead_flag;
-
-  if (warp == NW) {  // copies
-    int issued = 0;
-    for (int i = 0; i < n && !*dead; ++i) {
-      const int s = i % STAGES;
-      if (i >= STAGES && !__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], (i / STAGES - 1) & 1, p.spin_limit))) {
-        if (lane == 0) {
-          set_status(p.status, DEV_TIMEOUT, 25, i);
-          *dead = 1;
-        }
-        break;
-      }
-      if (i == p.drop) break;  // test hook: this chunk and those behind it are never brought
-      const DeltaChunk at = p.chunks[first + i];
-      unsigned char* st = chain_smem + s * Shape::stage;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(&full[s], DC_BLOCK);
-        bulk_copy_g2s(st + BLOCK_AT, p.blocks + ((long long)(first + i) * p.hv + h) * DC_BLOCK, DC_BLOCK, &full[s]);
-      }
-      copy_rows<DK / 8>(st, ROW, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, p.k.width, lane);
-      copy_rows<DK / 8>(st + Q_AT, ROW, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, p.k.width, lane);
-      copy_rows<2 * NW>(st + V_AT, VROW, p.v.p + at.row0 * p.v.ld + h * p.v.width + col0, p.v.ld, at.len, p.v.width - col0, lane);
-      arrive_when_copied(&full[s]);
-      issued = i + 1;
-    }
-    for (int i = max(0, issued - STAGES); i < issued; ++i) mbar_wait_bounded(&full[i % STAGES], (i / STAGES) & 1, DRAIN_LIMIT);  // nothing is in flight when the block leaves
-    return;
-  }
   if (warp >= warps) return;
+  if (n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem), first, h, kh, col0, warp, warps, lane, &full[0]);
 
   // S^T: labels g and g + 8 of the warp's 16, features 8 n + 2 t and the next
   float S[DK / 8][4];
@@ -557,16 +538,19 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
     }
 
   for (int i = 0; i < n; ++i) {
-    const int s = i % STAGES;
-    if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (i / STAGES) & 1, p.spin_limit))) {
-      if (lane == 0) {
-        set_status(p.status, DEV_TIMEOUT, 26, i);
-        *dead = 1;
-      }
+    const int s = i % STAGES, s1 = (i + 1) % STAGES;
+    bool ok = true;
+    if (i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
+      if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s1], ((i + 1) / STAGES - 1) & 1, p.spin_limit));
+      if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem) + s1 * Shape::stage, first + i + 1, h, kh, col0, warp, warps, lane, &full[s1]);
+    }
+    if (!ok || !__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (i / STAGES) & 1, p.spin_limit))) {
+      if (lane == 0) set_status(p.status, DEV_TIMEOUT, 25, i);
+      copies_done();  // none of this warp's is in flight when it leaves
       return;
     }
     unsigned char* st = chain_smem + s * Shape::stage;
-    const unsigned char* block = st + BLOCK_AT;
+    const unsigned char* block = st + Shape::block_at;
     const DeltaFactors* f = (const DeltaFactors*)(block + DC_FACTORS);
     const long long which = (long long)(first + i) * p.hv + h;
     const uint32_t k_nk = smem32(st) + lane_nk(lane, Shape::row), q_nk = k_nk + Q_AT, k_mk = smem32(st) + lane_mk(lane, Shape::row);
@@ -641,26 +625,19 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
       for (int y = x; y < 4; ++y) {
         ldsm(bh, t_nk + tri_at(y, x));
         ldsm(bl, t_nk + DC_T_LO + tri_at(y, x));
-        mma16(U[2 * y], hi, bh[0], bh[1]);
-        mma16(U[2 * y + 1], hi, bh[2], bh[3]);
-        mma16(U[2 * y], lo, bh[0], bh[1]);
-        mma16(U[2 * y + 1], lo, bh[2], bh[3]);
-        mma16(U[2 * y], hi, bl[0], bl[1]);
-        mma16(U[2 * y + 1], hi, bl[2], bl[3]);
+        mma_split(U[2 * y], U[2 * y + 1], hi, lo, bh, bl);
       }
     }
     // O^T += U^T P^T
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      uint32_t hi[4], lo[4], b[4];
+      uint32_t hi[4], lo[4], bh[4], bl[4];
       a_parts(U[2 * x], U[2 * x + 1], hi, lo);
 #pragma unroll
       for (int y = x; y < 4; ++y) {
-        ldsm(b, t_nk + DC_P + tri_at(y, x));
-        mma16(O[2 * y], hi, b[0], b[1]);
-        mma16(O[2 * y + 1], hi, b[2], b[3]);
-        mma16(O[2 * y], lo, b[0], b[1]);
-        mma16(O[2 * y + 1], lo, b[2], b[3]);
+        ldsm(bh, t_nk + DC_P + tri_at(y, x));
+        ldsm(bl, t_nk + DC_P_LO + tri_at(y, x));
+        mma_split(O[2 * y], O[2 * y + 1], hi, lo, bh, bl);
       }
     }
     if (SAVE) put_labels<true>(U, st + V_AT + warp * 32, VROW, lane, p.steps + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
@@ -694,7 +671,7 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_chain_kernel(const __grid_
     if (p.vec_out) put_labels<true>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, at.len, cols);
     else put_labels<false>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, at.len, cols);
     __syncwarp();
-    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem32(&empty[s])) : "memory");
+    if (lane == 0) arrive(&empty[s]);
   }
   if (p.W)
 #pragma unroll

@@ -12,7 +12,7 @@
 //   dg_i = sum_{a >= i > b} H_ab + sum_{a >= i} (scale c_a O'_a S^T q_a - beta_a c_a dR_a S^T k_a) + sum_{b < i} r_b U_b G^T k_b + e^{b_C} S.G,
 // the first sum from the end of the chunk on by the row sums of H less its column sums: the same numbers on both sides, so that what does not pass row i cancels.
 //
-// Rounding: G in two bf16 parts in the walk's products, as are dU, scale c O' and beta c dR; S, U, G, dR, F and E are rounded to bf16
+// Rounding: G, P, dU, scale c O' and beta c dR in two bf16 parts in the walk's products; S, U, G, dR, F and E are rounded to bf16
 // once where the third kernel multiplies them. Gradients leave as bf16.
 #pragma once
 
@@ -31,59 +31,28 @@ struct DeltaGradParams {
 };
 
 template <int DK, int NW>
-__global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_constant__ DeltaGradParams gp) {
-  using Shape = ChainShape<DK, NW>;
-  constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages;
-  constexpr int Q_AT = DC * ROW, V_AT = 2 * DC * ROW, BLOCK_AT = V_AT + DC * VROW;
+__global__ void __launch_bounds__(32 * NW) delta_back_kernel(const __grid_constant__ DeltaGradParams gp) {
   const DeltaChunkParams& p = gp.f;
+  using Shape = ChainShape<DK, NW>;
+  constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages, Q_AT = Shape::q_at, V_AT = Shape::v_at;  // bytes
   extern __shared__ __align__(16) unsigned char chain_smem[];
   __shared__ unsigned long long full[STAGES], empty[STAGES];
-  __shared__ int dead_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   kernel_started();
   kernel_inputs_ready();
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
-  const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);
+  const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
   if (tid == 0) {
-    dead_flag = 0;
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full[s], 33);
+      mbar_init(&full[s], 32 * warps);
       mbar_init(&empty[s], warps);
     }
     mbar_fence_init();
   }
   __syncthreads();
-  volatile int* dead = &dead_flag;
-
-  if (warp == NW) {  // copies, the last chunk first
-    int issued = 0;
-    for (int i = 0; i < n && !*dead; ++i) {
-      const int s = i % STAGES, chunk = first + n - 1 - i;
-      if (i >= STAGES && !__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], (i / STAGES - 1) & 1, p.spin_limit))) {
-        if (lane == 0) {
-          set_status(p.status, DEV_TIMEOUT, 27, i);
-          *dead = 1;
-        }
-        break;
-      }
-      if (i == p.drop) break;
-      const DeltaChunk at = p.chunks[chunk];
-      unsigned char* st = chain_smem + s * Shape::stage;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(&full[s], DC_BLOCK);
-        bulk_copy_g2s(st + BLOCK_AT, p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK, DC_BLOCK, &full[s]);
-      }
-      copy_rows<DK / 8>(st, ROW, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, p.k.width, lane);
-      copy_rows<DK / 8>(st + Q_AT, ROW, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, p.k.width, lane);
-      copy_rows<2 * NW>(st + V_AT, VROW, p.dout.p + at.row0 * p.dout.ld + h * p.dout.width + col0, p.dout.ld, at.len, p.dout.width - col0, lane);
-      arrive_when_copied(&full[s]);
-      issued = i + 1;
-    }
-    for (int i = max(0, issued - STAGES); i < issued; ++i) mbar_wait_bounded(&full[i % STAGES], (i / STAGES) & 1, DRAIN_LIMIT);
-    return;
-  }
   if (warp >= warps) return;
+  if (n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem), first + n - 1, h, kh, col0, warp, warps, lane, &full[0]);
 
   float G[DK / 8][4];  // G^T, as S^T in the forward walk
   const int label = col0 + warp * 16 + g;
@@ -97,17 +66,21 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
     }
 
   for (int i = 0; i < n; ++i) {
-    const int s = i % STAGES, chunk = first + n - 1 - i;
-    if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (i / STAGES) & 1, p.spin_limit))) {
-      if (lane == 0) {
-        set_status(p.status, DEV_TIMEOUT, 28, i);
-        *dead = 1;
-      }
+    const int s = i % STAGES, s1 = (i + 1) % STAGES;
+    bool ok = true;
+    if (i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
+      if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s1], ((i + 1) / STAGES - 1) & 1, p.spin_limit));
+      if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem) + s1 * Shape::stage, first + n - 2 - i, h, kh, col0, warp, warps, lane, &full[s1]);
+    }
+    if (!ok || !__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (i / STAGES) & 1, p.spin_limit))) {
+      if (lane == 0) set_status(p.status, DEV_TIMEOUT, 26, i);
+      copies_done();  // none of this warp's is in flight when it leaves
       return;
     }
     unsigned char* st = chain_smem + s * Shape::stage;
-    const unsigned char* block = st + BLOCK_AT;
+    const unsigned char* block = st + Shape::block_at;
     const DeltaFactors* f = (const DeltaFactors*)(block + DC_FACTORS);
+    const int chunk = first + n - 1 - i;
     const long long which = (long long)chunk * p.hv + h;
     const uint32_t k_nk = smem32(st) + lane_nk(lane, Shape::row), k_mk = smem32(st) + lane_mk(lane, Shape::row), q_mk = k_mk + Q_AT;
     const uint32_t t_mk = smem32(block) + tri_mk(lane), v_nk = smem32(st + V_AT) + warp * 32 + lane_nk(lane, Shape::vrow);
@@ -160,6 +133,9 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
         ldsm_t(b, t_mk + DC_P + tri_at(x, y));
         mma16(M[2 * y], a, b[0], b[1]);
         mma16(M[2 * y + 1], a, b[2], b[3]);
+        ldsm_t(b, t_mk + DC_P_LO + tri_at(x, y));
+        mma16(M[2 * y], a, b[0], b[1]);
+        mma16(M[2 * y + 1], a, b[2], b[3]);
       }
 #pragma unroll
       for (int z = 0; z < 4; ++z) {
@@ -189,12 +165,7 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
       for (int y = 0; y <= x; ++y) {
         ldsm_t(bh, t_mk + tri_at(x, y));
         ldsm_t(bl, t_mk + DC_T_LO + tri_at(x, y));
-        mma16(R[2 * y], hi, bh[0], bh[1]);
-        mma16(R[2 * y + 1], hi, bh[2], bh[3]);
-        mma16(R[2 * y], lo, bh[0], bh[1]);
-        mma16(R[2 * y + 1], lo, bh[2], bh[3]);
-        mma16(R[2 * y], hi, bl[0], bl[1]);
-        mma16(R[2 * y + 1], hi, bl[2], bl[3]);
+        mma_split(R[2 * y], R[2 * y + 1], hi, lo, bh, bl);
       }
     }
     put_labels<true>(R, st + V_AT + warp * 32, VROW, lane, gp.drs + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
@@ -227,7 +198,7 @@ __global__ void __launch_bounds__(32 * NW + 32) delta_back_kernel(const __grid_c
     if (gp.vec_dv) put_labels<true>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, at.len, cols);
     else put_labels<false>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, at.len, cols);
     __syncwarp();
-    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem32(&empty[s])) : "memory");
+    if (lane == 0) arrive(&empty[s]);
   }
   if (gp.dW0)
 #pragma unroll
@@ -315,7 +286,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     const unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK + DC_FACTORS;
     for (int i = tid; i < (int)sizeof(DeltaFactors) / 16; i += ROWS_THREADS) copy16(smem32((unsigned char*)f + i * 16), block + i * 16, true);
     bring(h, 0);
-    uint32_t P2[2][2], K2[2][2];  // two elements each of P and D o K K^T, laid out as dP and dA
+    uint32_t P2[2][2], L2[2][2], K2[2][2];  // two elements each of P (in two parts) and D o K K^T, laid out as dP and dA
     if (wc <= wr) {
       const long long which = (long long)chunk * p.hv + h;
       const unsigned char *from = p.blocks + which * DC_BLOCK + DC_P, *gram = p.gram + which * DC_TRI;
@@ -326,6 +297,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
         for (int e = 0; e < 2; ++e) {
           const int unit = at_tri + tri_unit(g + 8 * e, x) + 4 * t;
           P2[x][e] = __ldg((const uint32_t*)(from + unit));
+          L2[x][e] = __ldg((const uint32_t*)(from + DC_TRI + unit));
           K2[x][e] = __ldg((const uint32_t*)(gram + unit));
         }
     }
@@ -402,11 +374,12 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
         float F[2] = {}, E[2] = {};
         if (wc <= wr) {
           const float be = f->beta[i];
-          const uint32_t p2 = P2[x][e / 2], k2 = K2[x][e / 2];
+          const uint32_t p2 = P2[x][e / 2], l2 = L2[x][e / 2], k2 = K2[x][e / 2];
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const float d = exp2_fast((f->hi[i] - f->hi[j + y]) + (f->lo[i] - f->lo[j + y]));
-            const float pp = y ? __uint_as_float(p2 & 0xffff0000u) : __uint_as_float(p2 << 16), kk = y ? __uint_as_float(k2 & 0xffff0000u) : __uint_as_float(k2 << 16);
+            const float pp = y ? __uint_as_float(p2 & 0xffff0000u) + __uint_as_float(l2 & 0xffff0000u) : __uint_as_float(p2 << 16) + __uint_as_float(l2 << 16);
+            const float kk = y ? __uint_as_float(k2 & 0xffff0000u) : __uint_as_float(k2 << 16);
             const bool below = j + y < i;
             F[y] = j + y <= i ? p.scale * d * dP[x][e + y] : 0.0f;
             E[y] = below ? -d * dA[x][e + y] : 0.0f;
