@@ -437,16 +437,16 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
 }
 
 // ---- the walk over a chain's chunks ---------------------------------------------------------------------------------------------------------------
-// A block has a chain, a head and 16 NW labels of it: NW warps as described above. Each brings its share of the next chunk while it works on this one, so that a
-// scheduler's registers go to the two warps that multiply (a ninth warp that only copies would leave them 168 each). Three stages where they fit: a warp may be a
-// chunk ahead of the slowest.
+// A block has a chain, a head and 16 NW labels of it: NW warps as described above. Of eight each brings its share of the next chunk while it works on this one, so that a
+// scheduler's registers go to the two warps that multiply (a ninth warp that only copies would leave them 168 each); beside fewer there are four warps that
+// only copy. Three stages where they fit: a warp may be a chunk ahead of the slowest.
 template <int DK, int NW>
 struct ChainShape {
   static constexpr int row = DK + 8, vrow = 16 * NW + 8;
   static constexpr int q_at = DC * row * 2, v_at = 2 * q_at, block_at = v_at + DC * vrow * 2, stage = block_at + DC_BLOCK;
   static constexpr int stages = 3 * stage <= 226 * 1024 ? 3 : 2;
   static constexpr int smem = stages * stage;
-  static constexpr int threads = 32 * NW;
+  static constexpr int copiers = NW < 8 ? 4 : 0, threads = 32 * (NW + copiers);
 };
 
 // A warp's share of 64 rows of a tile, `UNITS` units of 16 bytes a row; zeros behind the chunk's end and from column `width` on. (A bulk copy for each row takes 64
@@ -474,6 +474,22 @@ __device__ __forceinline__ void bring_chunk(const DeltaChunkParams& p, const Del
 #pragma unroll 4
   for (int i = (warp * 32 + lane) * 16; i < DC_BLOCK; i += warps * 512) copy16(st + Shape::block_at + i, block + i, true);
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem32(full)) : "memory");
+}
+// A copying warp's work: its share of all n chunks, from `first` on in steps of 1 or -1
+template <int DK, int NW>
+__device__ __forceinline__ void bring_chunks(const DeltaChunkParams& p, const DeltaHeads& labels, uint32_t smem, int first, int step, int n, int h, int kh, int col0, int warp, int lane,
+                                             unsigned long long* full, unsigned long long* empty) {
+  using Shape = ChainShape<DK, NW>;
+  for (int i = 0; i < n; ++i) {
+    const int s = i % Shape::stages;
+    if (i >= Shape::stages && !__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], (i / Shape::stages - 1) & 1, p.spin_limit))) {
+      if (lane == 0) set_status(p.status, DEV_TIMEOUT, 27, i);
+      break;
+    }
+    if (i == p.drop) break;  // a test hook: this chunk and those behind it are never brought
+    bring_chunk<DK, NW>(p, labels, smem + s * Shape::stage, first + step * i, h, kh, col0, warp, Shape::copiers, lane, &full[s]);
+  }
+  copies_done();
 }
 __device__ __forceinline__ void arrive(unsigned long long* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem32(bar)) : "memory"); }
 
@@ -503,7 +519,7 @@ __device__ __forceinline__ void put_labels(const float (&x)[8][4], unsigned char
 }
 
 template <int DK, int NW, bool SAVE>
-__global__ void __launch_bounds__(32 * NW) delta_chain_kernel(const __grid_constant__ DeltaChunkParams p) {
+__global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kernel(const __grid_constant__ DeltaChunkParams p) {
   using Shape = ChainShape<DK, NW>;
   constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages, Q_AT = Shape::q_at, V_AT = Shape::v_at;  // bytes
   extern __shared__ __align__(16) unsigned char chain_smem[];
@@ -514,16 +530,22 @@ __global__ void __launch_bounds__(32 * NW) delta_chain_kernel(const __grid_const
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
+  constexpr bool COPIERS = Shape::copiers > 0;
+  const int bringers = COPIERS ? Shape::copiers : warps;
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full[s], 32 * warps);
+      mbar_init(&full[s], 32 * bringers);
       mbar_init(&empty[s], warps);
     }
     mbar_fence_init();
   }
   __syncthreads();
+  if (COPIERS && warp >= NW) {
+    bring_chunks<DK, NW>(p, p.v, smem32(chain_smem), first, 1, n, h, kh, col0, warp - NW, lane, full, empty);
+    return;
+  }
   if (warp >= warps) return;
-  if (n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem), first, h, kh, col0, warp, warps, lane, &full[0]);
+  if (!COPIERS && n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem), first, h, kh, col0, warp, warps, lane, &full[0]);
 
   // S^T: labels g and g + 8 of the warp's 16, features 8 n + 2 t and the next
   float S[DK / 8][4];
@@ -540,7 +562,7 @@ __global__ void __launch_bounds__(32 * NW) delta_chain_kernel(const __grid_const
   for (int i = 0; i < n; ++i) {
     const int s = i % STAGES, s1 = (i + 1) % STAGES;
     bool ok = true;
-    if (i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
+    if (!COPIERS && i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
       if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s1], ((i + 1) / STAGES - 1) & 1, p.spin_limit));
       if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem) + s1 * Shape::stage, first + i + 1, h, kh, col0, warp, warps, lane, &full[s1]);
     }

@@ -31,7 +31,7 @@ struct DeltaGradParams {
 };
 
 template <int DK, int NW>
-__global__ void __launch_bounds__(32 * NW) delta_back_kernel(const __grid_constant__ DeltaGradParams gp) {
+__global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel(const __grid_constant__ DeltaGradParams gp) {
   const DeltaChunkParams& p = gp.f;
   using Shape = ChainShape<DK, NW>;
   constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages, Q_AT = Shape::q_at, V_AT = Shape::v_at;  // bytes
@@ -43,16 +43,22 @@ __global__ void __launch_bounds__(32 * NW) delta_back_kernel(const __grid_consta
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
+  constexpr bool COPIERS = Shape::copiers > 0;
+  const int bringers = COPIERS ? Shape::copiers : warps;
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full[s], 32 * warps);
+      mbar_init(&full[s], 32 * bringers);
       mbar_init(&empty[s], warps);
     }
     mbar_fence_init();
   }
   __syncthreads();
+  if (COPIERS && warp >= NW) {
+    bring_chunks<DK, NW>(p, p.dout, smem32(chain_smem), first + n - 1, -1, n, h, kh, col0, warp - NW, lane, full, empty);
+    return;
+  }
   if (warp >= warps) return;
-  if (n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem), first + n - 1, h, kh, col0, warp, warps, lane, &full[0]);
+  if (!COPIERS && n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem), first + n - 1, h, kh, col0, warp, warps, lane, &full[0]);
 
   float G[DK / 8][4];  // G^T, as S^T in the forward walk
   const int label = col0 + warp * 16 + g;
@@ -68,7 +74,7 @@ __global__ void __launch_bounds__(32 * NW) delta_back_kernel(const __grid_consta
   for (int i = 0; i < n; ++i) {
     const int s = i % STAGES, s1 = (i + 1) % STAGES;
     bool ok = true;
-    if (i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
+    if (!COPIERS && i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
       if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s1], ((i + 1) / STAGES - 1) & 1, p.spin_limit));
       if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem) + s1 * Shape::stage, first + n - 2 - i, h, kh, col0, warp, warps, lane, &full[s1]);
     }

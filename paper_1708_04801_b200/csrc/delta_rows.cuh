@@ -30,26 +30,61 @@ struct DeltaRowsParams {
   DevStatus* status;
 };
 
-// four features from column c on, zeros behind dk
+// Four features from column c on, zeros behind dk, as loaded: what is converted on arrival is waited for on arrival
 template <typename XT>
-__device__ __forceinline__ void features4(const XT* row, int c, int dk, int vec, float (&f)[4]) {
-  if (vec) {
-    if (c < dk) {
-      if constexpr (sizeof(XT) == 4) {
-        const float4 r = __ldg((const float4*)(row + c));
-        f[0] = r.x, f[1] = r.y, f[2] = r.z, f[3] = r.w;
-      } else {
-        const uint2 r = __ldg((const uint2*)(row + c));
-        f[0] = __uint_as_float(r.x << 16), f[1] = __uint_as_float(r.x & 0xffff0000u), f[2] = __uint_as_float(r.y << 16), f[3] = __uint_as_float(r.y & 0xffff0000u);
-      }
+struct Features4;
+template <>
+struct Features4<float> {
+  float4 r;
+  __device__ __forceinline__ void load(const float* row, int c, int dk, int vec) {
+    r = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (vec) {
+      if (c < dk) r = __ldg((const float4*)(row + c));
     } else {
-      f[0] = f[1] = f[2] = f[3] = 0.0f;
+      if (c < dk) r.x = row[c];
+      if (c + 1 < dk) r.y = row[c + 1];
+      if (c + 2 < dk) r.z = row[c + 2];
+      if (c + 3 < dk) r.w = row[c + 3];
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = c + e < dk ? widen_scalar<XT>(row[c + e]) : 0.0f;
   }
-}
+  __device__ __forceinline__ void widen(float* f) const { f[0] = r.x, f[1] = r.y, f[2] = r.z, f[3] = r.w; }
+};
+template <>
+struct Features4<__nv_bfloat16> {
+  uint2 r;
+  __device__ __forceinline__ void load(const __nv_bfloat16* row, int c, int dk, int vec) {
+    r = make_uint2(0u, 0u);
+    if (vec) {
+      if (c < dk) r = __ldg((const uint2*)(row + c));
+    } else {
+      const unsigned short* at = (const unsigned short*)row;
+      unsigned short e[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i < dk) e[i] = at[c + i];
+      r = make_uint2(e[0] | (unsigned)e[1] << 16, e[2] | (unsigned)e[3] << 16);
+    }
+  }
+  __device__ __forceinline__ void widen(float* f) const {
+    f[0] = __uint_as_float(r.x << 16), f[1] = __uint_as_float(r.x & 0xffff0000u), f[2] = __uint_as_float(r.y << 16), f[3] = __uint_as_float(r.y & 0xffff0000u);
+  }
+};
+// What a row brings for one model, as loaded
+template <typename XT, int NJ>
+struct DeltaRow {
+  Features4<XT> k[NJ], q[NJ];
+  XT v, g, beta;
+  __device__ __forceinline__ void load(const XT* pk, const XT* pq, const XT* pv, const XT* pg, const XT* pb, int s, int dk, int vec) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      k[j].load(pk, 4 * (s + 8 * j), dk, vec);
+      q[j].load(pq, 4 * (s + 8 * j), dk, vec);
+    }
+    v = *pv;
+    g = *pg;
+    beta = *pb;
+  }
+};
 template <typename XT>
 __device__ __forceinline__ XT narrow_scalar(float v) {
   if constexpr (sizeof(XT) == 4) return v;
@@ -83,45 +118,93 @@ __device__ __forceinline__ float sum8(float v) {
 }
 
 // One row of one model: updates w (4 NJ features of this lane) and returns the answer (in all eight lanes).
-template <int NJ>
-__device__ __forceinline__ float delta_one_row(float (&w)[4 * NJ], const float (&k)[4 * NJ], const float (&q)[4 * NJ], float v, float g, float beta) {
-  const float a = expf(g < DELTA_MIN_G ? DELTA_MIN_G : g);
-  float wk = 0.0f, wq = 0.0f, kq = 0.0f;
+template <typename XT, int NJ>
+__device__ __forceinline__ float delta_one_row(float (&w)[4 * NJ], const DeltaRow<XT, NJ>& row) {
+  const float g = widen_scalar<XT>(row.g), a = expf(g < DELTA_MIN_G ? DELTA_MIN_G : g);
+  float wk[2] = {}, wq[2] = {}, kq[2] = {}, k[4 * NJ];
 #pragma unroll
-  for (int e = 0; e < 4 * NJ; ++e) {
-    w[e] *= a;
-    wk = fmaf(w[e], k[e], wk);
-    wq = fmaf(w[e], q[e], wq);
-    kq = fmaf(k[e], q[e], kq);
+  for (int j = 0; j < NJ; ++j) {
+    float q[4];
+    row.k[j].widen(k + 4 * j);
+    row.q[j].widen(q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * j + e;
+      wk[e & 1] = fmaf(w[i], k[i], wk[e & 1]);
+      wq[e & 1] = fmaf(w[i], q[e], wq[e & 1]);
+      kq[e & 1] = fmaf(k[i], q[e], kq[e & 1]);
+    }
   }
-  wk = sum8(wk), wq = sum8(wq), kq = sum8(kq);
-  const float delta = beta * (v - wk);
+  const float sk = sum8(wk[0] + wk[1]), sq = sum8(wq[0] + wq[1]), skq = sum8(kq[0] + kq[1]);
+  const float delta = widen_scalar<XT>(row.beta) * fmaf(-a, sk, widen_scalar<XT>(row.v));
 #pragma unroll
-  for (int e = 0; e < 4 * NJ; ++e) w[e] = fmaf(delta, k[e], w[e]);
-  return fmaf(delta, kq, wq);
+  for (int e = 0; e < 4 * NJ; ++e) w[e] = fmaf(a, w[e], delta * k[e]);
+  return fmaf(a, sq, delta * skq);
 }
 
 // ---- chains, row by row ---------------------------------------------------------------------------------------------------------
-// A warp has four models of a chain in registers and goes over the chain's rows. Bounds: the latency of a row (sums over eight lanes, about
-// 150 cycles); the loads of the next rows are under way meanwhile.
-constexpr int DELTA_WARPS = 4;
+// A block has 16 models of a chain, four to a warp, in registers and goes over the chain's rows, fp32. Features, queries, labels and gates of the next `batch` rows come to
+// shared memory by asynchronous copies of all threads while it works on this batch; a row's are read a row ahead. Bounds: issue of one warp per scheduler and
+// the latency of a row (sums over eight lanes and the step that depends on them). (Each lane bringing what it needs itself: 200 instructions a row and 820 cycles.)
+constexpr int DELTA_WARPS = 4, ROWS_MODELS = 4 * DELTA_WARPS, ROWS_BATCH = 16;
 
-template <typename XT, int NJ>
-__global__ void __launch_bounds__(32 * DELTA_WARPS) delta_rows_kernel(const __grid_constant__ DeltaRowsParams p) {
-  constexpr int AHEAD = 4;  // rows whose loads are under way
+// Heads of features that 16 neighbouring models can have, and floats of a row in shared memory: features and queries of those heads, a label, decay and step of each model
+__host__ __device__ constexpr int rows_heads(int hk, int hv, int dv) {
+  const int shared = hv / hk * dv, most = (ROWS_MODELS - 1 + shared - 1) / shared + 1;
+  return most < hk ? most : hk;
+}
+template <int NJ>
+__host__ __device__ constexpr int rows_floats(int heads) { return 2 * heads * 32 * NJ + 3 * ROWS_MODELS; }
+
+__device__ __forceinline__ void copy4(const void* to, const void* from, bool yes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(yes ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_features(const float* to, const float* row, int c, int dk, int vec) {
+  if (vec) {
+    const bool yes = c < dk;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(yes ? row + c : row), "r"(yes ? 16 : 0) : "memory");
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) copy4(to + e, c + e < dk ? row + c + e : row, c + e < dk);
+  }
+}
+
+template <int NJ>
+__global__ void __launch_bounds__(32 * DELTA_WARPS) delta_rows_kernel(const __grid_constant__ DeltaRowsParams p, int batch) {
+  constexpr int UNITS = 8 * NJ;  // of four features
+  extern __shared__ __align__(16) float batch_smem[];
   kernel_started();
   kernel_inputs_ready();
-  const int lane = threadIdx.x & 31, s = lane & 7, models = p.hv * p.dv;
-  const int groups = (models + 4 * DELTA_WARPS - 1) / (4 * DELTA_WARPS);
+  const int tid = threadIdx.x, lane = tid & 31, s = lane & 7, models = p.hv * p.dv, more = p.hv / p.hk;
+  const int groups = (models + ROWS_MODELS - 1) / ROWS_MODELS;
   const long long chain = blockIdx.x / groups;
-  const int R = ((int)(blockIdx.x % groups) * DELTA_WARPS + (threadIdx.x >> 5)) * 4 + (lane >> 3);
+  const int R0 = (int)(blockIdx.x % groups) * ROWS_MODELS, mine = tid >> 3, R = R0 + mine;  // a model has eight threads
   const bool there = R < models;
-  const int h = there ? R / p.dv : 0, hk = h / (p.hv / p.hk);
+  const int hk0 = R0 / p.dv / more, hk = there ? R / p.dv / more : hk0, heads = (min(R0 + ROWS_MODELS, models) - 1) / p.dv / more - hk0 + 1;
   const long long first = p.shard_off[chain], end = p.shard_off[chain + 1];
   if (first < 0 || end < first || end > p.n_rows) {  // the same for the whole block; other chains may be in order, and run
-    if (threadIdx.x == 0) set_status(p.status, DEV_BOUNDS, 22, chain);
+    if (tid == 0) set_status(p.status, DEV_BOUNDS, 22, chain);
     return;
   }
+  const int floats = rows_floats<NJ>(rows_heads(p.hk, p.hv, p.dv)), labels_at = 2 * heads * 32 * NJ;
+  auto bring = [&](long long t0, float* to) {  // rows t0 to t0 + batch - 1, as far as there are
+    const int n = (int)min((long long)batch, end - t0);
+    for (int u = tid; u < n * heads * 2 * UNITS; u += 32 * DELTA_WARPS) {
+      const int c = u % UNITS * 4, which = u / UNITS % 2, rest = u / (2 * UNITS), row = rest / heads, head = rest - row * heads;
+      const float* from = which ? (const float*)p.q + (t0 + row) * p.ld_q : (const float*)p.k + (t0 + row) * p.ld_k;
+      copy_features(to + row * floats + (2 * head + which) * 32 * NJ + c, from + (hk0 + head) * p.dk, c, p.dk, p.vec);
+    }
+    for (int u = tid; u < n * ROWS_MODELS; u += 32 * DELTA_WARPS) {
+      const int m = u % ROWS_MODELS, row = u / ROWS_MODELS, r = min(R0 + m, models - 1), h = r / p.dv;
+      float* at = to + row * floats + labels_at + m;
+      copy4(at, (const float*)p.v + (t0 + row) * p.ld_v + r, true);
+      copy4(at + ROWS_MODELS, (const float*)p.g + (t0 + row) * p.ld_g + h, true);
+      copy4(at + 2 * ROWS_MODELS, (const float*)p.beta + (t0 + row) * p.ld_beta + h, true);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  float* buffers[2] = {batch_smem, batch_smem + batch * floats};
+  if (first < end) bring(first, buffers[0]);
   float w[4 * NJ];
   const long long at = (chain * models + (there ? R : 0)) * p.dk;
 #pragma unroll
@@ -129,33 +212,39 @@ __global__ void __launch_bounds__(32 * DELTA_WARPS) delta_rows_kernel(const __gr
     if (p.W0 && there) model4(p.W0 + at, 4 * (s + 8 * j), p.dk, p.vec, w + 4 * j);
     else w[4 * j] = w[4 * j + 1] = w[4 * j + 2] = w[4 * j + 3] = 0.0f;
   }
-  struct Row {
-    float k[4 * NJ], q[4 * NJ], v, g, beta;
-  } rows[AHEAD];
-  auto load = [&](Row& r, long long t) {
-    if (t >= end) return;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      float f[4];
-      features4((const XT*)p.k + t * p.ld_k + hk * p.dk, 4 * (s + 8 * j), p.dk, p.vec, f);
-      r.k[4 * j] = f[0], r.k[4 * j + 1] = f[1], r.k[4 * j + 2] = f[2], r.k[4 * j + 3] = f[3];
-      features4((const XT*)p.q + t * p.ld_q + hk * p.dk, 4 * (s + 8 * j), p.dk, p.vec, f);
-      r.q[4 * j] = f[0], r.q[4 * j + 1] = f[1], r.q[4 * j + 2] = f[2], r.q[4 * j + 3] = f[3];
+  float* out = (float*)p.out + first * p.ld_out + R;
+  const int own = 2 * (hk - hk0) * 32 * NJ + 4 * s;
+  int which = 0;
+  for (long long t0 = first; t0 < end; t0 += batch, which ^= 1) {
+    if (t0 + batch < end) {
+      bring(t0 + batch, buffers[which ^ 1]);
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+    } else {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
-    r.v = widen_scalar<XT>(((const XT*)p.v)[t * p.ld_v + (there ? R : 0)]);
-    r.g = widen_scalar<XT>(((const XT*)p.g)[t * p.ld_g + h]);
-    r.beta = widen_scalar<XT>(((const XT*)p.beta)[t * p.ld_beta + h]);
-  };
+    __syncthreads();
+    const int n = (int)min((long long)batch, end - t0);
+    const float* from = which ? buffers[1] : buffers[0];
+    auto read = [&](DeltaRow<float, NJ>& row) {
 #pragma unroll
-  for (int a = 0; a < AHEAD; ++a) load(rows[a], first + a);
-  for (long long t = first; t < end; t += AHEAD) {
-#pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
-      if (t + a >= end) break;
-      const float o = delta_one_row<NJ>(w, rows[a].k, rows[a].q, rows[a].v, rows[a].g, rows[a].beta);
-      if (s == 0 && there) ((XT*)p.out)[(t + a) * p.ld_out + R] = narrow_scalar<XT>(p.scale * o);
-      load(rows[a], t + a + AHEAD);
+      for (int j = 0; j < NJ; ++j) {
+        row.k[j].r = *(const float4*)(from + own + 32 * j);
+        row.q[j].r = *(const float4*)(from + own + 32 * NJ + 32 * j);
+      }
+      row.v = from[labels_at + mine], row.g = from[labels_at + ROWS_MODELS + mine], row.beta = from[labels_at + 2 * ROWS_MODELS + mine];
+      from += floats;
+    };
+    DeltaRow<float, NJ> now, next;
+    read(now);
+#pragma unroll 2
+    for (int i = 0; i < n; ++i) {
+      if (i + 1 < n) read(next);
+      const float o = delta_one_row<float, NJ>(w, now);
+      if (s == 0 && there) *out = p.scale * o;
+      out += p.ld_out;
+      now = next;
     }
+    __syncthreads();
   }
   if (p.W && there)
 #pragma unroll
@@ -163,28 +252,31 @@ __global__ void __launch_bounds__(32 * DELTA_WARPS) delta_rows_kernel(const __gr
 }
 
 // ---- one row for each of many chains ------------------------------------------------------------------------------------------------
-// A block has 32 RI models of a chain, all on their way from memory before the first is used. Bounds: bytes, the models once in and once out.
+// A block has 32 models of a chain; they and what the row brings are on their way from memory together. Bounds: bytes, the models once in and once out. (Four models for each
+// group of eight lanes, 128 a block: 266 us instead of 178 for 256 rows of 32 heads of 128 x 128; two: 191.)
 // A slot that an earlier row has is left to that row: every block looks through the slots before its own, which come from L2 while its models come from memory.
 constexpr int STEP_THREADS = 256;
 
-template <typename XT, int NJ, int RI>
+template <typename XT, int NJ>
 __global__ void __launch_bounds__(STEP_THREADS) delta_step_kernel(const __grid_constant__ DeltaRowsParams p) {
   kernel_started();
   kernel_inputs_ready();
   const int lane = threadIdx.x & 31, s = lane & 7, models = p.hv * p.dv;
-  const int groups = (models + 32 * RI - 1) / (32 * RI);
+  const int groups = (models + 31) / 32;
   const long long row = blockIdx.x / groups;
-  const int R0 = (int)(blockIdx.x % groups) * 32 * RI + (threadIdx.x >> 5) * 4 + (lane >> 3);
+  const int R = (int)(blockIdx.x % groups) * 32 + (threadIdx.x >> 5) * 4 + (lane >> 3);
+  const bool there = R < models;
   const long long slot = p.slots ? p.slots[row] : row;
   const bool valid = slot >= 0 && slot < p.n_slots;
-  float w[RI][4 * NJ];
+  float w[4 * NJ] = {};
+  float* model = p.W + (valid && there ? (slot * models + R) * p.dk : 0);
+  if (valid && there)
 #pragma unroll
-  for (int i = 0; i < RI; ++i)
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      w[i][4 * j] = w[i][4 * j + 1] = w[i][4 * j + 2] = w[i][4 * j + 3] = 0.0f;
-      if (valid && R0 + 32 * i < models) model4(p.W + (slot * models + R0 + 32 * i) * p.dk, 4 * (s + 8 * j), p.dk, p.vec, w[i] + 4 * j);
-    }
+    for (int j = 0; j < NJ; ++j) model4(model, 4 * (s + 8 * j), p.dk, p.vec, w + 4 * j);
+  const int h = there ? R / p.dv : 0, hk = h / (p.hv / p.hk);
+  DeltaRow<XT, NJ> brought;
+  brought.load((const XT*)p.k + row * p.ld_k + hk * p.dk, (const XT*)p.q + row * p.ld_q + hk * p.dk, (const XT*)p.v + row * p.ld_v + (there ? R : 0), (const XT*)p.g + row * p.ld_g + h,
+               (const XT*)p.beta + row * p.ld_beta + h, s, p.dk, p.vec);
   int twice = 0;
   if (p.slots) {
     if (valid)
@@ -195,28 +287,11 @@ __global__ void __launch_bounds__(STEP_THREADS) delta_step_kernel(const __grid_c
     if (threadIdx.x == 0 && (twice || slot >= p.n_slots)) set_status(p.status, DEV_BOUNDS, 23, row);
     return;
   }
+  const float o = delta_one_row<XT, NJ>(w, brought);
+  if (there) {
+    if (s == 0) ((XT*)p.out)[row * p.ld_out + R] = narrow_scalar<XT>(p.scale * o);
 #pragma unroll
-  for (int i = 0; i < RI; ++i) {
-    const int R = R0 + 32 * i;
-    const bool there = R < models;
-    const int h = there ? R / p.dv : 0, hk = h / (p.hv / p.hk);
-    float k[4 * NJ], q[4 * NJ];
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      float f[4];
-      features4((const XT*)p.k + row * p.ld_k + hk * p.dk, 4 * (s + 8 * j), p.dk, p.vec, f);
-      k[4 * j] = f[0], k[4 * j + 1] = f[1], k[4 * j + 2] = f[2], k[4 * j + 3] = f[3];
-      features4((const XT*)p.q + row * p.ld_q + hk * p.dk, 4 * (s + 8 * j), p.dk, p.vec, f);
-      q[4 * j] = f[0], q[4 * j + 1] = f[1], q[4 * j + 2] = f[2], q[4 * j + 3] = f[3];
-    }
-    const float v = widen_scalar<XT>(((const XT*)p.v)[row * p.ld_v + (there ? R : 0)]);
-    const float g = widen_scalar<XT>(((const XT*)p.g)[row * p.ld_g + h]), beta = widen_scalar<XT>(((const XT*)p.beta)[row * p.ld_beta + h]);
-    const float o = delta_one_row<NJ>(w[i], k, q, v, g, beta);
-    if (there) {
-      if (s == 0) ((XT*)p.out)[row * p.ld_out + R] = narrow_scalar<XT>(p.scale * o);
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) put_model4(p.W + (slot * models + R) * p.dk, 4 * (s + 8 * j), p.dk, p.vec, w[i] + 4 * j);
-    }
+    for (int j = 0; j < NJ; ++j) put_model4(model, 4 * (s + 8 * j), p.dk, p.vec, w + 4 * j);
   }
 }
 

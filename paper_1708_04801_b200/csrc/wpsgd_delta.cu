@@ -55,27 +55,26 @@ DeltaRowsParams rows_params(const wpsgd_ctx* c, const wpsgd_delta_rows* r, void*
           r->heads_k, r->heads_v, r->dk, r->dv, r->scale, vec, c->status};
 }
 
-template <typename XT>
 wpsgd_status run_rows(wpsgd_ctx* c, const DeltaRowsParams& p) {
-  const unsigned grid = (unsigned)(p.n_chains * ((p.hv * p.dv + 4 * DELTA_WARPS - 1) / (4 * DELTA_WARPS)));
-  const cudaError_t e = p.dk <= 32   ? launch(delta_rows_kernel<XT, 1>, grid, 32 * DELTA_WARPS, 0, c->stream, p)
-                        : p.dk <= 64 ? launch(delta_rows_kernel<XT, 2>, grid, 32 * DELTA_WARPS, 0, c->stream, p)
-                                     : launch(delta_rows_kernel<XT, 4>, grid, 32 * DELTA_WARPS, 0, c->stream, p);
-  CU_TRY(c, e);
-  c->launches++;
-  return WPSGD_OK;
+  const unsigned grid = (unsigned)(p.n_chains * ((p.hv * p.dv + ROWS_MODELS - 1) / ROWS_MODELS));
+  auto go = [&](auto nj) {
+    constexpr int NJ = decltype(nj)::value;
+    const int row_bytes = rows_floats<NJ>(rows_heads(p.hk, p.hv, p.dv)) * 4, batch = std::max(1, std::min(ROWS_BATCH, 48 * 1024 / row_bytes));
+    CU_TRY(c, (allow_smem<delta_rows_kernel<NJ>>(c)));
+    CU_TRY(c, launch(delta_rows_kernel<NJ>, grid, 32 * DELTA_WARPS, (size_t)2 * batch * row_bytes, c->stream, p, batch));
+    c->launches++;
+    return WPSGD_OK;
+  };
+  return p.dk <= 32 ? go(std::integral_constant<int, 1>()) : p.dk <= 64 ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 4>());
 }
 
 template <typename XT>
 wpsgd_status run_step(wpsgd_ctx* c, const DeltaRowsParams& p) {
-  // 128 models a block where that leaves every SM four blocks: fewer blocks read features and look through the slots
-  const long long models = (long long)p.hv * p.dv;
-  const bool many = p.n_rows * ((models + 127) / 128) >= 148 * 4;
-  const long long grid = p.n_rows * ((models + (many ? 127 : 31)) / (many ? 128 : 32));
+  const long long models = (long long)p.hv * p.dv, grid = p.n_rows * ((models + 31) / 32);
   if (grid > INT32_MAX) return fail(c, WPSGD_ERR_UNSUPPORTED, "delta_step: too many models");
   auto go = [&](auto nj) {
     constexpr int NJ = decltype(nj)::value;
-    return many ? launch(delta_step_kernel<XT, NJ, 4>, (unsigned)grid, STEP_THREADS, 0, c->stream, p) : launch(delta_step_kernel<XT, NJ, 1>, (unsigned)grid, STEP_THREADS, 0, c->stream, p);
+return launch(delta_step_kernel<XT, NJ>, (unsigned)grid, STEP_THREADS, 0, c->stream, p);
   };
   CU_TRY(c, p.dk <= 32 ? go(std::integral_constant<int, 1>()) : p.dk <= 64 ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 4>()));
   c->launches++;
@@ -253,7 +252,7 @@ wpsgd_status wpsgd_delta_run(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const f
   if (use == WPSGD_DELTA_RUN_SAVE && rows->type != WPSGD_X_BF16) return refuse(c, "delta_run", "gradients are of bf16 rows", WPSGD_ERR_UNSUPPORTED);
   if (rows->n_chains == 0) return WPSGD_OK;
   DeviceGuard guard(c->device);
-  if (rows->type == WPSGD_X_F32) return run_rows<float>(c, rows_params(c, rows, out, ld_out, W0, W_out));
+  if (rows->type == WPSGD_X_F32) return run_rows(c, rows_params(c, rows, out, ld_out, W0, W_out));
   const bool save = use == WPSGD_DELTA_RUN_SAVE;
   const DeltaLayout lay(rows, save);
   if (!workspace || !aligned16(workspace) || workspace_bytes < (long long)lay.total) return refuse(c, "delta_run", "the workspace is NULL, not aligned to 16 bytes or too small");
