@@ -117,28 +117,40 @@ __device__ __forceinline__ float sum8(float v) {
   return v + __shfl_xor_sync(0xffffffffu, v, 4);
 }
 
-// One row of one model: updates w (4 NJ features of this lane) and returns the answer (in all eight lanes).
+// One row of one model: updates w (4 NJ features of this lane) and returns the answer (in all eight lanes). Operations on pairs of fp32: half the instructions.
 template <typename XT, int NJ>
 __device__ __forceinline__ float delta_one_row(float (&w)[4 * NJ], const DeltaRow<XT, NJ>& row) {
   const float g = widen_scalar<XT>(row.g), a = expf(g < DELTA_MIN_G ? DELTA_MIN_G : g);
-  float wk[2] = {}, wq[2] = {}, kq[2] = {}, k[4 * NJ];
+  uint64_t wk = 0, wq = 0, kq = 0, w2[2 * NJ], k2[2 * NJ];
+  auto pair = [](float x, float y) { return pair_of(__float_as_uint(x), __float_as_uint(y)); };
+  auto both = [](uint64_t v) {
+    const float2 h = halves(v);
+    return h.x + h.y;
+  };
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    float q[4];
-    row.k[j].widen(k + 4 * j);
+    float k[4], q[4];
+    row.k[j].widen(k);
     row.q[j].widen(q);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = 4 * j + e;
-      wk[e & 1] = fmaf(w[i], k[i], wk[e & 1]);
-      wq[e & 1] = fmaf(w[i], q[e], wq[e & 1]);
-      kq[e & 1] = fmaf(k[i], q[e], kq[e & 1]);
+    for (int e = 0; e < 2; ++e) {
+      const int i = 2 * j + e;
+      const uint64_t q2 = pair(q[2 * e], q[2 * e + 1]);
+      k2[i] = pair(k[2 * e], k[2 * e + 1]);
+      w2[i] = pair(w[2 * i], w[2 * i + 1]);
+      wk = fma2(w2[i], k2[i], wk);
+      wq = fma2(w2[i], q2, wq);
+      kq = fma2(k2[i], q2, kq);
     }
   }
-  const float sk = sum8(wk[0] + wk[1]), sq = sum8(wq[0] + wq[1]), skq = sum8(kq[0] + kq[1]);
+  const float sk = sum8(both(wk)), sq = sum8(both(wq)), skq = sum8(both(kq));
   const float delta = widen_scalar<XT>(row.beta) * fmaf(-a, sk, widen_scalar<XT>(row.v));
+  const uint64_t a2 = pair(a, a), d2 = pair(delta, delta);
 #pragma unroll
-  for (int e = 0; e < 4 * NJ; ++e) w[e] = fmaf(a, w[e], delta * k[e]);
+  for (int i = 0; i < 2 * NJ; ++i) {
+    const float2 h = halves(fma2(d2, k2[i], mul2(a2, w2[i])));
+    w[2 * i] = h.x, w[2 * i + 1] = h.y;
+  }
   return fmaf(a, sq, delta * skq);
 }
 
