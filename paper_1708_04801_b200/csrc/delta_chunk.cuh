@@ -92,6 +92,8 @@ __device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t at) {
 __device__ __forceinline__ void stsm_t(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+// The warp's number as the compiler knows it to be one for all lanes: branches on it need no way back to convergence
+__device__ __forceinline__ int warp_index() { return __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0); }
 __device__ __forceinline__ uint32_t smem32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t pack2(float x, float y) {  // x in the low half
   uint32_t r;
@@ -254,7 +256,7 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
   unsigned char* tris = prep_smem;  // over K and Q, once their products are done
   float* diag = (float*)(prep_smem + PrepShape<DK>::smem - PrepShape<DK>::diag);
   __shared__ float bhi[DC], blo[DC], betas[DC];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
   kernel_started();
   kernel_inputs_ready();
   const int chunk = blockIdx.x / p.hv, h = blockIdx.x % p.hv, kh = h / (p.hv / p.hk);
@@ -524,7 +526,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
   constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages, Q_AT = Shape::q_at, V_AT = Shape::v_at;  // bytes
   extern __shared__ __align__(16) unsigned char chain_smem[];
   __shared__ unsigned long long full[STAGES], empty[STAGES];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
   kernel_started();
   kernel_inputs_ready();
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);

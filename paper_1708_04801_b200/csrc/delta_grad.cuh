@@ -24,6 +24,7 @@ struct DeltaGradParams {
   DeltaChunkParams f;
   __nv_bfloat16* ends;   // [chunks][hv][dvp][DK]: G behind the chunk
   __nv_bfloat16* drs;    // [chunks][hv][DC][dvp]: dR
+  float* totals;         // [blocks][2][DC][DK]: sums over the heads of labels that share features
   const float* dW;
   float* dW0;
   __nv_bfloat16 *dq, *dk, *dv, *dg, *dbeta;
@@ -37,7 +38,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
   constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages, Q_AT = Shape::q_at, V_AT = Shape::v_at;  // bytes
   extern __shared__ __align__(16) unsigned char chain_smem[];
   __shared__ unsigned long long full[STAGES], empty[STAGES];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
   kernel_started();
   kernel_inputs_ready();
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
@@ -217,211 +218,260 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
 }
 
 // ---- gradients of the rows ---------------------------------------------------------------------------------------------------------------
-// One block of 16 warps for each chunk and head of features, which goes through the heads of labels that share them. A warp has 16 rows
-// and a quarter of the columns. Labels come in slices of 32 by cp.async, two slices under way; the sums over labels (O' S^T, dR S^T, U G^T, O' U^T, dR U^T) stay
-// in registers, and F and E go through shared memory to the products with K and Q.
-constexpr int ROWS_THREADS = 512, ROWS_SLICE = 32;
+// One block of 16 warps per SM goes through pieces of work, each a chunk and a head of labels; the heads that share features follow each other. A warp has 16
+// rows and a quarter of the columns. Labels come in slices of 64 by cp.async through a ring that runs on from one piece into the next; the sums over labels (O' S^T,
+// dR S^T, U G^T, O' U^T, dR U^T) stay in registers, and F and E go through shared memory to the products with K and Q. Sums over the diagonal of a product (dR.v of a
+// row, S.G) are taken from fragments that are there for others. One block's sums fill half of
+// an SM's registers.
+constexpr int ROWS_PARTS = 4, ROWS_THREADS = 128 * ROWS_PARTS, ROWS_SLICE = 64;  // parts of the columns, four warps each
 
 template <int DK>
 struct RowsShape {
   static constexpr int row = DK + 8, vrow = ROWS_SLICE + 8;
   static constexpr int models = ROWS_SLICE * row * 2, labels = DC * vrow * 2, stage = 2 * models + 4 * labels;
-  static constexpr int qk = 2 * DC * row * 2, tiles = 3 * DC_TILE_BYTES, sums = 4 * DC * 5 * 4, totals = 2 * DC * DK * 4;
-  static constexpr int smem(bool grouped) { return qk + 2 * stage + tiles + (int)sizeof(DeltaFactors) + sums + (grouped ? totals : 0); }
+  static constexpr int qk = 2 * DC * row * 2, tiles = 3 * DC_TRI, kept = DC_BLOCK - DC_P + DC_TRI, sums = (ROWS_PARTS * 3 + 4) * DC * 4;
+  static constexpr int stages = 2, smem = qk + tiles + kept + sums + stages * stage, totals = 2 * DC * DK;
 };
+static_assert(RowsShape<128>::smem <= 226 * 1024, "must fit an SM");
 
 template <int DK>
 __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __grid_constant__ DeltaGradParams gp) {
   using Shape = RowsShape<DK>;
-  constexpr int ROW = Shape::row, VROW = Shape::vrow, NT = DK / 32;  // tiles of 8 columns of a warp
+  constexpr int ROW = Shape::row, VROW = Shape::vrow, NT = DK / 8 / ROWS_PARTS, PAIRS = 4 / ROWS_PARTS;  // tiles of 8 columns of a warp; blocks of 16 columns of F and E
   const DeltaChunkParams& p = gp.f;
+  constexpr int STAGES = Shape::stages;
+  const int more = p.hv / p.hk;
   extern __shared__ __align__(16) unsigned char rows_smem[];
   __nv_bfloat16* Qs = (__nv_bfloat16*)rows_smem;
   __nv_bfloat16* Ks = Qs + DC * ROW;
-  unsigned char* stages = rows_smem + Shape::qk;
-  unsigned char* Fs = stages + 2 * Shape::stage;
-  unsigned char *Es = Fs + DC_TILE_BYTES, *Bs = Es + DC_TILE_BYTES;  // E, and beta E
-  DeltaFactors* f = (DeltaFactors*)(Bs + DC_TILE_BYTES);
-  float* sums = (float*)(f + 1);  // [4 quarters][DC][4]
-  float* cols = sums + 4 * DC * 4;  // [4 blocks of rows][DC]
-  float* totals = cols + 4 * DC;
-  __shared__ float label_dots[DC], model_dots[ROWS_THREADS / 32];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, wr = warp & 3, wc = warp >> 2;
+  unsigned char* Fs = rows_smem + Shape::qk;
+  unsigned char *Es = Fs + DC_TRI, *Bs = Es + DC_TRI;                         // E, and beta E
+  unsigned char *Ps = Bs + DC_TRI, *Gs = Ps + DC_BLOCK - DC_P;                     // P in two parts and the factors; D o K K^T
+  const DeltaFactors* f = (const DeltaFactors*)(Ps + DC_FACTORS - DC_P);
+  float* sums = (float*)(Gs + DC_TRI);  // [ROWS_PARTS][DC][3]
+  float* cols = sums + ROWS_PARTS * DC * 3;      // [4 blocks of rows][DC]
+  unsigned char* stages = (unsigned char*)(cols + 4 * DC);
+  float* totals = gp.totals + (size_t)blockIdx.x * Shape::totals;  // where several heads share features
+  __shared__ float model_dots[ROWS_THREADS / 32];
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3, wr = warp & 3, wc = warp >> 2;
   kernel_started();
   kernel_inputs_ready();
-  const int chunk = blockIdx.x / p.hk, kh = blockIdx.x % p.hk, more = p.hv / p.hk;
-  if (chunk >= p.chunk_off[p.n_chains]) return;
-  const DeltaChunk at = p.chunks[chunk];
   const int slices = (p.dvp + ROWS_SLICE - 1) / ROWS_SLICE;
-
-  for (int u = tid; u < DC * (DK / 8); u += ROWS_THREADS) {
-    const int row = u / (DK / 8), col = u % (DK / 8) * 8;
-    const bool there = row < at.len && col < p.k.width;
-    const long long i = there ? at.row0 + row : 0;
-    const int c = there ? kh * p.k.width + col : 0;
-    copy16(smem32(Ks + row * ROW + col), p.k.p + i * p.k.ld + c, there);
-    copy16(smem32(Qs + row * ROW + col), p.q.p + i * p.q.ld + c, there);
-  }
-  auto bring = [&](int h, int slice) {  // labels slice * 32 to + 31 of S, G, U, dR, O' and V
-    unsigned char* st = stages + (slice & 1) * Shape::stage;
-    const long long which = (long long)chunk * p.hv + h;
-    const int l0 = slice * ROWS_SLICE;
-    for (int u = tid; u < ROWS_SLICE * (DK / 8); u += ROWS_THREADS) {
-      const int l = u / (DK / 8), col = u % (DK / 8) * 8;
-      const bool there = l0 + l < p.dvp;
-      const long long from = there ? (which * p.dvp + l0 + l) * DK + col : 0;
-      copy16(smem32(st + (l * ROW + col) * 2), p.starts + from, there);
-      copy16(smem32(st + Shape::models + (l * ROW + col) * 2), gp.ends + from, there);
-    }
-    for (int u = tid; u < DC * (ROWS_SLICE / 8); u += ROWS_THREADS) {
-      const int row = u / (ROWS_SLICE / 8), col = u % (ROWS_SLICE / 8) * 8, l = l0 + col;
-      unsigned char* to = st + 2 * Shape::models + (row * VROW + col) * 2;
-      const bool there = l < p.dvp, o_there = row < at.len && l < p.dout.width, v_there = row < at.len && l < p.v.width;
-      const long long from = there ? (which * DC + row) * p.dvp + l : 0, i = row < at.len ? at.row0 + row : 0;
-      copy16(smem32(to), p.steps + from, there);
-      copy16(smem32(to + Shape::labels), gp.drs + from, there);
-      copy16(smem32(to + 2 * Shape::labels), p.dout.p + (o_there ? i * p.dout.ld + h * p.dout.width + l : 0), o_there);
-      copy16(smem32(to + 3 * Shape::labels), p.v.p + (v_there ? i * p.v.ld + h * p.v.width + l : 0), v_there);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+  // Pieces: all heads of labels of a (chunk, head of features), then the next of this block's. What a copy needs is kept beside them: a piece changes once in
+  // several slices, and the divisions would cost more instructions than the products.
+  const int chunks = p.chunk_off[p.n_chains], chunk_step = gridDim.x / p.hk, head_step = gridDim.x % p.hk;
+  struct Piece {
+    int chunk, kh, hh, slice, len;
+    long long row0;
   };
-
-  const int row0 = 16 * wr, colw = wc * (DK / 4);
-  for (int hh = 0; hh < more; ++hh) {
-    const int h = kh * more + hh;
-    const unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK + DC_FACTORS;
-    for (int i = tid; i < (int)sizeof(DeltaFactors) / 16; i += ROWS_THREADS) copy16(smem32((unsigned char*)f + i * 16), block + i * 16, true);
-    bring(h, 0);
-    uint32_t P2[2][2], L2[2][2], K2[2][2];  // two elements each of P (in two parts) and D o K K^T, laid out as dP and dA
-    if (wc <= wr) {
-      const long long which = (long long)chunk * p.hv + h;
-      const unsigned char *from = p.blocks + which * DC_BLOCK + DC_P, *gram = p.gram + which * DC_TRI;
-      const int at_tri = (wr * (wr + 1) / 2 + wc) * 512;
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int unit = at_tri + tri_unit(g + 8 * e, x) + 4 * t;
-          P2[x][e] = __ldg((const uint32_t*)(from + unit));
-          L2[x][e] = __ldg((const uint32_t*)(from + DC_TRI + unit));
-          K2[x][e] = __ldg((const uint32_t*)(gram + unit));
-        }
+  auto find = [&](Piece& w) {
+    if (w.chunk >= chunks) return;
+    const DeltaChunk at = p.chunks[w.chunk];
+    w.len = at.len;
+    w.row0 = at.row0;
+  };
+  // true: another piece
+  auto advance = [&](Piece& w) {
+    if (++w.slice < slices) return false;
+    w.slice = 0;
+    if (++w.hh < more) return true;
+    w.hh = 0;
+    w.chunk += chunk_step;
+    w.kh += head_step;
+    if (w.kh >= p.hk) {
+      w.kh -= p.hk;
+      ++w.chunk;
     }
-    float dP[2][4], dA[2][4], aQ[NT][4], aX[NT][4], aH[NT][4];
+    find(w);
+    return true;
+  };
+  const int row_l = tid / (ROWS_SLICE / 8), col_l = tid % (ROWS_SLICE / 8) * 8;  // of labels
+  static_assert(ROWS_THREADS == DC * ROWS_SLICE / 8, "a thread has a unit of each tile of labels");
+  const __nv_bfloat16 *from_s, *from_g, *from_u, *from_r, *from_o, *from_v;  // this thread's part of the next slice
+  auto aim = [&](const Piece& w) {
+    if (w.chunk >= chunks) return;
+    const int h = w.kh * more + w.hh;
+    const long long which = (long long)w.chunk * p.hv + h, kept = (which * DC + row_l) * p.dvp + col_l, i = w.row0 + (row_l < w.len ? row_l : 0);
+    from_s = p.starts + which * p.dvp * DK + tid * 8;
+    from_g = gp.ends + which * p.dvp * DK + tid * 8;
+    from_u = p.steps + kept;
+    from_r = gp.drs + kept;
+    from_o = p.dout.p + i * p.dout.ld + h * p.dout.width + col_l;
+    from_v = p.v.p + i * p.v.ld + h * p.v.width + col_l;
+  };
+  auto bring = [&](const Piece& w, int ring) {  // a slice of the labels of S, G, U, dR, O' and V
+    if (w.chunk >= chunks) return;
+    const int l0 = w.slice * ROWS_SLICE, l = l0 + col_l;
+    const uint32_t st = smem32(stages) + ring * Shape::stage;
+#pragma unroll
+    for (int u = tid; u < ROWS_SLICE * (DK / 8); u += ROWS_THREADS) {
+      const int at_l = u / (DK / 8), col = u % (DK / 8) * 8;
+      const bool there = l0 + at_l < p.dvp;
+      copy16(st + (at_l * ROW + col) * 2, there ? from_s + (u - tid) * 8 : p.starts, there);
+      copy16(st + Shape::models + (at_l * ROW + col) * 2, there ? from_g + (u - tid) * 8 : gp.ends, there);
+    }
+    const uint32_t to = st + 2 * Shape::models + (row_l * VROW + col_l) * 2;
+    const bool there = l < p.dvp, given = row_l < w.len && l < p.v.width;  // labels and their gradients are of one width, rounded up to 8
+    copy16(to, there ? from_u : p.steps, there);
+    copy16(to + Shape::labels, there ? from_r : gp.drs, there);
+    copy16(to + 2 * Shape::labels, given ? from_o : p.dout.p, given);
+    copy16(to + 3 * Shape::labels, given ? from_v : p.v.p, given);
+    from_s += ROWS_SLICE * DK, from_g += ROWS_SLICE * DK, from_u += ROWS_SLICE, from_r += ROWS_SLICE, from_o += ROWS_SLICE, from_v += ROWS_SLICE;
+  };
+  auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+
+  Piece now = {(int)(blockIdx.x / p.hk), (int)(blockIdx.x % p.hk), 0, 0, 0, 0};
+  find(now);
+  Piece next = now;
+  aim(next);
+  int at_ring = 0, next_ring = 0;
+  for (int i = 0; i + 1 < STAGES; ++i) {
+    bring(next, next_ring++);
+    commit();
+    if (advance(next)) aim(next);
+  }
+  const int row0 = 16 * wr, colw = wc * (DK / ROWS_PARTS), i0 = row0 + g, i1 = i0 + 8;
+  while (now.chunk < chunks) {
+    const int chunk = now.chunk, kh = now.kh, hh = now.hh, h = kh * more + hh;
+    const DeltaChunk at = {now.row0, now.len, 0};
+    float dP[2 * PAIRS][4], dA[2 * PAIRS][4], aQ[NT][4], aX[NT][4], aH[NT][4], rv[2][4], sg[2][4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      dP[0][e] = dP[1][e] = dA[0][e] = dA[1][e] = 0.0f;
+#pragma unroll
+      for (int x = 0; x < 2 * PAIRS; ++x) dP[x][e] = dA[x][e] = 0.0f;
 #pragma unroll
       for (int x = 0; x < NT; ++x) aQ[x][e] = aX[x][e] = aH[x][e] = 0.0f;
+      rv[0][e] = rv[1][e] = sg[0][e] = sg[1][e] = 0.0f;
     }
-    float label_dot = 0.0f, model_dot = 0.0f;  // of row tid / 8; of this thread's part of S and G
     for (int sl = 0; sl < slices; ++sl) {
-      if (sl + 1 < slices) {
-        bring(h, sl + 1);
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
-      } else {
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+      __syncthreads();  // this slice is there for all, and all have left the slice before
+      bring(next, next_ring);
+      if (advance(next)) aim(next);
+      if (++next_ring == STAGES) next_ring = 0;
+      if (sl == 0) {  // and what the piece needs after its slices: all have left that of the piece before
+        if (hh == 0) {
+          for (int u = tid; u < DC * (DK / 8); u += ROWS_THREADS) {
+            const int row = u / (DK / 8), col = u % (DK / 8) * 8;
+            const bool there = row < at.len && col < p.k.width;
+            const long long i = there ? at.row0 + row : 0;
+            const int c = there ? kh * p.k.width + col : 0;
+            copy16(smem32(Ks + row * ROW + col), p.k.p + i * p.k.ld + c, there);
+            copy16(smem32(Qs + row * ROW + col), p.q.p + i * p.q.ld + c, there);
+          }
+        }
+        const long long which = (long long)chunk * p.hv + h;
+        for (int i = tid * 16; i < DC_BLOCK - DC_P; i += ROWS_THREADS * 16) copy16(smem32(Ps) + i, p.blocks + which * DC_BLOCK + DC_P + i, true);
+        for (int i = tid * 16; i < DC_TRI; i += ROWS_THREADS * 16) copy16(smem32(Gs) + i, p.gram + which * DC_TRI + i, true);
       }
-      __syncthreads();
-      const unsigned char* st = stages + (sl & 1) * Shape::stage;
-      const uint32_t s_mk = smem32(st) + lane_mk(lane, ROW) + colw * 2, g_mk = s_mk + Shape::models;
-      const uint32_t u_at = smem32(st + 2 * Shape::models), a_mk = u_at + lane_mk(lane, VROW) + row0 * VROW * 2, u_nk = u_at + lane_nk(lane, VROW) + wc * 16 * VROW * 2;
+      commit();
+      const uint32_t st = smem32(stages) + at_ring * Shape::stage;
+      if (++at_ring == STAGES) at_ring = 0;
+      const uint32_t s_mk = st + lane_mk(lane, ROW) + colw * 2, g_mk = s_mk + Shape::models, u_at = st + 2 * Shape::models;
+      const uint32_t a_mk = u_at + lane_mk(lane, VROW) + row0 * VROW * 2, u_nk = u_at + lane_nk(lane, VROW) + wc * 16 * PAIRS * VROW * 2, v_nk = u_at + 3 * Shape::labels + lane_nk(lane, VROW) + row0 * VROW * 2;
 #pragma unroll
       for (int x = 0; x < ROWS_SLICE / 16; ++x) {
         uint32_t aU[4], aR[4], aO[4], b[4];
         ldsm(aU, a_mk + x * 32);
         ldsm(aR, a_mk + Shape::labels + x * 32);
         ldsm(aO, a_mk + 2 * Shape::labels + x * 32);
-        if (wc <= wr) {
-          ldsm(b, u_nk + x * 32);
-          mma16(dP[0], aO, b[0], b[1]);
-          mma16(dP[1], aO, b[2], b[3]);
-          mma16(dA[0], aR, b[0], b[1]);
-          mma16(dA[1], aR, b[2], b[3]);
+#pragma unroll
+        for (int y = 0; y < PAIRS; ++y) {
+          if (PAIRS * wc + y > wr) break;
+          ldsm(b, u_nk + y * 16 * VROW * 2 + x * 32);
+          mma16(dP[2 * y], aO, b[0], b[1]);
+          mma16(dP[2 * y + 1], aO, b[2], b[3]);
+          mma16(dA[2 * y], aR, b[0], b[1]);
+          mma16(dA[2 * y + 1], aR, b[2], b[3]);
+        }
+        if (wc == x % ROWS_PARTS) {  // dR.v of the warp's rows: the diagonal of dR V^T
+          ldsm(b, v_nk + x * 32);
+          mma16(rv[0], aR, b[0], b[1]);
+          mma16(rv[1], aR, b[2], b[3]);
         }
 #pragma unroll
         for (int y = 0; y < NT / 2; ++y) {
+          uint32_t bg[4];
           ldsm_t(b, s_mk + x * 16 * ROW * 2 + y * 32);
+          ldsm_t(bg, g_mk + x * 16 * ROW * 2 + y * 32);
           mma16(aQ[2 * y], aO, b[0], b[1]);
           mma16(aQ[2 * y + 1], aO, b[2], b[3]);
           mma16(aX[2 * y], aR, b[0], b[1]);
           mma16(aX[2 * y + 1], aR, b[2], b[3]);
-          ldsm_t(b, g_mk + x * 16 * ROW * 2 + y * 32);
-          mma16(aH[2 * y], aU, b[0], b[1]);
-          mma16(aH[2 * y + 1], aU, b[2], b[3]);
+          mma16(aH[2 * y], aU, bg[0], bg[1]);
+          mma16(aH[2 * y + 1], aU, bg[2], bg[3]);
+          if ((y & 3) == wr) {  // S.G: the diagonal of S^T G, the same 16 labels and features as both operands
+            const uint32_t as[4] = {b[0], b[2], b[1], b[3]};
+            mma16(sg[0], as, bg[0], bg[1]);
+            mma16(sg[1], as, bg[2], bg[3]);
+          }
         }
       }
-      {  // dR.v of a row by eight threads, four labels each; S.G by all
-        const unsigned char* lab = st + 2 * Shape::models + (tid / 8 * VROW + tid % 8 * 4) * 2;
-        const uint2 r = *(const uint2*)(lab + Shape::labels), v = *(const uint2*)(lab + 3 * Shape::labels);
-        label_dot = fmaf(__uint_as_float(r.x << 16), __uint_as_float(v.x << 16), label_dot);
-        label_dot = fmaf(__uint_as_float(r.x & 0xffff0000u), __uint_as_float(v.x & 0xffff0000u), label_dot);
-        label_dot = fmaf(__uint_as_float(r.y << 16), __uint_as_float(v.y << 16), label_dot);
-        label_dot = fmaf(__uint_as_float(r.y & 0xffff0000u), __uint_as_float(v.y & 0xffff0000u), label_dot);
-        for (int u = tid; u < ROWS_SLICE * (DK / 8); u += ROWS_THREADS) {
-          const unsigned char* m = st + (u / (DK / 8) * ROW + u % (DK / 8) * 8) * 2;
-          float x[8], y[8];
-          XVec<__nv_bfloat16>::widen(*(const uint4*)m, x);
-          XVec<__nv_bfloat16>::widen(*(const uint4*)(m + Shape::models), y);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) model_dot = fmaf(x[e], y[e], model_dot);
-        }
-      }
+      advance(now);
+    }
+    if (slices < STAGES) {  // what the piece needs next came with a slice that has not been waited for
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
       __syncthreads();
     }
 
-    // F, E and beta E of the warp's 16 x 16 elements, and the sums of H over its rows and columns
-    float row_p[2] = {}, row_a[2] = {}, col_h[2][2] = {};
+    // F, E and beta E of the warp's 16 x 32 elements, and the sums of H over its rows and columns
+    float row_p[2] = {}, row_a[2] = {};
+    const float be0 = f->beta[i0], be1 = f->beta[i1], hi0 = f->hi[i0], hi1 = f->hi[i1], lo0 = f->lo[i0], lo1 = f->lo[i1];
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int y = 0; y < PAIRS; ++y) {
+      if (PAIRS * wc + y > wr) break;
+      const int at_tri = (wr * (wr + 1) / 2 + PAIRS * wc + y) * 512;
 #pragma unroll
-      for (int e = 0; e < 4; e += 2) {
-        const int i = row0 + g + 4 * e, j = wc * 16 + 8 * x + 2 * t;
-        float F[2] = {}, E[2] = {};
-        if (wc <= wr) {
-          const float be = f->beta[i];
-          const uint32_t p2 = P2[x][e / 2], l2 = L2[x][e / 2], k2 = K2[x][e / 2];
+      for (int x = 0; x < 2; ++x) {
+        const int j = (PAIRS * wc + y) * 16 + 8 * x + 2 * t;
+        const float2 ch = *(const float2*)(f->hi + j), cl = *(const float2*)(f->lo + j);
+        float col_h[2] = {};
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const float d = exp2_fast((f->hi[i] - f->hi[j + y]) + (f->lo[i] - f->lo[j + y]));
-            const float pp = y ? __uint_as_float(p2 & 0xffff0000u) + __uint_as_float(l2 & 0xffff0000u) : __uint_as_float(p2 << 16) + __uint_as_float(l2 << 16);
-            const float kk = y ? __uint_as_float(k2 & 0xffff0000u) : __uint_as_float(k2 << 16);
-            const bool below = j + y < i;
-            F[y] = j + y <= i ? p.scale * d * dP[x][e + y] : 0.0f;
-            E[y] = below ? -d * dA[x][e + y] : 0.0f;
-            const float hp = below ? dP[x][e + y] * pp : 0.0f, ha = below ? -dA[x][e + y] * kk : 0.0f;
+        for (int e = 0; e < 4; e += 2) {
+          const int i = i0 + 4 * e, unit = at_tri + tri_unit(g + 4 * e, x) + 4 * t;
+          const float be = e ? be1 : be0, hi = e ? hi1 : hi0, lo = e ? lo1 : lo0;
+          const uint32_t p2 = *(const uint32_t*)(Ps + unit), l2 = *(const uint32_t*)(Ps + DC_TRI + unit), k2 = *(const uint32_t*)(Gs + unit);
+          const float d[2] = {exp2_fast((hi - ch.x) + (lo - cl.x)), exp2_fast((hi - ch.y) + (lo - cl.y))};
+          const float pp[2] = {__uint_as_float(p2 << 16) + __uint_as_float(l2 << 16), __uint_as_float(p2 & 0xffff0000u) + __uint_as_float(l2 & 0xffff0000u)};
+          const float kk[2] = {__uint_as_float(k2 << 16), __uint_as_float(k2 & 0xffff0000u)};
+          float F[2], E[2];
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const bool below = j + z < i;
+            const float dp = dP[2 * y + x][e + z], da = -dA[2 * y + x][e + z];
+            F[z] = j + z <= i ? p.scale * d[z] * dp : 0.0f;
+            E[z] = below ? d[z] * da : 0.0f;
+            const float hp = below ? dp * pp[z] : 0.0f, ha = below ? da * kk[z] : 0.0f;
             row_p[e / 2] += hp;
             row_a[e / 2] += ha;
-            col_h[x][y] += fmaf(be, ha, hp);
+            col_h[z] += fmaf(be, ha, hp);
           }
+          *(uint32_t*)(Fs + unit) = pack2(F[0], F[1]);
+          *(uint32_t*)(Es + unit) = pack2(E[0], E[1]);
+          *(uint32_t*)(Bs + unit) = pack2(be * E[0], be * E[1]);
         }
-        const int to = (i * DC_TILE + j) * 2;
-        *(uint32_t*)(Fs + to) = pack2(F[0], F[1]);
-        *(uint32_t*)(Es + to) = pack2(E[0], E[1]);
-        *(uint32_t*)(Bs + to) = pack2(f->beta[i] * E[0], f->beta[i] * E[1]);
-      }
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        float v = col_h[x][y];
-        v += __shfl_xor_sync(0xffffffffu, v, 4);
-        v += __shfl_xor_sync(0xffffffffu, v, 8);
-        v += __shfl_xor_sync(0xffffffffu, v, 16);
-        if (g == 0) cols[wr * DC + wc * 16 + 8 * x + 2 * t + y] = v;
+        for (int z = 0; z < 2; ++z) {
+          float v = col_h[z];
+          v += __shfl_xor_sync(0xffffffffu, v, 4);
+          v += __shfl_xor_sync(0xffffffffu, v, 8);
+          v += __shfl_xor_sync(0xffffffffu, v, 16);
+          if (g == 0) cols[wr * DC + j + z] = v;
+        }
       }
-    label_dot += __shfl_xor_sync(0xffffffffu, label_dot, 1);
-    label_dot += __shfl_xor_sync(0xffffffffu, label_dot, 2);
-    label_dot += __shfl_xor_sync(0xffffffffu, label_dot, 4);
-    if (tid % 8 == 0) label_dots[tid / 8] = label_dot;
-    model_dot = warp_sum(model_dot);
-    if (lane == 0) model_dots[warp] = model_dot;
+    }
+    const bool diagonal = t == g >> 1;  // this lane has elements (g, g) and (g + 8, g + 8) of the diagonal products
+    {
+      const float v = warp_sum(diagonal ? (g & 1 ? sg[0][1] + sg[1][3] : sg[0][0] + sg[1][2]) : 0.0f);
+      if (lane == 0) model_dots[warp] = v;
+    }
     __syncthreads();
 
-    const int i0 = row0 + g, i1 = i0 + 8;
-    const float c0 = f->c[i0], c1 = f->c[i1], r0 = f->r[i0], r1 = f->r[i1], be0 = f->beta[i0], be1 = f->beta[i1];
-    // of rows i0 and i1: what passes from S and from H's rows, x.k, k.(r U G^T)
-    float dots[3][2] = {{fmaf(be0, row_a[0], row_p[0]), fmaf(be1, row_a[1], row_p[1])}, {row_a[0], row_a[1]}, {0.0f, 0.0f}};
+    // of rows i0 and i1: what passes from S and from H's rows, dbeta, k.(r U G^T)
+    const float c0 = f->c[i0], c1 = f->c[i1], r0 = f->r[i0], r1 = f->r[i1], last = f->last;
+    float dots[3][2] = {{fmaf(be0, row_a[0], row_p[0]), fmaf(be1, row_a[1], row_p[1])},
+                        {row_a[0] + (diagonal ? (g & 1 ? rv[0][1] : rv[0][0]) : 0.0f), row_a[1] + (diagonal ? (g & 1 ? rv[1][3] : rv[1][2]) : 0.0f)},
+                        {0.0f, 0.0f}};
     auto pair_at = [&](const __nv_bfloat16* tile, int row, int x) {  // two elements of a row in the warp's columns
       const uint32_t v = *(const uint32_t*)(tile + row * ROW + colw + 8 * x + 2 * t);
       return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
@@ -440,14 +490,23 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
       dots[2][0] += k0.x * aH[x][0] + k0.y * aH[x][1];
       dots[2][1] += k1.x * aH[x][2] + k1.y * aH[x][3];
     }
+#pragma unroll
+    for (int d = 0; d < 3; ++d)
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        float v = dots[d][z];
+        v += __shfl_xor_sync(0xffffffffu, v, 1);
+        v += __shfl_xor_sync(0xffffffffu, v, 2);
+        if (t == 0) sums[(wc * DC + i0 + 8 * z) * 3 + d] = v;
+      }
     const uint32_t k_mk = smem32(Ks) + lane_mk(lane, ROW) + colw * 2, q_mk = smem32(Qs) + lane_mk(lane, ROW) + colw * 2;
-    const uint32_t f_mk = smem32(Fs) + lane_mk(lane, DC_TILE) + row0 * DC_TILE * 2, f_nk = smem32(Fs) + lane_nk(lane, DC_TILE) + row0 * 2;
+    const uint32_t f_mk = smem32(Fs) + tri_mk(lane) + wr * (wr + 1) / 2 * 512, f_nk = smem32(Fs) + tri_nk(lane) + wr * 512;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       uint32_t a[4], e[4], b[4];
       if (x <= wr) {  // rows of F and E: dQ and x
-        ldsm(a, f_mk + x * 32);
-        ldsm(e, f_mk + DC_TILE_BYTES + x * 32);
+        ldsm(a, f_mk + x * 512);
+        ldsm(e, f_mk + DC_TRI + x * 512);
 #pragma unroll
         for (int y = 0; y < NT / 2; ++y) {
           ldsm_t(b, k_mk + x * 16 * ROW * 2 + y * 32);
@@ -458,8 +517,8 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
         }
       }
       if (x >= wr) {  // columns of F and beta E: back
-        ldsm_t(a, f_nk + x * 16 * DC_TILE * 2);
-        ldsm_t(e, f_nk + 2 * DC_TILE_BYTES + x * 16 * DC_TILE * 2);
+        ldsm_t(a, f_nk + tri_at(x, 0));
+        ldsm_t(e, f_nk + 2 * DC_TRI + tri_at(x, 0));
 #pragma unroll
         for (int y = 0; y < NT / 2; ++y) {
           ldsm_t(b, q_mk + x * 16 * ROW * 2 + y * 32);
@@ -471,46 +530,34 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
         }
       }
     }
+    __syncthreads();  // sums are there; Q, K, F, E and the factors are free
+    // dQ (in aQ) and dK (in aX), added up over the heads of labels that share these features by the thread that has the elements
+    float4* mine = (float4*)totals + tid;
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
-      aX[x][0] = fmaf(be0, aX[x][0], aH[x][0]), aX[x][1] = fmaf(be0, aX[x][1], aH[x][1]);  // dK
+      aX[x][0] = fmaf(be0, aX[x][0], aH[x][0]), aX[x][1] = fmaf(be0, aX[x][1], aH[x][1]);
       aX[x][2] = fmaf(be1, aX[x][2], aH[x][2]), aX[x][3] = fmaf(be1, aX[x][3], aH[x][3]);
-    }
-#pragma unroll
-    for (int d = 0; d < 3; ++d)
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        float v = dots[d][z];
-        v += __shfl_xor_sync(0xffffffffu, v, 1);
-        v += __shfl_xor_sync(0xffffffffu, v, 2);
-        if (t == 0) sums[(wc * DC + i0 + 8 * z) * 4 + d] = v;
+      if (hh > 0) {
+        const float4 q = mine[2 * x * ROWS_THREADS], k = mine[(2 * x + 1) * ROWS_THREADS];
+        aQ[x][0] += q.x, aQ[x][1] += q.y, aQ[x][2] += q.z, aQ[x][3] += q.w;
+        aX[x][0] += k.x, aX[x][1] += k.y, aX[x][2] += k.z, aX[x][3] += k.w;
       }
-    // the heads of labels that share these features, added up by the thread that has the elements
-    if (more > 1) {
-#pragma unroll
-      for (int x = 0; x < NT; ++x)
-#pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          float2* tq = (float2*)(totals + (i0 + 4 * e) * DK + colw + 8 * x + 2 * t);
-          float2* tk = tq + DC * DK / 2;
-          if (hh > 0) {
-            const float2 q = *tq, k = *tk;
-            aQ[x][e] += q.x, aQ[x][e + 1] += q.y, aX[x][e] += k.x, aX[x][e + 1] += k.y;
-          }
-          if (hh + 1 < more) {
-            *tq = make_float2(aQ[x][e], aQ[x][e + 1]);
-            *tk = make_float2(aX[x][e], aX[x][e + 1]);
-          }
-        }
     }
-    if (hh + 1 == more) {
+    if (hh + 1 < more) {
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        mine[2 * x * ROWS_THREADS] = make_float4(aQ[x][0], aQ[x][1], aQ[x][2], aQ[x][3]);
+        mine[(2 * x + 1) * ROWS_THREADS] = make_float4(aX[x][0], aX[x][1], aX[x][2], aX[x][3]);
+      }
+    } else {
+      const long long to0 = ((at.row0 + i0) * p.hk + kh) * p.dk + colw + 2 * t, to1 = to0 + 8ll * p.hk * p.dk;
 #pragma unroll
       for (int x = 0; x < NT; ++x)
 #pragma unroll
         for (int e = 0; e < 4; e += 2) {
-          const int i = i0 + 4 * e, col = colw + 8 * x + 2 * t;
-          if (i >= at.len) continue;
-          const long long to = ((at.row0 + i) * p.hk + kh) * p.dk + col;
+          const int col = colw + 8 * x + 2 * t;
+          if ((e ? i1 : i0) >= at.len) continue;
+          const long long to = (e ? to1 : to0) + 8 * x;
           if (gp.vec_dk) {
             if (col < p.dk) {
               *(uint32_t*)(gp.dq + to) = pack2(aQ[x][e], aQ[x][e + 1]);
@@ -518,30 +565,31 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
             }
           } else {
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
-              if (col + y < p.dk) {
-                gp.dq[to + y] = __float2bfloat16_rn(aQ[x][e + y]);
-                gp.dk[to + y] = __float2bfloat16_rn(aX[x][e + y]);
+            for (int z = 0; z < 2; ++z)
+              if (col + z < p.dk) {
+                gp.dq[to + z] = __float2bfloat16_rn(aQ[x][e + z]);
+                gp.dk[to + z] = __float2bfloat16_rn(aX[x][e + z]);
               }
           }
         }
     }
-    __syncthreads();
     if (warp == 0) {  // two rows a lane: dbeta, and dg by a scan from the chunk's end
       float db[2], ahead = 0.0f;
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
         const int i = 2 * lane + z;
-        float v[3] = {0, 0, 0};
-        for (int w = 0; w < 4; ++w)
+        float v[3];
 #pragma unroll
-          for (int d = 0; d < 3; ++d) v[d] += sums[(w * DC + i) * 4 + d];
+        for (int d = 0; d < 3; ++d) {
+          v[d] = 0.0f;
+          for (int w = 0; w < ROWS_PARTS; ++w) v[d] += sums[(w * DC + i) * 3 + d];
+        }
         for (int w = i / 16; w < 4; ++w) v[0] -= cols[w * DC + i];
         db[z] = v[0] - v[2];
         ahead += v[2];
-        if (i < at.len) gp.dbeta[(at.row0 + i) * p.hv + h] = __float2bfloat16_rn(label_dots[i] + v[1]);
+        if (i < at.len) gp.dbeta[(at.row0 + i) * p.hv + h] = __float2bfloat16_rn(v[1]);
       }
-      const float decay = f->last * warp_sum(lane < ROWS_THREADS / 32 ? model_dots[lane] : 0.0f) + warp_sum(ahead);
+      const float decay = last * warp_sum(lane < ROWS_THREADS / 32 ? model_dots[lane] : 0.0f) + warp_sum(ahead);
       float sum = db[0] + db[1];  // of this lane's rows and all behind them
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -554,8 +602,8 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
         if (i < at.len) gp.dg[(at.row0 + i) * p.hv + h] = __float2bfloat16_rn(decay + sum - (z ? db[0] : 0.0f));
       }
     }
-    __syncthreads();
   }
+  copies_done();
 }
 
 }  // namespace wpsgd

@@ -185,17 +185,21 @@ wpsgd_status run_chunks(wpsgd_ctx* c, DeltaChunkParams p, const DeltaLayout& lay
   return w == 8 ? walk<DK, 8>(c, p, save) : w == 4 ? walk<DK, 4>(c, p, save) : w == 2 ? walk<DK, 2>(c, p, save) : walk<DK, 1>(c, p, save);
 }
 
+// Blocks that go through the chunks' rows: one per SM
+int rows_blocks(const wpsgd_delta_rows* r, const DeltaLayout& lay) { return (int)std::min<long long>(lay.chunks * r->heads_k, 148); }
+
 // The gradient's own workspace
 struct DeltaGradLayout {
   bool pack_o;
-  size_t dout, ends, drs, total;
+  size_t dout, ends, drs, totals, total;
   DeltaGradLayout(const wpsgd_delta_rows* r, const DeltaLayout& lay, const void* p, int64_t ld) {
     pack_o = r->dv % 8 != 0 || !aligned16(p) || ld % 8 != 0;
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     dout = 0;
     ends = up((size_t)r->n_rows * r->heads_v * lay.dv8 * 2);  // kept free also where the rows of dout are taken as they are: the size goes by `rows` alone
     drs = ends + up((size_t)lay.chunks * r->heads_v * lay.dvp * lay.DK * 2);
-    total = drs + up((size_t)lay.chunks * r->heads_v * DC * lay.dvp * 2);
+    totals = drs + up((size_t)lay.chunks * r->heads_v * DC * lay.dvp * 2);
+    total = totals + (r->heads_v > r->heads_k ? (size_t)rows_blocks(r, lay) * 2 * DC * lay.DK * 4 : 0);
   }
 };
 
@@ -209,13 +213,13 @@ wpsgd_status walk_back(wpsgd_ctx* c, const DeltaGradParams& p) {
 }
 
 template <int DK>
-wpsgd_status grad_chunks(wpsgd_ctx* c, DeltaGradParams p, const DeltaLayout& lay) {
+wpsgd_status grad_chunks(wpsgd_ctx* c, DeltaGradParams p, const DeltaLayout& lay, int blocks) {
   const int w = chain_warps((long long)p.f.n_chains * p.f.hv, p.f.dvp);
   p.f.slices = (p.f.dvp / 16 + w - 1) / w;
   const wpsgd_status s = w == 8 ? walk_back<DK, 8>(c, p) : w == 4 ? walk_back<DK, 4>(c, p) : w == 2 ? walk_back<DK, 2>(c, p) : walk_back<DK, 1>(c, p);
   if (s != WPSGD_OK || lay.chunks == 0) return s;
   CU_TRY(c, (allow_smem<delta_rowgrad_kernel<DK>>(c)));
-  CU_TRY(c, launch(delta_rowgrad_kernel<DK>, (unsigned)(lay.chunks * p.f.hk), ROWS_THREADS, RowsShape<DK>::smem(p.f.hv > p.f.hk), c->stream, p));
+  CU_TRY(c, launch(delta_rowgrad_kernel<DK>, (unsigned)blocks, ROWS_THREADS, RowsShape<DK>::smem, c->stream, p));
   c->launches++;
   return WPSGD_OK;
 }
@@ -293,7 +297,7 @@ wpsgd_status wpsgd_delta_grad(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const 
   }
   DeviceGuard guard(c->device);
   unsigned char* ws = (unsigned char*)workspace;
-  DeltaGradParams p = {chunk_params(c, rows, lay, (unsigned char*)saved), (__nv_bfloat16*)(ws + own.ends), (__nv_bfloat16*)(ws + own.drs), dW, dW0, (__nv_bfloat16*)dq, (__nv_bfloat16*)dk,
+  DeltaGradParams p = {chunk_params(c, rows, lay, (unsigned char*)saved), (__nv_bfloat16*)(ws + own.ends), (__nv_bfloat16*)(ws + own.drs), (float*)(ws + own.totals), dW, dW0, (__nv_bfloat16*)dq, (__nv_bfloat16*)dk,
                        (__nv_bfloat16*)dv, (__nv_bfloat16*)dg, (__nv_bfloat16*)dbeta, rows->dv % 8 == 0 && aligned16(dv), rows->dk % 2 == 0 && ((uintptr_t)dq | (uintptr_t)dk) % 4 == 0};
   p.f.dout = own.pack_o ? DeltaHeads{(const __nv_bfloat16*)(ws + own.dout), (long long)rows->heads_v * lay.dv8, rows->heads_v, lay.dv8}
                         : DeltaHeads{(const __nv_bfloat16*)dout, ld_dout, rows->heads_v, rows->dv};
@@ -301,7 +305,7 @@ wpsgd_status wpsgd_delta_grad(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const 
     const wpsgd_status s = pack_heads(c, dout, ld_dout, rows->heads_v, rows->dv, p.f.dout.p, n);
     if (s != WPSGD_OK) return s;
   }
-  return lay.DK == 64 ? grad_chunks<64>(c, p, lay) : grad_chunks<128>(c, p, lay);
+  return lay.DK == 64 ? grad_chunks<64>(c, p, lay, rows_blocks(rows, lay)) : grad_chunks<128>(c, p, lay, rows_blocks(rows, lay));
 }
 
 wpsgd_status wpsgd_delta_step(wpsgd_ctx* c, const wpsgd_delta_rows* rows, float* W, const int32_t* slots, int64_t n_slots, void* out, int64_t ld_out) {
