@@ -464,11 +464,19 @@ __device__ __forceinline__ void copy_rows(uint32_t to, int stride, const __nv_bf
     copy16(to + r * stride + col * 2, from + (there ? r * ld + col : 0), there);
   }
 }
+// Rows of a chain, and of its chunk i. (Looked up in the list of chunks by each warp, they would be waited for twice a chunk: 1400 of 12000 cycles.)
+struct DeltaSpan {
+  long long row0, rows;
+  __device__ __forceinline__ int len(int i) const { return (int)min((long long)DC, rows - (long long)i * DC); }
+};
 // A warp's share of a chunk: features, queries, labels (or their gradients) and the block of the first kernel. The barrier takes an arrival of every thread.
 template <int DK, int NW>
-__device__ __forceinline__ void bring_chunk(const DeltaChunkParams& p, const DeltaHeads& labels, uint32_t st, int chunk, int h, int kh, int col0, int warp, int warps, int lane, unsigned long long* full) {
+__device__ __forceinline__ void bring_chunk(const DeltaChunkParams& p, const DeltaHeads& labels, uint32_t st, int chunk, const DeltaSpan& span, int i, int h, int kh, int col0, int warp, int warps, int lane, unsigned long long* full) {
   using Shape = ChainShape<DK, NW>;
-  const DeltaChunk at = p.chunks[chunk];
+  const struct {
+    long long row0;
+    int len;
+  } at = {span.row0 + (long long)i * DC, span.len(i)};
   copy_rows<DK / 8>(st, Shape::row * 2, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, p.k.width, warp, warps, lane);
   copy_rows<DK / 8>(st + Shape::q_at, Shape::row * 2, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, p.q.width, warp, warps, lane);
   copy_rows<2 * NW>(st + Shape::v_at, Shape::vrow * 2, labels.p + at.row0 * labels.ld + h * labels.width + col0, labels.ld, at.len, labels.width - col0, warp, warps, lane);
@@ -477,9 +485,9 @@ __device__ __forceinline__ void bring_chunk(const DeltaChunkParams& p, const Del
   for (int i = (warp * 32 + lane) * 16; i < DC_BLOCK; i += warps * 512) copy16(st + Shape::block_at + i, block + i, true);
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem32(full)) : "memory");
 }
-// A copying warp's work: its share of all n chunks, from `first` on in steps of 1 or -1
+// A copying warp's work: its share of all n chunks, the last first where `back`
 template <int DK, int NW>
-__device__ __forceinline__ void bring_chunks(const DeltaChunkParams& p, const DeltaHeads& labels, uint32_t smem, int first, int step, int n, int h, int kh, int col0, int warp, int lane,
+__device__ __forceinline__ void bring_chunks(const DeltaChunkParams& p, const DeltaHeads& labels, uint32_t smem, int first, bool back, int n, const DeltaSpan& span, int h, int kh, int col0, int warp, int lane,
                                              unsigned long long* full, unsigned long long* empty) {
   using Shape = ChainShape<DK, NW>;
   for (int i = 0; i < n; ++i) {
@@ -489,7 +497,8 @@ __device__ __forceinline__ void bring_chunks(const DeltaChunkParams& p, const De
       break;
     }
     if (i == p.drop) break;  // a test hook: this chunk and those behind it are never brought
-    bring_chunk<DK, NW>(p, labels, smem + s * Shape::stage, first + step * i, h, kh, col0, warp, Shape::copiers, lane, &full[s]);
+    const int j = back ? n - 1 - i : i;
+    bring_chunk<DK, NW>(p, labels, smem + s * Shape::stage, first + j, span, j, h, kh, col0, warp, Shape::copiers, lane, &full[s]);
   }
   copies_done();
 }
@@ -532,6 +541,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
+  const DeltaSpan span = {p.shard_off[chain], p.shard_off[chain + 1] - p.shard_off[chain]};
   constexpr bool COPIERS = Shape::copiers > 0;
   const int bringers = COPIERS ? Shape::copiers : warps;
   if (tid == 0) {
@@ -543,11 +553,11 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
   }
   __syncthreads();
   if (COPIERS && warp >= NW) {
-    bring_chunks<DK, NW>(p, p.v, smem32(chain_smem), first, 1, n, h, kh, col0, warp - NW, lane, full, empty);
+    bring_chunks<DK, NW>(p, p.v, smem32(chain_smem), first, false, n, span, h, kh, col0, warp - NW, lane, full, empty);
     return;
   }
   if (warp >= warps) return;
-  if (!COPIERS && n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem), first, h, kh, col0, warp, warps, lane, &full[0]);
+  if (!COPIERS && n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem), first, span, 0, h, kh, col0, warp, warps, lane, &full[0]);
 
   // S^T: labels g and g + 8 of the warp's 16, features 8 n + 2 t and the next
   float S[DK / 8][4];
@@ -566,7 +576,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
     bool ok = true;
     if (!COPIERS && i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
       if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s1], ((i + 1) / STAGES - 1) & 1, p.spin_limit));
-      if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem) + s1 * Shape::stage, first + i + 1, h, kh, col0, warp, warps, lane, &full[s1]);
+      if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem) + s1 * Shape::stage, first + i + 1, span, i + 1, h, kh, col0, warp, warps, lane, &full[s1]);
     }
     if (!ok || !__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (i / STAGES) & 1, p.spin_limit))) {
       if (lane == 0) set_status(p.status, DEV_TIMEOUT, 25, i);
@@ -580,12 +590,12 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
     const uint32_t k_nk = smem32(st) + lane_nk(lane, Shape::row), q_nk = k_nk + Q_AT, k_mk = smem32(st) + lane_mk(lane, Shape::row);
     const uint32_t t_nk = smem32(block) + tri_nk(lane), v_nk = smem32(st + V_AT) + warp * 32 + lane_nk(lane, Shape::vrow);
 
-    // S^T K^T and S^T Q^T
-    float R[8][4], O[8][4];
+    // S^T K^T
+    float R[8][4];
 #pragma unroll
     for (int x = 0; x < 8; ++x)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) R[x][e] = O[x][e] = 0.0f;
+      for (int e = 0; e < 4; ++e) R[x][e] = 0.0f;
 #pragma unroll
     for (int x = 0; x < DK / 16; ++x) {
       uint32_t hi[4], lo[4], b[4][4];
@@ -609,15 +619,8 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
         mma16(R[2 * y], lo, b[y][0], b[y][1]);
         mma16(R[2 * y + 1], lo, b[y][2], b[y][3]);
       }
-#pragma unroll
-      for (int y = 0; y < 4; ++y) ldsm(b[y], q_nk + y * 16 * ROW + x * 32);
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        mma16(O[2 * y], hi, b[y][0], b[y][1]);
-        mma16(O[2 * y + 1], hi, b[y][2], b[y][3]);
-      }
     }
-    // R^T = beta (V^T - c S^T K^T), and the answers' share of the models
+    // R^T = beta (V^T - c S^T K^T)
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
       uint32_t v[4];
@@ -631,16 +634,14 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
         R[x][1] = be.y * (__uint_as_float(v0 & 0xffff0000u) - c.y * R[x][1]);
         R[x][2] = be.x * (__uint_as_float(v1 << 16) - c.x * R[x][2]);
         R[x][3] = be.y * (__uint_as_float(v1 & 0xffff0000u) - c.y * R[x][3]);
-        const float cx = p.scale * c.x, cy = p.scale * c.y;
-        O[x][0] *= cx, O[x][1] *= cy, O[x][2] *= cx, O[x][3] *= cy;
       }
     }
-    // U^T = R^T T^T: rows of T from the block of 16 columns on
-    float U[8][4];
+    // U^T = R^T T^T, rows of T from the block of 16 columns on: chains of dependent products, between them S^T Q^T, which waits for nothing
+    float U[8][4], O[8][4];
 #pragma unroll
     for (int x = 0; x < 8; ++x)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) U[x][e] = 0.0f;
+      for (int e = 0; e < 4; ++e) U[x][e] = O[x][e] = 0.0f;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       uint32_t hi[4], lo[4], bh[4], bl[4];
@@ -651,8 +652,33 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
         ldsm(bl, t_nk + DC_T_LO + tri_at(y, x));
         mma_split(U[2 * y], U[2 * y + 1], hi, lo, bh, bl);
       }
+#pragma unroll
+      for (int z = x * DK / 64; z < (x + 1) * DK / 64; ++z) {
+        const uint32_t a[4] = {pack2(S[2 * z][0], S[2 * z][1]), pack2(S[2 * z][2], S[2 * z][3]), pack2(S[2 * z + 1][0], S[2 * z + 1][1]), pack2(S[2 * z + 1][2], S[2 * z + 1][3])};
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          ldsm(bh, q_nk + y * 16 * ROW + z * 32);
+          mma16(O[2 * y], a, bh[0], bh[1]);
+          mma16(O[2 * y + 1], a, bh[2], bh[3]);
+        }
+      }
     }
-    // O^T += U^T P^T
+    if (SAVE) put_labels<true>(U, st + V_AT + warp * 32, VROW, lane, p.steps + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
+    // O^T = scale c S^T Q^T + U^T P^T, and S^T <- e^{b_C} S^T + (r U)^T K
+    const uint64_t last = pair_of(__float_as_uint(f->last), __float_as_uint(f->last));
+#pragma unroll
+    for (int x = 0; x < DK / 8; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        const float2 v = halves(mul2(last, pair_of(__float_as_uint(S[x][e]), __float_as_uint(S[x][e + 1]))));
+        S[x][e] = v.x, S[x][e + 1] = v.y;
+      }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const float2 c = *(const float2*)(f->c + 8 * x + 2 * t);
+      const float cx = p.scale * c.x, cy = p.scale * c.y;
+      O[x][0] *= cx, O[x][1] *= cy, O[x][2] *= cx, O[x][3] *= cy;
+    }
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       uint32_t hi[4], lo[4], bh[4], bl[4];
@@ -663,17 +689,6 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
         ldsm(bl, t_nk + DC_P_LO + tri_at(y, x));
         mma_split(O[2 * y], O[2 * y + 1], hi, lo, bh, bl);
       }
-    }
-    if (SAVE) put_labels<true>(U, st + V_AT + warp * 32, VROW, lane, p.steps + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
-    // S^T <- e^{b_C} S^T + (r U)^T K
-    const float last = f->last;
-#pragma unroll
-    for (int x = 0; x < DK / 8; ++x)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) S[x][e] *= last;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      uint32_t hi[4], lo[4], b[4];
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
         const float2 r = *(const float2*)(f->r + 16 * x + 8 * z + 2 * t);
@@ -682,18 +697,17 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
       a_parts(U[2 * x], U[2 * x + 1], hi, lo);
 #pragma unroll
       for (int y = 0; y < DK / 16; ++y) {
-        ldsm_t(b, k_mk + x * 16 * ROW + y * 32);
-        mma16(S[2 * y], hi, b[0], b[1]);
-        mma16(S[2 * y + 1], hi, b[2], b[3]);
-        mma16(S[2 * y], lo, b[0], b[1]);
-        mma16(S[2 * y + 1], lo, b[2], b[3]);
+        ldsm_t(bh, k_mk + x * 16 * ROW + y * 32);
+        mma16(S[2 * y], hi, bh[0], bh[1]);
+        mma16(S[2 * y + 1], hi, bh[2], bh[3]);
+        mma16(S[2 * y], lo, bh[0], bh[1]);
+        mma16(S[2 * y + 1], lo, bh[2], bh[3]);
       }
     }
-    const DeltaChunk at = p.chunks[first + i];
-    __nv_bfloat16* out = p.out + at.row0 * p.ld_out + h * p.dv + col0 + warp * 16;
+    __nv_bfloat16* out = p.out + (span.row0 + (long long)i * DC) * p.ld_out + h * p.dv + col0 + warp * 16;
     const int cols = min(16, p.dv - col0 - warp * 16);
-    if (p.vec_out) put_labels<true>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, at.len, cols);
-    else put_labels<false>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, at.len, cols);
+    if (p.vec_out) put_labels<true>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, span.len(i), cols);
+    else put_labels<false>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, span.len(i), cols);
     __syncwarp();
     if (lane == 0) arrive(&empty[s]);
   }

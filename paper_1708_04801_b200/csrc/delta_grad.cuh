@@ -44,6 +44,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
+  const DeltaSpan span = {p.shard_off[chain], p.shard_off[chain + 1] - p.shard_off[chain]};
   constexpr bool COPIERS = Shape::copiers > 0;
   const int bringers = COPIERS ? Shape::copiers : warps;
   if (tid == 0) {
@@ -55,11 +56,11 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
   }
   __syncthreads();
   if (COPIERS && warp >= NW) {
-    bring_chunks<DK, NW>(p, p.dout, smem32(chain_smem), first + n - 1, -1, n, h, kh, col0, warp - NW, lane, full, empty);
+    bring_chunks<DK, NW>(p, p.dout, smem32(chain_smem), first, true, n, span, h, kh, col0, warp - NW, lane, full, empty);
     return;
   }
   if (warp >= warps) return;
-  if (!COPIERS && n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem), first + n - 1, h, kh, col0, warp, warps, lane, &full[0]);
+  if (!COPIERS && n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem), first + n - 1, span, n - 1, h, kh, col0, warp, warps, lane, &full[0]);
 
   float G[DK / 8][4];  // G^T, as S^T in the forward walk
   const int label = col0 + warp * 16 + g;
@@ -77,7 +78,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
     bool ok = true;
     if (!COPIERS && i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
       if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s1], ((i + 1) / STAGES - 1) & 1, p.spin_limit));
-      if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem) + s1 * Shape::stage, first + n - 2 - i, h, kh, col0, warp, warps, lane, &full[s1]);
+      if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem) + s1 * Shape::stage, first + n - 2 - i, span, n - 2 - i, h, kh, col0, warp, warps, lane, &full[s1]);
     }
     if (!ok || !__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (i / STAGES) & 1, p.spin_limit))) {
       if (lane == 0) set_status(p.status, DEV_TIMEOUT, 26, i);
@@ -125,47 +126,37 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
       const float2 r = *(const float2*)(f->r + 8 * x + 2 * t);
       M[x][0] *= r.x, M[x][1] *= r.y, M[x][2] *= r.x, M[x][3] *= r.y;
     }
-    const float last = f->last;
+    const uint64_t last = pair_of(__float_as_uint(f->last), __float_as_uint(f->last));
 #pragma unroll
     for (int x = 0; x < DK / 8; ++x)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) G[x][e] *= last;
-    // ... and G^T + (scale c O')^T Q
+      for (int e = 0; e < 4; e += 2) {
+        const float2 v = halves(mul2(last, pair_of(__float_as_uint(G[x][e]), __float_as_uint(G[x][e + 1]))));
+        G[x][e] = v.x, G[x][e + 1] = v.y;
+      }
+    uint32_t o[4][4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      uint32_t a[4], b[4], hi[4], lo[4];
-      ldsm_t(a, v_nk + x * 16 * VROW);
+      uint32_t b[4];
+      ldsm_t(o[x], v_nk + x * 16 * VROW);
 #pragma unroll
       for (int y = 0; y <= x; ++y) {
         ldsm_t(b, t_mk + DC_P + tri_at(x, y));
-        mma16(M[2 * y], a, b[0], b[1]);
-        mma16(M[2 * y + 1], a, b[2], b[3]);
+        mma16(M[2 * y], o[x], b[0], b[1]);
+        mma16(M[2 * y + 1], o[x], b[2], b[3]);
         ldsm_t(b, t_mk + DC_P_LO + tri_at(x, y));
-        mma16(M[2 * y], a, b[0], b[1]);
-        mma16(M[2 * y + 1], a, b[2], b[3]);
-      }
-#pragma unroll
-      for (int z = 0; z < 4; ++z) {
-        const float2 c = *(const float2*)(f->c + 16 * x + 8 * (z >> 1) + 2 * t);
-        split2(p.scale * c.x * __uint_as_float(a[z] << 16), p.scale * c.y * __uint_as_float(a[z] & 0xffff0000u), hi[z], lo[z]);
-      }
-#pragma unroll
-      for (int y = 0; y < DK / 16; ++y) {
-        ldsm_t(b, q_mk + x * 16 * ROW + y * 32);
-        mma16(G[2 * y], hi, b[0], b[1]);
-        mma16(G[2 * y + 1], hi, b[2], b[3]);
-        mma16(G[2 * y], lo, b[0], b[1]);
-        mma16(G[2 * y + 1], lo, b[2], b[3]);
+        mma16(M[2 * y], o[x], b[0], b[1]);
+        mma16(M[2 * y + 1], o[x], b[2], b[3]);
       }
     }
-    // dR^T = dU^T T: columns of T up to the block of 16 rows
+    // dR^T = dU^T T, columns of T up to the block of 16 rows: chains of dependent products, between them G^T + (scale c O')^T Q
     float R[8][4];
 #pragma unroll
     for (int x = 0; x < 8; ++x)
 #pragma unroll
       for (int e = 0; e < 4; ++e) R[x][e] = 0.0f;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
+    for (int x = 3; x >= 0; --x) {
       uint32_t hi[4], lo[4], bh[4], bl[4];
       a_parts(M[2 * x], M[2 * x + 1], hi, lo);
 #pragma unroll
@@ -173,6 +164,19 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
         ldsm_t(bh, t_mk + tri_at(x, y));
         ldsm_t(bl, t_mk + DC_T_LO + tri_at(x, y));
         mma_split(R[2 * y], R[2 * y + 1], hi, lo, bh, bl);
+      }
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        const float2 c = *(const float2*)(f->c + 16 * x + 8 * (z >> 1) + 2 * t);
+        split2(p.scale * c.x * __uint_as_float(o[x][z] << 16), p.scale * c.y * __uint_as_float(o[x][z] & 0xffff0000u), hi[z], lo[z]);
+      }
+#pragma unroll
+      for (int y = 0; y < DK / 16; ++y) {
+        ldsm_t(bh, q_mk + x * 16 * ROW + y * 32);
+        mma16(G[2 * y], hi, bh[0], bh[1]);
+        mma16(G[2 * y + 1], hi, bh[2], bh[3]);
+        mma16(G[2 * y], lo, bh[0], bh[1]);
+        mma16(G[2 * y + 1], lo, bh[2], bh[3]);
       }
     }
     put_labels<true>(R, st + V_AT + warp * 32, VROW, lane, gp.drs + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
@@ -199,11 +203,10 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
         mma16(G[2 * y + 1], lo, b[2], b[3]);
       }
     }
-    const DeltaChunk at = p.chunks[chunk];
-    __nv_bfloat16* out = gp.dv + (at.row0 * p.hv + h) * p.dv + col0 + warp * 16;
+    __nv_bfloat16* out = gp.dv + ((span.row0 + (long long)(n - 1 - i) * DC) * p.hv + h) * p.dv + col0 + warp * 16;
     const int cols = min(16, p.dv - col0 - warp * 16);
-    if (gp.vec_dv) put_labels<true>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, at.len, cols);
-    else put_labels<false>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, at.len, cols);
+    if (gp.vec_dv) put_labels<true>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, span.len(n - 1 - i), cols);
+    else put_labels<false>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, span.len(n - 1 - i), cols);
     __syncwarp();
     if (lane == 0) arrive(&empty[s]);
   }
