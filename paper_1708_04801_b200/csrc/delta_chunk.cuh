@@ -18,6 +18,8 @@
 // two products, T R and P U three. The answers, which leave as bf16, take S as one bf16 part (1e-3 of them; one part of P would be 2.5e-3).
 #pragma once
 
+#include <cuda.h>
+
 #include "async.cuh"
 #include "common.cuh"
 #include "delta_rows.cuh"
@@ -73,6 +75,7 @@ struct DeltaChunkParams {
   __nv_bfloat16* out;
   long long ld_out;
   int vec_out, slices;
+  int maps;  // whole chunks come by tensor maps
   long long spin_limit, drop;
   DevStatus* status;
 };
@@ -112,6 +115,13 @@ __device__ __forceinline__ void a_parts(const float (&x)[4], const float (&y)[4]
   split2(y[0], y[1], hi[2], lo[2]);
   split2(y[2], y[3], hi[3], lo[3]);
 }
+// Features and queries of a chunk in shared memory: 64 columns to a tile, rows of 128 bytes whose 16-byte units are exchanged as a tensor map's 128-byte swizzle does, unit u of row r
+// at u ^ (r & 7). wide_nk and wide_mk: a lane's offset for the 16 x 16 elements at (0, 0), as lane_nk and lane_mk; those at row 16 i and column 16 j are at wide(offset, i, j).
+constexpr int WIDE_BYTES = DC * 128;
+__device__ __forceinline__ uint32_t wide_unit(int row, int unit) { return row * 128 + ((unit ^ (row & 7)) << 4); }
+__device__ __forceinline__ uint32_t wide_nk(int lane) { return wide_unit((lane & 7) + ((lane >> 4) & 1) * 8, (lane >> 3) & 1); }
+__device__ __forceinline__ uint32_t wide_mk(int lane) { return wide_unit((lane & 7) + ((lane >> 3) & 1) * 8, (lane >> 4) & 1); }
+__device__ __forceinline__ uint32_t wide(uint32_t offset, int i, int j) { return (offset ^ (j % 4 << 5)) + i * 2048 + j / 4 * WIDE_BYTES; }
 // Byte offset of a lane's row for 16 x 16 elements at (0, 0) of a tile with `stride` elements a row. lane_nk: B operand of [n][k] (plain), A operand of [k][m]
 // (transposed); lane_mk: A operand of [m][k] (plain), B operand of [k][n] (transposed).
 __device__ __forceinline__ uint32_t lane_nk(int lane, int stride) { return (((lane & 7) + ((lane >> 4) & 1) * 8) * stride + ((lane >> 3) & 1) * 8) * 2; }
@@ -444,63 +454,99 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
 // only copy. Three stages where they fit: a warp may be a chunk ahead of the slowest.
 template <int DK, int NW>
 struct ChainShape {
-  static constexpr int row = DK + 8, vrow = 16 * NW + 8;
-  static constexpr int q_at = DC * row * 2, v_at = 2 * q_at, block_at = v_at + DC * vrow * 2, stage = block_at + DC_BLOCK;
-  static constexpr int stages = 3 * stage <= 226 * 1024 ? 3 : 2;
-  static constexpr int smem = stages * stage;
+  static constexpr int vrow = 16 * NW + 8;  // elements
+  static constexpr int q_at = DK / 64 * WIDE_BYTES, v_at = 2 * q_at, block_at = v_at + DC * vrow * 2, stage = (block_at + DC_BLOCK + 1023) / 1024 * 1024;
+  static constexpr int stages = 3 * stage <= 225 * 1024 ? 3 : 2;
+  static constexpr int smem = stages * stage + 1024;  // tiles start on 1024 bytes
   static constexpr int copiers = NW < 8 ? 4 : 0, threads = 32 * (NW + copiers);
 };
 
-// A warp's share of 64 rows of a tile, `UNITS` units of 16 bytes a row; zeros behind the chunk's end and from column `width` on. (A bulk copy for each row takes 64
-// cycles to issue, whatever its size: 0.8 ms for 16384 chunks of 128 features and labels.)
-template <int UNITS>
-__device__ __forceinline__ void copy_rows(uint32_t to, int stride, const __nv_bfloat16* from, long long ld, int len, int width, int warp, int warps, int lane) {
+// A warp's share of 64 rows of a tile, `UNITS` units of 16 bytes a row, unit u of row r at place(r, u); zeros behind the chunk's end and from column `width` on. (A bulk copy for each row
+// takes 64 cycles to issue, whatever its size: 0.8 ms for 16384 chunks of 128 features and labels.)
+template <int UNITS, typename Place>
+__device__ __forceinline__ void copy_rows(Place place, const __nv_bfloat16* from, long long ld, int len, int width, int warp, int warps, int lane) {
   constexpr int per = 32 / UNITS;  // rows at a time
   static_assert(UNITS <= 32 && 32 % UNITS == 0, "a warp has whole rows");
-  const int col = lane % UNITS * 8;
+  const int unit = lane % UNITS;
 #pragma unroll 4
   for (int r = warp * per + lane / UNITS; r < DC; r += warps * per) {
-    const bool there = col < width && r < len;
-    copy16(to + r * stride + col * 2, from + (there ? r * ld + col : 0), there);
+    const bool there = unit * 8 < width && r < len;
+    copy16(place(r, unit), from + (there ? r * ld + unit * 8 : 0), there);
   }
 }
+// 64 rows and 64 columns from (x, y) of the rows that a tensor map describes
+__device__ __forceinline__ void tma_tile(uint32_t to, const CUtensorMap* map, int x, int y, unsigned long long* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(smem32(bar)) : "memory");
+}
+__device__ __forceinline__ void bulk_block(uint32_t to, const void* from, uint32_t bytes, unsigned long long* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(smem32(bar)) : "memory");
+}
+
 // Rows of a chain, and of its chunk i. (Looked up in the list of chunks by each warp, they would be waited for twice a chunk: 1400 of 12000 cycles.)
 struct DeltaSpan {
   long long row0, rows;
   __device__ __forceinline__ int len(int i) const { return (int)min((long long)DC, rows - (long long)i * DC); }
 };
-// A warp's share of a chunk: features, queries, labels (or their gradients) and the block of the first kernel. The barrier takes an arrival of every thread.
+// Tensor maps of the rows of all heads of features and queries: whole chunks come by them where a head has all the features of its tiles. (All of a chunk by 16-byte copies of the warps
+// cost 200 of 850 us for 65536 rows of 16 heads: they share the way to shared memory with the operands.)
+struct DeltaMaps {
+  CUtensorMap k, q;
+};
+// The barriers of a stage: `rows` takes an arrival of every thread that brings, `bulk` one and the bytes of what one thread asks for
+struct ChunkBarriers {
+  unsigned long long rows, bulk, empty;
+};
+// A warp's share of a chunk: features, queries, labels (or their gradients) and the block of the first kernel.
 template <int DK, int NW>
-__device__ __forceinline__ void bring_chunk(const DeltaChunkParams& p, const DeltaHeads& labels, uint32_t st, int chunk, const DeltaSpan& span, int i, int h, int kh, int col0, int warp, int warps, int lane, unsigned long long* full) {
+__device__ __forceinline__ void bring_chunk(const DeltaChunkParams& p, const DeltaMaps& maps, const DeltaHeads& labels, uint32_t st, int chunk, const DeltaSpan& span, int i, int h, int kh, int col0,
+                                            int warp, int warps, int lane, ChunkBarriers* bars) {
   using Shape = ChainShape<DK, NW>;
-  const struct {
-    long long row0;
-    int len;
-  } at = {span.row0 + (long long)i * DC, span.len(i)};
-  copy_rows<DK / 8>(st, Shape::row * 2, p.k.p + at.row0 * p.k.ld + kh * p.k.width, p.k.ld, at.len, p.k.width, warp, warps, lane);
-  copy_rows<DK / 8>(st + Shape::q_at, Shape::row * 2, p.q.p + at.row0 * p.q.ld + kh * p.q.width, p.q.ld, at.len, p.q.width, warp, warps, lane);
-  copy_rows<2 * NW>(st + Shape::v_at, Shape::vrow * 2, labels.p + at.row0 * labels.ld + h * labels.width + col0, labels.ld, at.len, labels.width - col0, warp, warps, lane);
-  const unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK;
-#pragma unroll 4
-  for (int i = (warp * 32 + lane) * 16; i < DC_BLOCK; i += warps * 512) copy16(st + Shape::block_at + i, block + i, true);
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem32(full)) : "memory");
+  const long long row0 = span.row0 + (long long)i * DC;
+  const int len = span.len(i);
+  const bool whole = p.maps && len == DC;
+  if (warp == 0 && elect_one()) {
+    mbar_arrive_expect_tx(&bars->bulk, DC_BLOCK + (whole ? 2 * Shape::q_at : 0));
+    if (whole)
+#pragma unroll
+      for (int j = 0; j < DK / 64; ++j) {
+        tma_tile(st + j * WIDE_BYTES, &maps.k, kh * DK + j * 64, (int)row0, &bars->bulk);
+        tma_tile(st + Shape::q_at + j * WIDE_BYTES, &maps.q, kh * DK + j * 64, (int)row0, &bars->bulk);
+      }
+    bulk_block(st + Shape::block_at, p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK, DC_BLOCK, &bars->bulk);
+  }
+  if (!whole) {
+    auto place = [&](int r, int u) { return st + wide_unit(r, u & 7) + u / 8 * WIDE_BYTES; };
+    copy_rows<DK / 8>(place, p.k.p + row0 * p.k.ld + kh * p.k.width, p.k.ld, len, p.k.width, warp, warps, lane);
+    copy_rows<DK / 8>([&](int r, int u) { return place(r, u) + Shape::q_at; }, p.q.p + row0 * p.q.ld + kh * p.q.width, p.q.ld, len, p.q.width, warp, warps, lane);
+  }
+  copy_rows<2 * NW>([&](int r, int u) { return st + Shape::v_at + (r * Shape::vrow + u * 8) * 2; }, labels.p + row0 * labels.ld + h * labels.width + col0, labels.ld, len, labels.width - col0, warp,
+                    warps, lane);
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem32(&bars->rows)) : "memory");
+}
+// What the warp that asks for bulk copies does when it gives up: chunks `from` to `to` - 1 are in flight
+template <int STAGES>
+__device__ __forceinline__ void bulk_done(ChunkBarriers* bars, int from, int to) {
+  for (int i = from; i < to; ++i) mbar_wait_bounded(&bars[i % STAGES].bulk, (i / STAGES) & 1, DRAIN_LIMIT);
 }
 // A copying warp's work: its share of all n chunks, the last first where `back`
 template <int DK, int NW>
-__device__ __forceinline__ void bring_chunks(const DeltaChunkParams& p, const DeltaHeads& labels, uint32_t smem, int first, bool back, int n, const DeltaSpan& span, int h, int kh, int col0, int warp, int lane,
-                                             unsigned long long* full, unsigned long long* empty) {
+__device__ __forceinline__ void bring_chunks(const DeltaChunkParams& p, const DeltaMaps& maps, const DeltaHeads& labels, uint32_t smem, int first, bool back, int n, const DeltaSpan& span, int h,
+                                             int kh, int col0, int warp, int lane, ChunkBarriers* bars) {
   using Shape = ChainShape<DK, NW>;
+  int brought = 0;
   for (int i = 0; i < n; ++i) {
     const int s = i % Shape::stages;
-    if (i >= Shape::stages && !__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], (i / Shape::stages - 1) & 1, p.spin_limit))) {
+    if (i >= Shape::stages && !__all_sync(0xffffffffu, mbar_wait_bounded(&bars[s].empty, (i / Shape::stages - 1) & 1, p.spin_limit))) {
       if (lane == 0) set_status(p.status, DEV_TIMEOUT, 27, i);
       break;
     }
     if (i == p.drop) break;  // a test hook: this chunk and those behind it are never brought
     const int j = back ? n - 1 - i : i;
-    bring_chunk<DK, NW>(p, labels, smem + s * Shape::stage, first + j, span, j, h, kh, col0, warp, Shape::copiers, lane, &full[s]);
+    bring_chunk<DK, NW>(p, maps, labels, smem + s * Shape::stage, first + j, span, j, h, kh, col0, warp, Shape::copiers, lane, &bars[s]);
+    brought = i + 1;
   }
   copies_done();
+  if (warp == 0) bulk_done<Shape::stages>(bars, max(0, brought - Shape::stages), brought);  // nothing is in flight when the block ends
 }
 __device__ __forceinline__ void arrive(unsigned long long* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem32(bar)) : "memory"); }
 
@@ -530,34 +576,39 @@ __device__ __forceinline__ void put_labels(const float (&x)[8][4], unsigned char
 }
 
 template <int DK, int NW, bool SAVE>
-__global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kernel(const __grid_constant__ DeltaChunkParams p) {
+__global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kernel(const __grid_constant__ DeltaChunkParams p, const __grid_constant__ DeltaMaps maps) {
   using Shape = ChainShape<DK, NW>;
-  constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages, Q_AT = Shape::q_at, V_AT = Shape::v_at;  // bytes
-  extern __shared__ __align__(16) unsigned char chain_smem[];
-  __shared__ unsigned long long full[STAGES], empty[STAGES];
+  constexpr int VROW = Shape::vrow * 2, STAGES = Shape::stages;  // bytes
+  constexpr bool COPIERS = Shape::copiers > 0;
+  extern __shared__ unsigned char chain_smem[];
+  __shared__ ChunkBarriers bars[STAGES];
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
+  unsigned char* const ring = chain_smem + (-smem32(chain_smem) & 1023u);
   kernel_started();
   kernel_inputs_ready();
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
   const DeltaSpan span = {p.shard_off[chain], p.shard_off[chain + 1] - p.shard_off[chain]};
-  constexpr bool COPIERS = Shape::copiers > 0;
-  const int bringers = COPIERS ? Shape::copiers : warps;
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full[s], 32 * bringers);
-      mbar_init(&empty[s], warps);
+      mbar_init(&bars[s].rows, 32 * (COPIERS ? Shape::copiers : warps));
+      mbar_init(&bars[s].bulk, 1);
+      mbar_init(&bars[s].empty, warps);
     }
     mbar_fence_init();
   }
   __syncthreads();
   if (COPIERS && warp >= NW) {
-    bring_chunks<DK, NW>(p, p.v, smem32(chain_smem), first, false, n, span, h, kh, col0, warp - NW, lane, full, empty);
+    bring_chunks<DK, NW>(p, maps, p.v, smem32(ring), first, false, n, span, h, kh, col0, warp - NW, lane, bars);
     return;
   }
   if (warp >= warps) return;
-  if (!COPIERS && n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem), first, span, 0, h, kh, col0, warp, warps, lane, &full[0]);
+  int brought = 0;
+  if (!COPIERS && n > 0 && p.drop != 0) {
+    bring_chunk<DK, NW>(p, maps, p.v, smem32(ring), first, span, 0, h, kh, col0, warp, warps, lane, &bars[0]);
+    brought = 1;
+  }
 
   // S^T: labels g and g + 8 of the warp's 16, features 8 n + 2 t and the next
   float S[DK / 8][4];
@@ -575,20 +626,25 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
     const int s = i % STAGES, s1 = (i + 1) % STAGES;
     bool ok = true;
     if (!COPIERS && i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
-      if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s1], ((i + 1) / STAGES - 1) & 1, p.spin_limit));
-      if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.v, smem32(chain_smem) + s1 * Shape::stage, first + i + 1, span, i + 1, h, kh, col0, warp, warps, lane, &full[s1]);
+      if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars[s1].empty, ((i + 1) / STAGES - 1) & 1, p.spin_limit));
+      if (ok && i + 1 != p.drop) {
+        bring_chunk<DK, NW>(p, maps, p.v, smem32(ring) + s1 * Shape::stage, first + i + 1, span, i + 1, h, kh, col0, warp, warps, lane, &bars[s1]);
+        brought = i + 2;
+      }
     }
-    if (!ok || !__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (i / STAGES) & 1, p.spin_limit))) {
+    ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&bars[s].bulk, (i / STAGES) & 1, p.spin_limit));
+    if (!ok || !__all_sync(0xffffffffu, mbar_wait_bounded(&bars[s].rows, (i / STAGES) & 1, p.spin_limit))) {
       if (lane == 0) set_status(p.status, DEV_TIMEOUT, 25, i);
-      copies_done();  // none of this warp's is in flight when it leaves
+      copies_done();  // nothing of this warp's is in flight when it leaves
+      if (!COPIERS && warp == 0) bulk_done<STAGES>(bars, max(0, brought - STAGES), brought);
       return;
     }
-    unsigned char* st = chain_smem + s * Shape::stage;
+    unsigned char* st = ring + s * Shape::stage;
     const unsigned char* block = st + Shape::block_at;
     const DeltaFactors* f = (const DeltaFactors*)(block + DC_FACTORS);
     const long long which = (long long)(first + i) * p.hv + h;
-    const uint32_t k_nk = smem32(st) + lane_nk(lane, Shape::row), q_nk = k_nk + Q_AT, k_mk = smem32(st) + lane_mk(lane, Shape::row);
-    const uint32_t t_nk = smem32(block) + tri_nk(lane), v_nk = smem32(st + V_AT) + warp * 32 + lane_nk(lane, Shape::vrow);
+    const uint32_t k_at = smem32(st), q_at = k_at + Shape::q_at, nk = wide_nk(lane), mk = wide_mk(lane);
+    const uint32_t t_nk = smem32(block) + tri_nk(lane), v_nk = smem32(st + Shape::v_at) + warp * 32 + lane_nk(lane, Shape::vrow);
 
     // S^T K^T
     float R[8][4];
@@ -608,7 +664,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
         to[4 * DK + 4] = hi[3];
       }
 #pragma unroll
-      for (int y = 0; y < 4; ++y) ldsm(b[y], k_nk + y * 16 * ROW + x * 32);
+      for (int y = 0; y < 4; ++y) ldsm(b[y], k_at + wide(nk, y, x));
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
         mma16(R[2 * y], hi, b[y][0], b[y][1]);
@@ -657,13 +713,13 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
         const uint32_t a[4] = {pack2(S[2 * z][0], S[2 * z][1]), pack2(S[2 * z][2], S[2 * z][3]), pack2(S[2 * z + 1][0], S[2 * z + 1][1]), pack2(S[2 * z + 1][2], S[2 * z + 1][3])};
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-          ldsm(bh, q_nk + y * 16 * ROW + z * 32);
+          ldsm(bh, q_at + wide(nk, y, z));
           mma16(O[2 * y], a, bh[0], bh[1]);
           mma16(O[2 * y + 1], a, bh[2], bh[3]);
         }
       }
     }
-    if (SAVE) put_labels<true>(U, st + V_AT + warp * 32, VROW, lane, p.steps + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
+    if (SAVE) put_labels<true>(U, st + Shape::v_at + warp * 32, VROW, lane, p.steps + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
     // O^T = scale c S^T Q^T + U^T P^T, and S^T <- e^{b_C} S^T + (r U)^T K
     const uint64_t last = pair_of(__float_as_uint(f->last), __float_as_uint(f->last));
 #pragma unroll
@@ -697,7 +753,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
       a_parts(U[2 * x], U[2 * x + 1], hi, lo);
 #pragma unroll
       for (int y = 0; y < DK / 16; ++y) {
-        ldsm_t(bh, k_mk + x * 16 * ROW + y * 32);
+        ldsm_t(bh, k_at + wide(mk, x, y));
         mma16(S[2 * y], hi, bh[0], bh[1]);
         mma16(S[2 * y + 1], hi, bh[2], bh[3]);
         mma16(S[2 * y], lo, bh[0], bh[1]);
@@ -706,10 +762,11 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
     }
     __nv_bfloat16* out = p.out + (span.row0 + (long long)i * DC) * p.ld_out + h * p.dv + col0 + warp * 16;
     const int cols = min(16, p.dv - col0 - warp * 16);
-    if (p.vec_out) put_labels<true>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, span.len(i), cols);
-    else put_labels<false>(O, st + V_AT + warp * 32, VROW, lane, out, p.ld_out, span.len(i), cols);
+    if (p.vec_out) put_labels<true>(O, st + Shape::v_at + warp * 32, VROW, lane, out, p.ld_out, span.len(i), cols);
+    else put_labels<false>(O, st + Shape::v_at + warp * 32, VROW, lane, out, p.ld_out, span.len(i), cols);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // a stage's rows may have come by copies of threads, and come by the tensor map next
     __syncwarp();
-    if (lane == 0) arrive(&empty[s]);
+    if (lane == 0) arrive(&bars[s].empty);
   }
   if (p.W)
 #pragma unroll

@@ -32,35 +32,40 @@ struct DeltaGradParams {
 };
 
 template <int DK, int NW>
-__global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel(const __grid_constant__ DeltaGradParams gp) {
+__global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel(const __grid_constant__ DeltaGradParams gp, const __grid_constant__ DeltaMaps maps) {
   const DeltaChunkParams& p = gp.f;
   using Shape = ChainShape<DK, NW>;
-  constexpr int ROW = Shape::row * 2, VROW = Shape::vrow * 2, STAGES = Shape::stages, Q_AT = Shape::q_at, V_AT = Shape::v_at;  // bytes
-  extern __shared__ __align__(16) unsigned char chain_smem[];
-  __shared__ unsigned long long full[STAGES], empty[STAGES];
+  constexpr int VROW = Shape::vrow * 2, STAGES = Shape::stages;  // bytes
+  constexpr bool COPIERS = Shape::copiers > 0;
+  extern __shared__ unsigned char chain_smem[];
+  __shared__ ChunkBarriers bars[STAGES];
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
+  unsigned char* const ring = chain_smem + (-smem32(chain_smem) & 1023u);
   kernel_started();
   kernel_inputs_ready();
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
   const DeltaSpan span = {p.shard_off[chain], p.shard_off[chain + 1] - p.shard_off[chain]};
-  constexpr bool COPIERS = Shape::copiers > 0;
-  const int bringers = COPIERS ? Shape::copiers : warps;
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full[s], 32 * bringers);
-      mbar_init(&empty[s], warps);
+      mbar_init(&bars[s].rows, 32 * (COPIERS ? Shape::copiers : warps));
+      mbar_init(&bars[s].bulk, 1);
+      mbar_init(&bars[s].empty, warps);
     }
     mbar_fence_init();
   }
   __syncthreads();
   if (COPIERS && warp >= NW) {
-    bring_chunks<DK, NW>(p, p.dout, smem32(chain_smem), first, true, n, span, h, kh, col0, warp - NW, lane, full, empty);
+    bring_chunks<DK, NW>(p, maps, p.dout, smem32(ring), first, true, n, span, h, kh, col0, warp - NW, lane, bars);
     return;
   }
   if (warp >= warps) return;
-  if (!COPIERS && n > 0 && p.drop != 0) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem), first + n - 1, span, n - 1, h, kh, col0, warp, warps, lane, &full[0]);
+  int brought = 0;
+  if (!COPIERS && n > 0 && p.drop != 0) {
+    bring_chunk<DK, NW>(p, maps, p.dout, smem32(ring), first + n - 1, span, n - 1, h, kh, col0, warp, warps, lane, &bars[0]);
+    brought = 1;
+  }
 
   float G[DK / 8][4];  // G^T, as S^T in the forward walk
   const int label = col0 + warp * 16 + g;
@@ -77,21 +82,26 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
     const int s = i % STAGES, s1 = (i + 1) % STAGES;
     bool ok = true;
     if (!COPIERS && i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
-      if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[s1], ((i + 1) / STAGES - 1) & 1, p.spin_limit));
-      if (ok && i + 1 != p.drop) bring_chunk<DK, NW>(p, p.dout, smem32(chain_smem) + s1 * Shape::stage, first + n - 2 - i, span, n - 2 - i, h, kh, col0, warp, warps, lane, &full[s1]);
+      if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars[s1].empty, ((i + 1) / STAGES - 1) & 1, p.spin_limit));
+      if (ok && i + 1 != p.drop) {
+        bring_chunk<DK, NW>(p, maps, p.dout, smem32(ring) + s1 * Shape::stage, first + n - 2 - i, span, n - 2 - i, h, kh, col0, warp, warps, lane, &bars[s1]);
+        brought = i + 2;
+      }
     }
-    if (!ok || !__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], (i / STAGES) & 1, p.spin_limit))) {
+    ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&bars[s].bulk, (i / STAGES) & 1, p.spin_limit));
+    if (!ok || !__all_sync(0xffffffffu, mbar_wait_bounded(&bars[s].rows, (i / STAGES) & 1, p.spin_limit))) {
       if (lane == 0) set_status(p.status, DEV_TIMEOUT, 26, i);
-      copies_done();  // none of this warp's is in flight when it leaves
+      copies_done();  // nothing of this warp's is in flight when it leaves
+      if (!COPIERS && warp == 0) bulk_done<STAGES>(bars, max(0, brought - STAGES), brought);
       return;
     }
-    unsigned char* st = chain_smem + s * Shape::stage;
+    unsigned char* st = ring + s * Shape::stage;
     const unsigned char* block = st + Shape::block_at;
     const DeltaFactors* f = (const DeltaFactors*)(block + DC_FACTORS);
     const int chunk = first + n - 1 - i;
     const long long which = (long long)chunk * p.hv + h;
-    const uint32_t k_nk = smem32(st) + lane_nk(lane, Shape::row), k_mk = smem32(st) + lane_mk(lane, Shape::row), q_mk = k_mk + Q_AT;
-    const uint32_t t_mk = smem32(block) + tri_mk(lane), v_nk = smem32(st + V_AT) + warp * 32 + lane_nk(lane, Shape::vrow);
+    const uint32_t k_at = smem32(st), q_at = k_at + Shape::q_at, nk = wide_nk(lane), mk = wide_mk(lane);
+    const uint32_t t_mk = smem32(block) + tri_mk(lane), v_nk = smem32(st + Shape::v_at) + warp * 32 + lane_nk(lane, Shape::vrow);
 
     // dU^T = r G^T K^T + O'^T P
     float M[8][4];
@@ -109,7 +119,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
       to[4] = hi[2];
       to[4 * DK + 4] = hi[3];
 #pragma unroll
-      for (int y = 0; y < 4; ++y) ldsm(b[y], k_nk + y * 16 * ROW + x * 32);
+      for (int y = 0; y < 4; ++y) ldsm(b[y], k_at + wide(nk, y, x));
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
         mma16(M[2 * y], hi, b[y][0], b[y][1]);
@@ -172,14 +182,14 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
       }
 #pragma unroll
       for (int y = 0; y < DK / 16; ++y) {
-        ldsm_t(bh, q_mk + x * 16 * ROW + y * 32);
+        ldsm_t(bh, q_at + wide(mk, x, y));
         mma16(G[2 * y], hi, bh[0], bh[1]);
         mma16(G[2 * y + 1], hi, bh[2], bh[3]);
         mma16(G[2 * y], lo, bh[0], bh[1]);
         mma16(G[2 * y + 1], lo, bh[2], bh[3]);
       }
     }
-    put_labels<true>(R, st + V_AT + warp * 32, VROW, lane, gp.drs + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
+    put_labels<true>(R, st + Shape::v_at + warp * 32, VROW, lane, gp.drs + which * DC * p.dvp + col0 + warp * 16, p.dvp, DC, 16);
     // G^T -= (beta c dR)^T K
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -196,7 +206,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
       a_parts(y0, y1, hi, lo);
 #pragma unroll
       for (int y = 0; y < DK / 16; ++y) {
-        ldsm_t(b, k_mk + x * 16 * ROW + y * 32);
+        ldsm_t(b, k_at + wide(mk, x, y));
         mma16(G[2 * y], hi, b[0], b[1]);
         mma16(G[2 * y + 1], hi, b[2], b[3]);
         mma16(G[2 * y], lo, b[0], b[1]);
@@ -205,10 +215,11 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
     }
     __nv_bfloat16* out = gp.dv + ((span.row0 + (long long)(n - 1 - i) * DC) * p.hv + h) * p.dv + col0 + warp * 16;
     const int cols = min(16, p.dv - col0 - warp * 16);
-    if (gp.vec_dv) put_labels<true>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, span.len(n - 1 - i), cols);
-    else put_labels<false>(R, st + V_AT + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, span.len(n - 1 - i), cols);
+    if (gp.vec_dv) put_labels<true>(R, st + Shape::v_at + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, span.len(n - 1 - i), cols);
+    else put_labels<false>(R, st + Shape::v_at + warp * 32, VROW, lane, out, (long long)p.hv * p.dv, span.len(n - 1 - i), cols);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
-    if (lane == 0) arrive(&empty[s]);
+    if (lane == 0) arrive(&bars[s].empty);
   }
   if (gp.dW0)
 #pragma unroll

@@ -2,6 +2,8 @@
 // clusters, checks of memory that must not overlap.
 #pragma once
 
+#include <cuda.h>
+
 #include <atomic>
 
 #include "context.cuh"
@@ -40,6 +42,19 @@ cudaError_t launch_clusters(void (*kern)(P...), dim3 grid, dim3 block, size_t sm
   return cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
 }
 
+// The driver's encoder of tensor maps, asked for by name: the library does not link against the driver.
+inline decltype(&cuTensorMapEncodeTiled) tensor_map_encoder() {
+  static const auto fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      f = nullptr;
+    }
+    return (decltype(&cuTensorMapEncodeTiled))f;
+  }();
+  return fn;
+}
 inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }

@@ -149,6 +149,18 @@ wpsgd_status pack_heads(wpsgd_ctx* c, const void* from, long long ld, int heads,
   return WPSGD_OK;
 }
 
+// Tensor maps of features and queries for the walks, 64 rows by 64 columns at a time; false: whole heads do not fill such tiles, or sizes that a map cannot describe
+bool encode_maps(DeltaMaps* maps, const DeltaChunkParams& p) {
+  if ((p.k.width != 64 && p.k.width != 128) || p.n_rows < DC || !tensor_map_encoder()) return false;
+  auto encode = [&](CUtensorMap* map, const DeltaHeads& h) {
+    const cuuint64_t dims[2] = {(cuuint64_t)h.heads * h.width, (cuuint64_t)p.n_rows}, strides[1] = {(cuuint64_t)h.ld * 2};
+    const cuuint32_t box[2] = {64, DC}, steps[2] = {1, 1};
+    return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (void*)h.p, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  return encode(&maps->k, p.k) && encode(&maps->q, p.q);
+}
+
 // Warps (of 16 labels) of a block that walks a chain: as many as leave every SM a block, so that few blocks bring the same rows
 int chain_warps(long long heads, int dvp) {
   int w = 8;
@@ -157,15 +169,15 @@ int chain_warps(long long heads, int dvp) {
 }
 
 template <int DK, int NW>
-wpsgd_status walk(wpsgd_ctx* c, const DeltaChunkParams& p, bool save) {
+wpsgd_status walk(wpsgd_ctx* c, const DeltaChunkParams& p, const DeltaMaps& maps, bool save) {
   using Shape = ChainShape<DK, NW>;
   const unsigned grid = (unsigned)((long long)p.n_chains * p.hv * p.slices);
   if (save) {
     CU_TRY(c, (allow_smem<delta_chain_kernel<DK, NW, true>>(c)));
-    CU_TRY(c, launch(delta_chain_kernel<DK, NW, true>, grid, Shape::threads, Shape::smem, c->stream, p));
+    CU_TRY(c, launch(delta_chain_kernel<DK, NW, true>, grid, Shape::threads, Shape::smem, c->stream, p, maps));
   } else {
     CU_TRY(c, (allow_smem<delta_chain_kernel<DK, NW, false>>(c)));
-    CU_TRY(c, launch(delta_chain_kernel<DK, NW, false>, grid, Shape::threads, Shape::smem, c->stream, p));
+    CU_TRY(c, launch(delta_chain_kernel<DK, NW, false>, grid, Shape::threads, Shape::smem, c->stream, p, maps));
   }
   c->launches++;
   return WPSGD_OK;
@@ -182,7 +194,9 @@ wpsgd_status run_chunks(wpsgd_ctx* c, DeltaChunkParams p, const DeltaLayout& lay
   }
   const int w = chain_warps((long long)p.n_chains * p.hv, p.dvp);
   p.slices = (p.dvp / 16 + w - 1) / w;
-  return w == 8 ? walk<DK, 8>(c, p, save) : w == 4 ? walk<DK, 4>(c, p, save) : w == 2 ? walk<DK, 2>(c, p, save) : walk<DK, 1>(c, p, save);
+  DeltaMaps maps = {};
+  p.maps = encode_maps(&maps, p);
+  return w == 8 ? walk<DK, 8>(c, p, maps, save) : w == 4 ? walk<DK, 4>(c, p, maps, save) : w == 2 ? walk<DK, 2>(c, p, maps, save) : walk<DK, 1>(c, p, maps, save);
 }
 
 // Blocks that go through the chunks' rows: one per SM
@@ -204,10 +218,10 @@ struct DeltaGradLayout {
 };
 
 template <int DK, int NW>
-wpsgd_status walk_back(wpsgd_ctx* c, const DeltaGradParams& p) {
+wpsgd_status walk_back(wpsgd_ctx* c, const DeltaGradParams& p, const DeltaMaps& maps) {
   using Shape = ChainShape<DK, NW>;
   CU_TRY(c, (allow_smem<delta_back_kernel<DK, NW>>(c)));
-  CU_TRY(c, launch(delta_back_kernel<DK, NW>, (unsigned)((long long)p.f.n_chains * p.f.hv * p.f.slices), Shape::threads, Shape::smem, c->stream, p));
+  CU_TRY(c, launch(delta_back_kernel<DK, NW>, (unsigned)((long long)p.f.n_chains * p.f.hv * p.f.slices), Shape::threads, Shape::smem, c->stream, p, maps));
   c->launches++;
   return WPSGD_OK;
 }
@@ -216,7 +230,9 @@ template <int DK>
 wpsgd_status grad_chunks(wpsgd_ctx* c, DeltaGradParams p, const DeltaLayout& lay, int blocks) {
   const int w = chain_warps((long long)p.f.n_chains * p.f.hv, p.f.dvp);
   p.f.slices = (p.f.dvp / 16 + w - 1) / w;
-  const wpsgd_status s = w == 8 ? walk_back<DK, 8>(c, p) : w == 4 ? walk_back<DK, 4>(c, p) : w == 2 ? walk_back<DK, 2>(c, p) : walk_back<DK, 1>(c, p);
+  DeltaMaps maps = {};
+  p.f.maps = encode_maps(&maps, p.f);
+  const wpsgd_status s = w == 8 ? walk_back<DK, 8>(c, p, maps) : w == 4 ? walk_back<DK, 4>(c, p, maps) : w == 2 ? walk_back<DK, 2>(c, p, maps) : walk_back<DK, 1>(c, p, maps);
   if (s != WPSGD_OK || lay.chunks == 0) return s;
   CU_TRY(c, (allow_smem<delta_rowgrad_kernel<DK>>(c)));
   CU_TRY(c, launch(delta_rowgrad_kernel<DK>, (unsigned)blocks, ROWS_THREADS, RowsShape<DK>::smem, c->stream, p));

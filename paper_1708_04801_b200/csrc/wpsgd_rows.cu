@@ -78,19 +78,6 @@ struct MarginsCall {
   MarginsParams p;
 };
 
-// The driver's encoder of tensor maps, asked for by name: the library does not link against the driver.
-decltype(&cuTensorMapEncodeTiled) tensor_map_encoder() {
-  static const auto fn = [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
-      cudaGetLastError();
-      f = nullptr;
-    }
-    return (decltype(&cuTensorMapEncodeTiled))f;
-  }();
-  return fn;
-}
 // Boxes of 128 columns and `box_rows` rows of an 8-bit matrix; what lies outside it reads as zeros.
 bool encode_rows8(CUtensorMap* map, const uint8_t* base, long long d, long long rows, long long ld, int box_rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
