@@ -76,6 +76,7 @@ struct DeltaChunkParams {
   long long ld_out;
   int vec_out, slices;
   int maps;  // whole chunks come by tensor maps
+  int prep_heads;
   long long spin_limit, drop;
   DevStatus* status;
 };
@@ -223,11 +224,11 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool yes) 
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory"); }
 
 // ---- T, P and the factors of a chunk ----------------------------------------------------------------------------------------------------------
-// One block of four warps for each chunk and head. K K^T and Q K^T on the tensor cores, a warp with 16 rows and the columns up to them; then T by blocks: the four
+// One block of four warps for each chunk and head of labels, or the heads of labels that share features (`prep_heads` of them) where there are many. K K^T and Q K^T on the tensor cores, a warp with 16 rows and the columns up to them; then T by blocks: the four
 // diagonal blocks of 16 by substitution in fp32, a column to a lane, and what is below them by T_10 = -T_11 A_10 T_00, first for blocks of 16, then for
 // those of 32. These products are taken transposed, T_10^T = -(T_00^T A_10^T) T_11^T: the accumulator of the first is the A operand of the second, and
 // every factor is in two bf16 parts, three products each.
-constexpr int PREP_THREADS = 128;
+constexpr int PREP_THREADS = 128, PREP_HEADS = PREP_THREADS / 32;  // heads of labels of a block at most: a warp has the gates of each
 
 template <int DK>
 struct PrepShape {
@@ -265,11 +266,11 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
   __nv_bfloat16* Qs = Ks + DC * ROW;
   unsigned char* tris = prep_smem;  // over K and Q, once their products are done
   float* diag = (float*)(prep_smem + PrepShape<DK>::smem - PrepShape<DK>::diag);
-  __shared__ float bhi[DC], blo[DC], betas[DC];
+  __shared__ float bhis[PREP_HEADS][DC], blos[PREP_HEADS][DC], steps[PREP_HEADS][DC];
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
   kernel_started();
   kernel_inputs_ready();
-  const int chunk = blockIdx.x / p.hv, h = blockIdx.x % p.hv, kh = h / (p.hv / p.hk);
+  const int groups = p.hv / p.prep_heads, chunk = blockIdx.x / groups, h0 = blockIdx.x % groups * p.prep_heads, kh = h0 / (p.hv / p.hk);
   if (chunk >= p.chunk_off[p.n_chains]) return;
   const DeltaChunk at = p.chunks[chunk];
 
@@ -281,8 +282,8 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
     copy16(smem32(Ks + row * ROW + col), p.k.p + i * p.k.ld + c, there);
     copy16(smem32(Qs + row * ROW + col), p.q.p + i * p.q.ld + c, there);
   }
-  unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK;
-  if (warp == 0) {  // b by a scan over the lanes, two rows a lane, in 64 bits
+  if (warp < p.prep_heads) {  // b of a head by a scan over a warp's lanes, two rows a lane, in 64 bits
+    const int h = h0 + warp;
     double d[2];
     float beta[2];
 #pragma unroll
@@ -299,15 +300,15 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
       if (lane >= o) sum += v;
     }
     const double last = __shfl_sync(0xffffffffu, sum, 31);
-    DeltaFactors* f = (DeltaFactors*)(block + DC_FACTORS);
+    DeltaFactors* f = (DeltaFactors*)(p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK + DC_FACTORS);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int row = 2 * lane + i;
       const double b = i ? sum : sum - d[1], b2 = b * 1.4426950408889634;
       const float hi = (float)b2, lo = (float)(b2 - (double)hi);
-      bhi[row] = hi;
-      blo[row] = lo;
-      betas[row] = beta[i];
+      bhis[warp][row] = hi;
+      blos[warp][row] = lo;
+      steps[warp][row] = beta[i];
       f->c[row] = expf((float)b);
       f->r[row] = expf((float)(last - b));
       f->beta[row] = beta[i];
@@ -342,110 +343,114 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
       mma16(qk[n][1], aq, b[2], b[3]);
     }
   }
-  __syncthreads();
-  const float hi0 = bhi[warp * 16 + g], lo0 = blo[warp * 16 + g], hi1 = bhi[warp * 16 + g + 8], lo1 = blo[warp * 16 + g + 8], be0 = betas[warp * 16 + g], be1 = betas[warp * 16 + g + 8];
+  for (int h = h0; h < h0 + p.prep_heads; ++h) {
+    unsigned char* block = p.blocks + ((long long)chunk * p.hv + h) * DC_BLOCK;
+    const float *bhi = bhis[h - h0], *blo = blos[h - h0], *betas = steps[h - h0];
+    __syncthreads();  // also: K and Q, or the triangles of the head before, have been read
+    const float hi0 = bhi[warp * 16 + g], lo0 = blo[warp * 16 + g], hi1 = bhi[warp * 16 + g + 8], lo1 = blo[warp * 16 + g + 8], be0 = betas[warp * 16 + g], be1 = betas[warp * 16 + g + 8];
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    if (n > warp) break;
-    unsigned char* to = tris + (warp * (warp + 1) / 2 + n) * 512;
+    for (int n = 0; n < 4; ++n) {
+      if (n > warp) break;
+      unsigned char* to = tris + (warp * (warp + 1) / 2 + n) * 512;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int col = n * 16 + i * 8 + 2 * t;
-      const float2 ch = *(const float2*)(bhi + col), cl = *(const float2*)(blo + col);
+      for (int i = 0; i < 2; ++i) {
+        const int col = n * 16 + i * 8 + 2 * t;
+        const float2 ch = *(const float2*)(bhi + col), cl = *(const float2*)(blo + col);
 #pragma unroll
-      for (int e = 0; e < 4; e += 2) {
-        const int row = warp * 16 + g + 4 * e;
-        const float hi = e ? hi1 : hi0, lo = e ? lo1 : lo0, be = e ? be1 : be0;
-        float d0 = exp2_fast((hi - ch.x) + (lo - cl.x)), d1 = exp2_fast((hi - ch.y) + (lo - cl.y));
-        if (n == warp) {  // selected, not multiplied: above the diagonal the exponent is of the other sign
-          d0 = col <= row ? d0 : 0.0f;
-          d1 = col + 1 <= row ? d1 : 0.0f;
-        }
-        const int unit = tri_unit(g + 4 * e, i) + 4 * t;
-        uint32_t h2, l2;
-        split2(p.scale * d0 * qk[n][i][e], p.scale * d1 * qk[n][i][e + 1], h2, l2);
-        *(uint32_t*)(to + P_AT + unit) = h2;
-        *(uint32_t*)(to + P_AT + DC_TRI + unit) = l2;
-        const float k0 = d0 * kk[n][i][e], k1 = d1 * kk[n][i][e + 1], a0 = be * k0, a1 = be * k1;
-        if (p.gram) *(uint32_t*)(p.gram + ((long long)chunk * p.hv + h) * DC_TRI + (warp * (warp + 1) / 2 + n) * 512 + unit) = pack2(k0, k1);
-        if (n == warp) {
-          float* a = diag + (warp * 16 + g + 4 * e) * 17 + i * 8 + 2 * t;
-          a[0] = a0;  // the substitution reads below the diagonal only
-          a[1] = a1;
-        } else {
-          split2(a0, a1, h2, l2);
-          *(uint32_t*)(to + A_AT + unit) = h2;
-          *(uint32_t*)(to + A_AT + DC_TRI + unit) = l2;
+        for (int e = 0; e < 4; e += 2) {
+          const int row = warp * 16 + g + 4 * e;
+          const float hi = e ? hi1 : hi0, lo = e ? lo1 : lo0, be = e ? be1 : be0;
+          float d0 = exp2_fast((hi - ch.x) + (lo - cl.x)), d1 = exp2_fast((hi - ch.y) + (lo - cl.y));
+          if (n == warp) {  // selected, not multiplied: above the diagonal the exponent is of the other sign
+            d0 = col <= row ? d0 : 0.0f;
+            d1 = col + 1 <= row ? d1 : 0.0f;
+          }
+          const int unit = tri_unit(g + 4 * e, i) + 4 * t;
+          uint32_t h2, l2;
+          split2(p.scale * d0 * qk[n][i][e], p.scale * d1 * qk[n][i][e + 1], h2, l2);
+          *(uint32_t*)(to + P_AT + unit) = h2;
+          *(uint32_t*)(to + P_AT + DC_TRI + unit) = l2;
+          const float k0 = d0 * kk[n][i][e], k1 = d1 * kk[n][i][e + 1], a0 = be * k0, a1 = be * k1;
+          if (p.gram) *(uint32_t*)(p.gram + ((long long)chunk * p.hv + h) * DC_TRI + (warp * (warp + 1) / 2 + n) * 512 + unit) = pack2(k0, k1);
+          if (n == warp) {
+            float* a = diag + (warp * 16 + g + 4 * e) * 17 + i * 8 + 2 * t;
+            a[0] = a0;  // the substitution reads below the diagonal only
+            a[1] = a1;
+          } else {
+            split2(a0, a1, h2, l2);
+            *(uint32_t*)(to + A_AT + unit) = h2;
+            *(uint32_t*)(to + A_AT + DC_TRI + unit) = l2;
+          }
         }
       }
     }
-  }
-  __syncwarp();
-  if (lane < 16) {  // column `lane` of the warp's diagonal block
-    const float* a = diag + warp * 16 * 17;
-    unsigned char* to = tris + T_AT + (warp * (warp + 1) / 2 + warp) * 512;
-    float x[16];
+    __syncwarp();
+    if (lane < 16) {  // column `lane` of the warp's diagonal block
+      const float* a = diag + warp * 16 * 17;
+      unsigned char* to = tris + T_AT + (warp * (warp + 1) / 2 + warp) * 512;
+      float x[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float s = i == lane ? 1.0f : 0.0f;
+      for (int i = 0; i < 16; ++i) {
+        float s = i == lane ? 1.0f : 0.0f;
 #pragma unroll
-      for (int m = 0; m < i; ++m) s = fmaf(-a[i * 17 + m], x[m], s);
-      x[i] = s;
-      const __nv_bfloat16 hi = __float2bfloat16_rn(s);
-      const int unit = tri_unit(i, lane >> 3) + (lane & 7) * 2;
-      *(__nv_bfloat16*)(to + unit) = hi;
-      *(__nv_bfloat16*)(to + DC_T_LO + unit) = __float2bfloat16_rn(s - __bfloat162float(hi));
-    }
-  }
-  __syncthreads();
-  const uint32_t nk = smem32(tris) + tri_nk(lane);
-  if (warp & 1) {  // blocks (1, 0) and (3, 2)
-    const int o = warp - 1, d0 = (o * (o + 1) / 2 + o) * 512, d1 = (warp * (warp + 1) / 2 + warp) * 512, od = (warp * (warp + 1) / 2 + o) * 512;
-    float x[2][4] = {}, y[2][4] = {};
-    uint32_t ah[4], al[4], bh[4], bl[4];
-    ldsm_t(ah, nk + T_AT + d0);
-    ldsm_t(al, nk + T_AT + DC_T_LO + d0);
-    ldsm(bh, nk + A_AT + od);
-    ldsm(bl, nk + A_AT + DC_TRI + od);
-    mma_split(x[0], x[1], ah, al, bh, bl);
-    a_parts(x[0], x[1], ah, al);
-    ldsm(bh, nk + T_AT + d1);
-    ldsm(bl, nk + T_AT + DC_T_LO + d1);
-    mma_split(y[0], y[1], ah, al, bh, bl);
-    put_negative_t(nk + T_AT + od, y[0], y[1]);
-  }
-  __syncthreads();
-  {  // the block of 32: columns 16 j of it, rows 32 + 16 i
-    const int j = warp & 1, i = warp >> 1;
-    float x[4][4] = {}, y[2][4] = {};
-    uint32_t ah[4], al[4], bh[4], bl[4];
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {  // X^T = T_00^T A_10^T over rows of T_00 from its diagonal on
-      if (m < j) continue;
-      const int tt = (m * (m + 1) / 2 + j) * 512;
-      ldsm_t(ah, nk + T_AT + tt);
-      ldsm_t(al, nk + T_AT + DC_T_LO + tt);
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int aa = tri_at(2 + n, m);
-        ldsm(bh, nk + A_AT + aa);
-        ldsm(bl, nk + A_AT + DC_TRI + aa);
-        mma_split(x[2 * n], x[2 * n + 1], ah, al, bh, bl);
+        for (int m = 0; m < i; ++m) s = fmaf(-a[i * 17 + m], x[m], s);
+        x[i] = s;
+        const __nv_bfloat16 hi = __float2bfloat16_rn(s);
+        const int unit = tri_unit(i, lane >> 3) + (lane & 7) * 2;
+        *(__nv_bfloat16*)(to + unit) = hi;
+        *(__nv_bfloat16*)(to + DC_T_LO + unit) = __float2bfloat16_rn(s - __bfloat162float(hi));
       }
     }
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      if (m > i) continue;
-      const int tt = ((2 + i) * (3 + i) / 2 + 2 + m) * 512;
-      a_parts(x[2 * m], x[2 * m + 1], ah, al);
-      ldsm(bh, nk + T_AT + tt);
-      ldsm(bl, nk + T_AT + DC_T_LO + tt);
+    __syncthreads();
+    const uint32_t nk = smem32(tris) + tri_nk(lane);
+    if (warp & 1) {  // blocks (1, 0) and (3, 2)
+      const int o = warp - 1, d0 = (o * (o + 1) / 2 + o) * 512, d1 = (warp * (warp + 1) / 2 + warp) * 512, od = (warp * (warp + 1) / 2 + o) * 512;
+      float x[2][4] = {}, y[2][4] = {};
+      uint32_t ah[4], al[4], bh[4], bl[4];
+      ldsm_t(ah, nk + T_AT + d0);
+      ldsm_t(al, nk + T_AT + DC_T_LO + d0);
+      ldsm(bh, nk + A_AT + od);
+      ldsm(bl, nk + A_AT + DC_TRI + od);
+      mma_split(x[0], x[1], ah, al, bh, bl);
+      a_parts(x[0], x[1], ah, al);
+      ldsm(bh, nk + T_AT + d1);
+      ldsm(bl, nk + T_AT + DC_T_LO + d1);
       mma_split(y[0], y[1], ah, al, bh, bl);
+      put_negative_t(nk + T_AT + od, y[0], y[1]);
     }
-    put_negative_t(nk + T_AT + ((2 + i) * (3 + i) / 2 + j) * 512, y[0], y[1]);
+    __syncthreads();
+    {  // the block of 32: columns 16 j of it, rows 32 + 16 i
+      const int j = warp & 1, i = warp >> 1;
+      float x[4][4] = {}, y[2][4] = {};
+      uint32_t ah[4], al[4], bh[4], bl[4];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {  // X^T = T_00^T A_10^T over rows of T_00 from its diagonal on
+        if (m < j) continue;
+        const int tt = (m * (m + 1) / 2 + j) * 512;
+        ldsm_t(ah, nk + T_AT + tt);
+        ldsm_t(al, nk + T_AT + DC_T_LO + tt);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const int aa = tri_at(2 + n, m);
+          ldsm(bh, nk + A_AT + aa);
+          ldsm(bl, nk + A_AT + DC_TRI + aa);
+          mma_split(x[2 * n], x[2 * n + 1], ah, al, bh, bl);
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        if (m > i) continue;
+        const int tt = ((2 + i) * (3 + i) / 2 + 2 + m) * 512;
+        a_parts(x[2 * m], x[2 * m + 1], ah, al);
+        ldsm(bh, nk + T_AT + tt);
+        ldsm(bl, nk + T_AT + DC_T_LO + tt);
+        mma_split(y[0], y[1], ah, al, bh, bl);
+      }
+      put_negative_t(nk + T_AT + ((2 + i) * (3 + i) / 2 + j) * 512, y[0], y[1]);
+    }
+    __syncthreads();
+    for (int u = tid; u < 4 * DC_TRI / 16; u += PREP_THREADS) *(uint4*)(block + u * 16) = *(const uint4*)(tris + u * 16);
   }
-  __syncthreads();
-  for (int u = tid; u < 4 * DC_TRI / 16; u += PREP_THREADS) *(uint4*)(block + u * 16) = *(const uint4*)(tris + u * 16);
 }
 
 // ---- the walk over a chain's chunks ---------------------------------------------------------------------------------------------------------------

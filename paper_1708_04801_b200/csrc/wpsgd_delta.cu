@@ -189,7 +189,11 @@ wpsgd_status run_chunks(wpsgd_ctx* c, DeltaChunkParams p, const DeltaLayout& lay
   c->launches++;
   if (lay.chunks > 0) {
     CU_TRY(c, (allow_smem<delta_prepare_kernel<DK>>(c)));
-    CU_TRY(c, launch(delta_prepare_kernel<DK>, (unsigned)(lay.chunks * p.hv), PREP_THREADS, PrepShape<DK>::smem, c->stream, p));
+    // heads that share features by one block where that leaves every SM eight: their products of features are formed once
+    p.prep_heads = 1;
+    for (int n = 2; n <= PREP_HEADS && lay.chunks * p.hv / n >= 148 * 8; ++n)
+      if (p.hv / p.hk % n == 0) p.prep_heads = n;
+    CU_TRY(c, launch(delta_prepare_kernel<DK>, (unsigned)(lay.chunks * (p.hv / p.prep_heads)), PREP_THREADS, PrepShape<DK>::smem, c->stream, p));
     c->launches++;
   }
   const int w = chain_warps((long long)p.n_chains * p.hv, p.dvp);
