@@ -1,5 +1,6 @@
 // C ABI of the operators that lay rows out by node and bring them back (see include/wpsgd.h). Argument checks, choice of forms, launches.
 #include <algorithm>
+#include <type_traits>
 
 #include "nodes.cuh"
 #include "rows_host.cuh"
@@ -136,7 +137,16 @@ wpsgd_status wpsgd_combine_rows_grad(wpsgd_ctx* c, const void* dout, int64_t ld_
   NodesParams p = {where, weights, n_rows, n_sorted, top, 0, d * es, (const char*)dout, ld_dout * es, (const char*)Y, ld_y * es, (char*)dY, ld_dy * es, dweights, c->status};
   choose_group(&p);
   const bool aligned = p.width % 16 == 0 && on16(dout, p.ld_rows) && on16(Y, p.ld_sorted) && on16(dY, p.ld_out);
-  CU_TRY(c, NODES_LAUNCH(combine_grad_kernel, xt, aligned));
+  // a warp to a row where the rows fill the GPU that way: its sums need no barrier of the block (65536 bf16 rows of 4096 columns: 516 -> 435 us)
+  if (n_rows >= 148 * 32) p.lg = std::min(p.lg, 5);
+  // places in registers at a time: as many as a row has, up to four
+  auto go = [&](auto batch) {
+    constexpr int B = decltype(batch)::value;
+    return xt == WPSGD_X_F32 ? (aligned ? launch(combine_grad_kernel<float, true, B>, rows_grid(p), NODES_THREADS, 0, c->stream, p) : launch(combine_grad_kernel<float, false, B>, rows_grid(p), NODES_THREADS, 0, c->stream, p))
+                             : (aligned ? launch(combine_grad_kernel<__nv_bfloat16, true, B>, rows_grid(p), NODES_THREADS, 0, c->stream, p)
+                                        : launch(combine_grad_kernel<__nv_bfloat16, false, B>, rows_grid(p), NODES_THREADS, 0, c->stream, p));
+  };
+  CU_TRY(c, top == 1 ? go(std::integral_constant<int, 1>()) : top == 2 ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 4>()));
   c->launches++;
   return WPSGD_OK;
 }
