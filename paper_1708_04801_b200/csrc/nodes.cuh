@@ -32,6 +32,79 @@ struct SortParams {
 
 __device__ __forceinline__ void cluster_barrier() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
+// A warp's places in order: f(place, node as given, node or -1, lanes with the same node)
+template <typename F>
+__device__ __forceinline__ void go_over_places(const int* node, long long begin, long long end, int n, int lane, F f) {
+  constexpr int AHEAD = 8;  // loads in flight: one at a time would wait 600 cycles for each 32 places
+  for (long long at = begin; at < end; at += 32 * AHEAD) {
+    int key[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const long long e = at + a * 32 + lane;
+      key[a] = e < end ? node[e] : -1;
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      if (at + a * 32 >= end) break;
+      const int k = key[a] >= 0 && key[a] < n ? key[a] : -1;
+      f(at + a * 32 + lane, key[a], k, __match_any_sync(0xffffffffu, k));
+      __syncwarp();
+    }
+  }
+}
+// Counts of a warp's places by node
+__device__ __forceinline__ void count_places(const SortParams& p, unsigned* mine, long long begin, long long end, int lane) {
+  go_over_places(p.node, begin, end, p.nodes, lane, [&](long long e, int given, int k, unsigned same) {
+    if (k >= 0 && lane == __ffs(same) - 1) mine[k] += __popc(same);
+    if (given >= p.nodes) set_status(p.status, DEV_BOUNDS, 20, e);
+  });
+}
+// Positions handed out from a warp's counters, which hold the next position of each node
+__device__ __forceinline__ void place_rows(const SortParams& p, unsigned* mine, long long begin, long long end, int lane, int* order) {
+  go_over_places(p.node, begin, end, p.nodes, lane, [&](long long e, int, int k, unsigned same) {
+    int pos = -1;
+    if (k >= 0) pos = (int)(mine[k] + __popc(same & ((1u << lane) - 1)));
+    __syncwarp();
+    if (k >= 0 && lane == __ffs(same) - 1) mine[k] += __popc(same);
+    if (e < end) p.where[e] = pos;
+    if (k >= 0 && order) order[pos] = (int)e;
+  });
+}
+// Counters of a block's warps: of each node those of earlier warps; returns into totals[] those of all
+__device__ __forceinline__ void add_up_warps(const SortParams& p, unsigned* counters, unsigned* totals, int tid) {
+  for (int k = tid; k < p.nodes; k += SORT_THREADS) {
+    unsigned sum = 0;
+    for (int w = 0; w < p.warps; ++w) {
+      const unsigned c = counters[(size_t)w * p.nodes + k];
+      counters[(size_t)w * p.nodes + k] = sum;
+      sum += c;
+    }
+    totals[k] = sum;
+  }
+}
+// Exclusive sums of `value` over the threads of a block, and `carry` moved on by all of them
+__device__ __forceinline__ unsigned block_scan(unsigned value, unsigned& carry, unsigned* warp_sums, int warp, int lane) {
+  unsigned sum = value;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned v = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += v;
+  }
+  if (lane == 31) warp_sums[warp] = sum;
+  __syncthreads();
+  const unsigned w = warp_sums[lane];
+  unsigned ws = w;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned v = __shfl_up_sync(0xffffffffu, ws, o);
+    if (lane >= o) ws += v;
+  }
+  const unsigned before = carry + __shfl_sync(0xffffffffu, ws - w, warp) + sum - value;
+  carry += __shfl_sync(0xffffffffu, ws, 31);
+  __syncthreads();
+  return before;
+}
+
 __global__ void __launch_bounds__(SORT_THREADS) sort_rows_kernel(const __grid_constant__ SortParams p) {
   extern __shared__ unsigned sort_smem[];
   unsigned* totals = sort_smem;                // [nodes] of this block
@@ -48,41 +121,9 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_rows_kernel(const __grid_co
 
   const long long begin = ((long long)rank * p.warps + warp) * p.run, end = min(begin + p.run, p.places);
   unsigned* mine = counters + (size_t)warp * n;
-  constexpr int AHEAD = 8;  // loads in flight: one at a time would wait 600 cycles for each 32 places
-  // calls f(place, node or -1, lanes with the same node) for the warp's places in order
-  auto go_over = [&](auto f) {
-    for (long long at = begin; at < end; at += 32 * AHEAD) {
-      int key[AHEAD];
-#pragma unroll
-      for (int a = 0; a < AHEAD; ++a) {
-        const long long e = at + a * 32 + lane;
-        key[a] = e < end ? p.node[e] : -1;
-      }
-#pragma unroll
-      for (int a = 0; a < AHEAD; ++a) {
-        if (at + a * 32 >= end) break;
-        const int k = key[a] >= 0 && key[a] < n ? key[a] : -1;
-        f(at + a * 32 + lane, key[a], k, __match_any_sync(0xffffffffu, k));
-        __syncwarp();
-      }
-    }
-  };
-  if (warp < p.warps) {
-    go_over([&](long long e, int given, int k, unsigned same) {
-      if (k >= 0 && lane == __ffs(same) - 1) mine[k] += __popc(same);
-      if (given >= n) set_status(p.status, DEV_BOUNDS, 20, e);
-    });
-  }
+  if (warp < p.warps) count_places(p, mine, begin, end, lane);
   __syncthreads();
-  for (int k = tid; k < n; k += SORT_THREADS) {  // counters: places of earlier warps
-    unsigned sum = 0;
-    for (int w = 0; w < p.warps; ++w) {
-      const unsigned c = counters[(size_t)w * n + k];
-      counters[(size_t)w * n + k] = sum;
-      sum += c;
-    }
-    totals[k] = sum;
-  }
+  add_up_warps(p, counters, totals, tid);
   cluster_barrier();
 
   unsigned carry = 0;  // places of lower nodes
@@ -97,78 +138,138 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_rows_kernel(const __grid_co
         if (r < rank) before += c;
         all += c;
       }
-    unsigned sum = all;  // over the nodes up to this one
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const unsigned v = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += v;
-    }
-    if (lane == 31) warp_sums[warp] = sum;
-    __syncthreads();
-    unsigned w = warp_sums[lane], ws = w;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const unsigned v = __shfl_up_sync(0xffffffffu, ws, o);
-      if (lane >= o) ws += v;
-    }
-    const unsigned first = carry + __shfl_sync(0xffffffffu, ws - w, warp) + sum - all;
-    carry += __shfl_sync(0xffffffffu, ws, 31);
+    const unsigned first = block_scan(all, carry, warp_sums, warp, lane);
     if (k < n) {
       if (rank == 0) p.shard_off[k] = first;
       for (int v = 0; v < p.warps; ++v) counters[(size_t)v * n + k] += first + before;
     }
-    __syncthreads();
   }
+  __syncthreads();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this block has read the others' totals
   if (rank == 0 && tid == 0) p.shard_off[n] = carry;
 
-  if (warp < p.warps) {
-    go_over([&](long long e, int, int k, unsigned same) {
-      int pos = -1;
-      if (k >= 0) pos = (int)(mine[k] + __popc(same & ((1u << lane) - 1)));
-      __syncwarp();
-      if (k >= 0 && lane == __ffs(same) - 1) mine[k] += __popc(same);
-      if (e < end) p.where[e] = pos;
-      if (k >= 0 && p.order) p.order[pos] = (int)e;
-    });
-  }
+  if (warp < p.warps) place_rows(p, mine, begin, end, lane, p.order);
   if (p.order)
     for (long long i = carry + (long long)rank * SORT_THREADS + tid; i < p.places; i += (long long)blocks * SORT_THREADS) p.order[i] = -1;
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // no block leaves while its totals are read
 }
 
+// Many places: blocks all over the GPU, in four steps. The counts of the blocks, [blocks][nodes], stand in `order` until the positions are known, which is why it
+// has to be there: no memory beyond the arguments is used.
+__global__ void __launch_bounds__(SORT_THREADS) sort_count_kernel(const __grid_constant__ SortParams p) {
+  extern __shared__ unsigned sort_smem[];
+  unsigned* counters = sort_smem + p.nodes;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = p.nodes;
+  kernel_started();
+  for (int i = tid; i < p.warps * n; i += SORT_THREADS) counters[i] = 0;
+  kernel_inputs_ready();
+  __syncthreads();
+  const long long begin = ((long long)blockIdx.x * p.warps + warp) * p.run, end = min(begin + p.run, p.places);
+  if (warp < p.warps) count_places(p, counters + (size_t)warp * n, begin, end, lane);
+  __syncthreads();
+  for (int k = tid; k < n; k += SORT_THREADS) {
+    unsigned sum = 0;
+    for (int w = 0; w < p.warps; ++w) sum += counters[(size_t)w * n + k];
+    p.order[(size_t)blockIdx.x * n + k] = (int)sum;
+  }
+}
+// First position of each node in each block, from its counts
+__global__ void __launch_bounds__(SORT_THREADS) sort_scan_kernel(const __grid_constant__ SortParams p, int blocks) {
+  __shared__ unsigned warp_sums[32];
+  const int tid = threadIdx.x, n = p.nodes;
+  kernel_started();
+  kernel_inputs_ready();
+  unsigned carry = 0;
+  for (int base = 0; base < n; base += SORT_THREADS) {
+    const int k = base + tid;
+    unsigned all = 0;
+    if (k < n)
+      for (int b0 = 0; b0 < blocks; b0 += 16) {  // read before written: loads behind a store to the same array would wait for each other
+        unsigned c[16];
+#pragma unroll
+        for (int b = 0; b < 16; ++b) c[b] = b0 + b < blocks ? (unsigned)p.order[(size_t)(b0 + b) * n + k] : 0;
+#pragma unroll
+        for (int b = 0; b < 16; ++b) {
+          if (b0 + b < blocks) p.order[(size_t)(b0 + b) * n + k] = (int)all;
+          all += c[b];
+        }
+      }
+    const unsigned first = block_scan(all, carry, warp_sums, tid >> 5, tid & 31);
+    if (k < n) p.shard_off[k] = first;
+  }
+  if (tid == 0) p.shard_off[n] = carry;
+}
+__global__ void __launch_bounds__(SORT_THREADS) sort_place_kernel(const __grid_constant__ SortParams p) {
+  extern __shared__ unsigned sort_smem[];
+  unsigned *totals = sort_smem, *counters = sort_smem + p.nodes;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = p.nodes;
+  kernel_started();
+  for (int i = tid; i < p.warps * n; i += SORT_THREADS) counters[i] = 0;
+  kernel_inputs_ready();
+  __syncthreads();
+  const long long begin = ((long long)blockIdx.x * p.warps + warp) * p.run, end = min(begin + p.run, p.places);
+  unsigned* mine = counters + (size_t)warp * n;
+  if (warp < p.warps) go_over_places(p.node, begin, end, n, lane, [&](long long, int, int k, unsigned same) {
+    if (k >= 0 && lane == __ffs(same) - 1) mine[k] += __popc(same);
+  });
+  __syncthreads();
+  add_up_warps(p, counters, totals, tid);
+  for (int k = tid; k < n; k += SORT_THREADS) {
+    const unsigned first = (unsigned)p.shard_off[k] + (unsigned)p.order[(size_t)blockIdx.x * n + k];
+    for (int v = 0; v < p.warps; ++v) counters[(size_t)v * n + k] += first;
+  }
+  __syncthreads();
+  if (warp < p.warps) place_rows(p, mine, begin, end, lane, nullptr);
+}
+__global__ void __launch_bounds__(256) sort_order_kernel(const __grid_constant__ SortParams p) {
+  kernel_started();
+  kernel_inputs_ready();
+  const long long kept = p.shard_off[p.nodes];
+  for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < p.places; e += (long long)gridDim.x * 256) {
+    const int pos = p.where[e];
+    if (pos >= 0) p.order[pos] = (int)e;
+    if (e >= kept) p.order[e] = -1;
+  }
+}
+
 // ---- rows at any place in memory, by 16 bytes ----------------------------------------------------------------------------------
-// 16 bytes of a row from byte `c` on (c may be negative or reach behind the row's `width`: those bytes are anything). Where the row's bytes do not
-// start on 16, the two aligned units around them are read, if any byte of the row lies in them, and shifted together.
-template <bool ALIGNED>
-__device__ __forceinline__ uint4 row16(const char* row, long long c, long long width) {
-  if constexpr (ALIGNED) {
-    return ld_stream16(row + c);
-  } else {
-    const unsigned off = (unsigned)((uintptr_t)(row + c) & 15);
-    const uint4* at = (const uint4*)(row + c - off);
-    const long long from = c - off;  // of the first unit in the row
+// A row as units of 16 bytes that start where those of another row do that lies elsewhere: unit u has the bytes from `skew` + 16 u on (skew -15 to 0, so the first and the
+// last unit may reach outside the row: those bytes are anything). Where they do not start on 16 in memory, the two aligned units around them are read, if any byte
+// of the row lies in them, and shifted together; what is the same for all units of a row is worked out once.
+template <typename XT>
+struct ShiftedRow {
+  const uint4* at;  // the aligned unit in which unit 0 starts
+  unsigned off;     // and how far into it
+  int lo, n;        // aligned units lo to lo + n - 1 have bytes of the row
+  __device__ __forceinline__ void find(const char* row, int width, int skew) {
+    const char* start = row + skew;
+    off = (unsigned)((uintptr_t)start & 15);
+    at = (const uint4*)(start - off);
+    lo = (int)(row - (const char*)at) >> 4;
+    n = ((int)(row - (const char*)at) + width - 1 >> 4) - lo + 1;
+  }
+  __device__ __forceinline__ uint4 unit(int u) const {
     uint4 a = make_uint4(0, 0, 0, 0), b = a;
-    if (from + 16 > 0 && from < width) a = __ldg(at);
-    if (off == 0) return a;
-    if (from + 32 > 0 && from + 16 < width) b = __ldg(at + 1);
+    if ((unsigned)(u - lo) < (unsigned)n) a = __ldg(at + u);
+    if (off != 0 && (unsigned)(u + 1 - lo) < (unsigned)n) b = __ldg(at + u + 1);
     unsigned w0 = a.x, w1 = a.y, w2 = a.z, w3 = a.w, w4 = b.x, w5 = b.y, w6 = b.z, w7 = b.w;
     if (off & 8) w0 = w2, w1 = w3, w2 = w4, w3 = w5, w4 = w6, w5 = w7;
     if (off & 4) w0 = w1, w1 = w2, w2 = w3, w3 = w4, w4 = w5;
+    if (sizeof(XT) == 4) return make_uint4(w0, w1, w2, w3);
     const unsigned bits = (off & 3) * 8;
     return make_uint4(__funnelshift_r(w0, w1, bits), __funnelshift_r(w1, w2, bits), __funnelshift_r(w2, w3, bits), __funnelshift_r(w3, w4, bits));
   }
-}
+};
 // 16 bytes to a row from byte `c` on, a multiple of 16 in memory; those that lie in the row are written.
 template <typename XT, bool ALIGNED>
-__device__ __forceinline__ void put16(char* row, long long c, long long width, uint4 v) {
+__device__ __forceinline__ void put16(char* row, int c, int width, uint4 v) {
   if (ALIGNED || (c >= 0 && c + 16 <= width)) {
     *(uint4*)(row + c) = v;
   } else {
     const unsigned w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 16 / (int)sizeof(XT); ++i) {
-      const long long at = c + i * (int)sizeof(XT);
+      const int at = c + i * (int)sizeof(XT);
       if (at < 0 || at >= width) continue;
       if constexpr (sizeof(XT) == 4) *(unsigned*)(row + at) = w[i];
       else *(unsigned short*)(row + at) = (unsigned short)(w[i / 2] >> (16 * (i % 2)));
@@ -199,7 +300,7 @@ struct NodesParams {
   const float* weights;  // [n_rows, top], or NULL: all 1
   long long n_rows, n_sorted;
   int top, lg;
-  long long width;            // bytes of a row
+  int width;                  // bytes of a row
   const char* rows;           // [n_rows]: read by gather and by the gradient
   long long ld_rows;          // strides in bytes
   const char* sorted;         // [n_sorted]: read by combine and by the gradient
@@ -229,7 +330,7 @@ __global__ void __launch_bounds__(NODES_THREADS) gather_rows_kernel(const __grid
   for (long long i = (long long)blockIdx.x * per + (threadIdx.x >> p.lg); i < p.n_rows; i += (long long)gridDim.x * per) {
     const char* row = p.rows + i * p.ld_rows;
     if constexpr (ALIGNED) {
-      for (long long c = t * 16; c < p.width; c += 4 * step) {
+      for (int c = t * 16; c < p.width; c += 4 * step) {
         uint4 v[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -248,13 +349,18 @@ __global__ void __launch_bounds__(NODES_THREADS) gather_rows_kernel(const __grid
         const int pos = position(p, i * p.top + j, t == 0);
         if (pos < 0) continue;
         char* out = p.out + pos * p.ld_out;
-        for (long long c = t * 16 - (long long)((uintptr_t)out & 15); c < p.width; c += 4 * step) {
+        const int skew = -(int)((uintptr_t)out & 15);
+        ShiftedRow<XT> from;
+        from.find(row, p.width, skew);
+        for (int u0 = t; skew + u0 * 16 < p.width; u0 += 4 << p.lg) {
           uint4 v[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = row16<false>(row, c + u * step, p.width);
+          for (int u = 0; u < 4; ++u) v[u] = from.unit(u0 + (u << p.lg));
 #pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (c + u * step < p.width) put16<XT, false>(out, c + u * step, p.width, v[u]);
+          for (int u = 0; u < 4; ++u) {
+            const int c = skew + (u0 + (u << p.lg)) * 16;
+            if (c < p.width) put16<XT, false>(out, c, p.width, v[u]);
+          }
         }
       }
     }
@@ -262,41 +368,62 @@ __global__ void __launch_bounds__(NODES_THREADS) gather_rows_kernel(const __grid
 }
 
 // out[i] = sum_j weights[i, j] sorted[where[i, j]], j ascending, in fp32. Places without a position are left out, whatever their weight.
-// Four places of a unit are under way at a time. Bounds: bytes.
-template <typename XT, bool ALIGNED>
+// Four units are under way at a time, of PLACES places each (rows of more places have them found anew for each unit). Bounds: bytes.
+template <typename XT, bool ALIGNED, int PLACES>
 __global__ void __launch_bounds__(NODES_THREADS) combine_rows_kernel(const __grid_constant__ NodesParams p) {
-  constexpr int V = XVec<XT>::V;
+  constexpr int V = XVec<XT>::V, UNITS = !ALIGNED ? 1 : PLACES == 1 ? 4 : 2;
   kernel_started();
   kernel_inputs_ready();
-  const int per = NODES_THREADS >> p.lg, t = threadIdx.x & ((1 << p.lg) - 1), step = 16 << p.lg;
+  const int per = NODES_THREADS >> p.lg, g = 1 << p.lg, t = threadIdx.x & (g - 1);
   for (long long i = (long long)blockIdx.x * per + (threadIdx.x >> p.lg); i < p.n_rows; i += (long long)gridDim.x * per) {
     char* out = p.out + i * p.ld_out;
-    for (long long c = t * 16 - (ALIGNED ? 0 : (long long)((uintptr_t)out & 15)); c < p.width; c += step) {
-      float acc[V];
+    const int skew = ALIGNED ? 0 : -(int)((uintptr_t)out & 15);
+    const char* at[PLACES];
+    ShiftedRow<XT> from[PLACES];
+    float w[PLACES];
+    auto find = [&](int j) {  // places from j on; at NULL: none
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc[e] = 0.0f;
-      for (int j = 0; j < p.top; j += 4) {
-        uint4 v[4];
-        float w[4];
-        bool there[4];
+      for (int a = 0; a < PLACES; ++a) {
+        const int pos = j + a < p.top ? position(p, i * p.top + j + a, t == 0) : -1;
+        at[a] = pos >= 0 ? p.sorted + pos * p.ld_sorted : nullptr;
+        w[a] = pos >= 0 && p.weights ? __ldg(p.weights + i * p.top + j + a) : 1.0f;
+        if (!ALIGNED && pos >= 0) from[a].find(at[a], p.width, skew);
+      }
+    };
+    if (p.top <= PLACES) find(0);
+    for (int u0 = t; skew + u0 * 16 < p.width; u0 += UNITS * g) {
+      float acc[UNITS][V];
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          const int pos = j + a < p.top ? position(p, i * p.top + j + a, t == 0 && c <= 0) : -1;
-          there[a] = pos >= 0;
-          w[a] = there[a] ? (p.weights ? __ldg(p.weights + i * p.top + j + a) : 1.0f) : 0.0f;
-          v[a] = make_uint4(0, 0, 0, 0);
-          if (there[a]) v[a] = row16<ALIGNED>(p.sorted + pos * p.ld_sorted, c, p.width);
-        }
+      for (int u = 0; u < UNITS; ++u)
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          if (!there[a]) continue;
-          float f[V];
-          XVec<XT>::widen(v[a], f);
+        for (int e = 0; e < V; ++e) acc[u][e] = 0.0f;
+      for (int j = 0; j < p.top; j += PLACES) {
+        if (p.top > PLACES) find(j);
+        uint4 v[UNITS][PLACES];
 #pragma unroll
-          for (int e = 0; e < V; ++e) acc[e] = fmaf(w[a], f[e], acc[e]);
+        for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+          for (int a = 0; a < PLACES; ++a) {
+            if constexpr (ALIGNED) v[u][a] = ld_stream16_if(at[a] + (u0 + u * g) * 16, at[a] != nullptr && (u0 + u * g) * 16 < p.width);
+            else if (at[a]) v[u][a] = from[a].unit(u0 + u * g);
+          }
+#pragma unroll
+        for (int a = 0; a < PLACES; ++a) {
+          if (!at[a]) continue;
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            float f[V];
+            XVec<XT>::widen(v[u][a], f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[u][e] = fmaf(w[a], f[e], acc[u][e]);
+          }
         }
       }
-      put16<XT, ALIGNED>(out, c, p.width, narrow16<XT>(acc));
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        const int c = skew + (u0 + u * g) * 16;
+        if (c < p.width) put16<XT, ALIGNED>(out, c, p.width, narrow16<XT>(acc[u]));
+      }
     }
   }
 }
@@ -328,7 +455,7 @@ __global__ void __launch_bounds__(NODES_THREADS) combine_grad_kernel(const __gri
       }
       if constexpr (ALIGNED) {
         if (row_there)
-          for (long long c = t * 16; c < p.width; c += UNITS * step) {
+          for (int c = t * 16; c < p.width; c += UNITS * step) {
             uint4 dv[UNITS], v[UNITS][BATCH];
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
@@ -361,15 +488,20 @@ __global__ void __launch_bounds__(NODES_THREADS) combine_grad_kernel(const __gri
         for (int a = 0; a < BATCH; ++a) {
           if (pos[a] < 0) continue;
           char* out = p.out + pos[a] * p.ld_out;
-          const char* from = p.sorted + pos[a] * p.ld_sorted;
-          for (long long c = t * 16 - (long long)((uintptr_t)out & 15); c < p.width; c += step) {
+          const int skew = -(int)((uintptr_t)out & 15);
+          ShiftedRow<XT> ds, fs;
+          ds.find(row, p.width, skew);
+          fs.find(p.sorted + pos[a] * p.ld_sorted, p.width, skew);
+#pragma unroll 2
+          for (int u = t; skew + u * 16 < p.width; u += g) {
             float d[V], f[V], o[V];
-            XVec<XT>::widen(row16<false>(row, c, p.width), d);
-            XVec<XT>::widen(row16<false>(from, c, p.width), f);
+            const int c = skew + u * 16;
+            XVec<XT>::widen(ds.unit(u), d);
+            XVec<XT>::widen(fs.unit(u), f);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-              const long long at = c + e * (int)sizeof(XT);
-              if (at >= 0 && at < p.width) dot[a] = fmaf(d[e], f[e], dot[a]);
+              const bool in = (unsigned)(c + e * (int)sizeof(XT)) < (unsigned)p.width;
+              dot[a] = fmaf(in ? d[e] : 0.0f, in ? f[e] : 0.0f, dot[a]);
               o[e] = w[a] * d[e];
             }
             put16<XT, false>(out, c, p.width, narrow16<XT>(o));

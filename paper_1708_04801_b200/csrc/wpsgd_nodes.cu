@@ -1,6 +1,5 @@
 // C ABI of the operators that lay rows out by node and bring them back (see include/wpsgd.h). Argument checks, choice of forms, launches.
 #include <algorithm>
-#include <type_traits>
 
 #include "nodes.cuh"
 #include "rows_host.cuh"
@@ -21,7 +20,7 @@ const char* check_rows(const void* p, wpsgd_xtype xt, int64_t ld, int64_t d, int
   if (!known(xt)) return "unknown type";
   if (d < 1 || ld < d || n < 0) return "rows need at least one column, a stride of at least d and no negative count";
   if (d > INT64_MAX / 8 / std::max<int64_t>(n, 1) || ld > INT64_MAX / 8 / std::max<int64_t>(n, 1)) return "rows that pass 63 bits";
-  if (n > INT32_MAX) return "2^31 rows and more";
+  if (n > INT32_MAX || d > INT32_MAX / 8) return "2^31 rows and more, or rows of 2^31 bytes";
   if (n > 0 && !p) return "rows are NULL";
   if ((uintptr_t)p % element_size(xt)) return "rows are not aligned to their elements";
   return nullptr;
@@ -41,11 +40,12 @@ void choose_group(NodesParams* p) {
 }
 unsigned rows_grid(const NodesParams& p) { return (unsigned)grid_for(p.n_rows, NODES_THREADS >> p.lg, 1 << 20); }
 
-#define NODES_LAUNCH(kernel, xt, aligned)                                                                                       \
-  ((xt) == WPSGD_X_F32 ? ((aligned) ? launch(kernel<float, true>, rows_grid(p), NODES_THREADS, 0, c->stream, p)                 \
-                                    : launch(kernel<float, false>, rows_grid(p), NODES_THREADS, 0, c->stream, p))               \
-                       : ((aligned) ? launch(kernel<__nv_bfloat16, true>, rows_grid(p), NODES_THREADS, 0, c->stream, p)         \
-                                    : launch(kernel<__nv_bfloat16, false>, rows_grid(p), NODES_THREADS, 0, c->stream, p)))
+#define NODES_LAUNCH(kernel, ...) launch(kernel<__VA_ARGS__>, rows_grid(p), NODES_THREADS, 0, c->stream, p)
+#define NODES_LAUNCH_ANY(kernel, ...)                                                                                                                \
+  (xt == WPSGD_X_F32 ? (aligned ? NODES_LAUNCH(kernel, float, true, ##__VA_ARGS__) : NODES_LAUNCH(kernel, float, false, ##__VA_ARGS__)) \
+                     : (aligned ? NODES_LAUNCH(kernel, __nv_bfloat16, true, ##__VA_ARGS__) : NODES_LAUNCH(kernel, __nv_bfloat16, false, ##__VA_ARGS__)))
+// by the places that are in registers at a time: as many as a row has, up to four
+#define NODES_LAUNCH_PLACES(kernel) (top == 1 ? NODES_LAUNCH_ANY(kernel, 1) : top == 2 ? NODES_LAUNCH_ANY(kernel, 2) : NODES_LAUNCH_ANY(kernel, 4))
 
 wpsgd_status refuse(wpsgd_ctx* c, const char* call, const char* why) { return fail(c, WPSGD_ERR_INVALID_ARG, std::string(call) + ": " + why); }
 
@@ -66,6 +66,22 @@ wpsgd_status wpsgd_sort_rows(wpsgd_ctx* c, const int32_t* node, int64_t n_rows, 
     return refuse(c, "sort_rows", "arrays overlap");
   DeviceGuard guard(c->device);
   SortParams p = {node, places, n_nodes, 0, 0, where, order, (long long*)shard_off, c->status};
+  // Many places and blocks enough whose counts fit `order`: 131072 places on 128 nodes 30 us by a cluster of 8 blocks, 17 by the GPU. The scan over blocks is one
+  // block's, so that there are fewer of them for more nodes.
+  const long long many = std::min<long long>({148ll, 65536ll / n_nodes, places / 2 / n_nodes, (places + 2047) / 2048});
+  if (order && places >= 32768 && many >= 12) {
+    p.warps = (int)std::min<long long>(32, SORT_COUNTERS / n_nodes);
+    p.run = ((places + many * p.warps - 1) / (many * p.warps) + 31) / 32 * 32;
+    const size_t smem = ((size_t)n_nodes * (p.warps + 1)) * 4;
+    CU_TRY(c, (allow_smem<sort_count_kernel>(c)));
+    CU_TRY(c, (allow_smem<sort_place_kernel>(c)));
+    CU_TRY(c, launch(sort_count_kernel, (unsigned)many, SORT_THREADS, smem, c->stream, p));
+    CU_TRY(c, launch(sort_scan_kernel, 1, SORT_THREADS, 0, c->stream, p, (int)many));
+    CU_TRY(c, launch(sort_place_kernel, (unsigned)many, SORT_THREADS, smem, c->stream, p));
+    CU_TRY(c, launch(sort_order_kernel, (unsigned)grid_for(places, 256), 256, 0, c->stream, p));
+    c->launches += 4;
+    return WPSGD_OK;
+  }
   // blocks: a run of 128 places for each warp before another block is worth its exchange (131072 places: 8 blocks)
   const unsigned blocks = places <= 4096 ? 1 : places <= 8192 ? 2 : places <= 16384 ? 4 : 8;
   p.warps = (int)std::max(1ll, std::min<long long>({32ll, (long long)SORT_COUNTERS / n_nodes, (places + 32 * blocks - 1) / (32 * blocks)}));
@@ -87,10 +103,10 @@ wpsgd_status wpsgd_gather_rows(wpsgd_ctx* c, const void* X, wpsgd_xtype xt, int6
   if (n_rows == 0) return WPSGD_OK;
   DeviceGuard guard(c->device);
   const long long es = (long long)element_size(xt);
-  NodesParams p = {where, nullptr, n_rows, n_sorted, top, 0, d * es, (const char*)X, ld_x * es, nullptr, 0, (char*)out, ld_out * es, nullptr, c->status};
+  NodesParams p = {where, nullptr, n_rows, n_sorted, top, 0, (int)(d * es), (const char*)X, ld_x * es, nullptr, 0, (char*)out, ld_out * es, nullptr, c->status};
   choose_group(&p);
   const bool aligned = p.width % 16 == 0 && on16(X, p.ld_rows) && on16(out, p.ld_out);
-  CU_TRY(c, NODES_LAUNCH(gather_rows_kernel, xt, aligned));
+  CU_TRY(c, NODES_LAUNCH_ANY(gather_rows_kernel));
   c->launches++;
   return WPSGD_OK;
 }
@@ -109,10 +125,10 @@ wpsgd_status wpsgd_combine_rows(wpsgd_ctx* c, const void* Y, wpsgd_xtype xt, int
   if (n_rows == 0) return WPSGD_OK;
   DeviceGuard guard(c->device);
   const long long es = (long long)element_size(xt);
-  NodesParams p = {where, weights, n_rows, n_sorted, top, 0, d * es, nullptr, 0, (const char*)Y, ld_y * es, (char*)out, ld_out * es, nullptr, c->status};
+  NodesParams p = {where, weights, n_rows, n_sorted, top, 0, (int)(d * es), nullptr, 0, (const char*)Y, ld_y * es, (char*)out, ld_out * es, nullptr, c->status};
   choose_group(&p);
   const bool aligned = p.width % 16 == 0 && on16(Y, p.ld_sorted) && on16(out, p.ld_out);
-  CU_TRY(c, NODES_LAUNCH(combine_rows_kernel, xt, aligned));
+  CU_TRY(c, NODES_LAUNCH_PLACES(combine_rows_kernel));
   c->launches++;
   return WPSGD_OK;
 }
@@ -134,19 +150,12 @@ wpsgd_status wpsgd_combine_rows_grad(wpsgd_ctx* c, const void* dout, int64_t ld_
   if (n_rows == 0) return WPSGD_OK;
   DeviceGuard guard(c->device);
   const long long es = (long long)element_size(xt);
-  NodesParams p = {where, weights, n_rows, n_sorted, top, 0, d * es, (const char*)dout, ld_dout * es, (const char*)Y, ld_y * es, (char*)dY, ld_dy * es, dweights, c->status};
+  NodesParams p = {where, weights, n_rows, n_sorted, top, 0, (int)(d * es), (const char*)dout, ld_dout * es, (const char*)Y, ld_y * es, (char*)dY, ld_dy * es, dweights, c->status};
   choose_group(&p);
   const bool aligned = p.width % 16 == 0 && on16(dout, p.ld_rows) && on16(Y, p.ld_sorted) && on16(dY, p.ld_out);
   // a warp to a row where the rows fill the GPU that way: its sums need no barrier of the block (65536 bf16 rows of 4096 columns: 516 -> 435 us)
   if (n_rows >= 148 * 32) p.lg = std::min(p.lg, 5);
-  // places in registers at a time: as many as a row has, up to four
-  auto go = [&](auto batch) {
-    constexpr int B = decltype(batch)::value;
-    return xt == WPSGD_X_F32 ? (aligned ? launch(combine_grad_kernel<float, true, B>, rows_grid(p), NODES_THREADS, 0, c->stream, p) : launch(combine_grad_kernel<float, false, B>, rows_grid(p), NODES_THREADS, 0, c->stream, p))
-                             : (aligned ? launch(combine_grad_kernel<__nv_bfloat16, true, B>, rows_grid(p), NODES_THREADS, 0, c->stream, p)
-                                        : launch(combine_grad_kernel<__nv_bfloat16, false, B>, rows_grid(p), NODES_THREADS, 0, c->stream, p));
-  };
-  CU_TRY(c, top == 1 ? go(std::integral_constant<int, 1>()) : top == 2 ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 4>()));
+  CU_TRY(c, NODES_LAUNCH_PLACES(combine_grad_kernel));
   c->launches++;
   return WPSGD_OK;
 }

@@ -59,6 +59,7 @@ def strided(t, pad, offset=0, fill=77.0):
 @pytest.mark.parametrize("n,top,nodes,dropped", [
     (1, 1, 1, 0.0), (1, 1, 5, 1.0), (0, 3, 7, 0.0), (7, 3, 4, 0.3), (31, 1, 2, 0.0), (64, 2, 16, 0.0), (333, 3, 1000, 0.2), (4096, 1, 3, 0.0),
     (4097, 1, 1, 0.1), (5000, 2, 128, 0.0), (9000, 2, 37, 0.5), (40001, 2, 1025, 0.1), (70000, 2, 16384, 0.0), (300, 2, 16384, 0.1), (50001, 8, 129, 0.02),
+    (32768, 1, 64, 0.0), (33000, 1, 1300, 0.9), (100003, 3, 2, 0.3), (40000, 5, 2048, 0.0), (300000, 2, 100, 1.0), (65536, 1, 5461, 0.0), (1 << 20, 2, 64, 0.01),
 ])
 def test_sort_rows(ctx, n, top, nodes, dropped):
     node = assignment(n, top, nodes, n + nodes, dropped)
