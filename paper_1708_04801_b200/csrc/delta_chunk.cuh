@@ -197,23 +197,34 @@ __global__ void __launch_bounds__(PLAN_THREADS) delta_plan_kernel(const __grid_c
   }
 }
 
-// Heads of a width that is no multiple of 8, or that do not start on 16 bytes, laid out anew: [n_rows][heads][width rounded up], zeros behind.
-// Rows outside the chains are copied too, and not used.
-__global__ void __launch_bounds__(256) delta_pack_kernel(const __nv_bfloat16* from, long long ld, int heads, int width, __nv_bfloat16* to, int width8, long long n_rows) {
+// Heads of a width that is no multiple of 8, or that do not start on 16 bytes, laid out anew: [n_rows][heads][width rounded up], zeros behind. Up to three tensors in one launch,
+// one for each blockIdx.y. Rows outside the chains are copied too, and not used.
+struct DeltaPack {
+  struct {
+    const __nv_bfloat16* from;
+    long long ld;
+    __nv_bfloat16* to;
+    int heads, width;
+  } t[3];
+  long long n_rows;
+};
+__global__ void __launch_bounds__(256) delta_pack_kernel(const __grid_constant__ DeltaPack p) {
   kernel_started();
   kernel_inputs_ready();
-  const long long units = n_rows * heads * (width8 / 8);
+  const auto& t = p.t[blockIdx.y];
+  const int per = (t.width + 7) / 8;
+  const long long units = p.n_rows * t.heads * per;
   for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < units; u += (long long)gridDim.x * 256) {
-    const long long head = row_of(u, width8 / 8), row = row_of(head, heads);
-    const int col = (int)(u - head * (width8 / 8)) * 8, h = (int)(head - row * heads);
-    const unsigned short* src = (const unsigned short*)from + row * ld + (long long)h * width;
+    const long long head = row_of(u, per), row = row_of(head, t.heads);
+    const int col = (int)(u - head * per) * 8, h = (int)(head - row * t.heads);
+    const unsigned short* src = (const unsigned short*)t.from + row * t.ld + (long long)h * t.width;
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t a = col + 2 * i < width ? src[col + 2 * i] : 0, b = col + 2 * i + 1 < width ? src[col + 2 * i + 1] : 0;
+      const uint32_t a = col + 2 * i < t.width ? src[col + 2 * i] : 0, b = col + 2 * i + 1 < t.width ? src[col + 2 * i + 1] : 0;
       w[i] = a | b << 16;
     }
-    *(uint4*)(to + head * width8 + col) = make_uint4(w[0], w[1], w[2], w[3]);
+    *(uint4*)(t.to + head * per * 8 + col) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 

@@ -141,13 +141,22 @@ DeltaChunkParams chunk_params(const wpsgd_ctx* c, const wpsgd_delta_rows* r, con
   return p;
 }
 
-wpsgd_status pack_heads(wpsgd_ctx* c, const void* from, long long ld, int heads, int width, const __nv_bfloat16* to, long long n) {
-  const int width8 = (width + 7) / 8 * 8;
-  if (n == 0) return WPSGD_OK;
-  CU_TRY(c, launch(delta_pack_kernel, grid_for(n * heads * (width8 / 8), 256), 256, 0, c->stream, (const __nv_bfloat16*)from, ld, heads, width, (__nv_bfloat16*)to, width8, n));
-  c->launches++;
-  return WPSGD_OK;
-}
+struct Packs {
+  DeltaPack p = {};
+  int n = 0;
+  long long most = 0;  // units of the largest
+  void add(const void* from, long long ld, int heads, int width, const __nv_bfloat16* to) {
+    p.t[n++] = {(const __nv_bfloat16*)from, ld, (__nv_bfloat16*)to, heads, width};
+    most = std::max(most, (long long)heads * ((width + 7) / 8));
+  }
+  wpsgd_status launch_for(wpsgd_ctx* c, long long n_rows) {
+    if (n == 0 || n_rows == 0) return WPSGD_OK;
+    p.n_rows = n_rows;
+    CU_TRY(c, launch(delta_pack_kernel, dim3(grid_for(n_rows * most, 256), n), 256, 0, c->stream, p));
+    c->launches++;
+    return WPSGD_OK;
+  }
+};
 
 // Tensor maps of features and queries for the walks, 64 rows by 64 columns at a time; false: whole heads do not fill such tiles, or sizes that a map cannot describe
 bool encode_maps(DeltaMaps* maps, const DeltaChunkParams& p) {
@@ -285,10 +294,11 @@ wpsgd_status wpsgd_delta_run(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const f
   DeltaChunkParams p = chunk_params(c, rows, lay, (unsigned char*)workspace);
   p.W0 = W0, p.W = W_out, p.out = (__nv_bfloat16*)out, p.ld_out = ld_out;
   p.vec_out = rows->dv % 8 == 0 && ld_out % 8 == 0 && aligned16(out);
-  wpsgd_status s = WPSGD_OK;
-  if (lay.pack_k) s = pack_heads(c, rows->q, rows->ld_q, rows->heads_k, rows->dk, p.q.p, rows->n_rows);
-  if (lay.pack_k && s == WPSGD_OK) s = pack_heads(c, rows->k, rows->ld_k, rows->heads_k, rows->dk, p.k.p, rows->n_rows);
-  if (lay.pack_v && s == WPSGD_OK) s = pack_heads(c, rows->v, rows->ld_v, rows->heads_v, rows->dv, p.v.p, rows->n_rows);
+  Packs packs;
+  if (lay.pack_k) packs.add(rows->q, rows->ld_q, rows->heads_k, rows->dk, p.q.p);
+  if (lay.pack_k) packs.add(rows->k, rows->ld_k, rows->heads_k, rows->dk, p.k.p);
+  if (lay.pack_v) packs.add(rows->v, rows->ld_v, rows->heads_v, rows->dv, p.v.p);
+  const wpsgd_status s = packs.launch_for(c, rows->n_rows);
   if (s != WPSGD_OK) return s;
   return lay.DK == 64 ? run_chunks<64>(c, p, lay, save) : run_chunks<128>(c, p, lay, save);
 }
@@ -321,10 +331,10 @@ wpsgd_status wpsgd_delta_grad(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const 
                        (__nv_bfloat16*)dv, (__nv_bfloat16*)dg, (__nv_bfloat16*)dbeta, rows->dv % 8 == 0 && aligned16(dv), rows->dk % 2 == 0 && ((uintptr_t)dq | (uintptr_t)dk) % 4 == 0};
   p.f.dout = own.pack_o ? DeltaHeads{(const __nv_bfloat16*)(ws + own.dout), (long long)rows->heads_v * lay.dv8, rows->heads_v, lay.dv8}
                         : DeltaHeads{(const __nv_bfloat16*)dout, ld_dout, rows->heads_v, rows->dv};
-  if (own.pack_o) {
-    const wpsgd_status s = pack_heads(c, dout, ld_dout, rows->heads_v, rows->dv, p.f.dout.p, n);
-    if (s != WPSGD_OK) return s;
-  }
+  Packs packs;
+  if (own.pack_o) packs.add(dout, ld_dout, rows->heads_v, rows->dv, p.f.dout.p);
+  const wpsgd_status s = packs.launch_for(c, n);
+  if (s != WPSGD_OK) return s;
   return lay.DK == 64 ? grad_chunks<64>(c, p, lay, rows_blocks(rows, lay)) : grad_chunks<128>(c, p, lay, rows_blocks(rows, lay));
 }
 

@@ -120,6 +120,65 @@ def test_run(ctx, lengths, first, behind, hk, hv, dk, dv, start, dtype):
     check_run(rows, off, got, W0)
 
 
+# what the library chooses from: labels shared by 8, 4 or 2 warps of a block, heads that share features formed together, rows by tensor maps or not, rings that go round
+FORMS = [([260, 200, 130, 64] * 10, 2, 4, 128, 128), ([260, 200, 130, 64] * 10, 4, 4, 64, 64), ([3] * 600, 4, 8, 128, 128), ([1, 65] * 150, 2, 6, 64, 64), ([2] * 400, 4, 12, 24, 32),
+         ([70] * 80, 2, 2, 72, 120)]
+
+
+@pytest.mark.parametrize("lengths,hk,hv,dk,dv", FORMS)
+def test_run_forms(ctx, lengths, hk, hv, dk, dv):
+    rows = make(sum(lengths), hk, hv, dk, dv, torch.bfloat16, 21)
+    off = offsets(lengths)
+    W0 = torch.randn((len(lengths), hv, dv, dk), generator=gen(3))
+    on = [x.cuda() for x in rows]
+    got = ctx.delta_run(*on, off.cuda(), W0=W0.cuda())
+    ctx.check()
+    out, W = got
+    # row by row in fp32, which has tests of its own against 64 bits, stands for the recurrence; sizes from there too
+    exact_out, exact_W = ctx.delta_run(*[x.float() for x in on], off.cuda(), W0=W0.cuda())
+    sized_out, sized_W = ctx.delta_run(on[0].float().abs(), on[1].float().abs(), 3 * on[2].float().abs(), on[3].float(), on[4].float(), off.cuda(), W0=W0.abs().cuda())
+    ctx.check()
+    assert float((W - exact_W).norm()) <= 2.0 ** -13 * float(exact_W.norm() + sized_W.norm())
+    assert float((out.float() - exact_out).norm()) <= 3 * 2.0 ** -8 * float(exact_out.norm())
+
+
+@pytest.mark.parametrize("lengths,hk,hv,dk,dv", FORMS)
+def test_gradients_forms(ctx, lengths, hk, hv, dk, dv):
+    """Gradients of many chains at once are, bit for bit, those of the chains a few at a time, which other tests hold against 64 bits."""
+    n = sum(lengths)
+    rows = [x.cuda() for x in make(n, hk, hv, dk, dv, torch.bfloat16, 22)]
+    dout = torch.randn((n, hv, dv), generator=gen(4)).to(torch.bfloat16).cuda()
+    off = offsets(lengths)
+    out, W, saved = ctx.delta_run(*rows, off.cuda(), save=True)
+    got = ctx.delta_grad(saved, dout)[:5]
+    for a, b in ((0, 1), (len(lengths) - 2, len(lengths))):
+        part = slice(int(off[a]), int(off[b]))
+        few = [x[part].contiguous() for x in rows]
+        o, w, kept = ctx.delta_run(*few, (off[a:b + 1] - off[a]).cuda(), save=True)
+        same = [torch.equal(x[part], y) for x, y in zip(got, ctx.delta_grad(kept, dout[part].contiguous())[:5])]
+        assert torch.equal(out[part], o) and torch.equal(W[a:b], w) and all(same), same
+    ctx.check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_nothing_to_run(ctx, dtype):
+    rows = [x.cuda() for x in make(5, 1, 2, 16, 8, dtype)]
+    W0 = torch.randn((3, 2, 8, 16), generator=gen(1)).cuda()
+    out = torch.full((5, 2, 8), 7.0, dtype=dtype, device="cuda")
+    _, W = ctx.delta_run(*rows, torch.tensor([2, 2, 2, 2]).cuda(), W0=W0, out=out)             # chains without rows keep their models
+    assert torch.equal(W, W0) and bool((out == 7).all())
+    _, W = ctx.delta_run(*[x[:0] for x in rows], torch.tensor([0, 0]).cuda())                      # no rows at all
+    assert W.shape == (1, 2, 8, 16) and float(W.abs().max()) == 0.0
+    o, W = ctx.delta_run(*rows, torch.tensor([0]).cuda(), out=out)                              # no chains
+    assert W.shape[0] == 0 and bool((o == 7).all())
+    ctx.delta_step(*[x[:0] for x in rows], W0)
+    if dtype is torch.bfloat16:
+        _, _, saved = ctx.delta_run(*rows, torch.tensor([2, 2, 2, 2]).cuda(), save=True)
+        dW = torch.randn((3, 2, 8, 16), generator=gen(2)).cuda()
+        assert torch.equal(ctx.delta_grad(saved, rows[2], dW, start=True)[5], dW)
+    ctx.check()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_run_strides_scale_and_models_in_place(ctx, dtype):
     # q, k and v of one wide row, as one projection leaves them; answers into part of wider rows; models updated where they are
@@ -360,28 +419,25 @@ def test_two_graphs_and_another_stream(P):
             graph.reset()
 
 
-@pytest.mark.parametrize("limit", [1, 1 << 20])
-def test_a_wait_that_runs_out_is_reported(P, limit):
-    rows = [x.cuda() for x in make(700, 1, 1, 64, 64, torch.bfloat16)]
-    off = offsets([700]).cuda()
-    dout = torch.zeros_like(rows[2])
+@pytest.mark.parametrize("limit", [1, 4096])
+@pytest.mark.parametrize("chains,dv", [(1, 64), (160, 128)])  # warps that only copy beside those that multiply, and warps that do both
+def test_a_wait_that_runs_out_is_reported(P, limit, chains, dv):
+    rows = [x.cuda() for x in make(400 * chains, 1, 1, 64, dv, torch.bfloat16)]
+    off = offsets([400] * chains).cuda()
     with P.Context(1, 1) as c:
-        _, _, saved = c.delta_run(*rows, off, save=True)
+        want, _, saved = c.delta_run(*rows, off, save=True)
         c.check()
-        c.set_option("test_drop_block", 5)
-        if limit == 1:
-            c.set_option("spin_limit", 4096)
-        c.delta_run(*rows, off)
-        with pytest.raises(P.WpsgdError) as e:
-            c.check()
-        assert e.value.status_name == "TIMEOUT"
-    with P.Context(1, 1) as c:
-        c.set_option("test_drop_block", 5)
-        c.set_option("spin_limit", 4096)
-        c.delta_grad(saved, dout)
-        with pytest.raises(P.WpsgdError) as e:
-            c.check()
-        assert e.value.status_name == "TIMEOUT"
+        for call in (lambda: c.delta_run(*rows, off), lambda: c.delta_grad(saved, rows[2])):
+            c.set_option("test_drop_block", 5)
+            c.set_option("spin_limit", limit)
+            call()
+            with pytest.raises(P.WpsgdError) as e:
+                c.check()
+            assert e.value.status_name == "TIMEOUT"
+        c.set_option("test_drop_block", -1)
+        c.set_option("spin_limit", 1 << 20)
+        assert torch.equal(c.delta_run(*rows, off)[0], want)   # and the context goes on
+        c.check()
 
 
 # ---- single rows -------------------------------------------------------------------------------------------------------------
