@@ -109,7 +109,8 @@ wpsgd_status wpsgd_destroy(wpsgd_ctx* ctx);
  *   "test_drop_block" test hook of the bounded waits, not for production use: the rows of that block of every chain
  *                     are never requested, so the wait for them runs out and WPSGD_ERR_TIMEOUT is reported by
  *                     wpsgd_check; -1 (default) = off. Of wpsgd_margins_fp8 it drops that block of 128 columns, of
- *                     wpsgd_objective_grad the rows that each group of threads takes in that round (rows in bulk copies). */
+ *                     wpsgd_objective_grad the rows that each group of threads takes in that round (rows in bulk copies), of wpsgd_delta_run and
+ *                     wpsgd_delta_grad on bf16 rows that chunk of every chain and those behind it. */
 wpsgd_status wpsgd_set_option(wpsgd_ctx* ctx, const char* name, int64_t value);
 
 /* Node numbers that enter the sample stream in place of 0..k-1 (HOST [k], >= 0; NULL restores the

@@ -81,9 +81,9 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
   for (int i = 0; i < n; ++i) {
     const int s = i % STAGES, s1 = (i + 1) % STAGES;
     bool ok = true;
-    if (!COPIERS && i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): one that is never brought
+    if (!COPIERS && i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): from which on none is brought
       if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars[s1].empty, ((i + 1) / STAGES - 1) & 1, p.spin_limit));
-      if (ok && i + 1 != p.drop) {
+      if (ok && (p.drop < 0 || i + 1 < p.drop)) {
         bring_chunk<DK, NW>(p, maps, p.dout, smem32(ring) + s1 * Shape::stage, first + n - 2 - i, span, n - 2 - i, h, kh, col0, warp, warps, lane, &bars[s1]);
         brought = i + 2;
       }

@@ -122,7 +122,7 @@ def test_run(ctx, lengths, first, behind, hk, hv, dk, dv, start, dtype):
 
 # what the library chooses from: labels shared by 8, 4 or 2 warps of a block, heads that share features formed together, rows by tensor maps or not, rings that go round
 FORMS = [([260, 200, 130, 64] * 10, 2, 4, 128, 128), ([260, 200, 130, 64] * 10, 4, 4, 64, 64), ([3] * 600, 4, 8, 128, 128), ([1, 65] * 150, 2, 6, 64, 64), ([2] * 400, 4, 12, 24, 32),
-         ([70] * 80, 2, 2, 72, 120)]
+         ([70] * 80, 2, 2, 72, 120), ([200, 3] * 80, 1, 1, 128, 72)]
 
 
 @pytest.mark.parametrize("lengths,hk,hv,dk,dv", FORMS)
