@@ -605,7 +605,6 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
   __shared__ ChunkBarriers bars[STAGES];
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
   unsigned char* const ring = chain_smem + (-smem32(chain_smem) & 1023u);
-  kernel_started();
   kernel_inputs_ready();
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
@@ -789,6 +788,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
     __syncwarp();
     if (lane == 0) arrive(&bars[s].empty);
   }
+  kernel_started();
   if (p.W)
 #pragma unroll
     for (int x = 0; x < DK / 8; ++x)

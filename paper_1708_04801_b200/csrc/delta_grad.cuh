@@ -47,7 +47,6 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
   __shared__ ChunkBarriers bars[STAGES];
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
   unsigned char* const ring = chain_smem + (-smem32(chain_smem) & 1023u);
-  kernel_started();
   kernel_inputs_ready();
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
@@ -227,6 +226,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
     __syncwarp();
     if (lane == 0) arrive(&bars[s].empty);
   }
+  kernel_started();
   if (gp.dW0)
 #pragma unroll
     for (int x = 0; x < DK / 8; ++x)
@@ -274,7 +274,6 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
   float* totals = gp.totals + (size_t)blockIdx.x * Shape::totals;  // where several heads share features
   __shared__ float model_dots[ROWS_THREADS / 32];
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3, wr = warp & 3, wc = warp >> 2;
-  kernel_started();
   kernel_inputs_ready();
   const int slices = (p.dvp + ROWS_SLICE - 1) / ROWS_SLICE;
   // Pieces: all heads of labels of a (chunk, head of features), then the next of this block's. What a copy needs is kept beside them: a piece changes once in
@@ -623,6 +622,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
       }
     }
   }
+  kernel_started();
   copies_done();
 }
 

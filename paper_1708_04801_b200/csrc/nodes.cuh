@@ -236,6 +236,14 @@ __global__ void __launch_bounds__(256) sort_order_kernel(const __grid_constant__
 // A row as units of 16 bytes that start where those of another row do that lies elsewhere: unit u has the bytes from `skew` + 16 u on (skew -15 to 0, so the first and the
 // last unit may reach outside the row: those bytes are anything). Where they do not start on 16 in memory, the two aligned units around them are read, if any byte
 // of the row lies in them, and shifted together; what is the same for all units of a row is worked out once.
+// Read-only 16 bytes where `yes`, zeros elsewhere: a predicate, not a branch. Neighbouring units of a shifted row share them in L1.
+__device__ __forceinline__ uint4 ld16_if(const void* p, bool yes) {
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %5, 0;\n\t@p ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];\n\t}"
+               : "+r"(r.x), "+r"(r.y), "+r"(r.z), "+r"(r.w)
+               : "l"(p), "r"((int)yes));
+  return r;
+}
 template <typename XT>
 struct ShiftedRow {
   const uint4* at;  // the aligned unit in which unit 0 starts
@@ -248,11 +256,15 @@ struct ShiftedRow {
     lo = (int)(row - (const char*)at) >> 4;
     n = ((int)(row - (const char*)at) + width - 1 >> 4) - lo + 1;
   }
-  __device__ __forceinline__ uint4 unit(int u) const {
-    uint4 a = make_uint4(0, 0, 0, 0), b = a;
-    if ((unsigned)(u - lo) < (unsigned)n) a = __ldg(at + u);
-    if (off != 0 && (unsigned)(u + 1 - lo) < (unsigned)n) b = __ldg(at + u + 1);
-    unsigned w0 = a.x, w1 = a.y, w2 = a.z, w3 = a.w, w4 = b.x, w5 = b.y, w6 = b.z, w7 = b.w;
+  // the two aligned units of unit u, asked for; and the unit itself, once they are there. Apart, so that several can be under way
+  struct Raw {
+    uint4 a, b;
+  };
+  __device__ __forceinline__ Raw ask(int u, bool yes) const {
+    return {ld16_if(at + u, yes && (unsigned)(u - lo) < (unsigned)n), ld16_if(at + u + 1, yes && off != 0 && (unsigned)(u + 1 - lo) < (unsigned)n)};
+  }
+  __device__ __forceinline__ uint4 unit(const Raw& raw) const {
+    unsigned w0 = raw.a.x, w1 = raw.a.y, w2 = raw.a.z, w3 = raw.a.w, w4 = raw.b.x, w5 = raw.b.y, w6 = raw.b.z, w7 = raw.b.w;
     if (off & 8) w0 = w2, w1 = w3, w2 = w4, w3 = w5, w4 = w6, w5 = w7;
     if (off & 4) w0 = w1, w1 = w2, w2 = w3, w3 = w4, w4 = w5;
     if (sizeof(XT) == 4) return make_uint4(w0, w1, w2, w3);
@@ -353,13 +365,13 @@ __global__ void __launch_bounds__(NODES_THREADS) gather_rows_kernel(const __grid
         ShiftedRow<XT> from;
         from.find(row, p.width, skew);
         for (int u0 = t; skew + u0 * 16 < p.width; u0 += 4 << p.lg) {
-          uint4 v[4];
+          typename ShiftedRow<XT>::Raw v[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = from.unit(u0 + (u << p.lg));
+          for (int u = 0; u < 4; ++u) v[u] = from.ask(u0 + (u << p.lg), true);
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int c = skew + (u0 + (u << p.lg)) * 16;
-            if (c < p.width) put16<XT, false>(out, c, p.width, v[u]);
+            if (c < p.width) put16<XT, false>(out, c, p.width, from.unit(v[u]));
           }
         }
       }
@@ -370,7 +382,7 @@ __global__ void __launch_bounds__(NODES_THREADS) gather_rows_kernel(const __grid
 // out[i] = sum_j weights[i, j] sorted[where[i, j]], j ascending, in fp32. Places without a position are left out, whatever their weight.
 // Four units are under way at a time, of PLACES places each (rows of more places have them found anew for each unit). Bounds: bytes.
 template <typename XT, bool ALIGNED, int PLACES>
-__global__ void __launch_bounds__(NODES_THREADS) combine_rows_kernel(const __grid_constant__ NodesParams p) {
+__global__ void __launch_bounds__(NODES_THREADS, 4) combine_rows_kernel(const __grid_constant__ NodesParams p) {
   constexpr int V = XVec<XT>::V, UNITS = !ALIGNED ? 1 : PLACES == 1 ? 4 : 2;
   kernel_started();
   kernel_inputs_ready();
@@ -387,7 +399,7 @@ __global__ void __launch_bounds__(NODES_THREADS) combine_rows_kernel(const __gri
         const int pos = j + a < p.top ? position(p, i * p.top + j + a, t == 0) : -1;
         at[a] = pos >= 0 ? p.sorted + pos * p.ld_sorted : nullptr;
         w[a] = pos >= 0 && p.weights ? __ldg(p.weights + i * p.top + j + a) : 1.0f;
-        if (!ALIGNED && pos >= 0) from[a].find(at[a], p.width, skew);
+        if (!ALIGNED) from[a].find(pos >= 0 ? at[a] : p.sorted, p.width, skew);
       }
     };
     if (p.top <= PLACES) find(0);
@@ -400,13 +412,22 @@ __global__ void __launch_bounds__(NODES_THREADS) combine_rows_kernel(const __gri
       for (int j = 0; j < p.top; j += PLACES) {
         if (p.top > PLACES) find(j);
         uint4 v[UNITS][PLACES];
+        if constexpr (ALIGNED) {
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u)
+          for (int u = 0; u < UNITS; ++u)
 #pragma unroll
-          for (int a = 0; a < PLACES; ++a) {
-            if constexpr (ALIGNED) v[u][a] = ld_stream16_if(at[a] + (u0 + u * g) * 16, at[a] != nullptr && (u0 + u * g) * 16 < p.width);
-            else if (at[a]) v[u][a] = from[a].unit(u0 + u * g);
-          }
+            for (int a = 0; a < PLACES; ++a) v[u][a] = ld_stream16_if(at[a] + (u0 + u * g) * 16, at[a] != nullptr && (u0 + u * g) * 16 < p.width);
+        } else {
+          typename ShiftedRow<XT>::Raw raw[UNITS][PLACES];
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+            for (int a = 0; a < PLACES; ++a) raw[u][a] = from[a].ask(u0 + u * g, at[a] != nullptr);
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+            for (int a = 0; a < PLACES; ++a) v[u][a] = from[a].unit(raw[u][a]);
+        }
 #pragma unroll
         for (int a = 0; a < PLACES; ++a) {
           if (!at[a]) continue;
@@ -492,19 +513,25 @@ __global__ void __launch_bounds__(NODES_THREADS) combine_grad_kernel(const __gri
           ShiftedRow<XT> ds, fs;
           ds.find(row, p.width, skew);
           fs.find(p.sorted + pos[a] * p.ld_sorted, p.width, skew);
-#pragma unroll 2
-          for (int u = t; skew + u * 16 < p.width; u += g) {
-            float d[V], f[V], o[V];
-            const int c = skew + u * 16;
-            XVec<XT>::widen(ds.unit(u), d);
-            XVec<XT>::widen(fs.unit(u), f);
+          for (int u0 = t; skew + u0 * 16 < p.width; u0 += 2 * g) {
+            typename ShiftedRow<XT>::Raw dr[2], fr[2];
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-              const bool in = (unsigned)(c + e * (int)sizeof(XT)) < (unsigned)p.width;
-              dot[a] = fmaf(in ? d[e] : 0.0f, in ? f[e] : 0.0f, dot[a]);
-              o[e] = w[a] * d[e];
+            for (int u = 0; u < 2; ++u) dr[u] = ds.ask(u0 + u * g, true), fr[u] = fs.ask(u0 + u * g, true);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int c = skew + (u0 + u * g) * 16;
+              if (c >= p.width) break;
+              float d[V], f[V], o[V];
+              XVec<XT>::widen(ds.unit(dr[u]), d);
+              XVec<XT>::widen(fs.unit(fr[u]), f);
+#pragma unroll
+              for (int e = 0; e < V; ++e) {
+                const bool in = (unsigned)(c + e * (int)sizeof(XT)) < (unsigned)p.width;
+                dot[a] = fmaf(in ? d[e] : 0.0f, in ? f[e] : 0.0f, dot[a]);
+                o[e] = w[a] * d[e];
+              }
+              put16<XT, false>(out, c, p.width, narrow16<XT>(o));
             }
-            put16<XT, false>(out, c, p.width, narrow16<XT>(o));
           }
         }
       }
