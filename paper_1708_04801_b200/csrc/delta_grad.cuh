@@ -123,6 +123,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
       to[4 * DK] = hi[1];
       to[4] = hi[2];
       to[4 * DK + 4] = hi[3];
+      if (NW == 8 && i == 0 && !gp.dW) continue;  // a gradient of zeros: nothing to multiply
 #pragma unroll
       for (int y = 0; y < 4; ++y) ldsm(b[y], k_at + wide(nk, y, x));
 #pragma unroll
