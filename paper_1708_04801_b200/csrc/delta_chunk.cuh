@@ -508,6 +508,11 @@ struct DeltaSpan {
   long long row0, rows;
   __device__ __forceinline__ int len(int i) const { return (int)min((long long)DC, rows - (long long)i * DC); }
 };
+// From the list of chunks, which was checked: the offsets may have changed since a run that a gradient follows
+__device__ __forceinline__ DeltaSpan span_of(const DeltaChunkParams& p, int first, int n) {
+  if (n == 0) return {0, 0};
+  return {p.chunks[first].row0, (long long)(n - 1) * DC + p.chunks[first + n - 1].len};
+}
 // Tensor maps of the rows of all heads of features and queries: whole chunks come by them where a head has all the features of its tiles. (All of a chunk by 16-byte copies of the warps
 // cost 200 of 850 us for 65536 rows of 16 heads: they share the way to shared memory with the operands.)
 struct DeltaMaps {
@@ -609,7 +614,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
-  const DeltaSpan span = {p.shard_off[chain], p.shard_off[chain + 1] - p.shard_off[chain]};
+  const DeltaSpan span = span_of(p, first, n);
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&bars[s].rows, 32 * (COPIERS ? Shape::copiers : warps));

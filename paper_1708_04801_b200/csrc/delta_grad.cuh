@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
   const int slice = blockIdx.x % p.slices, h = blockIdx.x / p.slices % p.hv, chain = p.order[blockIdx.x / p.slices / p.hv], kh = h / (p.hv / p.hk);
   const int col0 = slice * 16 * NW, warps = min(NW, (p.dvp - col0) / 16);  // warps with labels
   const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
-  const DeltaSpan span = {p.shard_off[chain], p.shard_off[chain + 1] - p.shard_off[chain]};
+  const DeltaSpan span = span_of(p, first, n);
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&bars[s].rows, 32 * (COPIERS ? Shape::copiers : warps));

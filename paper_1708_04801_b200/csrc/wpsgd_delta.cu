@@ -74,7 +74,7 @@ wpsgd_status run_step(wpsgd_ctx* c, const DeltaRowsParams& p) {
   if (grid > INT32_MAX) return fail(c, WPSGD_ERR_UNSUPPORTED, "delta_step: too many models");
   auto go = [&](auto nj) {
     constexpr int NJ = decltype(nj)::value;
-return launch(delta_step_kernel<XT, NJ>, (unsigned)grid, STEP_THREADS, 0, c->stream, p);
+    return launch(delta_step_kernel<XT, NJ>, (unsigned)grid, STEP_THREADS, 0, c->stream, p);
   };
   CU_TRY(c, p.dk <= 32 ? go(std::integral_constant<int, 1>()) : p.dk <= 64 ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 4>()));
   c->launches++;
