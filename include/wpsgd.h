@@ -328,10 +328,10 @@ wpsgd_status wpsgd_combine_rows_grad(wpsgd_ctx* ctx, const void* dout, int64_t l
  * Rows: all of one type, DEVICE, row t of q at q + t * ld_q: q, k [n_rows, heads_k, dk], v [n_rows, heads_v, dv], g, beta [n_rows, heads_v], heads one behind
  * the other. Rows outside every chain are not read. dk and dv at most 128 (WPSGD_ERR_UNSUPPORTED). g is at most 0 in use; below -128 it counts as -128 (its
  * exponential is 0 in fp32). Lengths and offsets are read on the device: offsets that decrease or leave [0, n_rows] are reported by the next wpsgd_check
- * (WPSGD_ERR_CUDA), and nothing is computed.
+ * (WPSGD_ERR_CUDA); the chains concerned, or all of them, are left out then.
  *
  * Models are fp32, [n_chains, heads_v, dv, dk], and are kept in fp32 on the way. bf16 rows are taken 64 at a time on the tensor cores: products with
- * models, with the inverse of a chunk's triangular system and with its steps split their fp32 side into two bf16 parts (relative error of the models 3e-6 or so
+ * models, with the inverse of a chunk's triangular system and with its steps split their fp32 side into two bf16 parts (relative error of the models 4e-6
  * against 64 bits), answers and gradients use some operands rounded to bf16 once. fp32 rows are taken one by one in fp32. A NaN or an infinity stays in its
  * chain and head; in bf16 rows it can reach the answers of up to 15 rows before it.
  *

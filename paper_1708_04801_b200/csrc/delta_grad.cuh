@@ -274,7 +274,9 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
   unsigned char* stages = (unsigned char*)(cols + 4 * DC);
   float* totals = gp.totals + (size_t)blockIdx.x * Shape::totals;  // where several heads share features
   __shared__ float model_dots[ROWS_THREADS / 32];
-  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3, wr = warp & 3, wc = warp >> 2;
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
+  // block of 16 rows and quarter of the columns. The ten warps with a block of F and E come first, so that no scheduler has more than three of them
+  const int up = warp - 10, wr = warp < 10 ? (warp >= 1) + (warp >= 3) + (warp >= 6) : (up >= 3) + (up >= 5), wc = warp < 10 ? warp - wr * (wr + 1) / 2 : up < 3 ? up + 1 : up < 5 ? up - 1 : 3;
   kernel_inputs_ready();
   const int slices = (p.dvp + ROWS_SLICE - 1) / ROWS_SLICE;
   // Pieces: all heads of labels of a (chunk, head of features), then the next of this block's. What a copy needs is kept beside them: a piece changes once in
