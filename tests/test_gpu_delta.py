@@ -347,6 +347,55 @@ def test_gradients_of_strided_rows_and_at_the_ends_of_the_gates(ctx):
     assert all(v <= GRAD_NORM for v in away.values()), away
 
 
+@pytest.mark.parametrize("dtype,width,at", [(torch.bfloat16, 1 << 20, 0), (torch.bfloat16, (1 << 20) + 1, 3), (torch.float32, 1 << 19, 0)])
+def test_rows_that_lie_past_32_bits(ctx, dtype, width, at):
+    # slices of one tensor of 2^31 elements and more; the same rows one behind the other give the same bits
+    lengths, hk, hv, dk, dv = [2000, 63, 2041], 2, 4, 128, 64
+    n, off = sum(lengths), offsets(lengths).cuda()
+    rows = [x.cuda() for x in make(n, hk, hv, dk, dv, dtype, 31)]
+    wide = torch.empty((n + 1, width), dtype=dtype, device="cuda")
+    far_rows, c = [], at
+    for x in rows + [rows[2], rows[2]]:  # and places for the answers and their gradient
+        far_rows.append(wide[1:, c:c + x[0].numel()].unflatten(1, x.shape[1:]))
+        far_rows[-1].copy_(x)
+        c += (x[0].numel() + 7) // 8 * 8
+    save = dtype is torch.bfloat16
+    want = ctx.delta_run(*rows, off, save=save)
+    got = ctx.delta_run(*far_rows[:5], off, out=far_rows[5], save=save)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    if save:
+        assert all(torch.equal(a, b) for a, b in zip(ctx.delta_grad(got[2], far_rows[6])[:5], ctx.delta_grad(want[2], rows[2])[:5]))
+    ctx.check()
+
+
+def test_workspaces_and_models_past_32_bits(ctx):
+    lengths, hk, hv, dk, dv = [4000] * 104 + [77, 4003], 2, 16, 128, 128
+    n, off = sum(lengths), offsets(lengths)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v, gate, beta, dout = (torch.randn(s, generator=g, device="cuda", dtype=torch.bfloat16) for s in ((n, hk, dk), (n, hk, dk), (n, hv, dv), (n, hv), (n, hv), (n, hv, dv)))
+    rows = [q / 11, k / 11, v, -gate.abs(), torch.sigmoid(beta)]
+    out, W, saved = ctx.delta_run(*rows, off.cuda(), save=True)
+    assert saved.args[-1].numel() > 1 << 32
+    got = ctx.delta_grad(saved, dout)[:5]
+    a, b = len(lengths) - 2, len(lengths)
+    part = slice(int(off[a]), int(off[b]))
+    few = [x[part].contiguous() for x in rows]
+    o, w, kept = ctx.delta_run(*few, (off[a:b + 1] - off[a]).cuda(), save=True)
+    assert torch.equal(out[part], o) and torch.equal(W[a:b], w)
+    assert all(torch.equal(x[part], y) for x, y in zip(got, ctx.delta_grad(kept, dout[part].contiguous())[:5]))
+    # single rows on models of which the last lie past 2^31 elements
+    del saved, got
+    slots = (1 << 31) // (hv * dv * dk) + 5
+    pool = torch.zeros((slots, hv, dv, dk), device="cuda")
+    pool[-2:] = w
+    one = [x[-2:].contiguous() for x in rows]
+    mine = w.clone()
+    want = ctx.delta_step(*one, mine)
+    answer = ctx.delta_step(*one, pool, torch.tensor([slots - 2, slots - 1], dtype=torch.int32).cuda())
+    ctx.check()
+    assert torch.equal(answer, want) and torch.equal(pool[-2:], mine) and float(pool[:-2].abs().max()) == 0.0
+
+
 # ---- all of it together ------------------------------------------------------------------------------------------------------------
 def test_rows_to_chains_and_back_with_gradients(ctx):
     """A router's rows sorted by chain, run through them, brought back with weights, and the gradients all the way to the inputs."""
