@@ -34,10 +34,11 @@ namespace wpsgd {
 constexpr int DC = 64;             // rows of a chunk
 constexpr int DC_TILE = DC + 8;    // elements from row to row of a 64 x 64 tile in shared memory: ldmatrix reads 8 rows from 8 different bank groups
 constexpr int DC_TILE_BYTES = DC * DC_TILE * 2;
-// Lower triangles are kept as their ten blocks of 16 x 16, 512 bytes each, block (i, j) at i (i + 1) / 2 + j. A row of a block is two units of 16 bytes, swapped in rows 4 to 7 and
-// 12 to 15, so that the 8 rows that ldmatrix reads at a time lie in different banks.
+// Lower triangles are kept as their ten blocks of 16 x 16, 512 bytes each, column by column: the blocks of a column of blocks are 16 to 64 rows of one
+// operand of tcgen05. A row of a block is two units of 16 bytes, swapped in rows 4 to 7 and 12 to 15 (the swizzle of 32 bytes), so that the 8 rows that ldmatrix reads at a time lie in
+// different banks.
 constexpr int DC_TRI = 10 * 512;
-__host__ __device__ constexpr int tri_at(int i, int j) { return (i * (i + 1) / 2 + j) * 512; }
+__host__ __device__ constexpr int tri_at(int i, int j) { return (i + j * (7 - j) / 2) * 512; }
 __device__ __forceinline__ int tri_unit(int row, int half) { return row * 32 + ((half ^ (row >> 2 & 1)) << 4); }
 // What the first kernel leaves for each chunk and head, brought by one copy: T and P in two parts each, the factors of the rows. b is held as b log2(e) = hi + lo
 // (its sums are formed in 64 bits): D_ij = 2^{(hi_i - hi_j) + (lo_i - lo_j)} is then as good as its fp32 exponent.
@@ -72,7 +73,7 @@ struct DeltaChunkParams {
   int* order;          // [n_chains]: longest first
   DeltaChunk* chunks;  // [chunk_off[n_chains]]
   unsigned char* blocks;        // [chunks][hv][DC_BLOCK]
-  __nv_bfloat16* starts;        // [chunks][hv][dvp][DK]: models before the chunk, for the gradient
+  __nv_bfloat16* starts;        // [chunks][hv][DK / 8][dvp][8]: models before the chunk, for the gradient
   __nv_bfloat16* steps;         // [chunks][hv][DC][dvp]: U
   unsigned char* gram;          // [chunks][hv][DC_TRI]: D_ij k_i.k_j, for the gradient; NULL where it is not kept
   const float* W0;
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       if (n > warp) break;
-      unsigned char* to = tris + (warp * (warp + 1) / 2 + n) * 512;
+      unsigned char* to = tris + tri_at(warp, n);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int col = n * 16 + i * 8 + 2 * t;
@@ -387,7 +388,7 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
           *(uint32_t*)(to + P_AT + unit) = h2;
           *(uint32_t*)(to + P_AT + DC_TRI + unit) = l2;
           const float k0 = d0 * kk[n][i][e], k1 = d1 * kk[n][i][e + 1], a0 = be * k0, a1 = be * k1;
-          if (p.gram) *(uint32_t*)(p.gram + ((long long)chunk * p.hv + h) * DC_TRI + (warp * (warp + 1) / 2 + n) * 512 + unit) = pack2(k0, k1);
+          if (p.gram) *(uint32_t*)(p.gram + ((long long)chunk * p.hv + h) * DC_TRI + tri_at(warp, n) + unit) = pack2(k0, k1);
           if (n == warp) {
             float* a = diag + (warp * 16 + g + 4 * e) * 17 + i * 8 + 2 * t;
             a[0] = a0;  // the substitution reads below the diagonal only
@@ -403,7 +404,7 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
     __syncwarp();
     if (lane < 16) {  // column `lane` of the warp's diagonal block
       const float* a = diag + warp * 16 * 17;
-      unsigned char* to = tris + T_AT + (warp * (warp + 1) / 2 + warp) * 512;
+      unsigned char* to = tris + T_AT + tri_at(warp, warp);
       float x[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
     __syncthreads();
     const uint32_t nk = smem32(tris) + tri_nk(lane);
     if (warp & 1) {  // blocks (1, 0) and (3, 2)
-      const int o = warp - 1, d0 = (o * (o + 1) / 2 + o) * 512, d1 = (warp * (warp + 1) / 2 + warp) * 512, od = (warp * (warp + 1) / 2 + o) * 512;
+      const int o = warp - 1, d0 = tri_at(o, o), d1 = tri_at(warp, warp), od = tri_at(warp, o);
       float x[2][4] = {}, y[2][4] = {};
       uint32_t ah[4], al[4], bh[4], bl[4];
       ldsm_t(ah, nk + T_AT + d0);
@@ -442,7 +443,7 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
 #pragma unroll
       for (int m = 0; m < 2; ++m) {  // X^T = T_00^T A_10^T over rows of T_00 from its diagonal on
         if (m < j) continue;
-        const int tt = (m * (m + 1) / 2 + j) * 512;
+        const int tt = tri_at(m, j);
         ldsm_t(ah, nk + T_AT + tt);
         ldsm_t(al, nk + T_AT + DC_T_LO + tt);
 #pragma unroll
@@ -456,13 +457,13 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         if (m > i) continue;
-        const int tt = ((2 + i) * (3 + i) / 2 + 2 + m) * 512;
+        const int tt = tri_at(2 + i, 2 + m);
         a_parts(x[2 * m], x[2 * m + 1], ah, al);
         ldsm(bh, nk + T_AT + tt);
         ldsm(bl, nk + T_AT + DC_T_LO + tt);
         mma_split(y[0], y[1], ah, al, bh, bl);
       }
-      put_negative_t(nk + T_AT + ((2 + i) * (3 + i) / 2 + j) * 512, y[0], y[1]);
+      put_negative_t(nk + T_AT + tri_at(2 + i, j), y[0], y[1]);
     }
     __syncthreads();
     for (int u = tid; u < 4 * DC_TRI / 16; u += PREP_THREADS) *(uint4*)(block + u * 16) = *(const uint4*)(tris + u * 16);
@@ -557,7 +558,7 @@ __device__ __forceinline__ void bulk_done(ChunkBarriers* bars, int from, int to)
 // A copying warp's work: its share of all n chunks, the last first where `back`
 template <int DK, int NW>
 __device__ __forceinline__ void bring_chunks(const DeltaChunkParams& p, const DeltaMaps& maps, const DeltaHeads& labels, uint32_t smem, int first, bool back, int n, const DeltaSpan& span, int h,
-                                             int kh, int col0, int warp, int lane, ChunkBarriers* bars) {
+                                             int kh, int col0, int warp, int warps, int lane, ChunkBarriers* bars) {
   using Shape = ChainShape<DK, NW>;
   int brought = 0;
   for (int i = 0; i < n; ++i) {
@@ -568,7 +569,7 @@ __device__ __forceinline__ void bring_chunks(const DeltaChunkParams& p, const De
     }
     if (i == p.drop) break;  // a test hook: this chunk and those behind it are never brought
     const int j = back ? n - 1 - i : i;
-    bring_chunk<DK, NW>(p, maps, labels, smem + s * Shape::stage, first + j, span, j, h, kh, col0, warp, Shape::copiers, lane, &bars[s]);
+    bring_chunk<DK, NW>(p, maps, labels, smem + s * Shape::stage, first + j, span, j, h, kh, col0, warp, warps, lane, &bars[s]);
     brought = i + 1;
   }
   copies_done();
@@ -625,7 +626,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
   }
   __syncthreads();
   if (COPIERS && warp >= NW) {
-    bring_chunks<DK, NW>(p, maps, p.v, smem32(ring), first, false, n, span, h, kh, col0, warp - NW, lane, bars);
+    bring_chunks<DK, NW>(p, maps, p.v, smem32(ring), first, false, n, span, h, kh, col0, warp - NW, Shape::copiers, lane, bars);
     return;
   }
   if (warp >= warps) return;
@@ -685,11 +686,11 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
       uint32_t hi[4], lo[4], b[4][4];
       a_parts(S[2 * x], S[2 * x + 1], hi, lo);
       if (SAVE) {  // models before the chunk, one bf16 part
-        uint32_t* to = (uint32_t*)(p.starts + (which * p.dvp + label) * DK + 16 * x + 2 * t);
+        uint32_t* to = (uint32_t*)(p.starts + ((which * (DK / 8) + 2 * x) * p.dvp + label) * 8 + 2 * t);
         to[0] = hi[0];
-        to[4 * DK] = hi[1];
-        to[4] = hi[2];
-        to[4 * DK + 4] = hi[3];
+        to[32] = hi[1];
+        to[4 * p.dvp] = hi[2];
+        to[4 * p.dvp + 32] = hi[3];
       }
       if (zero) continue;
 #pragma unroll

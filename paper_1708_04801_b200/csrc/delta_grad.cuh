@@ -28,7 +28,7 @@ namespace wpsgd {
 
 struct DeltaGradParams {
   DeltaChunkParams f;
-  __nv_bfloat16* ends;   // [chunks][hv][dvp][DK]: G behind the chunk
+  __nv_bfloat16* ends;   // [chunks][hv][DK / 8][dvp][8]: G behind the chunk
   __nv_bfloat16* drs;    // [chunks][hv][DC][dvp]: dR
   float* totals;         // [blocks][2][DC][DK]: sums over the heads of labels that share features
   const float* dW;
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
   }
   __syncthreads();
   if (COPIERS && warp >= NW) {
-    bring_chunks<DK, NW>(p, maps, p.dout, smem32(ring), first, true, n, span, h, kh, col0, warp - NW, lane, bars);
+    bring_chunks<DK, NW>(p, maps, p.dout, smem32(ring), first, true, n, span, h, kh, col0, warp - NW, Shape::copiers, lane, bars);
     return;
   }
   if (warp >= warps) return;
@@ -118,11 +118,11 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
     for (int x = 0; x < DK / 16; ++x) {
       uint32_t hi[4], lo[4], b[4][4];
       a_parts(G[2 * x], G[2 * x + 1], hi, lo);
-      uint32_t* to = (uint32_t*)(gp.ends + (which * p.dvp + label) * DK + 16 * x + 2 * t);
+      uint32_t* to = (uint32_t*)(gp.ends + ((which * (DK / 8) + 2 * x) * p.dvp + label) * 8 + 2 * t);
       to[0] = hi[0];
-      to[4 * DK] = hi[1];
-      to[4] = hi[2];
-      to[4 * DK + 4] = hi[3];
+      to[32] = hi[1];
+      to[4 * p.dvp] = hi[2];
+      to[4 * p.dvp + 32] = hi[3];
       if (NW == 8 && i == 0 && !gp.dW) continue;  // a gradient of zeros: nothing to multiply
 #pragma unroll
       for (int y = 0; y < 4; ++y) ldsm(b[y], k_at + wide(nk, y, x));
@@ -314,8 +314,8 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     if (w.chunk >= chunks) return;
     const int h = w.kh * more + w.hh;
     const long long which = (long long)w.chunk * p.hv + h, kept = (which * DC + row_l) * p.dvp + col_l, i = w.row0 + (row_l < w.len ? row_l : 0);
-    from_s = p.starts + which * p.dvp * DK + tid * 8;
-    from_g = gp.ends + which * p.dvp * DK + tid * 8;
+    from_s = p.starts + which * p.dvp * DK;
+    from_g = gp.ends + which * p.dvp * DK;
     from_u = p.steps + kept;
     from_r = gp.drs + kept;
     from_o = p.dout.p + i * p.dout.ld + h * p.dout.width + col_l;
@@ -327,10 +327,10 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     const uint32_t st = smem32(stages) + ring * Shape::stage;
 #pragma unroll
     for (int u = tid; u < ROWS_SLICE * (DK / 8); u += ROWS_THREADS) {
-      const int at_l = u / (DK / 8), col = u % (DK / 8) * 8;
+      const int at_l = u % ROWS_SLICE, unit = u / ROWS_SLICE, from = (unit * p.dvp + at_l) * 8;
       const bool there = l0 + at_l < p.dvp;
-      copy16(st + (at_l * ROW + col) * 2, there ? from_s + (u - tid) * 8 : p.starts, there);
-      copy16(st + Shape::models + (at_l * ROW + col) * 2, there ? from_g + (u - tid) * 8 : gp.ends, there);
+      copy16(st + (at_l * ROW + unit * 8) * 2, there ? from_s + from : p.starts, there);
+      copy16(st + Shape::models + (at_l * ROW + unit * 8) * 2, there ? from_g + from : gp.ends, there);
     }
     const uint32_t to = st + 2 * Shape::models + (row_l * VROW + col_l) * 2;
     const bool there = l < p.dvp, given = row_l < w.len && l < p.v.width;  // labels and their gradients are of one width, rounded up to 8
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     copy16(to + Shape::labels, there ? from_r : gp.drs, there);
     copy16(to + 2 * Shape::labels, given ? from_o : p.dout.p, given);
     copy16(to + 3 * Shape::labels, given ? from_v : p.v.p, given);
-    from_s += ROWS_SLICE * DK, from_g += ROWS_SLICE * DK, from_u += ROWS_SLICE, from_r += ROWS_SLICE, from_o += ROWS_SLICE, from_v += ROWS_SLICE;
+    from_s += ROWS_SLICE * 8, from_g += ROWS_SLICE * 8, from_u += ROWS_SLICE, from_r += ROWS_SLICE, from_o += ROWS_SLICE, from_v += ROWS_SLICE;
   };
   auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
 
@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
 #pragma unroll
     for (int y = 0; y < PAIRS; ++y) {
       if (PAIRS * wc + y > wr) break;
-      const int at_tri = (wr * (wr + 1) / 2 + PAIRS * wc + y) * 512;
+      const int at_tri = tri_at(wr, PAIRS * wc + y);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int j = (PAIRS * wc + y) * 16 + 8 * x + 2 * t;
@@ -522,13 +522,13 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
         if (t == 0) sums[(wc * DC + i0 + 8 * z) * 3 + d] = v;
       }
     const uint32_t k_mk = smem32(Ks) + lane_mk(lane, ROW) + colw * 2, q_mk = smem32(Qs) + lane_mk(lane, ROW) + colw * 2;
-    const uint32_t f_mk = smem32(Fs) + tri_mk(lane) + wr * (wr + 1) / 2 * 512, f_nk = smem32(Fs) + tri_nk(lane) + wr * 512;
+    const uint32_t f_mk = smem32(Fs) + tri_mk(lane) + tri_at(wr, 0), f_nk = smem32(Fs) + tri_nk(lane) + tri_at(0, wr);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       uint32_t a[4], e[4], b[4];
       if (x <= wr) {  // rows of F and E: dQ and x
-        ldsm(a, f_mk + x * 512);
-        ldsm(e, f_mk + DC_TRI + x * 512);
+        ldsm(a, f_mk + tri_at(0, x));
+        ldsm(e, f_mk + DC_TRI + tri_at(0, x));
 #pragma unroll
         for (int y = 0; y < NT / 2; ++y) {
           ldsm_t(b, k_mk + x * 16 * ROW * 2 + y * 32);

@@ -1,0 +1,347 @@
+// The walk over a chain's chunks by tcgen05: all labels of a head (up to 128) are the lanes of tensor memory (see delta_chunk.cuh for the mathematics).
+//
+// Everything that ties one product to the next has labels as rows: S^T [labels x features], R^T and U^T [labels x 64]. They are A operands in tensor memory, written there by
+// eight warps that take the accumulators out (a thread has a label and half of the columns), so that K, Q, T and P, as they lie in shared memory, are B operands of all
+// products: K and Q tiles of 128 bytes a row with the 128-byte swizzle (K once with features as k and once with rows as k), T and P columns of 16 x 16 blocks with the 32-byte swizzle. A
+// chunk is a string of three products with the warps' work between them: R^T = S^T K^T (two parts of S), U^T = R^T T^T (three pairs of parts, columns from the block on), and
+// dS^T = (r U)^T K (two parts); S^T Q^T and U^T P^T run beside it, and the answers leave while the next chunk's first product runs. S stays in registers in fp32.
+//
+// Roles: warps 0 to 7 as above, three warps that bring the chunks, one thread that issues the products.
+#pragma once
+
+#include "delta_chunk.cuh"
+#include "tmem.cuh"
+
+namespace wpsgd {
+
+constexpr int WALK_LABELS = 128, WALK_WARPS = 8, WALK_COPIERS = 3, WALK_THREADS = 32 * (WALK_WARPS + WALK_COPIERS + 1);
+constexpr uint32_t WALK_COLUMNS = 512;
+// Columns of tensor memory. fp32: dS, R and then U, the answers. bf16: two parts each of S, of R and then r U, of U.
+constexpr uint32_t TM_DS = 0, TM_R = 128, TM_O = 192, TM_S = 256, TM_S_LO = 320, TM_RH = 384, TM_RL = 416, TM_UH = 448, TM_UL = 480;
+
+// A wait that gives up after its own limit, or when another role has. False: leave.
+struct WalkWait {
+  long long limit;
+  volatile int* dead;
+  __device__ __forceinline__ bool operator()(unsigned long long* bar, uint32_t parity) const {
+    for (long long i = 0; i < limit; ++i) {
+      if (mbar_try_wait(bar, parity)) return true;
+      if (*dead) break;
+    }
+    return false;
+  }
+  __device__ __forceinline__ bool warp(unsigned long long* bar, uint32_t parity) const { return __all_sync(0xffffffffu, (*this)(bar, parity)); }
+};
+
+// What the roles tell each other: products done (one arrival each), operands written or accumulators read (one of each warp)
+struct WalkBarriers {
+  unsigned long long r_done, q_done, u_done, s_done, o_done, s_there, r_there, u_there, o_read, drained;
+};
+
+// 32 fp32 to two bf16 parts
+__device__ __forceinline__ void split32(const float (&x)[32], uint32_t (&hi)[16], uint32_t (&lo)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) split2(x[2 * i], x[2 * i + 1], hi[i], lo[i]);
+}
+
+template <int DK, bool SAVE>
+__global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __grid_constant__ DeltaChunkParams p, const __grid_constant__ DeltaMaps maps) {
+  using Shape = ChainShape<DK, 8>;
+  constexpr int STAGES = Shape::stages, HALF = DK / 2;  // features of a thread
+  extern __shared__ unsigned char chain_smem[];
+  __shared__ ChunkBarriers bars[STAGES];
+  __shared__ WalkBarriers w;
+  __shared__ uint32_t tmem_base;
+  __shared__ int dead_flag;
+  volatile int* dead = &dead_flag;
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
+  unsigned char* const ring = chain_smem + (-smem32(chain_smem) & 1023u);
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&bars[s].rows, 32 * WALK_COPIERS);
+      mbar_init(&bars[s].bulk, 1);
+      mbar_init(&bars[s].empty, WALK_WARPS + 1);
+    }
+    for (unsigned long long* b : {&w.r_done, &w.q_done, &w.u_done, &w.s_done, &w.o_done, &w.drained}) mbar_init(b, 1);
+    for (unsigned long long* b : {&w.s_there, &w.r_there, &w.u_there, &w.o_read}) mbar_init(b, WALK_WARPS);
+    dead_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == WALK_WARPS + WALK_COPIERS) tmem_alloc(&tmem_base, WALK_COLUMNS);
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tm = tmem_base;
+  kernel_inputs_ready();
+  const int h = blockIdx.x % p.hv, chain = p.order[blockIdx.x / p.hv], kh = h / (p.hv / p.hk);
+  const int first = p.chunk_off[chain], n = p.chunk_off[chain + 1] - first;
+  const DeltaSpan span = span_of(p, first, n);
+  const WalkWait wait = {p.spin_limit, dead};
+  auto give_up = [&](int i) {
+    *dead = 1;
+    set_status(p.status, DEV_TIMEOUT, 25, i);
+  };
+
+  if (warp >= WALK_WARPS && warp < WALK_WARPS + WALK_COPIERS) {
+    bring_chunks<DK, 8>(p, maps, p.v, smem32(ring), first, false, n, span, h, kh, 0, warp - WALK_WARPS, WALK_COPIERS, lane, bars);
+  } else if (warp == WALK_WARPS + WALK_COPIERS) {
+    if (elect_one()) {
+      int i = 0;
+      for (; i < n; ++i) {
+        const int s = i % STAGES;
+        const uint32_t k_at = smem32(ring + s * Shape::stage), q_at = k_at + Shape::q_at, t_at = k_at + Shape::block_at;
+        if (!wait(&bars[s].bulk, (i / STAGES) & 1) || !wait(&bars[s].rows, (i / STAGES) & 1) || !wait(&w.s_there, i & 1)) break;
+        if (!p.maps || span.len(i) < DC) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // features and queries that threads have copied
+        tmem_fence_after();
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int x = 0; x < DK / 16; ++x)
+            mma_bf16(tm + TM_R, tm + (part ? TM_S_LO : TM_S) + 8 * x, mma_operand(k_at + x / 4 * WIDE_BYTES + x % 4 * 32), mma_shape16(DC, false), part || x);
+        mma_commit(&w.r_done);
+        if (i > 0 && !wait(&w.o_read, (i - 1) & 1)) break;
+        tmem_fence_after();
+#pragma unroll
+        for (int x = 0; x < DK / 16; ++x) mma_bf16(tm + TM_O, tm + TM_S + 8 * x, mma_operand(q_at + x / 4 * WIDE_BYTES + x % 4 * 32), mma_shape16(DC, false), x > 0);
+        mma_commit(&w.q_done);
+        // a triangle's column of blocks x: rows of the result from 16 x on
+        auto triangle = [&](uint32_t d, uint32_t hi, uint32_t lo, uint32_t at, bool add) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            mma_bf16(tm + d + 16 * x, tm + hi + 8 * x, mma_operand32(at + tri_at(x, x)), mma_shape16(DC - 16 * x, false), add || x);
+            mma_bf16(tm + d + 16 * x, tm + lo + 8 * x, mma_operand32(at + tri_at(x, x)), mma_shape16(DC - 16 * x, false), true);
+            mma_bf16(tm + d + 16 * x, tm + hi + 8 * x, mma_operand32(at + DC_T_LO + tri_at(x, x)), mma_shape16(DC - 16 * x, false), true);
+          }
+        };
+        if (!wait(&w.r_there, i & 1)) break;
+        tmem_fence_after();
+        triangle(TM_R, TM_RH, TM_RL, t_at, false);
+        mma_commit(&w.u_done);
+        if (!wait(&w.u_there, i & 1)) break;
+        tmem_fence_after();
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) mma_bf16(tm + TM_DS, tm + (part ? TM_RL : TM_RH) + 8 * x, mma_operand_outer(k_at + x * 2048, WIDE_BYTES), mma_shape16(DK, true), part || x);
+        mma_commit(&w.s_done);
+        triangle(TM_O, TM_UH, TM_UL, t_at + DC_P, true);
+        mma_commit(&w.o_done);
+        mma_commit(&bars[s].empty);
+      }
+      if (i < n) give_up(i);
+      mma_commit(&w.drained);  // what was issued is done before tensor and shared memory go
+      mbar_wait_bounded(&w.drained, 0, DRAIN_LIMIT);
+    }
+    __syncwarp();
+  } else {
+    const uint32_t lanes = tm + ((uint32_t)(warp & 3) << 21);  // the warp's 32 lanes
+    const int half = warp >> 2, label = (warp & 3) * 32 + lane, t0 = half * 32, f0 = half * HALF;
+    const bool there = label < p.dv;
+    const long long model = (((long long)chain * p.hv + h) * p.dv + label) * p.dk;
+    const bool vec = p.dk % 4 == 0 && (((uintptr_t)p.W0 | (uintptr_t)p.W) & 15) == 0;
+    float S[HALF];
+#pragma unroll
+    for (int x = 0; x < HALF; x += 4) {
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (p.W0 && there) {
+        const float* from = p.W0 + model + f0 + x;
+        const int left = p.dk - f0 - x;
+        if (vec) {
+          if (left > 0) v = *(const float4*)from;
+        } else {
+          if (left > 0) v.x = from[0];
+          if (left > 1) v.y = from[1];
+          if (left > 2) v.z = from[2];
+          if (left > 3) v.w = from[3];
+        }
+      }
+      S[x] = v.x, S[x + 1] = v.y, S[x + 2] = v.z, S[x + 3] = v.w;
+    }
+    // 32 labels of 32 rows: from threads that have a label each, by way of the place where the warp's labels came in, to rows in memory
+    const int labels0 = (warp & 3) * 32;
+    auto turn = [&](const uint32_t (&words)[16], int s) {
+      unsigned short* at = (unsigned short*)(ring + s * Shape::stage + Shape::v_at) + t0 * Shape::vrow + label;
+      __syncwarp();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        at[2 * e * Shape::vrow] = (unsigned short)words[e];
+        at[(2 * e + 1) * Shape::vrow] = (unsigned short)(words[e] >> 16);
+      }
+      __syncwarp();
+    };
+    auto rows_out = [&](auto vec, int s, __nv_bfloat16* to, long long ld, int rows, int cols) {
+      const unsigned char* from = ring + s * Shape::stage + Shape::v_at + (t0 * Shape::vrow + labels0) * 2;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int row = 8 * u + lane / 4, col = lane % 4 * 8;
+        if (row >= rows || col >= cols) continue;
+        const uint4 v = *(const uint4*)(from + (row * Shape::vrow + col) * 2);
+        __nv_bfloat16* o = to + row * ld + col;
+        if (decltype(vec)::value) {
+          *(uint4*)o = v;
+        } else {
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (col + e < cols) ((unsigned short*)o)[e] = (unsigned short)(w[e / 2] >> (16 * (e % 2)));
+        }
+      }
+    };
+    uint32_t answers[16], steps[16];
+    auto put_answers = [&](int i) {  // and the stage may be filled anew: its rows may have come by copies of threads, and come by the tensor map next
+      turn(answers, i % STAGES);
+      __nv_bfloat16* out = p.out + (span.row0 + (long long)i * DC + t0) * p.ld_out + h * p.dv + labels0;
+      if (p.vec_out) rows_out(std::true_type(), i % STAGES, out, p.ld_out, span.len(i) - t0, p.dv - labels0);
+      else rows_out(std::false_type(), i % STAGES, out, p.ld_out, span.len(i) - t0, p.dv - labels0);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    };
+    float last = 1.0f;
+    bool ok = true;
+    for (int i = 0; i <= n; ++i) {
+      const int s = i % STAGES;
+      const unsigned char* st = ring + s * Shape::stage;
+      const DeltaFactors* f = (const DeltaFactors*)(st + Shape::block_at + DC_FACTORS);
+      const long long which = (long long)(first + i) * p.hv + h;
+      uint32_t v[32], hi[16], lo[16];
+      float x[32];
+      // S^T <- e^{b_C} S^T + dS^T, and its parts
+      if (i > 0) {
+        if (!(ok = wait.warp(&w.s_done, (i - 1) & 1))) break;
+        tmem_fence_after();
+      }
+#pragma unroll
+      for (int j = 0; j < HALF / 32; ++j) {
+        if (i > 0) {
+          tmem_load32(lanes + TM_DS + f0 + 32 * j, v);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) S[32 * j + e] = fmaf(last, S[32 * j + e], __uint_as_float(v[e]));
+        }
+        if (i == n) continue;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) split2(S[32 * j + 2 * e], S[32 * j + 2 * e + 1], hi[e], lo[e]);
+        tmem_store16(lanes + TM_S + f0 / 2 + 16 * j, hi);
+        tmem_store16(lanes + TM_S_LO + f0 / 2 + 16 * j, lo);
+        if (SAVE && label < p.dvp) {  // models before the chunk, one bf16 part
+          uint4* to = (uint4*)p.starts + (which * (DK / 8) + f0 / 8 + 4 * j) * p.dvp + label;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) to[e * p.dvp] = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
+        }
+      }
+      if (i < n) {
+        tmem_wait_store();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive(&w.s_there);
+      }
+      // the answers of the chunk before, two rows in a word
+      if (i > 0) {
+        if (!(ok = wait.warp(&w.o_done, (i - 1) & 1))) break;
+        tmem_fence_after();
+        tmem_load32(lanes + TM_O + t0, v);
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive(&w.o_read);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) answers[e] = pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+      }
+      if (i == n) {
+        if (i > 0) put_answers(i - 1);
+        break;
+      }
+      // R^T = beta (V^T - c S^T K^T)
+      if (!(ok = wait.warp(&bars[s].bulk, (i / STAGES) & 1) && wait.warp(&bars[s].rows, (i / STAGES) & 1))) break;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) x[e] = __bfloat162float(((const __nv_bfloat16*)(st + Shape::v_at))[(t0 + e) * Shape::vrow + label]);
+      if (!(ok = wait.warp(&w.r_done, i & 1))) break;
+      tmem_fence_after();
+      tmem_load32(lanes + TM_R + t0, v);
+#pragma unroll
+      for (int e = 0; e < 32; e += 4) {
+        const float4 c = *(const float4*)(f->c + t0 + e), be = *(const float4*)(f->beta + t0 + e);
+        const float cs[4] = {c.x, c.y, c.z, c.w}, bs[4] = {be.x, be.y, be.z, be.w};
+#pragma unroll
+        for (int z = 0; z < 4; ++z) x[e + z] = bs[z] * (x[e + z] - cs[z] * __uint_as_float(v[e + z]));
+      }
+      split32(x, hi, lo);
+      tmem_store16(lanes + TM_RH + t0 / 2, hi);
+      tmem_store16(lanes + TM_RL + t0 / 2, lo);
+      tmem_wait_store();
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(&w.r_there);
+      if (i > 0) {
+        put_answers(i - 1);
+        __syncwarp();
+        if (lane == 0) arrive(&bars[(i - 1) % STAGES].empty);
+      }
+      // scale c S^T Q^T, to which U^T P^T is added
+      if (!(ok = wait.warp(&w.q_done, i & 1))) break;
+      tmem_fence_after();
+      tmem_load32(lanes + TM_O + t0, v);
+#pragma unroll
+      for (int e = 0; e < 32; e += 4) {
+        const float4 c = *(const float4*)(f->c + t0 + e);
+        v[e] = __float_as_uint(p.scale * c.x * __uint_as_float(v[e]));
+        v[e + 1] = __float_as_uint(p.scale * c.y * __uint_as_float(v[e + 1]));
+        v[e + 2] = __float_as_uint(p.scale * c.z * __uint_as_float(v[e + 2]));
+        v[e + 3] = __float_as_uint(p.scale * c.w * __uint_as_float(v[e + 3]));
+      }
+      tmem_store16(lanes + TM_O + t0, v);
+      tmem_store16(lanes + TM_O + t0 + 16, v + 16);
+      // U and r U
+      if (!(ok = wait.warp(&w.u_done, i & 1))) break;
+      tmem_fence_after();
+      tmem_load32(lanes + TM_R + t0, v);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
+      split32(x, hi, lo);
+      tmem_store16(lanes + TM_UH + t0 / 2, hi);
+      tmem_store16(lanes + TM_UL + t0 / 2, lo);
+      if (SAVE) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) steps[e] = hi[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 32; e += 4) {
+        const float4 r = *(const float4*)(f->r + t0 + e);
+        x[e] *= r.x, x[e + 1] *= r.y, x[e + 2] *= r.z, x[e + 3] *= r.w;
+      }
+      last = f->last;
+      split32(x, hi, lo);
+      tmem_store16(lanes + TM_RH + t0 / 2, hi);
+      tmem_store16(lanes + TM_RL + t0 / 2, lo);
+      tmem_wait_store();
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(&w.u_there);
+      if (SAVE) {  // while S^T is formed
+        turn(steps, s);
+        rows_out(std::true_type(), s, p.steps + (which * DC + t0) * p.dvp + labels0, p.dvp, 32, p.dvp - labels0);
+      }
+    }
+    if (!ok) {
+      if (lane == 0) give_up(n);
+    } else if (p.W && there) {
+      float* to = p.W + model + f0;
+#pragma unroll
+      for (int x = 0; x < HALF; x += 4) {
+        const int left = p.dk - f0 - x;
+        if (vec) {
+          if (left > 0) *(float4*)(to + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < left) to[x + e] = S[x + e];
+        }
+      }
+    }
+    __syncwarp();
+  }
+  kernel_started();
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  if (warp == WALK_WARPS + WALK_COPIERS) tmem_free(tm, WALK_COLUMNS);
+}
+
+}  // namespace wpsgd

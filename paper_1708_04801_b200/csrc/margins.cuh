@@ -29,6 +29,7 @@
 #include "async.cuh"
 #include "common.cuh"
 #include "quantize.cuh"
+#include "tmem.cuh"
 
 namespace wpsgd {
 
@@ -69,10 +70,6 @@ struct MarginsParams {
 };
 
 // ---- tcgen05 ---------------------------------------------------------------------------------------------------------------
-// Shared-memory operand, rows of 128 bytes with 128-byte swizzle, 8 rows (1024 bytes) to the next group of rows
-__device__ __forceinline__ uint64_t mma_operand(uint32_t addr) {
-  return (uint64_t)((addr & 0x3ffff) >> 4) | 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
 // D fp32, A and B e4m3, both with contiguous k, M = 128
 template <int BN>
 __host__ __device__ constexpr uint32_t mma_shape() { return 1u << 4 | (uint32_t)(BN >> 3) << 17 | (uint32_t)(MG_ROWS >> 4) << 24; }
@@ -80,18 +77,6 @@ __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uin
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
                "r"(shape), "r"((uint32_t)add)
                : "memory");
-}
-__device__ __forceinline__ void mma_commit(unsigned long long* bar) {  // the barrier is arrived at when all products issued so far are done
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"((uint32_t)__cvta_generic_to_shared(bar)) : "memory");
-}
-__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_alloc(uint32_t* to, uint32_t cols) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "r"(cols) : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t cols) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
 }
 // 8 columns of a warp's 32 lanes in the order of matrix fragments: thread t gets columns 2 (t % 4) and the next of lanes t / 4 (v[0], v[1]),
 // t / 4 + 8 (v[2], v[3]), t / 4 + 16 and t / 4 + 24

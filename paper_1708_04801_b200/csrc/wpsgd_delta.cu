@@ -5,6 +5,7 @@
 #include "delta_chunk.cuh"
 #include "delta_grad.cuh"
 #include "delta_rows.cuh"
+#include "delta_walk.cuh"
 #include "rows_host.cuh"
 
 using namespace wpsgd;
@@ -192,6 +193,24 @@ wpsgd_status walk(wpsgd_ctx* c, const DeltaChunkParams& p, const DeltaMaps& maps
   return WPSGD_OK;
 }
 
+#ifndef WALK_MIN
+#define WALK_MIN 33
+#endif
+template <int DK>
+wpsgd_status walk_tmem(wpsgd_ctx* c, const DeltaChunkParams& p, const DeltaMaps& maps, bool save) {
+  constexpr int smem = ChainShape<DK, 8>::smem;
+  const unsigned grid = (unsigned)((long long)p.n_chains * p.hv);
+  if (save) {
+    CU_TRY(c, (allow_smem<delta_walk_kernel<DK, true>>(c)));
+    CU_TRY(c, launch(delta_walk_kernel<DK, true>, grid, WALK_THREADS, smem, c->stream, p, maps));
+  } else {
+    CU_TRY(c, (allow_smem<delta_walk_kernel<DK, false>>(c)));
+    CU_TRY(c, launch(delta_walk_kernel<DK, false>, grid, WALK_THREADS, smem, c->stream, p, maps));
+  }
+  c->launches++;
+  return WPSGD_OK;
+}
+
 template <int DK>
 wpsgd_status run_chunks(wpsgd_ctx* c, DeltaChunkParams p, const DeltaLayout& lay, bool save) {
   CU_TRY(c, launch(delta_plan_kernel, 1, PLAN_THREADS, 0, c->stream, p));
@@ -209,6 +228,7 @@ wpsgd_status run_chunks(wpsgd_ctx* c, DeltaChunkParams p, const DeltaLayout& lay
   p.slices = (p.dvp / 16 + w - 1) / w;
   DeltaMaps maps = {};
   p.maps = encode_maps(&maps, p);
+  if (p.dvp >= WALK_MIN) return walk_tmem<DK>(c, p, maps, save);
   return w == 8 ? walk<DK, 8>(c, p, maps, save) : w == 4 ? walk<DK, 4>(c, p, maps, save) : w == 2 ? walk<DK, 2>(c, p, maps, save) : walk<DK, 1>(c, p, maps, save);
 }
 
