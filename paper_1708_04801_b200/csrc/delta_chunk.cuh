@@ -73,7 +73,7 @@ struct DeltaChunkParams {
   int* order;          // [n_chains]: longest first
   DeltaChunk* chunks;  // [chunk_off[n_chains]]
   unsigned char* blocks;        // [chunks][hv][DC_BLOCK]
-  __nv_bfloat16* starts;        // [chunks][hv][DK / 8][dvp][8]: models before the chunk, for the gradient
+  __nv_bfloat16* starts;        // [chunks][hv][dvp x DK]: models before the chunk, for the gradient, see model_unit
   __nv_bfloat16* steps;         // [chunks][hv][DC][dvp]: U
   unsigned char* gram;          // [chunks][hv][DC_TRI]: D_ij k_i.k_j, for the gradient; NULL where it is not kept
   const float* W0;
@@ -86,6 +86,14 @@ struct DeltaChunkParams {
   long long spin_limit, drop;
   DevStatus* status;
 };
+
+// Models of a chunk and head as they are kept for the gradients of the rows: 64 labels at a time (fewer at the end), of these 8 features at a time, so that a
+// warp whose threads have a label each, or 8 labels and 8 features, writes whole lines. First element of a unit of 8 features.
+constexpr int MODEL_SLICE = 64;
+__device__ __forceinline__ int model_labels(int label, int dvp) { return min(MODEL_SLICE, dvp - label / MODEL_SLICE * MODEL_SLICE); }
+__device__ __forceinline__ int model_unit(int label, int unit, int dvp, int DK) {
+  return label / MODEL_SLICE * MODEL_SLICE * DK + (unit * model_labels(label, dvp) + label % MODEL_SLICE) * 8;
+}
 
 // ---- tensor-core helpers ------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -686,11 +694,11 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
       uint32_t hi[4], lo[4], b[4][4];
       a_parts(S[2 * x], S[2 * x + 1], hi, lo);
       if (SAVE) {  // models before the chunk, one bf16 part
-        uint32_t* to = (uint32_t*)(p.starts + ((which * (DK / 8) + 2 * x) * p.dvp + label) * 8 + 2 * t);
+        uint32_t* to = (uint32_t*)(p.starts + which * p.dvp * DK + model_unit(label, 2 * x, p.dvp, DK) + 2 * t);
         to[0] = hi[0];
         to[32] = hi[1];
-        to[4 * p.dvp] = hi[2];
-        to[4 * p.dvp + 32] = hi[3];
+        to[4 * model_labels(label, p.dvp)] = hi[2];
+        to[4 * model_labels(label, p.dvp) + 32] = hi[3];
       }
       if (zero) continue;
 #pragma unroll

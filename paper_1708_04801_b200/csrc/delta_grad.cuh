@@ -28,7 +28,7 @@ namespace wpsgd {
 
 struct DeltaGradParams {
   DeltaChunkParams f;
-  __nv_bfloat16* ends;   // [chunks][hv][DK / 8][dvp][8]: G behind the chunk
+  __nv_bfloat16* ends;   // [chunks][hv][dvp x DK]: G behind the chunk, as starts
   __nv_bfloat16* drs;    // [chunks][hv][DC][dvp]: dR
   float* totals;         // [blocks][2][DC][DK]: sums over the heads of labels that share features
   const float* dW;
@@ -118,11 +118,11 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_back_kernel
     for (int x = 0; x < DK / 16; ++x) {
       uint32_t hi[4], lo[4], b[4][4];
       a_parts(G[2 * x], G[2 * x + 1], hi, lo);
-      uint32_t* to = (uint32_t*)(gp.ends + ((which * (DK / 8) + 2 * x) * p.dvp + label) * 8 + 2 * t);
+      uint32_t* to = (uint32_t*)(gp.ends + which * p.dvp * DK + model_unit(label, 2 * x, p.dvp, DK) + 2 * t);
       to[0] = hi[0];
       to[32] = hi[1];
-      to[4 * p.dvp] = hi[2];
-      to[4 * p.dvp + 32] = hi[3];
+      to[4 * model_labels(label, p.dvp)] = hi[2];
+      to[4 * model_labels(label, p.dvp) + 32] = hi[3];
       if (NW == 8 && i == 0 && !gp.dW) continue;  // a gradient of zeros: nothing to multiply
 #pragma unroll
       for (int y = 0; y < 4; ++y) ldsm(b[y], k_at + wide(nk, y, x));
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     const uint32_t st = smem32(stages) + ring * Shape::stage;
 #pragma unroll
     for (int u = tid; u < ROWS_SLICE * (DK / 8); u += ROWS_THREADS) {
-      const int at_l = u % ROWS_SLICE, unit = u / ROWS_SLICE, from = (unit * p.dvp + at_l) * 8;
+      const int at_l = u % ROWS_SLICE, unit = u / ROWS_SLICE, from = (unit * model_labels(l0, p.dvp) + at_l) * 8;
       const bool there = l0 + at_l < p.dvp;
       copy16(st + (at_l * ROW + unit * 8) * 2, there ? from_s + from : p.starts, there);
       copy16(st + Shape::models + (at_l * ROW + unit * 8) * 2, there ? from_g + from : gp.ends, there);
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     copy16(to + Shape::labels, there ? from_r : gp.drs, there);
     copy16(to + 2 * Shape::labels, given ? from_o : p.dout.p, given);
     copy16(to + 3 * Shape::labels, given ? from_v : p.v.p, given);
-    from_s += ROWS_SLICE * 8, from_g += ROWS_SLICE * 8, from_u += ROWS_SLICE, from_r += ROWS_SLICE, from_o += ROWS_SLICE, from_v += ROWS_SLICE;
+    from_s += ROWS_SLICE * DK, from_g += ROWS_SLICE * DK, from_u += ROWS_SLICE, from_r += ROWS_SLICE, from_o += ROWS_SLICE, from_v += ROWS_SLICE;
   };
   auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
 

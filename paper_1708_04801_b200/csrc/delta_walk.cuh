@@ -188,12 +188,11 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
       }
     };
     uint32_t answers[16], steps[16];
-    auto put_answers = [&](int i) {  // and the stage may be filled anew: its rows may have come by copies of threads, and come by the tensor map next
+    auto put_answers = [&](int i) {
       turn(answers, i % STAGES);
       __nv_bfloat16* out = p.out + (span.row0 + (long long)i * DC + t0) * p.ld_out + h * p.dv + labels0;
       if (p.vec_out) rows_out(std::true_type(), i % STAGES, out, p.ld_out, span.len(i) - t0, p.dv - labels0);
       else rows_out(std::false_type(), i % STAGES, out, p.ld_out, span.len(i) - t0, p.dv - labels0);
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     };
     float last = 1.0f;
     bool ok = true;
@@ -222,9 +221,9 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
         tmem_store16(lanes + TM_S + f0 / 2 + 16 * j, hi);
         tmem_store16(lanes + TM_S_LO + f0 / 2 + 16 * j, lo);
         if (SAVE && label < p.dvp) {  // models before the chunk, one bf16 part
-          uint4* to = (uint4*)p.starts + (which * (DK / 8) + f0 / 8 + 4 * j) * p.dvp + label;
+          uint4* to = (uint4*)(p.starts + which * p.dvp * DK + model_unit(label, f0 / 8 + 4 * j, p.dvp, DK));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) to[e * p.dvp] = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
+          for (int e = 0; e < 4; ++e) to[e * model_labels(label, p.dvp)] = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
         }
       }
       if (i < n) {
