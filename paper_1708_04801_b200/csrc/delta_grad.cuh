@@ -249,7 +249,7 @@ constexpr int ROWS_PARTS = 4, ROWS_THREADS = 128 * ROWS_PARTS, ROWS_SLICE = 64; 
 template <int DK>
 struct RowsShape {
   static constexpr int row = DK + 8, vrow = ROWS_SLICE + 8;
-  static constexpr int models = ROWS_SLICE * row * 2, labels = DC * vrow * 2, stage = 2 * models + 4 * labels;
+  static constexpr int models = ROWS_SLICE * DK * 2, labels = DC * vrow * 2, stage = 2 * models + 4 * labels;
   static constexpr int qk = 2 * DC * row * 2, tiles = 3 * DC_TRI, kept = DC_BLOCK - DC_P + DC_TRI, sums = (ROWS_PARTS * 3 + 4) * DC * 4;
   static constexpr int stages = 2, smem = qk + tiles + kept + sums + stages * stage, totals = 2 * DC * DK;
 };
@@ -329,8 +329,8 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
     for (int u = tid; u < ROWS_SLICE * (DK / 8); u += ROWS_THREADS) {
       const int at_l = u % ROWS_SLICE, unit = u / ROWS_SLICE, from = (unit * model_labels(l0, p.dvp) + at_l) * 8;
       const bool there = l0 + at_l < p.dvp;
-      copy16(st + (at_l * ROW + unit * 8) * 2, there ? from_s + from : p.starts, there);
-      copy16(st + Shape::models + (at_l * ROW + unit * 8) * 2, there ? from_g + from : gp.ends, there);
+      copy16(st + unit * ROWS_SLICE * 16 + at_l * 16, there ? from_s + from : p.starts, there);
+      copy16(st + Shape::models + unit * ROWS_SLICE * 16 + at_l * 16, there ? from_g + from : gp.ends, there);
     }
     const uint32_t to = st + 2 * Shape::models + (row_l * VROW + col_l) * 2;
     const bool there = l < p.dvp, given = row_l < w.len && l < p.v.width;  // labels and their gradients are of one width, rounded up to 8
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
       commit();
       const uint32_t st = smem32(stages) + at_ring * Shape::stage;
       if (++at_ring == STAGES) at_ring = 0;
-      const uint32_t s_mk = st + lane_mk(lane, ROW) + colw * 2, g_mk = s_mk + Shape::models, u_at = st + 2 * Shape::models;
+      const uint32_t s_mk = st + (lane & 15) * 16 + ((lane >> 4) + colw / 8) * ROWS_SLICE * 16, g_mk = s_mk + Shape::models, u_at = st + 2 * Shape::models;
       const uint32_t a_mk = u_at + lane_mk(lane, VROW) + row0 * VROW * 2, u_nk = u_at + lane_nk(lane, VROW) + wc * 16 * PAIRS * VROW * 2, v_nk = u_at + 3 * Shape::labels + lane_nk(lane, VROW) + row0 * VROW * 2;
 #pragma unroll
       for (int x = 0; x < ROWS_SLICE / 16; ++x) {
@@ -414,8 +414,8 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
 #pragma unroll
         for (int y = 0; y < NT / 2; ++y) {
           uint32_t bg[4];
-          ldsm_t(b, s_mk + x * 16 * ROW * 2 + y * 32);
-          ldsm_t(bg, g_mk + x * 16 * ROW * 2 + y * 32);
+          ldsm_t(b, s_mk + x * 256 + y * 2 * ROWS_SLICE * 16);
+          ldsm_t(bg, g_mk + x * 256 + y * 2 * ROWS_SLICE * 16);
           mma16(aQ[2 * y], aO, b[0], b[1]);
           mma16(aQ[2 * y + 1], aO, b[2], b[3]);
           mma16(aX[2 * y], aR, b[0], b[1]);

@@ -35,14 +35,8 @@ struct WalkWait {
 
 // What the roles tell each other: products done (one arrival each), operands written or accumulators read (one of each warp)
 struct WalkBarriers {
-  unsigned long long r_done, q_done, u_done, s_done, o_done, s_there, r_there, u_there, o_read, drained;
+  unsigned long long r_done, q_done, u_done, s_done, o_done, drained, s_there[2], r_there, u_there, o_read, o_scaled;
 };
-
-// 32 fp32 to two bf16 parts
-__device__ __forceinline__ void split32(const float (&x)[32], uint32_t (&hi)[16], uint32_t (&lo)[16]) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) split2(x[2 * i], x[2 * i + 1], hi[i], lo[i]);
-}
 
 template <int DK, bool SAVE>
 __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __grid_constant__ DeltaChunkParams p, const __grid_constant__ DeltaMaps maps) {
@@ -63,7 +57,7 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
       mbar_init(&bars[s].empty, WALK_WARPS + 1);
     }
     for (unsigned long long* b : {&w.r_done, &w.q_done, &w.u_done, &w.s_done, &w.o_done, &w.drained}) mbar_init(b, 1);
-    for (unsigned long long* b : {&w.s_there, &w.r_there, &w.u_there, &w.o_read}) mbar_init(b, WALK_WARPS);
+    for (unsigned long long* b : {&w.s_there[0], &w.s_there[1], &w.r_there, &w.u_there, &w.o_read, &w.o_scaled}) mbar_init(b, WALK_WARPS);
     dead_flag = 0;
     mbar_fence_init();
   }
@@ -90,20 +84,24 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
       for (; i < n; ++i) {
         const int s = i % STAGES;
         const uint32_t k_at = smem32(ring + s * Shape::stage), q_at = k_at + Shape::q_at, t_at = k_at + Shape::block_at;
-        if (!wait(&bars[s].bulk, (i / STAGES) & 1) || !wait(&bars[s].rows, (i / STAGES) & 1) || !wait(&w.s_there, i & 1)) break;
+        if (!wait(&bars[s].bulk, (i / STAGES) & 1) || !wait(&bars[s].rows, (i / STAGES) & 1)) break;
         if (!p.maps || span.len(i) < DC) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // features and queries that threads have copied
-        tmem_fence_after();
+        bool there = true;
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
+        for (int j = 0; j < HALF / 32; ++j) {  // 32 features of either half at a time, as they come
+          there = there && wait(&w.s_there[j], i & 1);
+          if (!there) break;
+          tmem_fence_after();
 #pragma unroll
-          for (int x = 0; x < DK / 16; ++x)
-            mma_bf16(tm + TM_R, tm + (part ? TM_S_LO : TM_S) + 8 * x, mma_operand(k_at + x / 4 * WIDE_BYTES + x % 4 * 32), mma_shape16(DC, false), part || x);
+          for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const int x = y / 2 * (HALF / 16) + 2 * j + y % 2;
+              mma_bf16(tm + TM_R, tm + (part ? TM_S_LO : TM_S) + 8 * x, mma_operand(k_at + x / 4 * WIDE_BYTES + x % 4 * 32), mma_shape16(DC, false), j || part || y);
+            }
+        }
+        if (!there) break;
         mma_commit(&w.r_done);
-        if (i > 0 && !wait(&w.o_read, (i - 1) & 1)) break;
-        tmem_fence_after();
-#pragma unroll
-        for (int x = 0; x < DK / 16; ++x) mma_bf16(tm + TM_O, tm + TM_S + 8 * x, mma_operand(q_at + x / 4 * WIDE_BYTES + x % 4 * 32), mma_shape16(DC, false), x > 0);
-        mma_commit(&w.q_done);
         // a triangle's column of blocks x: rows of the result from 16 x on
         auto triangle = [&](uint32_t d, uint32_t hi, uint32_t lo, uint32_t at, bool add) {
 #pragma unroll
@@ -117,6 +115,11 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
         tmem_fence_after();
         triangle(TM_R, TM_RH, TM_RL, t_at, false);
         mma_commit(&w.u_done);
+        if (i > 0 && !wait(&w.o_read, (i - 1) & 1)) break;
+        tmem_fence_after();
+#pragma unroll
+        for (int x = 0; x < DK / 16; ++x) mma_bf16(tm + TM_O, tm + TM_S + 8 * x, mma_operand(q_at + x / 4 * WIDE_BYTES + x % 4 * 32), mma_shape16(DC, false), x > 0);
+        mma_commit(&w.q_done);
         if (!wait(&w.u_there, i & 1)) break;
         tmem_fence_after();
 #pragma unroll
@@ -124,6 +127,8 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
 #pragma unroll
           for (int x = 0; x < 4; ++x) mma_bf16(tm + TM_DS, tm + (part ? TM_RL : TM_RH) + 8 * x, mma_operand_outer(k_at + x * 2048, WIDE_BYTES), mma_shape16(DK, true), part || x);
         mma_commit(&w.s_done);
+        if (!wait(&w.o_scaled, i & 1)) break;
+        tmem_fence_after();
         triangle(TM_O, TM_UH, TM_UL, t_at + DC_P, true);
         mma_commit(&w.o_done);
         mma_commit(&bars[s].empty);
@@ -157,16 +162,16 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
       }
       S[x] = v.x, S[x + 1] = v.y, S[x + 2] = v.z, S[x + 3] = v.w;
     }
-    // 32 labels of 32 rows: from threads that have a label each, by way of the place where the warp's labels came in, to rows in memory
-    const int labels0 = (warp & 3) * 32;
-    auto turn = [&](const uint32_t (&words)[16], int s) {
-      unsigned short* at = (unsigned short*)(ring + s * Shape::stage + Shape::v_at) + t0 * Shape::vrow + label;
+    const int labels0 = (warp & 3) * 32, g = lane >> 2, t = lane & 3;
+    const uint32_t own = smem32(ring) + Shape::v_at + (t0 * Shape::vrow + labels0) * 2, own_nk = own + lane_nk(lane, Shape::vrow);  // where the warp's labels come in
+    // The warp's labels (a word has two rows) to rows in memory, by way of that place
+    auto turn = [&](const uint32_t (&words)[2][8], int s) {
       __syncwarp();
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        at[2 * e * Shape::vrow] = (unsigned short)words[e];
-        at[(2 * e + 1) * Shape::vrow] = (unsigned short)(words[e] >> 16);
-      }
+      for (int z = 0; z < 2; ++z)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+          stsm_t(own_nk + s * Shape::stage + z * 32 + y * 16 * Shape::vrow * 2, words[z][4 * y], words[z][4 * y + 1], words[z][4 * y + 2], words[z][4 * y + 3]);
       __syncwarp();
     };
     auto rows_out = [&](auto vec, int s, __nv_bfloat16* to, long long ld, int rows, int cols) {
@@ -187,12 +192,39 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
         }
       }
     };
-    uint32_t answers[16], steps[16];
+    // 32 labels and rows of an accumulator: acc[z][4 n + e], label 16 z + g (e < 2) or 8 further, row t0 + 8 n + 2 t + e % 2
+    uint32_t acc[2][16];
+    auto take = [&](uint32_t at) {
+      tmem_load_tiles(lanes + at + t0, acc[0]);
+      tmem_load_tiles(lanes + at + t0 + (16u << 16), acc[1]);
+      tmem_wait_load(acc[0], acc[1]);
+    };
     auto put_answers = [&](int i) {
-      turn(answers, i % STAGES);
+      uint32_t words[2][8];
+#pragma unroll
+      for (int z = 0; z < 2; ++z)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) words[z][e] = pack2(__uint_as_float(acc[z][2 * e]), __uint_as_float(acc[z][2 * e + 1]));
+      turn(words, i % STAGES);
       __nv_bfloat16* out = p.out + (span.row0 + (long long)i * DC + t0) * p.ld_out + h * p.dv + labels0;
       if (p.vec_out) rows_out(std::true_type(), i % STAGES, out, p.ld_out, span.len(i) - t0, p.dv - labels0);
       else rows_out(std::false_type(), i % STAGES, out, p.ld_out, span.len(i) - t0, p.dv - labels0);
+    };
+    auto tell = [&](unsigned long long* bar) {
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(bar);
+    };
+    // two parts of x, four values to a tile of 8 columns, to operands
+    auto put_parts = [&](const float (&x)[2][16], uint32_t hi_at, uint32_t lo_at, uint32_t (&hi)[2][8]) {
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        uint32_t lo[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) split2(x[z][2 * e], x[z][2 * e + 1], hi[z][e], lo[e]);
+        tmem_store_words(lanes + hi_at + t0 / 2 + ((uint32_t)z << 20), hi[z]);
+        tmem_store_words(lanes + lo_at + t0 / 2 + ((uint32_t)z << 20), lo);
+      }
     };
     float last = 1.0f;
     bool ok = true;
@@ -201,8 +233,6 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
       const unsigned char* st = ring + s * Shape::stage;
       const DeltaFactors* f = (const DeltaFactors*)(st + Shape::block_at + DC_FACTORS);
       const long long which = (long long)(first + i) * p.hv + h;
-      uint32_t v[32], hi[16], lo[16];
-      float x[32];
       // S^T <- e^{b_C} S^T + dS^T, and its parts
       if (i > 0) {
         if (!(ok = wait.warp(&w.s_done, (i - 1) & 1))) break;
@@ -211,110 +241,118 @@ __global__ void __launch_bounds__(WALK_THREADS, 1) delta_walk_kernel(const __gri
 #pragma unroll
       for (int j = 0; j < HALF / 32; ++j) {
         if (i > 0) {
+          uint32_t v[32];
           tmem_load32(lanes + TM_DS + f0 + 32 * j, v);
 #pragma unroll
           for (int e = 0; e < 32; ++e) S[32 * j + e] = fmaf(last, S[32 * j + e], __uint_as_float(v[e]));
         }
         if (i == n) continue;
+        uint32_t hi[16], lo[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) split2(S[32 * j + 2 * e], S[32 * j + 2 * e + 1], hi[e], lo[e]);
         tmem_store16(lanes + TM_S + f0 / 2 + 16 * j, hi);
         tmem_store16(lanes + TM_S_LO + f0 / 2 + 16 * j, lo);
-        if (SAVE && label < p.dvp) {  // models before the chunk, one bf16 part
-          uint4* to = (uint4*)(p.starts + which * p.dvp * DK + model_unit(label, f0 / 8 + 4 * j, p.dvp, DK));
+        tmem_wait_store();
+        tell(&w.s_there[j]);
+      }
+      if (i == n) {
+        if (i > 0) {
+          if (!(ok = wait.warp(&w.o_done, (i - 1) & 1))) break;
+          tmem_fence_after();
+          take(TM_O);
+          put_answers(i - 1);
+        }
+        break;
+      }
+      if (SAVE && label < p.dvp) {  // models before the chunk, one bf16 part
+        uint4* to = (uint4*)(p.starts + which * p.dvp * DK + model_unit(label, f0 / 8, p.dvp, DK));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) to[e * model_labels(label, p.dvp)] = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
+        for (int e = 0; e < HALF / 8; ++e)
+          to[e * model_labels(label, p.dvp)] = make_uint4(pack2(S[8 * e], S[8 * e + 1]), pack2(S[8 * e + 2], S[8 * e + 3]), pack2(S[8 * e + 4], S[8 * e + 5]), pack2(S[8 * e + 6], S[8 * e + 7]));
+      }
+      // R^T = beta (V^T - c S^T K^T)
+      float x[2][16];
+      uint32_t words[2][8];
+      {
+        uint32_t v[2][2][4];
+        if (!(ok = wait.warp(&bars[s].bulk, (i / STAGES) & 1) && wait.warp(&bars[s].rows, (i / STAGES) & 1))) break;
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) ldsm_t(v[z][y], own_nk + s * Shape::stage + z * 32 + y * 16 * Shape::vrow * 2);
+        if (!(ok = wait.warp(&w.r_done, i & 1))) break;
+        tmem_fence_after();
+        take(TM_R);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const float2 c = *(const float2*)(f->c + t0 + 8 * m + 2 * t), be = *(const float2*)(f->beta + t0 + 8 * m + 2 * t);
+#pragma unroll
+          for (int z = 0; z < 2; ++z)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t two = v[z][m / 2][m % 2 * 2 + e];
+              x[z][4 * m + 2 * e] = be.x * (__uint_as_float(two << 16) - c.x * __uint_as_float(acc[z][4 * m + 2 * e]));
+              x[z][4 * m + 2 * e + 1] = be.y * (__uint_as_float(two & 0xffff0000u) - c.y * __uint_as_float(acc[z][4 * m + 2 * e + 1]));
+            }
         }
       }
-      if (i < n) {
-        tmem_wait_store();
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) arrive(&w.s_there);
-      }
-      // the answers of the chunk before, two rows in a word
+      put_parts(x, TM_RH, TM_RL, words);
+      tmem_wait_store();
+      tell(&w.r_there);
+      // the answers of the chunk before, while U^T is formed; then its stage may be filled anew
       if (i > 0) {
         if (!(ok = wait.warp(&w.o_done, (i - 1) & 1))) break;
         tmem_fence_after();
-        tmem_load32(lanes + TM_O + t0, v);
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) arrive(&w.o_read);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) answers[e] = pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
-      }
-      if (i == n) {
-        if (i > 0) put_answers(i - 1);
-        break;
-      }
-      // R^T = beta (V^T - c S^T K^T)
-      if (!(ok = wait.warp(&bars[s].bulk, (i / STAGES) & 1) && wait.warp(&bars[s].rows, (i / STAGES) & 1))) break;
-#pragma unroll
-      for (int e = 0; e < 32; ++e) x[e] = __bfloat162float(((const __nv_bfloat16*)(st + Shape::v_at))[(t0 + e) * Shape::vrow + label]);
-      if (!(ok = wait.warp(&w.r_done, i & 1))) break;
-      tmem_fence_after();
-      tmem_load32(lanes + TM_R + t0, v);
-#pragma unroll
-      for (int e = 0; e < 32; e += 4) {
-        const float4 c = *(const float4*)(f->c + t0 + e), be = *(const float4*)(f->beta + t0 + e);
-        const float cs[4] = {c.x, c.y, c.z, c.w}, bs[4] = {be.x, be.y, be.z, be.w};
-#pragma unroll
-        for (int z = 0; z < 4; ++z) x[e + z] = bs[z] * (x[e + z] - cs[z] * __uint_as_float(v[e + z]));
-      }
-      split32(x, hi, lo);
-      tmem_store16(lanes + TM_RH + t0 / 2, hi);
-      tmem_store16(lanes + TM_RL + t0 / 2, lo);
-      tmem_wait_store();
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive(&w.r_there);
-      if (i > 0) {
+        take(TM_O);
+        tell(&w.o_read);
         put_answers(i - 1);
         __syncwarp();
         if (lane == 0) arrive(&bars[(i - 1) % STAGES].empty);
       }
-      // scale c S^T Q^T, to which U^T P^T is added
-      if (!(ok = wait.warp(&w.q_done, i & 1))) break;
-      tmem_fence_after();
-      tmem_load32(lanes + TM_O + t0, v);
-#pragma unroll
-      for (int e = 0; e < 32; e += 4) {
-        const float4 c = *(const float4*)(f->c + t0 + e);
-        v[e] = __float_as_uint(p.scale * c.x * __uint_as_float(v[e]));
-        v[e + 1] = __float_as_uint(p.scale * c.y * __uint_as_float(v[e + 1]));
-        v[e + 2] = __float_as_uint(p.scale * c.z * __uint_as_float(v[e + 2]));
-        v[e + 3] = __float_as_uint(p.scale * c.w * __uint_as_float(v[e + 3]));
-      }
-      tmem_store16(lanes + TM_O + t0, v);
-      tmem_store16(lanes + TM_O + t0 + 16, v + 16);
       // U and r U
       if (!(ok = wait.warp(&w.u_done, i & 1))) break;
       tmem_fence_after();
-      tmem_load32(lanes + TM_R + t0, v);
+      take(TM_R);
 #pragma unroll
-      for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
-      split32(x, hi, lo);
-      tmem_store16(lanes + TM_UH + t0 / 2, hi);
-      tmem_store16(lanes + TM_UL + t0 / 2, lo);
-      if (SAVE) {
+      for (int z = 0; z < 2; ++z)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) steps[e] = hi[e];
-      }
+        for (int e = 0; e < 16; ++e) x[z][e] = __uint_as_float(acc[z][e]);
+      uint32_t scaled[2][8];
+      put_parts(x, TM_UH, TM_UL, words);
 #pragma unroll
-      for (int e = 0; e < 32; e += 4) {
-        const float4 r = *(const float4*)(f->r + t0 + e);
-        x[e] *= r.x, x[e + 1] *= r.y, x[e + 2] *= r.z, x[e + 3] *= r.w;
+      for (int m = 0; m < 4; ++m) {
+        const float2 r = *(const float2*)(f->r + t0 + 8 * m + 2 * t);
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) x[z][4 * m + e] *= r.x, x[z][4 * m + e + 1] *= r.y;
       }
       last = f->last;
-      split32(x, hi, lo);
-      tmem_store16(lanes + TM_RH + t0 / 2, hi);
-      tmem_store16(lanes + TM_RL + t0 / 2, lo);
+      put_parts(x, TM_RH, TM_RL, scaled);
       tmem_wait_store();
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive(&w.u_there);
-      if (SAVE) {  // while S^T is formed
-        turn(steps, s);
+      tell(&w.u_there);
+      // scale c S^T Q^T, to which U^T P^T is added, while dS^T is formed
+      if (!(ok = wait.warp(&w.q_done, i & 1))) break;
+      tmem_fence_after();
+      take(TM_O);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float2 c = *(const float2*)(f->c + t0 + 8 * m + 2 * t);
+        const float cx = p.scale * c.x, cy = p.scale * c.y;
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            acc[z][4 * m + e] = __float_as_uint(cx * __uint_as_float(acc[z][4 * m + e]));
+            acc[z][4 * m + e + 1] = __float_as_uint(cy * __uint_as_float(acc[z][4 * m + e + 1]));
+          }
+      }
+      tmem_store_tiles(lanes + TM_O + t0, acc[0]);
+      tmem_store_tiles(lanes + TM_O + t0 + (16u << 16), acc[1]);
+      tmem_wait_store();
+      tell(&w.o_scaled);
+      if (SAVE) {
+        turn(words, s);
         rows_out(std::true_type(), s, p.steps + (which * DC + t0) * p.dvp + labels0, p.dvp, 32, p.dvp - labels0);
       }
     }
