@@ -614,7 +614,7 @@ template <int DK, int NW, bool SAVE>
 __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kernel(const __grid_constant__ DeltaChunkParams p, const __grid_constant__ DeltaMaps maps) {
   using Shape = ChainShape<DK, NW>;
   constexpr int VROW = Shape::vrow * 2, STAGES = Shape::stages;  // bytes
-  constexpr bool COPIERS = Shape::copiers > 0;
+  static_assert(Shape::copiers > 0, "chunks are brought by warps of their own");
   extern __shared__ unsigned char chain_smem[];
   __shared__ ChunkBarriers bars[STAGES];
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -626,24 +626,18 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
   const DeltaSpan span = span_of(p, first, n);
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&bars[s].rows, 32 * (COPIERS ? Shape::copiers : warps));
+      mbar_init(&bars[s].rows, 32 * Shape::copiers);
       mbar_init(&bars[s].bulk, 1);
       mbar_init(&bars[s].empty, warps);
     }
     mbar_fence_init();
   }
   __syncthreads();
-  if (COPIERS && warp >= NW) {
+  if (warp >= NW) {
     bring_chunks<DK, NW>(p, maps, p.v, smem32(ring), first, false, n, span, h, kh, col0, warp - NW, Shape::copiers, lane, bars);
     return;
   }
   if (warp >= warps) return;
-  int brought = 0;
-  if (!COPIERS && n > 0 && p.drop != 0) {
-    bring_chunk<DK, NW>(p, maps, p.v, smem32(ring), first, span, 0, h, kh, col0, warp, warps, lane, &bars[0]);
-    brought = 1;
-  }
-
   // S^T: labels g and g + 8 of the warp's 16, features 8 n + 2 t and the next
   float S[DK / 8][4];
   const int label = col0 + warp * 16 + g;
@@ -657,20 +651,10 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
     }
 
   for (int i = 0; i < n; ++i) {
-    const int s = i % STAGES, s1 = (i + 1) % STAGES;
-    bool ok = true;
-    if (!COPIERS && i + 1 < n) {  // the next chunk, once all have left the one that was there; p.drop (a test hook): from which on none is brought
-      if (i + 1 >= STAGES) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars[s1].empty, ((i + 1) / STAGES - 1) & 1, p.spin_limit));
-      if (ok && (p.drop < 0 || i + 1 < p.drop)) {
-        bring_chunk<DK, NW>(p, maps, p.v, smem32(ring) + s1 * Shape::stage, first + i + 1, span, i + 1, h, kh, col0, warp, warps, lane, &bars[s1]);
-        brought = i + 2;
-      }
-    }
-    ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&bars[s].bulk, (i / STAGES) & 1, p.spin_limit));
-    if (!ok || !__all_sync(0xffffffffu, mbar_wait_bounded(&bars[s].rows, (i / STAGES) & 1, p.spin_limit))) {
+    const int s = i % STAGES;
+    const bool there = __all_sync(0xffffffffu, mbar_wait_bounded(&bars[s].bulk, (i / STAGES) & 1, p.spin_limit));
+    if (!there || !__all_sync(0xffffffffu, mbar_wait_bounded(&bars[s].rows, (i / STAGES) & 1, p.spin_limit))) {
       if (lane == 0) set_status(p.status, DEV_TIMEOUT, 25, i);
-      copies_done();  // nothing of this warp's is in flight when it leaves
-      if (!COPIERS && warp == 0) bulk_done<STAGES>(bars, max(0, brought - STAGES), brought);
       return;
     }
     unsigned char* st = ring + s * Shape::stage;
@@ -680,9 +664,6 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
     const uint32_t k_at = smem32(st), q_at = k_at + Shape::q_at, nk = wide_nk(lane), mk = wide_mk(lane);
     const uint32_t t_nk = smem32(block) + tri_nk(lane), v_nk = smem32(st + Shape::v_at) + warp * 32 + lane_nk(lane, Shape::vrow);
 
-    // Models of zeros: nothing to multiply. The branch keeps products of different features apart, which two warps to a scheduler gain by (65536 rows of 16 heads 747 -> 703 us)
-    // and one alone loses by (5 chunks of 64 features 17.0 -> 19.3 us).
-    const bool zero = NW == 8 && i == 0 && !p.W0;
     // S^T K^T
     float R[8][4];
 #pragma unroll
@@ -700,7 +681,6 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
         to[4 * model_labels(label, p.dvp)] = hi[2];
         to[4 * model_labels(label, p.dvp) + 32] = hi[3];
       }
-      if (zero) continue;
 #pragma unroll
       for (int y = 0; y < 4; ++y) ldsm(b[y], k_at + wide(nk, y, x));
 #pragma unroll
@@ -746,7 +726,6 @@ __global__ void __launch_bounds__(ChainShape<DK, NW>::threads) delta_chain_kerne
         ldsm(bl, t_nk + DC_T_LO + tri_at(y, x));
         mma_split(U[2 * y], U[2 * y + 1], hi, lo, bh, bl);
       }
-      if (zero) continue;
 #pragma unroll
       for (int z = x * DK / 64; z < (x + 1) * DK / 64; ++z) {
         const uint32_t a[4] = {pack2(S[2 * z][0], S[2 * z][1]), pack2(S[2 * z][2], S[2 * z][3]), pack2(S[2 * z + 1][0], S[2 * z + 1][1]), pack2(S[2 * z + 1][2], S[2 * z + 1][3])};

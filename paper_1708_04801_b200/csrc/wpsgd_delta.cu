@@ -193,9 +193,10 @@ wpsgd_status walk(wpsgd_ctx* c, const DeltaChunkParams& p, const DeltaMaps& maps
   return WPSGD_OK;
 }
 
-#ifndef WALK_MIN
-#define WALK_MIN 33
-#endif
+// Labels from which on a head walks by tcgen05, whose products have 128 of them whatever there are; fewer are at most four warps of mma.sync. By mma.sync and by tcgen05, us: 16384 rows,
+// 32 chains, 16 heads of 64 features and 32 labels 81 and 88, 64 x 64 87 and 91, 128 x 64 110 and 109, 64 x 128 144 and 97, 128 x 96 197 and 116, 128 x 128 205 and 127; one chain of 8192
+// rows, 2 heads of 128 x 128 358 and 334. (Not by the number of chains: what a chain gives does not depend on the others. 4 chunks of 15 chains and heads of 128 x 128: 20 and 25.)
+constexpr int WALK_MIN = 65;
 template <int DK>
 wpsgd_status walk_tmem(wpsgd_ctx* c, const DeltaChunkParams& p, const DeltaMaps& maps, bool save) {
   constexpr int smem = ChainShape<DK, 8>::smem;
@@ -224,12 +225,12 @@ wpsgd_status run_chunks(wpsgd_ctx* c, DeltaChunkParams p, const DeltaLayout& lay
     CU_TRY(c, launch(delta_prepare_kernel<DK>, (unsigned)(lay.chunks * (p.hv / p.prep_heads)), PREP_THREADS, PrepShape<DK>::smem, c->stream, p));
     c->launches++;
   }
-  const int w = chain_warps((long long)p.n_chains * p.hv, p.dvp);
-  p.slices = (p.dvp / 16 + w - 1) / w;
   DeltaMaps maps = {};
   p.maps = encode_maps(&maps, p);
   if (p.dvp >= WALK_MIN) return walk_tmem<DK>(c, p, maps, save);
-  return w == 8 ? walk<DK, 8>(c, p, maps, save) : w == 4 ? walk<DK, 4>(c, p, maps, save) : w == 2 ? walk<DK, 2>(c, p, maps, save) : walk<DK, 1>(c, p, maps, save);
+  const int w = chain_warps((long long)p.n_chains * p.hv, p.dvp);
+  p.slices = (p.dvp / 16 + w - 1) / w;
+  return w == 4 ? walk<DK, 4>(c, p, maps, save) : w == 2 ? walk<DK, 2>(c, p, maps, save) : walk<DK, 1>(c, p, maps, save);
 }
 
 // Blocks that go through the chunks' rows: one per SM
