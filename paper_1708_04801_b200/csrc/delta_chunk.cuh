@@ -8,15 +8,14 @@
 // Only S ties the chunks of a chain together. So a first kernel forms T = (I + A)^{-1} and P for all chunks at once, and a second walks
 // the chunks of each chain: three products a chunk with S, T and K, and two for the answers.
 //
-// Columns of S, U, R and O (labels) know nothing of each other. A warp of the second kernel has 16 labels for good: S^T, [16 x dk], is the fp32 accumulator
-// of mma.sync m16n8k16, whose layout is that of the A operand of the next product, so S, R and U go from product to product
+// Columns of S, U, R and O (labels) know nothing of each other, and every product that ties one chunk to the next has labels as rows of its A operand. Heads of more than 64 labels
+// walk by tcgen05, with labels as the lanes of tensor memory (delta_walk.cuh). Here are those of fewer, which would leave most of its 128 rows empty: a warp has 16 labels for good:
+// S^T, [16 x dk], is the fp32 accumulator of mma.sync m16n8k16, whose layout is that of the A operand of the next product, so S, R and U go from product to product
 // in registers, K, Q, T and P come from shared memory as B operands (with ldmatrix, transposed where needed), and nothing is exchanged
-// between warps: no barrier but those of the ring that brings the chunks. tcgen05 would have to carry S, R and U through tensor memory and shared memory
-// between five dependent products of 64 x 16 to 128 columns, and a chain has no other work to hide that behind.
+// between warps: no barrier but those of the ring that brings the chunks.
 //
 // Bounds, 65536 rows in 16 chains of four speeds, 8 heads of features and 16 of labels, 128 x 128: the first kernel 205 us, latency of its steps between barriers
-// (1.6 instructions a cycle, four blocks an SM); the second 750 us, 440 products of a warp and chunk: tensor pipe 55 % and shared memory (every warp reads all
-// operands for its 16 labels) 65 % of the time, with two warps to a scheduler and 14 % of it spent on SMs that have run out of chains. Many chains and heads fill the
+// (1.6 instructions a cycle, four blocks an SM); the second 370 us (by mma.sync 720, tensor pipe 55 % and shared memory 65 % of the time). Many chains and heads fill the
 // GPU; a single one is bound by the latency of a chunk.
 //
 // Rounding: an fp32 factor x enters a product as two bf16 parts, x = hi + lo (2^-17 of x is left out): K S and K^T U
@@ -479,9 +478,8 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
 }
 
 // ---- the walk over a chain's chunks ---------------------------------------------------------------------------------------------------------------
-// A block has a chain, a head and 16 NW labels of it: NW warps as described above. Of eight each brings its share of the next chunk while it works on this one, so that a
-// scheduler's registers go to the two warps that multiply (a ninth warp that only copies would leave them 168 each); beside fewer there are four warps that
-// only copy. Three stages where they fit: a warp may be a chunk ahead of the slowest.
+// A block has a chain, a head and 16 NW labels of it: NW warps as described above, beside four that only copy. (Backward there may be eight, and each brings its share of the next
+// chunk while it works on this one, so that a scheduler's registers go to the two warps that multiply: a ninth warp that only copies would leave them 168 each.) Three stages where they fit: a warp may be a chunk ahead of the slowest.
 template <int DK, int NW>
 struct ChainShape {
   static constexpr int vrow = 16 * NW + 8;  // elements

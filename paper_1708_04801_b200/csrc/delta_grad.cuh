@@ -15,8 +15,8 @@
 // Rounding: G, P, dU, scale c O' and beta c dR in two bf16 parts in the walk's products; S, U, G, dR, F and E are rounded to bf16
 // once where the third kernel multiplies them. Gradients leave as bf16: those of the labels are off by that rounding alone (1.7e-3 of their norm), the others by 2.5e-3 to 3e-3.
 //
-// Bounds, 32768 rows in 16 chains, 8 heads of features and 16 of labels, 128 x 128: the walk 455 us, as the forward one (the run that keeps what this needs: 460); the third kernel
-// 610 us, of which its copies alone would take 220 and the tensor pipe is active for 200: the steps between the products (F and E, sums, the way out) wait for each
+// Bounds, 32768 rows in 16 chains, 8 heads of features and 16 of labels, 128 x 128: the walk 436 us, by mma.sync as the forward one of few labels; the third kernel
+// 620 us, of which its copies alone would take 220 and the tensor pipe is active for 200: the steps between the products (F and E, sums, the way out) wait for each
 // other at barriers, and 128 registers hold no second piece of work. Tried and slower, 3216 chunks and heads of 128 x 128 (241 us): two blocks of 8 warps an SM with half of
 // the columns each, F and E formed twice (321); 8 warps with 255 registers (275, when 16 took 268); the sums over heads that share features in shared memory instead of
 // a ring of whole slices (267).

@@ -7,6 +7,12 @@
 // dS^T = (r U)^T K (two parts); S^T Q^T and U^T P^T run beside it, and the answers leave while the next chunk's first product runs. S stays in registers in fp32.
 //
 // Roles: eight warps with S, as above; four that scale and bring out the answers; three that bring the chunks; one thread that issues the products.
+//
+// Bounds: the string. 56 products of 16 of k a chunk are 1900 cycles of the tensor cores at 128 x 128; a chunk takes 4700: S to two parts 900, its product 600, R 570, T R 700, r U 400, the
+// step of S 600, and 450 of waiting for barriers that are complete (160 to 190 cycles each). 65536 rows in 16 chains of 8 heads of features and 16 of labels, 128 x 128: 370 us; by mma.sync
+// 720; with the answers by the eight warps, between the other steps, 394; with them and the labels by threads that have a label each, 445 (a store of 2 bytes a lane for each row: 615).
+// With models and steps kept for a gradient, half the rows: 227 (their stores, 48 KB a chunk, take 1800 cycles of the string). Tried and slower: one lane that polls for its warp (394 to
+// 440), the next labels loaded before S (370 to 390), models kept while U is formed (227 to 231).
 #pragma once
 
 #include "delta_chunk.cuh"

@@ -98,6 +98,7 @@ def check_run(rows, off, got, W0=None, scale=None, exact_rows=None):
 CASES = [  # lengths, first row, rows behind, heads_k, heads_v, dk, dv
     ([1], 0, 0, 1, 1, 1, 1), ([0, 3, 0], 0, 2, 1, 1, 5, 3), ([7, 1, 64], 3, 5, 2, 2, 16, 16), ([65, 63, 64, 0], 0, 0, 1, 2, 64, 64), ([130], 1, 0, 2, 6, 128, 128),
     ([33, 100, 200], 0, 1, 3, 3, 60, 33), ([257, 5], 0, 0, 1, 3, 97, 128), ([90], 0, 0, 2, 2, 128, 17), ([300], 0, 7, 1, 1, 32, 8), ([64, 128], 0, 0, 1, 1, 72, 40),
+    ([65, 0, 200], 2, 3, 1, 2, 40, 128), ([64, 129], 0, 0, 2, 2, 64, 65), ([1, 320], 0, 1, 1, 1, 128, 81),
 ]
 
 
@@ -120,9 +121,9 @@ def test_run(ctx, lengths, first, behind, hk, hv, dk, dv, start, dtype):
     check_run(rows, off, got, W0)
 
 
-# what the library chooses from: labels shared by 8, 4 or 2 warps of a block, heads that share features formed together, rows by tensor maps or not, rings that go round
+# what the library chooses from: labels as lanes of tensor memory or shared by 8, 4 or 2 warps of a block, heads that share features formed together, rows by tensor maps or not, rings that go round
 FORMS = [([260, 200, 130, 64] * 10, 2, 4, 128, 128), ([260, 200, 130, 64] * 10, 4, 4, 64, 64), ([3] * 600, 4, 8, 128, 128), ([1, 65] * 150, 2, 6, 64, 64), ([2] * 400, 4, 12, 24, 32),
-         ([70] * 80, 2, 2, 72, 120), ([200, 3] * 80, 1, 1, 128, 72)]
+         ([70] * 80, 2, 2, 72, 120), ([200, 3] * 80, 1, 1, 128, 72), ([200, 3] * 80, 1, 2, 64, 128), ([150, 64] * 40, 2, 2, 24, 100)]
 
 
 @pytest.mark.parametrize("lengths,hk,hv,dk,dv", FORMS)
@@ -469,7 +470,7 @@ def test_two_graphs_and_another_stream(P):
 
 
 @pytest.mark.parametrize("limit", [1, 4096])
-@pytest.mark.parametrize("chains,dv", [(1, 64), (160, 128)])  # warps that only copy beside those that multiply, and warps that do both
+@pytest.mark.parametrize("chains,dv", [(1, 64), (160, 64), (160, 128), (2, 128)])  # warps that only copy beside those that multiply, warps that do both, tcgen05
 def test_a_wait_that_runs_out_is_reported(P, limit, chains, dv):
     rows = [x.cuda() for x in make(400 * chains, 1, 1, 64, dv, torch.bfloat16)]
     off = offsets([400] * chains).cuda()
