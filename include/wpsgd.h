@@ -318,6 +318,11 @@ wpsgd_status wpsgd_combine_rows_grad(wpsgd_ctx* ctx, const void* dout, int64_t l
                                      int64_t d, int64_t n_sorted, const int32_t* where, const float* weights, int64_t n_rows,
                                      int32_t top, void* dY, int64_t ld_dy, float* dweights);
 
+/* For new memory that wpsgd_gather_rows or wpsgd_combine_rows_grad is to write, before that call: rows of out that no place has get zeros (so may
+ * the others, which that call writes). marks DEVICE [(n_sorted + 31) / 32], 4-byte aligned, is memory of the caller, used until the call's work has ended. */
+wpsgd_status wpsgd_clear_rows(wpsgd_ctx* ctx, const int32_t* where, int64_t n_rows, int32_t top, void* out, wpsgd_xtype xt, int64_t ld_out, int64_t d,
+                              int64_t n_sorted, uint32_t* marks);
+
 /* ---- Chains whose labels are vectors (gated delta rule) -----------------------------------------------------------------------------
  * A chain owns the rows [shard_off[c], shard_off[c+1]) and runs over them once, in order. Each of its heads_v heads keeps dv linear models on dk
  * features, W [dv, dk]; a row t brings features k_t, a vector of labels v_t, a step size beta_t and a log decay g_t, and is answered at q_t:

@@ -22,7 +22,7 @@ EXPORTED_SYMBOLS = [
     "wpsgd_last_error", "wpsgd_continue_csr", "wpsgd_validate_csr", "wpsgd_span_valid", "wpsgd_sample_indices_host",
     "wpsgd_check_static", "wpsgd_solve_host_csr", "wpsgd_quantize_rows", "wpsgd_margins_fp8", "wpsgd_objective_grad",
     "wpsgd_objective_grad_fp8", "wpsgd_grad_list_create", "wpsgd_grad_list_destroy", "wpsgd_grad_norm", "wpsgd_clip_grad_norm",
-    "wpsgd_sort_rows", "wpsgd_gather_rows", "wpsgd_combine_rows", "wpsgd_combine_rows_grad",
+    "wpsgd_sort_rows", "wpsgd_gather_rows", "wpsgd_combine_rows", "wpsgd_combine_rows_grad", "wpsgd_clear_rows",
     "wpsgd_delta_workspace", "wpsgd_delta_run", "wpsgd_delta_grad", "wpsgd_delta_step",
 ]
 
@@ -93,6 +93,7 @@ def load_library() -> ctypes.CDLL:
     lib.wpsgd_gather_rows.argtypes = [vp, vp, ci, i64, i64, vp, i64, i32, vp, i64, i64]
     lib.wpsgd_combine_rows.argtypes = [vp, vp, ci, i64, i64, i64, vp, vp, i64, i32, vp, i64]
     lib.wpsgd_combine_rows_grad.argtypes = [vp, vp, i64, vp, i64, ci, i64, i64, vp, vp, i64, i32, vp, i64, vp]
+    lib.wpsgd_clear_rows.argtypes = [vp, vp, i64, i32, vp, ci, i64, i64, i64, vp]
     lib.wpsgd_delta_workspace.argtypes = [vp, ci, ctypes.POINTER(i64)]
     lib.wpsgd_delta_run.argtypes = [vp, vp, vp, vp, vp, i64, ci, vp, i64]
     lib.wpsgd_delta_grad.argtypes = [vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64]
@@ -547,7 +548,7 @@ class Context:
         return r if r.__class__ is not int else self._ck(r, "wpsgd_combine_rows")
 
     def combine_rows_grad(self, dout, Y, where, weights=None, dY=None, dweights=None):
-        """Gradients of combine_rows: (dY like Y, whose rows without a place stay as they are, and dweights [n, top] fp32)."""
+        """Gradients of combine_rows: (dY like Y, and dweights [n, top] fp32). Rows of Y that no place has: zeros in a new dY, a given one keeps what it has there."""
         r = self._rows.combine_rows_grad(*self._head, dout, Y, where, weights, dY, dweights)
         return r if r.__class__ is tuple else self._ck(r, "wpsgd_combine_rows_grad")
 

@@ -258,6 +258,13 @@ bool int32_of(PyObject* o, const char* what, int32_t* v) {
   return n == (int32_t)n;
 }
 
+// A new tensor of rows that a call is about to write where a place has them: zeros elsewhere. 0, or the library's status
+int cleared(const Call& c, const Matrix& where, const at::Tensor& rows) {
+  const int64_t n = rows.size(0), d = rows.size(1);
+  const at::Tensor marks = empty(c, {(n + 31) / 32}, {1}, at::kInt);
+  return wpsgd_clear_rows(c.ctx, (const int32_t*)where.p, where.n, (int32_t)where.ld, rows.data_ptr(), element(rows.scalar_type()), d, d, n, (uint32_t*)marks.data_ptr());
+}
+
 // (head, node, n_nodes) -> (where, order, shard_off)
 PyObject* sort_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
@@ -329,8 +336,13 @@ PyObject* combine_rows_grad(PyObject*, PyObject* const* args, Py_ssize_t n_args)
   if (args[7] != Py_None && (!places(args[7], c, at::kFloat, "weights", &weights) || !same_places(where, weights, "weights"))) return nullptr;
   if (dout.n != where.n) return PyErr_Format(PyExc_ValueError, "dout has %lld rows, where %lld", (long long)dout.n, (long long)where.n);
   Output dy, dw;
-  if (args[8] == Py_None) dy.take(empty(c, {y.n, d}, {d, 1}, y.type));
-  else dy.take(args[8]);
+  if (args[8] == Py_None) {
+    at::Tensor t = empty(c, {y.n, d}, {d, 1}, y.type);
+    if (const int st = cleared(c, where, t)) return PyLong_FromLong(st);
+    dy.take(std::move(t));
+  } else {
+    dy.take(args[8]);
+  }
   if (args[9] == Py_None) dw.take(empty(c, {where.n, where.ld}, {where.ld, 1}, at::kFloat));
   else dw.take(args[9]);
   if (!rows_like(dy.o, c, d, &y, "dY", &to) || !places(dw.o, c, at::kFloat, "dweights", &tow) || !same_places(where, tow, "dweights")) return nullptr;

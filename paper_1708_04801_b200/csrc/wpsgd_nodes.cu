@@ -160,4 +160,27 @@ wpsgd_status wpsgd_combine_rows_grad(wpsgd_ctx* c, const void* dout, int64_t ld_
   return WPSGD_OK;
 }
 
+wpsgd_status wpsgd_clear_rows(wpsgd_ctx* c, const int32_t* where, int64_t n_rows, int32_t top, void* out, wpsgd_xtype xt, int64_t ld_out, int64_t d, int64_t n_sorted, uint32_t* marks) {
+  if (!c) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "ctx is NULL");
+  if (const char* why = check_places(where, n_rows, top)) return refuse(c, "clear_rows", why);
+  if (const char* why = check_rows(out, xt, ld_out, d, n_sorted)) return refuse(c, "clear_rows", why);
+  if ((n_sorted > 0 && !marks) || (uintptr_t)marks % 4) return refuse(c, "clear_rows", "marks are NULL or not aligned to their elements");
+  const long long es = (long long)element_size(xt), words = (n_sorted + 31) / 32 * 4, places = n_rows * top * 4ll;
+  const Region to = rows_region(out, xt, ld_out, d, n_sorted), bits = {marks, words, words, 1}, in = {where, places, places, 1};
+  if (meet(to, bits) || meet(to, in) || meet(bits, in)) return refuse(c, "clear_rows", "arrays overlap");
+  if (n_sorted == 0) return WPSGD_OK;
+  DeviceGuard guard(c->device);
+  // Few bytes: all of them in one launch. 16 MB take as long as the three launches do.
+  if (n_sorted * d * es <= 16 << 20 && ld_out * es <= INT32_MAX) {
+    CU_TRY(c, cudaMemset2DAsync(out, ld_out * es, 0, d * es, n_sorted, c->stream));
+    return WPSGD_OK;
+  }
+  const ClearParams p = {where, n_rows * top, n_sorted, marks, (char*)out, ld_out * es, (int)(d * es), (int)es};
+  CU_TRY(c, cudaMemsetAsync(marks, 0, words, c->stream));
+  CU_TRY(c, launch(mark_places_kernel, (unsigned)grid_for(std::max(p.places, 1ll), 256), 256, 0, c->stream, p));
+  CU_TRY(c, launch(clear_rows_kernel, (unsigned)grid_for((n_sorted + 31) / 32, 8), 256, 0, c->stream, p));
+  c->launches += 2;
+  return WPSGD_OK;
+}
+
 }  // extern "C"

@@ -1,0 +1,88 @@
+"""Rows that a call leaves out, through the public entry points: tensors that a call itself makes hold zeros there and nothing left over, models of chains that are
+left out are those they started from, and rows outside every chain are not read. Everything here is exact."""
+import ctypes
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def P(wpsgd_lib):
+    import paper_1708_04801_b200 as pkg
+
+    return pkg
+
+
+@pytest.fixture(scope="module")
+def ctx(P):
+    with P.Context(4, 8) as c:
+        yield c
+        c.check()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def leave_nans(*like):
+    """Memory of these shapes given back full of NaN, enough of it that the next tensor of such a shape is made of it."""
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    made = [torch.full(shape, float("nan"), dtype=dtype, device="cuda") for shape, dtype in like for _ in range(40)]
+    torch.cuda.synchronize()
+    del made
+
+
+def chain_rows(n, hk, hv, dk, dv, dtype, seed=0):
+    g = gen(seed + n)
+    q, k, v = (torch.randn(s, generator=g) for s in ((n, hk, dk), (n, hk, dk), (n, hv, dv)))
+    q, k = (x / x.norm(dim=-1, keepdim=True).clamp_min(1e-6) for x in (q, k))
+    decay = -torch.exp(torch.randn((n, hv), generator=g) - 2.0)
+    return [x.to(dtype).cuda() for x in (q, k, v, decay, torch.sigmoid(torch.randn((n, hv), generator=g)))]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,top,d", [(1, 1, 8), (40, 2, 999), (300, 3, 64), (3001, 4, 1001), (2500, 2, 4096)])
+def test_new_gradients_of_combine_are_zeros_where_no_place_is(ctx, dtype, n, top, d):
+    node = torch.randint(0, 5, (n, top), generator=gen(n), dtype=torch.int32)
+    node[torch.rand((n, top), generator=gen(1)) < 0.3] = -1
+    node[0, 0] = -1
+    where, _, off = ctx.sort_rows(node.cuda(), 5)
+    y, dout = (torch.randn(s, generator=gen(i)).to(dtype).cuda() for i, s in enumerate([(n * top, d), (n, d)]))
+    w = torch.rand((n, top), generator=gen(2)).cuda()
+    want, want_w = ctx.combine_rows_grad(dout, y, where, w, torch.zeros_like(y))
+    leave_nans((y.shape, dtype))
+    dy, dw = ctx.combine_rows_grad(dout, y, where, w)
+    ctx.check()
+    assert int(off[-1]) < n * top and torch.equal(dy, want) and torch.equal(dw, want_w)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n_sorted,d,pad,offset", [(1, 1, 0, 0), (33, 7, 1, 3), (100, 64, 0, 0), (4001, 2100, 0, 0), (4001, 2100, 5, 3), (2000, 5003, 2, 1), (1 << 21, 5, 0, 1), (700, 20000, 8, 8)])
+def test_clear_rows(P, ctx, dtype, n_sorted, d, pad, offset):
+    """Rows without a place are zeros after it, what lies between rows is as it was; few bytes and many, rows that start anywhere."""
+    lib = P.load_library()
+    flat = torch.full((offset + n_sorted * (d + pad) + 64,), 7.0, dtype=dtype, device="cuda")
+    rows = flat[offset:offset + n_sorted * (d + pad)].view(n_sorted, d + pad)
+    where = torch.randint(-1, n_sorted + 2, (n_sorted // 3 + 1, 2), generator=gen(d), dtype=torch.int32)
+    where[0, 0], where[0, 1] = n_sorted - 1, 2 ** 31 - 1
+    marks = torch.full(((n_sorted + 31) // 32,), -1, dtype=torch.int32, device="cuda")
+    on = where.cuda()
+    torch.cuda.synchronize()
+    assert lib.wpsgd_clear_rows(ctx._h, on.data_ptr(), len(where), 2, rows.data_ptr(), int(dtype is torch.bfloat16), d + pad, d, n_sorted, marks.data_ptr()) == 0
+    ctx.check()
+    has = torch.zeros(n_sorted, dtype=torch.bool)
+    has[where[(where >= 0) & (where < n_sorted)].long()] = True
+    without = (~has).cuda()
+    assert not bool(rows[without, :d].any()) and bool((rows[:, d:] == 7).all()) and bool((flat[:offset] == 7).all()) and bool((flat[offset + n_sorted * (d + pad):] == 7).all())
+    if n_sorted * d * flat.element_size() > 16 << 20:
+        assert bool((rows[~without, :d] == 7).all())  # many bytes: no other row is touched
+    for args in ((None, len(where), 2, rows.data_ptr(), 0, d + pad, d, n_sorted, marks.data_ptr()), (on.data_ptr(), len(where), 2, rows.data_ptr(), 0, d + pad, d, n_sorted, None),
+                 (on.data_ptr(), len(where), 2, rows.data_ptr(), 7, d + pad, d, n_sorted, marks.data_ptr()), (on.data_ptr(), len(where), 0, rows.data_ptr(), 0, d + pad, d, n_sorted, marks.data_ptr()),
+                 (on.data_ptr(), len(where), 2, on.data_ptr(), 0, 1, 1, 1, marks.data_ptr()), (on.data_ptr(), len(where), 2, marks.data_ptr(), 0, 1, 1, 1, marks.data_ptr()),
+                 (on.data_ptr(), len(where), 2, rows.data_ptr(), 0, d + pad, d, n_sorted, on.data_ptr())):
+        assert lib.wpsgd_clear_rows(ctx._h, *args) == 1 and lib.wpsgd_last_error(ctx._h).startswith(b"clear_rows:")
