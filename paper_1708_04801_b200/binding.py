@@ -538,7 +538,8 @@ class Context:
         return r if r.__class__ is tuple else self._ck(r, "wpsgd_sort_rows")
 
     def gather_rows(self, X, where, out=None):
-        """Rows in the order of their nodes: out[where[i, j]] = X[i]. A new `out` has a row for every place; rows without one stay as they are."""
+        """Rows in the order of their nodes: out[where[i, j]] = X[i]. A new `out` has a row for every place, zeros in those behind the last
+        position; rows of a given one that no place has stay as they are."""
         r = self._rows.gather_rows(*self._head, X, where, out)
         return r if r.__class__ is not int else self._ck(r, "wpsgd_gather_rows")
 

@@ -294,8 +294,13 @@ PyObject* gather_rows(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   if (!count(n_args, 7) || !head(args, &c) || (d = columns(args[4], c, "X")) < 0 || !rows_like(args[4], c, d, nullptr, "X", &x) || !places(args[5], c, at::kInt, "where", &where)) return nullptr;
   if (x.n != where.n) return PyErr_Format(PyExc_ValueError, "where has %lld rows, X %lld", (long long)where.n, (long long)x.n);
   Output out;
-  if (args[6] == Py_None) out.take(empty(c, {where.n * where.ld, d}, {d, 1}, x.type));
-  else out.take(args[6]);
+  if (args[6] == Py_None) {
+    at::Tensor t = empty(c, {where.n * where.ld, d}, {d, 1}, x.type);
+    if (const int st = cleared(c, where, t)) return PyLong_FromLong(st);
+    out.take(std::move(t));
+  } else {
+    out.take(args[6]);
+  }
   if (!rows_like(out.o, c, d, &x, "out", &to)) return nullptr;
   const wpsgd_status st = wpsgd_gather_rows(c.ctx, x.p, element(x.type), x.ld, d, (const int32_t*)where.p, where.n, (int32_t)where.ld, to.p, to.ld, to.n);
   if (st) return PyLong_FromLong(st);

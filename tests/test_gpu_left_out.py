@@ -86,3 +86,18 @@ def test_clear_rows(P, ctx, dtype, n_sorted, d, pad, offset):
                  (on.data_ptr(), len(where), 2, on.data_ptr(), 0, 1, 1, 1, marks.data_ptr()), (on.data_ptr(), len(where), 2, marks.data_ptr(), 0, 1, 1, 1, marks.data_ptr()),
                  (on.data_ptr(), len(where), 2, rows.data_ptr(), 0, d + pad, d, n_sorted, on.data_ptr())):
         assert lib.wpsgd_clear_rows(ctx._h, *args) == 1 and lib.wpsgd_last_error(ctx._h).startswith(b"clear_rows:")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,top,d", [(1, 1, 8), (40, 2, 999), (300, 3, 64), (3001, 4, 1001), (2500, 2, 4096)])
+def test_new_rows_of_gather_are_zeros_where_no_place_is(ctx, dtype, n, top, d):
+    node = torch.randint(0, 5, (n, top), generator=gen(n), dtype=torch.int32)
+    node[torch.rand((n, top), generator=gen(1)) < 0.3] = -1
+    node[0, 0] = -1
+    where, _, off = ctx.sort_rows(node.cuda(), 5)
+    x = torch.randn((n, d), generator=gen(3)).to(dtype).cuda()
+    want = ctx.gather_rows(x, where, torch.zeros((n * top, d), dtype=dtype, device="cuda"))
+    leave_nans(((n * top, d), dtype))
+    got = ctx.gather_rows(x, where)
+    ctx.check()
+    assert int(off[-1]) < n * top and torch.equal(got, want)
