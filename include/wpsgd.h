@@ -370,7 +370,7 @@ wpsgd_status wpsgd_delta_run(wpsgd_ctx* ctx, const wpsgd_delta_rows* rows, const
  * only read.
  *   dout       DEVICE [n_rows, heads_v, dv], rows ld_dout apart: gradient of out.
  *   dW         DEVICE [n_chains, heads_v, dv, dk] fp32: gradient of the models at the end, or NULL for zeros.
- *   dq, dk, dv, dg, dbeta   DEVICE, contiguous, of the rows' type, shaped as q, k, v, g and beta; rows outside every chain stay as they are.
+ *   dq, dk, dv, dg, dbeta   DEVICE, contiguous, of the rows' type, shaped as q, k, v, g and beta; zeros in rows outside every chain.
  *   dW0        DEVICE fp32: gradient of the models at the start, or NULL. May be dW. */
 wpsgd_status wpsgd_delta_grad(wpsgd_ctx* ctx, const wpsgd_delta_rows* rows, const void* saved, int64_t saved_bytes, const void* dout, int64_t ld_dout, const float* dW,
                               void* dq, void* dk, void* dv, void* dg, void* dbeta, float* dW0, void* workspace, int64_t workspace_bytes);

@@ -565,7 +565,7 @@ class Context:
 
     def delta_grad(self, saved: "DeltaSaved", dout, dW=None, start: bool = False):
         """Gradients of a delta_run with save=True from those of its answers and, if given, of its final models: (dq, dk, dv, dg, dbeta, dW0), the
-        last None unless start=True asks for the gradient of the models it started from. Rows outside every chain are not written."""
+        last None unless start=True asks for the gradient of the models it started from. Rows outside every chain have gradients of zero."""
         r = self._rows.delta_grad(*self._head, *saved.args, dout, dW, bool(start))
         return r if r.__class__ is tuple else self._ck(r, "wpsgd_delta_grad")
 

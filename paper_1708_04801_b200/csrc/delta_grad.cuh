@@ -255,6 +255,29 @@ struct RowsShape {
 };
 static_assert(RowsShape<128>::smem <= 226 * 1024, "must fit an SM");
 
+// Zeros in elements from `begin` to `end` - 1, by the threads of the whole grid
+__device__ __forceinline__ void clear_span(__nv_bfloat16* p, long long begin, long long end) {
+  unsigned short* const first = (unsigned short*)p + begin;
+  const long long n = end - begin, ahead = min((long long)((-(uintptr_t)first & 15) / 2), n), units = (n - ahead) / 8;  // elements before the first whole 16 bytes, and those
+  const long long at = (long long)blockIdx.x * blockDim.x + threadIdx.x, step = (long long)gridDim.x * blockDim.x;
+  for (long long u = at; u < units; u += step) *(uint4*)(first + ahead + u * 8) = make_uint4(0u, 0u, 0u, 0u);
+  if (at < n - units * 8) first[at < ahead ? at : at + units * 8] = 0;  // fewer than 16 at the ends
+}
+// Rows outside every chain have no part in the answers: their gradients are zeros
+__device__ __noinline__ void clear_outside(const DeltaGradParams& gp, long long lo, long long hi) {
+  const DeltaChunkParams& p = gp.f;
+  const long long wk = (long long)p.hk * p.dk, wv = (long long)p.hv * p.dv;
+  for (int side = 0; side < 2; ++side) {
+    const long long begin = side ? hi : 0, end = side ? p.n_rows : lo;
+    if (begin >= end) continue;
+    clear_span(gp.dq, begin * wk, end * wk);
+    clear_span(gp.dk, begin * wk, end * wk);
+    clear_span(gp.dv, begin * wv, end * wv);
+    clear_span(gp.dg, begin * p.hv, end * p.hv);
+    clear_span(gp.dbeta, begin * p.hv, end * p.hv);
+  }
+}
+
 template <int DK>
 __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __grid_constant__ DeltaGradParams gp) {
   using Shape = RowsShape<DK>;
@@ -282,6 +305,10 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
   // Pieces: all heads of labels of a (chunk, head of features), then the next of this block's. What a copy needs is kept beside them: a piece changes once in
   // several slices, and the divisions would cost more instructions than the products.
   const int chunks = p.chunk_off[p.n_chains], chunk_step = gridDim.x / p.hk, head_step = gridDim.x % p.hk;
+  {
+    const long long lo = chunks > 0 ? p.chunks[0].row0 : 0, hi = chunks > 0 ? p.chunks[chunks - 1].row0 + p.chunks[chunks - 1].len : 0;
+    if (lo > 0 || hi < p.n_rows) clear_outside(gp, lo, hi);
+  }
   struct Piece {
     int chunk, kh, hh, slice, len;
     long long row0;

@@ -334,7 +334,12 @@ wpsgd_status wpsgd_delta_grad(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const 
   const long long n = rows->n_rows, wk = (long long)rows->heads_k * rows->dk * 2, wv = (long long)rows->heads_v * rows->dv * 2, wh = rows->heads_v * 2ll, models = model_bytes(rows, rows->n_chains);
   if (ld_dout < wv / 2 || ld_dout > INT64_MAX / 8 / std::max<long long>(n, 1) || (n > 0 && (!dout || !dq || !dk || !dv || !dg || !dbeta))) return refuse(c, "delta_grad", "NULL argument, or the stride of dout is below the width of a row");
   if (((uintptr_t)dout | (uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv | (uintptr_t)dg | (uintptr_t)dbeta) % 2 || ((uintptr_t)dW | (uintptr_t)dW0) % 4) return refuse(c, "delta_grad", "an argument is not aligned to its elements");
-  if (rows->n_chains == 0) return WPSGD_OK;
+  if (rows->n_chains == 0) {  // all rows are outside
+    DeviceGuard guard(c->device);
+    if (n > 0)
+      for (const auto& [p, bytes] : {std::pair<void*, long long>{dq, n * wk}, {dk, n * wk}, {dv, n * wv}, {dg, n * wh}, {dbeta, n * wh}}) CU_TRY(c, cudaMemsetAsync(p, 0, bytes, c->stream));
+    return WPSGD_OK;
+  }
   const DeltaLayout lay(rows, true);
   const DeltaGradLayout own(rows, lay, dout, ld_dout);
   if (!saved || !aligned16(saved) || saved_bytes < (long long)lay.total) return refuse(c, "delta_grad", "what the run saved is NULL, not aligned to 16 bytes or too small");

@@ -101,3 +101,25 @@ def test_new_rows_of_gather_are_zeros_where_no_place_is(ctx, dtype, n, top, d):
     got = ctx.gather_rows(x, where)
     ctx.check()
     assert int(off[-1]) < n * top and torch.equal(got, want)
+
+
+LEFT = [  # lengths, first row, rows behind, heads_k, heads_v, dk, dv
+    ([1, 1], 0, 1, 1, 1, 16, 16), ([0, 30, 65], 7, 200, 2, 4, 64, 32), ([100, 28], 300, 5, 2, 2, 60, 33), ([64], 1, 0, 1, 3, 128, 128), ([0, 0], 4, 90, 1, 2, 31, 70), ([], 0, 66, 1, 2, 24, 16),
+    ([5] * 40, 3000, 3000, 1, 1, 128, 80),
+]
+
+
+@pytest.mark.parametrize("lengths,first,behind,hk,hv,dk,dv", LEFT)
+def test_gradients_of_rows_outside_every_chain_are_zeros(ctx, lengths, first, behind, hk, hv, dk, dv):
+    n, end = first + sum(lengths) + behind, first + sum(lengths)
+    rows = chain_rows(n, hk, hv, dk, dv, torch.bfloat16)
+    off = torch.tensor([first] + lengths).cumsum(0).cuda()
+    dout = torch.randn((n, hv, dv), generator=gen(4)).to(torch.bfloat16).cuda()
+    _, _, saved = ctx.delta_run(*rows, off, save=True)
+    leave_nans(*[(x.shape, torch.bfloat16) for x in rows])
+    got = ctx.delta_grad(saved, dout)[:5]
+    ctx.check()
+    few = [x[first:end].contiguous() for x in rows]  # the same rows without those around them
+    want = ctx.delta_grad(ctx.delta_run(*few, off - first, save=True)[2], dout[first:end].contiguous())[:5] if end > first else [x[:0] for x in rows]
+    for a, b in zip(got, want):
+        assert torch.equal(a[first:end], b) and not bool(a[:first].any()) and not bool(a[end:].any())
