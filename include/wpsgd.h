@@ -352,7 +352,7 @@ typedef struct {
   float scale;
 } wpsgd_delta_rows;
 
-typedef enum { WPSGD_DELTA_RUN = 0, WPSGD_DELTA_RUN_SAVE = 1, WPSGD_DELTA_GRAD = 2 } wpsgd_delta_use;
+typedef enum { WPSGD_DELTA_RUN = 0, WPSGD_DELTA_RUN_SAVE = 1, WPSGD_DELTA_GRAD = 2, WPSGD_DELTA_NEW_OUT = 4 } wpsgd_delta_use;
 
 /* Bytes of workspace for `rows` (sizes, strides, pointers and type are read; nothing is followed): for wpsgd_delta_run, for wpsgd_delta_run whose
  * workspace then goes to wpsgd_delta_grad, and for wpsgd_delta_grad itself. */
@@ -362,7 +362,8 @@ wpsgd_status wpsgd_delta_workspace(const wpsgd_delta_rows* rows, wpsgd_delta_use
  *   W0         DEVICE [n_chains, heads_v, dv, dk] models to start from, or NULL for zeros.
  *   W_out      DEVICE, the same shape: the models at the end, or NULL. May be W0.
  *   out        DEVICE [n_rows, heads_v, dv], rows ld_out apart, of the rows' type. Rows outside every chain stay as they are.
- *   use        WPSGD_DELTA_RUN, or WPSGD_DELTA_RUN_SAVE (bf16 rows): the workspace keeps what wpsgd_delta_grad needs. */
+ *   use        WPSGD_DELTA_RUN, or WPSGD_DELTA_RUN_SAVE (bf16 rows): the workspace keeps what wpsgd_delta_grad needs. With WPSGD_DELTA_NEW_OUT added, out is new
+ *              memory: rows outside every chain get zeros. (The workspace's size is that of the use without it.) */
 wpsgd_status wpsgd_delta_run(wpsgd_ctx* ctx, const wpsgd_delta_rows* rows, const float* W0, float* W_out, void* out, int64_t ld_out,
                              wpsgd_delta_use use, void* workspace, int64_t workspace_bytes);
 

@@ -557,7 +557,8 @@ class Context:
     def delta_run(self, q, k, v, g, beta, shard_off, W0=None, scale: Optional[float] = None, W_out=None, out=None, save: bool = False):
         """Runs chains of the gated delta rule (see wpsgd_delta_run): q, k [n, heads_k, dk], v [n, heads_v, dv], g (log decay) and beta
         [n, heads_v], float32 or bfloat16, shard_off [n_chains + 1] int64 on the device. Returns (out like v, models [n_chains, heads_v, dv, dk] fp32), and
-        with save=True (bfloat16) a DeltaSaved for delta_grad as well. scale defaults to dk ** -0.5."""
+        with save=True (bfloat16) a DeltaSaved for delta_grad as well. scale defaults to dk ** -0.5. Rows outside every chain: zeros in a new out, a given one
+        keeps what it has there."""
         r = self._rows.delta_run(*self._head, q, k, v, g, beta, scale, shard_off, W0, W_out, out, bool(save))
         if r.__class__ is not tuple:
             self._ck(r, "wpsgd_delta_run")

@@ -80,6 +80,7 @@ struct DeltaChunkParams {
   __nv_bfloat16* out;
   long long ld_out;
   int vec_out, slices;
+  int new_out;  // answers of rows outside the chains are set to zeros
   int maps;  // whole chunks come by tensor maps
   int prep_heads;
   long long spin_limit, drop;
@@ -281,6 +282,20 @@ __device__ __forceinline__ void put_negative_t(uint32_t at, const float (&c0)[4]
   stsm_t(at + DC_T_LO, lo[0], lo[1], lo[2], lo[3]);
 }
 
+// Answers of rows outside the chains set to zeros: every `blocks`th such row from the `block`th on
+__device__ __noinline__ void clear_answers(const DeltaChunkParams& p, int chunks, long long block, long long blocks) {
+  const long long lo = chunks > 0 ? p.chunks[0].row0 : 0, hi = chunks > 0 ? p.chunks[chunks - 1].row0 + p.chunks[chunks - 1].len : 0;
+  const int width = p.hv * p.dv;
+  for (long long i = block; i < lo + p.n_rows - hi; i += blocks) {
+    __nv_bfloat16* row = p.out + (i < lo ? i : hi + i - lo) * p.ld_out;
+    if (p.vec_out) {
+      for (int c = threadIdx.x * 8; c < width; c += PREP_THREADS * 8) *(uint4*)(row + c) = make_uint4(0u, 0u, 0u, 0u);
+    } else {
+      for (int c = threadIdx.x; c < width; c += PREP_THREADS) ((unsigned short*)row)[c] = 0;
+    }
+  }
+}
+
 template <int DK>
 __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __grid_constant__ DeltaChunkParams p) {
   constexpr int ROW = PrepShape<DK>::row;
@@ -295,7 +310,11 @@ __global__ void __launch_bounds__(PREP_THREADS) delta_prepare_kernel(const __gri
   kernel_started();
   kernel_inputs_ready();
   const int groups = p.hv / p.prep_heads, chunk = blockIdx.x / groups, h0 = blockIdx.x % groups * p.prep_heads, kh = h0 / (p.hv / p.hk);
-  if (chunk >= p.chunk_off[p.n_chains]) return;
+  const int chunks = p.chunk_off[p.n_chains];
+  if (chunk >= chunks) {
+    if (p.new_out) clear_answers(p, chunks, (long long)blockIdx.x - (long long)chunks * groups, (long long)gridDim.x - (long long)chunks * groups);
+    return;
+  }
   const DeltaChunk at = p.chunks[chunk];
 
   for (int u = tid; u < DC * (DK / 8); u += PREP_THREADS) {

@@ -264,8 +264,9 @@ __device__ __forceinline__ void clear_span(__nv_bfloat16* p, long long begin, lo
   if (at < n - units * 8) first[at < ahead ? at : at + units * 8] = 0;  // fewer than 16 at the ends
 }
 // Rows outside every chain have no part in the answers: their gradients are zeros
-__device__ __noinline__ void clear_outside(const DeltaGradParams& gp, long long lo, long long hi) {
+__device__ __forceinline__ void clear_outside(const DeltaGradParams& gp, int chunks) {
   const DeltaChunkParams& p = gp.f;
+  const long long lo = chunks > 0 ? p.chunks[0].row0 : 0, hi = chunks > 0 ? p.chunks[chunks - 1].row0 + p.chunks[chunks - 1].len : 0;
   const long long wk = (long long)p.hk * p.dk, wv = (long long)p.hv * p.dv;
   for (int side = 0; side < 2; ++side) {
     const long long begin = side ? hi : 0, end = side ? p.n_rows : lo;
@@ -305,10 +306,6 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
   // Pieces: all heads of labels of a (chunk, head of features), then the next of this block's. What a copy needs is kept beside them: a piece changes once in
   // several slices, and the divisions would cost more instructions than the products.
   const int chunks = p.chunk_off[p.n_chains], chunk_step = gridDim.x / p.hk, head_step = gridDim.x % p.hk;
-  {
-    const long long lo = chunks > 0 ? p.chunks[0].row0 : 0, hi = chunks > 0 ? p.chunks[chunks - 1].row0 + p.chunks[chunks - 1].len : 0;
-    if (lo > 0 || hi < p.n_rows) clear_outside(gp, lo, hi);
-  }
   struct Piece {
     int chunk, kh, hh, slice, len;
     long long row0;
@@ -654,6 +651,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) delta_rowgrad_kernel(const __gri
   }
   kernel_started();
   copies_done();
+  clear_outside(gp, chunks);
 }
 
 }  // namespace wpsgd

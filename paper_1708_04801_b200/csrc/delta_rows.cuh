@@ -27,6 +27,7 @@ struct DeltaRowsParams {
   int hk, hv, dk, dv;
   float scale;
   int vec;  // features and models can be loaded four at a time
+  int new_out;  // answers of rows outside the chains are set to zeros
   DevStatus* status;
 };
 
@@ -261,6 +262,15 @@ __global__ void __launch_bounds__(32 * DELTA_WARPS) delta_rows_kernel(const __gr
   if (p.W && there)
 #pragma unroll
     for (int j = 0; j < NJ; ++j) put_model4(p.W + at, 4 * (s + 8 * j), p.dk, p.vec, w + 4 * j);
+  if (p.new_out) {  // rows before the first chain and behind the last, the block's 16 columns of them
+    const int col = R0 + (tid & 15);
+    auto clear = [&](long long begin, long long stop) {
+      for (long long r = begin + (tid >> 4); r < stop; r += 2 * DELTA_WARPS)
+        if (col < models) ((float*)p.out)[r * p.ld_out + col] = 0.0f;
+    };
+    if (chain == 0) clear(0, first);
+    if (chain + 1 == p.n_chains) clear(end, p.n_rows);
+  }
 }
 
 // ---- one row for each of many chains ------------------------------------------------------------------------------------------------

@@ -473,7 +473,8 @@ PyObject* delta_run(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   at::Tensor ws;
   int64_t bytes = 0;
   workspace(c, r, use, &ws, &bytes);
-  const wpsgd_status st = wpsgd_delta_run(c.ctx, &r, W0, W1, (void*)o.p, o.ld, use, bytes ? ws.data_ptr() : nullptr, bytes);
+  const wpsgd_delta_use whole = args[13] == Py_None ? (wpsgd_delta_use)(use | WPSGD_DELTA_NEW_OUT) : use;
+  const wpsgd_status st = wpsgd_delta_run(c.ctx, &r, W0, W1, (void*)o.p, o.ld, whole, bytes ? ws.data_ptr() : nullptr, bytes);
   if (st) return PyLong_FromLong(st);
   if (use == WPSGD_DELTA_RUN_SAVE) saved.take(std::move(ws));
   else saved.take(Py_None);

@@ -53,7 +53,7 @@ DeltaRowsParams rows_params(const wpsgd_ctx* c, const wpsgd_delta_rows* r, void*
   const size_t es = element_size(r->type), unit = 4 * es;
   const bool vec = r->dk % 4 == 0 && ((uintptr_t)r->q | (uintptr_t)r->k) % unit == 0 && (r->ld_q | r->ld_k) % 4 == 0 && aligned16(W0) && aligned16(W);
   return {r->q, r->k, r->v, r->g, r->beta, r->ld_q, r->ld_k, r->ld_v, r->ld_g, r->ld_beta, ld_out, out, W0, W, r->n_rows, (const long long*)r->shard_off, r->n_chains, nullptr, 0,
-          r->heads_k, r->heads_v, r->dk, r->dv, r->scale, vec, c->status};
+          r->heads_k, r->heads_v, r->dk, r->dv, r->scale, vec, 0, c->status};
 }
 
 wpsgd_status run_rows(wpsgd_ctx* c, const DeltaRowsParams& p) {
@@ -222,7 +222,8 @@ wpsgd_status run_chunks(wpsgd_ctx* c, DeltaChunkParams p, const DeltaLayout& lay
     p.prep_heads = 1;
     for (int n = 2; n <= PREP_HEADS && lay.chunks * p.hv / n >= 148 * 8; ++n)
       if (p.hv / p.hk % n == 0) p.prep_heads = n;
-    CU_TRY(c, launch(delta_prepare_kernel<DK>, (unsigned)(lay.chunks * (p.hv / p.prep_heads)), PREP_THREADS, PrepShape<DK>::smem, c->stream, p));
+    const long long blocks = lay.chunks + p.new_out;  // those of no chunk clear what is outside the chains; one at least
+    CU_TRY(c, launch(delta_prepare_kernel<DK>, (unsigned)(blocks * (p.hv / p.prep_heads)), PREP_THREADS, PrepShape<DK>::smem, c->stream, p));
     c->launches++;
   }
   DeltaMaps maps = {};
@@ -302,12 +303,19 @@ wpsgd_status wpsgd_delta_run(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const f
   if (((uintptr_t)W0 | (uintptr_t)W_out) % 4) return refuse(c, "delta_run", "models are not aligned to their elements");
   const Region to = {out, wv * es, ld_out * es, rows->n_rows}, from = block_of(W0, model_bytes(rows, rows->n_chains)), models = block_of(W_out, model_bytes(rows, rows->n_chains));
   if (meets_rows(to, rows, true) || meets_rows(models, rows, true) || meet(to, from) || meet(to, models) || (W0 != W_out && meet(from, models))) return refuse(c, "delta_run", "an output overlaps an input or another output");
-  if (use != WPSGD_DELTA_RUN && use != WPSGD_DELTA_RUN_SAVE) return refuse(c, "delta_run", "unknown use");
-  if (use == WPSGD_DELTA_RUN_SAVE && rows->type != WPSGD_X_BF16) return refuse(c, "delta_run", "gradients are of bf16 rows", WPSGD_ERR_UNSUPPORTED);
-  if (rows->n_chains == 0) return WPSGD_OK;
+  if ((int)use & ~(WPSGD_DELTA_RUN_SAVE | WPSGD_DELTA_NEW_OUT)) return refuse(c, "delta_run", "unknown use");
+  const bool save = (int)use & WPSGD_DELTA_RUN_SAVE, new_out = (int)use & WPSGD_DELTA_NEW_OUT;
+  if (save && rows->type != WPSGD_X_BF16) return refuse(c, "delta_run", "gradients are of bf16 rows", WPSGD_ERR_UNSUPPORTED);
   DeviceGuard guard(c->device);
-  if (rows->type == WPSGD_X_F32) return run_rows(c, rows_params(c, rows, out, ld_out, W0, W_out));
-  const bool save = use == WPSGD_DELTA_RUN_SAVE;
+  if (rows->n_chains == 0) {  // all rows are outside
+    if (new_out && rows->n_rows > 0) CU_TRY(c, cudaMemset2DAsync(out, (rows->n_rows > 1 ? ld_out : wv) * es, 0, wv * es, rows->n_rows, c->stream));
+    return WPSGD_OK;
+  }
+  if (rows->type == WPSGD_X_F32) {
+    DeltaRowsParams p = rows_params(c, rows, out, ld_out, W0, W_out);
+    p.new_out = new_out;
+    return run_rows(c, p);
+  }
   const DeltaLayout lay(rows, save);
   if (!workspace || !aligned16(workspace) || workspace_bytes < (long long)lay.total) return refuse(c, "delta_run", "the workspace is NULL, not aligned to 16 bytes or too small");
   const Region ws = block_of(workspace, (long long)lay.total);
@@ -315,6 +323,7 @@ wpsgd_status wpsgd_delta_run(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const f
   DeltaChunkParams p = chunk_params(c, rows, lay, (unsigned char*)workspace);
   p.W0 = W0, p.W = W_out, p.out = (__nv_bfloat16*)out, p.ld_out = ld_out;
   p.vec_out = rows->dv % 8 == 0 && ld_out % 8 == 0 && aligned16(out);
+  p.new_out = new_out;
   Packs packs;
   if (lay.pack_k) packs.add(rows->q, rows->ld_q, rows->heads_k, rows->dk, p.q.p);
   if (lay.pack_k) packs.add(rows->k, rows->ld_k, rows->heads_k, rows->dk, p.k.p);

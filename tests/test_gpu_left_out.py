@@ -123,3 +123,20 @@ def test_gradients_of_rows_outside_every_chain_are_zeros(ctx, lengths, first, be
     want = ctx.delta_grad(ctx.delta_run(*few, off - first, save=True)[2], dout[first:end].contiguous())[:5] if end > first else [x[:0] for x in rows]
     for a, b in zip(got, want):
         assert torch.equal(a[first:end], b) and not bool(a[:first].any()) and not bool(a[end:].any())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lengths,first,behind,hk,hv,dk,dv", LEFT)
+def test_new_answers_of_rows_outside_every_chain_are_zeros(ctx, lengths, first, behind, hk, hv, dk, dv, dtype):
+    n, end = first + sum(lengths) + behind, first + sum(lengths)
+    rows = chain_rows(n, hk, hv, dk, dv, dtype)
+    off = torch.tensor([first] + lengths).cumsum(0).cuda()
+    want = torch.full((n, hv, dv), 5.0, dtype=dtype, device="cuda")
+    W = ctx.delta_run(*rows, off, out=want)[1]
+    assert bool((want[:first] == 5).all()) and bool((want[end:] == 5).all())  # a tensor that is given keeps what it has there
+    calls = [False, True] if dtype is torch.bfloat16 else [False]
+    for save in calls:
+        leave_nans((want.shape, dtype))
+        got = ctx.delta_run(*rows, off, save=save)
+        assert torch.equal(got[0][first:end], want[first:end]) and not bool(got[0][:first].any()) and not bool(got[0][end:].any()) and torch.equal(got[1], W)
+    ctx.check()
