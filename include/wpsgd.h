@@ -333,7 +333,8 @@ wpsgd_status wpsgd_clear_rows(wpsgd_ctx* ctx, const int32_t* where, int64_t n_ro
  * Rows: all of one type, DEVICE, row t of q at q + t * ld_q: q, k [n_rows, heads_k, dk], v [n_rows, heads_v, dv], g, beta [n_rows, heads_v], heads one behind
  * the other. Rows outside every chain are not read. dk and dv at most 128 (WPSGD_ERR_UNSUPPORTED). g is at most 0 in use; below -128 it counts as -128 (its
  * exponential is 0 in fp32). Lengths and offsets are read on the device: offsets that decrease or leave [0, n_rows] are reported by the next wpsgd_check
- * (WPSGD_ERR_CUDA); the chains concerned, or all of them, are left out then.
+ * (WPSGD_ERR_CUDA); the chains concerned (fp32 rows) or all of them (bf16 rows) are left out then: no row of theirs is answered, and they end with the models that they
+ * started from.
  *
  * Models are fp32, [n_chains, heads_v, dv, dk], and are kept in fp32 on the way. bf16 rows are taken 64 at a time on the tensor cores: products with
  * models, with the inverse of a chunk's triangular system and with its steps split their fp32 side into two bf16 parts (relative error of the models 4e-6

@@ -182,6 +182,23 @@ __device__ __forceinline__ void copy_features(const float* to, const float* row,
   }
 }
 
+// A model whose chain is left out ends as it started; eight threads have it
+__device__ __noinline__ void keep_model(const DeltaRowsParams& p, long long model, int s) {
+  for (long long i = model * p.dk + s; i < (model + 1) * p.dk; i += 8) p.W[i] = p.W0 ? p.W0[i] : 0.0f;
+}
+
+// Answers of the rows before the first chain and behind the last set to zeros, a block's 16 columns of them. (Apart, as keep_model: written out in the kernel they cost
+// 333 rows of 4 heads 0.5 of 17.7 us by other registers for the rows' loop.)
+__device__ __noinline__ void clear_outside_columns(const DeltaRowsParams& p, long long chain, long long first, long long end, int R0, int models) {
+  const int col = R0 + (threadIdx.x & 15);
+  auto clear = [&](long long begin, long long stop) {
+    for (long long r = begin + (threadIdx.x >> 4); r < stop; r += 2 * DELTA_WARPS)
+      if (col < models) ((float*)p.out)[r * p.ld_out + col] = 0.0f;
+  };
+  if (chain == 0) clear(0, first);
+  if (chain + 1 == p.n_chains) clear(end, p.n_rows);
+}
+
 template <int NJ>
 __global__ void __launch_bounds__(32 * DELTA_WARPS) delta_rows_kernel(const __grid_constant__ DeltaRowsParams p, int batch) {
   constexpr int UNITS = 8 * NJ;  // of four features
@@ -196,6 +213,7 @@ __global__ void __launch_bounds__(32 * DELTA_WARPS) delta_rows_kernel(const __gr
   const long long first = p.shard_off[chain], end = p.shard_off[chain + 1];
   if (first < 0 || end < first || end > p.n_rows) {  // the same for the whole block; other chains may be in order, and run
     if (tid == 0) set_status(p.status, DEV_BOUNDS, 22, chain);
+    if (p.W && there) keep_model(p, chain * models + R, s);
     return;
   }
   const int floats = rows_floats<NJ>(rows_heads(p.hk, p.hv, p.dv)), labels_at = 2 * heads * 32 * NJ;
@@ -262,15 +280,7 @@ __global__ void __launch_bounds__(32 * DELTA_WARPS) delta_rows_kernel(const __gr
   if (p.W && there)
 #pragma unroll
     for (int j = 0; j < NJ; ++j) put_model4(p.W + at, 4 * (s + 8 * j), p.dk, p.vec, w + 4 * j);
-  if (p.new_out) {  // rows before the first chain and behind the last, the block's 16 columns of them
-    const int col = R0 + (tid & 15);
-    auto clear = [&](long long begin, long long stop) {
-      for (long long r = begin + (tid >> 4); r < stop; r += 2 * DELTA_WARPS)
-        if (col < models) ((float*)p.out)[r * p.ld_out + col] = 0.0f;
-    };
-    if (chain == 0) clear(0, first);
-    if (chain + 1 == p.n_chains) clear(end, p.n_rows);
-  }
+  if (p.new_out) clear_outside_columns(p, chain, first, end, R0, models);
 }
 
 // ---- one row for each of many chains ------------------------------------------------------------------------------------------------

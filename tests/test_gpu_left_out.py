@@ -140,3 +140,24 @@ def test_new_answers_of_rows_outside_every_chain_are_zeros(ctx, lengths, first, 
         got = ctx.delta_run(*rows, off, save=save)
         assert torch.equal(got[0][first:end], want[first:end]) and not bool(got[0][:first].any()) and not bool(got[0][end:].any()) and torch.equal(got[1], W)
     ctx.check()
+
+
+@pytest.mark.parametrize("start", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_chains_that_are_left_out_keep_their_models(P, dtype, start):
+    rows = chain_rows(50, 1, 2, 16, 24, dtype)
+    W0 = torch.randn((2, 2, 24, 16), generator=gen(1)).cuda() if start else None
+    for off, good in (([0, 30, 20], 0), ([20, 10, 50], 1), ([0, 51, 52], None), ([-1, 20, 1 << 40], None)):
+        with P.Context(1, 1) as c:
+            out = torch.full((50, 2, 24), 7.0, dtype=dtype, device="cuda")
+            leave_nans(((2, 2, 24, 16), torch.float32))
+            _, W = c.delta_run(*rows, torch.tensor(off).cuda(), W0=W0, out=out)
+            with pytest.raises(P.WpsgdError):
+                c.check()
+            want, answered = (torch.zeros_like(W) if W0 is None else W0.clone()), torch.zeros(50, dtype=torch.bool)
+            if good is not None and dtype is torch.float32:  # row by row, chains whose offsets are in order run; in chunks none does
+                part = slice(off[good], off[good + 1])
+                answered[part] = True
+                o, want[good:good + 1] = c.delta_run(*[x[part] for x in rows], torch.tensor([0, off[good + 1] - off[good]]).cuda(), W0=None if W0 is None else W0[good:good + 1])
+                assert torch.equal(out[part], o)
+            assert torch.equal(W, want) and bool((out[~answered] == 7).all())
