@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) delta_plan_kernel(const __grid_c
 }
 
 // Heads of a width that is no multiple of 8, or that do not start on 16 bytes, laid out anew: [n_rows][heads][width rounded up], zeros behind. Up to three tensors in one launch,
-// one for each blockIdx.y. Rows outside the chains are copied too, and not used.
+// one for each blockIdx.y. Rows outside the chains are left out.
 struct DeltaPack {
   struct {
     const __nv_bfloat16* from;
@@ -220,15 +220,18 @@ struct DeltaPack {
     __nv_bfloat16* to;
     int heads, width;
   } t[3];
-  long long n_rows;
+  const int* chunk_off;  // of the plan
+  const DeltaChunk* chunks;
+  int n_chains;
 };
 __global__ void __launch_bounds__(256) delta_pack_kernel(const __grid_constant__ DeltaPack p) {
   kernel_started();
   kernel_inputs_ready();
   const auto& t = p.t[blockIdx.y];
-  const int per = (t.width + 7) / 8;
-  const long long units = p.n_rows * t.heads * per;
-  for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < units; u += (long long)gridDim.x * 256) {
+  const int per = (t.width + 7) / 8, chunks = p.chunk_off[p.n_chains];
+  if (chunks == 0) return;
+  const long long units = (long long)t.heads * per, begin = p.chunks[0].row0 * units, end = (p.chunks[chunks - 1].row0 + p.chunks[chunks - 1].len) * units;
+  for (long long u = begin + (long long)blockIdx.x * 256 + threadIdx.x; u < end; u += (long long)gridDim.x * 256) {
     const long long head = row_of(u, per), row = row_of(head, t.heads);
     const int col = (int)(u - head * per) * 8, h = (int)(head - row * t.heads);
     const unsigned short* src = (const unsigned short*)t.from + row * t.ld + (long long)h * t.width;

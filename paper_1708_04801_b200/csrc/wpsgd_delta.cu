@@ -150,10 +150,10 @@ struct Packs {
     p.t[n++] = {(const __nv_bfloat16*)from, ld, (__nv_bfloat16*)to, heads, width};
     most = std::max(most, (long long)heads * ((width + 7) / 8));
   }
-  wpsgd_status launch_for(wpsgd_ctx* c, long long n_rows) {
-    if (n == 0 || n_rows == 0) return WPSGD_OK;
-    p.n_rows = n_rows;
-    CU_TRY(c, launch(delta_pack_kernel, dim3(grid_for(n_rows * most, 256), n), 256, 0, c->stream, p));
+  wpsgd_status launch_for(wpsgd_ctx* c, const DeltaChunkParams& plan) {  // behind the plan's kernel
+    if (n == 0 || plan.n_rows == 0) return WPSGD_OK;
+    p.chunk_off = plan.chunk_off, p.chunks = plan.chunks, p.n_chains = plan.n_chains;
+    CU_TRY(c, launch(delta_pack_kernel, dim3(grid_for(plan.n_rows * most, 256), n), 256, 0, c->stream, p));
     c->launches++;
     return WPSGD_OK;
   }
@@ -213,9 +213,10 @@ wpsgd_status walk_tmem(wpsgd_ctx* c, const DeltaChunkParams& p, const DeltaMaps&
 }
 
 template <int DK>
-wpsgd_status run_chunks(wpsgd_ctx* c, DeltaChunkParams p, const DeltaLayout& lay, bool save) {
+wpsgd_status run_chunks(wpsgd_ctx* c, DeltaChunkParams p, const DeltaLayout& lay, bool save, Packs& packs) {
   CU_TRY(c, launch(delta_plan_kernel, 1, PLAN_THREADS, 0, c->stream, p));
   c->launches++;
+  if (const wpsgd_status s = packs.launch_for(c, p)) return s;
   if (lay.chunks > 0) {
     CU_TRY(c, (allow_smem<delta_prepare_kernel<DK>>(c)));
     // heads that share features by one block where that leaves every SM eight: their products of features are formed once
@@ -328,9 +329,7 @@ wpsgd_status wpsgd_delta_run(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const f
   if (lay.pack_k) packs.add(rows->q, rows->ld_q, rows->heads_k, rows->dk, p.q.p);
   if (lay.pack_k) packs.add(rows->k, rows->ld_k, rows->heads_k, rows->dk, p.k.p);
   if (lay.pack_v) packs.add(rows->v, rows->ld_v, rows->heads_v, rows->dv, p.v.p);
-  const wpsgd_status s = packs.launch_for(c, rows->n_rows);
-  if (s != WPSGD_OK) return s;
-  return lay.DK == 64 ? run_chunks<64>(c, p, lay, save) : run_chunks<128>(c, p, lay, save);
+  return lay.DK == 64 ? run_chunks<64>(c, p, lay, save, packs) : run_chunks<128>(c, p, lay, save, packs);
 }
 
 wpsgd_status wpsgd_delta_grad(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const void* saved, int64_t saved_bytes, const void* dout, int64_t ld_dout, const float* dW, void* dq, void* dk,
@@ -368,8 +367,7 @@ wpsgd_status wpsgd_delta_grad(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const 
                         : DeltaHeads{(const __nv_bfloat16*)dout, ld_dout, rows->heads_v, rows->dv};
   Packs packs;
   if (own.pack_o) packs.add(dout, ld_dout, rows->heads_v, rows->dv, p.f.dout.p);
-  const wpsgd_status s = packs.launch_for(c, n);
-  if (s != WPSGD_OK) return s;
+  if (const wpsgd_status s = packs.launch_for(c, p.f)) return s;
   return lay.DK == 64 ? grad_chunks<64>(c, p, lay, rows_blocks(rows, lay)) : grad_chunks<128>(c, p, lay, rows_blocks(rows, lay));
 }
 

@@ -161,3 +161,44 @@ def test_chains_that_are_left_out_keep_their_models(P, dtype, start):
                 o, want[good:good + 1] = c.delta_run(*[x[part] for x in rows], torch.tensor([0, off[good + 1] - off[good]]).cuda(), W0=None if W0 is None else W0[good:good + 1])
                 assert torch.equal(out[part], o)
             assert torch.equal(W, want) and bool((out[~answered] == 7).all())
+
+
+class DeltaRows(ctypes.Structure):
+    """wpsgd_delta_rows"""
+
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k", "v", "g", "beta")] + [(n, ctypes.c_int64) for n in ("ld_q", "ld_k", "ld_v", "ld_g", "ld_beta")]
+                + [("shard_off", ctypes.c_void_p), ("n_rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("n_chains", "heads_k", "heads_v", "dk", "dv")]
+                + [("type", ctypes.c_int), ("scale", ctypes.c_float)])
+
+
+def c_rows(rows, off, n_chains=None):
+    q, k, v, g, beta = rows
+    assert all(x.is_contiguous() for x in rows)
+    return DeltaRows(*[x.data_ptr() for x in rows], *[x[0].numel() for x in rows], None if off is None else off.data_ptr(), len(q), len(off) - 1 if n_chains is None else n_chains, q.shape[1],
+                     v.shape[1], q.shape[2], v.shape[2], int(q.dtype is torch.bfloat16), 0.5)
+
+
+@pytest.mark.parametrize("first,end", [(70, 131), (0, 64), (200, 200)])
+def test_rows_outside_every_chain_are_not_read(P, ctx, first, end):
+    """Heads that are laid out anew: the workspaces hold the same, to the byte, whatever stands in rows outside the chains."""
+    lib, n = P.load_library(), 200
+    off = torch.tensor([first, first, end]).cuda()
+    kept = []
+    for other in (1.0, -2.0):
+        rows = chain_rows(n, 2, 2, 60, 33, torch.bfloat16)
+        dout = torch.randn((n, 2, 33), generator=gen(9)).to(torch.bfloat16).cuda()
+        for x in rows + [dout]:
+            x[:first] = other
+            x[end:] = other
+        r, size = c_rows(rows, off), ctypes.c_int64()
+        spaces, outs = [], [torch.full_like(dout, 3.0)] + [torch.zeros_like(x) for x in rows]
+        for use in (1, 2):
+            assert lib.wpsgd_delta_workspace(ctypes.byref(r), use, ctypes.byref(size)) == 0
+            spaces.append(torch.full((size.value,), 0x5A, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        assert lib.wpsgd_delta_run(ctx._h, ctypes.byref(r), None, None, outs[0].data_ptr(), 66, 1, spaces[0].data_ptr(), spaces[0].numel()) == 0
+        assert lib.wpsgd_delta_grad(ctx._h, ctypes.byref(r), spaces[0].data_ptr(), spaces[0].numel(), dout.data_ptr(), 66, None, *[x.data_ptr() for x in outs[1:]], None, spaces[1].data_ptr(),
+                                    spaces[1].numel()) == 0
+        ctx.check()
+        kept.append(spaces + outs)
+    assert all(torch.equal(a, b) for a, b in zip(*kept))
