@@ -373,6 +373,13 @@ wpsgd_status wpsgd_delta_grad(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const 
 
 wpsgd_status wpsgd_delta_step(wpsgd_ctx* c, const wpsgd_delta_rows* rows, float* W, const int32_t* slots, int64_t n_slots, void* out, int64_t ld_out) {
   if (!c) return fail(nullptr, WPSGD_ERR_INVALID_ARG, "ctx is NULL");
+  wpsgd_delta_rows single;
+  if (rows) {  // chains are not looked at: whatever stands there is not a reason to refuse
+    single = *rows;
+    single.n_chains = 0;
+    single.shard_off = nullptr;
+    rows = &single;
+  }
   if (const char* why = check_shape(rows)) return refuse(c, "delta_step", why);
   if (const char* why = check_limits(rows)) return refuse(c, "delta_step", why, WPSGD_ERR_UNSUPPORTED);
   if (const char* why = check_delta_rows(rows, false)) return refuse(c, "delta_step", why);

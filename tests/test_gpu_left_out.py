@@ -202,3 +202,16 @@ def test_rows_outside_every_chain_are_not_read(P, ctx, first, end):
         ctx.check()
         kept.append(spaces + outs)
     assert all(torch.equal(a, b) for a, b in zip(*kept))
+
+
+def test_a_step_does_not_look_at_the_number_of_chains(P, ctx):
+    lib = P.load_library()
+    rows = chain_rows(6, 1, 2, 16, 8, torch.float32)
+    W = torch.zeros((6, 2, 8, 16), device="cuda")
+    want = ctx.delta_step(*rows, W.clone(), scale=0.5)
+    for n_chains in (-1, 1 << 30, 0):
+        r, out, mine = c_rows(rows, None, n_chains), torch.zeros_like(want), W.clone()
+        torch.cuda.synchronize()
+        assert lib.wpsgd_delta_step(ctx._h, ctypes.byref(r), mine.data_ptr(), None, 6, out.data_ptr(), 16) == 0
+        ctx.check()
+        assert torch.equal(out, want)
