@@ -380,7 +380,8 @@ wpsgd_status wpsgd_delta_grad(wpsgd_ctx* ctx, const wpsgd_delta_rows* rows, cons
 /* One row for each of n_rows chains, on models that stay where they are: the form for serving. shard_off and n_chains are not used.
  *   W          DEVICE [n_slots, heads_v, dv, dk] fp32, updated in place.
  *   slots      DEVICE [n_rows] int32: the models of each row; negative: the row is padding, its answer stays as it is. NULL: row i has models i. A slot
- *              past the end, or one that an earlier row has, counts as negative and is reported by the next wpsgd_check (WPSGD_ERR_CUDA).
+ *              past the end, or one that an earlier row has, counts as negative and is reported by the next wpsgd_check (WPSGD_ERR_CUDA). At most
+ *              4194304 rows by slots (WPSGD_ERR_UNSUPPORTED).
  *   out        DEVICE [n_rows, heads_v, dv], rows ld_out apart. */
 wpsgd_status wpsgd_delta_step(wpsgd_ctx* ctx, const wpsgd_delta_rows* rows, float* W, const int32_t* slots, int64_t n_slots, void* out, int64_t ld_out);
 

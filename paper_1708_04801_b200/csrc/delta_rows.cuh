@@ -284,10 +284,12 @@ __global__ void __launch_bounds__(32 * DELTA_WARPS) delta_rows_kernel(const __gr
 }
 
 // ---- one row for each of many chains ------------------------------------------------------------------------------------------------
-// A block has 32 models of a chain; they and what the row brings are on their way from memory together. Bounds: bytes, the models once in and once out. (Four models for each
+// A block has 32 models of a row at a time; they and what the row brings are on their way from memory together. Bounds: bytes, the models once in and once
+// out (85 % of the copy rate for heads of 128 x 128; 131072 rows of one head of 16 x 16: 13 %, a block each of which half has no model). (Four models for each
 // group of eight lanes, 128 a block: 266 us instead of 178 for 256 rows of 32 heads of 128 x 128; two: 191.)
-// A slot that an earlier row has is left to that row: every block looks through the slots before its own, which come from L2 while its models come from memory.
-constexpr int STEP_THREADS = 256;
+// A slot that an earlier row has is left to that row. With few rows every block looks through the slots before its own, which come from L2 while its models come from memory; that is
+// n^2 / 2 slots for each 32 models. With more, a block has a run of rows, and looks through the slots before them once for all: they are kept in a hash table in shared memory.
+constexpr int STEP_THREADS = 256, STEP_RUN = 2048;  // rows of a run at most; the table has twice as many places and more
 
 template <typename XT, int NJ>
 __global__ void __launch_bounds__(STEP_THREADS) delta_step_kernel(const __grid_constant__ DeltaRowsParams p) {
@@ -324,6 +326,89 @@ __global__ void __launch_bounds__(STEP_THREADS) delta_step_kernel(const __grid_c
     if (s == 0) ((XT*)p.out)[row * p.ld_out + R] = narrow_scalar<XT>(p.scale * o);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) put_model4(model, 4 * (s + 8 * j), p.dk, p.vec, w + 4 * j);
+  }
+}
+
+// Many rows with slots: a block has `run` of them, one behind the other. table: 2^lg slots (twice `run` at least), -1 where there is none; first: the first row of
+// the run that has the slot, -1 where an earlier run has it.
+template <typename XT, int NJ>
+__global__ void __launch_bounds__(STEP_THREADS) delta_step_runs_kernel(const __grid_constant__ DeltaRowsParams p, int run, int lg) {
+  const int places = 1 << lg;
+  extern __shared__ int step_smem[];
+  int *table = step_smem, *first = table + places, *slots = first + places;  // slots: [run]
+  const int tid = threadIdx.x, models = p.hv * p.dv, groups = (models + 31) / 32;
+  const long long row0 = (long long)blockIdx.x * run;
+  const int n = (int)min((long long)run, p.n_rows - row0);
+  kernel_started();
+  for (int i = tid; i < places; i += STEP_THREADS) table[i] = -1, first[i] = run;
+  kernel_inputs_ready();
+  __syncthreads();
+  auto place = [&](int slot) { return (int)((unsigned)slot * 2654435769u >> (32 - lg)); };  // the high bits: slots that lie equally far apart spread too
+  for (int i = tid; i < n; i += STEP_THREADS) {
+    const int slot = p.slots[row0 + i];
+    slots[i] = slot;
+    if (slot < 0 || slot >= p.n_slots) continue;
+    int at = place(slot);
+    for (;; at = (at + 1) & (places - 1)) {  // ends: half of the places stay empty
+      const int there = atomicCAS(table + at, -1, slot);
+      if (there == -1 || there == slot) break;
+    }
+    atomicMin(first + at, i);
+  }
+  __syncthreads();
+  auto look = [&](int slot) {  // of an earlier run
+    for (int at = place(slot); table[at] != -1; at = (at + 1) & (places - 1))
+      if (table[at] == slot) {
+        first[at] = -1;
+        break;
+      }
+  };
+  constexpr int AHEAD = 8;
+  for (long long r0 = tid; r0 < row0; r0 += STEP_THREADS * AHEAD) {
+    int slot[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) slot[a] = r0 + a * STEP_THREADS < row0 ? p.slots[r0 + a * STEP_THREADS] : -1;
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a)
+      if (slot[a] >= 0) look(slot[a]);
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += STEP_THREADS) {  // slots[i]: -1 from here on where the row has no models to step
+    const int slot = slots[i];
+    if (slot < 0) continue;
+    bool mine = slot < p.n_slots;
+    if (mine) {
+      int at = place(slot);
+      while (table[at] != slot) at = (at + 1) & (places - 1);
+      mine = first[at] == i;
+    }
+    if (!mine) {
+      set_status(p.status, DEV_BOUNDS, 23, row0 + i);
+      slots[i] = -1;
+    }
+  }
+  __syncthreads();
+  const int s = tid & 7;
+  for (int i = 0; i < n; ++i) {
+    if (slots[i] < 0) continue;
+    const long long row = row0 + i, model0 = (long long)slots[i] * models;
+    for (int R = tid >> 3; R < groups * 32; R += 32) {  // all lanes go round: they add up together
+      const bool there = R < models;
+      float w[4 * NJ] = {};
+      float* model = p.W + (model0 + (there ? R : 0)) * p.dk;
+      if (there)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) model4(model, 4 * (s + 8 * j), p.dk, p.vec, w + 4 * j);
+      const int h = there ? R / p.dv : 0, hk = h / (p.hv / p.hk);
+      DeltaRow<XT, NJ> brought;
+      brought.load((const XT*)p.k + row * p.ld_k + hk * p.dk, (const XT*)p.q + row * p.ld_q + hk * p.dk, (const XT*)p.v + row * p.ld_v + (there ? R : 0), (const XT*)p.g + row * p.ld_g + h,
+                   (const XT*)p.beta + row * p.ld_beta + h, s, p.dk, p.vec);
+      const float o = delta_one_row<XT, NJ>(w, brought);
+      if (!there) continue;
+      if (s == 0) ((XT*)p.out)[row * p.ld_out + R] = narrow_scalar<XT>(p.scale * o);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) put_model4(model, 4 * (s + 8 * j), p.dk, p.vec, w + 4 * j);
+    }
   }
 }
 

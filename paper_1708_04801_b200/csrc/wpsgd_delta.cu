@@ -69,13 +69,23 @@ wpsgd_status run_rows(wpsgd_ctx* c, const DeltaRowsParams& p) {
   return p.dk <= 32 ? go(std::integral_constant<int, 1>()) : p.dk <= 64 ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 4>());
 }
 
+// Rows by slots: from how many on a block has a run of them, so that the slots before it are looked through once and not in each block, and how many such blocks. By a block for each
+// row and by runs, us (bf16, 16 x 16; fp32, 4 heads of 32 x 32; bf16, 128 x 128): 8192 rows 37 and 43, 136 and 115, 211 and 186; 16384 85 and 80, 331 and 221, 469 and 367; 131072 2725 and
+// 529, 10640 and 1700. (Without slots 131072 rows take 313 and 1452; runs for 2, 4 or 8 blocks an SM: 760, 680 and 738 for 16 x 16.) Their time still has a part that grows with the square
+// of the rows, n^2 / 4096 slots of 4 bytes where runs are of 2048: the most rows keep it at a few ms.
+constexpr long long STEP_RUNS_FROM = 4096, STEP_BLOCKS = 148 * 6, STEP_MAX_ROWS = 1 << 22;
 template <typename XT>
 wpsgd_status run_step(wpsgd_ctx* c, const DeltaRowsParams& p) {
   const long long models = (long long)p.hv * p.dv, grid = p.n_rows * ((models + 31) / 32);
   if (grid > INT32_MAX) return fail(c, WPSGD_ERR_UNSUPPORTED, "delta_step: too many models");
+  const int step_runs = p.slots && p.n_rows > STEP_RUNS_FROM;
   auto go = [&](auto nj) {
     constexpr int NJ = decltype(nj)::value;
-    return launch(delta_step_kernel<XT, NJ>, (unsigned)grid, STEP_THREADS, 0, c->stream, p);
+    if (!step_runs) return launch(delta_step_kernel<XT, NJ>, (unsigned)grid, STEP_THREADS, 0, c->stream, p);
+    const int run = (int)std::min<long long>(STEP_RUN, (p.n_rows + STEP_BLOCKS - 1) / STEP_BLOCKS);
+    int lg = 6;
+    while (1 << lg < 2 * run) ++lg;
+    return launch(delta_step_runs_kernel<XT, NJ>, (unsigned)((p.n_rows + run - 1) / run), STEP_THREADS, ((size_t)(2 << lg) + run) * 4, c->stream, p, run, lg);
   };
   CU_TRY(c, p.dk <= 32 ? go(std::integral_constant<int, 1>()) : p.dk <= 64 ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 4>()));
   c->launches++;
@@ -387,6 +397,7 @@ wpsgd_status wpsgd_delta_step(wpsgd_ctx* c, const wpsgd_delta_rows* rows, float*
   if (ld_out < wv || ld_out > INT64_MAX / 8 / std::max<int64_t>(rows->n_rows, 1) || (rows->n_rows > 0 && (!out || !W)) || (uintptr_t)out % es || (uintptr_t)W % 4 || (uintptr_t)slots % 4)
     return refuse(c, "delta_step", "NULL or misaligned argument, or a stride below the width of a row");
   if (n_slots < 0 || n_slots > INT64_MAX / 8 / per_slot) return refuse(c, "delta_step", "negative number of slots, or models that pass 63 bits");
+  if (slots && rows->n_rows > STEP_MAX_ROWS) return refuse(c, "delta_step", "more than 4194304 rows by slots", WPSGD_ERR_UNSUPPORTED);
   if (!slots && n_slots < rows->n_rows) return refuse(c, "delta_step", "fewer models than rows, and no slots");
   const Region to = {out, wv * es, ld_out * es, rows->n_rows}, models = block_of(W, n_slots * per_slot), places = block_of(slots, rows->n_rows * 4);
   if (meets_rows(to, rows, false) || meets_rows(models, rows, false) || meet(to, models) || meet(to, places) || meet(models, places)) return refuse(c, "delta_step", "an output overlaps an input or another output");
