@@ -286,7 +286,8 @@ wpsgd_status wpsgd_clip_grad_norm(wpsgd_ctx* ctx, const wpsgd_grad_list* list, d
 
 /* ---- Rows that go to several nodes ---------------------------------------------------------------------------------------------
  * A row has `top` places, each with a node. wpsgd_sort_rows gives every place a position among the rows sorted by node, and the nodes'
- * shards; wpsgd_gather_rows lays the rows out in that order, as wpsgd_run and wpsgd_delta_run take them; wpsgd_combine_rows brings what the
+ * shards; wpsgd_gather_rows lays the rows out in that order, as wpsgd_delta_run takes them (and wpsgd_run, whose shard_off is on the host: copy it there once the stream has come so far;
+ * labels go through wpsgd_gather_rows as rows of one column); wpsgd_combine_rows brings what the
  * nodes give back to the rows' order, added up with a weight for each place. The gradient of gather is combine without weights, that of combine
  * is wpsgd_combine_rows_grad. The calls use the context's stream and device, allocate nothing and can be captured. Rows are fp32 or bf16, of
  * any width d, stride and alignment of their elements; rows that do not start on 16 bytes are read in whole aligned 16-byte units: up to 15 bytes
