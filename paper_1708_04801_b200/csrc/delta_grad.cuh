@@ -12,8 +12,9 @@
 //   dg_i = sum_{a >= i > b} H_ab + sum_{a >= i} (scale c_a O'_a S^T q_a - beta_a c_a dR_a S^T k_a) + sum_{b < i} r_b U_b G^T k_b + e^{b_C} S.G,
 // the first sum from the end of the chunk on by the row sums of H less its column sums: the same numbers on both sides, so that what does not pass row i cancels.
 //
-// Rounding: G, P, dU, scale c O' and beta c dR in two bf16 parts in the walk's products; S, U, G, dR, F and E are rounded to bf16
-// once where the third kernel multiplies them. Gradients leave as bf16: those of the labels are off by that rounding alone (1.7e-3 of their norm), the others by 2.5e-3 to 3e-3.
+// Rounding: G, P, dU, scale c O' and beta c dR in two bf16 parts in the walk's products; S, U, G, dR, F, E and beta E are rounded to bf16 once where the third kernel multiplies them, and
+// D o K K^T (which dg and dbeta take, by A) as it is kept: second parts would cost the third kernel, whose time goes with what it brings, a fifth more memory and twice the products. Gradients
+// leave as bf16: those of the labels are off by that rounding alone (1.7e-3 of their norm), the others by 2.4e-3 to 3e-3.
 //
 // Bounds, 32768 rows in 16 chains, 8 heads of features and 16 of labels, 128 x 128: the walk 436 us, by mma.sync as the forward one of few labels; the third kernel
 // 620 us, of which its copies alone would take 220 and the tensor pipe is active for 200: the steps between the products (F and E, sums, the way out) wait for each

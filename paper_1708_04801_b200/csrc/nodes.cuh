@@ -9,13 +9,12 @@
 namespace wpsgd {
 
 // ---- sorting ---------------------------------------------------------------------------------------------------------------
-// A stable counting sort in one launch: a cluster of blocks, each warp with a run of places and a counter per node in shared
-// memory. Count; add up over warps, blocks and nodes; go over the places again and hand the positions out. Lanes with the same node
-// find each other with one match instruction, so no counter is reached twice at a time and positions do not depend on timing.
+// A stable counting sort, by one of two forms. Up to 32767 places, without `order`, or with more nodes than many blocks' counts fit: one launch, a cluster of up to 8 blocks, each warp with a run
+// of places and a counter per node in shared memory. Count; add up over warps, blocks (through distributed shared memory, about 2 us) and nodes; go over the places again and hand the positions out.
+// More places: the same over up to 148 blocks in four launches (count, scan, place, order), whose latencies are less than what 8 blocks need for so many (131072 places on 128 nodes: 30 us by the
+// cluster, 17 by four launches). Lanes with the same node find each other with one match instruction, so no counter is reached twice at a time and positions do not depend on timing.
 //
-// Bounds: latency. The places are read twice and the positions written once (1.5 MB for 131072 places), by at most 8 blocks: a
-// cluster's blocks exchange their counts through distributed shared memory in about 2 us, where a second launch and a grid-wide scan
-// would take as long each.
+// Bounds: latency. The places are read twice and the positions written once (1.5 MB for 131072 places).
 constexpr int SORT_THREADS = 1024;
 constexpr int SORT_COUNTERS = 32768;      // of all warps of a block
 constexpr int SORT_MAX_NODES = 16384;     // counters of two warps, and a total per node beside them
@@ -380,7 +379,8 @@ __global__ void __launch_bounds__(NODES_THREADS) gather_rows_kernel(const __grid
 }
 
 // out[i] = sum_j weights[i, j] sorted[where[i, j]], j ascending, in fp32. Places without a position are left out, whatever their weight.
-// Four units are under way at a time, of PLACES places each (rows of more places have them found anew for each unit). Bounds: bytes.
+// Units under way at a time, of PLACES places each: four where a row has one place, two where it has more, one where rows start off 16 bytes, each read as two aligned ones (rows of more than
+// PLACES places have them found anew for each unit). Bounds: bytes.
 template <typename XT, bool ALIGNED, int PLACES>
 __global__ void __launch_bounds__(NODES_THREADS, 4) combine_rows_kernel(const __grid_constant__ NodesParams p) {
   constexpr int V = XVec<XT>::V, UNITS = !ALIGNED ? 1 : PLACES == 1 ? 4 : 2;

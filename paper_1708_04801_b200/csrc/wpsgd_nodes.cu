@@ -82,7 +82,7 @@ wpsgd_status wpsgd_sort_rows(wpsgd_ctx* c, const int32_t* node, int64_t n_rows, 
     c->launches += 4;
     return WPSGD_OK;
   }
-  // blocks: a run of 128 places for each warp before another block is worth its exchange (131072 places: 8 blocks)
+  // blocks: a run of 128 places for each warp before another block is worth its exchange
   const unsigned blocks = places <= 4096 ? 1 : places <= 8192 ? 2 : places <= 16384 ? 4 : 8;
   p.warps = (int)std::max(1ll, std::min<long long>({32ll, (long long)SORT_COUNTERS / n_nodes, (places + 32 * blocks - 1) / (32 * blocks)}));
   p.run = ((places + (long long)blocks * p.warps - 1) / ((long long)blocks * p.warps) + 31) / 32 * 32;
