@@ -319,7 +319,9 @@ wpsgd_status wpsgd_delta_run(wpsgd_ctx* c, const wpsgd_delta_rows* rows, const f
   if (save && rows->type != WPSGD_X_BF16) return refuse(c, "delta_run", "gradients are of bf16 rows", WPSGD_ERR_UNSUPPORTED);
   DeviceGuard guard(c->device);
   if (rows->n_chains == 0) {  // all rows are outside
-    if (new_out && rows->n_rows > 0) CU_TRY(c, cudaMemset2DAsync(out, (rows->n_rows > 1 ? ld_out : wv) * es, 0, wv * es, rows->n_rows, c->stream));
+    const bool whole = ld_out * es <= INT32_MAX;  // rows further apart than a copy of rows can be are cleared one by one
+    if (new_out && rows->n_rows > 0 && whole) CU_TRY(c, cudaMemset2DAsync(out, ld_out * es, 0, wv * es, rows->n_rows, c->stream));
+    for (int64_t i = 0; new_out && !whole && i < rows->n_rows; ++i) CU_TRY(c, cudaMemsetAsync((char*)out + i * ld_out * es, 0, wv * es, c->stream));
     return WPSGD_OK;
   }
   if (rows->type == WPSGD_X_F32) {

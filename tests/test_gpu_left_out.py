@@ -215,3 +215,25 @@ def test_a_step_does_not_look_at_the_number_of_chains(P, ctx):
         assert lib.wpsgd_delta_step(ctx._h, ctypes.byref(r), mine.data_ptr(), None, 6, out.data_ptr(), 16) == 0
         ctx.check()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lengths,first,behind,hk,hv,dk,dv", LEFT)
+@pytest.mark.parametrize("pad,by", [(0, 1), (5, 0), (8, 8)])
+def test_new_answers_in_rows_further_apart(P, ctx, lengths, first, behind, hk, hv, dk, dv, pad, by, dtype):
+    """WPSGD_DELTA_NEW_OUT on rows with a stride that start anywhere: zeros outside the chains, and what lies between the rows is as it was."""
+    lib, n, width = P.load_library(), first + sum(lengths) + behind, hv * dv
+    rows = chain_rows(n, hk, hv, dk, dv, dtype)
+    off = torch.tensor([first] + lengths).cumsum(0).cuda()
+    want = ctx.delta_run(*rows, off, scale=0.5)[0].flatten(1)
+    r, size = c_rows(rows, off), ctypes.c_int64()
+    assert lib.wpsgd_delta_workspace(ctypes.byref(r), 0, ctypes.byref(size)) == 0
+    space = torch.zeros(size.value + 16, dtype=torch.uint8, device="cuda")
+    flat = torch.full((by + n * (width + pad) + 8,), 7.0, dtype=dtype, device="cuda")
+    out = flat[by:by + n * (width + pad)].view(n, width + pad)
+    torch.cuda.synchronize()
+    assert lib.wpsgd_delta_run(ctx._h, ctypes.byref(r), None, None, out.data_ptr(), width + pad, 4, space.data_ptr(), size.value) == 0
+    ctx.check()
+    assert torch.equal(out[:, :width], want) and bool((out[:, width:] == 7).all()) and bool((flat[:by] == 7).all()) and bool((flat[by + n * (width + pad):] == 7).all())
+    for use in (2, 3, 6, 8, -1):
+        assert lib.wpsgd_delta_run(ctx._h, ctypes.byref(r), None, None, out.data_ptr(), width + pad, use, space.data_ptr(), size.value) == 1
