@@ -572,7 +572,8 @@ class Context:
 
     def delta_step(self, q, k, v, g, beta, W, slots=None, scale: Optional[float] = None, out=None):
         """One row for each of n chains on models W [n_slots, heads_v, dv, dk] (fp32, updated in place); slots [n] int32 says whose models each
-        row has (negative: none; None: row i has models i). Returns the answers [n, heads_v, dv]."""
+        row has (negative: none; None: row i has models i). Returns the answers [n, heads_v, dv]; that of a row without models is not written, in a new out
+        neither."""
         r = self._rows.delta_step(*self._head, q, k, v, g, beta, scale, W, slots, out)
         return r if r.__class__ is not int else self._ck(r, "wpsgd_delta_step")
 

@@ -237,3 +237,34 @@ def test_new_answers_in_rows_further_apart(P, ctx, lengths, first, behind, hk, h
     assert torch.equal(out[:, :width], want) and bool((out[:, width:] == 7).all()) and bool((flat[:by] == 7).all()) and bool((flat[by + n * (width + pad):] == 7).all())
     for use in (2, 3, 6, 8, -1):
         assert lib.wpsgd_delta_run(ctx._h, ctypes.byref(r), None, None, out.data_ptr(), width + pad, use, space.data_ptr(), size.value) == 1
+
+
+@pytest.mark.parametrize("n,d", [(200, 64), (3000, 2000)])
+def test_replayed_with_other_places(P, d, n):
+    """A graph's own tensors, few bytes and many: rows that lose their place between replays are zeros again."""
+    top, k = 2, 7
+    s = torch.cuda.Stream()
+    x, w = torch.randn((n, d), generator=gen(1)).cuda(), torch.rand((n, top), generator=gen(2)).cuda()
+    nodes = []
+    for seed, dropped in ((3, 0.0), (4, 0.6), (5, 0.2)):
+        node = torch.randint(0, k, (n, top), generator=gen(seed), dtype=torch.int32)
+        node[torch.rand((n, top), generator=gen(seed + 10)) < dropped] = -1
+        nodes.append(node.cuda())
+    at = nodes[0].clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s), P.Context(k, d, stream=s) as c:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            where, _, off = c.sort_rows(at)
+            rows = c.gather_rows(x, where)
+            dy, dw = c.combine_rows_grad(x, rows, where, w)
+        for node in nodes:
+            at.copy_(node)
+            graph.replay()
+            want_where, _, want_off = c.sort_rows(node)
+            want = c.gather_rows(x, want_where, torch.zeros_like(rows))
+            want_dy, want_dw = c.combine_rows_grad(x, want, want_where, w, torch.zeros_like(rows))
+            s.synchronize()
+            assert torch.equal(where, want_where) and torch.equal(rows, want) and torch.equal(dy, want_dy) and torch.equal(dw, want_dw)
+        c.check()
+        graph.reset()
